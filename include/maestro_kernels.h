@@ -85,6 +85,23 @@ ms_status ms_k_rope_table(int32_t max_pos, int32_t head_dim, float base, float *
 ms_status ms_k_rope(int32_t dtype, int32_t n, int32_t n_heads, int32_t head_dim, int64_t row_stride,
                     void *x, const int32_t *pos, const float *table, int32_t inverse, void *stream);
 
+/* RMSNorm of every query and key head and its rotation, in one pass over packed rows of [Q heads | K heads | V heads]:
+ *   y = R(pos) (x (mean over the head of x^2 + eps)^-1/2 g),   g = g_q[head_dim] or g_k[head_dim] of `dtype`, shared by the heads of a kind,
+ * with R and table[max_pos, head_dim / 2] as in ms_k_rope; a position outside [0, max_pos) does not rotate.  Rounded once.
+ * x_stride / y_stride: elements between rows.  y == x (same stride): in place, V heads are left alone; otherwise y must not overlap
+ * x and receives the V heads too.  head_dim: a multiple of 16, at most 512; 16-byte aligned rows, gains and table. */
+ms_status ms_k_qk_norm_rope_forward(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float eps,
+                                    const void *x, int64_t x_stride, const void *g_q, const void *g_k, const int32_t *pos,
+                                    const float *table, int32_t max_pos, void *y, int64_t y_stride, void *stream);
+/* Its gradients from dy, with x the forward call's input: dx for the query and key heads, dg_q / dg_k fp32 [head_dim], accumulated
+ * (they may be the same row).  dx == dy (same stride): in place, the V heads' gradients are left alone; otherwise dx must not overlap dy
+ * and receives them too.  dx must not overlap x.  No atomics: the same call gives the same bits. */
+size_t ms_k_qk_norm_rope_backward_scratch_bytes(int32_t head_dim);
+ms_status ms_k_qk_norm_rope_backward(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float eps,
+                                     const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *g_q,
+                                     const void *g_k, const int32_t *pos, const float *table, int32_t max_pos, void *dx,
+                                     int64_t dx_stride, float *dg_q, float *dg_k, void *scratch, void *stream);
+
 /* kind 0 SwiGLU: up[n, 2f] = [gate | up] -> a[n, f] = silu(gate) * up.
  * kind 1 GELU (erf): up[n, f] -> a[n, f]. */
 ms_status ms_k_act_forward(int32_t kind, int32_t dtype, int32_t n, int32_t f, const void *up, void *a,
@@ -99,6 +116,16 @@ ms_status ms_k_embedding_forward(int32_t dtype, int32_t out_fp32, int32_t n, int
 /* d_table[ids[t], :] += dx[t, :]  (fp32, atomic). */
 ms_status ms_k_embedding_backward(int32_t dtype, int32_t n, int32_t d, int32_t vocab, const int32_t *ids,
                                   const void *dx, float *d_table, void *stream);
+
+/* x[t, :] = scale * table[ids[t], :], the product in fp32, rounded once; ids outside the table embed as zeros. */
+ms_status ms_k_embedding_scaled_forward(int32_t dtype, int32_t out_fp32, int32_t n, int32_t d, int32_t vocab, float scale,
+                                        const int32_t *ids, const void *table, void *x, void *stream);
+/* d_table[v, :] += scale * sum over the tokens t with ids[t] == v of dx[t, :]  (fp32), the tokens sorted by id: every row's sum has
+ * one order, so the same call gives the same bits (ms_k_embedding_backward adds with atomics).  Ids outside the table receive no
+ * gradient.  At most 2^24 tokens.  scratch: 16-byte aligned, ..._scratch_bytes(n, d, vocab); contents are not kept. */
+size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_t d, int32_t vocab);
+ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, int32_t d, int32_t vocab, float scale, const int32_t *ids,
+                                         const void *dx, float *d_table, void *scratch, size_t scratch_bytes, void *stream);
 
 /* out[j] += sum_t x[t, j]  (fp32 [c], accumulated).  scratch as for the norm backward with d = c. */
 ms_status ms_k_colsum(int32_t dtype, int32_t n, int32_t c, const void *x, float *out, void *scratch,

@@ -406,6 +406,130 @@ def k_embedding_backward(ids, dx, vocab, d_table=None):
     return d_table
 
 
+# The entry points below take device tensors of one device and check them here; outputs and scratch that are not given are allocated
+# per call, so calls on several streams, devices or captured graphs share nothing.
+def _args(*types):
+    kinds = {"i": C.c_int32, "l": C.c_int64, "f": C.c_float, "p": C.c_void_p, "z": C.c_size_t}
+    return [kinds[k] for k in "".join(types)]
+
+
+_ARGTYPES = {
+    "ms_k_qk_norm_rope_forward": _args("iiiiif", "plpppp", "ipl", "p"),
+    "ms_k_qk_norm_rope_backward": _args("iiiiif", "plplpppp", "ipl", "pppp"),
+    "ms_k_embedding_scaled_forward": _args("iiiiif", "pppp"),
+    "ms_k_embedding_sorted_backward": _args("iiiif", "ppppzp"),
+}
+_SCRATCH = {
+    "ms_k_qk_norm_rope_backward_scratch_bytes": _args("i"),
+    "ms_k_embedding_sorted_backward_scratch_bytes": _args("iii"),
+}
+_fns = {}
+
+
+def _fn(name):
+    f = _fns.get(name)
+    if f is None:
+        f = getattr(lib(), name)
+        f.argtypes = _ARGTYPES.get(name) or _SCRATCH[name]
+        f.restype = C.c_size_t if name in _SCRATCH else C.c_int
+        _fns[name] = f
+    return f
+
+
+def _call(name, dev, *args):
+    """The library's entry point on the current stream of `dev`, which is made the current device for the call."""
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    if dev.index == torch.cuda.current_device():
+        _check(_fn(name)(*args, stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(_fn(name)(*args, stream))
+
+
+def _need(name, t, dtypes, shape, device, rows=False):
+    """t: a tensor of one of `dtypes` and of `shape` (None: any size) on `device` (None: any GPU), contiguous, or, with `rows`, a matrix
+    whose rows are."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise ValueError(f"{name}: expected a tensor of {' or '.join(str(d) for d in dtypes)}, got {getattr(t, 'dtype', type(t).__name__)}")
+    if t.dim() != len(shape) or any(s is not None and s != a for s, a in zip(shape, t.shape)):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name}: expected a tensor on {device or 'a GPU'}, got one on {t.device}")
+    if not (t.is_contiguous() or (rows and t.stride(1) == 1 and t.stride(0) >= t.shape[1])):
+        raise ValueError(f"{name}: expected {'rows with unit stride' if rows else 'a contiguous tensor'}, got strides {t.stride()}")
+
+
+def _ld(t):
+    """Elements between the rows of a matrix (a single row may carry any stride)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+_STORE = (torch.bfloat16, torch.float32)
+
+
+def _qkn_args(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, pos, table, what):
+    n, dev = x.shape[0], x.device
+    _need(what, x, _STORE, (None, (n_q_heads + 2 * n_kv_heads) * head_dim), None, rows=True)
+    _need("g_q", g_q, (x.dtype,), (head_dim,), dev)
+    _need("g_k", g_k, (x.dtype,), (head_dim,), dev)
+    _need("pos", pos, (torch.int32,), (n,), dev)
+    _need("table", table, (torch.float32,), (None, head_dim // 2, 2), dev)
+    return n, dev
+
+
+def k_qk_norm_rope_forward(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, eps, pos, table, out=None):
+    """RMSNorm (gains g_q / g_k) and rotation of the query and key heads of x [n, (n_q + 2 n_kv) head_dim]; V heads are copied.  out=x: in
+    place.  pos, table: k_positions, k_rope_table."""
+    n, dev = _qkn_args(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, pos, table, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    elif out is not x:
+        _need("out", out, (x.dtype,), x.shape, dev, rows=True)
+    _call("ms_k_qk_norm_rope_forward", dev, _dt(x.dtype), n, n_q_heads, n_kv_heads, head_dim, eps, x.data_ptr(), _ld(x), g_q.data_ptr(),
+          g_k.data_ptr(), pos.data_ptr(), table.data_ptr(), table.shape[0], out.data_ptr(), _ld(out))
+    return out
+
+
+def k_qk_norm_rope_backward(dy, x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, eps, pos, table, dg_q, dg_k, out=None):
+    """Returns dx (V heads: dy's); x is the forward call's input.  dg_q / dg_k (fp32) are accumulated in place.  out=dy: in place."""
+    n, dev = _qkn_args(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, pos, table, "x")
+    _need("dy", dy, (x.dtype,), x.shape, dev, rows=True)
+    _need("dg_q", dg_q, (torch.float32,), (head_dim,), dev)
+    _need("dg_k", dg_k, (torch.float32,), (head_dim,), dev)
+    if out is None:
+        out = torch.empty(dy.shape, dtype=dy.dtype, device=dev)
+    elif out is not dy:
+        _need("out", out, (x.dtype,), x.shape, dev, rows=True)
+    sc = torch.empty(_fn("ms_k_qk_norm_rope_backward_scratch_bytes")(head_dim), dtype=torch.uint8, device=dev)
+    _call("ms_k_qk_norm_rope_backward", dev, _dt(x.dtype), n, n_q_heads, n_kv_heads, head_dim, eps, dy.data_ptr(), _ld(dy), x.data_ptr(),
+          _ld(x), g_q.data_ptr(), g_k.data_ptr(), pos.data_ptr(), table.data_ptr(), table.shape[0], out.data_ptr(), _ld(out),
+          dg_q.data_ptr(), dg_k.data_ptr(), sc.data_ptr())
+    return out
+
+
+def k_embedding_scaled_forward(ids, table, scale, out_fp32=False):
+    """scale * table[ids]; ids outside the table give zeros."""
+    _need("table", table, _STORE, (None, None), None)
+    _need("ids", ids, (torch.int32,), (None,), table.device)
+    n, (vocab, d) = ids.shape[0], table.shape
+    x = torch.empty((n, d), dtype=torch.float32 if out_fp32 else table.dtype, device=table.device)
+    _call("ms_k_embedding_scaled_forward", table.device, _dt(table.dtype), int(out_fp32), n, d, vocab, scale, ids.data_ptr(), table.data_ptr(), x.data_ptr())
+    return x
+
+
+def k_embedding_sorted_backward(ids, dx, scale, d_table):
+    """d_table (fp32 [vocab, d], accumulated in place and returned) += scale * the sums of dx's rows by id, in token order."""
+    _need("dx", dx, _STORE, (None, None), None)
+    n, d = dx.shape
+    _need("ids", ids, (torch.int32,), (n,), dx.device)
+    _need("d_table", d_table, (torch.float32,), (None, d), dx.device)
+    vocab = d_table.shape[0]
+    sc = torch.empty(_fn("ms_k_embedding_sorted_backward_scratch_bytes")(n, d, vocab), dtype=torch.uint8, device=dx.device)
+    _call("ms_k_embedding_sorted_backward", dx.device, _dt(dx.dtype), n, d, vocab, scale, ids.data_ptr(), dx.data_ptr(), d_table.data_ptr(),
+          sc.data_ptr(), sc.numel())
+    return d_table
+
+
 def k_colsum(x, out=None):
     n, c = x.shape
     out = torch.zeros(c, dtype=torch.float32, device=x.device) if out is None else out
