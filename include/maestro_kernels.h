@@ -61,6 +61,37 @@ ms_status ms_k_swiglu_linear_backward(int32_t dtype, int32_t n, int32_t out, int
 ms_status ms_k_gemm_swiglu(int32_t M, int32_t F, int32_t K, const void *A, int64_t lda, const void *W, int64_t ldw,
                            void *act, int64_t ldact, void *gate_up, int64_t ldgu, void *stream);
 
+/* 8-bit operands of a frozen section: e4m3 codes (1 byte, at most 448) and one power of two for each block of 128 columns of a row
+ * (block_rows = 1: activations) or of 128 x 128 (block_rows = 128: weights), kept as its exponent byte: value = code * 2^(byte - 127),
+ * the least power that brings the block's largest finite magnitude to 448 or below; 1 for zeros.  Infinities and NaN become NaN codes.
+ * q [n, k], rows ldq apart; scales [n or ceil(n / 128)] rows lds apart (a multiple of 4, at least that of ceil(k / 128)), padding
+ * up to the next multiple of 4 is written as 127.  k % 16 == 0, 16-byte aligned rows of x and q. */
+ms_status ms_k_fp8_quantize(int32_t dtype, int32_t block_rows, int32_t n, int32_t k, const void *x, int64_t ldx, void *q, int64_t ldq,
+                            void *scales, int64_t lds, void *stream);
+/* The same (block_rows = 1) of RMSNorm(x[n, d]) g and of silu(gate) * up, gate_up [n, 2f] with rows ldgu apart: evaluated in fp32 and
+ * rounded only to the codes. */
+ms_status ms_k_norm_fp8(int32_t dtype, int32_t x_fp32, int32_t n, int32_t d, float eps, const void *x, const void *g, void *q, int64_t ldq,
+                        void *scales, int64_t lds, void *stream);
+ms_status ms_k_swiglu_fp8(int32_t dtype, int32_t n, int32_t f, const void *gate_up, int64_t ldgu, void *q, int64_t ldq, void *scales,
+                          int64_t lds, void *stream);
+/* C[M,N] = A[M,K] W[N,K]^T (+ residual) of such operands: A with scales sA [M, blocks], W with sW [ceil(N / 128), blocks].  c_fp32 = 0: C is
+ * bf16, 1: fp32, 2: fp32 with the matrix cores' 8-bit sums, as for bf16: eight consecutive k are summed on a grid 2^-13 of the largest of
+ * their products (1.5e-5 of the result on normal data) at twice the rate; 1 sums in fp32 throughout.  The residual [M,N] is bf16 or fp32
+ * and may be C.  Results for up to 64 rows differ from those of more rows in the order of the sums (K is split then).
+ * K % 16 == 0; any M, N. */
+ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W, int64_t ldw,
+                        const void *sW, int64_t ldsw, void *C, int64_t ldc, int32_t c_fp32, const void *residual, int64_t ldr,
+                        int32_t residual_fp32, void *stream);
+/* Kernel selection of these products, for measurements and tests, as ms_k_gemm_config: 0 = by shape; 256256, 128128, 128129, 64128, 64129
+ * or 64064 = that tile for any number of rows (fp32 sums have no 256256; SwiGLU has 256, 128 and 64 rows). */
+ms_status ms_k_gemm_fp8_config(int32_t tile);
+/* Gate/up projection with SwiGLU and the next operand's quantisation: codes and scales of silu(A Wg^T) * (A Wu^T), W [2F, K] = gate rows,
+ * then up rows; nothing in between is rounded.  F % 16 == 0.  scratch: ..._scratch_bytes(M, F, K) bytes (0: may be NULL), 16-byte aligned. */
+size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K);
+ms_status ms_k_gemm_fp8_swiglu(int32_t M, int32_t F, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W,
+                               int64_t ldw, const void *sW, int64_t ldsw, void *q, int64_t ldq, void *scales, int64_t lds,
+                               void *scratch, size_t scratch_bytes, void *stream);
+
 /* kind 0: RMSNorm y = x rstd g; kind 1: LayerNorm y = (x - mean) rstd g + b.
  * mean (kind 1 only) and rstd are fp32 [n] outputs kept for the backward pass.
  * x_fp32 != 0: x is fp32 although dtype is bf16 (g, b, y stay bf16). */

@@ -418,10 +418,16 @@ _ARGTYPES = {
     "ms_k_qk_norm_rope_backward": _args("iiiiif", "plplpppp", "ipl", "pppp"),
     "ms_k_embedding_scaled_forward": _args("iiiiif", "pppp"),
     "ms_k_embedding_sorted_backward": _args("iiiif", "ppppzp"),
+    "ms_k_fp8_quantize": _args("iiii", "plplplp"),
+    "ms_k_norm_fp8": _args("iiiif", "ppplplp"),
+    "ms_k_swiglu_fp8": _args("iii", "plplplp"),
+    "ms_k_gemm_fp8": _args("iii", "plplplpl", "plipli", "p"),
+    "ms_k_gemm_fp8_swiglu": _args("iii", "plplplpl", "plpl", "pzp"),
 }
 _SCRATCH = {
     "ms_k_qk_norm_rope_backward_scratch_bytes": _args("i"),
     "ms_k_embedding_sorted_backward_scratch_bytes": _args("iii"),
+    "ms_k_gemm_fp8_swiglu_scratch_bytes": _args("iii"),
 }
 _fns = {}
 
@@ -528,6 +534,87 @@ def k_embedding_sorted_backward(ids, dx, scale, d_table):
     _call("ms_k_embedding_sorted_backward", dx.device, _dt(dx.dtype), n, d, vocab, scale, ids.data_ptr(), dx.data_ptr(), d_table.data_ptr(),
           sc.data_ptr(), sc.numel())
     return d_table
+
+
+def _codes(n, k, scale_rows, device):
+    """Empty codes [n, k] and scale bytes (rows of whole words)."""
+    return (torch.empty((n, k), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((scale_rows, (k + 511) // 512 * 4), dtype=torch.uint8, device=device))
+
+
+def k_fp8_quantize(x, block_rows=1):
+    """(codes e4m3 [n, k], scale bytes): value = code * 2^(byte - 127), a byte per block of block_rows (1 or 128) x 128."""
+    _need("x", x, _STORE, (None, None), None, rows=True)
+    n, k = x.shape
+    q, s = _codes(n, k, n if block_rows == 1 else (n + 127) // 128, x.device)
+    _call("ms_k_fp8_quantize", x.device, _dt(x.dtype), block_rows, n, k, x.data_ptr(), _ld(x), q.data_ptr(), k, s.data_ptr(), s.shape[1])
+    return q, s
+
+
+def k_norm_fp8(x, g, eps):
+    """Codes and scale bytes of RMSNorm(x) g; x may be fp32 while g is bf16."""
+    _need("x", x, _STORE, (None, None), None)
+    n, d = x.shape
+    _need("g", g, (x.dtype, torch.bfloat16), (d,), x.device)
+    q, s = _codes(n, d, n, x.device)
+    _call("ms_k_norm_fp8", x.device, _dt(g.dtype), int(x.dtype == torch.float32), n, d, eps, x.data_ptr(), g.data_ptr(), q.data_ptr(), d,
+          s.data_ptr(), s.shape[1])
+    return q, s
+
+
+def k_swiglu_fp8(gate_up):
+    """Codes and scale bytes of silu(gate) * up, gate_up [n, 2 f]."""
+    _need("gate_up", gate_up, _STORE, (None, None), None, rows=True)
+    n, f = gate_up.shape[0], gate_up.shape[1] // 2
+    q, s = _codes(n, f, n, gate_up.device)
+    _call("ms_k_swiglu_fp8", gate_up.device, _dt(gate_up.dtype), n, f, gate_up.data_ptr(), _ld(gate_up), q.data_ptr(), f, s.data_ptr(), s.shape[1])
+    return q, s
+
+
+def _fp8_args(a, sa, w, sw):
+    _need("a", a, (torch.float8_e4m3fn,), (None, None), None, rows=True)
+    (m, k), dev = a.shape, a.device
+    words = (k + 511) // 512 * 4
+    _need("sa", sa, (torch.uint8,), (m, words), dev, rows=True)
+    _need("w", w, (torch.float8_e4m3fn,), (None, k), dev, rows=True)
+    _need("sw", sw, (torch.uint8,), ((w.shape[0] + 127) // 128, words), dev, rows=True)
+    return m, w.shape[0], k, a.data_ptr(), _ld(a), sa.data_ptr(), _ld(sa), w.data_ptr(), _ld(w), sw.data_ptr(), _ld(sw)
+
+
+def k_gemm_fp8(a, sa, w, sw, residual=None, c=None, c_fp32=None, fast_sums=False):
+    """a w^T (+ residual) of 8-bit operands as k_fp8_quantize makes them (a: block_rows=1, w: 128).  The result is bf16, or fp32 if c_fp32
+    (by default: if the residual is); c: a tensor to write to, which may be the residual.  fast_sums: an fp32 result from the 8-bit
+    matrix cores' sums, which a bf16 result always has."""
+    args = _fp8_args(a, sa, w, sw)
+    m, n, dev = args[0], args[1], a.device
+    if residual is not None:
+        _need("residual", residual, _STORE, (m, n), dev, rows=True)
+    if c is None:
+        f32 = residual is not None and residual.dtype == torch.float32 if c_fp32 is None else c_fp32
+        c = torch.empty((m, n), dtype=torch.float32 if f32 else torch.bfloat16, device=dev)
+    else:
+        _need("c", c, _STORE, (m, n), dev, rows=True)
+    _call("ms_k_gemm_fp8", dev, *args, c.data_ptr(), _ld(c), (2 if fast_sums else 1) if c.dtype == torch.float32 else 0, residual.data_ptr() if residual is not None else None,
+          _ld(residual) if residual is not None else 0, int(residual is not None and residual.dtype == torch.float32))
+    return c
+
+
+def k_gemm_fp8_config(tile=0):
+    """Tile of the 8-bit products (tests, measurements): 0 / 256256 / 128128 / 128129 / 64128 / 64129 / 64064."""
+    _check(lib().ms_k_gemm_fp8_config(int(tile)))
+
+
+def k_gemm_fp8_swiglu(a, sa, w, sw):
+    """Codes and scale bytes of silu(a wg^T) * (a wu^T), w [2 f, k] = gate rows, then up rows."""
+    args = _fp8_args(a, sa, w, sw)
+    m, f, k, dev = args[0], args[1] // 2, args[2], a.device
+    if args[1] % 2:
+        raise ValueError(f"w: expected gate rows and as many up rows, got {args[1]}")
+    q, s = _codes(m, f, m, dev)
+    nb = _fn("ms_k_gemm_fp8_swiglu_scratch_bytes")(m, f, k)
+    sc = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    _call("ms_k_gemm_fp8_swiglu", dev, m, f, *args[2:], q.data_ptr(), f, s.data_ptr(), s.shape[1], sc.data_ptr() if nb else None, nb)
+    return q, s
 
 
 def k_colsum(x, out=None):

@@ -1,0 +1,743 @@
+// Products in 8-bit floating point with a power-of-two scale for each block of 128 (fp8_quantize.h):
+//   C[m, n] (+ residual) = sum over blocks b of 2^(ea[m, b] + ew[n / 128, b]) sum_{k in b} a[m, k] w[n, k]
+// on v_mfma_scale_f32_16x16x128_f8f6f4, whose contraction is one block deep and which takes both exponents as operands: a block's scale costs
+// no vector instruction, and the sum stays in the fp32 accumulator.  (The instruction has a scale per 32; the four of a block are
+// the same byte.  With all of them equal, any permutation of a block's k that both operands share gives the same result.)
+//
+// The weights are the instruction's row operand, so that a lane ends up with four consecutive outputs n of one token m.  Weight
+// rows are dealt to a wave's NI fragment blocks so that those of all blocks join up: row r of block j is output 4 NI (r / 4) + 4 j + r % 4, and a
+// lane holds 4 NI consecutive outputs, which leave in 16-byte stores straight from the accumulators.
+// SwiGLU: half of the blocks are gate rows, the others the up rows of the same columns.
+//
+// Precision: the instruction sums eight consecutive k on a grid 2^-13 of the largest product's power of two and cuts off what lies below;
+// the sums of eight are added in fp32 (measured with single products: a second one 2^-14 of the first is lost among the same eight, not
+// among others).  On normal data that is 1.5e-5 of the result, a hundredth of the rounding to bf16, and results in bf16 and SwiGLU's codes
+// are computed so.  An fp32 result is computed on v_mfma_f32_16x16x32_bf16 instead, half the rate, from the codes widened to bf16 (exact): fp32
+// sums throughout; unless the caller asks for the fast ones.
+//
+//   * gemm_fp8_pp_kernel: 256 tokens x 256 outputs, operands through LDS, two wave groups that take turns;
+//   * gemm_fp8_ring_kernel: smaller tiles through LDS, for grids that do not fill the chip with the large one, and fp32 results;
+//   * gemm_fp8_direct_kernel: up to 64 tokens, fragments straight from global memory, K split over the waves of a workgroup.
+// All but the last add up K in ascending order, one accumulator per output, so they give the same bits.
+#include <atomic>
+#include <utility>
+
+#include "fp8_quantize.h"
+#include "launch.h"
+#include "launch_plan.h"
+#include "mfma_tiles.h"
+
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kBlk = 128;             // K tile = scale block, in codes = bytes
+constexpr int kPanel = 112, kSegment = 108;   // K tiles whose scales a workgroup has room for in LDS, and takes at a time
+
+struct Fp8Params {
+    const uint8_t *A, *sA, *W, *sW;
+    long lda, ldsa, ldw, ldsw;
+    void *C;
+    const void *R;
+    long ldc, ldr;
+    int c_fp32, r_fp32, vec;          // vec: 16-byte accesses to C and R
+    uint8_t *sC;                      // SwiGLU: scales of the codes in C
+    long ldsc;
+    int M, N, K, F;                   // N: weight rows; SwiGLU: N = 2 F
+    int kb, tiles_m, tiles_n;
+};
+
+__device__ __forceinline__ f32x4 mfma(const i32x8 &w, const i32x8 &a, const f32x4 &c, int sw, int sa, std::integral_constant<int, 0>) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
+}
+__device__ __forceinline__ f32x4 mfma(const i32x8 &w, const i32x8 &a, const f32x4 &c, int sw, int sa, std::integral_constant<int, 1>) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 1, sw, 1, sa);
+}
+// The same in fp32 sums: 8 k of each lane at a time
+__device__ __forceinline__ bf16x8 widen8(int a, int b, float scale) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    const bf16x2 u = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+    return bf16x8{p[0], p[1], q[0], q[1], u[0], u[1], v[0], v[1]};
+}
+__device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((unsigned)(byte & 255) << 23); }
+__device__ __forceinline__ i32x8 join(const i32x4 &lo, const i32x4 &hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + __expf(-g)) * u; }
+
+// NV consecutive outputs of a row
+template <int NV> __device__ __forceinline__ void store_row(const Fp8Params &p, int m, int n, float *v) {
+    if (m >= p.M || n >= p.N) return;
+    if (p.vec) {                                         // (N is a multiple of 16: all of them are there)
+        if (p.R) {
+            if (p.r_fp32) {
+                const float4 *r = (const float4 *)((const float *)p.R + m * p.ldr + n);
+#pragma unroll
+                for (int q = 0; q < NV / 4; ++q) {
+                    const float4 t = r[q];
+                    v[4 * q] += t.x; v[4 * q + 1] += t.y; v[4 * q + 2] += t.z; v[4 * q + 3] += t.w;
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < NV / 8; ++q) {
+                    const Vec16<bf16_t> t = ldv((const bf16_t *)p.R + m * p.ldr + n + 8 * q);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[8 * q + e] += to_f32(t.v[e]);
+                }
+            }
+        }
+        if (p.c_fp32) {
+            float4 *c = (float4 *)((float *)p.C + m * p.ldc + n);
+#pragma unroll
+            for (int q = 0; q < NV / 4; ++q) c[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < NV / 8; ++q) {
+                Vec16<bf16_t> t;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t.v[e] = from_f32<bf16_t>(v[8 * q + e]);
+                stv((bf16_t *)p.C + m * p.ldc + n + 8 * q, t);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < NV; ++e) {
+        if (n + e < p.N) {
+            float f = v[e];
+            if (p.R) f += p.r_fp32 ? ((const float *)p.R)[m * p.ldr + n + e] : to_f32(((const bf16_t *)p.R)[m * p.ldr + n + e]);
+            if (p.c_fp32) ((float *)p.C)[m * p.ldc + n + e] = f;
+            else ((bf16_t *)p.C)[m * p.ldc + n + e] = from_f32<bf16_t>(f);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ up to 64 tokens
+// 16 MB tokens x 16 NI weight rows per workgroup; wave w takes the K tiles w, w + 8, ...: together the waves read 1 KB pieces of the rows.
+// D tiles are requested before the first is used.  The weights stream from HBM and bound it; a token row is read again by every
+// workgroup, from L2.
+constexpr int kDirectWaves = 8;
+template <int MB, int NI, int D, bool PRECISE>
+__global__ __launch_bounds__(64 * kDirectWaves) void gemm_fp8_direct_kernel(Fp8Params p) {
+    constexpr int COLS = 16 * NI, LDR = COLS + 4;
+    __shared__ __align__(16) float red[kDirectWaves][16][LDR];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int m0 = blockIdx.y * 16 * MB;
+    const long n0 = (long)blockIdx.x * COLS;
+    const long rows_w = p.N - n0 < COLS ? p.N - n0 : COLS, rows_a = p.M - m0 < 16 * MB ? p.M - m0 : 16 * MB;
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.W + n0 * p.ldw, (rows_w - 1) * p.ldw + p.K);
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(p.A + (long)m0 * p.lda, (rows_a - 1) * p.lda + p.K);
+    const uint8_t *sw_row = p.sW + n0 / kBlk * p.ldsw;                   // (a tile lies within one block of 128 rows)
+    unsigned wo[NI], ao[MB];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const int row = 4 * NI * (r >> 2) + 4 * j + (r & 3);
+        wo[j] = row < rows_w ? (unsigned)(row * p.ldw + 32 * g) : kOob;
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i) ao[i] = 16 * i + r < rows_a ? (unsigned)((16 * i + r) * p.lda + 32 * g) : kOob;
+    f32x4 acc[MB][NI];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int kt = wave; kt < p.kb; kt += kDirectWaves * D) {
+        i32x4 w[D][NI][2], a[D][MB][2];
+        int sa[D][MB], sw[D];
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            const int t = kt + u * kDirectWaves;
+            const bool in = t < p.kb;
+            const int k0 = in ? t * kBlk : 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned inv = in && k0 + 32 * g + 16 * h < p.K ? 0u : kOob;      // (K is a multiple of 16)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) w[u][j][h] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(rw, (wo[j] + 16 * h) | inv, k0, 0);
+#pragma unroll
+                for (int i = 0; i < MB; ++i) a[u][i][h] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(ra, (ao[i] + 16 * h) | inv, k0, 0);
+            }
+            sw[u] = in ? sw_row[t] : 127;
+#pragma unroll
+            for (int i = 0; i < MB; ++i) sa[u][i] = in && 16 * i + r < rows_a ? p.sA[(long)(m0 + 16 * i + r) * p.ldsa + t] : 127;
+        }
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            if constexpr (PRECISE) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    bf16x8 x[MB];
+#pragma unroll
+                    for (int i = 0; i < MB; ++i) x[i] = widen8(a[u][i][q >> 1][2 * (q & 1)], a[u][i][q >> 1][2 * (q & 1) + 1], scale_of(sa[u][i]));
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) {
+                        const bf16x8 y = widen8(w[u][j][q >> 1][2 * (q & 1)], w[u][j][q >> 1][2 * (q & 1) + 1], scale_of(sw[u]));
+#pragma unroll
+                        for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x[i], acc[i][j], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        acc[i][j] = mfma(join(w[u][j][0], w[u][j][1]), join(a[u][i][0], a[u][i][1]), acc[i][j], sw[u], sa[u][i], std::integral_constant<int, 0>{});
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        if (i) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NI; ++j) *(f32x4 *)&red[wave][r][4 * NI * g + 4 * j] = acc[i][j];
+        __syncthreads();
+        for (int idx = tid; idx < 16 * COLS; idx += 64 * kDirectWaves) {
+            const int ml = idx / COLS, nl = idx % COLS;
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < kDirectWaves; ++w) s += red[w][ml][nl];
+            const long m = m0 + 16 * i + ml, n = n0 + nl;
+            if (m < p.M && n < p.N) {
+                if (p.R) s += p.r_fp32 ? ((const float *)p.R)[m * p.ldr + n] : to_f32(((const bf16_t *)p.R)[m * p.ldr + n]);
+                if (p.c_fp32) ((float *)p.C)[m * p.ldc + n] = s;
+                else ((bf16_t *)p.C)[m * p.ldc + n] = from_f32<bf16_t>(s);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ operands through LDS
+// An LDS tile row is the 128 codes of a block, eight 16-byte pieces in the swizzled order of mfma_tiles.h.  A fragment is the pieces g and
+// 4 + g of a row (g = lane / 16) for both operands.
+__device__ __forceinline__ int piece_off(int row, int piece) { return row * kBlk + (swz(row, piece) << 4); }
+
+// Byte offset of LDS row 8 lg + lr of a wave's NI weight blocks (lr = lane / 8, lg counts 8-row groups of the blocks): the lane's part and the group's
+template <int NI> __device__ __forceinline__ int weight_row_lane(int lr) { return 4 * NI * (lr >> 2) + (lr & 3); }
+template <int NI> __device__ __forceinline__ int weight_row_group(int lg) { return 8 * NI * (lg & 1) + 4 * (lg >> 1); }
+
+// Scales of a workgroup's BM tokens and BN / 128 weight blocks for up to kPanel K tiles from tile t0 on, as pairs of K tiles: one 16-bit word
+// per pair and row.  Tiles past the end get 1: their codes arrive as zeros, and a scale may not turn those into NaN.
+template <int BM, int NW, int THREADS>
+__device__ __forceinline__ void stage_scales(const Fp8Params &p, uint16_t *pa, uint16_t *pw, int m0, const int *wblk, int t0, int nt, int tid) {
+    const int words = (nt + 3) >> 2;                     // four K tiles each
+    for (int i = tid; i < words * (BM + NW); i += THREADS) {
+        const int row = i / words, q = i % words, t = t0 + 4 * q;
+        unsigned v = 0x7f7f7f7fu;
+        if (row < BM) {
+            if (m0 + row < p.M) v = *(const unsigned *)(p.sA + (long)(m0 + row) * p.ldsa + t);
+        } else {
+            v = *(const unsigned *)(p.sW + (long)wblk[row - BM] * p.ldsw + t);
+        }
+        const int left = p.kb - t;
+        if (left < 4) v = (v & ((1u << (8 * left)) - 1)) | (0x7f7f7f7fu << (8 * left));
+        uint16_t *d = row < BM ? pa + (2 * q) * BM + row : pw + (2 * q) * NW + row - BM;
+        d[0] = (uint16_t)v;
+        d[row < BM ? BM : NW] = (uint16_t)(v >> 16);
+    }
+}
+
+// Which tile a workgroup has: each XCD (every eighth workgroup) works on a contiguous range of tiles, ordered in groups of `gm` rows of
+// tiles x all columns, so that it shares operand panels in its L2
+__device__ __forceinline__ void tile_of(const Fp8Params &p, int gm, int bm, int bn, int *m0, int *n0) {
+    const int nb = gridDim.x, b = blockIdx.x, per = nb >> 3, rem = nb & 7, x = b & 7, q = b >> 3;
+    const int pid = x * per + (x < rem ? x : rem) + q, width = gm * p.tiles_n;
+    const int first = pid / width * gm, rows = p.tiles_m - first < gm ? p.tiles_m - first : gm;
+    *m0 = (first + pid % width % rows) * bm;
+    *n0 = pid % width / rows * bn;
+}
+
+// SwiGLU tile of 128 activation columns: accumulator blocks 0, 1 are gate, 2, 3 up of the lane's columns 32 wn + 8 g .. + 7; the tile's width is their
+// scale block, so its maximum needs the four wave columns' maxima (mx: LDS, [4][BM])
+template <int MI, int BM, class ROW>
+__device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 (&acc)[MI][4], unsigned *mx, int m0, int n0, int wn, int g, ROW row) {
+    float v[MI][8];
+    const int n = n0 + wn * 32 + 8 * g;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        unsigned m = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[i][4 * j + e] = silu_mul(acc[i][j][e], acc[i][2 + j][e]);
+                m = max(m, fp8_finite_bits(v[i][4 * j + e]));
+            }
+        m = max(m, (unsigned)__shfl_xor((int)m, 16, 64));
+        m = max(m, (unsigned)__shfl_xor((int)m, 32, 64));
+        if (g == 0) mx[wn * BM + row(i)] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int ml = row(i), m = m0 + ml;
+        const int byte = fp8_scale_byte(max(max(mx[ml], mx[BM + ml]), max(mx[2 * BM + ml], mx[3 * BM + ml])));
+        const float is = fp8_inverse_scale(byte);
+        if (m < p.M) {
+            *(uint2 *)((uint8_t *)p.C + (long)m * p.ldc + n) = make_uint2(fp8_pack4(v[i][0] * is, v[i][1] * is, v[i][2] * is, v[i][3] * is),
+                                                                          fp8_pack4(v[i][4] * is, v[i][5] * is, v[i][6] * is, v[i][7] * is));
+            if (wn == 0 && g == 0) {
+                const int b = n0 / kBlk, blocks = p.F / kBlk;
+                uint8_t *s = p.sC + (long)m * p.ldsc + b;
+                s[0] = (uint8_t)byte;
+                if (b + 1 == blocks)
+                    for (int q = blocks; q & 3; ++q) s[q - b] = 127;
+            }
+        }
+    }
+}
+
+// 256 x 256 tile, two wave groups that take turns on the matrix cores: the arrangement of gemm_bf16_pp_kernel (gemm.hip) with a K tile of
+// 128 codes in the same 128-byte LDS rows and one MFMA where that has two.  "A" is the token operand (two halves of 128 rows), "B" the
+// weights (half h = blocks 2 h and 2 h + 1 of every wave column; SwiGLU: gate and up).
+struct Fp8Lds { uint8_t *a[2][2], *b[2][2]; };
+template <bool SWIGLU, bool TAIL>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_fp8_pp_kernel(Fp8Params p) {
+    constexpr int HS = 128 * kBlk;
+    __shared__ __align__(16) uint8_t A00[HS], A01[HS], A10[HS], A11[HS], B00[HS], B01[HS], B10[HS], B11[HS];
+    __shared__ __align__(16) uint16_t pa[kPanel / 2 * 256], pw[kPanel / 2 * 2];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane >> 3;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 2, wn = wave & 3;
+    int m0, n0;
+    tile_of(p, 4, 256, SWIGLU ? 128 : 256, &m0, &n0);
+    const long rows_a = p.M - m0 < 256 ? p.M - m0 : 256, rows_b = SWIGLU ? p.N - n0 : (p.N - n0 < 256 ? p.N - n0 : 256);
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(p.A + (long)m0 * p.lda, (rows_a - 1) * p.lda + p.K);
+    const __amdgpu_buffer_rsrc_t rb = make_rsrc(p.W + (long)n0 * p.ldw, (rows_b - 1) * p.ldw + p.K);
+    const int x = (lane & 7) ^ swz_row(lr);
+    const unsigned alane = (unsigned)(lr * p.lda), blane = (unsigned)(weight_row_lane<SWIGLU ? 2 : 4>(lr) * p.ldw);
+    const unsigned lda = (unsigned)p.lda, ldw = (unsigned)p.ldw;
+    int kt0 = 0, nk = 0;                                 // first K tile of the panel and their number
+    auto invalid = [&](int kt, int piece) __attribute__((always_inline)) {
+        unsigned inv = kt < nk ? 0u : kOob;
+        if (TAIL) inv |= (kt0 + kt) * kBlk + piece * 16 < p.K ? 0u : kOob;
+        return inv;
+    };
+    auto fetch_a = [&](int kt, int h, uint8_t *slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int lg = wave * 2 + i, piece = x ^ swz_row(8 * lg);
+            const unsigned voff = (alane + (unsigned)(h * 128 + lg * 8) * lda + (piece << 4)) | invalid(kt, piece);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(slot + lg * 8 * kBlk), 16, voff, kt < nk ? (kt0 + kt) * kBlk : 0, 0, 0);
+        }
+    };
+    auto fetch_b = [&](int kt, int h, uint8_t *slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int lg = wave * 2 + i, piece = x ^ swz_row(8 * lg), w = lg >> 2;
+            const unsigned row = SWIGLU ? (unsigned)(h * p.F + w * 32 + weight_row_group<2>(lg & 3)) : (unsigned)(w * 64 + weight_row_group<4>((lg & 3) + 4 * h));
+            const unsigned voff = (blane + row * ldw + (piece << 4)) | invalid(kt, piece);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(slot + lg * 8 * kBlk), 16, voff, kt < nk ? (kt0 + kt) * kBlk : 0, 0, 0);
+        }
+    };
+
+    f32x4 acc[8][4];                                     // [16-token block: 4 half + b][weight block]
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x8 af[4], ax[2], bf[4];                           // blocks 1 .. 3 of the present A half (af[0] unused), block 0 of each; weights
+    int sa[8], sw = 0;
+    int fo[2][2];                                        // [block parity][piece g / 4 + g] within a 64-row (A) piece
+    const int r16 = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int par = 0; par < 2; ++par)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) fo[par][q] = piece_off(par * 16 + r16, q * 4 + g) - par * 16 * kBlk;
+    auto frag = [&](const uint8_t *slot, int row0, int blk) __attribute__((always_inline)) {
+        const uint8_t *s = slot + (row0 + blk * 16) * kBlk;
+        return join(*(const i32x4 *)(s + fo[blk & 1][0]), *(const i32x4 *)(s + fo[blk & 1][1]));
+    };
+    auto read_a_first = [&](auto half, const uint8_t *slot) __attribute__((always_inline)) { ax[decltype(half)::value] = frag(slot, wm * 64, 0); };
+    auto read_a_rest = [&](const uint8_t *slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 1; b < 4; ++b) af[b] = frag(slot, wm * 64, b);
+    };
+    auto read_b = [&](auto half, const uint8_t *slot) __attribute__((always_inline)) {
+        constexpr int h = decltype(half)::value;
+        bf[2 * h] = frag(slot, wn * 32, 0);
+        bf[2 * h + 1] = frag(slot, wn * 32, 1);
+    };
+    // scales of half h's tokens (and the weights') for the pair of K tiles from kt on
+    auto read_sa = [&](auto half, int kt) __attribute__((always_inline)) {
+        constexpr int h = decltype(half)::value;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) sa[4 * h + b] = pa[(kt >> 1) * 256 + h * 128 + wm * 64 + b * 16 + r16];
+    };
+    int sw_next = 0;
+    auto read_sw = [&](int kt) __attribute__((always_inline)) { sw_next = pw[(kt >> 1) * 2 + (SWIGLU ? 0 : wn >> 1)]; };
+    // (SwiGLU: gate and up rows have scales of their own; their second block lies F rows on)
+    int su = 0, su_next = 0;
+    auto turn = [&](auto ah, auto bh, auto op) __attribute__((always_inline)) {
+        constexpr int h = decltype(ah)::value, gg = decltype(bh)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        wait_vmcnt_lgkm0<10>();
+        lds_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                acc[4 * h + b][2 * gg + c] = mfma(bf[2 * gg + c], b == 0 ? ax[h] : af[b], acc[4 * h + b][2 * gg + c], SWIGLU && gg ? su : sw, sa[4 * h + b], op);
+        __builtin_amdgcn_sched_barrier(0);
+        lds_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    // K tile kt (parity = F = its first B half) in stage slots a0, a1, f, s; nb / na: the next tile's first halves
+    auto tile = [&](int kt, auto F, uint8_t *a0, uint8_t *a1, uint8_t *f, uint8_t *s, const uint8_t *nb, const uint8_t *na) __attribute__((always_inline)) {
+        constexpr int fh = decltype(F)::value;
+        using FH = std::integral_constant<int, fh>;
+        using SH = std::integral_constant<int, 1 - fh>;
+        read_a_rest(a0);
+        if (fh == 0) read_sa(I1{}, kt);
+        fetch_b(kt + 2, fh, f);
+        turn(I0{}, FH{}, FH{});
+        read_b(SH{}, s);
+        read_a_first(I1{}, a1);
+        fetch_a(kt + 2, 0, a0);
+        turn(I0{}, SH{}, FH{});
+        read_a_rest(a1);
+        if (fh == 1) read_sa(I0{}, kt + 1);              // (the panel has a pair more than the tiles need)
+        fetch_b(kt + 2, 1 - fh, s);
+        turn(I1{}, SH{}, FH{});
+        read_b(SH{}, nb);
+        read_a_first(I0{}, na);
+        if (fh == 1) {
+            read_sw(kt + 1);
+            if (SWIGLU) su_next = pw[((kt + 1) >> 1) * 2 + 1];
+        }
+        fetch_a(kt + 2, 1, a1);
+        turn(I1{}, FH{}, FH{});
+        if (fh == 1) { sw = sw_next; su = su_next; }
+    };
+    int wblk[2];
+    if (SWIGLU) { wblk[0] = n0 / kBlk; wblk[1] = (p.F + n0) / kBlk; }
+    else { wblk[0] = n0 / kBlk; wblk[1] = (n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk; }
+    for (; kt0 < p.kb; kt0 += kSegment) {
+        nk = p.kb - kt0 < kSegment ? p.kb - kt0 : kSegment;
+        fetch_b(0, 0, B00); fetch_a(0, 0, A00); fetch_b(0, 1, B01); fetch_a(0, 1, A01);
+        fetch_b(1, 1, B11); fetch_a(1, 0, A10); fetch_b(1, 0, B10); fetch_a(1, 1, A11);
+        stage_scales<256, 2, 512>(p, pa, pw, m0, wblk, kt0, nk, tid);
+        wait_vmcnt_lgkm0<0>();
+        lds_barrier();
+        read_b(I0{}, B00);
+        read_a_first(I0{}, A00);
+        read_sa(I0{}, 0);
+        sw = SWIGLU ? pw[0] : pw[wn >> 1];
+        su = pw[1];
+        wait_vmcnt_lgkm0<10>();
+        lds_barrier();
+        if (wm == 1) lds_barrier();
+        for (int kt = 0; kt < nk; kt += 2) {             // an odd count is rounded up with a tile of zeros
+            tile(kt, I0{}, A00, A01, B00, B01, B11, A10);
+            tile(kt + 1, I1{}, A10, A11, B11, B10, B00, A00);
+        }
+        if (wm == 0) lds_barrier();
+        dma_publish_barrier();                           // what is still in flight must land before LDS is used again
+    }
+    const int mrow = m0 + wm * 64 + r16;
+    if constexpr (!SWIGLU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][j][e];
+            store_row<16>(p, mrow + (i >> 2) * 128 + (i & 3) * 16, n0 + wn * 64 + 16 * g, v);
+        }
+    } else {
+        swiglu_epilogue<8, 256>(p, acc, (unsigned *)A00, m0, n0, wn, g, [&](int i) { return wm * 64 + (i >> 2) * 128 + (i & 3) * 16 + r16; });
+    }
+}
+
+// The tile template's LDS stages as objects of their own (mfma_tiles.h, FastLds in gemm.hip, on why)
+template <int BM, int BN, int WM, int WN, int NST, bool SWIGLU, bool PRECISE>
+__device__ __forceinline__ void fp8_ring_body(const Fp8Params &p) {
+    constexpr int NW = WM * WN, THREADS = 64 * NW, NI = BN / WN / 16, MI = BM / WM / 16, LA = BM / 8 / NW, LB = BN / 8 / NW;
+    constexpr int NB = BN > kBlk || SWIGLU ? 2 : 1;      // weight scale blocks of a tile
+    static_assert(NST == 2 || NST == 4, "the parity of a K tile is that of its stage");
+    static_assert(LA * 8 * NW == BM && LB * 8 * NW == BN && NI == 4 && (!SWIGLU || BN == 256), "tile and waves");
+    constexpr bool RING = NST == 4;
+    __shared__ __align__(16) uint8_t A0[BM * kBlk], A1[BM * kBlk], A2[RING ? BM * kBlk : 16], A3[RING ? BM * kBlk : 16];
+    __shared__ __align__(16) uint8_t B0[BN * kBlk], B1[BN * kBlk], B2[RING ? BN * kBlk : 16], B3[RING ? BN * kBlk : 16];
+    __shared__ __align__(16) uint16_t pa[kPanel / 2 * BM], pw[kPanel / 2 * NB];
+    uint8_t *const As[4] = {A0, A1, A2, A3}, *const Bs[4] = {B0, B1, B2, B3};
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane >> 3, r16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+    int m0, n0;
+    tile_of(p, 8, BM, SWIGLU ? BN / 2 : BN, &m0, &n0);
+    const long rows_a = p.M - m0 < BM ? p.M - m0 : BM, rows_b = SWIGLU ? p.N - n0 : (p.N - n0 < BN ? p.N - n0 : BN);
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(p.A + (long)m0 * p.lda, (rows_a - 1) * p.lda + p.K);
+    const __amdgpu_buffer_rsrc_t rb = make_rsrc(p.W + (long)n0 * p.ldw, (rows_b - 1) * p.ldw + p.K);
+    const int x = (lane & 7) ^ swz_row(lr);
+    const unsigned alane = (unsigned)(lr * p.lda), blane = (unsigned)(weight_row_lane<SWIGLU ? 2 : NI>(lr) * p.ldw);
+    const unsigned lda = (unsigned)p.lda, ldw = (unsigned)p.ldw;
+    int kt0 = 0, nk = 0;
+    auto fetch = [&](int kt, uint8_t *as, uint8_t *bs) __attribute__((always_inline)) {
+        const int soff = kt < nk ? (kt0 + kt) * kBlk : 0;
+        auto invalid = [&](int piece) { return kt < nk && (kt0 + kt) * kBlk + piece * 16 < p.K ? 0u : kOob; };
+#pragma unroll
+        for (int i = 0; i < LA; ++i) {
+            const int lg = wave * LA + i, piece = x ^ swz_row(8 * lg);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(as + lg * 8 * kBlk), 16, (alane + (unsigned)(lg * 8) * lda + (piece << 4)) | invalid(piece), soff, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const int lg = wave * LB + i, piece = x ^ swz_row(8 * lg), w = lg / (2 * NI), lw = lg % (2 * NI);
+            const unsigned row = SWIGLU ? (unsigned)((lw >> 2) * p.F + w * 32 + weight_row_group<2>(lw & 3)) : (unsigned)(w * 16 * NI + weight_row_group<NI>(lw));
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(bs + lg * 8 * kBlk), 16, (blane + row * ldw + (piece << 4)) | invalid(piece), soff, 0, 0);
+        }
+    };
+    f32x4 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int arow = wm * MI * 16, brow = wn * NI * 16;
+    auto piece_of = [&](const uint8_t *tile, int row, int q) __attribute__((always_inline)) { return *(const i32x4 *)(tile + piece_off(row + r16, q * 4 + g)); };
+    int sa[MI], sw = 0, su = 0;
+    auto step = [&](auto parity, int kt, const uint8_t *as, const uint8_t *bs) __attribute__((always_inline)) {
+        constexpr int par = decltype(parity)::value;
+        if (par == 0) {                                  // scales of two K tiles
+#pragma unroll
+            for (int i = 0; i < MI; ++i) sa[i] = pa[(kt >> 1) * BM + arow + i * 16 + r16];
+            sw = pw[(kt >> 1) * NB + (!SWIGLU && NB == 2 ? wn * 16 * NI / kBlk : 0)];
+            if (SWIGLU) su = pw[(kt >> 1) * NB + 1];
+        }
+        i32x4 a[MI][2], b[NI][2];
+#pragma unroll
+        for (int j = 0; j < NI; ++j) { b[j][0] = piece_of(bs, brow + j * 16, 0); b[j][1] = piece_of(bs, brow + j * 16, 1); }
+#pragma unroll
+        for (int i = 0; i < MI; ++i) { a[i][0] = piece_of(as, arow + i * 16, 0); a[i][1] = piece_of(as, arow + i * 16, 1); }
+        if constexpr (PRECISE) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                bf16x8 y[NI];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) y[j] = widen8(b[j][q >> 1][2 * (q & 1)], b[j][q >> 1][2 * (q & 1) + 1], scale_of(sw >> (8 * par)));
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const bf16x8 v = widen8(a[i][q >> 1][2 * (q & 1)], a[i][q >> 1][2 * (q & 1) + 1], scale_of(sa[i] >> (8 * par)));
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[j], v, acc[i][j], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+                    acc[i][j] = mfma(join(b[j][0], b[j][1]), join(a[i][0], a[i][1]), acc[i][j], SWIGLU && j >= NI / 2 ? su : sw, sa[i], parity);
+        }
+    };
+    int wblk[2];
+    wblk[0] = n0 / kBlk;
+    wblk[1] = SWIGLU ? (p.F + n0) / kBlk : ((n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk);
+    for (; kt0 < p.kb; kt0 += kSegment) {
+        nk = p.kb - kt0 < kSegment ? p.kb - kt0 : kSegment;
+#pragma unroll
+        for (int k = 0; k < NST - 1; ++k) fetch(k, As[k], Bs[k]);
+        stage_scales<BM, NB, THREADS>(p, pa, pw, m0, wblk, kt0, nk, tid);
+        for (int kt = 0; kt < nk; kt += NST) {
+#pragma unroll
+            for (int k = 0; k < NST; ++k) {
+                if (k > 0 && kt + k >= nk) break;
+                // this tile has landed (own loads, then everybody's); the stage that the new loads go to was read a tile ago
+                wait_vmcnt_lgkm0<(NST - 2) * (LA + LB)>();
+                lds_barrier();
+                fetch(kt + k + NST - 1, As[(k + NST - 1) % NST], Bs[(k + NST - 1) % NST]);
+                if (k & 1) step(std::integral_constant<int, 1>{}, kt + k, As[k], Bs[k]);
+                else step(std::integral_constant<int, 0>{}, kt + k, As[k], Bs[k]);
+            }
+        }
+        dma_publish_barrier();
+    }
+    if constexpr (!SWIGLU) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            float v[4 * NI];
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][j][e];
+            store_row<4 * NI>(p, m0 + arow + i * 16 + r16, n0 + brow + 4 * NI * g, v);
+        }
+    } else {
+        swiglu_epilogue<MI, BM>(p, acc, (unsigned *)A0, m0, n0, wn, g, [&](int i) { return arow + i * 16 + r16; });
+    }
+}
+template <int BM, int BN, int WM, int WN, int NST, bool SWIGLU, bool PRECISE>
+__global__ __launch_bounds__(64 * WM * WN) void gemm_fp8_ring_kernel(Fp8Params p) { fp8_ring_body<BM, BN, WM, WN, NST, SWIGLU, PRECISE>(p); }
+
+// (named here because the host pass does not define all launch stubs of templates that only the launchers below use)
+#define MS_FP8_RING(BM, BN, WM, WN, NST)                                                    \
+    template __global__ void gemm_fp8_ring_kernel<BM, BN, WM, WN, NST, false, false>(Fp8Params); \
+    template __global__ void gemm_fp8_ring_kernel<BM, BN, WM, WN, NST, false, true>(Fp8Params)
+MS_FP8_RING(128, 128, 2, 2, 2);
+MS_FP8_RING(128, 128, 4, 2, 4);
+MS_FP8_RING(64, 128, 2, 2, 2);
+MS_FP8_RING(64, 128, 2, 2, 4);
+MS_FP8_RING(64, 64, 4, 1, 4);
+template __global__ void gemm_fp8_ring_kernel<128, 256, 2, 4, 2, true, false>(Fp8Params);
+template __global__ void gemm_fp8_ring_kernel<64, 256, 2, 4, 2, true, false>(Fp8Params);
+#undef MS_FP8_RING
+
+bool aligned(const void *p, int to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+ms_status check(const char *who, int M, int N, int K, const void *A, long lda, const void *sA, long ldsa, const void *W, long ldw, const void *sW, long ldsw) {
+    if (!A || !sA || !W || !sW || M < 0 || N <= 0 || K <= 0) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer or bad size", who);
+    if (K % 16) return ms_fail(MS_ERR_UNSUPPORTED, "%s: K=%d is not a multiple of 16", who, K);
+    const long words = (K + 511L) / 512 * 4;
+    if (lda < K || ldw < K || ldsa < words || ldsw < words) return ms_fail(MS_ERR_SHAPE, "%s: a row stride is less than a row", who);
+    if (lda % 16 || ldw % 16 || ldsa % 4 || ldsw % 4 || !aligned(A, 16) || !aligned(W, 16) || !aligned(sA, 4) || !aligned(sW, 4))
+        return ms_fail(MS_ERR_UNSUPPORTED, "%s: codes must have 16-byte, scales 4-byte aligned rows", who);
+    if (!ms_buffer_range_ok(256, K, lda, 1) || !ms_buffer_range_ok(256, K, ldw, 1)) return ms_fail(MS_ERR_UNSUPPORTED, "%s: rows are too far apart", who);
+    return MS_OK;
+}
+
+template <int MB, int NI, bool PRECISE> void launch_direct(const Fp8Params &p, hipStream_t s) {
+    gemm_fp8_direct_kernel<MB, NI, MB == 4 ? 1 : 2, PRECISE><<<dim3(ms_cdiv(p.N, 16 * NI), ms_cdiv(p.M, 16 * MB)), 64 * kDirectWaves, 0, s>>>(p);
+}
+template <bool PRECISE> void launch_direct(const Fp8Params &p, hipStream_t s) {
+    const int ni = p.N >= 64 * 256 ? 4 : p.N >= 32 * 256 ? 2 : 1;
+#define GO(MB)                                                 \
+    do {                                                       \
+        if (ni == 4) launch_direct<MB, 4, PRECISE>(p, s);      \
+        else if (ni == 2) launch_direct<MB, 2, PRECISE>(p, s); \
+        else launch_direct<MB, 1, PRECISE>(p, s);              \
+    } while (0)
+    if (p.M <= 16) GO(1); else if (p.M <= 32) GO(2); else GO(4);
+#undef GO
+}
+
+// tiles of a launch, or 0 if they do not fit one
+int tiles_of(Fp8Params &p, int bm, int bn, int cols, int threads) {
+    p.tiles_m = ms_cdiv(p.M, bm);
+    p.tiles_n = ms_cdiv(cols, bn);
+    const long tiles = (long)p.tiles_m * p.tiles_n;
+    return ms_launch_fits(tiles, threads) ? (int)tiles : 0;
+}
+template <int BM, int BN, int WM, int WN, int NST, bool SWIGLU, bool PRECISE> bool launch_ring(Fp8Params &p, hipStream_t s) {
+    const int tiles = tiles_of(p, BM, SWIGLU ? BN / 2 : BN, SWIGLU ? p.F : p.N, 64 * WM * WN);
+    if (tiles) gemm_fp8_ring_kernel<BM, BN, WM, WN, NST, SWIGLU, PRECISE><<<tiles, 64 * WM * WN, 0, s>>>(p);
+    return tiles != 0;
+}
+template <bool SWIGLU> bool launch_pp(Fp8Params &p, hipStream_t s) {
+    const int tiles = tiles_of(p, 256, SWIGLU ? 128 : 256, SWIGLU ? p.F : p.N, 512);
+    if (tiles && p.K % kBlk) gemm_fp8_pp_kernel<SWIGLU, true><<<tiles, 512, 0, s>>>(p);
+    else if (tiles) gemm_fp8_pp_kernel<SWIGLU, false><<<tiles, 512, 0, s>>>(p);
+    return tiles != 0;
+}
+
+// The tile that measurements and tests ask for (0: by shape), as in ms_k_gemm_config
+std::atomic<int> g_tile{0};
+
+// Tile codes: token rows * 1000 + outputs, + 1 for the deeper ring of stages
+enum { F256 = 256256, F128 = 128128, F128R = 128129, F64x128 = 64128, F64x128R = 64129, F64 = 64064 };
+int choose(const Fp8Params &p, bool precise) {
+    const int forced = g_tile.load();
+    if (forced && !(precise && forced == F256)) return forced;
+    const long t256 = (long)ms_cdiv(p.M, 256) * ms_cdiv(p.N, 256);
+    if (!precise && t256 >= 192) return F256;
+    const long t128 = (long)ms_cdiv(p.M, 128) * ms_cdiv(p.N, 128);
+    return t128 >= 256 ? F128 : F64x128;
+}
+template <bool PRECISE> bool launch_tile(int tile, Fp8Params &p, hipStream_t s) {
+    if (tile == F128) return launch_ring<128, 128, 2, 2, 2, false, PRECISE>(p, s);
+    if (tile == F128R) return launch_ring<128, 128, 4, 2, 4, false, PRECISE>(p, s);
+    if (tile == F64x128) return launch_ring<64, 128, 2, 2, 2, false, PRECISE>(p, s);
+    if (tile == F64x128R) return launch_ring<64, 128, 2, 2, 4, false, PRECISE>(p, s);
+    if (tile == F64) return launch_ring<64, 64, 4, 1, 4, false, PRECISE>(p, s);
+    return false;
+}
+ms_status launch_gemm(Fp8Params p, bool precise, hipStream_t s) {
+    ProfScope ps(0, 2.0 * p.M * p.N * p.K, s);
+    bool fits = true;
+    if (p.M <= 64 && !g_tile.load()) {
+        if (precise) launch_direct<true>(p, s); else launch_direct<false>(p, s);
+    } else {
+        const int tile = choose(p, precise);
+        fits = !precise && tile == F256 ? launch_pp<false>(p, s) : precise ? launch_tile<true>(tile, p, s) : launch_tile<false>(tile, p, s);
+    }
+    if (!fits) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8: %d x %d is too large for one launch", p.M, p.N);
+    MS_LAUNCH_CHECK();
+    return MS_OK;
+}
+
+// SwiGLU in the epilogue: gate and up rows of a tile's columns have to lie in whole blocks of 128 weight rows
+bool swiglu_fused(int M, int F, int K, long ldw) { return M > 64 && F % kBlk == 0 && ms_buffer_range_ok(2L * F, K, ldw, 1); }
+bool launch_swiglu(Fp8Params &p, hipStream_t s) {
+    const int forced = g_tile.load();
+    const long t256 = (long)ms_cdiv(p.M, 256) * ms_cdiv(p.F, 128), t128 = (long)ms_cdiv(p.M, 128) * ms_cdiv(p.F, 128);
+    const int tile = forced ? forced : t256 >= 192 ? F256 : t128 >= 192 ? F128 : F64x128;
+    if (tile == F256) return launch_pp<true>(p, s);
+    if (tile == F128 || tile == F128R) return launch_ring<128, 256, 2, 4, 2, true, false>(p, s);
+    return launch_ring<64, 256, 2, 4, 2, true, false>(p, s);
+}
+
+}  // namespace
+
+extern "C" ms_status ms_k_gemm_fp8_config(int32_t tile) {
+    if (tile != 0 && tile != F256 && tile != F128 && tile != F128R && tile != F64x128 && tile != F64x128R && tile != F64)
+        return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8_config: unknown tile %d", tile);
+    g_tile = tile;
+    return MS_OK;
+}
+
+extern "C" ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W,
+                                   int64_t ldw, const void *sW, int64_t ldsw, void *C, int64_t ldc, int32_t c_fp32, const void *residual,
+                                   int64_t ldr, int32_t residual_fp32, void *stream) {
+    if (M == 0) return MS_OK;
+    MS_TRY(check("gemm_fp8", M, N, K, A, lda, sA, ldsa, W, ldw, sW, ldsw));
+    if (!C || c_fp32 < 0 || c_fp32 > 2) return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8: null pointer or bad c_fp32");
+    if (ldc < N || (residual && ldr < N)) return ms_fail(MS_ERR_SHAPE, "gemm_fp8: a row stride is less than a row");
+    const int ec = c_fp32 ? 4 : 2, er = residual_fp32 ? 4 : 2;
+    if (!aligned(C, ec) || (residual && !aligned(residual, er))) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8: C or residual is not aligned to its type");
+    Fp8Params p = {};
+    p.A = (const uint8_t *)A; p.sA = (const uint8_t *)sA; p.W = (const uint8_t *)W; p.sW = (const uint8_t *)sW;
+    p.lda = lda; p.ldsa = ldsa; p.ldw = ldw; p.ldsw = ldsw;
+    p.C = C; p.ldc = ldc; p.R = residual; p.ldr = ldr; p.c_fp32 = c_fp32 != 0; p.r_fp32 = residual_fp32 != 0;
+    p.vec = N % 16 == 0 && ldc * ec % 16 == 0 && aligned(C, 16) && (!residual || (ldr * er % 16 == 0 && aligned(residual, 16)));
+    p.M = M; p.N = N; p.K = K; p.kb = ms_cdiv(K, kBlk);
+    return launch_gemm(p, c_fp32 == 1, (hipStream_t)stream);
+}
+
+extern "C" size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K) {
+    if (M <= 0 || F <= 0 || K <= 0 || swiglu_fused(M, F, K, K)) return 0;
+    return ms_align_up((size_t)M * 2 * F * sizeof(float));
+}
+
+extern "C" ms_status ms_k_gemm_fp8_swiglu(int32_t M, int32_t F, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W,
+                                          int64_t ldw, const void *sW, int64_t ldsw, void *q, int64_t ldq, void *scales, int64_t lds,
+                                          void *scratch, size_t scratch_bytes, void *stream) {
+    if (M == 0) return MS_OK;
+    if (F <= 0 || F > 0x3fffffff) return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8_swiglu: bad size");
+    MS_TRY(check("gemm_fp8_swiglu", M, 2 * F, K, A, lda, sA, ldsa, W, ldw, sW, ldsw));
+    if (!q || !scales) return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8_swiglu: null pointer");
+    if (F % 16) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8_swiglu: F=%d is not a multiple of 16", F);
+    if (ldq < F || lds < (F + 511L) / 512 * 4) return ms_fail(MS_ERR_SHAPE, "gemm_fp8_swiglu: a row stride is less than a row");
+    if (ldq % 16 || lds % 4 || !aligned(q, 16) || !aligned(scales, 4)) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8_swiglu: codes must have 16-byte, scales 4-byte aligned rows");
+    Fp8Params p = {};
+    p.A = (const uint8_t *)A; p.sA = (const uint8_t *)sA; p.W = (const uint8_t *)W; p.sW = (const uint8_t *)sW;
+    p.lda = lda; p.ldsa = ldsa; p.ldw = ldw; p.ldsw = ldsw;
+    p.M = M; p.N = 2 * F; p.K = K; p.F = F; p.kb = ms_cdiv(K, kBlk);
+    hipStream_t s = (hipStream_t)stream;
+    if (swiglu_fused(M, F, K, ldw)) {
+        p.C = q; p.ldc = ldq; p.sC = (uint8_t *)scales; p.ldsc = lds;
+        ProfScope ps(0, 4.0 * M * F * K, s);
+        if (!launch_swiglu(p, s)) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8_swiglu: %d x %d is too large for one launch", M, F);
+        MS_LAUNCH_CHECK();
+        return MS_OK;
+    }
+    // gate and up in fp32 first: the same numbers before the same activation
+    const size_t need = ms_align_up((size_t)M * 2 * F * sizeof(float));
+    if (!scratch || scratch_bytes < need) return ms_fail(MS_ERR_WORKSPACE, "gemm_fp8_swiglu: scratch %zu < %zu bytes", scratch_bytes, need);
+    if (!aligned(scratch, 16)) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8_swiglu: scratch must be 16-byte aligned");
+    p.C = scratch; p.ldc = 2L * F; p.c_fp32 = 1; p.vec = 1;
+    MS_TRY(launch_gemm(p, false, s));
+    return ms_k_swiglu_fp8(MS_F32, M, F, scratch, 2L * F, q, ldq, scales, lds, stream);
+}
