@@ -444,12 +444,14 @@ def _fn(name):
 
 def _call(name, dev, *args):
     """The library's entry point on the current stream of `dev`, which is made the current device for the call."""
-    stream = torch.cuda.current_stream(dev).cuda_stream
-    if dev.index == torch.cuda.current_device():
-        _check(_fn(name)(*args, stream))
+    f, i = _fn(name), dev.index
+    if i == torch._C._cuda_getDevice():
+        status = f(*args, torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(dev):
-            _check(_fn(name)(*args, stream))
+            status = f(*args, torch._C._cuda_getCurrentRawStream(i))
+    if status:
+        _check(status)
 
 
 def _need(name, t, dtypes, shape, device, rows=False):
@@ -457,11 +459,12 @@ def _need(name, t, dtypes, shape, device, rows=False):
     whose rows are."""
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise ValueError(f"{name}: expected a tensor of {' or '.join(str(d) for d in dtypes)}, got {getattr(t, 'dtype', type(t).__name__)}")
-    if t.dim() != len(shape) or any(s is not None and s != a for s, a in zip(shape, t.shape)):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    have = t.shape
+    if have != shape and (len(have) != len(shape) or any(s is not None and s != a for s, a in zip(shape, have))):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(have)}")
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name}: expected a tensor on {device or 'a GPU'}, got one on {t.device}")
-    if not (t.is_contiguous() or (rows and t.stride(1) == 1 and t.stride(0) >= t.shape[1])):
+    if not (t.is_contiguous() or (rows and t.stride(1) == 1 and t.stride(0) >= have[1])):
         raise ValueError(f"{name}: expected {'rows with unit stride' if rows else 'a contiguous tensor'}, got strides {t.stride()}")
 
 

@@ -6,10 +6,11 @@
 // The gradient needs no floating-point atomics: its sums have one order, so a run repeats bit for bit, and a row that thousands
 // of tokens share (padding, frequent words) is not added to by thousands of atomics.  Steps:
 //   1. stable radix sort of (id, token): per digit, a workgroup ranks its tokens and places them behind those of the workgroups
-//      before it (per-workgroup digit counts; integer atomics, whose order does not matter).  Ids outside the table sort last.
-//   2. every kTile sorted places x one 16-byte column vector per thread: one pass over dx.  A run of equal ids that lies within
+//      before it (per-workgroup digit counts; integer atomics, whose order does not matter).  Up to kSmall tokens one workgroup
+//      does all digits in LDS.  Ids outside the table sort last.
+//   2. pieces of 8 or 32 sorted places x one 16-byte column vector per thread: one pass over dx.  A run of equal ids that lies within
 //      the piece is added to the table; what continues from or into a neighbour goes to a row of partial sums.
-//   3. the runs that span pieces: their partial rows are added up and go to the table.
+//   3. the runs that span pieces (step 2 lists them): their partial rows are added up and go to the table.
 // HBM bounds step 2 (dx read once, touched rows read and written), launches and latency the sort.
 #include "common.h"
 #include "launch.h"
@@ -18,7 +19,7 @@
 namespace {
 
 constexpr int kSortThreads = 1024, kWaves = kSortThreads / 64, kDigitBits = 9, kBins = 1 << kDigitBits;
-constexpr int kTile = 32;                 // sorted places of a piece
+constexpr int kSmall = 4 * kSortThreads;  // tokens that one workgroup sorts in LDS
 constexpr int kMaxTokens = 1 << 24;
 
 // ------------------------------------------------------------------ forward
@@ -61,9 +62,10 @@ __device__ __forceinline__ unsigned key_of(int id, int vocab) { return (unsigned
 
 // Digit counts of every workgroup's tokens by the first digit; clears the counters that the passes add to
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int *__restrict__ ids, int n, int vocab, int per, int mask,
-                                                                  int *__restrict__ counts, int *__restrict__ next, long next_len) {
+                                                                  int *__restrict__ counts, int *__restrict__ next, long next_len, int *__restrict__ runs) {
     __shared__ int hist[kBins];
     const int tid = threadIdx.x;
+    if (blockIdx.x == 0 && tid == 0) *runs = 0;
     if (tid < kBins) hist[tid] = 0;
     __syncthreads();
     const long b0 = (long)blockIdx.x * per;
@@ -73,10 +75,48 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int *__r
     for (long i = (long)blockIdx.x * kSortThreads + tid; i < next_len; i += (long)gridDim.x * kSortThreads) next[i] = 0;
 }
 
+// Ranks of a workgroup's tokens by a digit: lanes of equal digits find each other by ballots, the first of them moves the wave's
+// counter on.  A wave has 64 IPT consecutive places, 64 of them per trip; hist[w][digit] ends up as the wave's count.
+template <int IPT>
+__device__ __forceinline__ void rank_digit(const unsigned (&key)[IPT], const bool (&valid)[IPT], int shift, int bits, int *hist, int (&rank)[IPT]) {
+    const int lane = threadIdx.x & 63, mask = (1 << bits) - 1;
+#pragma unroll
+    for (int r = 0; r < IPT; ++r) {
+        const int dg = (key[r] >> shift) & mask;
+        unsigned long long same = __ballot(valid[r]);
+        for (int k = 0; k < bits; ++k) {
+            const unsigned long long m = __ballot((dg >> k) & 1);
+            same &= (dg >> k) & 1 ? m : ~m;
+        }
+        const int before = __popcll(same & ((1ull << lane) - 1)), cnt = __popcll(same);
+        const int pre = hist[dg];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (valid[r] && before == 0) hist[dg] = pre + cnt;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        rank[r] = pre + before;
+    }
+}
+// Prefix sum of the first kBins threads' values over the workgroup's digits (all threads call it)
+__device__ __forceinline__ int scan_bins(int v, int *wsum) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    int inc = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(inc, o, 64);
+        if (lane >= o) inc += u;
+    }
+    if (lane == 63 && wv < kBins / 64) wsum[wv] = inc;
+    __syncthreads();
+    int add = 0;
+#pragma unroll
+    for (int w = 0; w < kBins / 64; ++w) add += w < wv ? wsum[w] : 0;
+    return inc - v + add;
+}
+
 // One stable pass by the digit (key >> shift) & mask.  ids != null: the keys are the ids and the values the token numbers.
-// counts: [workgroups][kBins] of this digit (null: there is one workgroup); next: the same for the following digit in the
-// new order, added to here.  A wave takes 64 IPT consecutive places, a trip 64 of them: lanes of equal digits find each other
-// by ballots, the first of them moves the wave's counter on.
+// counts: [workgroups][kBins] of this digit; next: the same for the following digit in the new order, added to here.
 template <int IPT>
 __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(const int *__restrict__ ids, const uint2 *__restrict__ in, int n, int vocab, int shift,
                                                                  int bits, const int *__restrict__ counts, int *__restrict__ next,
@@ -85,171 +125,238 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(const int *__re
     __shared__ int base[kBins];
     __shared__ int wsum[kBins / 64];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, mask = (1 << bits) - 1, per = kSortThreads * IPT;
-    for (int i = tid; i < kWaves * kBins; i += kSortThreads) (&hist[0][0])[i] = 0;
-    __syncthreads();
     const long b0 = (long)blockIdx.x * per + wv * 64 * IPT;
     uint2 kv[IPT];
+    unsigned key[IPT];
+    bool valid[IPT];
     int rank[IPT];
 #pragma unroll
     for (int r = 0; r < IPT; ++r) {
         const long i = b0 + r * 64 + lane;
-        const bool valid = i < n;
+        valid[r] = i < n;
         kv[r] = make_uint2(0, 0);
-        if (valid) kv[r] = ids ? make_uint2(key_of(ids[i], vocab), (unsigned)i) : in[i];
+        if (valid[r]) kv[r] = ids ? make_uint2(key_of(ids[i], vocab), (unsigned)i) : in[i];
+        key[r] = kv[r].x;
     }
-#pragma unroll
-    for (int r = 0; r < IPT; ++r) {
-        const bool valid = b0 + r * 64 + lane < n;
-        const int dg = (kv[r].x >> shift) & mask;
-        unsigned long long same = __ballot(valid);
-        for (int k = 0; k < bits; ++k) {
-            const unsigned long long m = __ballot((dg >> k) & 1);
-            same &= (dg >> k) & 1 ? m : ~m;
-        }
-        const int before = __popcll(same & ((1ull << lane) - 1)), cnt = __popcll(same);
-        const int pre = hist[wv][dg];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (valid && before == 0) hist[wv][dg] = pre + cnt;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        rank[r] = pre + before;
-    }
-    __syncthreads();
+    // all tokens of a digit, and those of the workgroups in front: two threads per digit, eight rows requested at a time
     int total = 0, ahead = 0;
+    {
+        const int d = tid & (kBins - 1), nb = gridDim.x, mine = blockIdx.x;
+        for (int b = tid >> kDigitBits; b < nb; b += 16) {
+            int c[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u] = b + 2 * u < nb ? counts[(long)(b + 2 * u) * kBins + d] : 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                total += c[u];
+                ahead += b + 2 * u < mine ? c[u] : 0;
+            }
+        }
+    }
+    for (int i = tid; i < kWaves * kBins; i += kSortThreads) (&hist[0][0])[i] = 0;
+    __syncthreads();
+    rank_digit<IPT>(key, valid, shift, bits, hist[wv], rank);
+    int *half = base;                                    // the upper half's sums on their way to the lower
+    if (tid >= kBins) half[tid - kBins] = total;
+    __syncthreads();
+    if (tid < kBins) total += half[tid];
+    __syncthreads();
+    if (tid >= kBins) half[tid - kBins] = ahead;
+    __syncthreads();
     if (tid < kBins) {
+        ahead += half[tid];
+        int before = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const int c = hist[w][tid];
-            hist[w][tid] = total;
-            total += c;
+            hist[w][tid] = before;
+            before += c;
         }
-        if (counts) {                                   // all tokens of this digit, and those of the workgroups in front
-            total = 0;
-            for (int b = 0; b < (int)gridDim.x; ++b) {
-                const int c = counts[(long)b * kBins + tid];
-                total += c;
-                ahead += b < (int)blockIdx.x ? c : 0;
-            }
-        }
-        int inc = total;                                // prefix sum over the digits
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(inc, o, 64);
-            if (lane >= o) inc += v;
-        }
-        if (lane == 63) wsum[wv] = inc;
-        base[tid] = inc - total + ahead;
     }
-    __syncthreads();
-    if (tid < kBins) {
-        int add = 0;
-        for (int w = 0; w < wv; ++w) add += wsum[w];
-        base[tid] += add;
-    }
+    const int first = scan_bins(tid < kBins ? total : 0, wsum);
+    if (tid < kBins) base[tid] = first + ahead;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < IPT; ++r) {
-        if (b0 + r * 64 + lane < n) {
-            const int dg = (kv[r].x >> shift) & mask;
+        if (valid[r]) {
+            const int dg = (key[r] >> shift) & mask;
             const int at = base[dg] + hist[wv][dg] + rank[r];
             out[at] = kv[r];
-            if (next) atomicAdd(next + (long)(at / per) * kBins + ((kv[r].x >> next_shift) & mask), 1);
+            if (next) atomicAdd(next + (long)(at / per) * kBins + ((key[r] >> next_shift) & mask), 1);
         }
+    }
+}
+
+// All digits of up to kSmall tokens in one workgroup
+template <int IPT>
+__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int *__restrict__ ids, int n, int vocab, int bits, int passes, uint2 *__restrict__ out,
+                                                                  int *__restrict__ runs) {
+    __shared__ int hist[kWaves][kBins];
+    __shared__ int base[kBins];
+    __shared__ int wsum[kBins / 64];
+    __shared__ uint2 item[kSortThreads * IPT];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, mask = (1 << bits) - 1, b0 = wv * 64 * IPT;
+    if (tid == 0) *runs = 0;
+    uint2 kv[IPT];
+    unsigned key[IPT];
+    bool valid[IPT];
+    int rank[IPT];
+#pragma unroll
+    for (int r = 0; r < IPT; ++r) {
+        const int i = b0 + r * 64 + lane;
+        valid[r] = i < n;
+        kv[r] = valid[r] ? make_uint2(key_of(ids[i], vocab), (unsigned)i) : make_uint2(0, 0);
+    }
+    for (int p = 0; p < passes; ++p) {
+        const int shift = p * bits;
+#pragma unroll
+        for (int r = 0; r < IPT; ++r) {
+            if (p && valid[r]) kv[r] = item[b0 + r * 64 + lane];
+            key[r] = kv[r].x;
+        }
+        for (int i = tid; i < kWaves * kBins; i += kSortThreads) (&hist[0][0])[i] = 0;
+        __syncthreads();
+        rank_digit<IPT>(key, valid, shift, bits, hist[wv], rank);
+        __syncthreads();
+        int total = 0;
+        if (tid < kBins) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const int c = hist[w][tid];
+                hist[w][tid] = total;
+                total += c;
+            }
+        }
+        const int first = scan_bins(total, wsum);
+        if (tid < kBins) base[tid] = first;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < IPT; ++r) {
+            if (!valid[r]) continue;
+            const int dg = (key[r] >> shift) & mask, at = base[dg] + hist[wv][dg] + rank[r];
+            if (p + 1 == passes) out[at] = kv[r];
+            else item[at] = kv[r];
+        }
+        __syncthreads();
     }
 }
 
 // ------------------------------------------------------------------ sums
-// part: [pieces][2][d]: row 0 the end of a run that began in an earlier piece, row 1 the part of a run that goes on in the next
-template <class T>
+// part: [pieces][2][d]: row 0 the end of a run that began in an earlier piece, row 1 the part of a run that goes on in the next.
+// runs[0] counts, runs[1 ..] list the pieces in which a run begins that goes on (in any order: each is added up by itself).
+// U places at a time: their rows of dx and the table rows of the runs that end there are requested together.
+template <class T, int TILE, int U>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint2 *__restrict__ sorted, const T *__restrict__ dx, float scale, int n, int vpr,
-                                                            int vocab, float *__restrict__ d_table, float *__restrict__ part, long total) {
-    constexpr int V = Vec16<T>::N, U = 8;
+                                                            int vocab, float *__restrict__ d_table, float *__restrict__ part, int *__restrict__ runs,
+                                                            long total) {
+    constexpr int V = Vec16<T>::N;
     const long i = (long)blockIdx.x * 256 + threadIdx.x;
     if (i >= total) return;
-    const long tile = i / vpr, d = (long)vpr * V;
-    const long cv = (i % vpr) * V;
-    const int p0 = (int)(tile * kTile), p1 = p0 + kTile < n ? p0 + kTile : n;
+    const int tile = (int)(total < 0x7fffffff ? (unsigned)i / (unsigned)vpr : i / vpr);
+    const long d = (long)vpr * V, cv = (i - (long)tile * vpr) * V;
+    const int p0 = tile * TILE, p1 = p0 + TILE < n ? p0 + TILE : n;
     const unsigned before = p0 > 0 ? sorted[p0 - 1].x : 0xffffffffu, after = p1 < n ? sorted[p1].x : 0xffffffffu;
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    unsigned run = sorted[p0].x;
-    bool first = true;                                   // the run that the piece begins with
     auto store = [&](float *o) {
 #pragma unroll
         for (int q = 0; q < V; q += 4) *(float4 *)(o + q) = make_float4(acc[q], acc[q + 1], acc[q + 2], acc[q + 3]);
     };
-    auto flush = [&]() {                                 // the run ends within the piece
-        if (run < (unsigned)vocab) {
-            if (first && run == before) {
-                store(part + tile * 2 * d + cv);
-            } else {
-                float *o = d_table + (long)run * d + cv;
-#pragma unroll
-                for (int q = 0; q < V; q += 4) {
-                    float4 v = *(float4 *)(o + q);
-                    v.x = __builtin_fmaf(scale, acc[q], v.x); v.y = __builtin_fmaf(scale, acc[q + 1], v.y);
-                    v.z = __builtin_fmaf(scale, acc[q + 2], v.z); v.w = __builtin_fmaf(scale, acc[q + 3], v.w);
-                    *(float4 *)(o + q) = v;
-                }
-            }
-        }
-        first = false;
-#pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    };
+    bool from_before = before != 0xffffffffu && sorted[p0].x == before;      // the present run began in an earlier piece
+    bool open = false;                                                       // a run goes on in the next piece, and began here
     for (int p = p0; p < p1; p += U) {
-        uint2 kv[U];
+        uint2 kv[U + 1];
         Vec16<T> v[U];
+        float4 old[U][V / 4];
+        bool end[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) kv[u] = sorted[p + u < p1 ? p + u : p1 - 1];
+        kv[U].x = p + U < p1 ? sorted[p + U].x : after;
+        const bool fb = from_before;
+        bool seen = false;                                                   // a run has ended among these places
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u < p1 && kv[u].x < (unsigned)vocab) v[u] = ldv(dx + (long)kv[u].y * d + cv);
+        for (int u = 0; u < U; ++u) {
+            const unsigned nextk = p + u + 1 < p1 ? kv[u + 1].x : after;
+            end[u] = p + u < p1 && kv[u].x != nextk;
+            if (p + u < p1 && kv[u].x < (unsigned)vocab) {
+                v[u] = ldv(dx + (long)kv[u].y * d + cv);
+                if (end[u] && (seen || !fb)) {
+                    const float *o = d_table + (long)kv[u].x * d + cv;
+#pragma unroll
+                    for (int q = 0; q < V / 4; ++q) old[u][q] = *(const float4 *)(o + 4 * q);
+                }
+            }
+            seen |= end[u];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p + u >= p1) break;
-            if (kv[u].x != run) { flush(); run = kv[u].x; }
-            if (run < (unsigned)vocab)
+            const bool in = kv[u].x < (unsigned)vocab;
+            if (in)
 #pragma unroll
                 for (int e = 0; e < V; ++e) acc[e] += to_f32(v[u].v[e]);
-        }
-    }
-    if (run == after) {
-        if (run < (unsigned)vocab) store(part + (tile * 2 + 1) * d + cv);
-    } else {
-        flush();
-    }
-}
-
-// A workgroup per piece and 128 columns: where a run begins in the piece and goes on behind it, the partial rows of that run, every
-// eighth by the same 32 threads, then the eight sums in order
-__global__ __launch_bounds__(256) void embedding_join_kernel(const uint2 *__restrict__ sorted, const float *__restrict__ part, float scale, int n, long d,
-                                                             int tiles, int vocab, float *__restrict__ d_table) {
-    __shared__ float4 sm[8][32];
-    const int tile = blockIdx.x, p0 = tile * kTile, p1 = p0 + kTile;
-    if (p1 >= n) return;
-    const unsigned run = sorted[p1 - 1].x;
-    if (run != sorted[p1].x || run >= (unsigned)vocab || (p0 > 0 && sorted[p0].x == run && sorted[p0 - 1].x == run)) return;
-    const int cl = threadIdx.x & 31, pl = threadIdx.x >> 5;
-    for (long c0 = (long)blockIdx.y * 128; c0 < d; c0 += (long)gridDim.y * 128) {
-        const long col = c0 + 4 * cl;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int q = tile + pl; q < tiles; q += 8) {
-            if (sorted[(long)q * kTile + (q == tile ? kTile - 1 : 0)].x != run) break;
-            const bool more = (long)(q + 1) * kTile < n && sorted[(long)(q + 1) * kTile].x == run;
-            if (col < d) {
-                const float4 v = *(const float4 *)(part + ((long)q * 2 + more) * d + col);
-                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            if (end[u]) {
+                if (in && from_before) {
+                    store(part + (long)tile * 2 * d + cv);
+                } else if (in) {
+                    float *o = d_table + (long)kv[u].x * d + cv;
+#pragma unroll
+                    for (int q = 0; q < V / 4; ++q) {
+                        const float4 t = old[u][q];
+                        *(float4 *)(o + 4 * q) = make_float4(__builtin_fmaf(scale, acc[4 * q], t.x), __builtin_fmaf(scale, acc[4 * q + 1], t.y),
+                                                             __builtin_fmaf(scale, acc[4 * q + 2], t.z), __builtin_fmaf(scale, acc[4 * q + 3], t.w));
+                    }
+                }
+                from_before = false;
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] = 0.f;
+            } else if (p + u + 1 == p1 && in) {
+                store(part + ((long)tile * 2 + 1) * d + cv);
+                open = !from_before;
             }
         }
-        sm[pl][cl] = s;
-        __syncthreads();
-        if (pl == 0 && col < d) {
+    }
+    if (open && cv == 0) runs[1 + atomicAdd(runs, 1)] = tile;
+}
+
+// The runs that span pieces.  A task is one of them and 256 columns: four row groups of 64 threads take every fourth partial row, eight
+// requested at a time; their sums are added in order.
+template <int TILE>
+__global__ __launch_bounds__(256) void embedding_join_kernel(const uint2 *__restrict__ sorted, const float *__restrict__ part, float scale, int n, long d,
+                                                             float *__restrict__ d_table, const int *__restrict__ runs) {
+    __shared__ float4 sm[4][64];
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, strips = (int)((d + 255) / 256), tiles = (n + TILE - 1) / TILE;
+    const long tasks = (long)runs[0] * strips;
+    for (long k = blockIdx.x; k < tasks; k += gridDim.x) {
+        const int tile = runs[1 + k / strips];
+        const long col = (k % strips) * 256 + 4 * lane;
+        const unsigned run = sorted[(long)(tile + 1) * TILE].x;
+        int last = tile + 1;                             // the piece in which the run ends: 64 pieces are looked at together
+        for (;; last += 64) {
+            const int q = last + 1 + lane;
+            const unsigned long long on = __ballot(q < tiles && sorted[(long)(q < tiles ? q : 0) * TILE].x == run);
+            if (~on) { last += __ffsll(~on) - 1; break; }
+        }
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (col < d) {
+            for (int q = tile + wv; q <= last; q += 32) {
+                float4 v[8];
 #pragma unroll
-            for (int k = 1; k < 8; ++k) {
-                const float4 v = sm[k][cl];
+                for (int u = 0; u < 8; ++u) {
+                    const int t = q + 4 * u;
+                    v[u] = t <= last ? *(const float4 *)(part + ((long)t * 2 + (t < last)) * d + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
+            }
+        }
+        sm[wv][lane] = s;
+        __syncthreads();
+        if (wv == 0 && col < d) {
+#pragma unroll
+            for (int w = 1; w < 4; ++w) {
+                const float4 v = sm[w][lane];
                 s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
             float4 *o = (float4 *)(d_table + (long)run * d + col), v = *o;
@@ -261,26 +368,29 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const uint2 *__rest
     }
 }
 
-struct SortPlan { int bits, passes, ipt, blocks; };
-SortPlan sort_plan(int n, int vocab) {
+struct SortPlan { int bits, passes, ipt, blocks, tile; };
+SortPlan sort_plan(int n, int vocab, int vpr) {
     SortPlan p;
     int bits = 1;
     while (bits < 31 && (vocab >> bits) > 0) ++bits;                 // keys 0 .. vocab
     p.passes = (bits + kDigitBits - 1) / kDigitBits;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.ipt = n <= 128 * kSortThreads ? 1 : n <= 512 * kSortThreads ? 4 : 16;
-    p.blocks = ms_cdiv(n, (long)p.ipt * kSortThreads);
+    p.blocks = n <= kSmall ? 1 : ms_cdiv(n, (long)p.ipt * kSortThreads);
+    // pieces of 8 places where 32 would leave the chip without work
+    p.tile = (long)n * vpr < 8192L * 256 ? 8 : 32;
     return p;
 }
-struct SortScratch { uint2 *a, *b; int *counts; float *part; size_t bytes; };
-SortScratch carve(void *ws, int n, int d, int vocab) {
-    const SortPlan p = sort_plan(n, vocab);
+struct SortScratch { uint2 *a, *b; int *counts, *runs; float *part; size_t bytes; };
+SortScratch carve(void *ws, const SortPlan &p, int n, int d) {
+    const size_t tiles = (size_t)ms_cdiv(n, p.tile);
     Arena a(ws);
     SortScratch s;
     s.a = a.take<uint2>((size_t)n * 8);
     s.b = a.take<uint2>((size_t)n * 8);
     s.counts = a.take<int>((size_t)p.passes * p.blocks * kBins * 4);
-    s.part = a.take<float>((size_t)ms_cdiv(n, kTile) * 2 * d * 4);
+    s.runs = a.take<int>((tiles + 1) * 4);
+    s.part = a.take<float>(tiles * 2 * d * 4);
     s.bytes = a.off;
     return s;
 }
@@ -323,7 +433,8 @@ extern "C" ms_status ms_k_embedding_scaled_forward(int32_t dtype, int32_t out_fp
 
 extern "C" size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_t d, int32_t vocab) {
     if (n <= 0 || n > kMaxTokens || d <= 0 || vocab <= 0 || vocab == 0x7fffffff) return 0;
-    return carve(nullptr, n, d, vocab).bytes;
+    // (pieces are as small for either type as for the one with fewer vectors per row)
+    return carve(nullptr, sort_plan(n, vocab, d / 8), n, d).bytes;
 }
 
 extern "C" ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, int32_t d, int32_t vocab, float scale, const int32_t *ids,
@@ -333,38 +444,47 @@ extern "C" ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, in
     if (!ids || !dx || !d_table || !scratch) return ms_fail(MS_ERR_INVALID_ARG, "embedding_sorted_backward: null pointer");
     if (n > kMaxTokens) return ms_fail(MS_ERR_UNSUPPORTED, "embedding_sorted_backward: %d tokens, at most %d", n, kMaxTokens);
     if (!aligned(dx) || !aligned(d_table) || !aligned(scratch)) return ms_fail(MS_ERR_UNSUPPORTED, "embedding_sorted_backward: dx, d_table and scratch must be 16-byte aligned");
-    const SortScratch sc = carve(scratch, n, d, vocab);
-    if (scratch_bytes < sc.bytes) return ms_fail(MS_ERR_WORKSPACE, "embedding_sorted_backward: scratch %zu < %zu bytes", scratch_bytes, sc.bytes);
-    const int vpr = d / (dtype == MS_BF16 ? 8 : 4), tiles = ms_cdiv(n, kTile);
+    const int vpr = d / (dtype == MS_BF16 ? 8 : 4);
+    const SortPlan p = sort_plan(n, vocab, vpr);
+    const SortScratch sc = carve(scratch, p, n, d);
+    const size_t need = ms_k_embedding_sorted_backward_scratch_bytes(n, d, vocab);
+    if (scratch_bytes < need) return ms_fail(MS_ERR_WORKSPACE, "embedding_sorted_backward: scratch %zu < %zu bytes", scratch_bytes, need);
+    const int tiles = ms_cdiv(n, p.tile);
     const long total = (long)tiles * vpr;
     if (!ms_launch_fits((total + 255) / 256, 256)) return ms_fail(MS_ERR_UNSUPPORTED, "embedding_sorted_backward: %d tokens of %d columns are too many for one launch", n, d);
-    const SortPlan p = sort_plan(n, vocab);
     hipStream_t s = (hipStream_t)stream;
     ProfScope ps(11, (double)n * d * (ms_dtype_size(dtype) + 8.0), s);
-    const long cb = (long)p.blocks * kBins;
-    const bool many = p.blocks > 1;
-    if (many) {
-        sort_count_kernel<<<p.blocks, kSortThreads, 0, s>>>(ids, n, vocab, p.ipt * kSortThreads, (1 << p.bits) - 1, sc.counts, sc.counts + cb, (p.passes - 1) * cb);
-        MS_LAUNCH_CHECK();
-    }
     const uint2 *in = nullptr;
-    for (int k = 0; k < p.passes; ++k) {
-        uint2 *out = (k & 1) ? sc.b : sc.a;
-        const int *counts = many ? sc.counts + k * cb : nullptr;
-        int *next = many && k + 1 < p.passes ? sc.counts + (k + 1) * cb : nullptr;
-#define GO(I) sort_pass_kernel<I><<<p.blocks, kSortThreads, 0, s>>>(k ? nullptr : ids, in, n, vocab, k * p.bits, p.bits, counts, next, (k + 1) * p.bits, out)
-        if (p.ipt == 1) GO(1); else if (p.ipt == 4) GO(4); else GO(16);
-#undef GO
+    if (p.blocks == 1) {
+        if (n <= kSortThreads) sort_small_kernel<1><<<1, kSortThreads, 0, s>>>(ids, n, vocab, p.bits, p.passes, sc.a, sc.runs);
+        else sort_small_kernel<4><<<1, kSortThreads, 0, s>>>(ids, n, vocab, p.bits, p.passes, sc.a, sc.runs);
         MS_LAUNCH_CHECK();
-        in = out;
+        in = sc.a;
+    } else {
+        const long cb = (long)p.blocks * kBins;
+        sort_count_kernel<<<p.blocks, kSortThreads, 0, s>>>(ids, n, vocab, p.ipt * kSortThreads, (1 << p.bits) - 1, sc.counts, sc.counts + cb, (p.passes - 1) * cb, sc.runs);
+        MS_LAUNCH_CHECK();
+        for (int k = 0; k < p.passes; ++k) {
+            uint2 *out = (k & 1) ? sc.b : sc.a;
+            int *next = k + 1 < p.passes ? sc.counts + (k + 1) * cb : nullptr;
+#define GO(I) sort_pass_kernel<I><<<p.blocks, kSortThreads, 0, s>>>(k ? nullptr : ids, in, n, vocab, k * p.bits, p.bits, sc.counts + k * cb, next, (k + 1) * p.bits, out)
+            if (p.ipt == 1) GO(1); else if (p.ipt == 4) GO(4); else GO(16);
+#undef GO
+            MS_LAUNCH_CHECK();
+            in = out;
+        }
     }
-    const int blocks = (int)((total + 255) / 256);
-    if (dtype == MS_BF16) embedding_sum_kernel<bf16_t><<<blocks, 256, 0, s>>>(in, (const bf16_t *)dx, scale, n, vpr, vocab, d_table, sc.part, total);
-    else embedding_sum_kernel<float><<<blocks, 256, 0, s>>>(in, (const float *)dx, scale, n, vpr, vocab, d_table, sc.part, total);
+    const int blocks = (int)((total + 255) / 256), strips = ms_cdiv(d, 256);
+    const long tasks = (long)(tiles - 1) * strips;       // at most
+#define GO(T, TILE, U) embedding_sum_kernel<T, TILE, U><<<blocks, 256, 0, s>>>(in, (const T *)dx, scale, n, vpr, vocab, d_table, sc.part, sc.runs, total)
+    if (dtype == MS_BF16) { if (p.tile == 8) GO(bf16_t, 8, 8); else GO(bf16_t, 32, 4); }
+    else { if (p.tile == 8) GO(float, 8, 8); else GO(float, 32, 8); }
+#undef GO
     MS_LAUNCH_CHECK();
-    if (tiles > 1) {
-        const int gy = ms_cdiv(d, 128);
-        embedding_join_kernel<<<dim3(tiles, gy < 65535 ? gy : 65535), 256, 0, s>>>(in, sc.part, scale, n, d, tiles, vocab, d_table);
+    if (tasks > 0) {
+        const int grid = (int)(tasks < 2048 ? tasks : 2048);
+        if (p.tile == 8) embedding_join_kernel<8><<<grid, 256, 0, s>>>(in, sc.part, scale, n, d, d_table, sc.runs);
+        else embedding_join_kernel<32><<<grid, 256, 0, s>>>(in, sc.part, scale, n, d, d_table, sc.runs);
         MS_LAUNCH_CHECK();
     }
     return MS_OK;

@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int kPartRows = 1024;      // workgroups of the backward kernel, one partial row of dg each
+constexpr int kPartRows = 768;       // workgroups of the backward kernel, one partial row of dg each
 
 template <int G> __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
@@ -137,17 +137,21 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
     const int dt = HPW / nh, dh = HPW % nh;
     long t = (s0 * HPW + hl) / nh;
     int h = (int)((s0 * HPW + hl) % nh);
+    Vec16<T> v0, v1, v2, v3;
+    auto load = [&](long t, int h) {
+        const long at = (long)(first + h) * a.hd + j * V;
+        const T *xp = (const T *)a.x + t * a.xs + at, *dp = (const T *)a.dy + t * a.dys + at;
+        v0 = ldv(xp); v1 = ldv(xp + half); v2 = ldv(dp); v3 = ldv(dp + half);
+    };
+    const bool some = s0 < s1;
+    if (some && live && t < a.n) load(t, h);
+    int p = some && t < a.n ? a.pos[t] : -1;
     for (long st = s0; st < s1; ++st) {
         const bool mine = live && t < a.n;
         float xl[V], xh[V], yl[V], yh[V], ss = 0.f;
-        Vec16<T> v0, v1, v2, v3;
-        const long at = (long)(first + h) * a.hd + j * V;
-        if (mine) {
-            const T *xp = (const T *)a.x + t * a.xs + at, *dp = (const T *)a.dy + t * a.dys + at;
-            v0 = ldv(xp); v1 = ldv(xp + half); v2 = ldv(dp); v3 = ldv(dp + half);
-        }
+        const long at = (long)(first + h) * a.hd + j * V, now = t;
         float c[V], s[V];
-        load_angles<V>(a, t < a.n ? a.pos[t] : -1, j * V, live, c, s);
+        load_angles<V>(a, p, j * V, live, c, s);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             xl[e] = mine ? to_f32(v0.v[e]) : 0.f; xh[e] = mine ? to_f32(v1.v[e]) : 0.f;
@@ -155,6 +159,11 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
             ss = __builtin_fmaf(xl[e], xl[e], ss);
             ss = __builtin_fmaf(xh[e], xh[e], ss);
         }
+        h += dh; t += dt;                                // the next heads are on their way while these are worked on
+        if (h >= nh) { h -= nh; ++t; }
+        const bool more = st + 1 < s1 && t < a.n;
+        if (more && live) load(t, h);
+        p = more ? a.pos[t] : -1;
         ss = group_sum<G>(ss);
         const float r = mine ? rsqrtf(ss * inv_hd + a.eps) : 0.f;
         float m = 0.f;
@@ -176,12 +185,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
                 ol.v[e] = from_f32<T>(__builtin_fmaf(-xl[e], m, yl[e]));
                 oh.v[e] = from_f32<T>(__builtin_fmaf(-xh[e], m, yh[e]));
             }
-            T *o = (T *)a.out + t * a.os + at;
+            T *o = (T *)a.out + now * a.os + at;
             stv(o, ol);
             stv(o + half, oh);
         }
-        h += dh; t += dt;
-        if (h >= nh) { h -= nh; ++t; }
     }
     // heads of the wave, then waves, in a fixed order
     __shared__ float red[4][2 * G * V];
