@@ -15,13 +15,14 @@
 // are computed so.  An fp32 result is computed on v_mfma_f32_16x16x32_bf16 instead, half the rate, from the codes widened to bf16 (exact): fp32
 // sums throughout; unless the caller asks for the fast ones.
 //
-//   * gemm_fp8_pp_kernel: 256 tokens x 256 outputs, operands through LDS, two wave groups that take turns;
+//   * gemm_fp8_big_kernel: 256 tokens x 256 outputs, operands through LDS;
 //   * gemm_fp8_ring_kernel: smaller tiles through LDS, for grids that do not fill the chip with the large one, and fp32 results;
 //   * gemm_fp8_direct_kernel: up to 64 tokens, fragments straight from global memory, K split over the waves of a workgroup.
 // All but the last add up K in ascending order, one accumulator per output, so they give the same bits.
 #include <atomic>
 #include <utility>
 
+#include "fp8_plan.h"
 #include "fp8_quantize.h"
 #include "launch.h"
 #include "launch_plan.h"
@@ -48,12 +49,13 @@ struct Fp8Params {
     int kb, tiles_m, tiles_n;
 };
 
-__device__ __forceinline__ f32x4 mfma(const i32x8 &w, const i32x8 &a, const f32x4 &c, int sw, int sa, std::integral_constant<int, 0>) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, sw, 0, sa);
+// W, A: which byte of sw, sa has the exponents
+template <int W, int A> __device__ __forceinline__ f32x4 mfma(const i32x8 &w, const i32x8 &a, const f32x4 &c, int sw, int sa) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, W, sw, A, sa);
 }
-__device__ __forceinline__ f32x4 mfma(const i32x8 &w, const i32x8 &a, const f32x4 &c, int sw, int sa, std::integral_constant<int, 1>) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 1, sw, 1, sa);
-}
+// f(0), f(1), ... with the index as a constant
+template <class F, int... I> __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F> __device__ __forceinline__ void each(F f) { each(std::make_integer_sequence<int, N>{}, f); }
 // The same in fp32 sums: 8 k of each lane at a time
 __device__ __forceinline__ bf16x8 widen8(int a, int b, float scale) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -114,96 +116,81 @@ template <int NV> __device__ __forceinline__ void store_row(const Fp8Params &p, 
 }
 
 // ------------------------------------------------------------------ up to 64 tokens
-// 16 MB tokens x 16 NI weight rows per workgroup; wave w takes the K tiles w, w + 8, ...: together the waves read 1 KB pieces of the rows.
+// 16 tokens x 16 NI weight rows per workgroup; wave w takes the K tiles w, w + 8, ...: together the waves read 1 KB pieces of the rows.
 // D tiles are requested before the first is used.  The weights stream from HBM and bound it; a token row is read again by every
-// workgroup, from L2.
+// workgroup, from L2.  us on cold weights, NI = 1 / 2 / 4: 4096 x 4096 5.3 / 6.3 / 9.7, 6144 x 4096 7.5 / 6.8 / 9.9, 22016 x 4096 19.1 / 18.6 / 26.4.
 constexpr int kDirectWaves = 8;
-template <int MB, int NI, int D, bool PRECISE>
+template <int NI, int D, bool PRECISE>
 __global__ __launch_bounds__(64 * kDirectWaves) void gemm_fp8_direct_kernel(Fp8Params p) {
     constexpr int COLS = 16 * NI, LDR = COLS + 4;
     __shared__ __align__(16) float red[kDirectWaves][16][LDR];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int m0 = blockIdx.y * 16 * MB;
+    const int m0 = blockIdx.y * 16;
     const long n0 = (long)blockIdx.x * COLS;
-    const long rows_w = p.N - n0 < COLS ? p.N - n0 : COLS, rows_a = p.M - m0 < 16 * MB ? p.M - m0 : 16 * MB;
+    const long rows_w = p.N - n0 < COLS ? p.N - n0 : COLS, rows_a = p.M - m0 < 16 ? p.M - m0 : 16;
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.W + n0 * p.ldw, (rows_w - 1) * p.ldw + p.K);
     const __amdgpu_buffer_rsrc_t ra = make_rsrc(p.A + (long)m0 * p.lda, (rows_a - 1) * p.lda + p.K);
     const uint8_t *sw_row = p.sW + n0 / kBlk * p.ldsw;                   // (a tile lies within one block of 128 rows)
-    unsigned wo[NI], ao[MB];
+    const uint8_t *sa_row = p.sA + (long)(m0 + (r < rows_a ? r : 0)) * p.ldsa;
+    unsigned wo[NI];
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
         const int row = 4 * NI * (r >> 2) + 4 * j + (r & 3);
-        wo[j] = row < rows_w ? (unsigned)(row * p.ldw + 32 * g) : kOob;
+        wo[j] = row < rows_w ? (unsigned)(row * p.ldw + 16 * g) : kOob;
     }
+    const unsigned ao = r < rows_a ? (unsigned)(r * p.lda + 16 * g) : kOob;
+    f32x4 acc[NI];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) ao[i] = 16 * i + r < rows_a ? (unsigned)((16 * i + r) * p.lda + 32 * g) : kOob;
-    f32x4 acc[MB][NI];
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NI; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int kt = wave; kt < p.kb; kt += kDirectWaves * D) {
-        i32x4 w[D][NI][2], a[D][MB][2];
-        int sa[D][MB], sw[D];
+        i32x4 w[D][NI][2], a[D][2];
+        int sa[D], sw[D];
 #pragma unroll
         for (int u = 0; u < D; ++u) {
             const int t = kt + u * kDirectWaves;
-            const bool in = t < p.kb;
+            const bool in = t < p.kb;                                    // a tile past the end: zeros, scaled by 1
             const int k0 = in ? t * kBlk : 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const unsigned inv = in && k0 + 32 * g + 16 * h < p.K ? 0u : kOob;      // (K is a multiple of 16)
+                const unsigned inv = in && k0 + 16 * g + 64 * h < p.K ? 0u : kOob;      // (K is a multiple of 16)
 #pragma unroll
-                for (int j = 0; j < NI; ++j) w[u][j][h] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(rw, (wo[j] + 16 * h) | inv, k0, 0);
-#pragma unroll
-                for (int i = 0; i < MB; ++i) a[u][i][h] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(ra, (ao[i] + 16 * h) | inv, k0, 0);
+                for (int j = 0; j < NI; ++j) w[u][j][h] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(rw, (wo[j] + 64 * h) | inv, k0, 0);
+                a[u][h] = (i32x4)__builtin_amdgcn_raw_buffer_load_b128(ra, (ao + 64 * h) | inv, k0, 0);
             }
             sw[u] = in ? sw_row[t] : 127;
-#pragma unroll
-            for (int i = 0; i < MB; ++i) sa[u][i] = in && 16 * i + r < rows_a ? p.sA[(long)(m0 + 16 * i + r) * p.ldsa + t] : 127;
+            sa[u] = in && r < rows_a ? sa_row[t] : 127;
         }
 #pragma unroll
         for (int u = 0; u < D; ++u) {
             if constexpr (PRECISE) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    bf16x8 x[MB];
+                    const bf16x8 x = widen8(a[u][q >> 1][2 * (q & 1)], a[u][q >> 1][2 * (q & 1) + 1], scale_of(sa[u]));
 #pragma unroll
-                    for (int i = 0; i < MB; ++i) x[i] = widen8(a[u][i][q >> 1][2 * (q & 1)], a[u][i][q >> 1][2 * (q & 1) + 1], scale_of(sa[u][i]));
-#pragma unroll
-                    for (int j = 0; j < NI; ++j) {
-                        const bf16x8 y = widen8(w[u][j][q >> 1][2 * (q & 1)], w[u][j][q >> 1][2 * (q & 1) + 1], scale_of(sw[u]));
-#pragma unroll
-                        for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x[i], acc[i][j], 0, 0, 0);
-                    }
+                    for (int j = 0; j < NI; ++j)
+                        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[u][j][q >> 1][2 * (q & 1)], w[u][j][q >> 1][2 * (q & 1) + 1], scale_of(sw[u])), x,
+                                                                         acc[j], 0, 0, 0);
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < MB; ++i)
-#pragma unroll
-                    for (int j = 0; j < NI; ++j)
-                        acc[i][j] = mfma(join(w[u][j][0], w[u][j][1]), join(a[u][i][0], a[u][i][1]), acc[i][j], sw[u], sa[u][i], std::integral_constant<int, 0>{});
+                for (int j = 0; j < NI; ++j) acc[j] = mfma<0, 0>(join(w[u][j][0], w[u][j][1]), join(a[u][0], a[u][1]), acc[j], sw[u], sa[u]);
             }
         }
     }
 #pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        if (i) __syncthreads();
+    for (int j = 0; j < NI; ++j) *(f32x4 *)&red[wave][r][4 * NI * g + 4 * j] = acc[j];
+    __syncthreads();
+    if (tid < 16 * COLS) {
+        const int ml = tid / COLS, nl = tid % COLS;
+        float s = 0.f;
 #pragma unroll
-        for (int j = 0; j < NI; ++j) *(f32x4 *)&red[wave][r][4 * NI * g + 4 * j] = acc[i][j];
-        __syncthreads();
-        for (int idx = tid; idx < 16 * COLS; idx += 64 * kDirectWaves) {
-            const int ml = idx / COLS, nl = idx % COLS;
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < kDirectWaves; ++w) s += red[w][ml][nl];
-            const long m = m0 + 16 * i + ml, n = n0 + nl;
-            if (m < p.M && n < p.N) {
-                if (p.R) s += p.r_fp32 ? ((const float *)p.R)[m * p.ldr + n] : to_f32(((const bf16_t *)p.R)[m * p.ldr + n]);
-                if (p.c_fp32) ((float *)p.C)[m * p.ldc + n] = s;
-                else ((bf16_t *)p.C)[m * p.ldc + n] = from_f32<bf16_t>(s);
-            }
+        for (int w = 0; w < kDirectWaves; ++w) s += red[w][ml][nl];
+        const long m = m0 + ml, n = n0 + nl;
+        if (m < p.M && n < p.N) {
+            if (p.R) s += p.r_fp32 ? ((const float *)p.R)[m * p.ldr + n] : to_f32(((const bf16_t *)p.R)[m * p.ldr + n]);
+            if (p.c_fp32) ((float *)p.C)[m * p.ldc + n] = s;
+            else ((bf16_t *)p.C)[m * p.ldc + n] = from_f32<bf16_t>(s);
         }
     }
 }
@@ -217,10 +204,11 @@ __device__ __forceinline__ int piece_off(int row, int piece) { return row * kBlk
 template <int NI> __device__ __forceinline__ int weight_row_lane(int lr) { return 4 * NI * (lr >> 2) + (lr & 3); }
 template <int NI> __device__ __forceinline__ int weight_row_group(int lg) { return 8 * NI * (lg & 1) + 4 * (lg >> 1); }
 
-// Scales of a workgroup's BM tokens and BN / 128 weight blocks for up to kPanel K tiles from tile t0 on, as pairs of K tiles: one 16-bit word
-// per pair and row.  Tiles past the end get 1: their codes arrive as zeros, and a scale may not turn those into NaN.
-template <int BM, int NW, int THREADS>
-__device__ __forceinline__ void stage_scales(const Fp8Params &p, uint16_t *pa, uint16_t *pw, int m0, const int *wblk, int t0, int nt, int tid) {
+// Scales of a workgroup's BM tokens and NW weight blocks for up to kPanel K tiles from tile t0 on.  pa: per K tile the bytes of the G fragment
+// blocks that a wave works on together, side by side, for each of their 16 rows: one read gets a lane's scales.  Tiles past the end get 1: their codes
+// arrive as zeros, and a scale may not turn those into NaN.
+template <int BM, int G, int NW, int THREADS>
+__device__ __forceinline__ void stage_scales(const Fp8Params &p, uint8_t *pa, uint8_t *pw, int m0, const int *wblk, int t0, int nt, int tid) {
     const int words = (nt + 3) >> 2;                     // four K tiles each
     for (int i = tid; i < words * (BM + NW); i += THREADS) {
         const int row = i / words, q = i % words, t = t0 + 4 * q;
@@ -232,9 +220,12 @@ __device__ __forceinline__ void stage_scales(const Fp8Params &p, uint16_t *pa, u
         }
         const int left = p.kb - t;
         if (left < 4) v = (v & ((1u << (8 * left)) - 1)) | (0x7f7f7f7fu << (8 * left));
-        uint16_t *d = row < BM ? pa + (2 * q) * BM + row : pw + (2 * q) * NW + row - BM;
-        d[0] = (uint16_t)v;
-        d[row < BM ? BM : NW] = (uint16_t)(v >> 16);
+        const int step = row < BM ? BM : NW;
+        uint8_t *d = row < BM ? pa + 4 * q * BM + (row / (16 * G) * 16 + row % 16) * G + row / 16 % G : pw + 4 * q * NW + row - BM;
+        d[0] = (uint8_t)v;
+        d[step] = (uint8_t)(v >> 8);
+        d[2 * step] = (uint8_t)(v >> 16);
+        d[3 * step] = (uint8_t)(v >> 24);
     }
 }
 
@@ -288,15 +279,20 @@ __device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 
     }
 }
 
-// 256 x 256 tile, two wave groups that take turns on the matrix cores: the arrangement of gemm_bf16_pp_kernel (gemm.hip) with a K tile of
-// 128 codes in the same 128-byte LDS rows and one MFMA where that has two.  "A" is the token operand (two halves of 128 rows), "B" the
-// weights (half h = blocks 2 h and 2 h + 1 of every wave column; SwiGLU: gate and up).
-struct Fp8Lds { uint8_t *a[2][2], *b[2][2]; };
+// 256 x 256 tile: eight waves (two per SIMD, which fill each other's gaps), wave tile 128 tokens x 64 outputs as four quarters (token half, weight half).
+//   * The quarters follow (A0 F)(A0 S)(A1 S)(A1 F), F / S = the weight half used first / second, which swap roles every K tile: one operand
+//     half changes at a time.  The fragments of A0 are replaced by those of A1 one by one, each behind the last MFMAs that read it, A1's by
+//     the next tile's A0; S is free in the last quarter, F in the first: 64 registers of fragments serve without a second set.
+//   * An operand tile is two halves of 128 rows with an LDS slot each and two stages: eight 16 KB slots.  Two barriers per K tile, in the
+//     first and third quarters behind half of their MFMAs, when the reads before them are long done; each hands over the slots that
+//     have been read, to loads of K tile t + 2, and what has landed: every half is requested 1.5 K tiles before it is read, and the
+//     waits are for all but the 8 youngest loads of a wave.
+//   * Half h of the weights is blocks 2 h and 2 h + 1 of every wave column; with SwiGLU gate and up.
 template <bool SWIGLU, bool TAIL>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_fp8_pp_kernel(Fp8Params p) {
+__device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     constexpr int HS = 128 * kBlk;
     __shared__ __align__(16) uint8_t A00[HS], A01[HS], A10[HS], A11[HS], B00[HS], B01[HS], B10[HS], B11[HS];
-    __shared__ __align__(16) uint16_t pa[kPanel / 2 * 256], pw[kPanel / 2 * 2];
+    __shared__ __align__(16) uint8_t pa[kPanel * 256], pw[kPanel * 2];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane >> 3;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 2, wn = wave & 3;
@@ -306,29 +302,39 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const __amdgpu_buffer_rsrc_t ra = make_rsrc(p.A + (long)m0 * p.lda, (rows_a - 1) * p.lda + p.K);
     const __amdgpu_buffer_rsrc_t rb = make_rsrc(p.W + (long)n0 * p.ldw, (rows_b - 1) * p.ldw + p.K);
     const int x = (lane & 7) ^ swz_row(lr);
-    const unsigned alane = (unsigned)(lr * p.lda), blane = (unsigned)(weight_row_lane<SWIGLU ? 2 : 4>(lr) * p.ldw);
     const unsigned lda = (unsigned)p.lda, ldw = (unsigned)p.ldw;
-    int kt0 = 0, nk = 0;                                 // first K tile of the panel and their number
+    int piece[2];                                        // of a wave's two 8-row groups: the lane's piece, its part of the offsets
+    unsigned al[2], bl[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        piece[i] = x ^ swz_row(8 * (wave * 2 + i));
+        al[i] = (unsigned)lr * lda + (piece[i] << 4);
+        bl[i] = (unsigned)weight_row_lane<SWIGLU ? 2 : 4>(lr) * ldw + (piece[i] << 4);
+    }
+    const int nk = p.kb;
+    int base = 0;                                        // first K tile of the panel of scales
     auto invalid = [&](int kt, int piece) __attribute__((always_inline)) {
         unsigned inv = kt < nk ? 0u : kOob;
-        if (TAIL) inv |= (kt0 + kt) * kBlk + piece * 16 < p.K ? 0u : kOob;
+        if (TAIL) inv |= kt * kBlk + piece * 16 < p.K ? 0u : kOob;
         return inv;
     };
+    // request half h of K tile kt (two loads per wave; a tile past the end arrives as zeros)
     auto fetch_a = [&](int kt, int h, uint8_t *slot) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int lg = wave * 2 + i, piece = x ^ swz_row(8 * lg);
-            const unsigned voff = (alane + (unsigned)(h * 128 + lg * 8) * lda + (piece << 4)) | invalid(kt, piece);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(slot + lg * 8 * kBlk), 16, voff, kt < nk ? (kt0 + kt) * kBlk : 0, 0, 0);
+            const int lg = wave * 2 + i;
+            unsigned row = (unsigned)(h * 128 + lg * 8) * lda;
+            asm volatile("" : "+s"(row));                // (kept out of the lane's registers: eight sums of the two would stay there for the whole loop)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(slot + lg * 8 * kBlk), 16, (al[i] + row) | invalid(kt, piece[i]), kt < nk ? kt * kBlk : 0, 0, 0);
         }
     };
     auto fetch_b = [&](int kt, int h, uint8_t *slot) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int lg = wave * 2 + i, piece = x ^ swz_row(8 * lg), w = lg >> 2;
-            const unsigned row = SWIGLU ? (unsigned)(h * p.F + w * 32 + weight_row_group<2>(lg & 3)) : (unsigned)(w * 64 + weight_row_group<4>((lg & 3) + 4 * h));
-            const unsigned voff = (blane + row * ldw + (piece << 4)) | invalid(kt, piece);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(slot + lg * 8 * kBlk), 16, voff, kt < nk ? (kt0 + kt) * kBlk : 0, 0, 0);
+            const int lg = wave * 2 + i, w = lg >> 2;
+            unsigned row = (SWIGLU ? (unsigned)(h * p.F + w * 32 + weight_row_group<2>(lg & 3)) : (unsigned)(w * 64 + weight_row_group<4>((lg & 3) + 4 * h))) * ldw;
+            asm volatile("" : "+s"(row));
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(slot + lg * 8 * kBlk), 16, (bl[i] + row) | invalid(kt, piece[i]), kt < nk ? kt * kBlk : 0, 0, 0);
         }
     };
 
@@ -337,9 +343,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    i32x8 af[4], ax[2], bf[4];                           // blocks 1 .. 3 of the present A half (af[0] unused), block 0 of each; weights
-    int sa[8], sw = 0;
-    int fo[2][2];                                        // [block parity][piece g / 4 + g] within a 64-row (A) piece
+    i32x8 af[4], bf[4];                                  // the present token half's blocks; weights
+    int sa[2], sw = 0;                                   // scales: a byte for each of a token half's four blocks; of the weights (SwiGLU: gate, up)
+    int fo[2][2];                                        // [block parity][piece g / 4 + g]
     const int r16 = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int par = 0; par < 2; ++par)
@@ -349,95 +355,99 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const uint8_t *s = slot + (row0 + blk * 16) * kBlk;
         return join(*(const i32x4 *)(s + fo[blk & 1][0]), *(const i32x4 *)(s + fo[blk & 1][1]));
     };
-    auto read_a_first = [&](auto half, const uint8_t *slot) __attribute__((always_inline)) { ax[decltype(half)::value] = frag(slot, wm * 64, 0); };
-    auto read_a_rest = [&](const uint8_t *slot) __attribute__((always_inline)) {
-#pragma unroll
-        for (int b = 1; b < 4; ++b) af[b] = frag(slot, wm * 64, b);
-    };
     auto read_b = [&](auto half, const uint8_t *slot) __attribute__((always_inline)) {
         constexpr int h = decltype(half)::value;
         bf[2 * h] = frag(slot, wn * 32, 0);
         bf[2 * h + 1] = frag(slot, wn * 32, 1);
     };
-    // scales of half h's tokens (and the weights') for the pair of K tiles from kt on
     auto read_sa = [&](auto half, int kt) __attribute__((always_inline)) {
         constexpr int h = decltype(half)::value;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) sa[4 * h + b] = pa[(kt >> 1) * 256 + h * 128 + wm * 64 + b * 16 + r16];
+        sa[h] = *(const int *)(pa + (kt - base) * 256 + ((h * 2 + wm) * 16 + r16) * 4);
     };
-    int sw_next = 0;
-    auto read_sw = [&](int kt) __attribute__((always_inline)) { sw_next = pw[(kt >> 1) * 2 + (SWIGLU ? 0 : wn >> 1)]; };
-    // (SwiGLU: gate and up rows have scales of their own; their second block lies F rows on)
-    int su = 0, su_next = 0;
-    auto turn = [&](auto ah, auto bh, auto op) __attribute__((always_inline)) {
-        constexpr int h = decltype(ah)::value, gg = decltype(bh)::value;
-        __builtin_amdgcn_sched_barrier(0);
-        wait_vmcnt_lgkm0<10>();
-        lds_barrier();
-        __builtin_amdgcn_sched_barrier(0);
+    auto weight_scale = [&](int kt) __attribute__((always_inline)) -> int {
+        if (SWIGLU) return *(const uint16_t *)(pw + kt * 2);
+        return pw[kt * 2 + (wn >> 1)];
+    };
+    auto mul = [&](auto ah, auto bh, auto block) __attribute__((always_inline)) {
+        constexpr int h = decltype(ah)::value, q = decltype(bh)::value, b = decltype(block)::value;
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-                acc[4 * h + b][2 * gg + c] = mfma(bf[2 * gg + c], b == 0 ? ax[h] : af[b], acc[4 * h + b][2 * gg + c], SWIGLU && gg ? su : sw, sa[4 * h + b], op);
+        for (int c = 0; c < 2; ++c)
+            acc[4 * h + b][2 * q + c] = mfma<SWIGLU ? q : 0, b>(bf[2 * q + c], af[b], acc[4 * h + b][2 * q + c], sw, sa[h]);
+    };
+    auto hand_over = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
+        wait_vmcnt_lgkm0<8>();
         lds_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
     using I0 = std::integral_constant<int, 0>;
     using I1 = std::integral_constant<int, 1>;
-    // K tile kt (parity = F = its first B half) in stage slots a0, a1, f, s; nb / na: the next tile's first halves
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+    // K tile kt (parity = fh = its first weight half) in stage slots a0, a1, f, s; nb / na: the next tile's first halves
     auto tile = [&](int kt, auto F, uint8_t *a0, uint8_t *a1, uint8_t *f, uint8_t *s, const uint8_t *nb, const uint8_t *na) __attribute__((always_inline)) {
         constexpr int fh = decltype(F)::value;
         using FH = std::integral_constant<int, fh>;
         using SH = std::integral_constant<int, 1 - fh>;
-        read_a_rest(a0);
-        if (fh == 0) read_sa(I1{}, kt);
-        fetch_b(kt + 2, fh, f);
-        turn(I0{}, FH{}, FH{});
+        mul(I0{}, FH{}, I0{});
+        mul(I0{}, FH{}, I1{});
+        hand_over();                                     // a0 and f have been read; a1 and s have landed
         read_b(SH{}, s);
-        read_a_first(I1{}, a1);
+        read_sa(I1{}, kt);
+        mul(I0{}, FH{}, I2{});
+        fetch_b(kt + 2, fh, f);
+        mul(I0{}, FH{}, I3{});
         fetch_a(kt + 2, 0, a0);
-        turn(I0{}, SH{}, FH{});
-        read_a_rest(a1);
-        if (fh == 1) read_sa(I0{}, kt + 1);              // (the panel has a pair more than the tiles need)
+        __builtin_amdgcn_sched_barrier(0);
+        each<4>([&](auto b) __attribute__((always_inline)) {
+            mul(I0{}, SH{}, b);
+            __builtin_amdgcn_sched_barrier(0);
+            af[b] = frag(a1, wm * 64, b);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        mul(I1{}, SH{}, I0{});
+        mul(I1{}, SH{}, I1{});
+        hand_over();                                     // a1 and s have been read; the next tile's first halves have landed
+        read_sa(I0{}, kt + 1);
+        const int sw1 = weight_scale(kt + 1 - base);
+        mul(I1{}, SH{}, I2{});
         fetch_b(kt + 2, 1 - fh, s);
-        turn(I1{}, SH{}, FH{});
-        read_b(SH{}, nb);
-        read_a_first(I0{}, na);
-        if (fh == 1) {
-            read_sw(kt + 1);
-            if (SWIGLU) su_next = pw[((kt + 1) >> 1) * 2 + 1];
-        }
+        mul(I1{}, SH{}, I3{});
         fetch_a(kt + 2, 1, a1);
-        turn(I1{}, FH{}, FH{});
-        if (fh == 1) { sw = sw_next; su = su_next; }
+        __builtin_amdgcn_sched_barrier(0);
+        read_b(SH{}, nb);
+        each<4>([&](auto b) __attribute__((always_inline)) {
+            mul(I1{}, FH{}, b);
+            __builtin_amdgcn_sched_barrier(0);
+            af[b] = frag(na, wm * 64, b);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        sw = sw1;
     };
     int wblk[2];
     if (SWIGLU) { wblk[0] = n0 / kBlk; wblk[1] = (p.F + n0) / kBlk; }
     else { wblk[0] = n0 / kBlk; wblk[1] = (n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk; }
-    for (; kt0 < p.kb; kt0 += kSegment) {
-        nk = p.kb - kt0 < kSegment ? p.kb - kt0 : kSegment;
-        fetch_b(0, 0, B00); fetch_a(0, 0, A00); fetch_b(0, 1, B01); fetch_a(0, 1, A01);
-        fetch_b(1, 1, B11); fetch_a(1, 0, A10); fetch_b(1, 0, B10); fetch_a(1, 1, A11);
-        stage_scales<256, 2, 512>(p, pa, pw, m0, wblk, kt0, nk, tid);
-        wait_vmcnt_lgkm0<0>();
-        lds_barrier();
-        read_b(I0{}, B00);
-        read_a_first(I0{}, A00);
-        read_sa(I0{}, 0);
-        sw = SWIGLU ? pw[0] : pw[wn >> 1];
-        su = pw[1];
-        wait_vmcnt_lgkm0<10>();
-        lds_barrier();
-        if (wm == 1) lds_barrier();
-        for (int kt = 0; kt < nk; kt += 2) {             // an odd count is rounded up with a tile of zeros
-            tile(kt, I0{}, A00, A01, B00, B01, B11, A10);
-            tile(kt + 1, I1{}, A10, A11, B11, B10, B00, A00);
+    fetch_b(0, 0, B00); fetch_a(0, 0, A00); fetch_b(0, 1, B01); fetch_a(0, 1, A01);           // in the loop's order
+    fetch_b(1, 1, B11); fetch_a(1, 0, A10); fetch_b(1, 0, B10); fetch_a(1, 1, A11);
+    stage_scales<256, 4, 2, 512>(p, pa, pw, m0, wblk, 0, nk < kPanel ? nk : kPanel, tid);
+    wait_vmcnt_lgkm0<12>();
+    lds_barrier();
+    read_b(I0{}, B00);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) af[b] = frag(A00, wm * 64, b);
+    read_sa(I0{}, 0);
+    sw = weight_scale(0);
+    for (int kt = 0; kt < nk; kt += 2) {                 // an odd count is rounded up with a tile of zeros
+        if (kt - base == kSegment) {                     // the next panel of scales (this tile's first ones have been read from the old one, which goes further)
+            base = kt;
+            __syncthreads();
+            stage_scales<256, 4, 2, 512>(p, pa, pw, m0, wblk, base, nk - base < kPanel ? nk - base : kPanel, tid);
+            __syncthreads();
         }
-        if (wm == 0) lds_barrier();
-        dma_publish_barrier();                           // what is still in flight must land before LDS is used again
+        tile(kt, I0{}, A00, A01, B00, B01, B11, A10);
+        tile(kt + 1, I1{}, A10, A11, B11, B10, B00, A00);
     }
+    dma_publish_barrier();                               // what is still in flight must land before LDS is used again
     const int mrow = m0 + wm * 64 + r16;
     if constexpr (!SWIGLU) {
 #pragma unroll
@@ -453,6 +463,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         swiglu_epilogue<8, 256>(p, acc, (unsigned *)A00, m0, n0, wn, g, [&](int i) { return wm * 64 + (i >> 2) * 128 + (i & 3) * 16 + r16; });
     }
 }
+template <bool SWIGLU, bool TAIL>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_fp8_big_kernel(Fp8Params p) { fp8_big_body<SWIGLU, TAIL>(p); }
+
+// Scheduling pattern: R LDS reads and V loads dealt to the first half of the MFMAs
+template <int R, int V, int... I> __device__ __forceinline__ void spread_over_mfmas(std::integer_sequence<int, I...>) {
+    constexpr int H = (int)sizeof...(I) / 2, RP = (R + H - 1) / H, VP = (V + H - 1) / H;
+    ((__builtin_amdgcn_sched_group_barrier(0x008, 1, 0), I < H ? __builtin_amdgcn_sched_group_barrier(0x100, RP, 0) : (void)0,
+      I < H ? __builtin_amdgcn_sched_group_barrier(0x020, VP, 0) : (void)0), ...);
+}
 
 // The tile template's LDS stages as objects of their own (mfma_tiles.h, FastLds in gemm.hip, on why)
 template <int BM, int BN, int WM, int WN, int NST, bool SWIGLU, bool PRECISE>
@@ -464,7 +483,7 @@ __device__ __forceinline__ void fp8_ring_body(const Fp8Params &p) {
     constexpr bool RING = NST == 4;
     __shared__ __align__(16) uint8_t A0[BM * kBlk], A1[BM * kBlk], A2[RING ? BM * kBlk : 16], A3[RING ? BM * kBlk : 16];
     __shared__ __align__(16) uint8_t B0[BN * kBlk], B1[BN * kBlk], B2[RING ? BN * kBlk : 16], B3[RING ? BN * kBlk : 16];
-    __shared__ __align__(16) uint16_t pa[kPanel / 2 * BM], pw[kPanel / 2 * NB];
+    __shared__ __align__(16) uint8_t pa[kPanel * BM], pw[kPanel * NB];
     uint8_t *const As[4] = {A0, A1, A2, A3}, *const Bs[4] = {B0, B1, B2, B3};
     const int tid = threadIdx.x, lane = tid & 63, lr = lane >> 3, r16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
@@ -499,59 +518,72 @@ __device__ __forceinline__ void fp8_ring_body(const Fp8Params &p) {
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int arow = wm * MI * 16, brow = wn * NI * 16;
     auto piece_of = [&](const uint8_t *tile, int row, int q) __attribute__((always_inline)) { return *(const i32x4 *)(tile + piece_off(row + r16, q * 4 + g)); };
-    int sa[MI], sw = 0, su = 0;
-    auto step = [&](auto parity, int kt, const uint8_t *as, const uint8_t *bs) __attribute__((always_inline)) {
+    // fragments and scales of a K tile, two sets: the next tile's are read while the matrix cores work on the present one
+    i32x4 a[2][MI][2], b[2][NI][2];
+    int sa[2], sw[2];                                    // (sa: a byte per token block, sw: SwiGLU: gate and up)
+    using word = std::conditional_t<MI == 4, int, std::conditional_t<MI == 2, uint16_t, uint8_t>>;
+    auto read = [&](auto parity, int kt, const uint8_t *as, const uint8_t *bs) __attribute__((always_inline)) {
         constexpr int par = decltype(parity)::value;
-        if (par == 0) {                                  // scales of two K tiles
 #pragma unroll
-            for (int i = 0; i < MI; ++i) sa[i] = pa[(kt >> 1) * BM + arow + i * 16 + r16];
-            sw = pw[(kt >> 1) * NB + (!SWIGLU && NB == 2 ? wn * 16 * NI / kBlk : 0)];
-            if (SWIGLU) su = pw[(kt >> 1) * NB + 1];
-        }
-        i32x4 a[MI][2], b[NI][2];
+        for (int j = 0; j < NI; ++j) { b[par][j][0] = piece_of(bs, brow + j * 16, 0); b[par][j][1] = piece_of(bs, brow + j * 16, 1); }
 #pragma unroll
-        for (int j = 0; j < NI; ++j) { b[j][0] = piece_of(bs, brow + j * 16, 0); b[j][1] = piece_of(bs, brow + j * 16, 1); }
-#pragma unroll
-        for (int i = 0; i < MI; ++i) { a[i][0] = piece_of(as, arow + i * 16, 0); a[i][1] = piece_of(as, arow + i * 16, 1); }
+        for (int i = 0; i < MI; ++i) { a[par][i][0] = piece_of(as, arow + i * 16, 0); a[par][i][1] = piece_of(as, arow + i * 16, 1); }
+        sa[par] = *(const word *)(pa + kt * BM + (wm * 16 + r16) * MI);
+        if (SWIGLU) sw[par] = *(const uint16_t *)(pw + kt * NB);
+        else sw[par] = pw[kt * NB + (NB == 2 ? wn * 16 * NI / kBlk : 0)];
+    };
+    auto step = [&](auto parity) __attribute__((always_inline)) {
+        constexpr int par = decltype(parity)::value;
         if constexpr (PRECISE) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 bf16x8 y[NI];
 #pragma unroll
-                for (int j = 0; j < NI; ++j) y[j] = widen8(b[j][q >> 1][2 * (q & 1)], b[j][q >> 1][2 * (q & 1) + 1], scale_of(sw >> (8 * par)));
+                for (int j = 0; j < NI; ++j) y[j] = widen8(b[par][j][q >> 1][2 * (q & 1)], b[par][j][q >> 1][2 * (q & 1) + 1], scale_of(sw[par]));
 #pragma unroll
                 for (int i = 0; i < MI; ++i) {
-                    const bf16x8 v = widen8(a[i][q >> 1][2 * (q & 1)], a[i][q >> 1][2 * (q & 1) + 1], scale_of(sa[i] >> (8 * par)));
+                    const bf16x8 v = widen8(a[par][i][q >> 1][2 * (q & 1)], a[par][i][q >> 1][2 * (q & 1) + 1], scale_of(sa[par] >> (8 * i)));
 #pragma unroll
                     for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[j], v, acc[i][j], 0, 0, 0);
                 }
             }
         } else {
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j)
-                    acc[i][j] = mfma(join(b[j][0], b[j][1]), join(a[i][0], a[i][1]), acc[i][j], SWIGLU && j >= NI / 2 ? su : sw, sa[i], parity);
+            each<MI>([&](auto block) __attribute__((always_inline)) {
+                constexpr int i = decltype(block)::value;
+                each<NI>([&](auto col) __attribute__((always_inline)) {
+                    constexpr int j = decltype(col)::value;
+                    acc[i][j] = mfma<SWIGLU && j >= NI / 2, i>(join(b[par][j][0], b[par][j][1]), join(a[par][i][0], a[par][i][1]), acc[i][j], sw[par], sa[par]);
+                });
+            });
         }
     };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
     int wblk[2];
     wblk[0] = n0 / kBlk;
     wblk[1] = SWIGLU ? (p.F + n0) / kBlk : ((n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk);
     for (; kt0 < p.kb; kt0 += kSegment) {
         nk = p.kb - kt0 < kSegment ? p.kb - kt0 : kSegment;
 #pragma unroll
-        for (int k = 0; k < NST - 1; ++k) fetch(k, As[k], Bs[k]);
-        stage_scales<BM, NB, THREADS>(p, pa, pw, m0, wblk, kt0, nk, tid);
-        for (int kt = 0; kt < nk; kt += NST) {
+        for (int k = 0; k < NST; ++k) fetch(k, As[k], Bs[k]);
+        stage_scales<BM, MI, NB, THREADS>(p, pa, pw, m0, wblk, kt0, nk, tid);
+        wait_vmcnt_lgkm0<(NST - 1) * (LA + LB)>();
+        lds_barrier();
+        read(I0{}, 0, A0, B0);
+        for (int kt = 0; kt < nk; kt += NST) {           // rounded up with tiles of zeros: a single loop exit keeps the accumulators in place
 #pragma unroll
             for (int k = 0; k < NST; ++k) {
-                if (k > 0 && kt + k >= nk) break;
-                // this tile has landed (own loads, then everybody's); the stage that the new loads go to was read a tile ago
+                // the next tile has landed (own loads, then everybody's), and everybody has read this one: its stage takes new loads
                 wait_vmcnt_lgkm0<(NST - 2) * (LA + LB)>();
                 lds_barrier();
-                fetch(kt + k + NST - 1, As[(k + NST - 1) % NST], Bs[(k + NST - 1) % NST]);
-                if (k & 1) step(std::integral_constant<int, 1>{}, kt + k, As[k], Bs[k]);
-                else step(std::integral_constant<int, 0>{}, kt + k, As[k], Bs[k]);
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int kn[4] = {1, NST == 2 ? 0 : 2, 3, 0};
+                if (k & 1) read(I0{}, kt + k + 1, As[kn[k]], Bs[kn[k]]); else read(I1{}, kt + k + 1, As[kn[k]], Bs[kn[k]]);
+                fetch(kt + k + NST, As[k], Bs[k]);
+                if (k & 1) step(I1{}); else step(I0{});
+                // the reads and loads between the MFMAs, spread over the first of them
+                if constexpr (!PRECISE) spread_over_mfmas<2 * (MI + NI), LA + LB>(std::make_integer_sequence<int, MI * NI>{});
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         dma_publish_barrier();
@@ -585,6 +617,10 @@ MS_FP8_RING(64, 64, 4, 1, 4);
 template __global__ void gemm_fp8_ring_kernel<128, 256, 2, 4, 2, true, false>(Fp8Params);
 template __global__ void gemm_fp8_ring_kernel<64, 256, 2, 4, 2, true, false>(Fp8Params);
 #undef MS_FP8_RING
+template __global__ void gemm_fp8_big_kernel<false, false>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<false, true>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<true, false>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<true, true>(Fp8Params);
 
 bool aligned(const void *p, int to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
@@ -599,21 +635,16 @@ ms_status check(const char *who, int M, int N, int K, const void *A, long lda, c
     return MS_OK;
 }
 
-template <int MB, int NI, bool PRECISE> void launch_direct(const Fp8Params &p, hipStream_t s) {
-    gemm_fp8_direct_kernel<MB, NI, MB == 4 ? 1 : 2, PRECISE><<<dim3(ms_cdiv(p.N, 16 * NI), ms_cdiv(p.M, 16 * MB)), 64 * kDirectWaves, 0, s>>>(p);
+template <int NI, bool PRECISE> void launch_direct(const Fp8Params &p, hipStream_t s) {
+    // D = 4 where that requests no more tiles past the end than 2 does (4096 deep: 5.3 us against 6.1, 8960 deep 8.1 against 7.4)
+    const int t = ms_cdiv(p.kb, kDirectWaves);
+    const dim3 grid(ms_cdiv(p.N, 16 * NI), ms_cdiv(p.M, 16));
+    if ((t + 3) / 4 * 2 == (t + 1) / 2) gemm_fp8_direct_kernel<NI, 4, PRECISE><<<grid, 64 * kDirectWaves, 0, s>>>(p);
+    else gemm_fp8_direct_kernel<NI, 2, PRECISE><<<grid, 64 * kDirectWaves, 0, s>>>(p);
 }
 template <bool PRECISE> void launch_direct(const Fp8Params &p, hipStream_t s) {
-    const int ni = p.N >= 64 * 256 ? 4 : p.N >= 32 * 256 ? 2 : 1;
-#define GO(MB)                                                 \
-    do {                                                       \
-        if (ni == 4) launch_direct<MB, 4, PRECISE>(p, s);      \
-        else if (ni == 2) launch_direct<MB, 2, PRECISE>(p, s); \
-        else launch_direct<MB, 1, PRECISE>(p, s);              \
-    } while (0)
-    if (p.M <= 16) GO(1); else if (p.M <= 32) GO(2); else GO(4);
-#undef GO
+    if (p.N <= 4096 && p.M <= 16) launch_direct<1, PRECISE>(p, s); else launch_direct<2, PRECISE>(p, s);
 }
-
 // tiles of a launch, or 0 if they do not fit one
 int tiles_of(Fp8Params &p, int bm, int bn, int cols, int threads) {
     p.tiles_m = ms_cdiv(p.M, bm);
@@ -626,26 +657,16 @@ template <int BM, int BN, int WM, int WN, int NST, bool SWIGLU, bool PRECISE> bo
     if (tiles) gemm_fp8_ring_kernel<BM, BN, WM, WN, NST, SWIGLU, PRECISE><<<tiles, 64 * WM * WN, 0, s>>>(p);
     return tiles != 0;
 }
-template <bool SWIGLU> bool launch_pp(Fp8Params &p, hipStream_t s) {
+template <bool SWIGLU> bool launch_big(Fp8Params &p, hipStream_t s) {
     const int tiles = tiles_of(p, 256, SWIGLU ? 128 : 256, SWIGLU ? p.F : p.N, 512);
-    if (tiles && p.K % kBlk) gemm_fp8_pp_kernel<SWIGLU, true><<<tiles, 512, 0, s>>>(p);
-    else if (tiles) gemm_fp8_pp_kernel<SWIGLU, false><<<tiles, 512, 0, s>>>(p);
+    if (tiles && p.K % kBlk) gemm_fp8_big_kernel<SWIGLU, true><<<tiles, 512, 0, s>>>(p);
+    else if (tiles) gemm_fp8_big_kernel<SWIGLU, false><<<tiles, 512, 0, s>>>(p);
     return tiles != 0;
 }
 
 // The tile that measurements and tests ask for (0: by shape), as in ms_k_gemm_config
 std::atomic<int> g_tile{0};
 
-// Tile codes: token rows * 1000 + outputs, + 1 for the deeper ring of stages
-enum { F256 = 256256, F128 = 128128, F128R = 128129, F64x128 = 64128, F64x128R = 64129, F64 = 64064 };
-int choose(const Fp8Params &p, bool precise) {
-    const int forced = g_tile.load();
-    if (forced && !(precise && forced == F256)) return forced;
-    const long t256 = (long)ms_cdiv(p.M, 256) * ms_cdiv(p.N, 256);
-    if (!precise && t256 >= 192) return F256;
-    const long t128 = (long)ms_cdiv(p.M, 128) * ms_cdiv(p.N, 128);
-    return t128 >= 256 ? F128 : F64x128;
-}
 template <bool PRECISE> bool launch_tile(int tile, Fp8Params &p, hipStream_t s) {
     if (tile == F128) return launch_ring<128, 128, 2, 2, 2, false, PRECISE>(p, s);
     if (tile == F128R) return launch_ring<128, 128, 4, 2, 4, false, PRECISE>(p, s);
@@ -657,11 +678,12 @@ template <bool PRECISE> bool launch_tile(int tile, Fp8Params &p, hipStream_t s) 
 ms_status launch_gemm(Fp8Params p, bool precise, hipStream_t s) {
     ProfScope ps(0, 2.0 * p.M * p.N * p.K, s);
     bool fits = true;
-    if (p.M <= 64 && !g_tile.load()) {
+    const int forced = g_tile.load();
+    if (forced ? forced == FDIRECT : fp8_direct(p.M, p.N)) {
         if (precise) launch_direct<true>(p, s); else launch_direct<false>(p, s);
     } else {
-        const int tile = choose(p, precise);
-        fits = !precise && tile == F256 ? launch_pp<false>(p, s) : precise ? launch_tile<true>(tile, p, s) : launch_tile<false>(tile, p, s);
+        const int tile = forced && !(precise && forced == F256) ? forced : precise ? fp8_choose(kFp8Precise, p.M, p.N, p.kb) : fp8_choose(kFp8Fast, p.M, p.N, p.kb);
+        fits = !precise && tile == F256 ? launch_big<false>(p, s) : precise ? launch_tile<true>(tile, p, s) : launch_tile<false>(tile, p, s);
     }
     if (!fits) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8: %d x %d is too large for one launch", p.M, p.N);
     MS_LAUNCH_CHECK();
@@ -671,10 +693,8 @@ ms_status launch_gemm(Fp8Params p, bool precise, hipStream_t s) {
 // SwiGLU in the epilogue: gate and up rows of a tile's columns have to lie in whole blocks of 128 weight rows
 bool swiglu_fused(int M, int F, int K, long ldw) { return M > 64 && F % kBlk == 0 && ms_buffer_range_ok(2L * F, K, ldw, 1); }
 bool launch_swiglu(Fp8Params &p, hipStream_t s) {
-    const int forced = g_tile.load();
-    const long t256 = (long)ms_cdiv(p.M, 256) * ms_cdiv(p.F, 128), t128 = (long)ms_cdiv(p.M, 128) * ms_cdiv(p.F, 128);
-    const int tile = forced ? forced : t256 >= 192 ? F256 : t128 >= 192 ? F128 : F64x128;
-    if (tile == F256) return launch_pp<true>(p, s);
+    const int forced = g_tile.load(), tile = forced ? forced : fp8_choose(kFp8Swiglu, p.M, p.N, p.kb);
+    if (tile == F256) return launch_big<true>(p, s);
     if (tile == F128 || tile == F128R) return launch_ring<128, 256, 2, 4, 2, true, false>(p, s);
     return launch_ring<64, 256, 2, 4, 2, true, false>(p, s);
 }
@@ -682,7 +702,7 @@ bool launch_swiglu(Fp8Params &p, hipStream_t s) {
 }  // namespace
 
 extern "C" ms_status ms_k_gemm_fp8_config(int32_t tile) {
-    if (tile != 0 && tile != F256 && tile != F128 && tile != F128R && tile != F64x128 && tile != F64x128R && tile != F64)
+    if (tile != 0 && tile != F256 && tile != F128 && tile != F128R && tile != F64x128 && tile != F64x128R && tile != F64 && tile != FDIRECT)
         return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8_config: unknown tile %d", tile);
     g_tile = tile;
     return MS_OK;
