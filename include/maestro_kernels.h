@@ -86,7 +86,7 @@ ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *A, int64_t 
  * or 64064 = that tile for any number of rows (fp32 sums have no 256256; SwiGLU has 256, 128 and 64 rows). */
 ms_status ms_k_gemm_fp8_config(int32_t tile);
 /* Gate/up projection with SwiGLU and the next operand's quantisation: codes and scales of silu(A Wg^T) * (A Wu^T), W [2F, K] = gate rows,
- * then up rows; nothing in between is rounded.  F % 16 == 0.  scratch: ..._scratch_bytes(M, F, K) bytes (0: may be NULL), 16-byte aligned. */
+ * then up rows; nothing in between is rounded.  F % 16 == 0.  scratch: ..._scratch_bytes(M, F, K) bytes (not less for more rows), 16-byte aligned. */
 size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K);
 ms_status ms_k_gemm_fp8_swiglu(int32_t M, int32_t F, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W,
                                int64_t ldw, const void *sW, int64_t ldsw, void *q, int64_t ldq, void *scales, int64_t lds,
@@ -153,7 +153,7 @@ ms_status ms_k_embedding_scaled_forward(int32_t dtype, int32_t out_fp32, int32_t
                                         const int32_t *ids, const void *table, void *x, void *stream);
 /* d_table[v, :] += scale * sum over the tokens t with ids[t] == v of dx[t, :]  (fp32), the tokens sorted by id: every row's sum has
  * one order, so the same call gives the same bits (ms_k_embedding_backward adds with atomics).  Ids outside the table receive no
- * gradient.  At most 2^24 tokens.  scratch: 16-byte aligned, ..._scratch_bytes(n, d, vocab); contents are not kept. */
+ * gradient.  At most 2^24 tokens.  scratch: 16-byte aligned, ..._scratch_bytes(n, d, vocab) (not less for more tokens); contents are not kept. */
 size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_t d, int32_t vocab);
 ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, int32_t d, int32_t vocab, float scale, const int32_t *ids,
                                          const void *dx, float *d_table, void *scratch, size_t scratch_bytes, void *stream);

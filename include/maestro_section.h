@@ -143,6 +143,35 @@ ms_status ms_section_forward_backward(const ms_section_config *cfg, const ms_sec
                                       void *d_x_in, void *workspace_dev, size_t workspace_bytes,
                                       void *stream);
 
+/* Decoder sections with options; the calls are those above otherwise (options == NULL: exactly those).
+ *   embed_scale  the embedding rows times this number are the first layer's input (1: as they are)
+ *   qk_norm      != 0: every query and key head is RMSNormed before its rotation, with gains q_norm_g, k_norm_g [head_dim] of
+ *                `dtype` in each layer and the section's norm_eps; option_grads has their gradients (fp32, accumulated)
+ *   fp8          != 0: the matrices w_qkv, w_o, w_up, w_down are e4m3 codes with scale bytes s_qkv .. s_down for blocks of 128 x 128, as
+ *                ms_k_fp8_quantize(block_rows = 128) writes them without padding (rows of in codes, of ceil(in / 512) * 4 scale bytes); their inputs
+ *                are quantised in blocks of 128 columns.  Forward only, dtype MS_BF16; d_model and d_ffn multiples of 16
+ * The embedding gradient of a section with options adds up its tokens sorted by id, in one order: no atomics (ms_k_embedding_sorted_backward). */
+typedef struct {
+    void *q_norm_g, *k_norm_g;
+    const void *s_qkv, *s_o, *s_up, *s_down;
+} ms_layer_options;
+typedef struct {
+    float embed_scale;
+    int32_t qk_norm, fp8;
+    const ms_layer_options *layers;      /* host array of n_layers entries (NULL without qk_norm and fp8) */
+} ms_section_options;
+size_t ms_section_workspace_bytes_with(const ms_section_config *cfg, const ms_section_options *options, int32_t max_tokens,
+                                       int32_t max_seqlen, int32_t need_backward);
+ms_status ms_section_forward_with(const ms_section_config *cfg, const ms_section_options *options, const ms_section_ptrs *weights,
+                                  const ms_batch *batch, const void *x_in, void *h_out, void *workspace_dev,
+                                  size_t workspace_bytes, void *stream);
+ms_status ms_section_forward_backward_with(const ms_section_config *cfg, const ms_section_options *options,
+                                           const ms_layer_options *option_grads, const ms_section_ptrs *weights,
+                                           const ms_section_ptrs *grads, const ms_batch *batch, const void *x_in, void *h_out,
+                                           const void *d_h_out, const ms_kd_config *kd, const void *h_teacher,
+                                           void *d_w_student, float *loss_dev, float *kl_per_token_dev, void *d_x_in,
+                                           void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* Vocabulary-chunked lm_head + temperature softmax + KL(teacher || student) (Sec. 3.1,
  * Sec. 4.2).  Never holds more than [n_tokens, chunk] logits per model.
  *   p = softmax(h_teacher Wt^T / T), q = softmax(h_student Ws^T / T)

@@ -54,7 +54,7 @@ def lib():
         _lib = C.CDLL(LIB_PATH)
         _lib.ms_last_error.restype = C.c_char_p
         for name in ["ms_section_workspace_bytes", "ms_kd_workspace_bytes", "ms_k_norm_backward_scratch_bytes",
-                     "ms_k_attention_backward_scratch_bytes"]:
+                     "ms_k_attention_backward_scratch_bytes", "ms_section_workspace_bytes_with"]:
             getattr(_lib, name).restype = C.c_size_t
     return _lib
 
@@ -142,8 +142,70 @@ def workspace(nbytes, device="cuda", tag="default"):
     return buf
 
 
-def section_workspace_bytes(cfg, max_tokens, max_seqlen, need_backward):
+_OPTION_FIELDS = ["q_norm_g", "k_norm_g", "s_qkv", "s_o", "s_up", "s_down"]
+
+
+class LayerOptions(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in _OPTION_FIELDS]
+
+
+class SectionOptionsC(C.Structure):
+    _fields_ = [("embed_scale", C.c_float), ("qk_norm", C.c_int32), ("fp8", C.c_int32), ("layers", C.POINTER(LayerOptions))]
+
+
+class SectionOptions:
+    """Options of a decoder section: embed_scale; layers: one dict per layer with q_norm_g and k_norm_g ([head_dim], in the section's dtype) if
+    qk_norm, and the scale bytes s_qkv, s_o, s_up, s_down of the matrices' codes if fp8 (see quantize_section)."""
+
+    def __init__(self, embed_scale=1.0, qk_norm=False, fp8=False, layers=None):
+        self.embed_scale, self.qk_norm, self.fp8, self.layers = float(embed_scale), bool(qk_norm), bool(fp8), layers
+
+    def check(self, cfg):
+        if (self.qk_norm or self.fp8) and (self.layers is None or len(self.layers) != cfg.n_layers):
+            raise ValueError(f"section options: expected a dict for each of {cfg.n_layers} layers")
+        words = lambda k: (k + 511) // 512 * 4
+        rows = lambda n: (n + 127) // 128
+        d, a, f = cfg.d_model, cfg.n_q_heads * cfg.head_dim, cfg.d_ffn
+        for lo in self.layers or ():
+            for k in ("q_norm_g", "k_norm_g") if self.qk_norm else ():
+                _need(k, lo.get(k), (_tdt(cfg.dtype),), (cfg.head_dim,), None)
+            if self.fp8:
+                for k, n, kin in (("s_qkv", cfg.d_qkv, d), ("s_o", d, a), ("s_up", 2 * f, d), ("s_down", d, f)):
+                    _need(k, lo.get(k), (torch.uint8,), (rows(n), words(kin)), None)
+
+    def c(self, cfg):
+        o = SectionOptionsC(self.embed_scale, int(self.qk_norm), int(self.fp8), _layer_options(self.layers, cfg.n_layers))
+        return o
+
+
+def _layer_options(layers, n):
+    if layers is None:
+        return None
+    arr = (LayerOptions * n)()
+    for i, lo in enumerate(layers):
+        for f in _OPTION_FIELDS:
+            t = lo.get(f)
+            setattr(arr[i], f, t.data_ptr() if t is not None else None)
+    return arr
+
+
+def quantize_section(weights):
+    """(weights with w_qkv, w_o, w_up and w_down as e4m3 codes, their scale bytes as the layers of SectionOptions(fp8=True))."""
+    out, layers = dict(weights, layers=[]), []
+    for lw in weights["layers"]:
+        lw, lo = dict(lw), {}
+        for k in ("qkv", "o", "up", "down"):
+            lw["w_" + k], lo["s_" + k] = k_fp8_quantize(lw["w_" + k], 128)
+        out["layers"].append(lw)
+        layers.append(lo)
+    return out, layers
+
+
+def section_workspace_bytes(cfg, max_tokens, max_seqlen, need_backward, options=None):
     c = _cfg_c(cfg)
+    if options is not None:
+        o = options.c(cfg)
+        return lib().ms_section_workspace_bytes_with(C.byref(c), C.byref(o), max_tokens, max_seqlen, int(need_backward))
     return lib().ms_section_workspace_bytes(C.byref(c), max_tokens, max_seqlen, int(need_backward))
 
 
@@ -153,24 +215,41 @@ def kd_workspace_bytes(kd, max_tokens):
     return lib().ms_kd_workspace_bytes(C.byref(c), max_tokens)
 
 
-def section_forward(cfg, weights, batch, x_in, h_out=None, ws=None):
+def section_forward(cfg, weights, batch, x_in, h_out=None, ws=None, options=None):
     c, w, b = _cfg_c(cfg), _ptrs_c(cfg, weights), batch.c()
+    if options is not None:
+        options.check(cfg)
     if h_out is None:
         h_out = torch.empty((batch.n_tokens, cfg.d_model), dtype=_tdt(cfg.dtype), device=x_in.device)
     if ws is None:
-        ws = workspace(section_workspace_bytes(cfg, batch.n_tokens, batch.max_seqlen, False), x_in.device)
+        ws = workspace(section_workspace_bytes(cfg, batch.n_tokens, batch.max_seqlen, False, options), x_in.device)
+    if options is not None:
+        o = options.c(cfg)
+        _check(lib().ms_section_forward_with(C.byref(c), C.byref(o), C.byref(w), C.byref(b), _p(x_in), _p(h_out), _p(ws),
+                                             C.c_size_t(ws.numel()), _stream()))
+        return h_out
     _check(lib().ms_section_forward(C.byref(c), C.byref(w), C.byref(b), _p(x_in), _p(h_out), _p(ws),
                                     C.c_size_t(ws.numel()), _stream()))
     return h_out
 
 
 def section_forward_backward(cfg, weights, grads, batch, x_in, d_h_out=None, kd=None, w_teacher=None, w_student=None,
-                             h_teacher=None, d_w_student=None, loss_scale=None, want_d_x_in=False, ws=None):
-    """Returns dict(h_out, loss, kl_tok, d_x_in); `grads` (and d_w_student) are accumulated in place."""
+                             h_teacher=None, d_w_student=None, loss_scale=None, want_d_x_in=False, ws=None, options=None,
+                             option_grads=None):
+    """Returns dict(h_out, loss, kl_tok, d_x_in); `grads` (and d_w_student) are accumulated in place.  option_grads: with
+    SectionOptions(qk_norm=True), fp32 q_norm_g and k_norm_g of each layer, accumulated too."""
+    if options is not None:
+        options.check(cfg)
+        if options.qk_norm:
+            if option_grads is None or len(option_grads) != cfg.n_layers:
+                raise ValueError(f"option_grads: expected a dict for each of {cfg.n_layers} layers")
+            for lg in option_grads:
+                for k in ("q_norm_g", "k_norm_g"):
+                    _need("gradient of " + k, lg.get(k), (torch.float32,), (cfg.head_dim,), None)
     c, w, g, b = _cfg_c(cfg), _ptrs_c(cfg, weights), _ptrs_c(cfg, grads), batch.c()
     dev, n = x_in.device, batch.n_tokens
     h_out = torch.empty((n, cfg.d_model), dtype=_tdt(cfg.dtype), device=dev)
-    need = section_workspace_bytes(cfg, n, batch.max_seqlen, True)
+    need = section_workspace_bytes(cfg, n, batch.max_seqlen, True, options)
     loss = kl = kdc = None
     if kd is not None:
         kdc = _kd_c(kd, w_teacher, w_student, (1.0 / max(n, 1)) if loss_scale is None else loss_scale)
@@ -180,6 +259,13 @@ def section_forward_backward(cfg, weights, grads, batch, x_in, d_h_out=None, kd=
     d_x_in = torch.empty_like(h_out) if (want_d_x_in and cfg.vocab == 0) else None
     if ws is None:
         ws = workspace(need, dev)
+    if options is not None:
+        o = options.c(cfg)
+        _check(lib().ms_section_forward_backward_with(
+            C.byref(c), C.byref(o), _layer_options(option_grads, cfg.n_layers), C.byref(w), C.byref(g), C.byref(b), _p(x_in), _p(h_out), _p(d_h_out),
+            C.byref(kdc) if kdc is not None else None, _p(h_teacher), _p(d_w_student), _p(loss), _p(kl), _p(d_x_in),
+            _p(ws), C.c_size_t(ws.numel()), _stream()))
+        return dict(h_out=h_out, loss=loss, kl_tok=kl, d_x_in=d_x_in)
     _check(lib().ms_section_forward_backward(
         C.byref(c), C.byref(w), C.byref(g), C.byref(b), _p(x_in), _p(h_out), _p(d_h_out),
         C.byref(kdc) if kdc is not None else None, _p(h_teacher), _p(d_w_student), _p(loss), _p(kl), _p(d_x_in),

@@ -368,6 +368,7 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const uint2 *__rest
     }
 }
 
+constexpr long kSmallPieces = 8192L * 256;       // vectors of dx below which pieces have 8 places
 struct SortPlan { int bits, passes, ipt, blocks, tile; };
 SortPlan sort_plan(int n, int vocab, int vpr) {
     SortPlan p;
@@ -378,7 +379,7 @@ SortPlan sort_plan(int n, int vocab, int vpr) {
     p.ipt = n <= 128 * kSortThreads ? 1 : n <= 512 * kSortThreads ? 4 : 16;
     p.blocks = n <= kSmall ? 1 : ms_cdiv(n, (long)p.ipt * kSortThreads);
     // pieces of 8 places where 32 would leave the chip without work
-    p.tile = (long)n * vpr < 8192L * 256 ? 8 : 32;
+    p.tile = (long)n * vpr < kSmallPieces ? 8 : 32;
     return p;
 }
 struct SortScratch { uint2 *a, *b; int *counts, *runs; float *part; size_t bytes; };
@@ -433,8 +434,16 @@ extern "C" ms_status ms_k_embedding_scaled_forward(int32_t dtype, int32_t out_fp
 
 extern "C" size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_t d, int32_t vocab) {
     if (n <= 0 || n > kMaxTokens || d <= 0 || vocab <= 0 || vocab == 0x7fffffff) return 0;
-    // (pieces are as small for either type as for the one with fewer vectors per row)
-    return carve(nullptr, sort_plan(n, vocab, d / 8), n, d).bytes;
+    // never less than for fewer tokens: where pieces or sorting workgroups grow, the count before that may need more (pieces are as small for
+    // either type as for the one with fewer vectors per row)
+    const int at[] = {n, kSmall, 128 * kSortThreads, 512 * kSortThreads, d / 8 > 0 ? (int)((kSmallPieces - 1) / (d / 8)) : n};
+    size_t most = 0;
+    for (int m : at) {
+        if (m > n || m <= 0) continue;
+        const size_t b = carve(nullptr, sort_plan(m, vocab, d / 8), m, d).bytes;
+        most = b > most ? b : most;
+    }
+    return most;
 }
 
 extern "C" ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, int32_t d, int32_t vocab, float scale, const int32_t *ids,

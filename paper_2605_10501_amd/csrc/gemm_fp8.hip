@@ -691,7 +691,7 @@ ms_status launch_gemm(Fp8Params p, bool precise, hipStream_t s) {
 }
 
 // SwiGLU in the epilogue: gate and up rows of a tile's columns have to lie in whole blocks of 128 weight rows
-bool swiglu_fused(int M, int F, int K, long ldw) { return M > 64 && F % kBlk == 0 && ms_buffer_range_ok(2L * F, K, ldw, 1); }
+bool swiglu_fused(int M, int F, int K, long ldw) { return M > kFp8DirectRows && F % kBlk == 0 && ms_buffer_range_ok(2L * F, K, ldw, 1); }
 bool launch_swiglu(Fp8Params &p, hipStream_t s) {
     const int forced = g_tile.load(), tile = forced ? forced : fp8_choose(kFp8Swiglu, p.M, p.N, p.kb);
     if (tile == F256) return launch_big<true>(p, s);
@@ -727,8 +727,9 @@ extern "C" ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *
 }
 
 extern "C" size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K) {
-    if (M <= 0 || F <= 0 || K <= 0 || swiglu_fused(M, F, K, K)) return 0;
-    return ms_align_up((size_t)M * 2 * F * sizeof(float));
+    if (M <= 0 || F <= 0 || K <= 0) return 0;
+    const int rows = swiglu_fused(M, F, K, K) && M > kFp8DirectRows ? kFp8DirectRows : M;       // never less than for fewer rows
+    return ms_align_up((size_t)rows * 2 * F * sizeof(float));
 }
 
 extern "C" ms_status ms_k_gemm_fp8_swiglu(int32_t M, int32_t F, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W,

@@ -73,6 +73,33 @@ ms_status launch_norm_backward(int kind, int dtype, int x_fp32, int n, int d, co
                                const float *rstd, const void *add, void *dx, float *pg, float *pb, int grid, hipStream_t s);
 ms_status launch_column_sums(int dtype, const ColSums &m, int n, int blocks, int rows, hipStream_t s);
 
+// Sections with options: what they call, as a table (section_options.hip), so that the executor itself does not depend on those kernels
+struct SectionOps {
+    decltype(&ms_k_embedding_scaled_forward) embed_forward;
+    decltype(&ms_k_embedding_sorted_backward) embed_backward;
+    decltype(&ms_k_embedding_sorted_backward_scratch_bytes) embed_backward_scratch;
+    decltype(&ms_k_qk_norm_rope_forward) qk_forward;
+    decltype(&ms_k_qk_norm_rope_backward) qk_backward;
+    decltype(&ms_k_qk_norm_rope_backward_scratch_bytes) qk_backward_scratch;
+    decltype(&ms_k_norm_fp8) fp8_norm;
+    decltype(&ms_k_fp8_quantize) fp8_quantize;
+    decltype(&ms_k_gemm_fp8) fp8_gemm;
+    decltype(&ms_k_gemm_fp8_swiglu) fp8_swiglu;
+    decltype(&ms_k_gemm_fp8_swiglu_scratch_bytes) fp8_swiglu_scratch;
+};
+struct SectionOptions {
+    const ms_section_options *o;
+    const ms_layer_options *grads;       // fp32 gradients of the query / key norms, per layer
+    const SectionOps *ops;
+};
+size_t section_workspace(const ms_section_config *cfg, const SectionOptions *opt, int32_t max_tokens, int32_t max_seqlen, bool backward);
+ms_status section_forward(const ms_section_config *cfg, const SectionOptions *opt, const ms_section_ptrs *weights, const ms_batch *batch,
+                          const void *x_in, void *h_out, void *workspace_dev, size_t workspace_bytes, void *stream);
+ms_status section_forward_backward(const ms_section_config *cfg, const SectionOptions *opt, const ms_section_ptrs *weights,
+                                   const ms_section_ptrs *grads, const ms_batch *batch, const void *x_in, void *h_out, const void *d_h_out,
+                                   const ms_kd_config *kd, const void *h_teacher, void *d_w_student, float *loss_dev, float *kl_per_token_dev,
+                                   void *d_x_in, void *workspace_dev, size_t workspace_bytes, void *stream);
+
 // KD-loss pieces (kd.hip)
 ms_status kd_forward_backward(const ms_kd_config *kd, int n_tokens, const void *h_teacher, const void *h_student,
                               float *loss_dev, float *kl_tok_dev, void *d_h_student, void *d_w_student,

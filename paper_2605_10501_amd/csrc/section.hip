@@ -9,6 +9,9 @@
 // norm backward that read it.  In forward+backward mode every layer keeps its
 // input, both normed activations, the (rotated) qkv, the attention output and log-sum-exp, the
 // post-attention residual, the FFN pre-activation and activation: nothing is recomputed.
+// A section with options (section_options.hip; `opt` is null for one without) may also scale its embedding rows, norm its query and
+// key heads (then the unnormed qkv is kept too), and, forward only, hold its matrices in 8 bits.
+#include <math.h>
 #include <vector>
 
 #include "common.h"
@@ -18,6 +21,7 @@ namespace {
 
 struct LayerBuf {
     void *x, *h1, *qkv, *o, *x2, *h2, *up, *act;
+    void *qkv_raw;                 // with query / key norms and a backward pass: their input
     float *lse, *rstd1, *mean1, *rstd2, *mean2;
 };
 
@@ -31,7 +35,9 @@ struct Plan {
     // backward temporaries
     void *dy0, *dy1, *dx2, *dh, *d_o, *dqkv, *da, *dup, *dhs;
     void *norm_scratch, *attn_scratch;
-    size_t norm_scratch_bytes, bytes;
+    void *qk_scratch, *embed_scratch;                      // options: gradients of query / key norms, of the embedding by sorted ids
+    void *code, *code_s, *act_code, *act_s, *fp8_scratch;  // options: 8-bit operands and their scales
+    size_t norm_scratch_bytes, embed_scratch_bytes, fp8_scratch_bytes, bytes;
     bool bwd;                      // layers keep their activations for a backward pass
 };
 
@@ -54,7 +60,10 @@ Dims dims_of(const ms_section_config *c, int n, int max_seqlen) {
     return m;
 }
 
-Plan make_plan(const ms_section_config *c, int n, int max_seqlen, bool bwd, void *ws) {
+// Bytes of the scale rows of n x cols codes
+size_t scale_cols(int cols) { return (size_t)(cols + 511) / 512 * 4; }
+
+Plan make_plan(const ms_section_config *c, const SectionOptions *opt, int n, int max_seqlen, bool bwd, void *ws) {
     const Dims m = dims_of(c, n, max_seqlen);
     Arena a(ws);
     Plan p = {};
@@ -63,12 +72,15 @@ Plan make_plan(const ms_section_config *c, int n, int max_seqlen, bool bwd, void
     auto res = [&](size_t cols) { return a.take<void>(N * cols * 4); };   // residual stream: fp32
     auto f32 = [&](size_t cnt) { return a.take<float>(cnt * 4); };
     const int nbuf = bwd ? c->n_layers : 1;
+    const bool qk = opt && opt->o->qk_norm, fp8 = opt && opt->o->fp8;
     p.bwd = bwd;
     p.layers.resize(nbuf);
     for (auto &l : p.layers) {
         l.x = bwd ? res(m.d) : nullptr;
-        l.h1 = act(m.d); l.qkv = act(m.dqkv); l.o = act(m.dattn); l.x2 = res(m.d); l.h2 = act(m.d);
-        l.up = act(m.dup); l.act = act(m.f);
+        if (!fp8) l.h1 = act(m.d);
+        l.qkv = act(m.dqkv); l.o = act(m.dattn); l.x2 = res(m.d);
+        if (!fp8) { l.h2 = act(m.d); l.up = act(m.dup); l.act = act(m.f); }
+        if (qk && bwd) l.qkv_raw = act(m.dqkv);
         l.lse = f32(N * m.nq); l.rstd1 = f32(N); l.mean1 = f32(N); l.rstd2 = f32(N); l.mean2 = f32(N);
     }
     if (!bwd) { p.xa = res(m.d); p.xb = res(m.d); }
@@ -83,6 +95,20 @@ Plan make_plan(const ms_section_config *c, int n, int max_seqlen, bool bwd, void
         p.norm_scratch_bytes = ms_k_norm_backward_scratch_bytes(widest);
         p.norm_scratch = a.take<void>(p.norm_scratch_bytes);
         p.attn_scratch = a.take<void>(ms_k_attention_backward_scratch_bytes(c->dtype, m.nq, m.nkv, m.hd, n));
+        if (qk) p.qk_scratch = a.take<void>(opt->ops->qk_backward_scratch(m.hd));
+        if (opt && c->vocab > 0) {
+            p.embed_scratch_bytes = opt->ops->embed_backward_scratch(n, m.d, c->vocab);
+            p.embed_scratch = a.take<void>(p.embed_scratch_bytes);
+        }
+    }
+    if (fp8) {
+        const int widest = m.d > m.dattn ? m.d : m.dattn;
+        p.code = a.take<void>(N * widest);
+        p.code_s = a.take<void>(N * scale_cols(widest));
+        p.act_code = a.take<void>(N * m.f);
+        p.act_s = a.take<void>(N * scale_cols(m.f));
+        p.fp8_scratch_bytes = opt->ops->fp8_swiglu_scratch(n, m.f, m.d);
+        p.fp8_scratch = a.take<void>(p.fp8_scratch_bytes);
     }
     p.bytes = a.off;
     return p;
@@ -107,7 +133,9 @@ ms_status validate_config(const ms_section_config *c) {
 }
 
 // Limits of the kernels this call will launch, so that nothing fails after the first launch.
-ms_status validate_limits(const ms_section_config *c, int n_tokens, bool backward) {
+ms_status validate_limits(const ms_section_config *c, const SectionOptions *opt, int n_tokens, bool backward) {
+    if (backward && opt && c->vocab > 0 && opt->ops->embed_backward_scratch(n_tokens, c->d_model, c->vocab) == 0)
+        return ms_fail(MS_ERR_UNSUPPORTED, "section: %d tokens are more than the embedding gradient sorts", n_tokens);
     if (backward && c->d_model > ms_norm_backward_max_d(c->dtype))
         return ms_fail(MS_ERR_UNSUPPORTED, "section: d_model=%d above %d, the widest row the norm backward kernel holds",
                        c->d_model, ms_norm_backward_max_d(c->dtype));
@@ -149,8 +177,34 @@ ms_status validate_ptrs(const ms_section_config *c, const ms_section_ptrs *w, co
     return MS_OK;
 }
 
+ms_status validate_options(const ms_section_config *c, const SectionOptions *opt, bool backward) {
+    if (!opt) return MS_OK;
+    const ms_section_options *o = opt->o;
+    if (c->arch != MS_DECODER) return ms_fail(MS_ERR_UNSUPPORTED, "section: options are for decoders");
+    if (!(o->embed_scale > -INFINITY && o->embed_scale < INFINITY)) return ms_fail(MS_ERR_INVALID_ARG, "section: embed_scale is not finite");
+    if ((o->qk_norm || o->fp8) && !o->layers) return ms_fail(MS_ERR_INVALID_ARG, "section: options without layers");
+    if (o->fp8 && backward) return ms_fail(MS_ERR_UNSUPPORTED, "section: 8-bit matrices are for forward-only sections");
+    if (o->fp8 && c->dtype != MS_BF16) return ms_fail(MS_ERR_UNSUPPORTED, "section: 8-bit matrices need bf16 activations");
+    if (o->fp8 && (c->d_model % 16 || c->d_ffn % 16))
+        return ms_fail(MS_ERR_UNSUPPORTED, "section: d_model=%d and d_ffn=%d must be multiples of 16 with 8-bit matrices", c->d_model, c->d_ffn);
+    return MS_OK;
+}
+ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions *opt, bool backward) {
+    if (!opt) return MS_OK;
+    const ms_section_options *o = opt->o;
+    if (o->qk_norm && backward && !opt->grads) return ms_fail(MS_ERR_INVALID_ARG, "section: options: null gradients of the query / key norms");
+    for (int i = 0; i < c->n_layers && (o->qk_norm || o->fp8); ++i) {
+        const ms_layer_options &l = o->layers[i];
+        if ((o->qk_norm && (!l.q_norm_g || !l.k_norm_g)) || (o->fp8 && (!l.s_qkv || !l.s_o || !l.s_up || !l.s_down)) ||
+            (o->qk_norm && backward && (!opt->grads[i].q_norm_g || !opt->grads[i].k_norm_g)))
+            return ms_fail(MS_ERR_INVALID_ARG, "section: options: null pointer in layer %d", i);
+    }
+    return MS_OK;
+}
+
 struct Exec {
     const ms_section_config *c;
+    const SectionOptions *opt;
     Dims m;
     const ms_batch *b;
     Plan *p;
@@ -193,7 +247,10 @@ struct Exec {
         const size_t bytes = (size_t)m.n * m.d * m.es;
         auto overlaps = [&](const void *q) { return q && (const char *)q < (const char *)x_in + bytes && (const char *)x_in < (const char *)q + bytes; };
         if (c->vocab > 0) {
-            MS_TRY(ms_k_embedding_forward(dt, 0, m.n, m.d, c->vocab, (const int32_t *)x_in, weights->embedding, buf, s));
+            if (opt && opt->o->embed_scale != 1.f)
+                MS_TRY(opt->ops->embed_forward(dt, 0, m.n, m.d, c->vocab, opt->o->embed_scale, (const int32_t *)x_in, weights->embedding, buf, s));
+            else
+                MS_TRY(ms_k_embedding_forward(dt, 0, m.n, m.d, c->vocab, (const int32_t *)x_in, weights->embedding, buf, s));
             x0 = *x = buf;
         } else if (dt == MS_F32) {
             x0 = *x = x_in;
@@ -206,15 +263,47 @@ struct Exec {
         return MS_OK;
     }
 
-    ms_status layer_forward(const ms_layer_ptrs &w, const void *x, LayerBuf &l, void *y) {
+    // Rotary embedding of qkv, and the norms of its query and key heads before it: from `raw`, or in place if that is null
+    ms_status rotate(int li, const void *raw, void *qkv) {
+        if (!opt || !opt->o->qk_norm) return ms_k_rope(dt, m.n, m.nq + m.nkv, m.hd, m.dqkv, qkv, p->pos, p->rope, 0, s);
+        const ms_layer_options &g = opt->o->layers[li];
+        return opt->ops->qk_forward(dt, m.n, m.nq, m.nkv, m.hd, c->norm_eps, raw ? raw : qkv, m.dqkv, g.q_norm_g, g.k_norm_g, p->pos, p->rope,
+                                    m.max_seqlen, qkv, m.dqkv, s);
+    }
+    // y[n, out] = x W^T (+ res) of 8-bit operands; with a residual, y is the fp32 stream (from the 8-bit units' sums, whose error is far below
+    // that of the operands)
+    ms_status linear_fp8(const void *code, const void *scales, int in, const void *W, const void *sW, int out, void *y, const void *res) {
+        return opt->ops->fp8_gemm(m.n, out, in, code, in, scales, scale_cols(in), W, in, sW, scale_cols(in), y, out, res ? 2 : 0, res, out,
+                                  res && fp32_stream(res), s);
+    }
+    // A layer whose matrices are in 8 bits: norms, attention output and activation are quantised where they are made or read
+    ms_status layer_forward_fp8(const ms_layer_ptrs &w, int li, const void *x, LayerBuf &l, void *y) {
+        const ms_layer_options &q = opt->o->layers[li];
+        const SectionOps &ops = *opt->ops;
+        MS_TRY(ops.fp8_norm(dt, fp32_stream(x), m.n, m.d, c->norm_eps, x, w.norm1_g, p->code, m.d, p->code_s, scale_cols(m.d), s));
+        MS_TRY(linear_fp8(p->code, p->code_s, m.d, w.w_qkv, q.s_qkv, m.dqkv, l.qkv, nullptr));
+        MS_TRY(rotate(li, nullptr, l.qkv));
+        MS_TRY(ms_k_attention_forward(dt, 1, m.nq, m.nkv, m.hd, m.n, b->n_seqs, m.max_seqlen, b->cu_seqlens_dev, l.qkv, l.o, l.lse, s));
+        MS_TRY(ops.fp8_quantize(dt, 1, m.n, m.dattn, l.o, m.dattn, p->code, m.dattn, p->code_s, scale_cols(m.dattn), s));
+        MS_TRY(linear_fp8(p->code, p->code_s, m.dattn, w.w_o, q.s_o, m.d, l.x2, x));
+        MS_TRY(ops.fp8_norm(dt, 1, m.n, m.d, c->norm_eps, l.x2, w.norm2_g, p->code, m.d, p->code_s, scale_cols(m.d), s));
+        MS_TRY(ops.fp8_swiglu(m.n, m.f, m.d, p->code, m.d, p->code_s, scale_cols(m.d), w.w_up, m.d, q.s_up, scale_cols(m.d), p->act_code, m.f, p->act_s,
+                              scale_cols(m.f), p->fp8_scratch, p->fp8_scratch_bytes, s));
+        return linear_fp8(p->act_code, p->act_s, m.f, w.w_down, q.s_down, m.d, y, l.x2);
+    }
+
+    ms_status layer_forward(const ms_layer_ptrs &w, int li, const void *x, LayerBuf &l, void *y) {
+        if (opt && opt->o->fp8) return layer_forward_fp8(w, li, x, l, y);
         bool done = false;
-        if (m.dec && dt == MS_F32)
+        const bool qk = opt && opt->o->qk_norm;
+        if (m.dec && dt == MS_F32 && !qk)
             MS_TRY(norm_qkv_rope_f32(m.n, m.d, m.nq + 2 * m.nkv, m.nq + m.nkv, m.hd, c->norm_eps, (const float *)x, (const float *)w.norm1_g,
                                      (const float *)w.w_qkv, p->pos, p->rope, (float *)l.qkv, p->bwd ? (float *)l.h1 : nullptr, l.rstd1, &done, s));
         if (!done) {
             MS_TRY(ms_k_norm_forward(kind, dt, fp32_stream(x), m.n, m.d, c->norm_eps, x, w.norm1_g, w.norm1_b, l.h1, l.mean1, l.rstd1, s));
-            MS_TRY(linear(l.h1, m.d, w.w_qkv, m.dec ? nullptr : w.b_qkv, m.dqkv, l.qkv, nullptr));
-            if (m.dec) MS_TRY(ms_k_rope(dt, m.n, m.nq + m.nkv, m.hd, m.dqkv, l.qkv, p->pos, p->rope, 0, s));
+            void *raw = qk && p->bwd ? l.qkv_raw : nullptr;
+            MS_TRY(linear(l.h1, m.d, w.w_qkv, m.dec ? nullptr : w.b_qkv, m.dqkv, raw ? raw : l.qkv, nullptr));
+            if (m.dec) MS_TRY(rotate(li, raw, l.qkv));
         }
         MS_TRY(ms_k_attention_forward(dt, m.dec, m.nq, m.nkv, m.hd, m.n, b->n_seqs, m.max_seqlen, b->cu_seqlens_dev,
                                       l.qkv, l.o, l.lse, s));
@@ -240,7 +329,7 @@ struct Exec {
     }
 
     // dy: gradient of the layer output; dx: gradient of the layer input (distinct buffers)
-    ms_status layer_backward(const ms_layer_ptrs &w, const ms_layer_ptrs &g, const LayerBuf &l, const void *dy, void *dx) {
+    ms_status layer_backward(const ms_layer_ptrs &w, const ms_layer_ptrs &g, int li, const LayerBuf &l, const void *dy, void *dx) {
         if (m.dec) {
             MS_TRY(ms_k_swiglu_linear_backward(dt, m.n, m.d, m.f, dy, w.w_down, l.act, l.up, p->da, p->dup, g.w_down, s));
         } else {
@@ -253,7 +342,13 @@ struct Exec {
         MS_TRY(linear_backward(p->dx2, m.d, w.w_o, m.dattn, l.o, p->d_o, g.w_o, g.b_o));
         MS_TRY(ms_k_attention_backward(dt, m.dec, m.nq, m.nkv, m.hd, m.n, b->n_seqs, m.max_seqlen, b->cu_seqlens_dev,
                                        l.qkv, l.o, l.lse, p->d_o, p->dqkv, p->attn_scratch, s));
-        if (m.dec) MS_TRY(ms_k_rope(dt, m.n, m.nq + m.nkv, m.hd, m.dqkv, p->dqkv, p->pos, p->rope, 1, s));
+        if (opt && opt->o->qk_norm) {
+            const ms_layer_options &q = opt->o->layers[li], &dq = opt->grads[li];
+            MS_TRY(opt->ops->qk_backward(dt, m.n, m.nq, m.nkv, m.hd, c->norm_eps, p->dqkv, m.dqkv, l.qkv_raw, m.dqkv, q.q_norm_g, q.k_norm_g, p->pos,
+                                         p->rope, m.max_seqlen, p->dqkv, m.dqkv, (float *)dq.q_norm_g, (float *)dq.k_norm_g, p->qk_scratch, s));
+        } else if (m.dec) {
+            MS_TRY(ms_k_rope(dt, m.n, m.nq + m.nkv, m.hd, m.dqkv, p->dqkv, p->pos, p->rope, 1, s));
+        }
         MS_TRY(linear_backward(p->dqkv, m.dqkv, w.w_qkv, m.d, l.h1, p->dh, g.w_qkv, g.b_qkv));
         MS_TRY(norm_backward_pending(kind, dt, fp32_stream(l.x), m.n, m.d, p->dh, l.x, w.norm1_g, l.mean1, l.rstd1, p->dx2, dx,
                                      (float *)g.norm1_g, (float *)g.norm1_b, &cols, s));
@@ -269,33 +364,33 @@ struct Exec {
 
 }  // namespace
 
-extern "C" size_t ms_section_workspace_bytes(const ms_section_config *cfg, int32_t max_tokens, int32_t max_seqlen,
-                                             int32_t need_backward) {
-    if (validate_config(cfg) != MS_OK || max_tokens < 0 || max_seqlen < 0) return 0;
-    return make_plan(cfg, max_tokens, max_seqlen, need_backward != 0, nullptr).bytes;
+size_t section_workspace(const ms_section_config *cfg, const SectionOptions *opt, int32_t max_tokens, int32_t max_seqlen, bool backward) {
+    if (validate_config(cfg) != MS_OK || validate_options(cfg, opt, backward) != MS_OK || max_tokens < 0 || max_seqlen < 0) return 0;
+    return make_plan(cfg, opt, max_tokens, max_seqlen, backward, nullptr).bytes;
 }
 
-extern "C" ms_status ms_section_forward(const ms_section_config *cfg, const ms_section_ptrs *weights,
-                                        const ms_batch *batch, const void *x_in, void *h_out, void *workspace_dev,
-                                        size_t workspace_bytes, void *stream) {
+ms_status section_forward(const ms_section_config *cfg, const SectionOptions *opt, const ms_section_ptrs *weights, const ms_batch *batch,
+                          const void *x_in, void *h_out, void *workspace_dev, size_t workspace_bytes, void *stream) {
     MS_TRY(validate_config(cfg));
+    MS_TRY(validate_options(cfg, opt, false));
     int max_seqlen = 0;
     MS_TRY(validate_batch(batch, &max_seqlen));
     if (batch->n_tokens == 0) return MS_OK;
-    MS_TRY(validate_limits(cfg, batch->n_tokens, false));
+    MS_TRY(validate_limits(cfg, opt, batch->n_tokens, false));
     MS_TRY(validate_ptrs(cfg, weights, "weights"));
+    MS_TRY(validate_option_ptrs(cfg, opt, false));
     if (!x_in || !h_out || !workspace_dev) return ms_fail(MS_ERR_INVALID_ARG, "section_forward: null pointer");
-    Plan p = make_plan(cfg, batch->n_tokens, max_seqlen, false, workspace_dev);
+    Plan p = make_plan(cfg, opt, batch->n_tokens, max_seqlen, false, workspace_dev);
     if (workspace_bytes < p.bytes)
         return ms_fail(MS_ERR_WORKSPACE, "section_forward: workspace %zu < %zu bytes", workspace_bytes, p.bytes);
-    Exec e{cfg, dims_of(cfg, batch->n_tokens, max_seqlen), batch, &p, (hipStream_t)stream, cfg->dtype,
+    Exec e{cfg, opt, dims_of(cfg, batch->n_tokens, max_seqlen), batch, &p, (hipStream_t)stream, cfg->dtype,
            cfg->arch == MS_ENCODER ? 1 : 0, {}, nullptr};
     MS_TRY(e.prologue());
     const void *x = nullptr;
     MS_TRY(e.first_input(x_in, weights, p.xa, nullptr, nullptr, &x));
     for (int li = 0; li < cfg->n_layers; ++li) {
         void *y = li + 1 == cfg->n_layers ? p.y_last : (x == p.xa ? p.xb : p.xa);
-        MS_TRY(e.layer_forward(weights->layers[li], x, p.layers[0], y));
+        MS_TRY(e.layer_forward(weights->layers[li], li, x, p.layers[0], y));
         e.x0 = nullptr;                       // (its buffer takes a later layer's fp32 stream)
         x = y;
     }
@@ -303,13 +398,12 @@ extern "C" ms_status ms_section_forward(const ms_section_config *cfg, const ms_s
                              h_out, p.mean_f, p.rstd_f, e.s);
 }
 
-extern "C" ms_status ms_section_forward_backward(const ms_section_config *cfg, const ms_section_ptrs *weights,
-                                                 const ms_section_ptrs *grads, const ms_batch *batch, const void *x_in,
-                                                 void *h_out, const void *d_h_out, const ms_kd_config *kd,
-                                                 const void *h_teacher, void *d_w_student, float *loss_dev,
-                                                 float *kl_per_token_dev, void *d_x_in, void *workspace_dev,
-                                                 size_t workspace_bytes, void *stream) {
+ms_status section_forward_backward(const ms_section_config *cfg, const SectionOptions *opt, const ms_section_ptrs *weights,
+                                   const ms_section_ptrs *grads, const ms_batch *batch, const void *x_in, void *h_out, const void *d_h_out,
+                                   const ms_kd_config *kd, const void *h_teacher, void *d_w_student, float *loss_dev, float *kl_per_token_dev,
+                                   void *d_x_in, void *workspace_dev, size_t workspace_bytes, void *stream) {
     MS_TRY(validate_config(cfg));
+    MS_TRY(validate_options(cfg, opt, true));
     int max_seqlen = 0;
     MS_TRY(validate_batch(batch, &max_seqlen));
     hipStream_t s = (hipStream_t)stream;
@@ -322,16 +416,17 @@ extern "C" ms_status ms_section_forward_backward(const ms_section_config *cfg, c
             return ms_fail(MS_ERR_SHAPE, "section_forward_backward: kd->h_student / dtype do not match the section");
         if (!loss_dev) return ms_fail(MS_ERR_INVALID_ARG, "section_forward_backward: loss_dev is null");
     }
-    MS_TRY(validate_limits(cfg, batch->n_tokens, true));
+    MS_TRY(validate_limits(cfg, opt, batch->n_tokens, true));
     MS_TRY(validate_ptrs(cfg, weights, "weights"));
     MS_TRY(validate_ptrs(cfg, grads, "grads"));
+    MS_TRY(validate_option_ptrs(cfg, opt, true));
     if (!x_in || !h_out || !workspace_dev || (kd && !h_teacher))
         return ms_fail(MS_ERR_INVALID_ARG, "section_forward_backward: null pointer");
-    Plan p = make_plan(cfg, batch->n_tokens, max_seqlen, true, workspace_dev);
+    Plan p = make_plan(cfg, opt, batch->n_tokens, max_seqlen, true, workspace_dev);
     const size_t kd_bytes = kd ? ms_kd_workspace_bytes(kd, batch->n_tokens) : 0;
     if (workspace_bytes < p.bytes + kd_bytes)
         return ms_fail(MS_ERR_WORKSPACE, "section_forward_backward: workspace %zu < %zu bytes", workspace_bytes, p.bytes + kd_bytes);
-    Exec e{cfg, dims_of(cfg, batch->n_tokens, max_seqlen), batch, &p, s, cfg->dtype, cfg->arch == MS_ENCODER ? 1 : 0,
+    Exec e{cfg, opt, dims_of(cfg, batch->n_tokens, max_seqlen), batch, &p, s, cfg->dtype, cfg->arch == MS_ENCODER ? 1 : 0,
            {(char *)p.norm_scratch, p.norm_scratch_bytes, 0, 0, {}}, nullptr};
     MS_TRY(e.prologue());
     const int L = cfg->n_layers;
@@ -340,7 +435,7 @@ extern "C" ms_status ms_section_forward_backward(const ms_section_config *cfg, c
     for (int li = 0; li < L; ++li) {
         void *y = li + 1 == L ? p.y_last : p.layers[li + 1].x;
         p.layers[li].x = const_cast<void *>(x);
-        MS_TRY(e.layer_forward(weights->layers[li], x, p.layers[li], y));
+        MS_TRY(e.layer_forward(weights->layers[li], li, x, p.layers[li], y));
         x = y;
     }
     MS_TRY(ms_k_norm_forward(e.kind, e.dt, 1, e.m.n, e.m.d, cfg->norm_eps, p.y_last, weights->final_norm_g,
@@ -356,10 +451,34 @@ extern "C" ms_status ms_section_forward_backward(const ms_section_config *cfg, c
                                  dy, (float *)grads->final_norm_g, (float *)grads->final_norm_b, &e.cols, s));
     for (int li = L - 1; li >= 0; --li) {
         void *dx = (li == 0 && cfg->vocab == 0 && d_x_in) ? d_x_in : (dy == p.dy0 ? p.dy1 : p.dy0);
-        MS_TRY(e.layer_backward(weights->layers[li], grads->layers[li], p.layers[li], dy, dx));
+        MS_TRY(e.layer_backward(weights->layers[li], grads->layers[li], li, p.layers[li], dy, dx));
         dy = dx;
     }
-    if (cfg->vocab > 0)
+    if (opt && cfg->vocab > 0)
+        MS_TRY(opt->ops->embed_backward(e.dt, e.m.n, e.m.d, cfg->vocab, opt->o->embed_scale, (const int32_t *)x_in, dy, (float *)grads->embedding,
+                                        p.embed_scratch, p.embed_scratch_bytes, s));
+    else if (cfg->vocab > 0)
         MS_TRY(ms_k_embedding_backward(e.dt, e.m.n, e.m.d, cfg->vocab, (const int32_t *)x_in, dy, (float *)grads->embedding, s));
     return MS_OK;
+}
+
+extern "C" size_t ms_section_workspace_bytes(const ms_section_config *cfg, int32_t max_tokens, int32_t max_seqlen,
+                                             int32_t need_backward) {
+    return section_workspace(cfg, nullptr, max_tokens, max_seqlen, need_backward != 0);
+}
+
+extern "C" ms_status ms_section_forward(const ms_section_config *cfg, const ms_section_ptrs *weights,
+                                        const ms_batch *batch, const void *x_in, void *h_out, void *workspace_dev,
+                                        size_t workspace_bytes, void *stream) {
+    return section_forward(cfg, nullptr, weights, batch, x_in, h_out, workspace_dev, workspace_bytes, stream);
+}
+
+extern "C" ms_status ms_section_forward_backward(const ms_section_config *cfg, const ms_section_ptrs *weights,
+                                                 const ms_section_ptrs *grads, const ms_batch *batch, const void *x_in,
+                                                 void *h_out, const void *d_h_out, const ms_kd_config *kd,
+                                                 const void *h_teacher, void *d_w_student, float *loss_dev,
+                                                 float *kl_per_token_dev, void *d_x_in, void *workspace_dev,
+                                                 size_t workspace_bytes, void *stream) {
+    return section_forward_backward(cfg, nullptr, weights, grads, batch, x_in, h_out, d_h_out, kd, h_teacher, d_w_student, loss_dev, kl_per_token_dev,
+                                    d_x_in, workspace_dev, workspace_bytes, stream);
 }
