@@ -543,15 +543,20 @@ def _call(name, dev, *args):
 def _need(name, t, dtypes, shape, device, rows=False):
     """t: a tensor of one of `dtypes` and of `shape` (None: any size) on `device` (None: any GPU), contiguous, or, with `rows`, a matrix
     whose rows are."""
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.is_cuda and (device is None or t.device == device) and t.is_contiguous():
+        return
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise ValueError(f"{name}: expected a tensor of {' or '.join(str(d) for d in dtypes)}, got {getattr(t, 'dtype', type(t).__name__)}")
-    have = t.shape
-    if have != shape and (len(have) != len(shape) or any(s is not None and s != a for s, a in zip(shape, have))):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(have)}")
+    if t.dim() != len(shape) or any(s is not None and s != a for s, a in zip(shape, t.shape)):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name}: expected a tensor on {device or 'a GPU'}, got one on {t.device}")
-    if not (t.is_contiguous() or (rows and t.stride(1) == 1 and t.stride(0) >= have[1])):
+    if not (t.is_contiguous() or (rows and t.stride(1) == 1 and t.stride(0) >= t.shape[1])):
         raise ValueError(f"{name}: expected {'rows with unit stride' if rows else 'a contiguous tensor'}, got strides {t.stride()}")
+
+
+def _n_rows(t):
+    return t.shape[0] if isinstance(t, torch.Tensor) and t.dim() == 2 else None
 
 
 def _ld(t):
@@ -559,16 +564,17 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-_STORE = (torch.bfloat16, torch.float32)
+_STORE, _F32, _I32 = (torch.bfloat16, torch.float32), (torch.float32,), (torch.int32,)
 
 
 def _qkn_args(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, pos, table, what):
-    n, dev = x.shape[0], x.device
-    _need(what, x, _STORE, (None, (n_q_heads + 2 * n_kv_heads) * head_dim), None, rows=True)
+    n = _n_rows(x)
+    _need(what, x, _STORE, (n, (n_q_heads + 2 * n_kv_heads) * head_dim), None, rows=True)
+    dev = x.device
     _need("g_q", g_q, (x.dtype,), (head_dim,), dev)
     _need("g_k", g_k, (x.dtype,), (head_dim,), dev)
-    _need("pos", pos, (torch.int32,), (n,), dev)
-    _need("table", table, (torch.float32,), (None, head_dim // 2, 2), dev)
+    _need("pos", pos, _I32, (n,), dev)
+    _need("table", table, _F32, (table.shape[0] if isinstance(table, torch.Tensor) and table.dim() else None, head_dim // 2, 2), dev)
     return n, dev
 
 
@@ -577,7 +583,7 @@ def k_qk_norm_rope_forward(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, eps, po
     place.  pos, table: k_positions, k_rope_table."""
     n, dev = _qkn_args(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, pos, table, "x")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     elif out is not x:
         _need("out", out, (x.dtype,), x.shape, dev, rows=True)
     _call("ms_k_qk_norm_rope_forward", dev, _dt(x.dtype), n, n_q_heads, n_kv_heads, head_dim, eps, x.data_ptr(), _ld(x), g_q.data_ptr(),
@@ -589,13 +595,13 @@ def k_qk_norm_rope_backward(dy, x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, ep
     """Returns dx (V heads: dy's); x is the forward call's input.  dg_q / dg_k (fp32) are accumulated in place.  out=dy: in place."""
     n, dev = _qkn_args(x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, pos, table, "x")
     _need("dy", dy, (x.dtype,), x.shape, dev, rows=True)
-    _need("dg_q", dg_q, (torch.float32,), (head_dim,), dev)
-    _need("dg_k", dg_k, (torch.float32,), (head_dim,), dev)
+    _need("dg_q", dg_q, _F32, (head_dim,), dev)
+    _need("dg_k", dg_k, _F32, (head_dim,), dev)
     if out is None:
-        out = torch.empty(dy.shape, dtype=dy.dtype, device=dev)
+        out = torch.empty_like(dy, memory_format=torch.contiguous_format)
     elif out is not dy:
         _need("out", out, (x.dtype,), x.shape, dev, rows=True)
-    sc = torch.empty(_fn("ms_k_qk_norm_rope_backward_scratch_bytes")(head_dim), dtype=torch.uint8, device=dev)
+    sc = dg_q.new_empty(_fn("ms_k_qk_norm_rope_backward_scratch_bytes")(head_dim) // 4)
     _call("ms_k_qk_norm_rope_backward", dev, _dt(x.dtype), n, n_q_heads, n_kv_heads, head_dim, eps, dy.data_ptr(), _ld(dy), x.data_ptr(),
           _ld(x), g_q.data_ptr(), g_k.data_ptr(), pos.data_ptr(), table.data_ptr(), table.shape[0], out.data_ptr(), _ld(out),
           dg_q.data_ptr(), dg_k.data_ptr(), sc.data_ptr())
@@ -605,9 +611,9 @@ def k_qk_norm_rope_backward(dy, x, n_q_heads, n_kv_heads, head_dim, g_q, g_k, ep
 def k_embedding_scaled_forward(ids, table, scale, out_fp32=False):
     """scale * table[ids]; ids outside the table give zeros."""
     _need("table", table, _STORE, (None, None), None)
-    _need("ids", ids, (torch.int32,), (None,), table.device)
+    _need("ids", ids, _I32, (None,), table.device)
     n, (vocab, d) = ids.shape[0], table.shape
-    x = torch.empty((n, d), dtype=torch.float32 if out_fp32 else table.dtype, device=table.device)
+    x = table.new_empty((n, d), dtype=torch.float32) if out_fp32 else table.new_empty((n, d))
     _call("ms_k_embedding_scaled_forward", table.device, _dt(table.dtype), int(out_fp32), n, d, vocab, scale, ids.data_ptr(), table.data_ptr(), x.data_ptr())
     return x
 
@@ -616,12 +622,12 @@ def k_embedding_sorted_backward(ids, dx, scale, d_table):
     """d_table (fp32 [vocab, d], accumulated in place and returned) += scale * the sums of dx's rows by id, in token order."""
     _need("dx", dx, _STORE, (None, None), None)
     n, d = dx.shape
-    _need("ids", ids, (torch.int32,), (n,), dx.device)
-    _need("d_table", d_table, (torch.float32,), (None, d), dx.device)
+    _need("ids", ids, _I32, (n,), dx.device)
+    _need("d_table", d_table, _F32, (None, d), dx.device)
     vocab = d_table.shape[0]
-    sc = torch.empty(_fn("ms_k_embedding_sorted_backward_scratch_bytes")(n, d, vocab), dtype=torch.uint8, device=dx.device)
+    sc = ids.new_empty((_fn("ms_k_embedding_sorted_backward_scratch_bytes")(n, d, vocab) + 3) // 4)
     _call("ms_k_embedding_sorted_backward", dx.device, _dt(dx.dtype), n, d, vocab, scale, ids.data_ptr(), dx.data_ptr(), d_table.data_ptr(),
-          sc.data_ptr(), sc.numel())
+          sc.data_ptr(), sc.numel() * 4)
     return d_table
 
 
