@@ -16,6 +16,11 @@ namespace {
 
 constexpr int kPartRows = 768;       // workgroups of the backward kernel, one partial row of dg each
 
+// Results leave non-temporally: 20011 tokens x 16 heads forward 33.9 -> 28.8 us, 4096 x 24 12.1 -> 9.8, backward 3-8 % (loads by that policy
+// too gain 2 % on the largest batches and lose up to 18 % on small ones)
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+template <class T> __device__ __forceinline__ void put(T *p, const Vec16<T> &r) { __builtin_nontemporal_store(*(const u32x4 *)&r, (u32x4 *)p); }
+
 template <int G> __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
     for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -90,8 +95,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_fwd_kernel(QknArgs a, int he
                     oh.v[e] = from_f32<T>(q * c[e] + p * s[e]);
                 }
                 if (h >= nqk) { ol = lo; oh = hi; }              // a V head is copied
-                stv(yr + (long)h * a.hd, ol);
-                stv(yr + (long)h * a.hd + half, oh);
+                put(yr + (long)h * a.hd, ol);
+                put(yr + (long)h * a.hd + half, oh);
             }
             lo = nlo; hi = nhi;
         }
@@ -112,7 +117,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
         const long col = (long)(a.nq + a.nkv) * a.hd;
         for (long i = (long)b * 256 + threadIdx.x; i < total; i += stride) {
             const long t = i / vpr, cv = i % vpr;
-            stv((T *)a.out + t * a.os + col + cv * V, ldv((const T *)a.dy + t * a.dys + col + cv * V));
+            put((T *)a.out + t * a.os + col + cv * V, ldv((const T *)a.dy + t * a.dys + col + cv * V));
         }
         return;
     }
@@ -138,13 +143,18 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
     long t = (s0 * HPW + hl) / nh;
     int h = (int)((s0 * HPW + hl) % nh);
     Vec16<T> v0, v1, v2, v3;
-    auto load = [&](long t, int h) {
+    auto load = [&](bool ok, long t, int h) {            // zeros where there is nothing (one test for the wave instead of selects for each element)
+        if (!__all(ok)) {
+            const uint4 z = make_uint4(0, 0, 0, 0);
+            *(uint4 *)&v0 = z; *(uint4 *)&v1 = z; *(uint4 *)&v2 = z; *(uint4 *)&v3 = z;
+        }
+        if (!ok) return;
         const long at = (long)(first + h) * a.hd + j * V;
         const T *xp = (const T *)a.x + t * a.xs + at, *dp = (const T *)a.dy + t * a.dys + at;
         v0 = ldv(xp); v1 = ldv(xp + half); v2 = ldv(dp); v3 = ldv(dp + half);
     };
     const bool some = s0 < s1;
-    if (some && live && t < a.n) load(t, h);
+    load(some && live && t < a.n, t, h);
     int p = some && t < a.n ? a.pos[t] : -1;
     for (long st = s0; st < s1; ++st) {
         const bool mine = live && t < a.n;
@@ -154,15 +164,15 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
         load_angles<V>(a, p, j * V, live, c, s);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            xl[e] = mine ? to_f32(v0.v[e]) : 0.f; xh[e] = mine ? to_f32(v1.v[e]) : 0.f;
-            yl[e] = mine ? to_f32(v2.v[e]) : 0.f; yh[e] = mine ? to_f32(v3.v[e]) : 0.f;
+            xl[e] = to_f32(v0.v[e]); xh[e] = to_f32(v1.v[e]);
+            yl[e] = to_f32(v2.v[e]); yh[e] = to_f32(v3.v[e]);
             ss = __builtin_fmaf(xl[e], xl[e], ss);
             ss = __builtin_fmaf(xh[e], xh[e], ss);
         }
         h += dh; t += dt;                                // the next heads are on their way while these are worked on
         if (h >= nh) { h -= nh; ++t; }
         const bool more = st + 1 < s1 && t < a.n;
-        if (more && live) load(t, h);
+        load(more && live, t, h);
         p = more ? a.pos[t] : -1;
         ss = group_sum<G>(ss);
         const float r = mine ? rsqrtf(ss * inv_hd + a.eps) : 0.f;
@@ -186,8 +196,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
                 oh.v[e] = from_f32<T>(__builtin_fmaf(-xh[e], m, yh[e]));
             }
             T *o = (T *)a.out + now * a.os + at;
-            stv(o, ol);
-            stv(o + half, oh);
+            put(o, ol);
+            put(o + half, oh);
         }
     }
     // heads of the wave, then waves, in a fixed order
