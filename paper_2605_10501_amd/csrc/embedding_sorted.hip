@@ -6,7 +6,7 @@
 // The gradient needs no floating-point atomics: its sums have one order, so a run repeats bit for bit, and a row that thousands
 // of tokens share (padding, frequent words) is not added to by thousands of atomics.  Steps:
 //   1. stable radix sort of (id, token): per digit, a workgroup ranks its tokens and places them behind those of the workgroups
-//      before it (per-workgroup digit counts; integer atomics, whose order does not matter).  Up to kSmall tokens one workgroup
+//      before it (per-workgroup digit counts; integer atomics in LDS, whose order does not matter).  Up to kSmall tokens one workgroup
 //      does all digits in LDS.  Ids outside the table sort last.
 //   2. pieces of 8 or 32 sorted places x one 16-byte column vector per thread: one pass over dx.  A run of equal ids that lies within
 //      the piece is added to the table; what continues from or into a neighbour goes to a row of partial sums.
@@ -21,6 +21,7 @@ namespace {
 constexpr int kSortThreads = 1024, kWaves = kSortThreads / 64, kDigitBits = 9, kBins = 1 << kDigitBits;
 constexpr int kSmall = 4 * kSortThreads;  // tokens that one workgroup sorts in LDS
 constexpr int kMaxTokens = 1 << 24;
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ forward
 template <class T, class TO, int U>
@@ -60,19 +61,19 @@ __global__ __launch_bounds__(256) void embedding_scaled_kernel(const int *__rest
 // ------------------------------------------------------------------ sort
 __device__ __forceinline__ unsigned key_of(int id, int vocab) { return (unsigned)id < (unsigned)vocab ? (unsigned)id : (unsigned)vocab; }
 
-// Digit counts of every workgroup's tokens by the first digit; clears the counters that the passes add to
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int *__restrict__ ids, int n, int vocab, int per, int mask,
-                                                                  int *__restrict__ counts, int *__restrict__ next, long next_len, int *__restrict__ runs) {
+// Digit counts of every workgroup's tokens.  (A pass that adds up the next one's counts with global atomics while it scatters saves this launch, but
+// frequent ids share their upper digit: 16384 tokens of a vocabulary of 32000 15 us a pass instead of 4 and 3 for the counts.)
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int *__restrict__ ids, const uint2 *__restrict__ in, int n, int vocab, int per, int shift,
+                                                                  int mask, int *__restrict__ counts, int *__restrict__ runs) {
     __shared__ int hist[kBins];
     const int tid = threadIdx.x;
     if (blockIdx.x == 0 && tid == 0) *runs = 0;
     if (tid < kBins) hist[tid] = 0;
     __syncthreads();
     const long b0 = (long)blockIdx.x * per;
-    for (int i = tid; i < per && b0 + i < n; i += kSortThreads) atomicAdd(&hist[key_of(ids[b0 + i], vocab) & mask], 1);
+    for (int i = tid; i < per && b0 + i < n; i += kSortThreads) atomicAdd(&hist[((ids ? key_of(ids[b0 + i], vocab) : in[b0 + i].x) >> shift) & mask], 1);
     __syncthreads();
     if (tid < kBins) counts[(long)blockIdx.x * kBins + tid] = hist[tid];
-    for (long i = (long)blockIdx.x * kSortThreads + tid; i < next_len; i += (long)gridDim.x * kSortThreads) next[i] = 0;
 }
 
 // Ranks of a workgroup's tokens by a digit: lanes of equal digits find each other by ballots, the first of them moves the wave's
@@ -116,11 +117,10 @@ __device__ __forceinline__ int scan_bins(int v, int *wsum) {
 }
 
 // One stable pass by the digit (key >> shift) & mask.  ids != null: the keys are the ids and the values the token numbers.
-// counts: [workgroups][kBins] of this digit; next: the same for the following digit in the new order, added to here.
+// counts: [workgroups][kBins] of this digit.
 template <int IPT>
 __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(const int *__restrict__ ids, const uint2 *__restrict__ in, int n, int vocab, int shift,
-                                                                 int bits, const int *__restrict__ counts, int *__restrict__ next,
-                                                                 int next_shift, uint2 *__restrict__ out) {
+                                                                 int bits, const int *__restrict__ counts, uint2 *__restrict__ out) {
     __shared__ int hist[kWaves][kBins];
     __shared__ int base[kBins];
     __shared__ int wsum[kBins / 64];
@@ -180,9 +180,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(const int *__re
     for (int r = 0; r < IPT; ++r) {
         if (valid[r]) {
             const int dg = (key[r] >> shift) & mask;
-            const int at = base[dg] + hist[wv][dg] + rank[r];
-            out[at] = kv[r];
-            if (next) atomicAdd(next + (long)(at / per) * kBins + ((key[r] >> next_shift) & mask), 1);
+            out[base[dg] + hist[wv][dg] + rank[r]] = kv[r];
         }
     }
 }
@@ -244,8 +242,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int *__r
 // ------------------------------------------------------------------ sums
 // part: [pieces][2][d]: row 0 the end of a run that began in an earlier piece, row 1 the part of a run that goes on in the next.
 // runs[0] counts, runs[1 ..] list the pieces in which a run begins that goes on (in any order: each is added up by itself).
-// U places at a time: their rows of dx and the table rows of the runs that end there are requested together.
-template <class T, int TILE, int U>
+// U places at a time: their rows of dx and the table rows of the runs that end there are requested together.  STREAM: dx by the non-temporal policy,
+// above 80 MB (us, without / with: 32768 x 1536 85.8 / 80.9, x 4096 190 / 159; 16384 x 1024, 34 MB, 51.4 / 56.5).
+template <class T, int TILE, int U, bool STREAM>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint2 *__restrict__ sorted, const T *__restrict__ dx, float scale, int n, int vpr,
                                                             int vocab, float *__restrict__ d_table, float *__restrict__ part, int *__restrict__ runs,
                                                             long total) {
@@ -280,7 +279,8 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint2 *__restr
             const unsigned nextk = p + u + 1 < p1 ? kv[u + 1].x : after;
             end[u] = p + u < p1 && kv[u].x != nextk;
             if (p + u < p1 && kv[u].x < (unsigned)vocab) {
-                v[u] = ldv(dx + (long)kv[u].y * d + cv);
+                if constexpr (STREAM) *(u32x4 *)&v[u] = __builtin_nontemporal_load((const u32x4 *)(dx + (long)kv[u].y * d + cv));
+                else v[u] = ldv(dx + (long)kv[u].y * d + cv);
                 if (end[u] && (seen || !fb)) {
                     const float *o = d_table + (long)kv[u].x * d + cv;
 #pragma unroll
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const uint2 *__rest
     }
 }
 
-constexpr long kSmallPieces = 8192L * 256;       // vectors of dx below which pieces have 8 places
+constexpr long kSmallPieces = 16384L * 256;      // vectors of dx below which pieces have 8 places
 struct SortPlan { int bits, passes, ipt, blocks, tile; };
 SortPlan sort_plan(int n, int vocab, int vpr) {
     SortPlan p;
@@ -389,7 +389,7 @@ SortScratch carve(void *ws, const SortPlan &p, int n, int d) {
     SortScratch s;
     s.a = a.take<uint2>((size_t)n * 8);
     s.b = a.take<uint2>((size_t)n * 8);
-    s.counts = a.take<int>((size_t)p.passes * p.blocks * kBins * 4);
+    s.counts = a.take<int>((size_t)p.blocks * kBins * 4);
     s.runs = a.take<int>((tiles + 1) * 4);
     s.part = a.take<float>(tiles * 2 * d * 4);
     s.bytes = a.off;
@@ -470,13 +470,12 @@ extern "C" ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, in
         MS_LAUNCH_CHECK();
         in = sc.a;
     } else {
-        const long cb = (long)p.blocks * kBins;
-        sort_count_kernel<<<p.blocks, kSortThreads, 0, s>>>(ids, n, vocab, p.ipt * kSortThreads, (1 << p.bits) - 1, sc.counts, sc.counts + cb, (p.passes - 1) * cb, sc.runs);
-        MS_LAUNCH_CHECK();
         for (int k = 0; k < p.passes; ++k) {
             uint2 *out = (k & 1) ? sc.b : sc.a;
-            int *next = k + 1 < p.passes ? sc.counts + (k + 1) * cb : nullptr;
-#define GO(I) sort_pass_kernel<I><<<p.blocks, kSortThreads, 0, s>>>(k ? nullptr : ids, in, n, vocab, k * p.bits, p.bits, sc.counts + k * cb, next, (k + 1) * p.bits, out)
+            const int *first = k ? nullptr : ids;
+            sort_count_kernel<<<p.blocks, kSortThreads, 0, s>>>(first, in, n, vocab, p.ipt * kSortThreads, k * p.bits, (1 << p.bits) - 1, sc.counts, sc.runs);
+            MS_LAUNCH_CHECK();
+#define GO(I) sort_pass_kernel<I><<<p.blocks, kSortThreads, 0, s>>>(first, in, n, vocab, k * p.bits, p.bits, sc.counts, out)
             if (p.ipt == 1) GO(1); else if (p.ipt == 4) GO(4); else GO(16);
 #undef GO
             MS_LAUNCH_CHECK();
@@ -485,10 +484,16 @@ extern "C" ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, in
     }
     const int blocks = (int)((total + 255) / 256), strips = ms_cdiv(d, 256);
     const long tasks = (long)(tiles - 1) * strips;       // at most
-#define GO(T, TILE, U) embedding_sum_kernel<T, TILE, U><<<blocks, 256, 0, s>>>(in, (const T *)dx, scale, n, vpr, vocab, d_table, sc.part, sc.runs, total)
+    const bool stream_dx = (double)n * d * ms_dtype_size(dtype) > 80e6;
+#define GO2(T, TILE, U, ST) embedding_sum_kernel<T, TILE, U, ST><<<blocks, 256, 0, s>>>(in, (const T *)dx, scale, n, vpr, vocab, d_table, sc.part, sc.runs, total)
+#define GO(T, TILE, U)                                                                    \
+    do {                                                                                  \
+        if (stream_dx) GO2(T, TILE, U, true); else GO2(T, TILE, U, false);                \
+    } while (0)
     if (dtype == MS_BF16) { if (p.tile == 8) GO(bf16_t, 8, 8); else GO(bf16_t, 32, 4); }
     else { if (p.tile == 8) GO(float, 8, 8); else GO(float, 32, 8); }
 #undef GO
+#undef GO2
     MS_LAUNCH_CHECK();
     if (tasks > 0) {
         const int grid = (int)(tasks < 2048 ? tasks : 2048);
