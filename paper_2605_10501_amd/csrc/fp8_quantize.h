@@ -17,6 +17,13 @@ __device__ __forceinline__ unsigned fp8_finite_bits(float v) {
     return b < 0x7f800000u ? b : 0u;
 }
 
+// silu(g) u, with the reciprocal instruction (1 ulp) instead of a division: the result is rounded to four bits.  One function, because whether an
+// epilogue or a pass of its own takes it depends on the sizes, and the codes must not.
+__device__ __forceinline__ float fp8_silu_mul(float g, float u) {
+#pragma clang fp contract(off)
+    return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)) * u;
+}
+
 __device__ __forceinline__ unsigned fp8_pack4(float a, float b, float c, float d) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);

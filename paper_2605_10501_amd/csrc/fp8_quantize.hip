@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void fp8_rows_kernel(const T *__restrict__ x, 
                 float u[8];
                 fp8_load8(x + row * ldx + k + c, u);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = v[e] / (1.f + __expf(-v[e])) * u[e];
+                for (int e = 0; e < 8; ++e) v[e] = fp8_silu_mul(v[e], u[e]);
             }
         }
         int byte;

@@ -66,8 +66,6 @@ __device__ __forceinline__ bf16x8 widen8(int a, int b, float scale) {
 __device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((unsigned)(byte & 255) << 23); }
 __device__ __forceinline__ i32x8 join(const i32x4 &lo, const i32x4 &hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + __expf(-g)) * u; }
-
 // NV consecutive outputs of a row
 template <int NV> __device__ __forceinline__ void store_row(const Fp8Params &p, int m, int n, float *v) {
     if (m >= p.M || n >= p.N) return;
@@ -252,9 +250,14 @@ __device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[i][4 * j + e] = silu_mul(acc[i][j][e], acc[i][2 + j][e]);
-                m = max(m, fp8_finite_bits(v[i][4 * j + e]));
+                v[i][4 * j + e] = fp8_silu_mul(acc[i][j][e], acc[i][2 + j][e]);
+                m = max(m, __float_as_uint(v[i][4 * j + e]) & 0x7fffffffu);
             }
+        if (__builtin_expect(__any(m >= 0x7f800000u), 0)) {
+            m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max(m, fp8_finite_bits(v[i][e]));
+        }
         m = max(m, (unsigned)__shfl_xor((int)m, 16, 64));
         m = max(m, (unsigned)__shfl_xor((int)m, 32, 64));
         if (g == 0) mx[wn * BM + row(i)] = m;
