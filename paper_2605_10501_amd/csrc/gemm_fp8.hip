@@ -50,6 +50,12 @@ struct Fp8Params {
 };
 
 // W, A: which byte of sw, sa has the exponents
+// The same with the accumulators bound to accumulation registers, where the compiler would copy them to and fro for a kernel that needs all 256.  It does
+// not see the latency: whoever reads the sums waits first.
+template <int W, int A> __device__ __forceinline__ void mfma_acc(const i32x8 &w, const i32x8 &a, f32x4 &c, int sw, int sa) {
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
+        : "+a"(c) : "v"(w), "v"(a), "v"(sw), "v"(sa), "n"(W & 1), "n"(A & 1), "n"(W >> 1), "n"(A >> 1));
+}
 template <int W, int A> __device__ __forceinline__ f32x4 mfma(const i32x8 &w, const i32x8 &a, const f32x4 &c, int sw, int sa) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, W, sw, A, sa);
 }
@@ -227,6 +233,20 @@ __device__ __forceinline__ void stage_scales(const Fp8Params &p, uint8_t *pa, ui
     }
 }
 
+// Most calls want bf16 without a residual.  The kernels have that by itself: store_row's other forms, unrolled over the accumulators, are ten
+// times the code, more than the instruction cache holds (256 x 256 tile, 32768 x 22016 x 4096: 2.60 ms with one form for all, 2.45 so).
+__device__ __forceinline__ bool plain_rows(const Fp8Params &p) { return p.vec && !p.c_fp32 && !p.R; }
+template <int NV> __device__ __forceinline__ void store_plain(const Fp8Params &p, int m, int n, const float *v) {
+    if (m >= p.M || n >= p.N) return;
+#pragma unroll
+    for (int q = 0; q < NV / 8; ++q) {
+        Vec16<bf16_t> t;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t.v[e] = from_f32<bf16_t>(v[8 * q + e]);
+        stv((bf16_t *)p.C + m * p.ldc + n + 8 * q, t);
+    }
+}
+
 // Which tile a workgroup has: each XCD (every eighth workgroup) works on a contiguous range of tiles, ordered in groups of `gm` rows of
 // tiles x all columns, so that it shares operand panels in its L2
 __device__ __forceinline__ void tile_of(const Fp8Params &p, int gm, int bm, int bn, int *m0, int *n0) {
@@ -237,26 +257,27 @@ __device__ __forceinline__ void tile_of(const Fp8Params &p, int gm, int bm, int 
     *n0 = pid % width / rows * bn;
 }
 
-// SwiGLU tile of 128 activation columns: accumulator blocks 0, 1 are gate, 2, 3 up of the lane's columns 32 wn + 8 g .. + 7; the tile's width is their
-// scale block, so its maximum needs the four wave columns' maxima (mx: LDS, [4][BM])
-template <int MI, int BM, class ROW>
-__device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 (&acc)[MI][4], unsigned *mx, int m0, int n0, int wn, int g, ROW row) {
-    float v[MI][8];
-    const int n = n0 + wn * 32 + 8 * g;
+// SwiGLU tile of 128 activation columns: the first half of the accumulator blocks is gate, the second up of the lane's 2 NJ consecutive columns; the
+// tile's width is their scale block, so its maximum needs the wave columns' maxima (mx: LDS, [WN][BM])
+template <int MI, int BM, int NJ, class ROW>
+__device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 (&acc)[MI][NJ], unsigned *mx, int m0, int n0, int wn, int g, ROW row) {
+    constexpr int NV = 2 * NJ, WN = kBlk / (4 * NV);     // a lane's consecutive columns, wave columns
+    float v[MI][NV];
+    const int n = n0 + wn * 4 * NV + NV * g;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         unsigned m = 0;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < NJ / 2; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[i][4 * j + e] = fp8_silu_mul(acc[i][j][e], acc[i][2 + j][e]);
+                v[i][4 * j + e] = fp8_silu_mul(acc[i][j][e], acc[i][NJ / 2 + j][e]);
                 m = max(m, __float_as_uint(v[i][4 * j + e]) & 0x7fffffffu);
             }
         if (__builtin_expect(__any(m >= 0x7f800000u), 0)) {
             m = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = max(m, fp8_finite_bits(v[i][e]));
+            for (int e = 0; e < NV; ++e) m = max(m, fp8_finite_bits(v[i][e]));
         }
         m = max(m, (unsigned)__shfl_xor((int)m, 16, 64));
         m = max(m, (unsigned)__shfl_xor((int)m, 32, 64));
@@ -266,11 +287,16 @@ __device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         const int ml = row(i), m = m0 + ml;
-        const int byte = fp8_scale_byte(max(max(mx[ml], mx[BM + ml]), max(mx[2 * BM + ml], mx[3 * BM + ml])));
+        unsigned most = mx[ml];
+#pragma unroll
+        for (int w = 1; w < WN; ++w) most = max(most, mx[w * BM + ml]);
+        const int byte = fp8_scale_byte(most);
         const float is = fp8_inverse_scale(byte);
         if (m < p.M) {
-            *(uint2 *)((uint8_t *)p.C + (long)m * p.ldc + n) = make_uint2(fp8_pack4(v[i][0] * is, v[i][1] * is, v[i][2] * is, v[i][3] * is),
-                                                                          fp8_pack4(v[i][4] * is, v[i][5] * is, v[i][6] * is, v[i][7] * is));
+            unsigned c[NV / 4];
+#pragma unroll
+            for (int q = 0; q < NV / 4; ++q) c[q] = fp8_pack4(v[i][4 * q] * is, v[i][4 * q + 1] * is, v[i][4 * q + 2] * is, v[i][4 * q + 3] * is);
+            __builtin_memcpy(__builtin_assume_aligned((uint8_t *)p.C + (long)m * p.ldc + n, NV), c, NV);
             if (wn == 0 && g == 0) {
                 const int b = n0 / kBlk, blocks = p.F / kBlk;
                 uint8_t *s = p.sC + (long)m * p.ldsc + b;
@@ -282,15 +308,19 @@ __device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 
     }
 }
 
-// 256 x 256 tile: eight waves (two per SIMD, which fill each other's gaps), wave tile 128 tokens x 64 outputs as four quarters (token half, weight half).
+// 256 x 256 tile: four waves, one per SIMD, wave tile 128 tokens x 128 outputs as four quarters (token half, weight half).  At full load the chip's
+// power bounds this kernel (a K tile takes 1.15 us on a few CUs, 1.5 us on all), so what counts is work per operand byte out of LDS: 128 KB of reads
+// per K tile, where eight waves of 128 x 64 read 192 KB (32768 x 22016 x 4096 with SwiGLU 2.32 -> 2.24 ms, 32768 x 4096 x 11008 1.13 -> 1.10).
+// Persistent workgroups that fetch the next tile behind their stores were no faster for the same reason.
 //   * The quarters follow (A0 F)(A0 S)(A1 S)(A1 F), F / S = the weight half used first / second, which swap roles every K tile: one operand
 //     half changes at a time.  The fragments of A0 are replaced by those of A1 one by one, each behind the last MFMAs that read it, A1's by
-//     the next tile's A0; S is free in the last quarter, F in the first: 64 registers of fragments serve without a second set.
+//     the next tile's A0; S is free in the last quarter, F in the first.
 //   * An operand tile is two halves of 128 rows with an LDS slot each and two stages: eight 16 KB slots.  Two barriers per K tile, in the
-//     first and third quarters behind half of their MFMAs, when the reads before them are long done; each hands over the slots that
+//     first and third quarters behind a quarter of their MFMAs, when the reads before them are done; each hands over the slots that
 //     have been read, to loads of K tile t + 2, and what has landed: every half is requested 1.5 K tiles before it is read, and the
-//     waits are for all but the 8 youngest loads of a wave.
-//   * Half h of the weights is blocks 2 h and 2 h + 1 of every wave column; with SwiGLU gate and up.
+//     waits are for all but the 16 youngest loads of a wave.  Reads and loads are dealt out between the MFMAs: nothing else fills a SIMD's gaps.
+//   * Half h of the weights is 64 rows of either wave column; with SwiGLU gate and up.  A lane's outputs are 8 consecutive ones of every 32, so that
+//     the four lanes of a row store 64 bytes side by side; with SwiGLU 16 consecutive ones, a byte each.
 template <bool SWIGLU, bool TAIL>
 __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     constexpr int HS = 128 * kBlk;
@@ -298,7 +328,7 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     __shared__ __align__(16) uint8_t pa[kPanel * 256], pw[kPanel * 2];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane >> 3;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 2, wn = wave & 3;
+    const int wm = wave >> 1, wn = wave & 1;
     int m0, n0;
     tile_of(p, 4, 256, SWIGLU ? 128 : 256, &m0, &n0);
     const long rows_a = p.M - m0 < 256 ? p.M - m0 : 256, rows_b = SWIGLU ? p.N - n0 : (p.N - n0 < 256 ? p.N - n0 : 256);
@@ -306,47 +336,44 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     const __amdgpu_buffer_rsrc_t rb = make_rsrc(p.W + (long)n0 * p.ldw, (rows_b - 1) * p.ldw + p.K);
     const int x = (lane & 7) ^ swz_row(lr);
     const unsigned lda = (unsigned)p.lda, ldw = (unsigned)p.ldw;
-    int piece[2];                                        // of a wave's two 8-row groups: the lane's piece, its part of the offsets
-    unsigned al[2], bl[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        piece[i] = x ^ swz_row(8 * (wave * 2 + i));
-        al[i] = (unsigned)lr * lda + (piece[i] << 4);
-        bl[i] = (unsigned)weight_row_lane<SWIGLU ? 2 : 4>(lr) * ldw + (piece[i] << 4);
-    }
+    // A wave fetches every fourth 8-row group of a half: 32 rows apart, so the lane's piece and its part of the offsets are the same in all
+    const int piece = x ^ swz_row(8 * wave);
+    const unsigned al = (unsigned)lr * lda + (piece << 4), bl = (unsigned)weight_row_lane<SWIGLU ? 4 : 2>(lr) * ldw + (piece << 4);
     const int nk = p.kb;
     int base = 0;                                        // first K tile of the panel of scales
-    auto invalid = [&](int kt, int piece) __attribute__((always_inline)) {
+    auto invalid = [&](int kt) __attribute__((always_inline)) {
         unsigned inv = kt < nk ? 0u : kOob;
         if (TAIL) inv |= kt * kBlk + piece * 16 < p.K ? 0u : kOob;
         return inv;
     };
-    // request half h of K tile kt (two loads per wave; a tile past the end arrives as zeros)
+    // request half h of K tile kt (four loads per wave; a tile past the end arrives as zeros)
+    auto load_a = [&](int kt, int h, int i, uint8_t *slot) __attribute__((always_inline)) {
+        const int lg = wave + 4 * i;
+        unsigned row = (unsigned)(h * 128 + lg * 8) * lda;
+        asm volatile("" : "+s"(row));                    // (added in the loop: the sums would fill the lane's registers)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(slot + lg * 8 * kBlk), 16, (al + row) | invalid(kt), kt < nk ? kt * kBlk : 0, 0, 0);
+    };
+    auto load_b = [&](int kt, int h, int i, uint8_t *slot) __attribute__((always_inline)) {
+        const int lg = wave + 4 * i, w = lg >> 3;
+        unsigned row = (SWIGLU ? (unsigned)(h * p.F + w * 64 + weight_row_group<4>(lg & 7)) : (unsigned)(w * 128 + h * 64 + (lg & 4) * 8 + weight_row_group<2>(lg & 3))) * ldw;
+        asm volatile("" : "+s"(row));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(slot + lg * 8 * kBlk), 16, (bl + row) | invalid(kt), kt < nk ? kt * kBlk : 0, 0, 0);
+    };
     auto fetch_a = [&](int kt, int h, uint8_t *slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int lg = wave * 2 + i;
-            unsigned row = (unsigned)(h * 128 + lg * 8) * lda;
-            asm volatile("" : "+s"(row));                // (kept out of the lane's registers: eight sums of the two would stay there for the whole loop)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(slot + lg * 8 * kBlk), 16, (al[i] + row) | invalid(kt, piece[i]), kt < nk ? kt * kBlk : 0, 0, 0);
-        }
+        for (int i = 0; i < 4; ++i) load_a(kt, h, i, slot);
     };
     auto fetch_b = [&](int kt, int h, uint8_t *slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int lg = wave * 2 + i, w = lg >> 2;
-            unsigned row = (SWIGLU ? (unsigned)(h * p.F + w * 32 + weight_row_group<2>(lg & 3)) : (unsigned)(w * 64 + weight_row_group<4>((lg & 3) + 4 * h))) * ldw;
-            asm volatile("" : "+s"(row));
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(slot + lg * 8 * kBlk), 16, (bl[i] + row) | invalid(kt, piece[i]), kt < nk ? kt * kBlk : 0, 0, 0);
-        }
+        for (int i = 0; i < 4; ++i) load_b(kt, h, i, slot);
     };
 
-    f32x4 acc[8][4];                                     // [16-token block: 4 half + b][weight block]
+    f32x4 acc[8][8];                                     // [16-token block: 4 half + b][weight block]
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    i32x8 af[4], bf[4];                                  // the present token half's blocks; weights
+        for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x8 af[4], bf[8];                                  // the present token half's blocks; weights
     int sa[2], sw = 0;                                   // scales: a byte for each of a token half's four blocks; of the weights (SwiGLU: gate, up)
     int fo[2][2];                                        // [block parity][piece g / 4 + g]
     const int r16 = lane & 15, g = lane >> 4;
@@ -360,8 +387,8 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     };
     auto read_b = [&](auto half, const uint8_t *slot) __attribute__((always_inline)) {
         constexpr int h = decltype(half)::value;
-        bf[2 * h] = frag(slot, wn * 32, 0);
-        bf[2 * h + 1] = frag(slot, wn * 32, 1);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) bf[4 * h + c] = frag(slot, wn * 64, c);
     };
     auto read_sa = [&](auto half, int kt) __attribute__((always_inline)) {
         constexpr int h = decltype(half)::value;
@@ -369,17 +396,17 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     };
     auto weight_scale = [&](int kt) __attribute__((always_inline)) -> int {
         if (SWIGLU) return *(const uint16_t *)(pw + kt * 2);
-        return pw[kt * 2 + (wn >> 1)];
+        return pw[kt * 2 + wn];
     };
-    auto mul = [&](auto ah, auto bh, auto block) __attribute__((always_inline)) {
-        constexpr int h = decltype(ah)::value, q = decltype(bh)::value, b = decltype(block)::value;
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-            acc[4 * h + b][2 * q + c] = mfma<SWIGLU ? q : 0, b>(bf[2 * q + c], af[b], acc[4 * h + b][2 * q + c], sw, sa[h]);
+    auto mul = [&](auto ah, auto bh, auto block, auto col) __attribute__((always_inline)) {
+        constexpr int h = decltype(ah)::value, q = decltype(bh)::value, b = decltype(block)::value, c = decltype(col)::value;
+        mfma_acc<SWIGLU ? q : 0, b>(bf[4 * q + c], af[b], acc[4 * h + b][4 * q + c], sw, sa[h]);
+        __builtin_amdgcn_sched_barrier(0);
     };
+    auto mul4 = [&](auto ah, auto bh, auto block) __attribute__((always_inline)) { each<4>([&](auto c) __attribute__((always_inline)) { mul(ah, bh, block, c); }); };
     auto hand_over = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
-        wait_vmcnt_lgkm0<8>();
+        wait_vmcnt_lgkm0<16>();
         lds_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -392,36 +419,39 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         constexpr int fh = decltype(F)::value;
         using FH = std::integral_constant<int, fh>;
         using SH = std::integral_constant<int, 1 - fh>;
-        mul(I0{}, FH{}, I0{});
-        mul(I0{}, FH{}, I1{});
+        mul4(I0{}, FH{}, I0{});
         hand_over();                                     // a0 and f have been read; a1 and s have landed
-        read_b(SH{}, s);
-        read_sa(I1{}, kt);
-        mul(I0{}, FH{}, I2{});
-        fetch_b(kt + 2, fh, f);
-        mul(I0{}, FH{}, I3{});
-        fetch_a(kt + 2, 0, a0);
-        __builtin_amdgcn_sched_barrier(0);
-        each<4>([&](auto b) __attribute__((always_inline)) {
-            mul(I0{}, SH{}, b);
+        each<12>([&](auto step) __attribute__((always_inline)) {
+            constexpr int t = decltype(step)::value;
+            mul(I0{}, FH{}, std::integral_constant<int, 1 + t / 4>{}, std::integral_constant<int, t % 4>{});
+            if (t < 4) bf[4 * SH::value + t % 4] = frag(s, wn * 64, t % 4);
+            if (t == 4) read_sa(I1{}, kt);
+            if (t >= 4 && t < 8) load_b(kt + 2, fh, t - 4, f);
+            if (t >= 8) load_a(kt + 2, 0, t - 8, a0);
             __builtin_amdgcn_sched_barrier(0);
+        });
+        each<4>([&](auto b) __attribute__((always_inline)) {
+            mul4(I0{}, SH{}, b);
             af[b] = frag(a1, wm * 64, b);
             __builtin_amdgcn_sched_barrier(0);
         });
-        mul(I1{}, SH{}, I0{});
-        mul(I1{}, SH{}, I1{});
+        mul4(I1{}, SH{}, I0{});
         hand_over();                                     // a1 and s have been read; the next tile's first halves have landed
-        read_sa(I0{}, kt + 1);
-        const int sw1 = weight_scale(kt + 1 - base);
-        mul(I1{}, SH{}, I2{});
-        fetch_b(kt + 2, 1 - fh, s);
-        mul(I1{}, SH{}, I3{});
-        fetch_a(kt + 2, 1, a1);
-        __builtin_amdgcn_sched_barrier(0);
-        read_b(SH{}, nb);
-        each<4>([&](auto b) __attribute__((always_inline)) {
-            mul(I1{}, FH{}, b);
+        int sw1 = 0;
+        each<12>([&](auto step) __attribute__((always_inline)) {
+            constexpr int t = decltype(step)::value;
+            mul(I1{}, SH{}, std::integral_constant<int, 1 + t / 4>{}, std::integral_constant<int, t % 4>{});
+            if (t == 0) read_sa(I0{}, kt + 1);
+            if (t == 1) sw1 = weight_scale(kt + 1 - base);
+            if (t < 4) load_b(kt + 2, 1 - fh, t, s);
+            if (t >= 4 && t < 8) load_a(kt + 2, 1, t - 4, a1);
             __builtin_amdgcn_sched_barrier(0);
+        });
+        each<4>([&](auto b) __attribute__((always_inline)) {
+            each<4>([&](auto c) __attribute__((always_inline)) {
+                mul(I1{}, FH{}, b, c);
+                if (b == 0) bf[4 * SH::value + c] = frag(nb, wn * 64, c);
+            });
             af[b] = frag(na, wm * 64, b);
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -432,8 +462,8 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     else { wblk[0] = n0 / kBlk; wblk[1] = (n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk; }
     fetch_b(0, 0, B00); fetch_a(0, 0, A00); fetch_b(0, 1, B01); fetch_a(0, 1, A01);           // in the loop's order
     fetch_b(1, 1, B11); fetch_a(1, 0, A10); fetch_b(1, 0, B10); fetch_a(1, 1, A11);
-    stage_scales<256, 4, 2, 512>(p, pa, pw, m0, wblk, 0, nk < kPanel ? nk : kPanel, tid);
-    wait_vmcnt_lgkm0<12>();
+    stage_scales<256, 4, 2, 256>(p, pa, pw, m0, wblk, 0, nk < kPanel ? nk : kPanel, tid);
+    wait_vmcnt_lgkm0<24>();
     lds_barrier();
     read_b(I0{}, B00);
 #pragma unroll
@@ -444,30 +474,44 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         if (kt - base == kSegment) {                     // the next panel of scales (this tile's first ones have been read from the old one, which goes further)
             base = kt;
             __syncthreads();
-            stage_scales<256, 4, 2, 512>(p, pa, pw, m0, wblk, base, nk - base < kPanel ? nk - base : kPanel, tid);
+            stage_scales<256, 4, 2, 256>(p, pa, pw, m0, wblk, base, nk - base < kPanel ? nk - base : kPanel, tid);
             __syncthreads();
         }
         tile(kt, I0{}, A00, A01, B00, B01, B11, A10);
         tile(kt + 1, I1{}, A10, A11, B11, B10, B00, A00);
     }
+    asm volatile("s_nop 15\n\ts_nop 15");               // the last products are there before anything reads them (the compiler does not see mfma_acc's latency)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
     dma_publish_barrier();                               // what is still in flight must land before LDS is used again
     const int mrow = m0 + wm * 64 + r16;
     if constexpr (!SWIGLU) {
+        auto rows = [&](auto store) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float v[16];
+            for (int i = 0; i < 8; ++i) {
+                int m = mrow + (i >> 2) * 128 + (i & 3) * 16;
+                asm volatile("" : "+v"(m));              // (row after row: together their copies and conditions would not fit the registers)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][j][e];
-            store_row<16>(p, mrow + (i >> 2) * 128 + (i & 3) * 16, n0 + wn * 64 + 16 * g, v);
-        }
+                for (int q = 0; q < 4; ++q) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = acc[i][2 * q + (e >> 2)][e & 3];
+                    store(m, n0 + wn * 128 + 32 * q + 8 * g, v);
+                }
+            }
+        };
+        if (plain_rows(p)) rows([&](int m, int n, float (&v)[8]) __attribute__((always_inline)) { store_plain<8>(p, m, n, v); });
+        else rows([&](int m, int n, float (&v)[8]) __attribute__((always_inline)) { store_row<8>(p, m, n, v); });
     } else {
         swiglu_epilogue<8, 256>(p, acc, (unsigned *)A00, m0, n0, wn, g, [&](int i) { return wm * 64 + (i >> 2) * 128 + (i & 3) * 16 + r16; });
     }
 }
 template <bool SWIGLU, bool TAIL>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_fp8_big_kernel(Fp8Params p) { fp8_big_body<SWIGLU, TAIL>(p); }
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void gemm_fp8_big_kernel(Fp8Params p) { fp8_big_body<SWIGLU, TAIL>(p); }
 
 // Scheduling pattern: R LDS reads and V loads dealt to the first half of the MFMAs
 template <int R, int V, int... I> __device__ __forceinline__ void spread_over_mfmas(std::integer_sequence<int, I...>) {
@@ -592,15 +636,19 @@ __device__ __forceinline__ void fp8_ring_body(const Fp8Params &p) {
         dma_publish_barrier();
     }
     if constexpr (!SWIGLU) {
+        auto rows = [&](auto store) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            float v[4 * NI];
+            for (int i = 0; i < MI; ++i) {
+                float v[4 * NI];
 #pragma unroll
-            for (int j = 0; j < NI; ++j)
+                for (int j = 0; j < NI; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][j][e];
-            store_row<4 * NI>(p, m0 + arow + i * 16 + r16, n0 + brow + 4 * NI * g, v);
-        }
+                    for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][j][e];
+                store(m0 + arow + i * 16 + r16, n0 + brow + 4 * NI * g, v);
+            }
+        };
+        if (plain_rows(p)) rows([&](int m, int n, float (&v)[4 * NI]) __attribute__((always_inline)) { store_plain<4 * NI>(p, m, n, v); });
+        else rows([&](int m, int n, float (&v)[4 * NI]) __attribute__((always_inline)) { store_row<4 * NI>(p, m, n, v); });
     } else {
         swiglu_epilogue<MI, BM>(p, acc, (unsigned *)A0, m0, n0, wn, g, [&](int i) { return arow + i * 16 + r16; });
     }
@@ -661,9 +709,9 @@ template <int BM, int BN, int WM, int WN, int NST, bool SWIGLU, bool PRECISE> bo
     return tiles != 0;
 }
 template <bool SWIGLU> bool launch_big(Fp8Params &p, hipStream_t s) {
-    const int tiles = tiles_of(p, 256, SWIGLU ? 128 : 256, SWIGLU ? p.F : p.N, 512);
-    if (tiles && p.K % kBlk) gemm_fp8_big_kernel<SWIGLU, true><<<tiles, 512, 0, s>>>(p);
-    else if (tiles) gemm_fp8_big_kernel<SWIGLU, false><<<tiles, 512, 0, s>>>(p);
+    const int tiles = tiles_of(p, 256, SWIGLU ? 128 : 256, SWIGLU ? p.F : p.N, 256);
+    if (tiles && p.K % kBlk) gemm_fp8_big_kernel<SWIGLU, true><<<tiles, 256, 0, s>>>(p);
+    else if (tiles) gemm_fp8_big_kernel<SWIGLU, false><<<tiles, 256, 0, s>>>(p);
     return tiles != 0;
 }
 
