@@ -160,7 +160,7 @@ class SectionOptions:
     def __init__(self, embed_scale=1.0, qk_norm=False, fp8=False, layers=None):
         self.embed_scale, self.qk_norm, self.fp8, self.layers = float(embed_scale), bool(qk_norm), bool(fp8), layers
 
-    def check(self, cfg):
+    def check(self, cfg, device=None):
         if (self.qk_norm or self.fp8) and (self.layers is None or len(self.layers) != cfg.n_layers):
             raise ValueError(f"section options: expected a dict for each of {cfg.n_layers} layers")
         words = lambda k: (k + 511) // 512 * 4
@@ -168,10 +168,10 @@ class SectionOptions:
         d, a, f = cfg.d_model, cfg.n_q_heads * cfg.head_dim, cfg.d_ffn
         for lo in self.layers or ():
             for k in ("q_norm_g", "k_norm_g") if self.qk_norm else ():
-                _need(k, lo.get(k), (_tdt(cfg.dtype),), (cfg.head_dim,), None)
+                _need(k, lo.get(k), (_tdt(cfg.dtype),), (cfg.head_dim,), device)
             if self.fp8:
                 for k, n, kin in (("s_qkv", cfg.d_qkv, d), ("s_o", d, a), ("s_up", 2 * f, d), ("s_down", d, f)):
-                    _need(k, lo.get(k), (torch.uint8,), (rows(n), words(kin)), None)
+                    _need(k, lo.get(k), (torch.uint8,), (rows(n), words(kin)), device)
 
     def c(self, cfg):
         o = SectionOptionsC(self.embed_scale, int(self.qk_norm), int(self.fp8), _layer_options(self.layers, cfg.n_layers))
@@ -187,6 +187,17 @@ def _layer_options(layers, n):
             t = lo.get(f)
             setattr(arr[i], f, t.data_ptr() if t is not None else None)
     return arr
+
+
+def _check_matrices(cfg, weights, options, device):
+    """Codes belong to sections with fp8, and nothing else does: a byte per number read as two would go past the end."""
+    d, a, f = cfg.d_model, cfg.n_q_heads * cfg.head_dim, cfg.d_ffn
+    for lw in weights["layers"]:
+        for k, n, kin in (("w_qkv", cfg.d_qkv, d), ("w_o", d, a), ("w_up", 2 * f, d), ("w_down", d, f)):
+            if options is not None and options.fp8:
+                _need(k, lw.get(k), (torch.float8_e4m3fn,), (n, kin), device)
+            elif lw.get(k) is not None and lw[k].dtype == torch.float8_e4m3fn:
+                raise ValueError(f"{k}: 8-bit codes need SectionOptions(fp8=True) with their scales")
 
 
 def quantize_section(weights):
@@ -216,9 +227,10 @@ def kd_workspace_bytes(kd, max_tokens):
 
 
 def section_forward(cfg, weights, batch, x_in, h_out=None, ws=None, options=None):
-    c, w, b = _cfg_c(cfg), _ptrs_c(cfg, weights), batch.c()
     if options is not None:
-        options.check(cfg)
+        options.check(cfg, x_in.device)
+    _check_matrices(cfg, weights, options, x_in.device)
+    c, w, b = _cfg_c(cfg), _ptrs_c(cfg, weights), batch.c()
     if h_out is None:
         h_out = torch.empty((batch.n_tokens, cfg.d_model), dtype=_tdt(cfg.dtype), device=x_in.device)
     if ws is None:
@@ -239,13 +251,14 @@ def section_forward_backward(cfg, weights, grads, batch, x_in, d_h_out=None, kd=
     """Returns dict(h_out, loss, kl_tok, d_x_in); `grads` (and d_w_student) are accumulated in place.  option_grads: with
     SectionOptions(qk_norm=True), fp32 q_norm_g and k_norm_g of each layer, accumulated too."""
     if options is not None:
-        options.check(cfg)
+        options.check(cfg, x_in.device)
         if options.qk_norm:
             if option_grads is None or len(option_grads) != cfg.n_layers:
                 raise ValueError(f"option_grads: expected a dict for each of {cfg.n_layers} layers")
             for lg in option_grads:
                 for k in ("q_norm_g", "k_norm_g"):
-                    _need("gradient of " + k, lg.get(k), (torch.float32,), (cfg.head_dim,), None)
+                    _need("gradient of " + k, lg.get(k), (torch.float32,), (cfg.head_dim,), x_in.device)
+    _check_matrices(cfg, weights, options, x_in.device)
     c, w, g, b = _cfg_c(cfg), _ptrs_c(cfg, weights), _ptrs_c(cfg, grads), batch.c()
     dev, n = x_in.device, batch.n_tokens
     h_out = torch.empty((n, cfg.d_model), dtype=_tdt(cfg.dtype), device=dev)
@@ -678,7 +691,7 @@ def _fp8_args(a, sa, w, sw):
 
 def k_gemm_fp8(a, sa, w, sw, residual=None, c=None, c_fp32=None, fast_sums=False):
     """a w^T (+ residual) of 8-bit operands as k_fp8_quantize makes them (a: block_rows=1, w: 128).  The result is bf16, or fp32 if c_fp32
-    (by default: if the residual is); c: a tensor to write to, which may be the residual.  fast_sums: an fp32 result from the 8-bit
+    (by default: if the residual is); c: a tensor to write to, which may be the residual (else they must not overlap).  fast_sums: an fp32 result from the 8-bit
     matrix cores' sums, which a bf16 result always has."""
     args = _fp8_args(a, sa, w, sw)
     m, n, dev = args[0], args[1], a.device

@@ -1,4 +1,6 @@
 """8-bit operands and their products: codes and scales bit by bit, products against the operands' values in 64 bits."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -364,3 +366,29 @@ def test_refusals_before_anything_is_launched():
     assert n(1, 0, 4, 128, float("nan"), 256, 256, 256, 128, 256, 4, None) == -1 and n(1, 0, 4, 128, 1e-6, 256, None, 256, 128, 256, 4, None) == -1
     assert n(1, 0, 4, 136, 1e-6, 256, 256, 256, 144, 256, 4, None) == -4 and n(1, 1, 4, 128, 1e-6, 256, 258, 256, 128, 256, 4, None) == -4
     assert f("ms_k_swiglu_fp8")(1, 4, 128, 256, 128, 256, 128, 256, 4, None) == -2
+
+
+def test_a_residual_that_overlaps_the_result_is_refused():
+    lib = B.lib()
+    v, M, N, K = C.c_void_p, 8, 32, 128
+
+    def call(c, ldc, c_fp32, r, ldr, r_fp32):
+        return lib.ms_k_gemm_fp8(M, N, K, v(16), C.c_int64(K), v(16), C.c_int64(4), v(16), C.c_int64(K), v(16), C.c_int64(4), v(c), C.c_int64(ldc),
+                                 c_fp32, v(r), C.c_int64(ldr), r_fp32, None)
+    base = 1 << 20
+    assert call(base, 64, 0, base + 2, 64, 0) == -1                         # one element on
+    assert call(base, 64, 0, base + 128, 64, 0) == -1                       # one row on
+    assert call(base, 64, 0, base, 96, 0) == -1                             # the same start, other rows
+    assert call(base, 64, 1, base, 64, 0) == -1 and call(base, 64, 0, base, 32, 1) == -1          # the same start, another type
+    assert call(base, 48, 0, base + 64, 48, 0) == -1                        # side by side in rows that hold one and a half
+
+
+@pytest.mark.gpu
+def test_residual_beside_the_result():
+    a, sa = B.k_fp8_quantize(torch.randn(70, 128, device="cuda"))
+    w, sw = B.k_fp8_quantize(torch.randn(32, 128, device="cuda"), 128)
+    both = torch.randn(70, 64, device="cuda").to(torch.bfloat16)
+    r = both[:, 32:]
+    ref = B.k_gemm_fp8(a, sa, w, sw, residual=r.clone())
+    B.k_gemm_fp8(a, sa, w, sw, residual=r, c=both[:, :32])
+    assert torch.equal(both[:, :32], ref)

@@ -269,3 +269,21 @@ def test_refusals_before_anything_is_launched():
         B.SectionOptions(qk_norm=True, layers=[{}]).check(config("bf16"))
     with pytest.raises(ValueError, match="q_norm_g"):
         B.SectionOptions(qk_norm=True, layers=[{}, {}]).check(config("bf16"))
+
+
+def test_codes_go_with_their_option():
+    cfg = config("bf16", n_layers=1)
+    d, a, f = cfg.d_model, cfg.n_q_heads * cfg.head_dim, cfg.d_ffn
+    sizes = {"w_qkv": (cfg.d_qkv, d), "w_o": (d, a), "w_up": (2 * f, d), "w_down": (d, f)}
+    plain = {k: torch.empty(s, dtype=torch.bfloat16) for k, s in sizes.items()}
+    codes = {k: torch.empty(s, dtype=torch.float8_e4m3fn) for k, s in sizes.items()}
+    ids = torch.zeros(4, dtype=torch.int32)
+    for k in sizes:                                                          # read as bf16, codes would end too early
+        with pytest.raises(ValueError, match=k + ".*fp8=True"):
+            B.section_forward(cfg, {"layers": [dict(plain, **{k: codes[k]})]}, None, ids)
+        with pytest.raises(ValueError, match=k + ".*fp8=True"):
+            B.section_forward_backward(cfg, {"layers": [dict(plain, **{k: codes[k]})]}, None, type("Batch", (), {"n_tokens": 4}), ids)
+    with pytest.raises(ValueError, match="w_qkv"):
+        B._check_matrices(cfg, {"layers": [plain]}, B.SectionOptions(fp8=True), None)
+    with pytest.raises(ValueError, match="w_qkv"):
+        B._check_matrices(cfg, {"layers": [dict(codes, w_qkv=codes["w_qkv"][1:])]}, B.SectionOptions(fp8=True), None)
