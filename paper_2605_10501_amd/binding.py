@@ -708,7 +708,7 @@ def k_gemm_fp8(a, sa, w, sw, residual=None, c=None, c_fp32=None, fast_sums=False
 
 
 def k_gemm_fp8_config(tile=0):
-    """Tile of the 8-bit products (tests, measurements): 0 / 256256 / 128128 / 128129 / 64128 / 64129 / 64064."""
+    """Tile of the 8-bit products (tests, measurements): 0 / 256256 / 256192 / 128128 / 128129 / 64128 / 64129 / 64064."""
     _check(lib().ms_k_gemm_fp8_config(int(tile)))
 
 

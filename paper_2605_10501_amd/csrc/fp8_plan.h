@@ -3,18 +3,20 @@
 #include <stddef.h>
 
 // Tile codes: token rows * 1000 + outputs, + 1 for the form with four LDS stages
-enum { F256 = 256256, F128 = 128128, F128R = 128129, F64x128 = 64128, F64x128R = 64129, F64 = 64064, FDIRECT = 16016 };
+enum { F256 = 256256, F192 = 256192, F128 = 128128, F128R = 128129, F64x128 = 64128, F64x128R = 64129, F64 = 64064, FDIRECT = 16016 };
 
 // us_per_ktile: per K tile of 128 with one workgroup per CU, few and all CUs busy, then with two per CU, few and all CUs with a second one;
 // us_round: prologue and epilogue of a round; us_call: once.  Fits to sweeps on MI355X with operands that have left the caches: 13 weight
-// matrices (256 x 688 .. 22016 x 4096) x 21 token counts (24 .. 16384) for 8-bit sums, 7 x 13 for fp32 sums, 4 x 16 for SwiGLU; K tiles are rounded
-// up to the kernel's stages.  The chosen tile is 0.3 % (fp32 sums 0.1, SwiGLU 0.1) slower than the best one in the mean, in 5 of the 428 cases
-// more than 6 % (us: 300 x 22016 x 4096 62, best 50; 1500 x 11008 x 2048 with SwiGLU 61, best 57).  Each tile is the best one of some
-// shapes: 256 x 256 of 60 of the 273, 128 x 128 of 43 and 35, 64 x 128 of 10 and 20, 64 x 64 of 105.
+// matrices (256 x 688 .. 22016 x 4096) x 21 token counts (24 .. 16384) for 8-bit sums, 7 x 13 for fp32 sums, 4 x 16 for SwiGLU, and 7 x 10 (896 x 4096 ..
+// 22016 x 4096, 65 .. 6000 tokens) for the 256-row tiles of 8-bit sums; K tiles are rounded up to the kernel's stages.  Over those 70 the chosen tile is
+// 0.1 % slower than the best one in the mean and 5 % at most (before there was one of 192 outputs, which fills last rounds that the others leave
+// half empty: 3.6 % and 48 %).  Each is the best one of some: 256 x 192 of 14 (4096 x 6144 x 4096: 89 us, 128 x 128 and 256 x 256 100), 256 x 256,
+// 128 x 128 and its ring of 12 each, 64 x 64 of 13, the ring of 64 x 128 of 7; 64 x 128 with two stages of some of the larger sweep.
 struct Fp8Tile { int code, bm, bn, per_cu, stages; double us_per_ktile[4], us_round, us_call; };
-constexpr Fp8Tile kFp8Fast[] = {{F256, 256, 256, 1, 2, {1.12, 1.51, 0, 0}, 6.7, 0.0},          {F128, 128, 128, 2, 2, {0.564, 0.758, 0.829, 0.939}, 2.7, 1.6},
-                                {F128R, 128, 128, 1, 4, {0.334, 0.483, 0, 0}, 2.6, 1.8},       {F64x128, 64, 128, 2, 2, {0.480, 0.598, 0.678, 0.715}, 1.0, 2.4},
-                                {F64x128R, 64, 128, 1, 4, {0.296, 0.349, 0, 0}, 2.6, 1.6},     {F64, 64, 64, 2, 4, {0.183, 0.227, 0.377, 0.386}, 1.3, 2.1}};
+constexpr Fp8Tile kFp8Fast[] = {{F256, 256, 256, 1, 2, {1.04, 1.42, 0, 0}, 9.2, 0.1},          {F192, 256, 192, 1, 2, {0.80, 1.11, 0, 0}, 7.9, 0.0},
+                                {F128, 128, 128, 2, 2, {0.564, 0.758, 0.829, 0.939}, 2.7, 1.6}, {F128R, 128, 128, 1, 4, {0.334, 0.483, 0, 0}, 2.6, 1.8},
+                                {F64x128, 64, 128, 2, 2, {0.480, 0.598, 0.678, 0.715}, 1.0, 2.4},  {F64x128R, 64, 128, 1, 4, {0.296, 0.349, 0, 0}, 2.6, 1.6},
+                                {F64, 64, 64, 2, 4, {0.183, 0.227, 0.377, 0.386}, 1.3, 2.1}};
 constexpr Fp8Tile kFp8Precise[] = {{F128, 128, 128, 2, 2, {0.864, 1.217, 1.593, 1.812}, 3.6, 2.5}, {F128R, 128, 128, 1, 4, {0.707, 0.963, 0, 0}, 5.7, 1.7},
                                    {F64x128, 64, 128, 2, 2, {0.644, 0.855, 1.261, 1.094}, 2.4, 1.3}, {F64x128R, 64, 128, 1, 4, {0.524, 0.638, 0, 0}, 3.7, 1.9},
                                    {F64, 64, 64, 2, 4, {0.333, 0.432, 0.663, 0.663}, 1.9, 2.2}};

@@ -15,8 +15,8 @@
 // are computed so.  An fp32 result is computed on v_mfma_f32_16x16x32_bf16 instead, half the rate, from the codes widened to bf16 (exact): fp32
 // sums throughout; unless the caller asks for the fast ones.
 //
-//   * gemm_fp8_big_kernel: 256 tokens x 256 outputs, operands through LDS;
-//   * gemm_fp8_ring_kernel: smaller tiles through LDS, for grids that do not fill the chip with the large one, and fp32 results;
+//   * gemm_fp8_big_kernel: 256 tokens x 256 or 192 outputs, operands through LDS;
+//   * gemm_fp8_ring_kernel: smaller tiles through LDS, for grids that do not fill the chip with the large ones, and fp32 results;
 //   * gemm_fp8_direct_kernel: up to 64 tokens, fragments straight from global memory, K split over the waves of a workgroup.
 // All but the last add up K in ascending order, one accumulator per output, so they give the same bits.
 #include <atomic>
@@ -211,8 +211,8 @@ template <int NI> __device__ __forceinline__ int weight_row_group(int lg) { retu
 // Scales of a workgroup's BM tokens and NW weight blocks for up to kPanel K tiles from tile t0 on.  pa: per K tile the bytes of the G fragment
 // blocks that a wave works on together, side by side, for each of their 16 rows: one read gets a lane's scales.  Tiles past the end get 1: their codes
 // arrive as zeros, and a scale may not turn those into NaN.
-template <int BM, int G, int NW, int THREADS>
-__device__ __forceinline__ void stage_scales(const Fp8Params &p, uint8_t *pa, uint8_t *pw, int m0, const int *wblk, int t0, int nt, int tid) {
+template <int BM, int G, int NW, int THREADS, class WBLK>
+__device__ __forceinline__ void stage_scales(const Fp8Params &p, uint8_t *pa, uint8_t *pw, int m0, WBLK wblk, int t0, int nt, int tid) {
     const int words = (nt + 3) >> 2;                     // four K tiles each
     for (int i = tid; i < words * (BM + NW); i += THREADS) {
         const int row = i / words, q = i % words, t = t0 + 4 * q;
@@ -220,7 +220,7 @@ __device__ __forceinline__ void stage_scales(const Fp8Params &p, uint8_t *pa, ui
         if (row < BM) {
             if (m0 + row < p.M) v = *(const unsigned *)(p.sA + (long)(m0 + row) * p.ldsa + t);
         } else {
-            v = *(const unsigned *)(p.sW + (long)wblk[row - BM] * p.ldsw + t);
+            v = *(const unsigned *)(p.sW + (long)wblk(row - BM) * p.ldsw + t);
         }
         const int left = p.kb - t;
         if (left < 4) v = (v & ((1u << (8 * left)) - 1)) | (0x7f7f7f7fu << (8 * left));
@@ -308,30 +308,34 @@ __device__ __forceinline__ void swiglu_epilogue(const Fp8Params &p, const f32x4 
     }
 }
 
-// 256 x 256 tile: four waves, one per SIMD, wave tile 128 tokens x 128 outputs as four quarters (token half, weight half).  At full load the chip's
-// power bounds this kernel (a K tile takes 1.15 us on a few CUs, 1.5 us on all), so what counts is work per operand byte out of LDS: 128 KB of reads
-// per K tile, where eight waves of 128 x 64 read 192 KB (32768 x 22016 x 4096 with SwiGLU 2.32 -> 2.24 ms, 32768 x 4096 x 11008 1.13 -> 1.10).
-// Persistent workgroups that fetch the next tile behind their stores were no faster for the same reason.
+// Tile of 256 tokens x BN = 256 or 192 outputs: four waves, one per SIMD, wave tile 128 tokens x BN / 2 outputs as four quarters (token half, weight
+// half).  At full load the chip's power bounds this kernel (a K tile of 256 x 256 takes 1.15 us on a few CUs, 1.5 us on all), so what counts is work
+// per operand byte out of LDS: 128 KB of reads per K tile, where eight waves of 128 x 64 read 192 KB (32768 x 22016 x 4096 with SwiGLU 2.32 -> 2.24
+// ms, 32768 x 4096 x 11008 1.13 -> 1.10).  Persistent workgroups that fetch the next tile behind their stores were no faster for the same reason.
 //   * The quarters follow (A0 F)(A0 S)(A1 S)(A1 F), F / S = the weight half used first / second, which swap roles every K tile: one operand
 //     half changes at a time.  The fragments of A0 are replaced by those of A1 one by one, each behind the last MFMAs that read it, A1's by
 //     the next tile's A0; S is free in the last quarter, F in the first.
-//   * An operand tile is two halves of 128 rows with an LDS slot each and two stages: eight 16 KB slots.  Two barriers per K tile, in the
-//     first and third quarters behind a quarter of their MFMAs, when the reads before them are done; each hands over the slots that
-//     have been read, to loads of K tile t + 2, and what has landed: every half is requested 1.5 K tiles before it is read, and the
-//     waits are for all but the 16 youngest loads of a wave.  Reads and loads are dealt out between the MFMAs: nothing else fills a SIMD's gaps.
-//   * Half h of the weights is 64 rows of either wave column; with SwiGLU gate and up.  A lane's outputs are 8 consecutive ones of every 32, so that
-//     the four lanes of a row store 64 bytes side by side; with SwiGLU 16 consecutive ones, a byte each.
-template <bool SWIGLU, bool TAIL>
+//   * An operand tile is two halves with an LDS slot each and two stages.  Two barriers per K tile, in the first and third quarters behind a
+//     quarter of their MFMAs, when the reads before them are done; each hands over the slots that have been read, to loads of K tile t + 2, and
+//     what has landed: every half is requested 1.5 K tiles before it is read, and the waits are for all but the youngest loads of a wave, those
+//     of four halves.  Reads and loads are dealt out between the MFMAs: nothing else fills a SIMD's gaps.
+//   * Half h of the weights is BN / 4 rows of either wave column; with SwiGLU gate and up.  A lane's outputs are 8 consecutive ones of every 32, so that
+//     the four lanes of a row store 64 bytes side by side (scale blocks of 192-wide tiles' columns change between such 32, hence a scale byte
+//     for each); with SwiGLU 16 consecutive ones, a byte each.
+//   * BN = 192 is for last rounds that 256 leaves half empty: 4096 x 6144 x 4096 102 -> 89 us, 777 x 22016 x 4096 99 -> 84.
+template <int BN, bool SWIGLU, bool TAIL>
 __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
-    constexpr int HS = 128 * kBlk;
-    __shared__ __align__(16) uint8_t A00[HS], A01[HS], A10[HS], A11[HS], B00[HS], B01[HS], B10[HS], B11[HS];
-    __shared__ __align__(16) uint8_t pa[kPanel * 256], pw[kPanel * 2];
+    constexpr int NB = BN / 64, LOADS = 4 + NB;          // weight blocks of a quarter; a wave's loads of an A and a B half
+    static_assert(BN % 64 == 0 && NB <= 4 && (!SWIGLU || BN == 256), "tile");
+    constexpr int HA = 128 * kBlk, HB = BN / 2 * kBlk, NW = SWIGLU ? 2 : 8;       // (scales: gate, up; or a byte per wave column and 32 outputs)
+    __shared__ __align__(16) uint8_t A00[HA], A01[HA], A10[HA], A11[HA], B00[HB], B01[HB], B10[HB], B11[HB];
+    __shared__ __align__(16) uint8_t pa[kPanel * 256], pw[kPanel * NW];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane >> 3;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1;
     int m0, n0;
-    tile_of(p, 4, 256, SWIGLU ? 128 : 256, &m0, &n0);
-    const long rows_a = p.M - m0 < 256 ? p.M - m0 : 256, rows_b = SWIGLU ? p.N - n0 : (p.N - n0 < 256 ? p.N - n0 : 256);
+    tile_of(p, 4, 256, SWIGLU ? 128 : BN, &m0, &n0);
+    const long rows_a = p.M - m0 < 256 ? p.M - m0 : 256, rows_b = SWIGLU ? p.N - n0 : (p.N - n0 < BN ? p.N - n0 : BN);
     const __amdgpu_buffer_rsrc_t ra = make_rsrc(p.A + (long)m0 * p.lda, (rows_a - 1) * p.lda + p.K);
     const __amdgpu_buffer_rsrc_t rb = make_rsrc(p.W + (long)n0 * p.ldw, (rows_b - 1) * p.ldw + p.K);
     const int x = (lane & 7) ^ swz_row(lr);
@@ -346,7 +350,7 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         if (TAIL) inv |= kt * kBlk + piece * 16 < p.K ? 0u : kOob;
         return inv;
     };
-    // request half h of K tile kt (four loads per wave; a tile past the end arrives as zeros)
+    // request half h of K tile kt (a tile past the end arrives as zeros)
     auto load_a = [&](int kt, int h, int i, uint8_t *slot) __attribute__((always_inline)) {
         const int lg = wave + 4 * i;
         unsigned row = (unsigned)(h * 128 + lg * 8) * lda;
@@ -354,8 +358,8 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(slot + lg * 8 * kBlk), 16, (al + row) | invalid(kt), kt < nk ? kt * kBlk : 0, 0, 0);
     };
     auto load_b = [&](int kt, int h, int i, uint8_t *slot) __attribute__((always_inline)) {
-        const int lg = wave + 4 * i, w = lg >> 3;
-        unsigned row = (SWIGLU ? (unsigned)(h * p.F + w * 64 + weight_row_group<4>(lg & 7)) : (unsigned)(w * 128 + h * 64 + (lg & 4) * 8 + weight_row_group<2>(lg & 3))) * ldw;
+        const int lg = wave + 4 * i, w = lg / (2 * NB), lw = lg % (2 * NB), block = h * NB + (lw >> 1);      // block: of the wave column
+        unsigned row = (SWIGLU ? (unsigned)(h * p.F + w * 64 + weight_row_group<4>(lw)) : (unsigned)(w * (BN / 2) + (block >> 1) * 32 + weight_row_group<2>((block & 1) * 2 + (lw & 1)))) * ldw;
         asm volatile("" : "+s"(row));
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(slot + lg * 8 * kBlk), 16, (bl + row) | invalid(kt), kt < nk ? kt * kBlk : 0, 0, 0);
     };
@@ -365,48 +369,56 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     };
     auto fetch_b = [&](int kt, int h, uint8_t *slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_b(kt, h, i, slot);
+        for (int i = 0; i < NB; ++i) load_b(kt, h, i, slot);
     };
 
-    f32x4 acc[8][8];                                     // [16-token block: 4 half + b][weight block]
+    f32x4 acc[8][2 * NB];                                     // [16-token block: 4 half + b][weight block]
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    i32x8 af[4], bf[8];                                  // the present token half's blocks; weights
-    int sa[2], sw = 0;                                   // scales: a byte for each of a token half's four blocks; of the weights (SwiGLU: gate, up)
-    int fo[2][2];                                        // [block parity][piece g / 4 + g]
+        for (int j = 0; j < 2 * NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x8 af[4], bf[2 * NB];                                  // the present token half's blocks; weights
+    int sa[2], sw = 0;                                   // scales: a byte for each of a token half's four blocks; of the weights (SwiGLU: gate, up; else per 32 outputs)
+    int fo[2][2], fb[2][2];                              // [block parity][piece g / 4 + g]; of the wave's blocks of weights
     const int r16 = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int par = 0; par < 2; ++par)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) fo[par][q] = piece_off(par * 16 + r16, q * 4 + g) - par * 16 * kBlk;
-    auto frag = [&](const uint8_t *slot, int row0, int blk) __attribute__((always_inline)) {
-        const uint8_t *s = slot + (row0 + blk * 16) * kBlk;
+        for (int q = 0; q < 2; ++q) {
+            fo[par][q] = piece_off(par * 16 + r16, q * 4 + g) - par * 16 * kBlk;
+            const int pb = (par + wn * NB) & 1;
+            fb[par][q] = piece_off(pb * 16 + r16, q * 4 + g) - pb * 16 * kBlk;
+        }
+    auto frag = [&](const uint8_t *slot, int blk) __attribute__((always_inline)) {
+        const uint8_t *s = slot + (wm * 64 + blk * 16) * kBlk;
         return join(*(const i32x4 *)(s + fo[blk & 1][0]), *(const i32x4 *)(s + fo[blk & 1][1]));
+    };
+    auto frag_b = [&](const uint8_t *slot, int blk) __attribute__((always_inline)) {
+        const uint8_t *s = slot + (wn * NB + blk) * 16 * kBlk;
+        return join(*(const i32x4 *)(s + fb[blk & 1][0]), *(const i32x4 *)(s + fb[blk & 1][1]));
     };
     auto read_b = [&](auto half, const uint8_t *slot) __attribute__((always_inline)) {
         constexpr int h = decltype(half)::value;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) bf[4 * h + c] = frag(slot, wn * 64, c);
+        for (int c = 0; c < NB; ++c) bf[NB * h + c] = frag_b(slot, c);
     };
     auto read_sa = [&](auto half, int kt) __attribute__((always_inline)) {
         constexpr int h = decltype(half)::value;
         sa[h] = *(const int *)(pa + (kt - base) * 256 + ((h * 2 + wm) * 16 + r16) * 4);
     };
     auto weight_scale = [&](int kt) __attribute__((always_inline)) -> int {
-        if (SWIGLU) return *(const uint16_t *)(pw + kt * 2);
-        return pw[kt * 2 + wn];
+        if (SWIGLU) return *(const uint16_t *)(pw + kt * NW);
+        return *(const int *)(pw + kt * NW + wn * 4);
     };
     auto mul = [&](auto ah, auto bh, auto block, auto col) __attribute__((always_inline)) {
         constexpr int h = decltype(ah)::value, q = decltype(bh)::value, b = decltype(block)::value, c = decltype(col)::value;
-        mfma_acc<SWIGLU ? q : 0, b>(bf[4 * q + c], af[b], acc[4 * h + b][4 * q + c], sw, sa[h]);
+        mfma_acc<SWIGLU ? q : (NB * q + c) / 2, b>(bf[NB * q + c], af[b], acc[4 * h + b][NB * q + c], sw, sa[h]);
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto mul4 = [&](auto ah, auto bh, auto block) __attribute__((always_inline)) { each<4>([&](auto c) __attribute__((always_inline)) { mul(ah, bh, block, c); }); };
+    auto mul_row = [&](auto ah, auto bh, auto block) __attribute__((always_inline)) { each<NB>([&](auto c) __attribute__((always_inline)) { mul(ah, bh, block, c); }); };
     auto hand_over = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
-        wait_vmcnt_lgkm0<16>();
+        wait_vmcnt_lgkm0<2 * LOADS>();
         lds_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -419,62 +431,64 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         constexpr int fh = decltype(F)::value;
         using FH = std::integral_constant<int, fh>;
         using SH = std::integral_constant<int, 1 - fh>;
-        mul4(I0{}, FH{}, I0{});
+        mul_row(I0{}, FH{}, I0{});
         hand_over();                                     // a0 and f have been read; a1 and s have landed
-        each<12>([&](auto step) __attribute__((always_inline)) {
-            constexpr int t = decltype(step)::value;
-            mul(I0{}, FH{}, std::integral_constant<int, 1 + t / 4>{}, std::integral_constant<int, t % 4>{});
-            if (t < 4) bf[4 * SH::value + t % 4] = frag(s, wn * 64, t % 4);
-            if (t == 4) read_sa(I1{}, kt);
-            if (t >= 4 && t < 8) load_b(kt + 2, fh, t - 4, f);
-            if (t >= 8) load_a(kt + 2, 0, t - 8, a0);
+        each<3 * NB>([&](auto step) __attribute__((always_inline)) {
+            constexpr int t = decltype(step)::value, l = t - (3 * NB - LOADS);
+            mul(I0{}, FH{}, std::integral_constant<int, 1 + t / NB>{}, std::integral_constant<int, t % NB>{});
+            if (t < NB) bf[NB * SH::value + t % NB] = frag_b(s, t % NB);
+            if (t == NB) read_sa(I1{}, kt);
+            if (l >= 0 && l < NB) load_b(kt + 2, fh, l, f);
+            if (l >= NB) load_a(kt + 2, 0, l - NB, a0);
             __builtin_amdgcn_sched_barrier(0);
         });
         each<4>([&](auto b) __attribute__((always_inline)) {
-            mul4(I0{}, SH{}, b);
-            af[b] = frag(a1, wm * 64, b);
+            mul_row(I0{}, SH{}, b);
+            af[b] = frag(a1, b);
             __builtin_amdgcn_sched_barrier(0);
         });
-        mul4(I1{}, SH{}, I0{});
+        mul_row(I1{}, SH{}, I0{});
         hand_over();                                     // a1 and s have been read; the next tile's first halves have landed
         int sw1 = 0;
-        each<12>([&](auto step) __attribute__((always_inline)) {
+        each<3 * NB>([&](auto step) __attribute__((always_inline)) {
             constexpr int t = decltype(step)::value;
-            mul(I1{}, SH{}, std::integral_constant<int, 1 + t / 4>{}, std::integral_constant<int, t % 4>{});
+            mul(I1{}, SH{}, std::integral_constant<int, 1 + t / NB>{}, std::integral_constant<int, t % NB>{});
             if (t == 0) read_sa(I0{}, kt + 1);
             if (t == 1) sw1 = weight_scale(kt + 1 - base);
-            if (t < 4) load_b(kt + 2, 1 - fh, t, s);
-            if (t >= 4 && t < 8) load_a(kt + 2, 1, t - 4, a1);
+            if (t < NB) load_b(kt + 2, 1 - fh, t, s);
+            if (t >= NB && t < LOADS) load_a(kt + 2, 1, t - NB, a1);
             __builtin_amdgcn_sched_barrier(0);
         });
         each<4>([&](auto b) __attribute__((always_inline)) {
-            each<4>([&](auto c) __attribute__((always_inline)) {
+            each<NB>([&](auto c) __attribute__((always_inline)) {
                 mul(I1{}, FH{}, b, c);
-                if (b == 0) bf[4 * SH::value + c] = frag(nb, wn * 64, c);
+                if (b == 0) bf[NB * SH::value + c] = frag_b(nb, c);
             });
-            af[b] = frag(na, wm * 64, b);
+            af[b] = frag(na, b);
             __builtin_amdgcn_sched_barrier(0);
         });
         sw = sw1;
     };
-    int wblk[2];
-    if (SWIGLU) { wblk[0] = n0 / kBlk; wblk[1] = (p.F + n0) / kBlk; }
-    else { wblk[0] = n0 / kBlk; wblk[1] = (n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk; }
+    auto wblk = [&](int i) __attribute__((always_inline)) {
+        if (SWIGLU) return i ? (p.F + n0) / kBlk : n0 / kBlk;
+        const int n = n0 + (i >> 2) * (BN / 2) + (i & 3) * 32;
+        return (n < p.N ? n : p.N - 1) / kBlk;
+    };
     fetch_b(0, 0, B00); fetch_a(0, 0, A00); fetch_b(0, 1, B01); fetch_a(0, 1, A01);           // in the loop's order
     fetch_b(1, 1, B11); fetch_a(1, 0, A10); fetch_b(1, 0, B10); fetch_a(1, 1, A11);
-    stage_scales<256, 4, 2, 256>(p, pa, pw, m0, wblk, 0, nk < kPanel ? nk : kPanel, tid);
-    wait_vmcnt_lgkm0<24>();
+    stage_scales<256, 4, NW, 256>(p, pa, pw, m0, wblk, 0, nk < kPanel ? nk : kPanel, tid);
+    wait_vmcnt_lgkm0<3 * LOADS>();
     lds_barrier();
     read_b(I0{}, B00);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) af[b] = frag(A00, wm * 64, b);
+    for (int b = 0; b < 4; ++b) af[b] = frag(A00, b);
     read_sa(I0{}, 0);
     sw = weight_scale(0);
     for (int kt = 0; kt < nk; kt += 2) {                 // an odd count is rounded up with a tile of zeros
         if (kt - base == kSegment) {                     // the next panel of scales (this tile's first ones have been read from the old one, which goes further)
             base = kt;
             __syncthreads();
-            stage_scales<256, 4, 2, 256>(p, pa, pw, m0, wblk, base, nk - base < kPanel ? nk - base : kPanel, tid);
+            stage_scales<256, 4, NW, 256>(p, pa, pw, m0, wblk, base, nk - base < kPanel ? nk - base : kPanel, tid);
             __syncthreads();
         }
         tile(kt, I0{}, A00, A01, B00, B01, B11, A10);
@@ -484,7 +498,7 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+        for (int j = 0; j < 2 * NB; ++j) asm volatile("" : "+a"(acc[i][j]));
     dma_publish_barrier();                               // what is still in flight must land before LDS is used again
     const int mrow = m0 + wm * 64 + r16;
     if constexpr (!SWIGLU) {
@@ -494,13 +508,13 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
                 int m = mrow + (i >> 2) * 128 + (i & 3) * 16;
                 asm volatile("" : "+v"(m));              // (row after row: together their copies and conditions would not fit the registers)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+                for (int j = 0; j < 2 * NB; ++j) asm volatile("" : "+a"(acc[i][j]));
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < NB; ++q) {
                     float v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = acc[i][2 * q + (e >> 2)][e & 3];
-                    store(m, n0 + wn * 128 + 32 * q + 8 * g, v);
+                    store(m, n0 + wn * (BN / 2) + 32 * q + 8 * g, v);
                 }
             }
         };
@@ -510,8 +524,8 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         swiglu_epilogue<8, 256>(p, acc, (unsigned *)A00, m0, n0, wn, g, [&](int i) { return wm * 64 + (i >> 2) * 128 + (i & 3) * 16 + r16; });
     }
 }
-template <bool SWIGLU, bool TAIL>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void gemm_fp8_big_kernel(Fp8Params p) { fp8_big_body<SWIGLU, TAIL>(p); }
+template <int BN, bool SWIGLU, bool TAIL>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void gemm_fp8_big_kernel(Fp8Params p) { fp8_big_body<BN, SWIGLU, TAIL>(p); }
 
 // Scheduling pattern: R LDS reads and V loads dealt to the first half of the MFMAs
 template <int R, int V, int... I> __device__ __forceinline__ void spread_over_mfmas(std::integer_sequence<int, I...>) {
@@ -606,9 +620,9 @@ __device__ __forceinline__ void fp8_ring_body(const Fp8Params &p) {
     };
     using I0 = std::integral_constant<int, 0>;
     using I1 = std::integral_constant<int, 1>;
-    int wblk[2];
-    wblk[0] = n0 / kBlk;
-    wblk[1] = SWIGLU ? (p.F + n0) / kBlk : ((n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk);
+    auto wblk = [&](int i) __attribute__((always_inline)) {
+        return i == 0 ? n0 / kBlk : SWIGLU ? (p.F + n0) / kBlk : ((n0 / kBlk + 1) * kBlk < p.N ? n0 / kBlk + 1 : n0 / kBlk);
+    };
     for (; kt0 < p.kb; kt0 += kSegment) {
         nk = p.kb - kt0 < kSegment ? p.kb - kt0 : kSegment;
 #pragma unroll
@@ -668,10 +682,12 @@ MS_FP8_RING(64, 64, 4, 1, 4);
 template __global__ void gemm_fp8_ring_kernel<128, 256, 2, 4, 2, true, false>(Fp8Params);
 template __global__ void gemm_fp8_ring_kernel<64, 256, 2, 4, 2, true, false>(Fp8Params);
 #undef MS_FP8_RING
-template __global__ void gemm_fp8_big_kernel<false, false>(Fp8Params);
-template __global__ void gemm_fp8_big_kernel<false, true>(Fp8Params);
-template __global__ void gemm_fp8_big_kernel<true, false>(Fp8Params);
-template __global__ void gemm_fp8_big_kernel<true, true>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<256, false, false>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<256, false, true>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<192, false, false>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<192, false, true>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<256, true, false>(Fp8Params);
+template __global__ void gemm_fp8_big_kernel<256, true, true>(Fp8Params);
 
 bool aligned(const void *p, int to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
@@ -716,10 +732,10 @@ template <int BM, int BN, int WM, int WN, int NST, bool SWIGLU, bool PRECISE> bo
     if (tiles) gemm_fp8_ring_kernel<BM, BN, WM, WN, NST, SWIGLU, PRECISE><<<tiles, 64 * WM * WN, 0, s>>>(p);
     return tiles != 0;
 }
-template <bool SWIGLU> bool launch_big(Fp8Params &p, hipStream_t s) {
-    const int tiles = tiles_of(p, 256, SWIGLU ? 128 : 256, SWIGLU ? p.F : p.N, 256);
-    if (tiles && p.K % kBlk) gemm_fp8_big_kernel<SWIGLU, true><<<tiles, 256, 0, s>>>(p);
-    else if (tiles) gemm_fp8_big_kernel<SWIGLU, false><<<tiles, 256, 0, s>>>(p);
+template <int BN, bool SWIGLU> bool launch_big(Fp8Params &p, hipStream_t s) {
+    const int tiles = tiles_of(p, 256, SWIGLU ? 128 : BN, SWIGLU ? p.F : p.N, 256);
+    if (tiles && p.K % kBlk) gemm_fp8_big_kernel<BN, SWIGLU, true><<<tiles, 256, 0, s>>>(p);
+    else if (tiles) gemm_fp8_big_kernel<BN, SWIGLU, false><<<tiles, 256, 0, s>>>(p);
     return tiles != 0;
 }
 
@@ -741,8 +757,8 @@ ms_status launch_gemm(Fp8Params p, bool precise, hipStream_t s) {
     if (forced ? forced == FDIRECT : fp8_direct(p.M, p.N)) {
         if (precise) launch_direct<true>(p, s); else launch_direct<false>(p, s);
     } else {
-        const int tile = forced && !(precise && forced == F256) ? forced : precise ? fp8_choose(kFp8Precise, p.M, p.N, p.kb) : fp8_choose(kFp8Fast, p.M, p.N, p.kb);
-        fits = !precise && tile == F256 ? launch_big<false>(p, s) : precise ? launch_tile<true>(tile, p, s) : launch_tile<false>(tile, p, s);
+        const int tile = forced && !(precise && (forced == F256 || forced == F192)) ? forced : precise ? fp8_choose(kFp8Precise, p.M, p.N, p.kb) : fp8_choose(kFp8Fast, p.M, p.N, p.kb);
+        fits = !precise && tile == F256 ? launch_big<256, false>(p, s) : !precise && tile == F192 ? launch_big<192, false>(p, s) : precise ? launch_tile<true>(tile, p, s) : launch_tile<false>(tile, p, s);
     }
     if (!fits) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8: %d x %d is too large for one launch", p.M, p.N);
     MS_LAUNCH_CHECK();
@@ -753,7 +769,7 @@ ms_status launch_gemm(Fp8Params p, bool precise, hipStream_t s) {
 bool swiglu_fused(int M, int F, int K, long ldw) { return M > kFp8DirectRows && F % kBlk == 0 && ms_buffer_range_ok(2L * F, K, ldw, 1); }
 bool launch_swiglu(Fp8Params &p, hipStream_t s) {
     const int forced = g_tile.load(), tile = forced ? forced : fp8_choose(kFp8Swiglu, p.M, p.N, p.kb);
-    if (tile == F256) return launch_big<true>(p, s);
+    if (tile == F256 || tile == F192) return launch_big<256, true>(p, s);
     if (tile == F128 || tile == F128R) return launch_ring<128, 256, 2, 4, 2, true, false>(p, s);
     return launch_ring<64, 256, 2, 4, 2, true, false>(p, s);
 }
@@ -761,7 +777,7 @@ bool launch_swiglu(Fp8Params &p, hipStream_t s) {
 }  // namespace
 
 extern "C" ms_status ms_k_gemm_fp8_config(int32_t tile) {
-    if (tile != 0 && tile != F256 && tile != F128 && tile != F128R && tile != F64x128 && tile != F64x128R && tile != F64 && tile != FDIRECT)
+    if (tile != 0 && tile != F256 && tile != F192 && tile != F128 && tile != F128R && tile != F64x128 && tile != F64x128R && tile != F64 && tile != FDIRECT)
         return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8_config: unknown tile %d", tile);
     g_tile = tile;
     return MS_OK;

@@ -392,3 +392,16 @@ def test_residual_beside_the_result():
     ref = B.k_gemm_fp8(a, sa, w, sw, residual=r.clone())
     B.k_gemm_fp8(a, sa, w, sw, residual=r, c=both[:, :32])
     assert torch.equal(both[:, :32], ref)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [s for s in SHAPES if s[0] > 1] + [(70, 191, 256), (70, 193, 256), (300, 448, 1152), (520, 1345, 384)])
+def test_tile_of_192_outputs_gives_the_same_bits(m, n, k, fp8_tile):
+    """Its wave columns begin and end inside the weights' scale blocks."""
+    a, w = operands(m, n, k)
+    res = normal(f"r{m}{n}", (m, n), 1.0)
+    calls = [lambda: B.k_gemm_fp8(*a, *w), lambda: B.k_gemm_fp8(*a, *w, residual=res), lambda: B.k_gemm_fp8(*a, *w, residual=res, c_fp32=True, fast_sums=True)]
+    fp8_tile(128128)
+    want = [f() for f in calls]
+    fp8_tile(256192)
+    assert all(torch.equal(f(), x) for f, x in zip(calls, want))
