@@ -29,6 +29,15 @@ __device__ __forceinline__ unsigned fp8_pack4(float a, float b, float c, float d
     return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
+// Maximum over 16 lanes, which are a row of the wave: by the vector ALU's lane permutations (pairs, quads, halves, mirror image), without a trip
+// through LDS
+__device__ __forceinline__ unsigned fp8_max16(unsigned m) {
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, true));        // quad_perm 1 0 3 2
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xf, 0xf, true));        // quad_perm 2 3 0 1
+    m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xf, 0xf, true));       // row_half_mirror
+    return max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x140, 0xf, 0xf, true));    // row_mirror
+}
+
 // Eight consecutive columns per lane, 16 lanes per block: codes and scale byte of the block
 __device__ __forceinline__ uint2 fp8_quantize8(const float *v, int *byte) {
     unsigned m = 0;
@@ -39,8 +48,7 @@ __device__ __forceinline__ uint2 fp8_quantize8(const float *v, int *byte) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) m = max(m, fp8_finite_bits(v[e]));
     }
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, o, 64));
+    m = fp8_max16(m);
     *byte = fp8_scale_byte(m);
     const float s = fp8_inverse_scale(*byte);
     return make_uint2(fp8_pack4(v[0] * s, v[1] * s, v[2] * s, v[3] * s), fp8_pack4(v[4] * s, v[5] * s, v[6] * s, v[7] * s));
@@ -48,8 +56,8 @@ __device__ __forceinline__ uint2 fp8_quantize8(const float *v, int *byte) {
 // The four blocks of a wave, as the word of their scales: blocks past the last one get 127
 __device__ __forceinline__ unsigned fp8_scale_word(int byte, int block, int blocks) {
     const unsigned v = block < blocks ? (unsigned)byte : 127u;
-    return (unsigned)__shfl((int)v, 0, 64) | (unsigned)__shfl((int)v, 16, 64) << 8 | (unsigned)__shfl((int)v, 32, 64) << 16 |
-           (unsigned)__shfl((int)v, 48, 64) << 24;
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 0) | (unsigned)__builtin_amdgcn_readlane((int)v, 16) << 8 |
+           (unsigned)__builtin_amdgcn_readlane((int)v, 32) << 16 | (unsigned)__builtin_amdgcn_readlane((int)v, 48) << 24;
 }
 
 template <class T> __device__ __forceinline__ void fp8_load8(const T *p, float *v) {

@@ -88,7 +88,9 @@ __global__ __launch_bounds__(256) void norm_fp8_kernel(const TX *__restrict__ x,
     }
 }
 
-// 128 x 128 blocks: one workgroup each, the block in registers between its maximum and its codes
+// 128 x 128 blocks: one workgroup each, the block in registers between its maximum and its codes, which leave non-temporally (22016 x 4096 53.1 ->
+// 51.6 us, 5.2 TB/s, 4096 x 11008 30.4 -> 26.6; rows, which a product reads next, are 2 % slower so)
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 template <class T>
 __global__ __launch_bounds__(256) void fp8_blocks_kernel(const T *__restrict__ x, long ldx, uint8_t *__restrict__ q, long ldq, uint8_t *__restrict__ s, long lds,
                                                          int n, int k) {
@@ -118,8 +120,8 @@ __global__ __launch_bounds__(256) void fp8_blocks_kernel(const T *__restrict__ x
     for (int i = 0; i < 8; ++i) {
         const long row = rb * 128 + i * 16 + (tid >> 4);
         if (row < n && c < k)
-            *(uint2 *)(q + row * ldq + c) = make_uint2(fp8_pack4(v[i][0] * is, v[i][1] * is, v[i][2] * is, v[i][3] * is),
-                                                       fp8_pack4(v[i][4] * is, v[i][5] * is, v[i][6] * is, v[i][7] * is));
+            __builtin_nontemporal_store(u32x2{fp8_pack4(v[i][0] * is, v[i][1] * is, v[i][2] * is, v[i][3] * is),
+                                              fp8_pack4(v[i][4] * is, v[i][5] * is, v[i][6] * is, v[i][7] * is)}, (u32x2 *)(q + row * ldq + c));
     }
     const int last = kb + 1 == blocks ? (blocks + 3) / 4 * 4 : kb + 1;       // the row's padding gets 127
     if (tid < last - kb) s[rb * lds + kb + tid] = (uint8_t)(tid == 0 ? byte : 127);
