@@ -37,7 +37,25 @@ __global__ __launch_bounds__(256) void fp8_rows_kernel(const T *__restrict__ x, 
     }
 }
 
-// RMSNorm, then the same: one wave per row, NC x 512 columns of it in registers (wider rows are read again)
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+// Eight columns as they are stored
+template <class T> struct Row8 { Vec16<T> h[8 / Vec16<T>::N]; };
+template <class T> __device__ __forceinline__ Row8<T> load8(const T *p, bool there) {
+    Row8<T> r = {};
+    if (there) {
+#pragma unroll
+        for (int i = 0; i < 8 / Vec16<T>::N; ++i) r.h[i] = ldv(p + i * Vec16<T>::N);
+    }
+    return r;
+}
+template <class T> __device__ __forceinline__ void floats(const Row8<T> &r, float *v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32(r.h[e / Vec16<T>::N].v[e % Vec16<T>::N]);
+}
+
+// RMSNorm, then the same: one wave per row, NC x 512 columns of it in registers as they are stored (wider rows are read again).  Latency bounds it
+// (loads, the row's sum, the codes), so that what counts is how many waves fit: 4096 columns of bf16 in 63 registers (32768 rows 78 us, 5.2 TB/s;
+// kept as floats in 90 it took 96), gains read again per row from L2 (held in registers across rows with the next row's loads, 208: 104).
 template <class T, class TX, int NC>
 __global__ __launch_bounds__(256) void norm_fp8_kernel(const TX *__restrict__ x, const T *__restrict__ g, uint8_t *__restrict__ q, long ldq,
                                                        uint8_t *__restrict__ s, long lds, int n, int d, float eps) {
@@ -45,15 +63,16 @@ __global__ __launch_bounds__(256) void norm_fp8_kernel(const TX *__restrict__ x,
     const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= n) return;
     const TX *xr = x + row * d;
-    float v[NC][8], ss = 0.f;
+    Row8<TX> v[NC];
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) v[i] = load8(xr + i * 512 + lane * 8, i * 512 + lane * 8 < d);
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int c = i * 512 + lane * 8;
+        float t[8];
+        floats(v[i], t);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-        if (c < d) fp8_load8(xr + c, v[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(v[i][e], v[i][e], ss);
+        for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(t[e], t[e], ss);
     }
     for (int c = NC * 512 + lane * 8; c < d; c += 512) {
         float t[8];
@@ -78,7 +97,16 @@ __global__ __launch_bounds__(256) void norm_fp8_kernel(const TX *__restrict__ x,
     };
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-        if (i < groups) emit(i, v[i]);
+        if (i < groups) {
+            float t[8];
+            if constexpr (sizeof(TX) == 2) {             // (unpacked again: as floats they would take twice the registers)
+                u32x4 raw = __builtin_bit_cast(u32x4, v[i].h[0]);
+                asm("" : "+v"(raw));
+                v[i].h[0] = __builtin_bit_cast(Vec16<TX>, raw);
+            }
+            floats(v[i], t);
+            emit(i, t);
+        }
     for (int i = NC; i < groups; ++i) {
         float t[8];
 #pragma unroll
