@@ -12,6 +12,7 @@
 // A section with options (section_options.hip; `opt` is null for one without) may also scale its embedding rows, norm its query and
 // key heads (then the unnormed qkv is kept too), and, forward only, hold its matrices in 8 bits.
 #include <math.h>
+#include <initializer_list>
 #include <vector>
 
 #include "common.h"
@@ -187,9 +188,12 @@ ms_status validate_options(const ms_section_config *c, const SectionOptions *opt
     if (o->fp8 && c->dtype != MS_BF16) return ms_fail(MS_ERR_UNSUPPORTED, "section: 8-bit matrices need bf16 activations");
     if (o->fp8 && (c->d_model % 16 || c->d_ffn % 16))
         return ms_fail(MS_ERR_UNSUPPORTED, "section: d_model=%d and d_ffn=%d must be multiples of 16 with 8-bit matrices", c->d_model, c->d_ffn);
+    if (o->fp8 && (long)c->n_q_heads * c->head_dim % 16) return ms_fail(MS_ERR_UNSUPPORTED, "section: %d heads of %d are no multiple of 16 columns, with 8-bit matrices", c->n_q_heads, c->head_dim);
+    if (o->qk_norm && (c->head_dim % 16 || c->head_dim > 512))
+        return ms_fail(MS_ERR_UNSUPPORTED, "section: head_dim=%d must be a multiple of 16 and at most 512 with query / key norms", c->head_dim);
     return MS_OK;
 }
-ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions *opt, bool backward) {
+ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions *opt, const ms_section_ptrs *weights, bool backward) {
     if (!opt) return MS_OK;
     const ms_section_options *o = opt->o;
     if (o->qk_norm && backward && !opt->grads) return ms_fail(MS_ERR_INVALID_ARG, "section: options: null gradients of the query / key norms");
@@ -198,6 +202,14 @@ ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions 
         if ((o->qk_norm && (!l.q_norm_g || !l.k_norm_g)) || (o->fp8 && (!l.s_qkv || !l.s_o || !l.s_up || !l.s_down)) ||
             (o->qk_norm && backward && (!opt->grads[i].q_norm_g || !opt->grads[i].k_norm_g)))
             return ms_fail(MS_ERR_INVALID_ARG, "section: options: null pointer in layer %d", i);
+        const ms_layer_ptrs &w = weights->layers[i];
+        auto off = [](std::initializer_list<const void *> ps, uintptr_t to) {
+            uintptr_t bits = 0;
+            for (const void *p : ps) bits |= (uintptr_t)p;
+            return bits % to != 0;
+        };
+        if ((o->qk_norm && off({l.q_norm_g, l.k_norm_g}, 16)) || (o->fp8 && (off({w.w_qkv, w.w_o, w.w_up, w.w_down}, 16) || off({l.s_qkv, l.s_o, l.s_up, l.s_down}, 4))))
+            return ms_fail(MS_ERR_UNSUPPORTED, "section: options: layer %d: gains and codes must be 16-byte, scales 4-byte aligned", i);
     }
     return MS_OK;
 }
@@ -378,7 +390,7 @@ ms_status section_forward(const ms_section_config *cfg, const SectionOptions *op
     if (batch->n_tokens == 0) return MS_OK;
     MS_TRY(validate_limits(cfg, opt, batch->n_tokens, false));
     MS_TRY(validate_ptrs(cfg, weights, "weights"));
-    MS_TRY(validate_option_ptrs(cfg, opt, false));
+    MS_TRY(validate_option_ptrs(cfg, opt, weights, false));
     if (!x_in || !h_out || !workspace_dev) return ms_fail(MS_ERR_INVALID_ARG, "section_forward: null pointer");
     Plan p = make_plan(cfg, opt, batch->n_tokens, max_seqlen, false, workspace_dev);
     if (workspace_bytes < p.bytes)
@@ -419,7 +431,7 @@ ms_status section_forward_backward(const ms_section_config *cfg, const SectionOp
     MS_TRY(validate_limits(cfg, opt, batch->n_tokens, true));
     MS_TRY(validate_ptrs(cfg, weights, "weights"));
     MS_TRY(validate_ptrs(cfg, grads, "grads"));
-    MS_TRY(validate_option_ptrs(cfg, opt, true));
+    MS_TRY(validate_option_ptrs(cfg, opt, weights, true));
     if (!x_in || !h_out || !workspace_dev || (kd && !h_teacher))
         return ms_fail(MS_ERR_INVALID_ARG, "section_forward_backward: null pointer");
     Plan p = make_plan(cfg, opt, batch->n_tokens, max_seqlen, true, workspace_dev);

@@ -287,3 +287,33 @@ def test_codes_go_with_their_option():
         B._check_matrices(cfg, {"layers": [plain]}, B.SectionOptions(fp8=True), None)
     with pytest.raises(ValueError, match="w_qkv"):
         B._check_matrices(cfg, {"layers": [dict(codes, w_qkv=codes["w_qkv"][1:])]}, B.SectionOptions(fp8=True), None)
+
+
+def test_sizes_and_alignment_are_refused_before_anything_is_launched():
+    """What the kernels behind the options would turn down in the middle of a section."""
+    lib = B.lib()
+
+    def call(qk=0, fp8=0, weights={}, options={}, backward=False, **over):
+        cfg = config("bf16", n_layers=1, **over)
+        c, host = B._cfg_c(cfg), (C.c_int32 * 2)(0, 4)
+        b = B.BatchC(4, 1, C.c_void_p(256), host)
+        lp, lo = (B.LayerPtrs * 1)(), (B.LayerOptions * 1)()
+        for f in B._LAYER_FIELDS:
+            setattr(lp[0], f, weights.get(f, 256))
+        for f in B._OPTION_FIELDS:
+            setattr(lo[0], f, options.get(f, 256))
+        w, v = B.SectionPtrs(256, lp, 256, 256), C.c_void_p(256)
+        o = B.SectionOptionsC(1.0, qk, fp8, lo)
+        if backward:
+            return lib.ms_section_forward_backward_with(C.byref(c), C.byref(o), lo, C.byref(w), C.byref(w), C.byref(b), v, v, v,
+                                                        None, None, None, None, None, None, v, C.c_size_t(16), None)
+        return lib.ms_section_forward_with(C.byref(c), C.byref(o), C.byref(w), C.byref(b), v, v, v, C.c_size_t(16), None)
+    assert call(qk=1) == -3 and call(fp8=1) == -3                            # all is right but the workspace
+    for f in ("q_norm_g", "k_norm_g"):
+        assert call(qk=1, options={f: 264}) == -4 and call(qk=1, options={f: 264}, backward=True) == -4 and call(fp8=1, options={f: 264}) == -3
+    for f in ("w_qkv", "w_o", "w_up", "w_down"):
+        assert call(fp8=1, weights={f: 264}) == -4 and call(qk=1, weights={f: 264}) == -3
+    for f in ("s_qkv", "s_o", "s_up", "s_down"):
+        assert call(fp8=1, options={f: 258}) == -4 and call(fp8=1, options={f: 260}) == -3
+    assert call(qk=1, head_dim=24) == -4 and call(qk=1, head_dim=520) == -4
+    assert call(fp8=1, n_q_heads=1, n_kv_heads=1, head_dim=24) == -4
