@@ -51,7 +51,9 @@ struct Fp8Params {
 
 // W, A: which byte of sw, sa has the exponents
 // The same with the accumulators bound to accumulation registers, where the compiler would copy them to and fro for a kernel that needs all 256.  It does
-// not see the latency: whoever reads the sums waits first.
+// not see what the instruction needs around it: whoever reads the sums waits first, and w, a, sw and sa are results of LDS reads as they come (a vector
+// instruction's result needs two idle states before it; in front of every product they cost 2 %, so they stand at the head of a K tile only,
+// where the compiler may put copies).
 template <int W, int A> __device__ __forceinline__ void mfma_acc(const i32x8 &w, const i32x8 &a, f32x4 &c, int sw, int sa) {
     asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
         : "+a"(c) : "v"(w), "v"(a), "v"(sw), "v"(sa), "n"(W & 1), "n"(A & 1), "n"(W >> 1), "n"(A >> 1));
@@ -327,7 +329,7 @@ template <int BN, bool SWIGLU, bool TAIL>
 __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
     constexpr int NB = BN / 64, LOADS = 4 + NB;          // weight blocks of a quarter; a wave's loads of an A and a B half
     static_assert(BN % 64 == 0 && NB <= 4 && (!SWIGLU || BN == 256), "tile");
-    constexpr int HA = 128 * kBlk, HB = BN / 2 * kBlk, NW = SWIGLU ? 2 : 8;       // (scales: gate, up; or a byte per wave column and 32 outputs)
+    constexpr int HA = 128 * kBlk, HB = BN / 2 * kBlk, NW = SWIGLU ? 4 : 8;       // (scales: gate, up and the same again: a word; or a byte per wave column and 32 outputs)
     __shared__ __align__(16) uint8_t A00[HA], A01[HA], A10[HA], A11[HA], B00[HB], B01[HB], B10[HB], B11[HB];
     __shared__ __align__(16) uint8_t pa[kPanel * 256], pw[kPanel * NW];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane >> 3;
@@ -407,8 +409,7 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         sa[h] = *(const int *)(pa + (kt - base) * 256 + ((h * 2 + wm) * 16 + r16) * 4);
     };
     auto weight_scale = [&](int kt) __attribute__((always_inline)) -> int {
-        if (SWIGLU) return *(const uint16_t *)(pw + kt * NW);
-        return *(const int *)(pw + kt * NW + wn * 4);
+        return *(const int *)(pw + kt * NW + (SWIGLU ? 0 : wn * 4));
     };
     auto mul = [&](auto ah, auto bh, auto block, auto col) __attribute__((always_inline)) {
         constexpr int h = decltype(ah)::value, q = decltype(bh)::value, b = decltype(block)::value, c = decltype(col)::value;
@@ -431,6 +432,7 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         constexpr int fh = decltype(F)::value;
         using FH = std::integral_constant<int, fh>;
         using SH = std::integral_constant<int, 1 - fh>;
+        asm volatile("s_nop 1");
         mul_row(I0{}, FH{}, I0{});
         hand_over();                                     // a0 and f have been read; a1 and s have landed
         each<3 * NB>([&](auto step) __attribute__((always_inline)) {
@@ -470,7 +472,7 @@ __device__ __forceinline__ void fp8_big_body(const Fp8Params &p) {
         sw = sw1;
     };
     auto wblk = [&](int i) __attribute__((always_inline)) {
-        if (SWIGLU) return i ? (p.F + n0) / kBlk : n0 / kBlk;
+        if (SWIGLU) return i & 1 ? (p.F + n0) / kBlk : n0 / kBlk;
         const int n = n0 + (i >> 2) * (BN / 2) + (i & 3) * 32;
         return (n < p.N ? n : p.N - 1) / kBlk;
     };
