@@ -193,9 +193,19 @@ ms_status validate_options(const ms_section_config *c, const SectionOptions *opt
         return ms_fail(MS_ERR_UNSUPPORTED, "section: head_dim=%d must be a multiple of 16 and at most 512 with query / key norms", c->head_dim);
     return MS_OK;
 }
-ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions *opt, const ms_section_ptrs *weights, bool backward) {
+ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions *opt, const ms_section_ptrs *weights, const ms_section_ptrs *grads) {
     if (!opt) return MS_OK;
     const ms_section_options *o = opt->o;
+    const bool backward = grads != nullptr;
+    auto off = [](std::initializer_list<const void *> ps, uintptr_t to) {
+        uintptr_t bits = 0;
+        for (const void *p : ps) bits |= (uintptr_t)p;
+        return bits % to != 0;
+    };
+    // (the scatter-add of a section without options takes any fp32 gradient; the sorted one would refuse it behind everything else)
+    if (c->vocab > 0 && ((backward && off({grads->embedding}, 16)) || (o->embed_scale != 1.f && off({weights->embedding}, 16))))
+        return ms_fail(MS_ERR_UNSUPPORTED, "section: options: the embedding's gradient, and its rows if they are scaled, must be 16-byte aligned");
+    if (off({weights->final_norm_g}, 16)) return ms_fail(MS_ERR_UNSUPPORTED, "section: options: final norm: gains must be 16-byte aligned");
     if (o->qk_norm && backward && !opt->grads) return ms_fail(MS_ERR_INVALID_ARG, "section: options: null gradients of the query / key norms");
     for (int i = 0; i < c->n_layers && (o->qk_norm || o->fp8); ++i) {
         const ms_layer_options &l = o->layers[i];
@@ -203,12 +213,8 @@ ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions 
             (o->qk_norm && backward && (!opt->grads[i].q_norm_g || !opt->grads[i].k_norm_g)))
             return ms_fail(MS_ERR_INVALID_ARG, "section: options: null pointer in layer %d", i);
         const ms_layer_ptrs &w = weights->layers[i];
-        auto off = [](std::initializer_list<const void *> ps, uintptr_t to) {
-            uintptr_t bits = 0;
-            for (const void *p : ps) bits |= (uintptr_t)p;
-            return bits % to != 0;
-        };
-        if ((o->qk_norm && off({l.q_norm_g, l.k_norm_g}, 16)) || (o->fp8 && (off({w.w_qkv, w.w_o, w.w_up, w.w_down}, 16) || off({l.s_qkv, l.s_o, l.s_up, l.s_down}, 4))))
+        if ((o->qk_norm && off({l.q_norm_g, l.k_norm_g}, 16)) ||
+            (o->fp8 && (off({w.norm1_g, w.norm2_g, w.w_qkv, w.w_o, w.w_up, w.w_down}, 16) || off({l.s_qkv, l.s_o, l.s_up, l.s_down}, 4))))
             return ms_fail(MS_ERR_UNSUPPORTED, "section: options: layer %d: gains and codes must be 16-byte, scales 4-byte aligned", i);
     }
     return MS_OK;
@@ -390,7 +396,7 @@ ms_status section_forward(const ms_section_config *cfg, const SectionOptions *op
     if (batch->n_tokens == 0) return MS_OK;
     MS_TRY(validate_limits(cfg, opt, batch->n_tokens, false));
     MS_TRY(validate_ptrs(cfg, weights, "weights"));
-    MS_TRY(validate_option_ptrs(cfg, opt, weights, false));
+    MS_TRY(validate_option_ptrs(cfg, opt, weights, nullptr));
     if (!x_in || !h_out || !workspace_dev) return ms_fail(MS_ERR_INVALID_ARG, "section_forward: null pointer");
     Plan p = make_plan(cfg, opt, batch->n_tokens, max_seqlen, false, workspace_dev);
     if (workspace_bytes < p.bytes)
@@ -431,7 +437,7 @@ ms_status section_forward_backward(const ms_section_config *cfg, const SectionOp
     MS_TRY(validate_limits(cfg, opt, batch->n_tokens, true));
     MS_TRY(validate_ptrs(cfg, weights, "weights"));
     MS_TRY(validate_ptrs(cfg, grads, "grads"));
-    MS_TRY(validate_option_ptrs(cfg, opt, weights, true));
+    MS_TRY(validate_option_ptrs(cfg, opt, weights, grads));
     if (!x_in || !h_out || !workspace_dev || (kd && !h_teacher))
         return ms_fail(MS_ERR_INVALID_ARG, "section_forward_backward: null pointer");
     Plan p = make_plan(cfg, opt, batch->n_tokens, max_seqlen, true, workspace_dev);

@@ -317,3 +317,32 @@ def test_sizes_and_alignment_are_refused_before_anything_is_launched():
         assert call(fp8=1, options={f: 258}) == -4 and call(fp8=1, options={f: 260}) == -3
     assert call(qk=1, head_dim=24) == -4 and call(qk=1, head_dim=520) == -4
     assert call(fp8=1, n_q_heads=1, n_kv_heads=1, head_dim=24) == -4
+
+
+def test_pointers_of_embedding_and_norms_are_refused_before_anything_is_launched():
+    """The sorted gradient is a backward call's last kernel, so that its refusal would leave all other gradients added up."""
+    lib = B.lib()
+
+    def call(qk=0, fp8=0, scale=1.0, weights={}, embedding=256, grad=256, final=256, backward=False, vocab=500):
+        cfg = config("bf16", n_layers=1, vocab=vocab)
+        c, host = B._cfg_c(cfg), (C.c_int32 * 2)(0, 4)
+        b = B.BatchC(4, 1, C.c_void_p(256), host)
+        lp, lo = (B.LayerPtrs * 1)(), (B.LayerOptions * 1)()
+        for f in B._LAYER_FIELDS:
+            setattr(lp[0], f, weights.get(f, 256))
+        for f in B._OPTION_FIELDS:
+            setattr(lo[0], f, 256)
+        w, g, v = B.SectionPtrs(embedding, lp, final, 256), B.SectionPtrs(grad, lp, 256, 256), C.c_void_p(256)
+        o = B.SectionOptionsC(scale, qk, fp8, lo)
+        if backward:
+            return lib.ms_section_forward_backward_with(C.byref(c), C.byref(o), lo, C.byref(w), C.byref(g), C.byref(b), v, v, v,
+                                                        None, None, None, None, None, None, v, C.c_size_t(16), None)
+        return lib.ms_section_forward_with(C.byref(c), C.byref(o), C.byref(w), C.byref(b), v, v, v, C.c_size_t(16), None)
+    assert call() == -3 and call(backward=True) == -3 and call(fp8=1) == -3              # all is right but the workspace
+    assert call(backward=True, grad=260) == -4 and b"embedding" in lib.ms_last_error()
+    assert call(scale=2.0, embedding=264) == -4 and call(scale=2.0, embedding=264, backward=True) == -4
+    assert call(embedding=264) == -3 and call(embedding=264, backward=True) == -3        # rows as they are may begin anywhere
+    assert call(vocab=0, grad=260, backward=True) == -3                                  # not an embedding's
+    assert call(final=264) == -4 and call(final=264, backward=True) == -4
+    for f in ("norm1_g", "norm2_g"):
+        assert call(fp8=1, weights={f: 264}) == -4 and f"layer 0".encode() in lib.ms_last_error()
