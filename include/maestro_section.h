@@ -144,7 +144,7 @@ ms_status ms_section_forward_backward(const ms_section_config *cfg, const ms_sec
                                       void *stream);
 
 /* Decoder sections with options; the calls are those above otherwise (options == NULL: exactly those).
- *   embed_scale  the embedding rows times this number are the first layer's input (1: as they are)
+ *   embed_scale  the embedding rows times this number are the first layer's input (1: as they are, the only value for a section with vocab == 0)
  *   qk_norm      != 0: every query and key head is RMSNormed before its rotation, with gains q_norm_g, k_norm_g [head_dim] of
  *                `dtype` in each layer and the section's norm_eps; option_grads has their gradients (fp32, accumulated)
  *   fp8          != 0: the matrices w_qkv, w_o, w_up, w_down are e4m3 codes with scale bytes s_qkv .. s_down for blocks of 128 x 128, as

@@ -183,6 +183,7 @@ ms_status validate_options(const ms_section_config *c, const SectionOptions *opt
     const ms_section_options *o = opt->o;
     if (c->arch != MS_DECODER) return ms_fail(MS_ERR_UNSUPPORTED, "section: options are for decoders");
     if (!(o->embed_scale > -INFINITY && o->embed_scale < INFINITY)) return ms_fail(MS_ERR_INVALID_ARG, "section: embed_scale is not finite");
+    if (c->vocab == 0 && o->embed_scale != 1.f) return ms_fail(MS_ERR_INVALID_ARG, "section: embed_scale=%g in a section that embeds nothing", o->embed_scale);
     if ((o->qk_norm || o->fp8) && !o->layers) return ms_fail(MS_ERR_INVALID_ARG, "section: options without layers");
     if (o->fp8 && backward) return ms_fail(MS_ERR_UNSUPPORTED, "section: 8-bit matrices are for forward-only sections");
     if (o->fp8 && c->dtype != MS_BF16) return ms_fail(MS_ERR_UNSUPPORTED, "section: 8-bit matrices need bf16 activations");

@@ -346,3 +346,14 @@ def test_pointers_of_embedding_and_norms_are_refused_before_anything_is_launched
     assert call(final=264) == -4 and call(final=264, backward=True) == -4
     for f in ("norm1_g", "norm2_g"):
         assert call(fp8=1, weights={f: 264}) == -4 and f"layer 0".encode() in lib.ms_last_error()
+
+
+def test_a_scale_without_an_embedding_is_refused():
+    cfg, o = B._cfg_c(config("bf16", vocab=0)), B.SectionOptionsC(2.0, 0, 0, None)
+    assert B.lib().ms_section_workspace_bytes_with(C.byref(cfg), C.byref(o), 4, 4, 0) == 0 and b"embeds nothing" in B.lib().ms_last_error()
+    o.embed_scale = 1.0
+    assert B.lib().ms_section_workspace_bytes_with(C.byref(cfg), C.byref(o), 4, 4, 0) > 0
+    host, v = (C.c_int32 * 2)(0, 4), C.c_void_p(256)
+    b, o.embed_scale = B.BatchC(4, 1, C.c_void_p(256), host), 2.0
+    assert B.lib().ms_section_forward_with(C.byref(cfg), C.byref(o), None, C.byref(b), v, v, v, C.c_size_t(16), None) == -1
+    assert b"embeds nothing" in B.lib().ms_last_error()
