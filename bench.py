@@ -279,7 +279,7 @@ def side_measurements(args, torch, B, wl, dev, work, tw, sw, wt, ws, ids, batch,
         bt = B.Batch([4096 * i for i in range(k + 1)])
         ids_k = wl.randint(0, "sweep.ids", nt, 0, t_cfg.vocab, dev)
         need = B.section_workspace_bytes(t_cfg, nt, 4096, False)
-        wsk = B.workspace(need, dev, "sweep")
+        wsk = B.workspace(need, dev)
         sec_k, _ = timed(torch, lambda: B.section_forward(t_cfg, tw, bt, ids_k, ws=wsk), max(3, args.steps // 2))
         sweep.append({"samples": k, "tokens": nt, "tokens_per_s": nt / sec_k, "workspace_bytes": need})
     # the student's AdamW update over all its parameters (outside the timed step: the metric is the KD step)
@@ -477,7 +477,6 @@ def main():
     kd_metric = "KD step tokens/s (teacher fwd + student fwd+bwd + fused KL loss), 1 GPU"
 
     def free():
-        B._ws_cache.clear()
         torch.cuda.empty_cache()
 
     def run_one(name, head):

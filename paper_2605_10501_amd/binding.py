@@ -131,15 +131,11 @@ def zero_grads(weights):
     return g
 
 
-_ws_cache = {}
-
-
-def workspace(nbytes, device="cuda", tag="default"):
-    """A cached byte buffer of at least nbytes (grown on demand)."""
-    buf = _ws_cache.get(tag)
-    if buf is None or buf.numel() < nbytes:
-        _ws_cache[tag] = buf = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
-    return buf
+def workspace(nbytes, device="cuda", tag=None):
+    """A byte buffer of at least nbytes, the caller's own (whatever the tag): PyTorch's allocator gives the memory to nobody else
+    before the current stream is done with it, or while a graph that is being captured may be replayed.  One kept here
+    would be shared by calls on two streams, a teacher's and a student's for instance."""
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
 _OPTION_FIELDS = ["q_norm_g", "k_norm_g", "s_qkv", "s_o", "s_up", "s_down"]

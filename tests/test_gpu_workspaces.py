@@ -1,0 +1,78 @@
+"""Calls that are given no workspace: each has its own, so that streams and captured graphs share nothing."""
+import pytest
+import torch
+
+from paper_2605_10501_amd import binding as B
+from paper_2605_10501_amd import workloads as wl
+
+
+def test_buffers_in_use_are_distinct_and_on_their_device():
+    a, b = B.workspace(1000, "cpu", "norm"), B.workspace(500, "cpu", "norm")
+    assert a.data_ptr() != b.data_ptr() and a.numel() >= 1000 and b.numel() >= 500
+    assert B.workspace(10, "meta", "norm").device.type == "meta" and B.workspace(10, "cpu", "norm").device.type == "cpu"
+    assert B.workspace(0, "cpu").numel() > 0
+
+
+def sections():
+    """A teacher in 8 bits and a student with norms and scale: (teacher call, student call), both without workspaces."""
+    t = wl.SectionConfig(arch="decoder", dtype="bf16", n_layers=3, d_model=512, n_q_heads=4, n_kv_heads=2, head_dim=64, d_ffn=1408, vocab=500)
+    s = wl.SectionConfig(arch="decoder", dtype="bf16", n_layers=2, d_model=256, n_q_heads=4, n_kv_heads=2, head_dim=64, d_ffn=688, vocab=500)
+    batch = B.Batch(wl.cu_seqlens_of([700, 1, 333, 514]))
+    ids = wl.randint(3, "ids", batch.n_tokens, 0, 500, "cuda")
+    tw8, layers = B.quantize_section(wl.section_weights(t, 3, "wt", "cuda"))
+    sw = wl.section_weights(s, 3, "ws", "cuda")
+    topt = B.SectionOptions(embed_scale=2.0, fp8=True, layers=layers)
+    gains = [{k: wl.normal(3, f"{k}{i}", (64,), 0.2, 1.0, torch.bfloat16, "cuda") for k in ("q_norm_g", "k_norm_g")} for i in range(2)]
+    sopt = B.SectionOptions(embed_scale=3.0, qk_norm=True, layers=gains)
+    dh = wl.normal(3, "dh", (batch.n_tokens, 256), 1.0, 0.0, torch.bfloat16, "cuda")
+
+    def student():
+        grads, ngrads = B.zero_grads(sw), [{k: torch.zeros(64, device="cuda") for k in g} for g in gains]
+        out = B.section_forward_backward(s, sw, grads, batch, ids, d_h_out=dh, options=sopt, option_grads=ngrads)
+        return out["h_out"], grads["embedding"], ngrads[0]["q_norm_g"], grads["layers"][0]["norm1_g"]
+    return lambda: B.section_forward(t, tw8, batch, ids, options=topt), student
+
+
+@pytest.mark.gpu
+def test_teacher_and_student_on_two_streams():
+    teacher, student = sections()
+    want_t, want_s = teacher(), student()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        for st in (a, b):
+            st.wait_stream(torch.cuda.current_stream())
+        got_t, got_s = [], []
+        for _ in range(4):                                           # neither stream waits for the other
+            with torch.cuda.stream(a):
+                got_t.append(teacher())
+            with torch.cuda.stream(b):
+                got_s.append(student())
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, want_t) for t in got_t)
+        # (attention's dQ adds up with atomics: gradients repeat up to bf16 roundings)
+        assert all(torch.equal(x, y) for s in got_s for x, y in zip(s[:1], want_s[:1]))
+        assert all(torch.allclose(x, y, rtol=2e-2, atol=2e-2 * float(y.abs().max())) for s in got_s for x, y in zip(s[1:], want_s[1:]))
+
+
+@pytest.mark.gpu
+def test_two_graphs_captured_without_workspaces():
+    teacher, student = sections()
+    want_t, want_s = teacher(), student()
+    gt, gs = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gt):
+        out_t = teacher()
+    with torch.cuda.graph(gs):
+        out_s = student()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        out_t.zero_(), out_s[0].zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(a):
+            gt.replay()
+        with torch.cuda.stream(b):
+            gs.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out_t, want_t) and torch.equal(out_s[0], want_s[0])
+        assert torch.allclose(out_s[1], want_s[1], rtol=2e-2, atol=2e-2 * float(want_s[1].abs().max()))
+        teacher(), student()
