@@ -4,6 +4,7 @@ Argument marshalling only: every step of the path runs inside the HIP library.  
 provides device memory and the current stream.  There is no CPU fallback: if the library is
 missing, loading fails.
 """
+import contextlib
 import ctypes as C
 import os
 
@@ -70,6 +71,12 @@ def _p(t):
 
 def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _on(device):
+    """`device` as the current one: the library launches there, on its current stream."""
+    same = device.type != "cuda" or device.index == torch.cuda.current_device()
+    return contextlib.nullcontext() if same else torch.cuda.device(device)
 
 
 def _dt(dtype):
@@ -233,11 +240,13 @@ def section_forward(cfg, weights, batch, x_in, h_out=None, ws=None, options=None
         ws = workspace(section_workspace_bytes(cfg, batch.n_tokens, batch.max_seqlen, False, options), x_in.device)
     if options is not None:
         o = options.c(cfg)
-        _check(lib().ms_section_forward_with(C.byref(c), C.byref(o), C.byref(w), C.byref(b), _p(x_in), _p(h_out), _p(ws),
-                                             C.c_size_t(ws.numel()), _stream()))
+        with _on(x_in.device):
+            _check(lib().ms_section_forward_with(C.byref(c), C.byref(o), C.byref(w), C.byref(b), _p(x_in), _p(h_out), _p(ws),
+                                                 C.c_size_t(ws.numel()), _stream()))
         return h_out
-    _check(lib().ms_section_forward(C.byref(c), C.byref(w), C.byref(b), _p(x_in), _p(h_out), _p(ws),
-                                    C.c_size_t(ws.numel()), _stream()))
+    with _on(x_in.device):
+        _check(lib().ms_section_forward(C.byref(c), C.byref(w), C.byref(b), _p(x_in), _p(h_out), _p(ws),
+                                        C.c_size_t(ws.numel()), _stream()))
     return h_out
 
 
@@ -270,15 +279,17 @@ def section_forward_backward(cfg, weights, grads, batch, x_in, d_h_out=None, kd=
         ws = workspace(need, dev)
     if options is not None:
         o = options.c(cfg)
-        _check(lib().ms_section_forward_backward_with(
-            C.byref(c), C.byref(o), _layer_options(option_grads, cfg.n_layers), C.byref(w), C.byref(g), C.byref(b), _p(x_in), _p(h_out), _p(d_h_out),
+        with _on(dev):
+            _check(lib().ms_section_forward_backward_with(
+                C.byref(c), C.byref(o), _layer_options(option_grads, cfg.n_layers), C.byref(w), C.byref(g), C.byref(b), _p(x_in), _p(h_out),
+                _p(d_h_out), C.byref(kdc) if kdc is not None else None, _p(h_teacher), _p(d_w_student), _p(loss), _p(kl), _p(d_x_in),
+                _p(ws), C.c_size_t(ws.numel()), _stream()))
+        return dict(h_out=h_out, loss=loss, kl_tok=kl, d_x_in=d_x_in)
+    with _on(dev):
+        _check(lib().ms_section_forward_backward(
+            C.byref(c), C.byref(w), C.byref(g), C.byref(b), _p(x_in), _p(h_out), _p(d_h_out),
             C.byref(kdc) if kdc is not None else None, _p(h_teacher), _p(d_w_student), _p(loss), _p(kl), _p(d_x_in),
             _p(ws), C.c_size_t(ws.numel()), _stream()))
-        return dict(h_out=h_out, loss=loss, kl_tok=kl, d_x_in=d_x_in)
-    _check(lib().ms_section_forward_backward(
-        C.byref(c), C.byref(w), C.byref(g), C.byref(b), _p(x_in), _p(h_out), _p(d_h_out),
-        C.byref(kdc) if kdc is not None else None, _p(h_teacher), _p(d_w_student), _p(loss), _p(kl), _p(d_x_in),
-        _p(ws), C.c_size_t(ws.numel()), _stream()))
     return dict(h_out=h_out, loss=loss, kl_tok=kl, d_x_in=d_x_in)
 
 

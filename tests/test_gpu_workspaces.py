@@ -1,4 +1,7 @@
-"""Calls that are given no workspace: each has its own, so that streams and captured graphs share nothing."""
+"""Calls that are given no workspace: each has its own, so that streams and captured graphs share nothing.  Section calls run on the
+device of their input."""
+import contextlib
+
 import pytest
 import torch
 
@@ -11,6 +14,30 @@ def test_buffers_in_use_are_distinct_and_on_their_device():
     assert a.data_ptr() != b.data_ptr() and a.numel() >= 1000 and b.numel() >= 500
     assert B.workspace(10, "meta", "norm").device.type == "meta" and B.workspace(10, "cpu", "norm").device.type == "cpu"
     assert B.workspace(0, "cpu").numel() > 0
+
+
+@pytest.mark.parametrize("options", [None, B.SectionOptions(embed_scale=2.0)])
+def test_section_calls_make_their_input_s_device_current(options, monkeypatch):
+    seen, current = [], []
+
+    @contextlib.contextmanager
+    def on(device):
+        current.append(device)
+        yield
+        current.pop()
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: 256 if "bytes" in name else seen.append((name, list(current))) or 0
+    monkeypatch.setattr(B, "_on", on)
+    monkeypatch.setattr(B, "lib", Library)
+    monkeypatch.setattr(B, "_stream", lambda: seen.append(("stream", list(current))))
+    cfg = wl.SectionConfig(arch="decoder", dtype="bf16", n_layers=1, d_model=64, n_q_heads=1, n_kv_heads=1, head_dim=64, d_ffn=64, vocab=10)
+    w = dict(wl.section_weights(cfg, 1, "w", "cpu"))
+    batch, ids = B.Batch([0, 4], device="cpu"), torch.zeros(4, dtype=torch.int32)
+    B.section_forward(cfg, w, batch, ids, options=options)
+    B.section_forward_backward(cfg, w, B.zero_grads(w), batch, ids, d_h_out=torch.zeros(4, 64), options=options)
+    assert len(seen) == 4 and all(c == [ids.device] for _, c in seen)
 
 
 def sections():
