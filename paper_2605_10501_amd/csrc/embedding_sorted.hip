@@ -13,14 +13,13 @@
 //   3. the runs that span pieces (step 2 lists them): their partial rows are added up and go to the table.
 // HBM bounds step 2 (dx read once, touched rows read and written), launches and latency the sort.
 #include "common.h"
+#include "embedding_plan.h"
 #include "launch.h"
 #include "launch_plan.h"
 
 namespace {
 
-constexpr int kSortThreads = 1024, kWaves = kSortThreads / 64, kDigitBits = 9, kBins = 1 << kDigitBits;
-constexpr int kSmall = 4 * kSortThreads;  // tokens that one workgroup sorts in LDS
-constexpr int kMaxTokens = 1 << 24;
+constexpr int kWaves = kSortThreads / 64, kBins = 1 << kDigitBits;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ forward
@@ -369,20 +368,6 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const uint2 *__rest
     }
 }
 
-constexpr long kSmallPieces = 16384L * 256;      // vectors of dx below which pieces have 8 places
-struct SortPlan { int bits, passes, ipt, blocks, tile; };
-SortPlan sort_plan(int n, int vocab, int vpr) {
-    SortPlan p;
-    int bits = 1;
-    while (bits < 31 && (vocab >> bits) > 0) ++bits;                 // keys 0 .. vocab
-    p.passes = (bits + kDigitBits - 1) / kDigitBits;
-    p.bits = (bits + p.passes - 1) / p.passes;
-    p.ipt = n <= 128 * kSortThreads ? 1 : n <= 512 * kSortThreads ? 4 : 16;
-    p.blocks = n <= kSmall ? 1 : ms_cdiv(n, (long)p.ipt * kSortThreads);
-    // pieces of 8 places where 32 would leave the chip without work
-    p.tile = (long)n * vpr < kSmallPieces ? 8 : 32;
-    return p;
-}
 struct SortScratch { uint2 *a, *b; int *counts, *runs; float *part; size_t bytes; };
 SortScratch carve(void *ws, const SortPlan &p, int n, int d) {
     const size_t tiles = (size_t)ms_cdiv(n, p.tile);
@@ -485,16 +470,11 @@ extern "C" ms_status ms_k_embedding_sorted_backward(int32_t dtype, int32_t n, in
     }
     const int blocks = (int)((total + 255) / 256), strips = ms_cdiv(d, 256);
     const long tasks = (long)(tiles - 1) * strips;       // at most
-    const bool stream_dx = (double)n * d * ms_dtype_size(dtype) > 80e6;
-#define GO2(T, TILE, U, ST) embedding_sum_kernel<T, TILE, U, ST><<<blocks, 256, 0, s>>>(in, (const T *)dx, scale, n, vpr, vocab, d_table, sc.part, sc.runs, total)
-#define GO(T, TILE, U)                                                                    \
-    do {                                                                                  \
-        if (stream_dx) GO2(T, TILE, U, true); else GO2(T, TILE, U, false);                \
-    } while (0)
-    if (dtype == MS_BF16) { if (p.tile == 8) GO(bf16_t, 8, 8); else GO(bf16_t, 32, 4); }
-    else { if (p.tile == 8) GO(float, 8, 8); else GO(float, 32, 8); }
+    const bool stream_dx = embedding_streams_dx(n, vpr);
+#define GO(T, TILE, U, ST) embedding_sum_kernel<T, TILE, U, ST><<<blocks, 256, 0, s>>>(in, (const T *)dx, scale, n, vpr, vocab, d_table, sc.part, sc.runs, total)
+    if (dtype == MS_BF16) { if (p.tile == 8) GO(bf16_t, 8, 8, false); else if (stream_dx) GO(bf16_t, 32, 4, true); else GO(bf16_t, 32, 4, false); }
+    else { if (p.tile == 8) GO(float, 8, 8, false); else if (stream_dx) GO(float, 32, 8, true); else GO(float, 32, 8, false); }
 #undef GO
-#undef GO2
     MS_LAUNCH_CHECK();
     if (tasks > 0) {
         const int grid = (int)(tasks < 2048 ? tasks : 2048);
