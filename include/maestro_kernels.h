@@ -120,7 +120,7 @@ ms_status ms_k_rope(int32_t dtype, int32_t n, int32_t n_heads, int32_t head_dim,
  *   y = R(pos) (x (mean over the head of x^2 + eps)^-1/2 g),   g = g_q[head_dim] or g_k[head_dim] of `dtype`, shared by the heads of a kind,
  * with R and table[max_pos, head_dim / 2] as in ms_k_rope; a position outside [0, max_pos) does not rotate.  Rounded once.
  * x_stride / y_stride: elements between rows.  y == x (same stride): in place, V heads are left alone; otherwise y must not overlap
- * x and receives the V heads too.  head_dim: a multiple of 16, at most 512; 16-byte aligned rows, gains and table. */
+ * x (side by side in rows of one length is apart) and receives the V heads too.  head_dim: a multiple of 16, at most 512; 16-byte aligned rows, gains and table. */
 ms_status ms_k_qk_norm_rope_forward(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float eps,
                                     const void *x, int64_t x_stride, const void *g_q, const void *g_k, const int32_t *pos,
                                     const float *table, int32_t max_pos, void *y, int64_t y_stride, void *stream);

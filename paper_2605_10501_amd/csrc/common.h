@@ -32,6 +32,14 @@ static inline size_t ms_align_up(size_t x, size_t a = 256) { return (x + a - 1) 
 static inline int ms_cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 static inline size_t ms_dtype_size(int dtype) { return dtype == MS_BF16 ? 2 : 4; }
 
+// Two matrices of n rows with no byte in common (ps, qs bytes between rows, pw, qw bytes of a row): one behind the other, or side by side in rows of the same length
+static inline bool ms_apart(const void *p, long ps, long pw, const void *q, long qs, long qw, long n) {
+    const char *a = (const char *)p, *b = (const char *)q;
+    if (a + (n - 1) * ps + pw <= b || b + (n - 1) * qs + qw <= a) return true;
+    const long d = ps == qs ? ((b - a) % ps + ps) % ps : 0;
+    return d >= pw && d + qw <= ps;
+}
+
 // Shape limits of the kernels, in one place so that a section call can check them before its first launch.
 constexpr int kNormMaxCache = 8;   // 16-byte vectors of a row that a lane of the norm kernels keeps in registers
 static inline int ms_norm_backward_max_d(int dtype) { return 64 * kNormMaxCache * (dtype == MS_BF16 ? 8 : 4); }

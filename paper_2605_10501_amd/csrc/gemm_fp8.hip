@@ -704,14 +704,6 @@ ms_status check(const char *who, int M, int N, int K, const void *A, long lda, c
     return MS_OK;
 }
 
-// Two matrices of n rows with no byte in common: one behind the other, or side by side in rows of the same length
-bool apart(const void *p, long ps, long pw, const void *q, long qs, long qw, long n) {
-    const char *a = (const char *)p, *b = (const char *)q;
-    if (a + (n - 1) * ps + pw <= b || b + (n - 1) * qs + qw <= a) return true;
-    const long d = ps == qs ? ((b - a) % ps + ps) % ps : 0;
-    return d >= pw && d + qw <= ps;
-}
-
 template <int NI, bool PRECISE> void launch_direct(const Fp8Params &p, hipStream_t s) {
     // D = 4 where that requests no more tiles past the end than 2 does (4096 deep: 5.3 us against 6.1, 8960 deep 8.1 against 7.4)
     const int t = ms_cdiv(p.kb, kDirectWaves);
@@ -794,7 +786,7 @@ extern "C" ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *
     if (ldc < N || (residual && ldr < N)) return ms_fail(MS_ERR_SHAPE, "gemm_fp8: a row stride is less than a row");
     const int ec = c_fp32 ? 4 : 2, er = residual_fp32 ? 4 : 2;
     if (!aligned(C, ec) || (residual && !aligned(residual, er))) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8: C or residual is not aligned to its type");
-    if (residual && !(residual == C && ldr == ldc && er == ec) && !apart(C, ldc * ec, (long)N * ec, residual, ldr * er, (long)N * er, M))
+    if (residual && !(residual == C && ldr == ldc && er == ec) && !ms_apart(C, ldc * ec, (long)N * ec, residual, ldr * er, (long)N * er, M))
         return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8: the residual is neither C nor apart from it");
     Fp8Params p = {};
     p.A = (const uint8_t *)A; p.sA = (const uint8_t *)sA; p.W = (const uint8_t *)W; p.sW = (const uint8_t *)sW;

@@ -218,11 +218,6 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QknArgs a, float 
     }
 }
 
-bool overlap(const void *p, long ps, const void *q, long qs, long n, long cols, long es) {
-    const char *a = (const char *)p, *b = (const char *)q;
-    return a < b + ((n - 1) * qs + cols) * es && b < a + ((n - 1) * ps + cols) * es;
-}
-
 ms_status check(const char *who, int dtype, const QknArgs &a, bool backward) {
     if (!a.x || !a.out || !a.g_q || !a.g_k || !a.pos || !a.table || (backward && !a.dy)) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer", who);
     if (dtype != MS_BF16 && dtype != MS_F32) return ms_fail(MS_ERR_INVALID_ARG, "%s: bad dtype %d", who, dtype);
@@ -237,9 +232,9 @@ ms_status check(const char *who, int dtype, const QknArgs &a, bool backward) {
     if (a.xs % V || is % V || a.os % V || (((uintptr_t)a.x | (uintptr_t)in | (uintptr_t)a.out | (uintptr_t)a.g_q | (uintptr_t)a.g_k | (uintptr_t)a.table) & 15))
         return ms_fail(MS_ERR_UNSUPPORTED, "%s: rows, gains and table must be 16-byte aligned", who);
     const long es = ms_dtype_size(dtype);
-    if (a.out == in ? a.os != is : overlap(in, is, a.out, a.os, a.n, all, es))
+    if (a.out == in ? a.os != is : !ms_apart(in, is * es, all * es, a.out, a.os * es, all * es, a.n))
         return ms_fail(MS_ERR_INVALID_ARG, "%s: the output is neither its input nor apart from it", who);
-    if (backward && overlap(a.x, a.xs, a.out, a.os, a.n, qk, es)) return ms_fail(MS_ERR_INVALID_ARG, "%s: dx overlaps x", who);
+    if (backward && !ms_apart(a.x, a.xs * es, qk * es, a.out, a.os * es, qk * es, a.n)) return ms_fail(MS_ERR_INVALID_ARG, "%s: dx overlaps x", who);
     return MS_OK;
 }
 

@@ -210,3 +210,22 @@ def test_binding_turns_down_wrong_tensors():
         B.k_qk_norm_rope_forward(x, 2, 2, 64, g_q, g_k, EPS, pos, table)
     with pytest.raises(ValueError, match="float16"):
         B.k_qk_norm_rope_forward(x.half(), 2, 1, 64, g_q, g_k, EPS, pos, table)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_views_side_by_side_are_apart(dtype):
+    n, nq, nkv, hd = 37, 3, 1, 64
+    x, dy, g_q, g_k, pos, table = inputs(n, nq, nkv, hd, dtype)
+    a, w = (nq, nkv, hd, g_q, g_k, EPS, pos, table), x.shape[1]
+    want = B.k_qk_norm_rope_forward(x, *a)
+    both = torch.full((n, 3 * w), 7.0, dtype=dtype, device="cuda")
+    both[:, w:2 * w] = x
+    for at in (0, 2 * w):                                         # in front of and behind its input in each row
+        assert torch.equal(B.k_qk_norm_rope_forward(both[:, w:2 * w], *a, out=both[:, at:at + w]), want)
+    assert torch.equal(both[:, w:2 * w], x)
+    g = [torch.zeros(hd, device="cuda") for _ in range(4)]
+    dx = B.k_qk_norm_rope_backward(dy, x, *a, g[0], g[1])
+    both[:, :w] = dy
+    assert torch.equal(B.k_qk_norm_rope_backward(both[:, :w], both[:, w:2 * w], *a, g[2], g[3], out=both[:, 2 * w:]), dx)
+    assert torch.equal(g[0], g[2]) and torch.equal(g[1], g[3]) and torch.equal(both[:, w:2 * w], x) and torch.equal(both[:, :w], dy)
