@@ -234,7 +234,8 @@ ms_status check(const char *who, int dtype, const QknArgs &a, bool backward) {
     const long es = ms_dtype_size(dtype);
     if (a.out == in ? a.os != is : !ms_apart(in, is * es, all * es, a.out, a.os * es, all * es, a.n))
         return ms_fail(MS_ERR_INVALID_ARG, "%s: the output is neither its input nor apart from it", who);
-    if (backward && !ms_apart(a.x, a.xs * es, qk * es, a.out, a.os * es, qk * es, a.n)) return ms_fail(MS_ERR_INVALID_ARG, "%s: dx overlaps x", who);
+    // (of x the query and key heads are read; dx has the V heads too unless it is dy)
+    if (backward && !ms_apart(a.x, a.xs * es, qk * es, a.out, a.os * es, (a.out == in ? qk : all) * es, a.n)) return ms_fail(MS_ERR_INVALID_ARG, "%s: dx overlaps x", who);
     return MS_OK;
 }
 

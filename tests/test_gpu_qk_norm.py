@@ -212,6 +212,15 @@ def test_binding_turns_down_wrong_tensors():
         B.k_qk_norm_rope_forward(x.half(), 2, 1, 64, g_q, g_k, EPS, pos, table)
 
 
+def test_dx_whose_v_heads_run_into_x_is_refused():
+    """Out of place, dx's last V heads would be written over the first query heads of an x that begins behind its key heads."""
+    def bwd(dx, dy=1 << 16, x=1 << 20):                           # 4 rows of (2 + 2) heads of 64 in bf16: 512 bytes, 384 of them query and key heads
+        return B._fn("ms_k_qk_norm_rope_backward")(1, 4, 2, 1, 64, 1e-6, dy, 256, x, 256, 256, 256, 256, 256, 8, dx, 256, 256, 512, 256, None)
+    x = 1 << 20
+    for dx in (x - 2048 + 128, x - 2048 + 16, x + 3 * 512 + 384 - 16):
+        assert bwd(dx) == -1 and b"dx overlaps x" in B.lib().ms_last_error(), dx
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_views_side_by_side_are_apart(dtype):
