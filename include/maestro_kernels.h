@@ -86,7 +86,8 @@ ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *A, int64_t 
  * 64128, 64129 or 64064 = that tile for any number of rows (fp32 sums have none of 256 rows; SwiGLU has one each of 256, 128 and 64). */
 ms_status ms_k_gemm_fp8_config(int32_t tile);
 /* Gate/up projection with SwiGLU and the next operand's quantisation: codes and scales of silu(A Wg^T) * (A Wu^T), W [2F, K] = gate rows,
- * then up rows; the 8-bit sums as for bf16 above, nothing in between is rounded.  F % 16 == 0.  scratch: ..._scratch_bytes(M, F, K) bytes (not less for more rows), 16-byte aligned. */
+ * then up rows; the 8-bit sums as for bf16 above, nothing in between is rounded.  F % 16 == 0.  scratch: ..._scratch_bytes(M, F, K) bytes (not less for more
+ * rows), 16-byte aligned, whatever the row strides; more makes calls faster whose 2F rows of W lie more than 4 GB apart. */
 size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K);
 ms_status ms_k_gemm_fp8_swiglu(int32_t M, int32_t F, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W,
                                int64_t ldw, const void *sW, int64_t ldsw, void *q, int64_t ldq, void *scales, int64_t lds,

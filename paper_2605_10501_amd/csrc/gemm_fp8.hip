@@ -744,11 +744,12 @@ template <bool PRECISE> bool launch_tile(int tile, Fp8Params &p, hipStream_t s) 
     if (tile == F64) return launch_ring<64, 64, 4, 1, 4, false, PRECISE>(p, s);
     return false;
 }
-ms_status launch_gemm(Fp8Params p, bool precise, hipStream_t s) {
+// rows: of the whole call, which may be a part of
+ms_status launch_gemm(Fp8Params p, int rows, bool precise, hipStream_t s) {
     ProfScope ps(0, 2.0 * p.M * p.N * p.K, s);
     bool fits = true;
     const int forced = g_tile.load();
-    if (forced ? forced == FDIRECT : fp8_direct(p.M, p.N)) {
+    if (forced ? forced == FDIRECT : fp8_direct(rows, p.N)) {
         if (precise) launch_direct<true>(p, s); else launch_direct<false>(p, s);
     } else {
         const int tile = forced && !(precise && (forced == F256 || forced == F192)) ? forced : precise ? fp8_choose(kFp8Precise, p.M, p.N, p.kb) : fp8_choose(kFp8Fast, p.M, p.N, p.kb);
@@ -794,7 +795,7 @@ extern "C" ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *
     p.C = C; p.ldc = ldc; p.R = residual; p.ldr = ldr; p.c_fp32 = c_fp32 != 0; p.r_fp32 = residual_fp32 != 0;
     p.vec = N % 16 == 0 && ldc * ec % 16 == 0 && aligned(C, 16) && (!residual || (ldr * er % 16 == 0 && aligned(residual, 16)));
     p.M = M; p.N = N; p.K = K; p.kb = ms_cdiv(K, kBlk);
-    return launch_gemm(p, c_fp32 == 1, (hipStream_t)stream);
+    return launch_gemm(p, M, c_fp32 == 1, (hipStream_t)stream);
 }
 
 extern "C" size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K) {
@@ -825,11 +826,21 @@ extern "C" ms_status ms_k_gemm_fp8_swiglu(int32_t M, int32_t F, int32_t K, const
         MS_LAUNCH_CHECK();
         return MS_OK;
     }
-    // gate and up in fp32 first: the same numbers before the same activation
-    const size_t need = ms_align_up((size_t)M * 2 * F * sizeof(float));
+    // Gate and up in fp32 first: the same numbers before the same activation.  As many rows at a time as the scratch has room for, which is all of
+    // them unless only the weights' row stride keeps the call from the kernels above.
+    const size_t row = (size_t)2 * F * sizeof(float), need = ms_k_gemm_fp8_swiglu_scratch_bytes(M, F, K);
     if (!scratch || scratch_bytes < need) return ms_fail(MS_ERR_WORKSPACE, "gemm_fp8_swiglu: scratch %zu < %zu bytes", scratch_bytes, need);
     if (!aligned(scratch, 16)) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8_swiglu: scratch must be 16-byte aligned");
+    const size_t room = scratch_bytes / row;
+    const int rows = room < (size_t)M ? (int)room : M;
     p.C = scratch; p.ldc = 2L * F; p.c_fp32 = 1; p.vec = 1;
-    MS_TRY(launch_gemm(p, false, s));
-    return ms_k_swiglu_fp8(MS_F32, M, F, scratch, 2L * F, q, ldq, scales, lds, stream);
+    for (int m = 0; m < M; m += rows) {
+        p.M = M - m < rows ? M - m : rows;
+        p.A = (const uint8_t *)A + (long)m * lda;
+        p.sA = (const uint8_t *)sA + (long)m * ldsa;
+        MS_TRY(launch_gemm(p, M, false, s));
+        MS_TRY(ms_k_swiglu_fp8(MS_F32, p.M, F, scratch, 2L * F, (uint8_t *)q + (long)m * ldq, ldq, (uint8_t *)scales + (long)m * lds, lds, stream));
+        if (M - m <= rows) break;                        // (m + rows could pass 2^31)
+    }
+    return MS_OK;
 }

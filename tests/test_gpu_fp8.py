@@ -405,3 +405,28 @@ def test_tile_of_192_outputs_gives_the_same_bits(m, n, k, fp8_tile):
     want = [f() for f in calls]
     fp8_tile(256192)
     assert all(torch.equal(f(), x) for f, x in zip(calls, want))
+
+
+@pytest.mark.gpu
+def test_gate_up_weights_with_rows_far_apart():
+    """2 f rows that one buffer descriptor does not reach: the scratch that the sizes ask for is enough."""
+    f, k, ld = 1024, 256, (1 << 21) + (1 << 16)
+    a, w = operands(300, 2 * f, k)
+    far = torch.empty(2 * f * ld, dtype=torch.uint8, device="cuda").view(2 * f, ld)[:, :k].view(E4M3)
+    far.copy_(w[0])
+    for m in (1, 40, 64, 65, 300):
+        x = a[0][:m], a[1][:m]
+        want, got = B.k_gemm_fp8_swiglu(*x, *w), B.k_gemm_fp8_swiglu(*x, far, w[1])
+        assert all(torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(want, got)), m
+
+
+def test_scratch_of_the_sizes_is_enough_for_any_row_stride():
+    f = B._fn
+    need = f("ms_k_gemm_fp8_swiglu_scratch_bytes")(300, 1024, 256)
+
+    def call(m, ldw, nb):                                                    # (nothing is there to launch on: what the host checks turn down is -3)
+        return f("ms_k_gemm_fp8_swiglu")(m, 1024, 256, 256, 256, 256, 4, 256, ldw, 256, 4, 256, 1024, 256, 8, 256, nb, None)
+    assert call(300, (1 << 21) + (1 << 16), need - 256) == -3 and call(40, 256, 40 * 8192 - 1) == -3
+    assert need == 64 * 8192
+    if not torch.cuda.is_available():
+        assert call(300, (1 << 21) + (1 << 16), need) != -3
