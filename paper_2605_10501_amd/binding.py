@@ -679,7 +679,8 @@ def k_norm_fp8(x, g, eps):
 
 def k_swiglu_fp8(gate_up):
     """Codes and scale bytes of silu(gate) * up, gate_up [n, 2 f]."""
-    _need("gate_up", gate_up, _STORE, (None, None), None, rows=True)
+    both = gate_up.shape[1] // 2 * 2 if isinstance(gate_up, torch.Tensor) and gate_up.dim() == 2 else None
+    _need("gate_up", gate_up, _STORE, (None, both), None, rows=True)
     n, f = gate_up.shape[0], gate_up.shape[1] // 2
     q, s = _codes(n, f, n, gate_up.device)
     _call("ms_k_swiglu_fp8", gate_up.device, _dt(gate_up.dtype), n, f, gate_up.data_ptr(), _ld(gate_up), q.data_ptr(), f, s.data_ptr(), s.shape[1])

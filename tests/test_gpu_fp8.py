@@ -430,3 +430,11 @@ def test_scratch_of_the_sizes_is_enough_for_any_row_stride():
     assert need == 64 * 8192
     if not torch.cuda.is_available():
         assert call(300, (1 << 21) + (1 << 16), need) != -3
+
+
+def test_gate_up_of_an_odd_number_of_columns_is_refused():
+    """Rows of 48 numbers of which a view shows 33: 16 gates, 16 ups and one that would be left out."""
+    with pytest.raises(ValueError, match="gate_up: expected shape"):
+        B.k_swiglu_fp8(torch.zeros((3, 48), dtype=BF16)[:, :33])
+    with pytest.raises(ValueError, match="on a GPU"):
+        B.k_swiglu_fp8(torch.zeros((3, 48), dtype=BF16)[:, :32])
