@@ -4,6 +4,8 @@ import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
 
+from paper_2605_10501_amd import mfma_check
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
@@ -11,6 +13,7 @@ OUT = os.path.join(HERE, "libmaestro_section.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["api.cpp", "profile.cpp", "scheduler.cpp", "kd_host.cpp", "column_work.cpp", "elementwise.hip", "qk_norm.hip", "embedding_sorted.hip", "gemm.hip", "fp8_quantize.hip", "gemm_fp8.hip", "linear_f32.hip", "attention.hip", "attention_mfma.hip", "kd.hip",
            "section.hip", "section_options.hip", "merger.hip", "probes.hip"]
+INLINE_PRODUCTS = {"gemm_fp8.hip": "gemm_fp8_big_kernel"}      # kernels with matrix products as inline assembly
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wno-unused-value"]
@@ -25,6 +28,8 @@ def _compile(src):
         raise RuntimeError(f"hipcc failed on {src}:\n{err}")
     if err.strip():
         sys.stderr.write(err + "\n")
+    if src in INLINE_PRODUCTS:
+        mfma_check.check(obj, INLINE_PRODUCTS[src])
     return obj
 
 

@@ -53,7 +53,7 @@ struct Fp8Params {
 // The same with the accumulators bound to accumulation registers, where the compiler would copy them to and fro for a kernel that needs all 256.  It does
 // not see what the instruction needs around it: whoever reads the sums waits first, and w, a, sw and sa are results of LDS reads as they come (a vector
 // instruction's result needs two idle states before it; in front of every product they cost 2 %, so they stand at the head of a K tile only,
-// where the compiler may put copies).
+// where the compiler may put copies).  The build looks through the compiled kernels for what stands too close (mfma_check.py).
 template <int W, int A> __device__ __forceinline__ void mfma_acc(const i32x8 &w, const i32x8 &a, f32x4 &c, int sw, int sa) {
     asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
         : "+a"(c) : "v"(w), "v"(a), "v"(sw), "v"(sa), "n"(W & 1), "n"(A & 1), "n"(W >> 1), "n"(A >> 1));
