@@ -178,6 +178,7 @@ ms_status validate_ptrs(const ms_section_config *c, const ms_section_ptrs *w, co
     return MS_OK;
 }
 
+// (head sizes are validate_config's: 64, 80 and 128 suit the options' kernels too)
 ms_status validate_options(const ms_section_config *c, const SectionOptions *opt, bool backward) {
     if (!opt) return MS_OK;
     const ms_section_options *o = opt->o;
@@ -189,9 +190,6 @@ ms_status validate_options(const ms_section_config *c, const SectionOptions *opt
     if (o->fp8 && c->dtype != MS_BF16) return ms_fail(MS_ERR_UNSUPPORTED, "section: 8-bit matrices need bf16 activations");
     if (o->fp8 && (c->d_model % 16 || c->d_ffn % 16))
         return ms_fail(MS_ERR_UNSUPPORTED, "section: d_model=%d and d_ffn=%d must be multiples of 16 with 8-bit matrices", c->d_model, c->d_ffn);
-    if (o->fp8 && (long)c->n_q_heads * c->head_dim % 16) return ms_fail(MS_ERR_UNSUPPORTED, "section: %d heads of %d are no multiple of 16 columns, with 8-bit matrices", c->n_q_heads, c->head_dim);
-    if (o->qk_norm && (c->head_dim % 16 || c->head_dim > 512))
-        return ms_fail(MS_ERR_UNSUPPORTED, "section: head_dim=%d must be a multiple of 16 and at most 512 with query / key norms", c->head_dim);
     return MS_OK;
 }
 ms_status validate_option_ptrs(const ms_section_config *c, const SectionOptions *opt, const ms_section_ptrs *weights, const ms_section_ptrs *grads) {

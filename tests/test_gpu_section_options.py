@@ -357,3 +357,31 @@ def test_a_scale_without_an_embedding_is_refused():
     b, o.embed_scale = B.BatchC(4, 1, C.c_void_p(256), host), 2.0
     assert B.lib().ms_section_forward_with(C.byref(cfg), C.byref(o), None, C.byref(b), v, v, v, C.c_size_t(16), None) == -1
     assert b"embeds nothing" in B.lib().ms_last_error()
+
+
+def test_refusals_name_their_reason():
+    """The same code has several causes: each refusal comes from its own check."""
+    lib, host = B.lib(), (C.c_int32 * 2)(0, 4)
+
+    def why(qk=0, fp8=0, scale=1.0, dtype="bf16", backward=False, n_tokens=4, **over):
+        c, lo = B._cfg_c(config(dtype, n_layers=1, **over)), (B.LayerOptions * 1)()
+        o = B.SectionOptionsC(scale, qk, fp8, lo)
+        cu = (C.c_int32 * 2)(0, n_tokens)
+        b, v = B.BatchC(n_tokens, 1, C.c_void_p(256), cu), C.c_void_p(256)
+        if backward:
+            status = lib.ms_section_forward_backward_with(C.byref(c), C.byref(o), lo, None, None, C.byref(b), v, v, v, None, None, None, None, None, None, v,
+                                                          C.c_size_t(16), None)
+        else:
+            status = lib.ms_section_forward_with(C.byref(c), C.byref(o), None, C.byref(b), v, v, v, C.c_size_t(16), None)
+        return status, lib.ms_last_error().decode()
+    for hd in (24, 96, 520):                                                  # whatever the options
+        for qk, fp8 in ((0, 0), (1, 0), (0, 1), (1, 1)):
+            status, text = why(qk, fp8, head_dim=hd)
+            assert status == -4 and f"head_dim={hd}" in text
+    for hd in (64, 80, 128):                                                  # the head sizes that there are suit every option: next come the weights
+        for n_q in (1, 3):
+            status, text = why(1, 1, head_dim=hd, n_q_heads=n_q, n_kv_heads=1)
+            assert status == -1 and "null weights" in text
+    assert why(fp8=1, d_ffn=344)[1].startswith("section: d_model=256 and d_ffn=344") and "forward-only" in why(fp8=1, backward=True)[1]
+    assert "bf16" in why(fp8=1, dtype="fp32")[1] and "for decoders" in why(arch="encoder", vocab=0)[1] and "not finite" in why(scale=float("nan"))[1]
+    assert "sorts" in why(backward=True, n_tokens=(1 << 24) + 8, n_q_heads=1, n_kv_heads=1, head_dim=64, dtype="fp32")[1]
