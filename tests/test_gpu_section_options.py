@@ -385,3 +385,56 @@ def test_refusals_name_their_reason():
     assert why(fp8=1, d_ffn=344)[1].startswith("section: d_model=256 and d_ffn=344") and "forward-only" in why(fp8=1, backward=True)[1]
     assert "bf16" in why(fp8=1, dtype="fp32")[1] and "for decoders" in why(arch="encoder", vocab=0)[1] and "not finite" in why(scale=float("nan"))[1]
     assert "sorts" in why(backward=True, n_tokens=(1 << 24) + 8, n_q_heads=1, n_kv_heads=1, head_dim=64, dtype="fp32")[1]
+
+
+@pytest.mark.gpu
+def test_training_steps_with_the_optimizer_in_one_graph():
+    """Teacher in 8 bits, student with norms and scale, distillation loss, AdamW: three replays are three eager steps.  Trained are the final gains, whose
+    gradient has one order of sums, so that states and gains have to be equal; the table's update, behind attention's atomics, goes to a copy."""
+    t, s = config("bf16", d_model=512, d_ffn=1408, n_layers=1), config("bf16", n_layers=1)
+    kd = wl.KDConfig(s.vocab - 500 % 8, t.d_model, s.d_model, 1.0, 128)
+    batch, tw, ids, _ = data(t)
+    _, sw, _, _ = data(s, 6)
+    tw8, layers = B.quantize_section(tw)
+    topt, norms = B.SectionOptions(embed_scale=t.d_model ** 0.5, fp8=True, layers=layers), gains(s, 6)
+    sopt = B.SectionOptions(embed_scale=s.d_model ** 0.5, qk_norm=True, layers=norms)
+    wt, wst = (wl.normal(8, k, (kd.vocab, d), 0.02, 0.0, BF16, "cuda") for k, d in (("wt", t.d_model), ("ws", s.d_model)))
+    grads, lr = B.zero_grads(sw), 0.05
+    ngrads = [{k: torch.zeros(s.head_dim, device="cuda") for k in l} for l in norms]
+
+    def fresh():
+        sw["final_norm_g"].copy_(first)
+        grads["final_norm_g"].zero_(), grads["embedding"].zero_()
+        for k, st in state.items():
+            st[0].copy_(start[k]), st[1].zero_(), st[2].zero_()
+    first = sw["final_norm_g"].clone()
+    start = {"final_norm_g": first.float(), "embedding": sw["embedding"].float()}
+    state = {k: [v.clone(), torch.zeros_like(v), torch.zeros_like(v)] for k, v in start.items()}
+
+    def step():
+        h_t = B.section_forward(t, tw8, batch, ids, options=topt)
+        out = B.section_forward_backward(s, sw, grads, batch, ids, kd=kd, w_teacher=wt, w_student=wst, h_teacher=h_t,
+                                         d_w_student=torch.zeros((kd.vocab, s.d_model), device="cuda"), options=sopt, option_grads=ngrads)
+        B.adamw_step(grads["final_norm_g"], *state["final_norm_g"], sw["final_norm_g"], 1, lr=lr, zero_grad=True)
+        B.adamw_step(grads["embedding"], *state["embedding"], None, 1, lr=lr, zero_grad=True)
+        return out["h_out"]
+    want = []
+    for _ in range(3):
+        want.append((step().clone(), sw["final_norm_g"].clone(), state["final_norm_g"][0].clone()))
+    assert not torch.equal(want[0][1], first) and not torch.equal(want[1][0], want[0][0])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        h = step()
+    fresh()
+    for k in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(h, want[k][0]) and torch.equal(sw["final_norm_g"], want[k][1]) and torch.equal(state["final_norm_g"][0], want[k][2]), k
+        B.section_forward(t, tw8, batch, ids, options=topt)               # the program's own work between the replays
+    # three steps of moments with the first one's bias correction move a number by at most 1 + sqrt(1 + 0.81 / 0.95) + sqrt(1 + 0.81 / 0.95 + (0.81 / 0.95)^2)
+    # = 3.97 lr (Cauchy's inequality), whatever its gradients; rows of ids that are not there stay
+    moved = (state["embedding"][0] - start["embedding"]).abs()
+    there = torch.zeros(s.vocab, dtype=torch.bool, device="cuda")
+    there[ids.long()] = True
+    assert bool(moved[there].any(1).all()) and not bool(moved[~there].any())
+    assert float(moved.max()) < 4 * lr and not bool(grads["embedding"].any())
