@@ -438,3 +438,43 @@ def test_gate_up_of_an_odd_number_of_columns_is_refused():
         B.k_swiglu_fp8(torch.zeros((3, 48), dtype=BF16)[:, :33])
     with pytest.raises(ValueError, match="on a GPU"):
         B.k_swiglu_fp8(torch.zeros((3, 48), dtype=BF16)[:, :32])
+
+
+def some_codes(n, k, tag):
+    """Codes of every kind but NaN."""
+    c = (wl.uniform(13, tag, n * k) * 256).to(torch.uint8).view(n, k)
+    return torch.where((c & 127) == 127, torch.full_like(c, 0x38), c).view(E4M3).cuda()
+
+
+# bytes of both operands; where their product leaves fp32's normal numbers there is nothing to compare
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(5, 48, 128), (100, 48, 144), (300, 256, 384)])
+@pytest.mark.parametrize("ea,ew", [(0, 127), (127, 0), (1, 130), (2, 140), (3, 127), (127, 3), (3, 240), (240, 3), (246, 3), (3, 246), (0, 246), (246, 0), (100, 10),
+                                   (246, 90), (90, 246)])
+def test_scales_at_the_ends_of_their_range(ea, ew, m, n, k):
+    sc = lambda rows, b: torch.full((rows, (k + 511) // 512 * 4), b, dtype=torch.uint8, device="cuda")
+    a, w = (some_codes(m, k, f"sa{m}{k}"), sc(m, ea)), (some_codes(n, k, f"sw{n}{k}"), sc((n + 127) // 128, ew))
+    ref, size = product(a, w)
+    one = 2.0 ** (127 - ea), 2.0 ** (127 - ew)                               # to the codes' own values, in which cut_off computes in fp32
+    cut = cut_off((a[0], sc(m, 127)), (w[0], sc(w[1].shape[0], 127))) / one[0] / one[1]
+    close(B.k_gemm_fp8(*a, *w, c_fp32=True, fast_sums=True), ref, size, k, "fast sums", cut)
+    # below 2^-124 a code times its scale is off by up to 2^-134, times the other operand's row
+    rounded = (2.0 ** -134 * (ea < 3) * values(*w, 128).cuda().abs().sum(1)[None] + 2.0 ** -134 * (ew < 3) * values(*a, 1).cuda().abs().sum(1)[:, None])
+    close(B.k_gemm_fp8(*a, *w, c_fp32=True), ref, size, k, "fp32 sums", rounded)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [6, 90])
+def test_products_of_the_smallest_and_largest_numbers(m):
+    """As the quantisers lay them out: bytes 0 .. 247."""
+    x = normal(f"ends{m}", (m, 256), 1.0, F32).clamp(-3, 3)
+    x[:, :128] *= torch.exp2(torch.arange(m, device="cuda") % 6 * 49.8 - 124.0)[:, None]
+    x[1, 5] = 3.2e38                                                         # byte 247
+    x[2, 7] = 2.0 ** -149
+    w = normal("endw", (40, 256), 2.0 ** -12, F32)
+    qa, qw = B.k_fp8_quantize(x), B.k_fp8_quantize(w, 128)
+    assert int(qa[1][1, 0]) == 247 and int(qa[1].min()) <= 5
+    ref, size = product(qa, qw)
+    cut = 7 * 2.0 ** -13 * size
+    close(B.k_gemm_fp8(*qa, *qw, c_fp32=True, fast_sums=True), ref, size, 256, "fast sums", cut)
+    close(B.k_gemm_fp8(*qa, *qw, c_fp32=True), ref, size, 256, "fp32 sums", 2.0 ** -134 * values(*qw, 128).cuda().abs().sum(1)[None])
