@@ -76,7 +76,7 @@ ms_status ms_k_swiglu_fp8(int32_t dtype, int32_t n, int32_t f, const void *gate_
                           int64_t lds, void *stream);
 /* C[M,N] = A[M,K] W[N,K]^T (+ residual) of such operands: A with scales sA [M, blocks], W with sW [ceil(N / 128), blocks].  c_fp32 = 0: C is
  * bf16, 1: fp32, 2: fp32 with the matrix cores' 8-bit sums, as for bf16: eight consecutive k are summed on a grid 2^-13 of the largest of
- * their products (1.5e-5 of the result on normal data) at twice the rate; 1 sums in fp32 throughout.  The residual [M,N] is bf16 or fp32
+ * their products (1.5e-5 of the result on normal data) at twice the rate; 1 sums in fp32 throughout; 3: bf16 from such sums.  The residual [M,N] is bf16 or fp32
  * and may be C (of C's type), else must not overlap it.  Results for up to 64 rows differ from those of more rows in the order of the sums (K is split then).
  * Scale bytes 0 .. 254 with the 8-bit sums.  The fp32 sums widen the codes to bf16: exact for bytes 3 .. 246, and for 247, the quantisers' largest (blocks
  * with a number above 2.98e38), up to codes of 240 (numbers up to 3.29e38), past which their products overflow; for 0 .. 2 (all numbers of the
@@ -89,7 +89,8 @@ ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *A, int64_t 
  * 64128, 64129 or 64064 = that tile for any number of rows (fp32 sums have none of 256 rows; SwiGLU has one each of 256, 128 and 64). */
 ms_status ms_k_gemm_fp8_config(int32_t tile);
 /* Gate/up projection with SwiGLU and the next operand's quantisation: codes and scales of silu(A Wg^T) * (A Wu^T), W [2F, K] = gate rows,
- * then up rows; the 8-bit sums as for bf16 above, nothing in between is rounded.  F % 16 == 0.  scratch: ..._scratch_bytes(M, F, K) bytes (not less for more
+ * then up rows; the 8-bit sums as for bf16 above, nothing in between is rounded (with fp32 sums: ms_k_gemm_fp8 into fp32 and
+ * ms_k_swiglu_fp8 of that).  F % 16 == 0.  scratch: ..._scratch_bytes(M, F, K) bytes (not less for more
  * rows), 16-byte aligned, whatever the row strides; more makes calls faster whose 2F rows of W lie more than 4 GB apart. */
 size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K);
 ms_status ms_k_gemm_fp8_swiglu(int32_t M, int32_t F, int32_t K, const void *A, int64_t lda, const void *sA, int64_t ldsa, const void *W,

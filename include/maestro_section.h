@@ -149,7 +149,8 @@ ms_status ms_section_forward_backward(const ms_section_config *cfg, const ms_sec
  *                `dtype` in each layer and the section's norm_eps; option_grads has their gradients (fp32, accumulated)
  *   fp8          != 0: the matrices w_qkv, w_o, w_up, w_down are e4m3 codes with scale bytes s_qkv .. s_down for blocks of 128 x 128, as
  *                ms_k_fp8_quantize(block_rows = 128) writes them without padding (rows of in codes, of ceil(in / 512) * 4 scale bytes); their inputs
- *                are quantised in blocks of 128 columns.  Forward only, dtype MS_BF16; d_model and d_ffn multiples of 16
+ *                are quantised in blocks of 128 columns.  Forward only, dtype MS_BF16; d_model and d_ffn multiples of 16.  The products' sums are the 8-bit
+ *                matrix cores' (ms_k_gemm_fp8 on their precision); fp8 == 2: fp32 sums throughout, at half the rate and with more workspace
  * The embedding gradient of a section with options adds up its tokens sorted by id, in one order: no atomics (ms_k_embedding_sorted_backward).
  * Alignment, refused (MS_ERR_UNSUPPORTED) before anything is launched: 16 bytes for final_norm_g, for the gradient of the embedding, for the
  * embedding if embed_scale != 1, for q_norm_g and k_norm_g, and with fp8 for norm1_g, norm2_g and the codes; 4 bytes for scale bytes. */

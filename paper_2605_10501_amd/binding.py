@@ -158,10 +158,14 @@ class SectionOptionsC(C.Structure):
 
 class SectionOptions:
     """Options of a decoder section: embed_scale; layers: one dict per layer with q_norm_g and k_norm_g ([head_dim], in the section's dtype) if
-    qk_norm, and the scale bytes s_qkv, s_o, s_up, s_down of the matrices' codes if fp8 (see quantize_section)."""
+    qk_norm, and the scale bytes s_qkv, s_o, s_up, s_down of the matrices' codes if fp8 (see quantize_section).  fp32_sums: the products of
+    8-bit matrices sum in fp32 throughout (k_gemm_fp8), at half the rate."""
 
-    def __init__(self, embed_scale=1.0, qk_norm=False, fp8=False, layers=None):
+    def __init__(self, embed_scale=1.0, qk_norm=False, fp8=False, layers=None, fp32_sums=False):
         self.embed_scale, self.qk_norm, self.fp8, self.layers = float(embed_scale), bool(qk_norm), bool(fp8), layers
+        self.fp32_sums = bool(fp32_sums)
+        if self.fp32_sums and not self.fp8:
+            raise ValueError("fp32_sums is a choice for fp8 matrices")
 
     def check(self, cfg, device=None):
         if (self.qk_norm or self.fp8) and (self.layers is None or len(self.layers) != cfg.n_layers):
@@ -177,7 +181,7 @@ class SectionOptions:
                     _need(k, lo.get(k), (torch.uint8,), (rows(n), words(kin)), device)
 
     def c(self, cfg):
-        o = SectionOptionsC(self.embed_scale, int(self.qk_norm), int(self.fp8), _layer_options(self.layers, cfg.n_layers))
+        o = SectionOptionsC(self.embed_scale, int(self.qk_norm), int(self.fp8) + int(self.fp32_sums), _layer_options(self.layers, cfg.n_layers))
         return o
 
 
@@ -697,10 +701,12 @@ def _fp8_args(a, sa, w, sw):
     return m, w.shape[0], k, a.data_ptr(), _ld(a), sa.data_ptr(), _ld(sa), w.data_ptr(), _ld(w), sw.data_ptr(), _ld(sw)
 
 
-def k_gemm_fp8(a, sa, w, sw, residual=None, c=None, c_fp32=None, fast_sums=False):
+def k_gemm_fp8(a, sa, w, sw, residual=None, c=None, c_fp32=None, fast_sums=False, fp32_sums=False):
     """a w^T (+ residual) of 8-bit operands as k_fp8_quantize makes them (a: block_rows=1, w: 128).  The result is bf16, or fp32 if c_fp32
     (by default: if the residual is); c: a tensor to write to, which may be the residual (else they must not overlap).  fast_sums: an fp32 result from the 8-bit
-    matrix cores' sums, which a bf16 result always has."""
+    matrix cores' sums, which a bf16 result has unless fp32_sums asks for an fp32 result's, at half the rate."""
+    if fast_sums and fp32_sums:
+        raise ValueError("k_gemm_fp8: fast_sums and fp32_sums exclude each other")
     args = _fp8_args(a, sa, w, sw)
     m, n, dev = args[0], args[1], a.device
     if residual is not None:
@@ -710,7 +716,8 @@ def k_gemm_fp8(a, sa, w, sw, residual=None, c=None, c_fp32=None, fast_sums=False
         c = torch.empty((m, n), dtype=torch.float32 if f32 else torch.bfloat16, device=dev)
     else:
         _need("c", c, _STORE, (m, n), dev, rows=True)
-    _call("ms_k_gemm_fp8", dev, *args, c.data_ptr(), _ld(c), (2 if fast_sums else 1) if c.dtype == torch.float32 else 0, residual.data_ptr() if residual is not None else None,
+    kind = (2 if fast_sums else 1) if c.dtype == torch.float32 else 3 if fp32_sums else 0
+    _call("ms_k_gemm_fp8", dev, *args, c.data_ptr(), _ld(c), kind, residual.data_ptr() if residual is not None else None,
           _ld(residual) if residual is not None else 0, int(residual is not None and residual.dtype == torch.float32))
     return c
 
@@ -720,12 +727,15 @@ def k_gemm_fp8_config(tile=0):
     _check(lib().ms_k_gemm_fp8_config(int(tile)))
 
 
-def k_gemm_fp8_swiglu(a, sa, w, sw):
-    """Codes and scale bytes of silu(a wg^T) * (a wu^T), w [2 f, k] = gate rows, then up rows."""
+def k_gemm_fp8_swiglu(a, sa, w, sw, fp32_sums=False):
+    """Codes and scale bytes of silu(a wg^T) * (a wu^T), w [2 f, k] = gate rows, then up rows.  fp32_sums: as for k_gemm_fp8, with gate and up
+    through memory."""
     args = _fp8_args(a, sa, w, sw)
     m, f, k, dev = args[0], args[1] // 2, args[2], a.device
     if args[1] % 2:
         raise ValueError(f"w: expected gate rows and as many up rows, got {args[1]}")
+    if fp32_sums:
+        return k_swiglu_fp8(k_gemm_fp8(a, sa, w, sw, c_fp32=True))
     q, s = _codes(m, f, m, dev)
     nb = _fn("ms_k_gemm_fp8_swiglu_scratch_bytes")(m, f, k)
     sc = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None

@@ -12,8 +12,8 @@
 // Precision: the instruction sums eight consecutive k on a grid 2^-13 of the largest product's power of two and cuts off what lies below;
 // the sums of eight are added in fp32 (measured with single products: a second one 2^-14 of the first is lost among the same eight, not
 // among others).  On normal data that is 1.5e-5 of the result, a hundredth of the rounding to bf16, and results in bf16 and SwiGLU's codes
-// are computed so.  An fp32 result is computed on v_mfma_f32_16x16x32_bf16 instead, half the rate, from the codes widened to bf16 (exact): fp32
-// sums throughout; unless the caller asks for the fast ones.
+// are computed so unless the caller asks for more.  An fp32 result is computed on v_mfma_f32_16x16x32_bf16 instead, half the rate, from the codes
+// widened to bf16 (exact): fp32 sums throughout; unless the caller asks for the fast ones.
 //
 //   * gemm_fp8_big_kernel: 256 tokens x 256 or 192 outputs, operands through LDS;
 //   * gemm_fp8_ring_kernel: smaller tiles through LDS, for grids that do not fill the chip with the large ones, and fp32 results;
@@ -785,19 +785,20 @@ extern "C" ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *
                                    int64_t ldr, int32_t residual_fp32, void *stream) {
     if (M == 0) return MS_OK;
     MS_TRY(check("gemm_fp8", M, N, K, A, lda, sA, ldsa, W, ldw, sW, ldsw));
-    if (!C || c_fp32 < 0 || c_fp32 > 2) return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8: null pointer or bad c_fp32");
+    if (!C || c_fp32 < 0 || c_fp32 > 3) return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8: null pointer or bad c_fp32");
     if (ldc < N || (residual && ldr < N)) return ms_fail(MS_ERR_SHAPE, "gemm_fp8: a row stride is less than a row");
-    const int ec = c_fp32 ? 4 : 2, er = residual_fp32 ? 4 : 2;
+    const bool f32 = c_fp32 == 1 || c_fp32 == 2, precise = c_fp32 & 1;
+    const int ec = f32 ? 4 : 2, er = residual_fp32 ? 4 : 2;
     if (!aligned(C, ec) || (residual && !aligned(residual, er))) return ms_fail(MS_ERR_UNSUPPORTED, "gemm_fp8: C or residual is not aligned to its type");
     if (residual && !(residual == C && ldr == ldc && er == ec) && !ms_apart(C, ldc * ec, (long)N * ec, residual, ldr * er, (long)N * er, M))
         return ms_fail(MS_ERR_INVALID_ARG, "gemm_fp8: the residual is neither C nor apart from it");
     Fp8Params p = {};
     p.A = (const uint8_t *)A; p.sA = (const uint8_t *)sA; p.W = (const uint8_t *)W; p.sW = (const uint8_t *)sW;
     p.lda = lda; p.ldsa = ldsa; p.ldw = ldw; p.ldsw = ldsw;
-    p.C = C; p.ldc = ldc; p.R = residual; p.ldr = ldr; p.c_fp32 = c_fp32 != 0; p.r_fp32 = residual_fp32 != 0;
+    p.C = C; p.ldc = ldc; p.R = residual; p.ldr = ldr; p.c_fp32 = f32; p.r_fp32 = residual_fp32 != 0;
     p.vec = N % 16 == 0 && ldc * ec % 16 == 0 && aligned(C, 16) && (!residual || (ldr * er % 16 == 0 && aligned(residual, 16)));
     p.M = M; p.N = N; p.K = K; p.kb = ms_cdiv(K, kBlk);
-    return launch_gemm(p, M, c_fp32 == 1, (hipStream_t)stream);
+    return launch_gemm(p, M, precise, (hipStream_t)stream);
 }
 
 extern "C" size_t ms_k_gemm_fp8_swiglu_scratch_bytes(int32_t M, int32_t F, int32_t K) {

@@ -86,6 +86,7 @@ struct SectionOps {
     decltype(&ms_k_gemm_fp8) fp8_gemm;
     decltype(&ms_k_gemm_fp8_swiglu) fp8_swiglu;
     decltype(&ms_k_gemm_fp8_swiglu_scratch_bytes) fp8_swiglu_scratch;
+    decltype(&ms_k_swiglu_fp8) fp8_swiglu_pass;
 };
 struct SectionOptions {
     const ms_section_options *o;

@@ -108,7 +108,7 @@ Plan make_plan(const ms_section_config *c, const SectionOptions *opt, int n, int
         p.code_s = a.take<void>(N * scale_cols(widest));
         p.act_code = a.take<void>(N * m.f);
         p.act_s = a.take<void>(N * scale_cols(m.f));
-        p.fp8_scratch_bytes = opt->ops->fp8_swiglu_scratch(n, m.f, m.d);
+        p.fp8_scratch_bytes = opt->o->fp8 == 2 ? N * 2 * m.f * 4 : opt->ops->fp8_swiglu_scratch(n, m.f, m.d);
         p.fp8_scratch = a.take<void>(p.fp8_scratch_bytes);
     }
     p.bytes = a.off;
@@ -287,11 +287,22 @@ struct Exec {
         return opt->ops->qk_forward(dt, m.n, m.nq, m.nkv, m.hd, c->norm_eps, raw ? raw : qkv, m.dqkv, g.q_norm_g, g.k_norm_g, p->pos, p->rope,
                                     m.max_seqlen, qkv, m.dqkv, s);
     }
+    bool fp32_sums() const { return opt->o->fp8 == 2; }
     // y[n, out] = x W^T (+ res) of 8-bit operands; with a residual, y is the fp32 stream (from the 8-bit units' sums, whose error is far below
-    // that of the operands)
+    // that of the operands, unless fp32 sums are asked for)
     ms_status linear_fp8(const void *code, const void *scales, int in, const void *W, const void *sW, int out, void *y, const void *res) {
-        return opt->ops->fp8_gemm(m.n, out, in, code, in, scales, scale_cols(in), W, in, sW, scale_cols(in), y, out, res ? 2 : 0, res, out,
-                                  res && fp32_stream(res), s);
+        return opt->ops->fp8_gemm(m.n, out, in, code, in, scales, scale_cols(in), W, in, sW, scale_cols(in), y, out,
+                                  res ? (fp32_sums() ? 1 : 2) : fp32_sums() ? 3 : 0, res, out, res && fp32_stream(res), s);
+    }
+    // codes of SwiGLU(x W^T)
+    ms_status swiglu_fp8(const void *W, const void *sW) {
+        const SectionOps &ops = *opt->ops;
+        if (!fp32_sums())
+            return ops.fp8_swiglu(m.n, m.f, m.d, p->code, m.d, p->code_s, scale_cols(m.d), W, m.d, sW, scale_cols(m.d), p->act_code, m.f, p->act_s,
+                                  scale_cols(m.f), p->fp8_scratch, p->fp8_scratch_bytes, s);
+        MS_TRY(ops.fp8_gemm(m.n, 2 * m.f, m.d, p->code, m.d, p->code_s, scale_cols(m.d), W, m.d, sW, scale_cols(m.d), p->fp8_scratch, 2L * m.f, 1, nullptr, 0,
+                            0, s));
+        return ops.fp8_swiglu_pass(MS_F32, m.n, m.f, p->fp8_scratch, 2L * m.f, p->act_code, m.f, p->act_s, scale_cols(m.f), s);
     }
     // A layer whose matrices are in 8 bits: norms, attention output and activation are quantised where they are made or read
     ms_status layer_forward_fp8(const ms_layer_ptrs &w, int li, const void *x, LayerBuf &l, void *y) {
@@ -304,8 +315,7 @@ struct Exec {
         MS_TRY(ops.fp8_quantize(dt, 1, m.n, m.dattn, l.o, m.dattn, p->code, m.dattn, p->code_s, scale_cols(m.dattn), s));
         MS_TRY(linear_fp8(p->code, p->code_s, m.dattn, w.w_o, q.s_o, m.d, l.x2, x));
         MS_TRY(ops.fp8_norm(dt, 1, m.n, m.d, c->norm_eps, l.x2, w.norm2_g, p->code, m.d, p->code_s, scale_cols(m.d), s));
-        MS_TRY(ops.fp8_swiglu(m.n, m.f, m.d, p->code, m.d, p->code_s, scale_cols(m.d), w.w_up, m.d, q.s_up, scale_cols(m.d), p->act_code, m.f, p->act_s,
-                              scale_cols(m.f), p->fp8_scratch, p->fp8_scratch_bytes, s));
+        MS_TRY(swiglu_fp8(w.w_up, q.s_up));
         return linear_fp8(p->act_code, p->act_s, m.f, w.w_down, q.s_down, m.d, y, l.x2);
     }
 

@@ -4,7 +4,8 @@
 namespace {
 const SectionOps kOps = {ms_k_embedding_scaled_forward, ms_k_embedding_sorted_backward, ms_k_embedding_sorted_backward_scratch_bytes,
                          ms_k_qk_norm_rope_forward, ms_k_qk_norm_rope_backward, ms_k_qk_norm_rope_backward_scratch_bytes,
-                         ms_k_norm_fp8, ms_k_fp8_quantize, ms_k_gemm_fp8, ms_k_gemm_fp8_swiglu, ms_k_gemm_fp8_swiglu_scratch_bytes};
+                         ms_k_norm_fp8, ms_k_fp8_quantize, ms_k_gemm_fp8, ms_k_gemm_fp8_swiglu, ms_k_gemm_fp8_swiglu_scratch_bytes,
+                         ms_k_swiglu_fp8};
 }
 
 extern "C" size_t ms_section_workspace_bytes_with(const ms_section_config *cfg, const ms_section_options *options, int32_t max_tokens,

@@ -478,3 +478,33 @@ def test_products_of_the_smallest_and_largest_numbers(m):
     cut = 7 * 2.0 ** -13 * size
     close(B.k_gemm_fp8(*qa, *qw, c_fp32=True, fast_sums=True), ref, size, 256, "fast sums", cut)
     close(B.k_gemm_fp8(*qa, *qw, c_fp32=True), ref, size, 256, "fp32 sums", 2.0 ** -134 * values(*qw, 128).cuda().abs().sum(1)[None])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(1, 4096, 2048), (17, 129, 1024), (100, 333, 688), (300, 2048, 4112), (2049, 144, 272), (777, 1280, 384)])
+def test_bf16_results_from_fp32_sums(m, n, k):
+    a, w = operands(m, n, k)
+    ref, size = product(a, w)
+    got = B.k_gemm_fp8(*a, *w, fp32_sums=True)
+    close(got, ref, size, k, "bf16 from fp32 sums")                          # without what the 8-bit sums cut off
+    assert got.dtype == BF16 and torch.equal(got, B.k_gemm_fp8(*a, *w, c_fp32=True).to(BF16))
+    res = normal(f"r{m}{n}", (m, n), 1.0)
+    assert torch.equal(B.k_gemm_fp8(*a, *w, residual=res, fp32_sums=True), B.k_gemm_fp8(*a, *w, residual=res, c_fp32=True).to(BF16))
+    if n % 32 == 0:
+        q, s = B.k_gemm_fp8_swiglu(*a, *w, fp32_sums=True)
+        g, u = ref.cpu().chunk(2, 1)
+        # fp32 sums move a value over a tie as seldom as other fp32 computing: their error of (k / 8 + ...) half steps at most reaches the codes as in
+        # test_gate_up_swiglu
+        eg, eu = ((k / 8 + k / 128 + 16) * 2 * U * size).cpu().chunk(2, 1)
+        near_codes(q, s, g / (1 + torch.exp(-g)) * u, 1e-2, 1.125 * (1.1 * (u.abs() + eu) * eg + g.abs() * eu))
+
+
+def test_one_kind_of_sums_is_asked_for():
+    with pytest.raises(ValueError, match="exclude"):
+        B.k_gemm_fp8(None, None, None, None, fast_sums=True, fp32_sums=True)
+    with pytest.raises(ValueError, match="fp8"):
+        B.SectionOptions(fp32_sums=True)
+    f = B._fn("ms_k_gemm_fp8")
+    call = lambda kind, ldc=64, c=256: f(4, 64, 128, 256, 128, 256, 4, 256, 128, 256, 4, c, ldc, kind, None, 0, 0, None)
+    assert call(4) == -1 and call(-1) == -1 and call(3, 63) == -2
+    assert call(3, c=257) == -4 and call(1, c=258) == -4                     # 3 is a bf16 result

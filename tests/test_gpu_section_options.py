@@ -438,3 +438,35 @@ def test_training_steps_with_the_optimizer_in_one_graph():
     there[ids.long()] = True
     assert bool(moved[there].any(1).all()) and not bool(moved[~there].any())
     assert float(moved.max()) < 4 * lr and not bool(grads["embedding"].any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lengths", [[1], [40, 9], [150, 63]])
+@pytest.mark.parametrize("d_ffn", [688, 640])
+def test_teacher_in_8_bits_with_fp32_sums(lengths, d_ffn):
+    cfg = config("bf16", d_ffn=d_ffn, n_layers=2)
+    batch = B.Batch(wl.cu_seqlens_of(lengths))
+    _, w, _, _ = data(cfg)
+    ids = wl.randint(4, "ids8", batch.n_tokens, 0, cfg.vocab, "cuda")
+    w8, scales = B.quantize_section(w)
+    norms, nq, nkv, hd, eps = gains(cfg, 5), cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, cfg.norm_eps
+    layers = [{**a, **b} for a, b in zip(scales, norms)]
+    h = B.section_forward(cfg, w8, batch, ids, options=B.SectionOptions(embed_scale=3.0, qk_norm=True, fp8=True, layers=layers, fp32_sums=True))
+    pos, table = B.k_positions(batch), B.k_rope_table(batch.max_seqlen, hd, cfg.rope_base)
+    x = B.k_embedding_scaled_forward(ids, w["embedding"], 3.0)
+    for lw, ls in zip(w8["layers"], layers):
+        qkv = B.k_gemm_fp8(*B.k_norm_fp8(x, lw["norm1_g"], eps), lw["w_qkv"], ls["s_qkv"], fp32_sums=True)
+        qkv = B.k_qk_norm_rope_forward(qkv, nq, nkv, hd, ls["q_norm_g"], ls["k_norm_g"], eps, pos, table)
+        x = B.k_gemm_fp8(*B.k_fp8_quantize(B.k_attention_forward(qkv, batch, nq, nkv, hd, True)[0]), lw["w_o"], ls["s_o"], residual=x, c_fp32=True)
+        act = B.k_swiglu_fp8(B.k_gemm_fp8(*B.k_norm_fp8(x, lw["norm2_g"], eps), lw["w_up"], ls["s_up"], c_fp32=True))
+        x = B.k_gemm_fp8(*act, lw["w_down"], ls["s_down"], residual=x, c_fp32=True)
+    assert torch.equal(h, B.k_norm_forward(0, x, w["final_norm_g"], None, eps)[0])
+    fast = B.section_forward(cfg, w8, batch, ids, options=B.SectionOptions(embed_scale=3.0, qk_norm=True, fp8=True, layers=layers))
+    assert torch.equal(fast, by_kernels(cfg, w8, scales, norms, batch, ids, 3.0)) and not torch.equal(h, fast)
+
+
+def test_workspace_of_fp32_sums():
+    cfg, fake = config("bf16", n_layers=1), [{"q_norm_g": None}]
+    size = lambda n, **o: B.section_workspace_bytes(cfg, n, n, False, B.SectionOptions(fp8=True, layers=fake, **o))
+    sizes = [size(n, fp32_sums=True) for n in (1, 2, 63, 64, 65, 130, 4096)]
+    assert sizes == sorted(sizes) and sizes[-1] >= 4096 * 2 * cfg.d_ffn * 4
