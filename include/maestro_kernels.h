@@ -86,7 +86,8 @@ ms_status ms_k_gemm_fp8(int32_t M, int32_t N, int32_t K, const void *A, int64_t 
                         const void *sW, int64_t ldsw, void *C, int64_t ldc, int32_t c_fp32, const void *residual, int64_t ldr,
                         int32_t residual_fp32, void *stream);
 /* Kernel selection of these products, for measurements and tests, as ms_k_gemm_config: 0 = by shape; 256256, 256192, 128128, 128129,
- * 64128, 64129 or 64064 = that tile for any number of rows (fp32 sums have none of 256 rows; SwiGLU has one each of 256, 128 and 64). */
+ * 64128, 64129 or 64064 = that tile for any number of rows (fp32 sums have none of 256 rows; SwiGLU has one each of 256, 128 and 64); 16016 = the
+ * kernel for few rows, for up to 1048560 (SwiGLU: its tile of 64). */
 ms_status ms_k_gemm_fp8_config(int32_t tile);
 /* Gate/up projection with SwiGLU and the next operand's quantisation: codes and scales of silu(A Wg^T) * (A Wu^T), W [2F, K] = gate rows,
  * then up rows; the 8-bit sums as for bf16 above, nothing in between is rounded (with fp32 sums: ms_k_gemm_fp8 into fp32 and

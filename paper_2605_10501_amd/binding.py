@@ -643,7 +643,7 @@ def k_embedding_scaled_forward(ids, table, scale, out_fp32=False):
 
 
 def k_embedding_sorted_backward(ids, dx, scale, d_table):
-    """d_table (fp32 [vocab, d], accumulated in place and returned) += scale * the sums of dx's rows by id, in token order."""
+    """d_table (fp32 [vocab, d], accumulated in place and returned) += scale * the sums of dx's rows by id, in an order that the ids alone fix."""
     _need("dx", dx, _STORE, (None, None), None)
     n, d = dx.shape
     _need("ids", ids, _I32, (n,), dx.device)
@@ -723,7 +723,7 @@ def k_gemm_fp8(a, sa, w, sw, residual=None, c=None, c_fp32=None, fast_sums=False
 
 
 def k_gemm_fp8_config(tile=0):
-    """Tile of the 8-bit products (tests, measurements): 0 / 256256 / 256192 / 128128 / 128129 / 64128 / 64129 / 64064."""
+    """Tile of the 8-bit products (tests, measurements): 0 / 256256 / 256192 / 128128 / 128129 / 64128 / 64129 / 64064; 16016: the kernel without tiles."""
     _check(lib().ms_k_gemm_fp8_config(int(tile)))
 
 

@@ -9,7 +9,7 @@ enum { F256 = 256256, F192 = 256192, F128 = 128128, F128R = 128129, F64x128 = 64
 // us_round: prologue and epilogue of a round; us_call: once.  Fits to sweeps on MI355X with operands that have left the caches: 13 weight
 // matrices (256 x 688 .. 22016 x 4096) x 21 token counts (24 .. 16384) for 8-bit sums, 7 x 13 for fp32 sums, 4 x 16 for SwiGLU, and 7 x 10 (896 x 4096 ..
 // 22016 x 4096, 65 .. 6000 tokens) for the 256-row tiles of 8-bit sums; K tiles are rounded up to the kernel's stages.  Over those 70 the chosen tile is
-// 0.1 % slower than the best one in the mean and 5 % at most (before there was one of 192 outputs, which fills last rounds that the others leave
+// 0.1 % slower than the best tile (the kernel without tiles left out) in the mean and 5 % at most (before there was one of 192 outputs, which fills last rounds that the others leave
 // half empty: 3.6 % and 48 %).  Each is the best one of some: 256 x 192 of 14 (4096 x 6144 x 4096: 89 us, 128 x 128 and 256 x 256 100), 256 x 256,
 // 128 x 128 and its ring of 12 each, 64 x 64 of 13, the ring of 64 x 128 of 7; 64 x 128 with two stages of some of the larger sweep.
 struct Fp8Tile { int code, bm, bn, per_cu, stages; double us_per_ktile[4], us_round, us_call; };
@@ -44,6 +44,9 @@ template <size_t N> inline int fp8_choose(const Fp8Tile (&tiles)[N], long m, lon
 }
 
 // The kernel without tiles in LDS: up to 16 rows, and up to 64 while the workgroups are all there at once, because each 16 rows read the
-// weights again (32 rows, us, without / with tiles: 4096 x 4096 8.5 / 9.6, 22016 x 4096 40 / 25)
+// weights again (32 rows, us, without / with tiles: 4096 x 4096 8.5 / 9.6, 22016 x 4096 41 / 25).  Above 64 rows it is still the faster one for small
+// matrices: 65 x 896 x 4096 9.2 / 10.5, 200 x 688 x 256 3.6 / 4.4, 600 x 688 x 256 4.9 / 4.5, in fp32 sums 293 x 256 x 688 3.8 / 7.0, 600 x 256 x 688 4.7 / 7.1; but there a row's bits
+// would depend on how many share the call.
 constexpr int kFp8DirectRows = 64;
+constexpr int kFp8DirectMost = 65535 * 16;       // rows of a launch
 inline bool fp8_direct(long M, long N) { return M <= 16 || (M <= kFp8DirectRows && (M + 15) / 16 * ((N + 31) / 32) <= 256); }

@@ -238,7 +238,9 @@ __device__ __forceinline__ void stage_scales(const Fp8Params &p, uint8_t *pa, ui
 }
 
 // Most calls want bf16 without a residual.  The kernels have that by itself: store_row's other forms, unrolled over the accumulators, are ten
-// times the code, more than the instruction cache holds (256 x 256 tile, 32768 x 22016 x 4096: 2.60 ms with one form for all, 2.45 so).
+// times the code, more than the instruction cache holds (256 x 256 tile, 32768 x 22016 x 4096: 2.60 ms with one form for all, 2.45 so).  Onto the fp32 stream, as
+// a section's output and down projections go, a product takes longer by what it reads and writes more (8 bytes per output instead of 2): 32768 x 4096 x 11008
+// 1.10 ms in bf16, 1.18 into fp32, 1.28 onto an fp32 residual; 32768 x 4096 x 4096 0.45, 0.50, 0.65; 777 x 2048 x 5504 18.2 us, 20.9, 20.9.
 __device__ __forceinline__ bool plain_rows(const Fp8Params &p) { return p.vec && !p.c_fp32 && !p.R; }
 template <int NV> __device__ __forceinline__ void store_plain(const Fp8Params &p, int m, int n, const float *v) {
     if (m >= p.M || n >= p.N) return;
@@ -752,7 +754,9 @@ ms_status launch_gemm(Fp8Params p, int rows, bool precise, hipStream_t s) {
     bool fits = true;
     const int forced = g_tile.load();
     if (forced ? forced == FDIRECT : fp8_direct(rows, p.N)) {
-        if (precise) launch_direct<true>(p, s); else launch_direct<false>(p, s);
+        fits = p.M <= kFp8DirectMost;
+        if (fits && precise) launch_direct<true>(p, s);
+        else if (fits) launch_direct<false>(p, s);
     } else {
         const int tile = forced && !(precise && (forced == F256 || forced == F192)) ? forced : precise ? fp8_choose(kFp8Precise, p.M, p.N, p.kb) : fp8_choose(kFp8Fast, p.M, p.N, p.kb);
         fits = !precise && tile == F256 ? launch_big<256, false>(p, s) : !precise && tile == F192 ? launch_big<192, false>(p, s) : precise ? launch_tile<true>(tile, p, s) : launch_tile<false>(tile, p, s);

@@ -508,3 +508,24 @@ def test_one_kind_of_sums_is_asked_for():
     call = lambda kind, ldc=64, c=256: f(4, 64, 128, 256, 128, 256, 4, 256, 128, 256, 4, c, ldc, kind, None, 0, 0, None)
     assert call(4) == -1 and call(-1) == -1 and call(3, 63) == -2
     assert call(3, c=257) == -4 and call(1, c=258) == -4                     # 3 is a bf16 result
+
+
+def test_the_kernel_for_few_rows_can_be_asked_for(fp8_tile):
+    """With any number of rows that one launch takes; more are refused."""
+    fp8_tile(16016)
+    f = B._fn("ms_k_gemm_fp8")
+    assert f(65535 * 16 + 1, 64, 128, 256, 128, 256, 4, 256, 128, 256, 4, 1 << 30, 64, 0, None, 0, 0, None) == -4
+    assert b"too large for one launch" in B.lib().ms_last_error()
+
+
+@pytest.mark.gpu
+def test_the_kernel_for_few_rows_with_many(fp8_tile):
+    a, w = operands(700, 100, 688)
+    ref, size = product(a, w)
+    fp8_tile(16016)
+    close(B.k_gemm_fp8(*a, *w), ref, size, 688, "bf16", cut_off(a, w))
+    close(B.k_gemm_fp8(*a, *w, c_fp32=True), ref, size, 688, "fp32")
+    a, w = operands(100, 256, 272)
+    got = B.k_gemm_fp8_swiglu(*a, *w)
+    fp8_tile(64128)
+    assert all(torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(got, B.k_gemm_fp8_swiglu(*a, *w)))
