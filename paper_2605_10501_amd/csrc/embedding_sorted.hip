@@ -1,7 +1,8 @@
 // Embedding rows times a scale, and the table's gradient from the tokens sorted by id.
 //
 //   forward   x[t] = round(scale E[id_t])
-//   backward  dE[v] += scale sum_{t: id_t = v} dx[t], tokens in ascending order within pieces of kTile sorted places, pieces in order
+//   backward  dE[v] += scale sum_{t: id_t = v} dx[t]: tokens in ascending order within pieces of 8 or 32 sorted places; of a run that spans pieces,
+//             every fourth piece in ascending order, then those four sums
 //
 // The gradient needs no floating-point atomics: its sums have one order, so a run repeats bit for bit, and a row that thousands
 // of tokens share (padding, frequent words) is not added to by thousands of atomics.  Steps:
@@ -10,7 +11,8 @@
 //      does all digits in LDS.  Ids outside the table sort last.
 //   2. pieces of 8 or 32 sorted places x one 16-byte column vector per thread: one pass over dx.  A run of equal ids that lies within
 //      the piece is added to the table; what continues from or into a neighbour goes to a row of partial sums.
-//   3. the runs that span pieces (step 2 lists them): their partial rows are added up and go to the table.
+//   3. the runs that span pieces (step 2 lists them): their partial rows are added up, in four interleaved groups whose sums follow in order, and go to
+//      the table.
 // HBM bounds step 2 (dx read once, touched rows read and written), launches and latency the sort.
 #include "common.h"
 #include "embedding_plan.h"
@@ -23,7 +25,8 @@ constexpr int kWaves = kSortThreads / 64, kBins = 1 << kDigitBits;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ forward
-// Rows leave non-temporally, table rows stay: 32768 tokens x 1536 25.1 -> 23.1 us (4.7 -> 5.1 TB/s with 12200 distinct ids), x 4096 78 -> 63, 4096 x 1024 3.9 -> 3.3
+// Rows leave non-temporally, table rows stay: 32768 tokens x 1536 25.1 -> 23.1 us, x 4096 78 -> 63, 4096 x 1024 3.9 -> 3.3 (repeated passes, which find the
+// batch's 12200 table rows in the caches; 35.9 us, 3.8 TB/s, for the first where they come from memory)
 template <class T, class TO, int U>
 __global__ __launch_bounds__(256) void embedding_scaled_kernel(const int *__restrict__ ids, const T *__restrict__ table, TO *__restrict__ x,
                                                                float scale, int n, int vpr, int vocab) {
@@ -243,7 +246,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int *__r
 // part: [pieces][2][d]: row 0 the end of a run that began in an earlier piece, row 1 the part of a run that goes on in the next.
 // runs[0] counts, runs[1 ..] list the pieces in which a run begins that goes on (in any order: each is added up by itself).
 // U places at a time: their rows of dx and the table rows of the runs that end there are requested together.  STREAM: dx by the non-temporal policy,
-// above 80 MB (us, without / with: 32768 x 1536 85.8 / 80.9, x 4096 190 / 159; 16384 x 1024, 34 MB, 51.4 / 56.5).
+// above 80 MB (us of the whole gradient, without / with, x 1536 in bf16: 34 MB 49 / 50, 50 MB 60 / 56, 67 MB 66 / 62, 101 MB 80 / 76, 202 MB 148 / 135; x 768 in fp32: 34
+// MB 38 / 40, 50 MB 42 / 44, 67 MB 48 / 48, 101 MB 62 / 58, 202 MB 101 / 91).
 template <class T, int TILE, int U, bool STREAM>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint2 *__restrict__ sorted, const T *__restrict__ dx, float scale, int n, int vpr,
                                                             int vocab, float *__restrict__ d_table, float *__restrict__ part, int *__restrict__ runs,

@@ -16,8 +16,8 @@ namespace {
 
 constexpr int kPartRows = 768;       // workgroups of the backward kernel, one partial row of dg each: three per CU, as its registers allow (four need spills and are no faster)
 
-// Results leave non-temporally: 20011 tokens x 16 heads forward 33.9 -> 28.8 us, 4096 x 24 12.1 -> 9.8, backward 3-8 % (loads by that policy
-// too gain 2 % on the largest batches and lose up to 18 % on small ones)
+// Results leave non-temporally: 20011 tokens x 16 heads forward 33.9 -> 28.8 us, 4096 x 24 12.1 -> 9.8, backward 3-8 % (repeated passes on operands that
+// the caches hold in part; 32.5 us on operands from memory.  Loads by that policy too gain 2 % on the largest batches and lose up to 18 % on small ones)
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 template <class T> __device__ __forceinline__ void put(T *p, const Vec16<T> &r) { __builtin_nontemporal_store(*(const u32x4 *)&r, (u32x4 *)p); }
 
@@ -261,7 +261,9 @@ extern "C" ms_status ms_k_qk_norm_rope_forward(int32_t dtype, int32_t n, int32_t
     MS_TRY(check("qk_norm_rope_forward", dtype, a, false));
     const int g = lanes_per_head(dtype, head_dim), hpw = 64 / g;
     const int heads = n_q_heads + (y == x ? 1 : 2) * n_kv_heads, steps = ms_cdiv(heads, hpw);
-    // few tokens: a wave per group of heads; many: a wave per token
+    // Few tokens: a wave per group of heads, for more waves; many: a wave per token, which reads its angles once.  us, group / token, operands from memory: 32 + 8
+    // heads of 128 in bf16 16 tokens 3.5 / 6.3, 1024 7.5 / 8.9, 2048 11.1 / 10.9, 4096 18.8 / 19.3, 6000 37.7 / 32.6, 32768 203 / 153; 12 + 2 heads 1024 4.7 / 5.1, 3000
+    // 7.4 / 6.8, 4096 8.3 / 7.7, 32768 49 / 44; 16 + 4 heads of 64 2048 5.4 / 5.6, 4096 8.1 / 7.1; 2 + 2 heads are one group
     const int spw = n >= 4096 ? steps : 1;
     const long gx = ms_cdiv(n, 4) < (1 << 20) ? ms_cdiv(n, 4) : (1 << 20);
     const dim3 grid((unsigned)gx, (unsigned)ms_cdiv(steps, spw));
