@@ -188,6 +188,8 @@ class SectionOptions:
 def _layer_options(layers, n):
     if layers is None:
         return None
+    if len(layers) > n:
+        raise ValueError(f"section options: {len(layers)} layers' worth for a section of {n}")
     arr = (LayerOptions * n)()
     for i, lo in enumerate(layers):
         for f in _OPTION_FIELDS:

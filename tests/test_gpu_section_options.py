@@ -470,3 +470,12 @@ def test_workspace_of_fp32_sums():
     size = lambda n, **o: B.section_workspace_bytes(cfg, n, n, False, B.SectionOptions(fp8=True, layers=fake, **o))
     sizes = [size(n, fp32_sums=True) for n in (1, 2, 63, 64, 65, 130, 4096)]
     assert sizes == sorted(sizes) and sizes[-1] >= 4096 * 2 * cfg.d_ffn * 4
+
+
+def test_options_for_more_layers_than_there_are_are_refused():
+    """Also where the section reads none of them."""
+    cfg = config("bf16", n_layers=2)
+    for o in (B.SectionOptions(embed_scale=2.0, layers=[{}] * 3), B.SectionOptions(qk_norm=True, layers=[{}] * 3)):
+        with pytest.raises(ValueError, match="section of 2"):
+            B.section_workspace_bytes(cfg, 8, 8, False, o)
+    assert B.section_workspace_bytes(cfg, 8, 8, False, B.SectionOptions(embed_scale=2.0, layers=[{}])) > 0
