@@ -203,6 +203,78 @@ ms_status ms_kd_loss_forward_backward_static(const ms_kd_config *kd, int32_t n_t
                                              const void *h_student, float *loss_dev, float *kl_per_token_dev,
                                              void *d_h_student, void *d_w_student, void *stream);
 
+/* Training on something else than a whole teacher, and what that takes: every call meets the vocabulary inside, as the
+ * distillation loss above does.  z = h w^T / T are the logits of a token, w the lm_head [vocab, hidden], h its hidden states
+ * [n_tokens, hidden]; q = softmax(z).
+ *   - labels: int32, one id per token; a token whose label is outside [0, vocab) (a prompt's, padding) is left out: it has log-probability 0
+ *     in the outputs, no term in the loss, a zero gradient, and nothing of it is read but its label: hidden states and the other per-token
+ *     inputs may hold anything there, NaN included.
+ *   - d_h (storage type, [n_tokens, hidden]) is overwritten, and may be h itself; d_w (fp32, [vocab, hidden]) is accumulated.  Either may be
+ *     NULL; both NULL: forward only.  loss_dev: device float.
+ *   - A bf16 head keeps e^(z - reference) of a block's tokens (bf16, [tokens, vocab]) between the two halves of the pass instead of computing the logits
+ *     twice; that is where the gradient of the logits is rounded to the storage type.  token_block: the tokens of a block (a multiple of 8;
+ *     0: as many as 16 GB hold).  A preference loss has all its tokens in one block.
+ *   - vocab and hidden: multiples of 8.  Alignment: 16 bytes for h, w, d_h and d_w, else 4.  Refused (MS_ERR_UNSUPPORTED) otherwise.
+ * n_tokens == 0: a loss of 0. */
+typedef struct {
+    int32_t vocab, hidden, dtype, token_block;
+    float temperature;             /* T                                                */
+    float loss_scale;              /* loss = loss_scale * sum of the terms             */
+    const void *w_dev;             /* [vocab, hidden]                                  */
+} ms_head_config;
+
+/* k: entries per token of ms_topk_kd_loss_forward_backward, 0 for the calls with labels */
+size_t ms_head_workspace_bytes(const ms_head_config *cfg, int32_t max_tokens, int32_t k, int32_t need_backward);
+size_t ms_preference_workspace_bytes(const ms_head_config *cfg, int32_t max_tokens, int32_t max_pairs, int32_t need_backward);
+size_t ms_top_logits_workspace_bytes(const ms_head_config *cfg, int32_t max_tokens, int32_t k);
+
+/* The k (1 .. 128) largest logits h w^T (without T) of each token, largest first, equal ones by their ids: values (fp32) and ids (int32), [n_tokens, k];
+ * lse [n_tokens] = ln sum_v e^z.  A token with a NaN among its logits has a NaN lse, and entries without meaning (ids in range or -1). */
+ms_status ms_top_logits(const ms_head_config *cfg, int32_t n_tokens, const void *h, int32_t k, float *values, int32_t *ids,
+                        float *lse, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Distillation from a teacher's k stored logits t of each token (top_logits fp32, top_ids int32, [n_tokens, k], in any order):
+ *   p = e^(t / T - L),  L = lse_teacher[token] (at the same T), or, if that is NULL, ln of the sum of the token's e^(t / T) (then sum p = 1)
+ *   kl_per_token = sum over the entries of p (ln p - ln q),   dz = (loss_scale / T) (q sum p - p)
+ * An entry whose id is outside [0, vocab), or stands in the token's list before it, is ignored; a token without an entry (or with none
+ * above -inf) is left out as above. */
+ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *cfg, int32_t n_tokens, const void *h, int32_t k,
+                                           const int32_t *top_ids, const float *top_logits, const float *lse_teacher,
+                                           float *loss_dev, float *kl_per_token_dev, void *d_h, void *d_w,
+                                           void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* logp[token] = ln q(label); backward: the gradients of sum_token d_logp logp (loss_scale is not used; logp may be NULL). */
+ms_status ms_token_logprobs(const ms_head_config *cfg, int32_t n_tokens, const void *h, const int32_t *labels, float *logp,
+                            void *workspace_dev, size_t workspace_bytes, void *stream);
+ms_status ms_token_logprobs_backward(const ms_head_config *cfg, int32_t n_tokens, const void *h, const int32_t *labels,
+                                     const float *d_logp, float *logp, void *d_h, void *d_w,
+                                     void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Clipped policy loss with a KL term; all inputs fp32 [n_tokens], weights and ref_logp may be NULL (1; no KL term, kl_coef is 0 then):
+ *   r = e^(logp - old_logp),  u = ref_logp - logp
+ *   loss_tok = weight (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^u - u - 1))
+ * A ratio on a border counts as inside.  loss_tok and logp [n_tokens] may be NULL. */
+typedef struct {
+    float clip_low, clip_high, kl_coef;     /* 0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0 */
+} ms_policy_config;
+ms_status ms_policy_loss_forward_backward(const ms_head_config *cfg, const ms_policy_config *policy, int32_t n_tokens,
+                                          const void *h, const int32_t *labels, const float *old_logp, const float *ref_logp,
+                                          const float *advantages, const float *weights, float *loss_dev, float *loss_tok,
+                                          float *logp, void *d_h, void *d_w, void *workspace_dev, size_t workspace_bytes,
+                                          void *stream);
+
+/* Preference loss: sequences 2 i and 2 i + 1 of the batch are the chosen and the rejected answer of pair i.
+ *   margin = sum_chosen (logp - ref_logp) - sum_rejected (logp - ref_logp),  x = beta margin    (ref_logp NULL: 0)
+ *   loss = loss_scale sum_pairs -(1 - label_smoothing) ln s(x) - label_smoothing ln s(-x),   s(x) = 1 / (1 + e^-x)
+ * A pair without any token that counts has margin 0 and no term.  margin [pairs] and logp [n_tokens] may be NULL. */
+typedef struct {
+    float beta, label_smoothing;            /* beta > 0, 0 <= label_smoothing < 1 */
+} ms_preference_config;
+ms_status ms_preference_loss_forward_backward(const ms_head_config *cfg, const ms_preference_config *preference,
+                                              const ms_batch *batch, const void *h, const int32_t *labels, const float *ref_logp,
+                                              float *loss_dev, float *margin, float *logp, void *d_h, void *d_w,
+                                              void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* Vision -> language hand-off (Sec. 2.1 and Sec. 4.1: the encoder's visual tokens are down-sampled 4:1 along the
  * sequence and joined with the text tokens to form the LLM's input; the operator itself is a reading: patch
  * merger + MLP projector).  Group g = visual tokens merge*g .. merge*g + merge-1 of the packed encoder output

@@ -535,11 +535,20 @@ _ARGTYPES = {
     "ms_k_swiglu_fp8": _args("iii", "plplplp"),
     "ms_k_gemm_fp8": _args("iii", "plplplpl", "plipli", "p"),
     "ms_k_gemm_fp8_swiglu": _args("iii", "plplplpl", "plpl", "pzp"),
+    "ms_top_logits": _args("pip", "ippp", "pzp"),
+    "ms_topk_kd_loss_forward_backward": _args("pip", "ippp", "pppp", "pzp"),
+    "ms_token_logprobs": _args("pippp", "pzp"),
+    "ms_token_logprobs_backward": _args("pipp", "pppp", "pzp"),
+    "ms_policy_loss_forward_backward": _args("ppipp", "pppp", "ppppp", "pzp"),
+    "ms_preference_loss_forward_backward": _args("ppppp", "p", "ppppp", "pzp"),
 }
 _SCRATCH = {
     "ms_k_qk_norm_rope_backward_scratch_bytes": _args("i"),
     "ms_k_embedding_sorted_backward_scratch_bytes": _args("iii"),
     "ms_k_gemm_fp8_swiglu_scratch_bytes": _args("iii"),
+    "ms_head_workspace_bytes": _args("piii"),
+    "ms_top_logits_workspace_bytes": _args("pii"),
+    "ms_preference_workspace_bytes": _args("piii"),
 }
 _fns = {}
 
@@ -743,6 +752,145 @@ def k_gemm_fp8_swiglu(a, sa, w, sw, fp32_sums=False):
     sc = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
     _call("ms_k_gemm_fp8_swiglu", dev, m, f, *args[2:], q.data_ptr(), f, s.data_ptr(), s.shape[1], sc.data_ptr() if nb else None, nb)
     return q, s
+
+
+# ------------------------------------------------------------------ losses and log-probabilities at the end of a section
+class _HeadCfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("vocab", "hidden", "dtype", "token_block")] + [("temperature", C.c_float), ("loss_scale", C.c_float), ("w_dev", C.c_void_p)]
+
+
+class _PolicyCfg(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_coef")]
+
+
+class _PreferenceCfg(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("beta", "label_smoothing")]
+
+
+def _head(h, w, temperature, loss_scale, token_block, need_d_h=False, d_w=None):
+    """(config, tokens, d_h or None), arguments checked."""
+    _need("h", h, _STORE, (None, None), None)
+    _need("w", w, (h.dtype,), (None, h.shape[1]), h.device)
+    if d_w is not None:
+        _need("d_w", d_w, _F32, w.shape, h.device)
+    c = _HeadCfg(w.shape[0], w.shape[1], _dt(h.dtype), int(token_block), float(temperature), float(loss_scale), w.data_ptr())
+    return c, h.shape[0], torch.empty_like(h) if need_d_h else None
+
+
+def _per_token(dev, n, **named):
+    for name, t in named.items():
+        if t is not None:
+            _need(name, t, _I32 if name == "labels" else _F32, (n,), dev)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _head_ws(ws, query, c, *args, device):
+    if ws is None:
+        return workspace(_fn(query)(C.byref(c), *args), device)
+    _need("ws", ws, (torch.uint8,), (None,), device)
+    return ws
+
+
+def head_workspace_bytes(w, max_tokens, k=0, need_backward=True, token_block=0):
+    """Workspace of the calls with labels (k = 0) or with k entries per token."""
+    c = _HeadCfg(w.shape[0], w.shape[1], _dt(w.dtype), int(token_block), 1.0, 1.0, w.data_ptr())
+    return _fn("ms_head_workspace_bytes")(C.byref(c), max_tokens, k, int(need_backward))
+
+
+def top_logits(h, w, k, temperature=1.0, token_block=0, ws=None):
+    """The k largest logits h w^T of each row, largest first (equal ones by their ids): (values fp32 [n, k], ids int32 [n, k], lse [n] of all logits / T)."""
+    c, n, _ = _head(h, w, temperature, 1.0, token_block)
+    dev = h.device
+    ws = _head_ws(ws, "ms_top_logits_workspace_bytes", c, n, k, device=dev)
+    values, ids = torch.empty((n, max(k, 0)), dtype=torch.float32, device=dev), torch.empty((n, max(k, 0)), dtype=torch.int32, device=dev)
+    lse = torch.empty(n, dtype=torch.float32, device=dev)
+    _call("ms_top_logits", dev, C.byref(c), n, h.data_ptr(), k, values.data_ptr(), ids.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel())
+    return values, ids, lse
+
+
+def topk_kd_loss_forward_backward(h, w, top_ids, top_logits, lse_teacher=None, temperature=1.0, loss_scale=None, need_d_h=True, d_w=None, token_block=0, ws=None):
+    """Distillation from a teacher's stored logits (top_ids int32, top_logits fp32, [n, k]; ids outside the vocabulary or repeated are ignored).
+    lse_teacher: log-sum-exp of the teacher's whole vocabulary at T; without it the entries' probabilities sum to 1.  Returns dict(loss, kl_tok, d_h);
+    d_w (fp32, as w) is accumulated in place.  loss_scale: 1 / n by default."""
+    n = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
+    c, n, d_h = _head(h, w, temperature, 1.0 / max(n, 1) if loss_scale is None else loss_scale, token_block, need_d_h, d_w)
+    dev = h.device
+    _need("top_ids", top_ids, _I32, (n, None), dev)
+    k = top_ids.shape[1]
+    _need("top_logits", top_logits, _F32, (n, k), dev)
+    _per_token(dev, n, lse_teacher=lse_teacher)
+    ws = _head_ws(ws, "ms_head_workspace_bytes", c, n, k, int(need_d_h or d_w is not None), device=dev)
+    loss, kl = torch.empty((), dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
+    _call("ms_topk_kd_loss_forward_backward", dev, C.byref(c), n, h.data_ptr(), k, top_ids.data_ptr(), top_logits.data_ptr(), _ptr(lse_teacher), loss.data_ptr(),
+          kl.data_ptr(), _ptr(d_h), _ptr(d_w), ws.data_ptr(), ws.numel())
+    return dict(loss=loss, kl_tok=kl, d_h=d_h)
+
+
+def token_logprobs(h, w, labels, temperature=1.0, token_block=0, ws=None):
+    """ln softmax(h w^T / T)[label] of each row, fp32 [n]; 0 where the label (int32) is outside the vocabulary."""
+    c, n, _ = _head(h, w, temperature, 1.0, token_block)
+    dev = h.device
+    _need("labels", labels, _I32, (n,), dev)
+    ws = _head_ws(ws, "ms_head_workspace_bytes", c, n, 0, 0, device=dev)
+    logp = torch.empty(n, dtype=torch.float32, device=dev)
+    _call("ms_token_logprobs", dev, C.byref(c), n, h.data_ptr(), labels.data_ptr(), logp.data_ptr(), ws.data_ptr(), ws.numel())
+    return logp
+
+
+def token_logprobs_backward(h, w, labels, d_logp, temperature=1.0, need_d_h=True, d_w=None, token_block=0, ws=None):
+    """Gradients of sum(d_logp * token_logprobs(h, w, labels)): dict(logp, d_h); d_w (fp32, as w) is accumulated in place."""
+    c, n, d_h = _head(h, w, temperature, 1.0, token_block, need_d_h, d_w)
+    dev = h.device
+    _need("labels", labels, _I32, (n,), dev)
+    _need("d_logp", d_logp, _F32, (n,), dev)
+    ws = _head_ws(ws, "ms_head_workspace_bytes", c, n, 0, 1, device=dev)
+    logp = torch.empty(n, dtype=torch.float32, device=dev)
+    _call("ms_token_logprobs_backward", dev, C.byref(c), n, h.data_ptr(), labels.data_ptr(), d_logp.data_ptr(), logp.data_ptr(), _ptr(d_h), _ptr(d_w), ws.data_ptr(), ws.numel())
+    return dict(logp=logp, d_h=d_h)
+
+
+def policy_loss_forward_backward(h, w, labels, old_logp, advantages, clip_low=0.2, clip_high=0.2, ref_logp=None, kl_coef=0.0, weights=None, temperature=1.0,
+                                 loss_scale=None, need_d_h=True, d_w=None, token_block=0, ws=None):
+    """Clipped policy loss over the tokens with a label inside the vocabulary, with a KL term towards ref_logp if kl_coef > 0; all per-token inputs fp32.
+    Returns dict(loss, loss_tok, logp, d_h); d_w (fp32, as w) is accumulated in place.  loss_scale: 1 / n by default."""
+    n = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
+    c, n, d_h = _head(h, w, temperature, 1.0 / max(n, 1) if loss_scale is None else loss_scale, token_block, need_d_h, d_w)
+    dev = h.device
+    _need("labels", labels, _I32, (n,), dev)
+    _need("old_logp", old_logp, _F32, (n,), dev)
+    _need("advantages", advantages, _F32, (n,), dev)
+    _per_token(dev, n, ref_logp=ref_logp, weights=weights)
+    pc = _PolicyCfg(clip_low, clip_high, kl_coef)
+    ws = _head_ws(ws, "ms_head_workspace_bytes", c, n, 0, int(need_d_h or d_w is not None), device=dev)
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    loss_tok, logp = (torch.empty(n, dtype=torch.float32, device=dev) for _ in range(2))
+    _call("ms_policy_loss_forward_backward", dev, C.byref(c), C.byref(pc), n, h.data_ptr(), labels.data_ptr(), old_logp.data_ptr(), _ptr(ref_logp), advantages.data_ptr(),
+          _ptr(weights), loss.data_ptr(), loss_tok.data_ptr(), logp.data_ptr(), _ptr(d_h), _ptr(d_w), ws.data_ptr(), ws.numel())
+    return dict(loss=loss, loss_tok=loss_tok, logp=logp, d_h=d_h)
+
+
+def preference_loss_forward_backward(h, w, labels, batch, beta, ref_logp=None, label_smoothing=0.0, temperature=1.0, loss_scale=None, need_d_h=True, d_w=None, ws=None):
+    """Preference loss; sequences 2 i and 2 i + 1 of `batch` (Batch) are the chosen and the rejected answer of pair i.  Returns dict(loss, margin [pairs],
+    logp, d_h); d_w (fp32, as w) is accumulated in place.  loss_scale: 1 / pairs by default."""
+    pairs = batch.n_seqs // 2
+    c, n, d_h = _head(h, w, temperature, 1.0 / max(pairs, 1) if loss_scale is None else loss_scale, 0, need_d_h, d_w)
+    dev = h.device
+    if batch.n_tokens != n:
+        raise ValueError(f"batch: expected sequences of {n} tokens, got {batch.n_tokens}")
+    if batch.cu_dev.device != dev:
+        raise ValueError(f"batch: expected one on {dev}, got {batch.cu_dev.device}")
+    _need("labels", labels, _I32, (n,), dev)
+    _per_token(dev, n, ref_logp=ref_logp)
+    pc, b = _PreferenceCfg(beta, label_smoothing), batch.c()
+    ws = _head_ws(ws, "ms_preference_workspace_bytes", c, n, pairs, int(need_d_h or d_w is not None), device=dev)
+    loss, margin = torch.empty((), dtype=torch.float32, device=dev), torch.empty(pairs, dtype=torch.float32, device=dev)
+    logp = torch.empty(n, dtype=torch.float32, device=dev)
+    _call("ms_preference_loss_forward_backward", dev, C.byref(c), C.byref(pc), C.byref(b), h.data_ptr(), labels.data_ptr(), _ptr(ref_logp), loss.data_ptr(),
+          margin.data_ptr(), logp.data_ptr(), _ptr(d_h), _ptr(d_w), ws.data_ptr(), ws.numel())
+    return dict(loss=loss, margin=margin, logp=logp, d_h=d_h)
 
 
 def k_colsum(x, out=None):

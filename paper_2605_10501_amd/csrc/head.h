@@ -1,0 +1,36 @@
+// Losses and log-probabilities at the end of a decoder section (head.hip): what a call needs of the workspace, and which calls are
+// accepted.  No device code: this part also builds for the host alone.
+#pragma once
+#include "common.h"
+
+constexpr int kHeadMaxTop = 128;             // entries of a token that the kernels hold
+constexpr int kStrip = 64;                   // columns that share one partial sum
+
+// Rows of hidden states meet the vocabulary a block of tokens at a time.  What a block keeps of every (row, vocabulary entry) lies in
+// slabs of `cols` columns, [slab][rows][cols], because a matrix product's operand has to be within reach of 32-bit offsets.
+struct HeadPlan {
+    int rows, cols, slabs, strips;           // of a block; strips over all slabs, cols / kStrip in each but the last
+    bool fast;                               // bf16 products whose epilogue meets the logits (head_gemm.hip)
+    int *slot, *token, *count;               // [rows] row of a token, [rows] token of a row (-1: none), [1] rows in use
+    void *h;                                 // [rows, hidden] hidden states of the rows, later times the row's factor
+    float *ref, *scale;                      // [rows] reference of a row's exponentials in units of log2 e, factor of a row's gradient
+    float2 *stat;                            // [rows] sum of exponentials and its reference
+    float *z_sel, *rho;                      // [rows, k] logits at the selected ids, and what a row has there in its gradient
+    float *log_p, *mass;                     // [rows, k], [rows] of the teacher's entries
+    int *ids;                                // [rows, k] the entries that count (-1: ignored)
+    int *key;                                // [rows] < 0: the token is left out
+    float *logp, *grad;                      // [rows] by token of the block
+    float2 *part;                            // [strips, rows]
+    float *d_h;                              // [rows, hidden]
+    void *z;                                 // slabs: logits (fp32), or their exponentials (bf16)
+    void *dz;                                // [rows, cols] gradient of a slab's logits where it does not take the logits' place
+    float *per_token, *margin;               // [n] terms of the loss, or [pairs] both
+    size_t bytes;
+};
+
+enum HeadUse { HEAD_TOP = 0, HEAD_FORWARD = 1, HEAD_BACKWARD = 2 };
+
+// pairs >= 0: a preference loss of that many pairs, all n tokens in one block
+HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws);
+long head_most_rows(const ms_head_config *c);                              // of a block
+ms_status validate_head(const ms_head_config *c, int n, int k, const char *what);

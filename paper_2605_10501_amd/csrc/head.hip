@@ -1,0 +1,791 @@
+// Losses, log-probabilities and top logits at the end of a decoder section (maestro_section.h).
+//
+// With x = z log2(e), z = h w^T / T the logits of a row (a token that counts), everything goes by sums of 2^(x - reference) over strips of 64 columns:
+//   lse = ln 2 (reference + log2 sum),   q_v = 2^(x_v - reference) / sum,   dz_v = scale_row q_v but at the few selected ids of the row
+// (its label, or the teacher's entries), where rho = dz / scale_row is q - 1 or q - p / sum p.  The logits there are dot products of their own.
+#include "common.h"
+#include "head.h"
+#include "launch.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Logits [slab][rows][cols] (or what is kept in their place)
+struct Slabs {
+    int rows, cols, vocab;
+    __device__ __forceinline__ long at(int row, int v) const {
+        const int s = v / cols;
+        return ((long)s * rows + row) * cols + (v - s * cols);
+    }
+};
+
+__device__ __forceinline__ float block_sum(float v, float *sm) {
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float r = 0.f;
+    for (int i = 0; i < (int)(blockDim.x >> 6); ++i) r += sm[i];
+    __syncthreads();
+    return r;
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// ------------------------------------------------------------------ which tokens count
+// The teacher's entries of a token, one wave each: the ids that count, ln p of each and the sum of p.
+__global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int vocab, float inv_t, const int *__restrict__ top_ids,
+                                                           const float *__restrict__ top, const float *__restrict__ lse_teacher,
+                                                           int *__restrict__ ids, float *__restrict__ log_p, float *__restrict__ mass, int *__restrict__ key) {
+    __shared__ int seen[4][kHeadMaxTop];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long t = (long)blockIdx.x * 4 + wave;
+    if (t < n)
+        for (int j = lane; j < k; j += 64) seen[wave][j] = top_ids[t * k + j];
+    __syncthreads();
+    if (t >= n) return;
+    float y[2], m = -INFINITY;
+    int id[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int j = lane + 64 * e;
+        id[e] = j < k ? seen[wave][j] : -1;
+        if (id[e] >= vocab) id[e] = -1;
+        if (id[e] >= 0)
+            for (int i = 0; i < j; ++i)
+                if (seen[wave][i] == id[e]) id[e] = -1;
+        y[e] = id[e] >= 0 ? top[t * k + j] * inv_t : -INFINITY;
+        m = fmaxf(m, y[e]);                                                     // (passes over NaN, which the sum has)
+    }
+    m = wave_max(m);
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (id[e] >= 0 && !(y[e] == -INFINITY)) s += expf(y[e] - (m == -INFINITY ? 0.f : m));
+    s = wave_sum(s);
+    const bool some = !(s == 0.f);                                              // an entry above -inf, or a NaN
+    const float L = lse_teacher ? (some ? lse_teacher[t] : 0.f) : m + logf(s);
+    float total = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int j = lane + 64 * e;
+        if (j >= k) continue;
+        const bool in = some && id[e] >= 0;
+        const float lp = in ? y[e] - L : -INFINITY;
+        ids[t * k + j] = in ? id[e] : -1;
+        log_p[t * k + j] = lp;
+        if (in) total += expf(lp);
+    }
+    total = wave_sum(total);
+    if (lane == 0) {
+        const bool counts = some && !(total == 0.f);
+        mass[t] = counts ? total : 0.f;
+        key[t] = counts ? 0 : -1;
+    }
+}
+
+// Rows of a block: row t for token t, or, with `compact`, the tokens that count (key in [0, limit)) in their order, without gaps.
+// One workgroup: a block has at most some 10^5 tokens, of which it reads four bytes.
+__global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__restrict__ key, int limit, int compact, int *__restrict__ slot,
+                                                         int *__restrict__ token, int *__restrict__ count) {
+    __shared__ int sm[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int base = 0;
+    for (int t0 = 0; t0 < n; t0 += 1024) {
+        const int t = t0 + threadIdx.x;
+        const bool in = t < n && key[t] >= 0 && key[t] < limit;
+        if (!compact) {
+            if (t < n) {
+                slot[t] = in ? t : -1;
+                token[t] = in ? t : -1;
+            }
+            continue;
+        }
+        const unsigned long long mask = __ballot(in);
+        if (lane == 0) sm[wave] = __popcll(mask);
+        __syncthreads();
+        int before = base, all = 0;
+        for (int i = 0; i < 16; ++i) {
+            if (i < wave) before += sm[i];
+            all += sm[i];
+        }
+        before += __popcll(mask & ((1ull << lane) - 1));
+        if (t < n) slot[t] = in ? before : -1;
+        if (in) token[before] = t;
+        base += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *count = compact ? base : n;
+}
+
+// ------------------------------------------------------------------ rows and their selected logits
+// Copies the hidden states of the rows together, and takes the logits of each row's k selected ids (h rows . w rows, fp32); the reference of the
+// row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.
+// W waves a row: one for a label, four for the teacher's entries, four ids at a time.  Rows that no token has (token -1) are zeros.
+template <class T, int W>
+__global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T *__restrict__ h, const T *__restrict__ w, const int *__restrict__ token,
+                                                           const int *__restrict__ count, const int *__restrict__ sel, float it2, T *__restrict__ out,
+                                                           float *__restrict__ z_sel, float *__restrict__ ref) {
+    __shared__ float sm[W];
+    const int row = blockIdx.x;
+    if (row >= *count) return;
+    const int t = token[row], lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int N = Vec16<T>::N;
+    if (t < 0) {
+        Vec16<T> zero;
+#pragma unroll
+        for (int e = 0; e < N; ++e) zero.v[e] = from_f32<T>(0.f);
+        for (int i = threadIdx.x * N; i < d; i += 64 * W * N) stv(out + (long)row * d + i, zero);
+        if (threadIdx.x == 0) ref[row] = 0.f;
+        return;
+    }
+    const T *hr = h + (long)t * d;
+    for (int i = threadIdx.x * N; i < d; i += 64 * W * N) stv(out + (long)row * d + i, ldv(hr + i));
+    float best = -INFINITY;
+    for (int j0 = wave * 4; j0 < k; j0 += 4 * W) {
+        const T *wr[4];
+        int id[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            id[j] = j0 + j < k ? sel[(long)t * k + j0 + j] : -1;
+            wr[j] = w + (long)(id[j] < 0 ? 0 : id[j]) * d;
+        }
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int i = lane * N; i < d; i += 64 * N) {
+            const Vec16<T> a = ldv(hr + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (id[j] < 0) continue;
+                const Vec16<T> b = ldv(wr[j] + i);
+#pragma unroll
+                for (int e = 0; e < N; ++e) acc[j] = __builtin_fmaf(to_f32(a.v[e]), to_f32(b.v[e]), acc[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[j] = wave_sum(acc[j]);
+            if (id[j] < 0) continue;
+            best = fmaxf(best, acc[j]);
+            if (lane == 0) z_sel[(long)row * k + j0 + j] = acc[j];
+        }
+    }
+    if (lane == 0) sm[wave] = best;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < W; ++i) best = fmaxf(best, sm[i]);
+        ref[row] = rintf(best * it2);
+    }
+}
+
+// ------------------------------------------------------------------ sums over the vocabulary
+// Stored fp32 logits: largest logit of a strip of 64 columns and sum of 2^(x - largest x).  One wave per strip, four per workgroup.
+__global__ __launch_bounds__(256) void head_strips_kernel(Slabs sl, int rows, int strips, const float *__restrict__ z, float it2, float2 *__restrict__ part) {
+    const int lane = threadIdx.x & 63, strip = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (strip >= strips) return;
+    for (int row = blockIdx.y; row < rows; row += gridDim.y) {
+        const int v = strip * kStrip + lane;
+        const bool in = v < sl.vocab;
+        const float a = in ? z[sl.at(row, v)] : -INFINITY;
+        const float m = wave_max(a), u = m == -INFINITY ? 0.f : m;                  // (differences first: exact near the largest, whatever its size)
+        const float s = wave_sum(in ? __builtin_amdgcn_exp2f((a - u) * it2) : 0.f);
+        if (lane == 0) part[(long)strip * sl.rows + row] = make_float2(m, s);
+    }
+}
+
+// Behind the vocabulary: sum of the strips' sums at a common reference.  part holds (offset, sum) of each strip [strips][ld]: stored logits' offsets are logits
+// (`unit` of x each), those of exponentials (`ref` given) count in x on top of the row's reference.
+// A workgroup takes `rows_per` rows (a power of two) and 1024 / rows_per shares of the strips.
+// stat[row] = (sum, offset); logp, lse: by token, where asked for.
+__global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, int rows_per, int strips, const float2 *__restrict__ part, float unit, const float *__restrict__ ref,
+                                                            const int *__restrict__ token, const int *__restrict__ count, const float *__restrict__ z_sel, float it2,
+                                                            float2 *__restrict__ stat, float *__restrict__ logp, float *__restrict__ lse) {
+    __shared__ float2 sm[1024];
+    const int r = threadIdx.x & (rows_per - 1), g = threadIdx.x / rows_per, groups = 1024 / rows_per;
+    const int row = blockIdx.x * rows_per + r, n = count ? *count : rows;
+    float m = -INFINITY, s = 0.f;
+    auto merge = [&](float mi, float si) {
+        const float to = fmaxf(m, mi), u = to == -INFINITY ? 0.f : to;
+        s = s * __builtin_amdgcn_exp2f((m - u) * unit) + si * __builtin_amdgcn_exp2f((mi - u) * unit);
+        m = to;
+    };
+    if (row < n)
+        for (int i = g; i < strips; i += groups) {
+            const float2 q = part[(long)i * ld + row];
+            merge(q.x, q.y);
+        }
+    sm[threadIdx.x] = make_float2(m, s);
+    for (int half = groups >> 1; half > 0; half >>= 1) {
+        __syncthreads();
+        if (g < half) {
+            const float2 q = sm[threadIdx.x + half * rows_per];
+            merge(q.x, q.y);
+            sm[threadIdx.x] = make_float2(m, s);
+        }
+    }
+    if (g != 0 || row >= n) return;
+    if (stat) stat[row] = make_float2(s, m);
+    const float base = ref ? ref[row] : 0.f, l2 = __log2f(s);
+    if (lse) lse[row] = kLn2 * (m * unit + l2);
+    if (logp) {
+        const int t = token[row];
+        // (x of the label - reference) first: both are near each other, and the rest is small where the label is likely
+        if (t >= 0) logp[t] = fminf(0.f, kLn2 * ((ref ? __builtin_fmaf(z_sel[row], it2, -base) - m : (z_sel[row] - m) * it2) - l2));
+    }
+}
+
+// ------------------------------------------------------------------ what a token's gradient is
+// Labels: dz = g / T (1_label - q), so scale = -g / T and rho = q - 1.
+__global__ __launch_bounds__(256) void head_label_rows_kernel(const int *__restrict__ count, const int *__restrict__ token, const float *__restrict__ logp,
+                                                              const float *__restrict__ grad, float inv_t, float *__restrict__ scale, float *__restrict__ rho) {
+    const int row = blockIdx.x * 256 + threadIdx.x;
+    if (row >= *count) return;
+    const int t = token[row];
+    scale[row] = t < 0 ? 0.f : -inv_t * grad[t];
+    rho[row] = t < 0 ? 0.f : expm1f(logp[t]);
+}
+
+struct PolicyArgs {
+    const float *old_logp, *ref_logp, *adv, *weights;
+    float low, high, kl, loss_scale;
+};
+__global__ __launch_bounds__(256) void head_policy_kernel(int n, const int *__restrict__ slot, PolicyArgs a, float *__restrict__ logp, float *__restrict__ grad,
+                                                          float *__restrict__ loss_tok) {
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t >= n) return;
+    if (slot[t] < 0) {
+        logp[t] = grad[t] = loss_tok[t] = 0.f;
+        return;
+    }
+    const float l = logp[t], adv = a.adv[t], wt = a.weights ? a.weights[t] : 1.f;
+    const float r = expf(l - a.old_logp[t]);
+    const bool inside = adv > 0.f ? r <= 1.f + a.high : r >= 1.f - a.low;          // (a NaN ratio is not; it is in `gain` all the same)
+    const float gain = adv == 0.f ? 0.f : adv * (inside || !(r == r) ? r : adv > 0.f ? 1.f + a.high : 1.f - a.low);
+    float loss = -gain, g = inside || !(r == r) ? -gain : 0.f;
+    if (a.ref_logp) {
+        const float u = a.ref_logp[t] - l, away = expm1f(u);
+        loss += a.kl * (away - u);
+        g -= a.kl * away;
+    }
+    loss_tok[t] = wt * loss;
+    grad[t] = a.loss_scale * wt * g;
+}
+
+// logp of the tokens that were left out (labels); the gradient that the caller gives
+__global__ __launch_bounds__(256) void head_given_kernel(int n, const int *__restrict__ slot, const float *__restrict__ d_logp, float *__restrict__ logp, float *__restrict__ grad) {
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t >= n) return;
+    if (slot[t] < 0) logp[t] = 0.f;
+    if (grad) grad[t] = slot[t] < 0 ? 0.f : d_logp[t];
+}
+
+// One workgroup per pair: margin, loss, and the gradient of every token of its two sequences.  Sums in 64 bits: differences of
+// some thousand logarithms each.
+__global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__ cu, const int *__restrict__ slot, const float *__restrict__ ref_logp, float beta, float smoothing,
+                                                         float loss_scale, float *__restrict__ logp, float *__restrict__ margin, float *__restrict__ loss, float *__restrict__ grad) {
+    __shared__ double sm[4];
+    __shared__ int any[4];
+    const int pair = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int a = cu[2 * pair], b = cu[2 * pair + 1], c = cu[2 * pair + 2];
+    double sum = 0.0;
+    int seen = 0;
+    for (int t = a + threadIdx.x; t < c; t += 256) {
+        if (slot[t] < 0) {
+            logp[t] = 0.f;
+            continue;
+        }
+        const double diff = (double)logp[t] - (ref_logp ? (double)ref_logp[t] : 0.0);
+        sum += t < b ? diff : -diff;
+        seen = 1;
+    }
+    sum = wave_sum_f64(sum);
+    const bool some = __any(seen);
+    if (lane == 0) {
+        sm[wave] = sum;
+        any[wave] = some;
+    }
+    __syncthreads();
+    const float m = (float)(sm[0] + sm[1] + sm[2] + sm[3]);
+    const bool counts = any[0] | any[1] | any[2] | any[3];
+    const float x = beta * m;
+    // -ln s(x) = max(-x, 0) + ln(1 + e^-|x|)
+    const float tail = log1pf(expf(-fabsf(x)));
+    const float lose = fmaxf(-x, 0.f) + tail, win = fmaxf(x, 0.f) + tail;
+    // s(x) - (1 - smoothing) = smoothing s(x) - (1 - smoothing) s(-x), each without cancellation
+    const float e = expf(-fabsf(x)), big = 1.f / (1.f + e), small = e / (1.f + e);
+    const float sp = x >= 0.f ? big : small, sn = x >= 0.f ? small : big;
+    const float g = x == x ? loss_scale * beta * (smoothing * sp - (1.f - smoothing) * sn) : x;
+    if (threadIdx.x == 0) {
+        margin[pair] = counts ? m : 0.f;
+        loss[pair] = !counts ? 0.f : x == x ? (1.f - smoothing) * lose + (smoothing > 0.f ? smoothing * win : 0.f) : x;
+    }
+    if (grad)
+        for (int t = a + threadIdx.x; t < c; t += 256) grad[t] = slot[t] < 0 ? 0.f : t < b ? g : -g;
+}
+
+// Teacher's entries, one wave per row: KL of the token, scale = loss_scale / T sum p, rho = q - p / sum p.
+__global__ __launch_bounds__(256) void head_entry_rows_kernel(int n, int k, const int *__restrict__ slot, const int *__restrict__ ids, const float *__restrict__ log_p,
+                                                              const float *__restrict__ mass, const float *__restrict__ z_sel, const float2 *__restrict__ stat, const float *__restrict__ ref,
+                                                              float it2, float coef, float *__restrict__ kl, float *__restrict__ scale, float *__restrict__ rho) {
+    const int lane = threadIdx.x & 63;
+    const long t = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= n) return;
+    const int row = slot[t];
+    if (row < 0) {
+        if (lane == 0) kl[t] = 0.f;
+        return;
+    }
+    const float2 st = stat[row];
+    const float base = ref ? ref[row] : 0.f, l2 = __log2f(st.x), inv_mass = 1.f / mass[t];
+    float sum = 0.f;
+    for (int j = lane; j < k; j += 64) {
+        if (ids[t * k + j] < 0) continue;
+        const float lp = log_p[t * k + j], p = expf(lp);
+        const float zj = z_sel[(long)row * k + j], lq = kLn2 * ((ref ? __builtin_fmaf(zj, it2, -base) - st.y : (zj - st.y) * it2) - l2);
+        if (!(p == 0.f)) sum += p * (lp - lq);
+        if (rho) rho[(long)row * k + j] = expf(lq) - p * inv_mass;
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) {
+        kl[t] = sum;
+        if (scale) scale[row] = coef * mass[t];
+    }
+}
+
+// one workgroup: the loss from its terms, in an order that only their number fixes
+__global__ __launch_bounds__(1024) void head_loss_kernel(const float *__restrict__ terms, int n, float loss_scale, float *__restrict__ loss) {
+    __shared__ float sm[16];
+    float acc = 0.f;
+    for (int i = threadIdx.x; i < n; i += 1024) acc += terms[i];
+    acc = block_sum(acc, sm);
+    if (threadIdx.x == 0) *loss = loss_scale * acc;
+}
+
+// ------------------------------------------------------------------ gradients
+// Stored fp32 logits of a slab -> their gradient (in place for fp32).  One workgroup per row.  A row without a token, or with scale 0, is zeros.
+template <class T>
+__global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int v0, int k, const int *__restrict__ token, const int *__restrict__ sel, const float *z, float it2,
+                                                      const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho, T *dz) {
+    const int row = blockIdx.x, t = token[row];
+    const float *zr = z + (long)row * d_cols;
+    T *o = dz + (long)row * d_cols;
+    const float c = t < 0 ? 0.f : scale[row];
+    if (c == 0.f) {
+        for (int i = threadIdx.x; i < cw; i += 256) o[i] = from_f32<T>(0.f);
+        return;
+    }
+    const float2 st = stat[row];
+    const float f = c / st.x;
+    for (int i = threadIdx.x; i < cw; i += 256) o[i] = from_f32<T>(f * __builtin_amdgcn_exp2f((zr[i] - st.y) * it2));
+    __syncthreads();
+    for (int j = threadIdx.x; j < k; j += 256) {
+        const int v = sel[(long)t * k + j] - v0;
+        if (v >= 0 && v < cw) o[v] = from_f32<T>(c * rho[(long)row * k + j]);
+    }
+}
+
+// d_h of the block's tokens: a row's sums times its factor; zeros for tokens that were left out
+template <class T>
+__global__ __launch_bounds__(256) void head_d_h_kernel(long total, int d, const int *__restrict__ slot, const float *__restrict__ sums, const float *__restrict__ factor, T *__restrict__ d_h) {
+    const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= total) return;
+    const int t = (int)(i / d), c = (int)(i - (long)t * d), row = slot[t];
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float f = row < 0 ? 0.f : factor ? factor[row] : 1.f;
+    if (row >= 0 && f != 0.f) {
+        v = *(const float4 *)(sums + (long)row * d + c);
+        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+    }
+    T *o = d_h + i;
+    o[0] = from_f32<T>(v.x); o[1] = from_f32<T>(v.y); o[2] = from_f32<T>(v.z); o[3] = from_f32<T>(v.w);
+}
+
+// ------------------------------------------------------------------ top logits
+// Order of values: larger first, equal ones by their place.  A NaN counts as larger than all.
+__device__ __forceinline__ unsigned ordered(float v) {
+    const unsigned u = __float_as_uint(v == v ? v + 0.f : INFINITY);                 // (+ 0: one zero)
+    return v == v ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 0xffffffffu;
+}
+__device__ __forceinline__ unsigned long long entry_key(float v, int place) { return (unsigned long long)ordered(v) << 32 | (0xffffffffu - (unsigned)place); }
+__device__ __forceinline__ float entry_value(unsigned long long key) {
+    const unsigned u = (unsigned)(key >> 32);
+    return u == 0xffffffffu ? NAN : __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+
+// sorts n (a power of two) keys in LDS, largest first
+__device__ __forceinline__ void sort_keys(unsigned long long *key, int n) {
+    for (int size = 2; size <= n; size <<= 1)
+        for (int step = size >> 1; step > 0; step >>= 1) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < n >> 1; i += blockDim.x) {
+                const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
+                const unsigned long long a = key[lo], b = key[hi];
+                if (((lo & size) == 0) == (a < b)) {
+                    key[lo] = b;
+                    key[hi] = a;
+                }
+            }
+        }
+    __syncthreads();
+}
+
+// The k largest logits of a row, one workgroup each.  They lie in the k strips with the largest maxima (equal ones by their place): an entry of another
+// strip has k maxima before it.  So: those strips, by the bits of the k-th largest maximum (four passes over a histogram of eight bits each); their entries
+// that are not below that maximum, which are few more than k; those sorted.
+constexpr int kTopThreads = 256;
+__global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int strips, int k, const float *__restrict__ z, const float2 *__restrict__ part,
+                                                               float *__restrict__ values, int *__restrict__ ids) {
+    __shared__ unsigned hist[256], sh_prefix;
+    __shared__ int sh_want, n_strips, n_keys, wsum[kTopThreads / 64];
+    __shared__ int list[kHeadMaxTop];
+    __shared__ unsigned long long keys[kHeadMaxTop * kStrip];
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int want = k < strips ? k : strips;
+    // the `want`-th largest maximum, eight bits at a time
+    unsigned prefix = 0;
+    int left = want;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = tid; i < 256; i += kTopThreads) hist[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < strips; i += kTopThreads) {
+            const unsigned o = ordered(part[(long)i * sl.rows + row].x);
+            if (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(o >> shift) & 255], 1u);
+        }
+        __syncthreads();
+        if (wave == 0) {                                                             // from the top bin down: where the count passes `left`
+            unsigned h[4], mine = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine += h[e] = hist[255 - (lane * 4 + e)];
+            unsigned upto = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const unsigned v = __shfl_up(upto, o, 64);
+                if (lane >= o) upto += v;
+            }
+            unsigned before = upto - mine;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (before < (unsigned)left && before + h[e] >= (unsigned)left) {
+                    sh_prefix = prefix | (unsigned)(255 - (lane * 4 + e)) << shift;
+                    sh_want = left - (int)before;
+                }
+                before += h[e];
+            }
+        }
+        __syncthreads();
+        prefix = sh_prefix;
+        left = sh_want;
+        __syncthreads();
+    }
+    // strips above it, and the first `left` of those equal to it
+    if (tid == 0) n_strips = n_keys = 0;
+    __syncthreads();
+    int equal = 0;
+    for (int i0 = 0; i0 < strips; i0 += kTopThreads) {
+        const int i = i0 + tid;
+        const unsigned o = i < strips ? ordered(part[(long)i * sl.rows + row].x) : 0;
+        const bool is = i < strips && o == prefix;
+        const unsigned long long mask = __ballot(is);
+        if (lane == 0) wsum[wave] = __popcll(mask);
+        __syncthreads();
+        int place = equal + __popcll(mask & ((1ull << lane) - 1));
+        for (int w = 0; w < kTopThreads / 64; ++w) {
+            if (w < wave) place += wsum[w];
+            equal += wsum[w];
+        }
+        if (i < strips && (o > prefix || (is && place < left))) {
+            const int at = atomicAdd(&n_strips, 1);
+            if (at < kHeadMaxTop) list[at] = i;
+        }
+        __syncthreads();
+    }
+    // their entries
+    const int strips_here = n_strips < want ? n_strips : want;
+    const unsigned floor_ = k <= strips ? prefix : 0u;
+    for (int i = wave; i < strips_here; i += kTopThreads / 64) {
+        const int v = list[i] * kStrip + lane;
+        if (v < sl.vocab) {
+            const float a = z[sl.at(row, v)];
+            if (ordered(a) >= floor_) keys[atomicAdd(&n_keys, 1)] = entry_key(a, v);  // (at most 64 of each of k strips)
+        }
+    }
+    __syncthreads();
+    const int have = n_keys;
+    int n = 2;
+    while (n < have) n <<= 1;
+    for (int i = have + tid; i < n; i += kTopThreads) keys[i] = 0;
+    sort_keys(keys, n);
+    for (int i = tid; i < k; i += kTopThreads) {
+        const bool in = i < have;
+        values[(long)row * k + i] = in ? entry_value(keys[i]) : -INFINITY;
+        ids[(long)row * k + i] = in ? (int)(0xffffffffu - (unsigned)keys[i]) : -1;
+    }
+}
+
+// ------------------------------------------------------------------ sequencing
+int rows_per_group(int rows) {      // rows of a workgroup of head_combine_kernel: 64 lanes on neighbouring rows where there are enough rows
+    int r = 1;
+    while (r < 64 && r * 2 <= rows) r <<= 1;
+    return r;
+}
+
+ms_status logits(const ms_head_config *c, const HeadPlan &p, int rows, const void *h, hipStream_t s) {
+    const int V = c->vocab, d = c->hidden;
+    const size_t es = ms_dtype_size(c->dtype);
+    const float it2 = kLog2e / c->temperature;
+    for (int i = 0; i < p.slabs; ++i) {
+        const int v0 = i * p.cols, cw = V - v0 < p.cols ? V - v0 : p.cols;
+        MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, (const char *)c->w_dev + (size_t)v0 * d * es, d, (float *)p.z + (size_t)i * p.rows * p.cols, p.cols, 1, 0,
+                         nullptr, nullptr, 0, 0, 1, s));
+    }
+    ProfScope ps(9, 4.0 * rows * V, s);
+    head_strips_kernel<<<dim3(ms_cdiv(p.strips, 4), rows < 32768 ? rows : 32768), 256, 0, s>>>(Slabs{p.rows, p.cols, V}, rows, p.strips, (const float *)p.z, it2, p.part);
+    MS_LAUNCH_CHECK();
+    return MS_OK;
+}
+
+ms_status combine(const HeadPlan &p, int rows, float unit, const float *ref, float it2, float2 *stat, float *logp, float *lse, const int *count, hipStream_t s) {
+    const int per = rows_per_group(rows);
+    ProfScope ps(9, 8.0 * rows * p.strips, s);
+    head_combine_kernel<<<ms_cdiv(rows, per), 1024, 0, s>>>(p.rows, rows, per, p.strips, p.part, unit, ref, p.token, count, p.z_sel, it2, stat, logp, lse);
+    MS_LAUNCH_CHECK();
+    return MS_OK;
+}
+
+// What the losses have in common, for the tokens t0 .. t0 + n of a call
+struct HeadCall {
+    const ms_head_config *c;
+    HeadPlan p;
+    int k;                               // selected ids of a row
+    const void *h;
+    void *d_h, *d_w;
+    hipStream_t s;
+};
+
+// Rows, their logits, sums over the vocabulary.  key / sel: per token of the block (labels, or the entries' keys and ids).  logp: labels only.
+ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int limit, const int *sel, float *logp) {
+    const ms_head_config *c = a.c;
+    const HeadPlan &p = a.p;
+    const int d = c->hidden;
+    const float it2 = kLog2e / c->temperature;
+    const char *h = (const char *)a.h + (size_t)t0 * d * ms_dtype_size(c->dtype);
+    {
+        ProfScope ps(11, 0, a.s);
+        head_rows_kernel<<<1, 1024, 0, a.s>>>(n, key, limit, p.fast, p.slot, p.token, p.count);
+    }
+    MS_LAUNCH_CHECK();
+    {
+        ProfScope ps(9, 0, a.s);
+#define GO(T, W) head_pick_kernel<T, W><<<n, 64 * W, 0, a.s>>>(d, a.k, (const T *)h, (const T *)c->w_dev, p.token, p.count, sel, it2, (T *)p.h, p.z_sel, p.ref)
+        if (c->dtype == MS_BF16) { if (a.k > 4) GO(bf16_t, 4); else GO(bf16_t, 1); }
+        else if (a.k > 4) GO(float, 4);
+        else GO(float, 1);
+#undef GO
+    }
+    MS_LAUNCH_CHECK();
+    MS_TRY(logits(c, p, n, p.h, a.s));
+    return combine(p, n, it2, nullptr, it2, p.stat, logp, nullptr, p.count, a.s);
+}
+
+// scale and rho are there: gradients of the block's hidden states and of the lm_head
+ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
+    const ms_head_config *c = a.c;
+    const HeadPlan &p = a.p;
+    const int d = c->hidden, V = c->vocab, dt = c->dtype;
+    const size_t es = ms_dtype_size(dt);
+    const float it2 = kLog2e / c->temperature;
+    for (int i = 0; i < p.slabs; ++i) {
+        const int v0 = i * p.cols, cw = V - v0 < p.cols ? V - v0 : p.cols;
+        const char *w = (const char *)c->w_dev + (size_t)v0 * d * es;
+        float *z = (float *)p.z + (size_t)i * p.rows * p.cols, *d_w = a.d_w ? (float *)a.d_w + (size_t)v0 * d : nullptr;
+        void *dz = dt == MS_F32 ? (void *)z : p.dz;
+        {
+            ProfScope ps(10, (4.0 + es) * n * cw, a.s);
+            if (dt == MS_F32) head_dz_kernel<float><<<n, 256, 0, a.s>>>(p.cols, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (float *)dz);
+            else head_dz_kernel<bf16_t><<<n, 256, 0, a.s>>>(p.cols, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (bf16_t *)dz);
+        }
+        MS_LAUNCH_CHECK();
+        if (a.d_h && a.d_w) MS_TRY(ms_k_linear_backward(dt, n, cw, d, dz, p.cols, w, p.h, p.d_h, 1, i > 0, d_w, a.s));
+        else if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, p.d_h, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
+        else MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 0, a.s));
+    }
+    if (!a.d_h) return MS_OK;
+    char *out = (char *)a.d_h + (size_t)t0 * d * es;
+    const long total = (long)n * d;
+    ProfScope ps(11, (4.0 + es) * total, a.s);
+    if (dt == MS_F32) head_d_h_kernel<float><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.slot, p.d_h, nullptr, (float *)out);
+    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.slot, p.d_h, nullptr, (bf16_t *)out);
+    MS_LAUNCH_CHECK();
+    return MS_OK;
+}
+
+ms_status total_loss(const float *terms, int n, float loss_scale, float *loss, hipStream_t s) {
+    head_loss_kernel<<<1, 1024, 0, s>>>(terms, n, loss_scale, loss);
+    MS_LAUNCH_CHECK();
+    return MS_OK;
+}
+
+bool aligned(const void *q, int by) { return ((uintptr_t)q & (by - 1)) == 0; }
+
+// Arguments that all calls have
+ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, int k, HeadUse use, int pairs, const void *h, void *d_h, void *d_w,
+                void *ws, size_t ws_bytes, void *stream) {
+    if (n && (!h || !ws)) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer", what);
+    if (!aligned(h, 16) || !aligned(c->w_dev, 16) || !aligned(d_h, 16) || !aligned(d_w, 16) || !aligned(ws, 16))
+        return ms_fail(MS_ERR_UNSUPPORTED, "%s: hidden states, lm_head, their gradients and the workspace must be 16-byte aligned", what);
+    a->c = c;
+    a->k = k ? k : 1;
+    a->h = h; a->d_h = d_h; a->d_w = d_w;
+    a->s = (hipStream_t)stream;
+    a->p = head_plan(c, n, k, use, pairs, ws);
+    if (n && ws_bytes < a->p.bytes) return ms_fail(MS_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", what, ws_bytes, a->p.bytes);
+    return MS_OK;
+}
+HeadUse use_of(const void *d_h, const void *d_w) { return d_h || d_w ? HEAD_BACKWARD : HEAD_FORWARD; }
+
+// A block whose tokens' d loss / d logp is in p.grad
+ms_status labels_backward(const HeadCall &a, int t0, int n, const int *labels, const float *logp) {
+    head_label_rows_kernel<<<ms_cdiv(n, 256), 256, 0, a.s>>>(a.p.count, a.p.token, logp, a.p.grad, 1.f / a.c->temperature, a.p.scale, a.p.rho);
+    MS_LAUNCH_CHECK();
+    return rows_backward(a, t0, n, labels);
+}
+
+}  // namespace
+
+extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const void *h, int32_t k, float *values, int32_t *ids, float *lse, void *ws,
+                                   size_t ws_bytes, void *stream) {
+    MS_TRY(validate_head(c, n, k, "top_logits"));
+    if (k < 1) return ms_fail(MS_ERR_UNSUPPORTED, "top_logits: k must be 1 .. %d and at most the vocabulary", kHeadMaxTop);
+    if (n == 0) return MS_OK;
+    if (!values || !ids || !lse) return ms_fail(MS_ERR_INVALID_ARG, "top_logits: null pointer");
+    HeadCall a;
+    MS_TRY(begin(&a, "top_logits", c, n, k, HEAD_TOP, -1, h, nullptr, nullptr, ws, ws_bytes, stream));
+    const HeadPlan &p = a.p;
+    for (int t0 = 0; t0 < n; t0 += p.rows) {
+        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        MS_TRY(logits(c, p, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
+        const float it2 = kLog2e / c->temperature;
+        MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, nullptr, lse + t0, nullptr, a.s));
+        head_top_kernel<<<nb, kTopThreads, 0, a.s>>>(Slabs{p.rows, p.cols, c->vocab}, p.strips, k, (const float *)p.z, p.part, values + (long)t0 * k, ids + (long)t0 * k);
+        MS_LAUNCH_CHECK();
+    }
+    return MS_OK;
+}
+
+extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, int32_t n, const void *h, int32_t k, const int32_t *top_ids, const float *top_logits,
+                                                      const float *lse_teacher, float *loss, float *kl_tok, void *d_h, void *d_w, void *ws, size_t ws_bytes, void *stream) {
+    MS_TRY(validate_head(c, n, k, "topk_kd"));
+    if (k < 1) return ms_fail(MS_ERR_UNSUPPORTED, "topk_kd: k must be 1 .. %d and at most the vocabulary", kHeadMaxTop);
+    if (!loss) return ms_fail(MS_ERR_INVALID_ARG, "topk_kd: loss_dev is null");
+    if (n == 0) return launch_fill_f32(loss, 1, 0.f, (hipStream_t)stream);
+    if (!top_ids || !top_logits) return ms_fail(MS_ERR_INVALID_ARG, "topk_kd: null pointer");
+    HeadCall a;
+    MS_TRY(begin(&a, "topk_kd", c, n, k, use_of(d_h, d_w), -1, h, d_h, d_w, ws, ws_bytes, stream));
+    const HeadPlan &p = a.p;
+    const bool back = d_h || d_w;
+    const float it2 = kLog2e / c->temperature, inv_t = 1.f / c->temperature;
+    float *kl = kl_tok ? kl_tok : p.per_token;
+    for (int t0 = 0; t0 < n; t0 += p.rows) {
+        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        head_entries_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, c->vocab, inv_t, top_ids + (long)t0 * k, top_logits + (long)t0 * k, lse_teacher ? lse_teacher + t0 : nullptr,
+                                                             p.ids, p.log_p, p.mass, p.key);
+        MS_LAUNCH_CHECK();
+        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr));
+        head_entry_rows_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, p.slot, p.ids, p.log_p, p.mass, p.z_sel, p.stat, nullptr, it2, c->loss_scale * inv_t, kl + t0,
+                                                                back ? p.scale : nullptr, back ? p.rho : nullptr);
+        MS_LAUNCH_CHECK();
+        if (back) MS_TRY(rows_backward(a, t0, nb, p.ids));
+    }
+    return total_loss(kl, n, c->loss_scale, loss, a.s);
+}
+
+static ms_status token_logprobs(const char *what, const ms_head_config *c, int n, const void *h, const int32_t *labels, const float *d_logp, float *logp, void *d_h, void *d_w,
+                                void *ws, size_t ws_bytes, void *stream) {
+    MS_TRY(validate_head(c, n, 0, what));
+    if (n == 0) return MS_OK;
+    const bool back = d_logp != nullptr;
+    if (!labels) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer", what);
+    HeadCall a;
+    MS_TRY(begin(&a, what, c, n, 0, back ? HEAD_BACKWARD : HEAD_FORWARD, -1, h, d_h, d_w, ws, ws_bytes, stream));
+    const HeadPlan &p = a.p;
+    for (int t0 = 0; t0 < n; t0 += p.rows) {
+        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        float *lp = logp ? logp + t0 : p.logp;
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp));
+        head_given_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, p.slot, back ? d_logp + t0 : nullptr, lp, back ? p.grad : nullptr);
+        MS_LAUNCH_CHECK();
+        if (back) MS_TRY(labels_backward(a, t0, nb, labels + t0, lp));
+    }
+    return MS_OK;
+}
+extern "C" ms_status ms_token_logprobs(const ms_head_config *c, int32_t n, const void *h, const int32_t *labels, float *logp, void *ws, size_t ws_bytes, void *stream) {
+    if (n > 0 && !logp) return ms_fail(MS_ERR_INVALID_ARG, "token_logprobs: null pointer");
+    return token_logprobs("token_logprobs", c, n, h, labels, nullptr, logp, nullptr, nullptr, ws, ws_bytes, stream);
+}
+extern "C" ms_status ms_token_logprobs_backward(const ms_head_config *c, int32_t n, const void *h, const int32_t *labels, const float *d_logp, float *logp, void *d_h, void *d_w,
+                                                void *ws, size_t ws_bytes, void *stream) {
+    if (n > 0 && (!d_logp || (!d_h && !d_w))) return ms_fail(MS_ERR_INVALID_ARG, "token_logprobs_backward: null pointer");
+    return token_logprobs("token_logprobs_backward", c, n, h, labels, d_logp, logp, d_h, d_w, ws, ws_bytes, stream);
+}
+
+extern "C" ms_status ms_policy_loss_forward_backward(const ms_head_config *c, const ms_policy_config *pc, int32_t n, const void *h, const int32_t *labels, const float *old_logp,
+                                                     const float *ref_logp, const float *advantages, const float *weights, float *loss, float *loss_tok, float *logp, void *d_h,
+                                                     void *d_w, void *ws, size_t ws_bytes, void *stream) {
+    MS_TRY(validate_head(c, n, 0, "policy_loss"));
+    if (!pc || !loss) return ms_fail(MS_ERR_INVALID_ARG, "policy_loss: null config or loss_dev");
+    if (!(pc->clip_low >= 0.f && pc->clip_low <= 1.f) || !(pc->clip_high >= 0.f && pc->clip_high < INFINITY) || !(pc->kl_coef >= 0.f && pc->kl_coef < INFINITY))
+        return ms_fail(MS_ERR_INVALID_ARG, "policy_loss: clip_low must be in [0, 1], clip_high and kl_coef not negative");
+    if (pc->kl_coef > 0.f && n > 0 && !ref_logp) return ms_fail(MS_ERR_INVALID_ARG, "policy_loss: kl_coef without ref_logp");
+    if (n == 0) return launch_fill_f32(loss, 1, 0.f, (hipStream_t)stream);
+    if (!labels || !old_logp || !advantages) return ms_fail(MS_ERR_INVALID_ARG, "policy_loss: null pointer");
+    HeadCall a;
+    MS_TRY(begin(&a, "policy_loss", c, n, 0, use_of(d_h, d_w), -1, h, d_h, d_w, ws, ws_bytes, stream));
+    const HeadPlan &p = a.p;
+    float *terms = loss_tok ? loss_tok : p.per_token;
+    for (int t0 = 0; t0 < n; t0 += p.rows) {
+        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        float *lp = logp ? logp + t0 : p.logp;
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp));
+        const PolicyArgs pa = {old_logp + t0, pc->kl_coef > 0.f ? ref_logp + t0 : nullptr, advantages + t0, weights ? weights + t0 : nullptr, pc->clip_low, pc->clip_high, pc->kl_coef,
+                               c->loss_scale};
+        head_policy_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, p.slot, pa, lp, p.grad ? p.grad : p.z_sel, terms + t0);
+        MS_LAUNCH_CHECK();
+        if (d_h || d_w) MS_TRY(labels_backward(a, t0, nb, labels + t0, lp));
+    }
+    return total_loss(terms, n, c->loss_scale, loss, a.s);
+}
+
+extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c, const ms_preference_config *pc, const ms_batch *batch, const void *h, const int32_t *labels,
+                                                         const float *ref_logp, float *loss, float *margin, float *logp, void *d_h, void *d_w, void *ws, size_t ws_bytes,
+                                                         void *stream) {
+    if (!batch) return ms_fail(MS_ERR_INVALID_ARG, "preference_loss: null batch");
+    const int n = batch->n_tokens, pairs = batch->n_seqs / 2;
+    MS_TRY(validate_head(c, n, 0, "preference_loss"));
+    if (!pc || !loss) return ms_fail(MS_ERR_INVALID_ARG, "preference_loss: null config or loss_dev");
+    if (!(pc->beta > 0.f && pc->beta < INFINITY) || !(pc->label_smoothing >= 0.f && pc->label_smoothing < 1.f))
+        return ms_fail(MS_ERR_INVALID_ARG, "preference_loss: beta must be positive and label_smoothing in [0, 1)");
+    const int32_t *cu = batch->cu_seqlens_host;
+    if (batch->n_seqs < 0 || batch->n_seqs % 2) return ms_fail(MS_ERR_SHAPE, "preference_loss: %d sequences are no pairs", batch->n_seqs);
+    if (!cu || !batch->cu_seqlens_dev) return ms_fail(MS_ERR_INVALID_ARG, "preference_loss: null cu_seqlens");
+    if (cu[0] != 0 || cu[batch->n_seqs] != n) return ms_fail(MS_ERR_SHAPE, "preference_loss: cu_seqlens must go from 0 to n_tokens");
+    for (int i = 0; i < batch->n_seqs; ++i)
+        if (cu[i + 1] < cu[i]) return ms_fail(MS_ERR_SHAPE, "preference_loss: cu_seqlens must not decrease");
+    if (n == 0) {
+        MS_TRY(launch_fill_f32(loss, 1, 0.f, (hipStream_t)stream));
+        return margin && pairs ? launch_fill_f32(margin, pairs, 0.f, (hipStream_t)stream) : MS_OK;
+    }
+    if (!labels) return ms_fail(MS_ERR_INVALID_ARG, "preference_loss: null pointer");
+    HeadCall a;
+    if (n > head_most_rows(c)) return ms_fail(MS_ERR_UNSUPPORTED, "preference_loss: %d tokens in one block, at most %ld", n, head_most_rows(c));
+    MS_TRY(begin(&a, "preference_loss", c, n, 0, use_of(d_h, d_w), pairs, h, d_h, d_w, ws, ws_bytes, stream));
+    const HeadPlan &p = a.p;
+    float *lp = logp ? logp : p.logp;
+    MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp));
+    head_pairs_kernel<<<pairs, 256, 0, a.s>>>(batch->cu_seqlens_dev, p.slot, ref_logp, pc->beta, pc->label_smoothing, c->loss_scale, lp, margin ? margin : p.margin, p.per_token,
+                                              p.grad);
+    MS_LAUNCH_CHECK();
+    if (d_h || d_w) MS_TRY(labels_backward(a, 0, n, labels, lp));
+    return total_loss(p.per_token, pairs, c->loss_scale, loss, a.s);
+}

@@ -1,0 +1,96 @@
+// Host-side plan and validation of the losses at the end of a section (see head.h); kernels and their sequencing are in head.hip.
+#include "head.h"
+#include <math.h>
+
+namespace {
+constexpr long kReach = (1L << 32) - (1L << 20);        // bytes that a buffer descriptor reaches, with room for a tile past the end
+constexpr long kBlockBytes = 16L << 30;                 // a block's exponentials or logits, if the caller does not say (288 GB per GPU)
+constexpr long kTopBlockBytes = 4L << 30;               // the same for logits that are only looked through
+long least(long a, long b) { return a < b ? a : b; }
+long round_up(long x, long a) { return (x + a - 1) / a * a; }
+}  // namespace
+
+long head_most_rows(const ms_head_config *c) { return least(kReach / (2L * c->hidden) - 512, kReach / (4 * 256) - 512); }
+
+HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws) {
+    HeadPlan p = {};
+    const bool whole = pairs >= 0;
+    const long V = c->vocab, d = c->hidden;
+    const size_t es = ms_dtype_size(c->dtype);
+    p.fast = false;
+    const bool keeps = use != HEAD_FORWARD || !p.fast;                       // something of every (row, vocabulary entry)
+    const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
+    // tokens of a block: the caller's choice, or what the memory above holds, in blocks of about equal size
+    long most = head_most_rows(c);
+    if (!whole) {
+        if (c->token_block > 0) most = least(most, c->token_block);
+        else if (keeps) most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
+    }
+    const long blocks = whole || n <= most ? 1 : (n + most - 1) / most;
+    p.rows = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
+    const long widest = least(kReach / (4 * (p.rows + 256L)), kReach / (2 * d) - 512);
+    p.slabs = (int)((V + widest - 1) / widest);
+    p.cols = p.slabs == 1 ? (int)V : (int)round_up((V + p.slabs - 1) / p.slabs, 256);
+    if (p.slabs > 1 && p.cols > widest) p.cols -= 256, p.slabs = (int)((V + p.cols - 1) / p.cols);
+    p.strips = (int)((V + kStrip - 1) / kStrip);
+    const size_t r = (size_t)p.rows;
+    Arena a(ws);
+    p.slot = a.take<int>(r * 4);
+    p.token = a.take<int>(r * 4);
+    p.count = a.take<int>(4);
+    p.h = a.take<void>(r * d * es);
+    p.ref = a.take<float>(r * 4);
+    p.stat = a.take<float2>(r * 8);
+    p.part = a.take<float2>(r * p.strips * 8);
+    if (use != HEAD_TOP) {
+        p.z_sel = a.take<float>(r * (k ? k : 1) * 4);
+        p.logp = a.take<float>(r * 4);
+        if (k) {
+            p.log_p = a.take<float>(r * k * 4);
+            p.mass = a.take<float>(r * 4);
+            p.ids = a.take<int>(r * k * 4);
+            p.key = a.take<int>(r * 4);
+        }
+        p.per_token = a.take<float>((size_t)(whole ? pairs : n) * 4);
+        if (whole) p.margin = a.take<float>((size_t)pairs * 4);
+    }
+    if (use == HEAD_BACKWARD) {
+        p.rho = a.take<float>(r * (k ? k : 1) * 4);
+        p.grad = a.take<float>(r * 4);
+        p.scale = a.take<float>(r * 4);
+        p.d_h = a.take<float>(r * d * 4);
+        if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(r * p.cols * 2);
+    }
+    if (keeps) p.z = a.take<void>((size_t)p.slabs * r * p.cols * ez);
+    p.bytes = a.off;
+    return p;
+}
+
+ms_status validate_head(const ms_head_config *c, int n, int k, const char *what) {
+    if (!c) return ms_fail(MS_ERR_INVALID_ARG, "%s: null config", what);
+    if (n < 0) return ms_fail(MS_ERR_INVALID_ARG, "%s: negative token count", what);
+    if (c->dtype != MS_BF16 && c->dtype != MS_F32) return ms_fail(MS_ERR_INVALID_ARG, "%s: bad dtype", what);
+    if (c->vocab <= 0 || c->hidden <= 0) return ms_fail(MS_ERR_SHAPE, "%s: vocab and hidden size must be positive", what);
+    if (c->vocab % 8 || c->hidden % 8) return ms_fail(MS_ERR_UNSUPPORTED, "%s: vocab and hidden size must be multiples of 8", what);
+    if ((long)c->hidden > 65536 || c->vocab > (1 << 24)) return ms_fail(MS_ERR_UNSUPPORTED, "%s: hidden size over 65536 or vocab over 2^24", what);
+    if (!(c->temperature > 0.f) || !isfinite(c->temperature) || !isfinite(1.f / c->temperature))
+        return ms_fail(MS_ERR_INVALID_ARG, "%s: temperature must be positive", what);
+    if (!isfinite(c->loss_scale)) return ms_fail(MS_ERR_INVALID_ARG, "%s: loss_scale must be finite", what);
+    if (c->token_block < 0 || c->token_block % 8) return ms_fail(MS_ERR_INVALID_ARG, "%s: token_block must be 0 or a positive multiple of 8", what);
+    if (k < 0 || k > kHeadMaxTop || k > c->vocab) return ms_fail(MS_ERR_UNSUPPORTED, "%s: k must be 1 .. %d and at most the vocabulary", what, kHeadMaxTop);
+    if (!c->w_dev) return ms_fail(MS_ERR_INVALID_ARG, "%s: null lm_head pointer", what);
+    return MS_OK;
+}
+
+static size_t bytes_of(const ms_head_config *c, int n, int k, HeadUse use, int pairs) {
+    if (!c || n < 0 || c->vocab <= 0 || c->hidden <= 0 || c->hidden > 65536 || c->vocab > (1 << 24) || c->token_block < 0 || k < 0 || k > kHeadMaxTop) return 0;
+    if (pairs >= 0 && n > head_most_rows(c)) return 0;
+    return head_plan(c, n, k, use, pairs, nullptr).bytes;
+}
+extern "C" size_t ms_top_logits_workspace_bytes(const ms_head_config *c, int32_t max_tokens, int32_t k) { return k < 1 ? 0 : bytes_of(c, max_tokens, k, HEAD_TOP, -1); }
+extern "C" size_t ms_head_workspace_bytes(const ms_head_config *c, int32_t max_tokens, int32_t k, int32_t need_backward) {
+    return bytes_of(c, max_tokens, k, need_backward ? HEAD_BACKWARD : HEAD_FORWARD, -1);
+}
+extern "C" size_t ms_preference_workspace_bytes(const ms_head_config *c, int32_t max_tokens, int32_t max_pairs, int32_t need_backward) {
+    return max_pairs < 0 ? 0 : bytes_of(c, max_tokens, 0, need_backward ? HEAD_BACKWARD : HEAD_FORWARD, max_pairs);
+}
