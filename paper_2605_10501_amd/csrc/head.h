@@ -2,6 +2,7 @@
 // accepted.  No device code: this part also builds for the host alone.
 #pragma once
 #include "common.h"
+#include "head_choice.h"
 
 constexpr int kHeadMaxTop = 128;             // entries of a token that the kernels hold
 constexpr int kStrip = 64;                   // columns that share one partial sum
@@ -21,7 +22,9 @@ struct HeadPlan {
     int *key;                                // [rows] < 0: the token is left out
     float *logp, *grad;                      // [rows] by token of the block
     float2 *part;                            // [strips, rows]
-    float *d_h;                              // [rows, hidden]
+    HeadChoice choice;                       // of the gradients' products (fast)
+    int parts;                               // of d_h
+    float *d_h;                              // [parts, rows, hidden]
     void *z;                                 // slabs: logits (fp32), or their exponentials (bf16)
     void *dz;                                // [rows, cols] gradient of a slab's logits where it does not take the logits' place
     float *per_token, *margin;               // [n] terms of the loss, or [pairs] both

@@ -5,6 +5,7 @@
 // (its label, or the teacher's entries), where rho = dz / scale_row is q - 1 or q - p / sum p.  The logits there are dot products of their own.
 #include "common.h"
 #include "head.h"
+#include "head_gemm.h"
 #include "launch.h"
 
 namespace {
@@ -196,14 +197,14 @@ __global__ __launch_bounds__(256) void head_strips_kernel(Slabs sl, int rows, in
 }
 
 // Behind the vocabulary: sum of the strips' sums at a common reference.  part holds (offset, sum) of each strip [strips][ld]: stored logits' offsets are logits
-// (`unit` of x each), those of exponentials (`ref` given) count in x on top of the row's reference.
-// A workgroup takes `rows_per` rows (a power of two) and 1024 / rows_per shares of the strips.
-// stat[row] = (sum, offset); logp, lse: by token, where asked for.
+// (`unit` of x each), those of exponentials (`ref` given) count in x on top of the row's reference.  A row's strips are shared by 64 threads whatever the number
+// of rows, so that a token's sum does not depend on its batch; a workgroup takes `rows_per` rows, up to 16 (128 bytes of neighbouring rows per strip).
+// stat[row] = (sum, offset); logp: by token, lse: by row, where asked for.
 __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, int rows_per, int strips, const float2 *__restrict__ part, float unit, const float *__restrict__ ref,
                                                             const int *__restrict__ token, const int *__restrict__ count, const float *__restrict__ z_sel, float it2,
                                                             float2 *__restrict__ stat, float *__restrict__ logp, float *__restrict__ lse) {
     __shared__ float2 sm[1024];
-    const int r = threadIdx.x & (rows_per - 1), g = threadIdx.x / rows_per, groups = 1024 / rows_per;
+    const int r = threadIdx.x & (rows_per - 1), g = threadIdx.x / rows_per;
     const int row = blockIdx.x * rows_per + r, n = count ? *count : rows;
     float m = -INFINITY, s = 0.f;
     auto merge = [&](float mi, float si) {
@@ -211,13 +212,18 @@ __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, in
         s = s * __builtin_amdgcn_exp2f((m - u) * unit) + si * __builtin_amdgcn_exp2f((mi - u) * unit);
         m = to;
     };
-    if (row < n)
-        for (int i = g; i < strips; i += groups) {
-            const float2 q = part[(long)i * ld + row];
-            merge(q.x, q.y);
+    if (row < n) {
+        const float2 *p = part + row;
+        for (int i = g; i < strips; i += 64 * 8) {
+            float2 q[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[e] = i + 64 * e < strips ? p[(long)(i + 64 * e) * ld] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) merge(q[e].x, q[e].y);
         }
+    }
     sm[threadIdx.x] = make_float2(m, s);
-    for (int half = groups >> 1; half > 0; half >>= 1) {
+    for (int half = 32; half > 0; half >>= 1) {
         __syncthreads();
         if (g < half) {
             const float2 q = sm[threadIdx.x + half * rows_per];
@@ -386,16 +392,58 @@ __global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int v0
     }
 }
 
-// d_h of the block's tokens: a row's sums times its factor; zeros for tokens that were left out
+// Exponentials of rows with a strip that is far above the row's reference (its label is 2^64 times less likely than another id): the strips' offsets are evened out.
+// One workgroup per row; hardly ever is there anything to do.
+__global__ __launch_bounds__(256) void head_even_kernel(Slabs sl, int strips, const int *__restrict__ count, const float2 *__restrict__ part, const float2 *__restrict__ stat, bf16_t *__restrict__ e) {
+    const int row = blockIdx.x, lane = threadIdx.x & 63;
+    if (row >= *count) return;
+    const float to = stat[row].y;
+    if (to == 0.f) return;
+    for (int i = threadIdx.x >> 6; i < strips; i += 4) {
+        const float off = part[(long)i * sl.rows + row].x;
+        const int v = i * kStrip + lane;
+        if (off == to || v >= sl.vocab) continue;
+        bf16_t *at = e + sl.at(row, v);
+        *at = (bf16_t)((float)*at * __builtin_amdgcn_exp2f(off - to));
+    }
+}
+
+// Exponentials -> gradient of the logits over the row's factor c = scale / sum: the selected ids get theirs, c goes onto the hidden states (for d_w) and is kept (for d_h).
+// One workgroup per row.  h, in the storage type, is rounded once more here.
+__global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k, const int *__restrict__ token, const int *__restrict__ count, const int *__restrict__ sel,
+                                                         const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho, bf16_t *__restrict__ e,
+                                                         bf16_t *__restrict__ h, float *__restrict__ factor) {
+    const int row = blockIdx.x;
+    if (row >= *count) return;
+    const int t = token[row];
+    const float sum = stat[row].x, sc = scale[row], c = sc == 0.f ? 0.f : sc / sum;
+    if (threadIdx.x == 0) factor[row] = c;
+    for (int j = threadIdx.x; j < k; j += 256) {
+        const int v = sel[(long)t * k + j];
+        if (v >= 0) e[sl.at(row, v)] = (bf16_t)(rho[(long)row * k + j] * sum);
+    }
+    for (int i = threadIdx.x * 8; i < d; i += 256 * 8) {
+        Vec16<bf16_t> a = ldv(h + (long)row * d + i);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) a.v[x] = (bf16_t)(c == 0.f ? 0.f : c * (float)a.v[x]);
+        stv(h + (long)row * d + i, a);
+    }
+}
+
+// d_h of the block's tokens: a row's sums (in `parts` parts) times its factor; zeros for tokens that were left out
 template <class T>
-__global__ __launch_bounds__(256) void head_d_h_kernel(long total, int d, const int *__restrict__ slot, const float *__restrict__ sums, const float *__restrict__ factor, T *__restrict__ d_h) {
+__global__ __launch_bounds__(256) void head_d_h_kernel(long total, int d, int parts, long part_ld, const int *__restrict__ slot, const float *__restrict__ sums, const float *__restrict__ factor,
+                                                       T *__restrict__ d_h) {
     const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= total) return;
     const int t = (int)(i / d), c = (int)(i - (long)t * d), row = slot[t];
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     const float f = row < 0 ? 0.f : factor ? factor[row] : 1.f;
     if (row >= 0 && f != 0.f) {
-        v = *(const float4 *)(sums + (long)row * d + c);
+        for (int q = 0; q < parts; ++q) {
+            const float4 a = *(const float4 *)(sums + q * part_ld + (long)row * d + c);
+            v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+        }
         v.x *= f; v.y *= f; v.z *= f; v.w *= f;
     }
     T *o = d_h + i;
@@ -525,21 +573,21 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int str
 }
 
 // ------------------------------------------------------------------ sequencing
-int rows_per_group(int rows) {      // rows of a workgroup of head_combine_kernel: 64 lanes on neighbouring rows where there are enough rows
-    int r = 1;
-    while (r < 64 && r * 2 <= rows) r <<= 1;
-    return r;
-}
-
-ms_status logits(const ms_head_config *c, const HeadPlan &p, int rows, const void *h, hipStream_t s) {
+// Logits of `rows` rows h and the sums of their strips: stored (fp32), or their exponentials at p.ref (fast losses; not stored in a forward pass)
+ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int rows, const void *h, hipStream_t s) {
     const int V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(c->dtype);
     const float it2 = kLog2e / c->temperature;
     for (int i = 0; i < p.slabs; ++i) {
         const int v0 = i * p.cols, cw = V - v0 < p.cols ? V - v0 : p.cols;
-        MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, (const char *)c->w_dev + (size_t)v0 * d * es, d, (float *)p.z + (size_t)i * p.rows * p.cols, p.cols, 1, 0,
-                         nullptr, nullptr, 0, 0, 1, s));
+        const char *w = (const char *)c->w_dev + (size_t)v0 * d * es;
+        const size_t slab = (size_t)i * p.rows * p.cols;
+        float2 *part = p.part + (size_t)(v0 / kStrip) * p.rows;
+        if (!p.fast) MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, w, d, (float *)p.z + slab, p.cols, 1, 0, nullptr, nullptr, 0, 0, 1, s));
+        else if (use == HEAD_TOP) MS_TRY(head_gemm_logits(rows, cw, d, h, w, it2, (float *)p.z + slab, p.cols, part, p.rows, s));
+        else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
     }
+    if (p.fast) return MS_OK;
     ProfScope ps(9, 4.0 * rows * V, s);
     head_strips_kernel<<<dim3(ms_cdiv(p.strips, 4), rows < 32768 ? rows : 32768), 256, 0, s>>>(Slabs{p.rows, p.cols, V}, rows, p.strips, (const float *)p.z, it2, p.part);
     MS_LAUNCH_CHECK();
@@ -547,9 +595,10 @@ ms_status logits(const ms_head_config *c, const HeadPlan &p, int rows, const voi
 }
 
 ms_status combine(const HeadPlan &p, int rows, float unit, const float *ref, float it2, float2 *stat, float *logp, float *lse, const int *count, hipStream_t s) {
-    const int per = rows_per_group(rows);
+    int per = 1;
+    while (per < 16 && per < rows) per <<= 1;
     ProfScope ps(9, 8.0 * rows * p.strips, s);
-    head_combine_kernel<<<ms_cdiv(rows, per), 1024, 0, s>>>(p.rows, rows, per, p.strips, p.part, unit, ref, p.token, count, p.z_sel, it2, stat, logp, lse);
+    head_combine_kernel<<<ms_cdiv(rows, per), per * 64, 0, s>>>(p.rows, rows, per, p.strips, p.part, unit, ref, p.token, count, p.z_sel, it2, stat, logp, lse);
     MS_LAUNCH_CHECK();
     return MS_OK;
 }
@@ -558,6 +607,7 @@ ms_status combine(const HeadPlan &p, int rows, float unit, const float *ref, flo
 struct HeadCall {
     const ms_head_config *c;
     HeadPlan p;
+    HeadUse use;
     int k;                               // selected ids of a row
     const void *h;
     void *d_h, *d_w;
@@ -585,8 +635,8 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
 #undef GO
     }
     MS_LAUNCH_CHECK();
-    MS_TRY(logits(c, p, n, p.h, a.s));
-    return combine(p, n, it2, nullptr, it2, p.stat, logp, nullptr, p.count, a.s);
+    MS_TRY(logits(c, p, a.use, n, p.h, a.s));
+    return combine(p, n, p.fast ? 1.f : it2, p.fast ? p.ref : nullptr, it2, p.stat, logp, nullptr, p.count, a.s);
 }
 
 // scale and rho are there: gradients of the block's hidden states and of the lm_head
@@ -596,9 +646,21 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
     const int d = c->hidden, V = c->vocab, dt = c->dtype;
     const size_t es = ms_dtype_size(dt);
     const float it2 = kLog2e / c->temperature;
+    if (p.fast) {
+        const Slabs sl = {p.rows, p.cols, V};
+        ProfScope ps(10, 4.0 * n * d, a.s);
+        head_even_kernel<<<n, 256, 0, a.s>>>(sl, p.strips, p.count, p.part, p.stat, (bf16_t *)p.z);
+        head_apply_kernel<<<n, 256, 0, a.s>>>(sl, d, a.k, p.token, p.count, sel, p.stat, p.scale, p.rho, (bf16_t *)p.z, (bf16_t *)p.h, p.ref);
+    }
+    MS_LAUNCH_CHECK();
     for (int i = 0; i < p.slabs; ++i) {
         const int v0 = i * p.cols, cw = V - v0 < p.cols ? V - v0 : p.cols;
         const char *w = (const char *)c->w_dev + (size_t)v0 * d * es;
+        if (p.fast) {
+            MS_TRY(head_gemm_backward(p.choice, n, cw, d, (const bf16_t *)p.z + (size_t)i * p.rows * p.cols, p.cols, w, p.h, a.d_h ? p.d_h : nullptr, i > 0,
+                                      a.d_w ? (float *)a.d_w + (size_t)v0 * d : nullptr, p.count, a.s));
+            continue;
+        }
         float *z = (float *)p.z + (size_t)i * p.rows * p.cols, *d_w = a.d_w ? (float *)a.d_w + (size_t)v0 * d : nullptr;
         void *dz = dt == MS_F32 ? (void *)z : p.dz;
         {
@@ -615,8 +677,9 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
     char *out = (char *)a.d_h + (size_t)t0 * d * es;
     const long total = (long)n * d;
     ProfScope ps(11, (4.0 + es) * total, a.s);
-    if (dt == MS_F32) head_d_h_kernel<float><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.slot, p.d_h, nullptr, (float *)out);
-    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.slot, p.d_h, nullptr, (bf16_t *)out);
+    const long part_ld = (long)n * d;
+    if (dt == MS_F32) head_d_h_kernel<float><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, 1, part_ld, p.slot, p.d_h, nullptr, (float *)out);
+    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.parts, part_ld, p.slot, p.d_h, p.fast ? p.ref : nullptr, (bf16_t *)out);
     MS_LAUNCH_CHECK();
     return MS_OK;
 }
@@ -636,6 +699,7 @@ ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, i
     if (!aligned(h, 16) || !aligned(c->w_dev, 16) || !aligned(d_h, 16) || !aligned(d_w, 16) || !aligned(ws, 16))
         return ms_fail(MS_ERR_UNSUPPORTED, "%s: hidden states, lm_head, their gradients and the workspace must be 16-byte aligned", what);
     a->c = c;
+    a->use = use;
     a->k = k ? k : 1;
     a->h = h; a->d_h = d_h; a->d_w = d_w;
     a->s = (hipStream_t)stream;
@@ -665,7 +729,7 @@ extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const voi
     const HeadPlan &p = a.p;
     for (int t0 = 0; t0 < n; t0 += p.rows) {
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
-        MS_TRY(logits(c, p, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
+        MS_TRY(logits(c, p, HEAD_TOP, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
         const float it2 = kLog2e / c->temperature;
         MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, nullptr, lse + t0, nullptr, a.s));
         head_top_kernel<<<nb, kTopThreads, 0, a.s>>>(Slabs{p.rows, p.cols, c->vocab}, p.strips, k, (const float *)p.z, p.part, values + (long)t0 * k, ids + (long)t0 * k);
@@ -693,7 +757,7 @@ extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, i
                                                              p.ids, p.log_p, p.mass, p.key);
         MS_LAUNCH_CHECK();
         MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr));
-        head_entry_rows_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, p.slot, p.ids, p.log_p, p.mass, p.z_sel, p.stat, nullptr, it2, c->loss_scale * inv_t, kl + t0,
+        head_entry_rows_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, p.slot, p.ids, p.log_p, p.mass, p.z_sel, p.stat, p.fast ? p.ref : nullptr, it2, c->loss_scale * inv_t, kl + t0,
                                                                 back ? p.scale : nullptr, back ? p.rho : nullptr);
         MS_LAUNCH_CHECK();
         if (back) MS_TRY(rows_backward(a, t0, nb, p.ids));

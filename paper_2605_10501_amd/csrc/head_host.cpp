@@ -6,6 +6,7 @@ namespace {
 constexpr long kReach = (1L << 32) - (1L << 20);        // bytes that a buffer descriptor reaches, with room for a tile past the end
 constexpr long kBlockBytes = 16L << 30;                 // a block's exponentials or logits, if the caller does not say (288 GB per GPU)
 constexpr long kTopBlockBytes = 4L << 30;               // the same for logits that are only looked through
+constexpr long kForwardRows = 65536;                    // tokens of a block that keeps only its strips' sums
 long least(long a, long b) { return a < b ? a : b; }
 long round_up(long x, long a) { return (x + a - 1) / a * a; }
 }  // namespace
@@ -17,21 +18,24 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     const bool whole = pairs >= 0;
     const long V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(c->dtype);
-    p.fast = false;
+    p.fast = c->dtype == MS_BF16 && d % 64 == 0;
     const bool keeps = use != HEAD_FORWARD || !p.fast;                       // something of every (row, vocabulary entry)
     const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
     // tokens of a block: the caller's choice, or what the memory above holds, in blocks of about equal size
     long most = head_most_rows(c);
     if (!whole) {
         if (c->token_block > 0) most = least(most, c->token_block);
-        else if (keeps) most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
+        else if (!keeps) most = least(most, kForwardRows);
+        else most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
     }
     const long blocks = whole || n <= most ? 1 : (n + most - 1) / most;
     p.rows = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
-    const long widest = least(kReach / (4 * (p.rows + 256L)), kReach / (2 * d) - 512);
+    long widest = kReach / (2 * d) - 512;
+    if (keeps) widest = least(widest, kReach / (long)(ez * (p.rows + 256L)));
     p.slabs = (int)((V + widest - 1) / widest);
     p.cols = p.slabs == 1 ? (int)V : (int)round_up((V + p.slabs - 1) / p.slabs, 256);
     if (p.slabs > 1 && p.cols > widest) p.cols -= 256, p.slabs = (int)((V + p.cols - 1) / p.cols);
+    if (p.fast) p.cols = (int)round_up(p.cols, 64);                          // (d_h's product reads whole K tiles)
     p.strips = (int)((V + kStrip - 1) / kStrip);
     const size_t r = (size_t)p.rows;
     Arena a(ws);
@@ -58,7 +62,12 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
         p.rho = a.take<float>(r * (k ? k : 1) * 4);
         p.grad = a.take<float>(r * 4);
         p.scale = a.take<float>(r * 4);
-        p.d_h = a.take<float>(r * d * 4);
+        p.parts = 1;
+        if (p.fast) {
+            p.choice = head_choose(p.rows, V < p.cols ? V : p.cols, d, true, true);
+            p.parts = p.choice.parts;
+        }
+        p.d_h = a.take<float>(r * p.parts * d * 4);
         if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(r * p.cols * 2);
     }
     if (keeps) p.z = a.take<void>((size_t)p.slabs * r * p.cols * ez);
