@@ -5,6 +5,8 @@
 #include "head_choice.h"
 
 constexpr int kHeadMaxTop = 128;             // entries of a token that the kernels hold
+constexpr int kHeadFixes = 4;                // of a token's entries whose gradients are completed in fp32
+constexpr int kHeadScan = 4096;              // rows of such, up to which each looks for the others of its id by itself
 constexpr int kStrip = 64;                   // columns that share one partial sum
 
 // Rows of hidden states meet the vocabulary a block of tokens at a time.  What a block keeps of every (row, vocabulary entry) lies in
@@ -20,8 +22,13 @@ struct HeadPlan {
     float *log_p, *mass;                     // [rows, k], [rows] of the teacher's entries
     int *ids;                                // [rows, k] the entries that count (-1: ignored)
     int *key;                                // [rows] < 0: the token is left out
-    float *logp, *grad;                      // [rows] by token of the block
+    float *logp;                             // [rows] by token of the block
     float2 *part;                            // [strips, rows]
+    int fixes;                               // selected ids of a row whose part of the gradients is completed in fp32 (fast)
+    int *fix_id;                             // [rows, fixes], -1: none
+    float *fix_rest;                         // [rows, fixes] what the stored gradient of the logit lacks
+    void *fix, *fix_scratch;                 // [rows fixes, hidden] what d_w's row lacks; for the sum over the rows of an id
+    size_t fix_scratch_bytes;
     HeadChoice choice;                       // of the gradients' products (fast)
     int parts;                               // of d_h
     float *d_h;                              // [parts, rows, hidden]

@@ -243,26 +243,27 @@ __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, in
 }
 
 // ------------------------------------------------------------------ what a token's gradient is
-// Labels: dz = g / T (1_label - q), so scale = -g / T and rho = q - 1.
-__global__ __launch_bounds__(256) void head_label_rows_kernel(const int *__restrict__ count, const int *__restrict__ token, const float *__restrict__ logp,
-                                                              const float *__restrict__ grad, float inv_t, float *__restrict__ scale, float *__restrict__ rho) {
-    const int row = blockIdx.x * 256 + threadIdx.x;
-    if (row >= *count) return;
-    const int t = token[row];
-    scale[row] = t < 0 ? 0.f : -inv_t * grad[t];
-    rho[row] = t < 0 ? 0.f : expm1f(logp[t]);
-}
+// Labels: dz = g / T (1_label - q), g = d loss / d logp, so scale = -g / T and rho = q - 1.
+struct LabelRows {
+    const int *slot;
+    float *scale, *rho, minus_inv_t;                                            // scale null: forward only
+    __device__ __forceinline__ void set(int row, float g, float logp) const {
+        if (!scale) return;
+        scale[row] = minus_inv_t * g;
+        rho[row] = expm1f(logp);
+    }
+};
 
 struct PolicyArgs {
     const float *old_logp, *ref_logp, *adv, *weights;
     float low, high, kl, loss_scale;
 };
-__global__ __launch_bounds__(256) void head_policy_kernel(int n, const int *__restrict__ slot, PolicyArgs a, float *__restrict__ logp, float *__restrict__ grad,
-                                                          float *__restrict__ loss_tok) {
+__global__ __launch_bounds__(256) void head_policy_kernel(int n, LabelRows rows, PolicyArgs a, float *__restrict__ logp, float *__restrict__ loss_tok) {
     const int t = blockIdx.x * 256 + threadIdx.x;
     if (t >= n) return;
-    if (slot[t] < 0) {
-        logp[t] = grad[t] = loss_tok[t] = 0.f;
+    const int row = rows.slot[t];
+    if (row < 0) {
+        logp[t] = loss_tok[t] = 0.f;
         return;
     }
     const float l = logp[t], adv = a.adv[t], wt = a.weights ? a.weights[t] : 1.f;
@@ -276,21 +277,22 @@ __global__ __launch_bounds__(256) void head_policy_kernel(int n, const int *__re
         g -= a.kl * away;
     }
     loss_tok[t] = wt * loss;
-    grad[t] = a.loss_scale * wt * g;
+    rows.set(row, a.loss_scale * wt * g, l);
 }
 
-// logp of the tokens that were left out (labels); the gradient that the caller gives
-__global__ __launch_bounds__(256) void head_given_kernel(int n, const int *__restrict__ slot, const float *__restrict__ d_logp, float *__restrict__ logp, float *__restrict__ grad) {
+// logp of the tokens that were left out; the gradient that the caller gives
+__global__ __launch_bounds__(256) void head_given_kernel(int n, LabelRows rows, const float *__restrict__ d_logp, float *__restrict__ logp) {
     const int t = blockIdx.x * 256 + threadIdx.x;
     if (t >= n) return;
-    if (slot[t] < 0) logp[t] = 0.f;
-    if (grad) grad[t] = slot[t] < 0 ? 0.f : d_logp[t];
+    const int row = rows.slot[t];
+    if (row < 0) logp[t] = 0.f;
+    else if (rows.scale) rows.set(row, d_logp[t], logp[t]);
 }
 
 // One workgroup per pair: margin, loss, and the gradient of every token of its two sequences.  Sums in 64 bits: differences of
 // some thousand logarithms each.
-__global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__ cu, const int *__restrict__ slot, const float *__restrict__ ref_logp, float beta, float smoothing,
-                                                         float loss_scale, float *__restrict__ logp, float *__restrict__ margin, float *__restrict__ loss, float *__restrict__ grad) {
+__global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__ cu, LabelRows rows, const float *__restrict__ ref_logp, float beta, float smoothing,
+                                                         float loss_scale, float *__restrict__ logp, float *__restrict__ margin, float *__restrict__ loss) {
     __shared__ double sm[4];
     __shared__ int any[4];
     const int pair = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__
     double sum = 0.0;
     int seen = 0;
     for (int t = a + threadIdx.x; t < c; t += 256) {
-        if (slot[t] < 0) {
+        if (rows.slot[t] < 0) {
             logp[t] = 0.f;
             continue;
         }
@@ -327,8 +329,11 @@ __global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__
         margin[pair] = counts ? m : 0.f;
         loss[pair] = !counts ? 0.f : x == x ? (1.f - smoothing) * lose + (smoothing > 0.f ? smoothing * win : 0.f) : x;
     }
-    if (grad)
-        for (int t = a + threadIdx.x; t < c; t += 256) grad[t] = slot[t] < 0 ? 0.f : t < b ? g : -g;
+    if (rows.scale)
+        for (int t = a + threadIdx.x; t < c; t += 256) {
+            const int row = rows.slot[t];
+            if (row >= 0) rows.set(row, t < b ? g : -g, logp[t]);
+        }
 }
 
 // Teacher's entries, one wave per row: KL of the token, scale = loss_scale / T sum p, rho = q - p / sum p.
@@ -377,7 +382,7 @@ __global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int v0
     const int row = blockIdx.x, t = token[row];
     const float *zr = z + (long)row * d_cols;
     T *o = dz + (long)row * d_cols;
-    const float c = t < 0 ? 0.f : scale[row];
+    const float c = t < 0 ? 0.f : scale[row];                                   // (a row without a token has none)
     if (c == 0.f) {
         for (int i = threadIdx.x; i < cw; i += 256) o[i] = from_f32<T>(0.f);
         return;
@@ -392,48 +397,125 @@ __global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int v0
     }
 }
 
-// Exponentials of rows with a strip that is far above the row's reference (its label is 2^64 times less likely than another id): the strips' offsets are evened out.
-// One workgroup per row; hardly ever is there anything to do.
-__global__ __launch_bounds__(256) void head_even_kernel(Slabs sl, int strips, const int *__restrict__ count, const float2 *__restrict__ part, const float2 *__restrict__ stat, bf16_t *__restrict__ e) {
-    const int row = blockIdx.x, lane = threadIdx.x & 63;
-    if (row >= *count) return;
-    const float to = stat[row].y;
-    if (to == 0.f) return;
-    for (int i = threadIdx.x >> 6; i < strips; i += 4) {
-        const float off = part[(long)i * sl.rows + row].x;
-        const int v = i * kStrip + lane;
-        if (off == to || v >= sl.vocab) continue;
-        bf16_t *at = e + sl.at(row, v);
-        *at = (bf16_t)((float)*at * __builtin_amdgcn_exp2f(off - to));
+// Exponentials -> gradient of the logits over the row's factor c = scale / sum: the selected ids get theirs, c goes onto the hidden states (for d_w) and is kept (for d_h).  One
+// workgroup per row.  Strips that are far above the row's reference (its label is 2^64 times less likely than another id) have offsets, which are evened out first.
+//
+// The exponentials are rounded to the storage type where they are stored, and c h here.  The selected ids with the largest gradients are most of the gradient's norm (a label's is the sum
+// of all others'), so what those two roundings take from them is put back: rest = dz - c (stored e), which d_h adds times its row of w, and dz h - (stored e) (stored c h),
+// a row that head_fix_kernel or the sorted sums of embedding_sorted.hip add to the id's row of d_w.  Error of d_w, rounded to bf16 by itself, against 64 bits: 2.9e-3 without, with
+// 1.8e-3; the rounding alone is 1.7e-3.
+__global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k, int strips, const float2 *__restrict__ part, const int *__restrict__ token, const int *__restrict__ count,
+                                                         const int *__restrict__ sel, const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho,
+                                                         bf16_t *__restrict__ e, bf16_t *__restrict__ h, float *__restrict__ factor, int fixes, int *__restrict__ fix_id,
+                                                         float *__restrict__ fix_rest, bf16_t *__restrict__ fix) {
+    __shared__ float s_dz[kHeadFixes], s_e[kHeadFixes];
+    __shared__ int s_id[kHeadFixes];
+    const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (row >= *count) {
+        if ((int)threadIdx.x < fixes) fix_id[(long)row * fixes + threadIdx.x] = -1;
+        return;
     }
-}
-
-// Exponentials -> gradient of the logits over the row's factor c = scale / sum: the selected ids get theirs, c goes onto the hidden states (for d_w) and is kept (for d_h).
-// One workgroup per row.  h, in the storage type, is rounded once more here.
-__global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k, const int *__restrict__ token, const int *__restrict__ count, const int *__restrict__ sel,
-                                                         const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho, bf16_t *__restrict__ e,
-                                                         bf16_t *__restrict__ h, float *__restrict__ factor) {
-    const int row = blockIdx.x;
-    if (row >= *count) return;
     const int t = token[row];
-    const float sum = stat[row].x, sc = scale[row], c = sc == 0.f ? 0.f : sc / sum;
-    if (threadIdx.x == 0) factor[row] = c;
-    for (int j = threadIdx.x; j < k; j += 256) {
-        const int v = sel[(long)t * k + j];
-        if (v >= 0) e[sl.at(row, v)] = (bf16_t)(rho[(long)row * k + j] * sum);
+    const float2 st = stat[row];
+    if (st.y != 0.f) {
+        for (int i = wave; i < strips; i += 4) {
+            const float off = part[(long)i * sl.rows + row].x;
+            const int v = i * kStrip + lane;
+            if (off == st.y || v >= sl.vocab) continue;
+            bf16_t *at = e + sl.at(row, v);
+            *at = (bf16_t)((float)*at * __builtin_amdgcn_exp2f(off - st.y));
+        }
+        __syncthreads();
     }
-    for (int i = threadIdx.x * 8; i < d; i += 256 * 8) {
-        Vec16<bf16_t> a = ldv(h + (long)row * d + i);
+    const float sc = scale[row], c = sc == 0.f ? 0.f : sc / st.x;
+    if (threadIdx.x == 0) factor[row] = c;
+    if (wave == 0) {
+        float r[2];
+        int id[2];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) a.v[x] = (bf16_t)(c == 0.f ? 0.f : c * (float)a.v[x]);
-        stv(h + (long)row * d + i, a);
+        for (int x = 0; x < 2; ++x) {
+            const int j = lane + 64 * x;
+            id[x] = j < k ? sel[(long)t * k + j] : -1;
+            r[x] = id[x] >= 0 ? rho[(long)row * k + j] : 0.f;
+            if (id[x] >= 0) e[sl.at(row, id[x])] = (bf16_t)(r[x] * st.x);
+        }
+        float least = 0.f;                                                      // an eighth of the largest: the others are left as they are
+        for (int f = 0; f < fixes; ++f) {
+            float a0 = id[0] >= 0 ? fabsf(r[0]) : -1.f, a1 = id[1] >= 0 ? fabsf(r[1]) : -1.f;
+            const float mine = fmaxf(a0, a1), best = wave_max(mine);
+            if (f == 0) least = 0.125f * best;
+            const unsigned long long who = __ballot(mine == best);
+            const bool there = sc != 0.f && best > 0.f && best >= least && who;
+            if (who && lane == __ffsll((long long)who) - 1) {
+                const int x = a0 >= a1 ? 0 : 1;
+                const float rx = x ? r[1] : r[0], held = (float)(bf16_t)(rx * st.x);
+                const int at = there ? (x ? id[1] : id[0]) : -1;
+                s_id[f] = at;
+                s_dz[f] = sc * rx;
+                s_e[f] = held;
+                fix_id[(long)row * fixes + f] = at;
+                fix_rest[(long)row * fixes + f] = __builtin_fmaf(-c, held, sc * rx);
+                if (x) id[1] = -1; else id[0] = -1;
+            } else if (!who && lane == 0) {
+                s_id[f] = -1;
+                fix_id[(long)row * fixes + f] = -1;
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x * 8; i < d; i += 256 * 8) {
+        const Vec16<bf16_t> a = ldv(h + (long)row * d + i);
+        Vec16<bf16_t> b;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) b.v[x] = (bf16_t)(c == 0.f ? 0.f : c * (float)a.v[x]);
+        stv(h + (long)row * d + i, b);
+        for (int f = 0; f < fixes; ++f) {
+            if (s_id[f] < 0) continue;
+            Vec16<bf16_t> o;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) o.v[x] = (bf16_t)__builtin_fmaf(s_dz[f], (float)a.v[x], -s_e[f] * (float)b.v[x]);
+            stv(fix + ((long)row * fixes + f) * d + i, o);
+        }
     }
 }
 
-// d_h of the block's tokens: a row's sums (in `parts` parts) times its factor; zeros for tokens that were left out
+// d_w[id] += the rows of `fix` with that id, in their order; n <= kHeadScan of them.  A workgroup per row and 512 columns: the first row of an id sums them all.
+__global__ __launch_bounds__(64) void head_fix_kernel(int n, int d, const int *__restrict__ id, const bf16_t *__restrict__ fix, float *__restrict__ d_w) {
+    __shared__ short same[kHeadScan];
+    const int i = blockIdx.x, lane = threadIdx.x, mine = id[i];
+    if (mine < 0) return;
+    for (int j0 = 0; j0 < i; j0 += 64)
+        if (__any(j0 + lane < i && id[j0 + lane] == mine)) return;
+    int rows = 0;
+    for (int j0 = i; j0 < n; j0 += 64) {
+        const bool is = j0 + lane < n && id[j0 + lane] == mine;
+        const unsigned long long mask = __ballot(is);
+        if (is) same[rows + __popcll(mask & ((1ull << lane) - 1))] = (short)(j0 + lane);
+        rows += __popcll(mask);
+    }
+    __syncthreads();
+    const int col = blockIdx.y * 512 + lane * 8;
+    if (col >= d) return;
+    float acc[8] = {};
+    for (int j = 0; j < rows; j += 4) {
+        Vec16<bf16_t> a[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) a[u] = ldv(fix + (long)same[j + u < rows ? j + u : rows - 1] * d + col);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (j + u < rows)
+#pragma unroll
+                for (int x = 0; x < 8; ++x) acc[x] += (float)a[u].v[x];
+    }
+    float *o = d_w + (long)mine * d + col;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) o[x] += acc[x];
+}
+
+// d_h of the block's tokens: a row's sums (in `parts` parts) times its factor, and what the selected ids' lack; zeros for tokens that were left out
 template <class T>
 __global__ __launch_bounds__(256) void head_d_h_kernel(long total, int d, int parts, long part_ld, const int *__restrict__ slot, const float *__restrict__ sums, const float *__restrict__ factor,
-                                                       T *__restrict__ d_h) {
+                                                       int fixes, const int *__restrict__ fix_id, const float *__restrict__ fix_rest, const bf16_t *__restrict__ w, T *__restrict__ d_h) {
     const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= total) return;
     const int t = (int)(i / d), c = (int)(i - (long)t * d), row = slot[t];
@@ -445,6 +527,16 @@ __global__ __launch_bounds__(256) void head_d_h_kernel(long total, int d, int pa
             v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
         }
         v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+        for (int q = 0; q < fixes; ++q) {
+            const int id = fix_id[(long)row * fixes + q];
+            if (id < 0) continue;
+            const float rest = fix_rest[(long)row * fixes + q];
+            const bf16_t *a = w + (long)id * d + c;
+            v.x = __builtin_fmaf(rest, (float)a[0], v.x);
+            v.y = __builtin_fmaf(rest, (float)a[1], v.y);
+            v.z = __builtin_fmaf(rest, (float)a[2], v.z);
+            v.w = __builtin_fmaf(rest, (float)a[3], v.w);
+        }
     }
     T *o = d_h + i;
     o[0] = from_f32<T>(v.x); o[1] = from_f32<T>(v.y); o[2] = from_f32<T>(v.z); o[3] = from_f32<T>(v.w);
@@ -649,8 +741,8 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
     if (p.fast) {
         const Slabs sl = {p.rows, p.cols, V};
         ProfScope ps(10, 4.0 * n * d, a.s);
-        head_even_kernel<<<n, 256, 0, a.s>>>(sl, p.strips, p.count, p.part, p.stat, (bf16_t *)p.z);
-        head_apply_kernel<<<n, 256, 0, a.s>>>(sl, d, a.k, p.token, p.count, sel, p.stat, p.scale, p.rho, (bf16_t *)p.z, (bf16_t *)p.h, p.ref);
+        head_apply_kernel<<<n, 256, 0, a.s>>>(sl, d, a.k, p.strips, p.part, p.token, p.count, sel, p.stat, p.scale, p.rho, (bf16_t *)p.z, (bf16_t *)p.h, p.ref, p.fixes, p.fix_id, p.fix_rest,
+                                              (bf16_t *)p.fix);
     }
     MS_LAUNCH_CHECK();
     for (int i = 0; i < p.slabs; ++i) {
@@ -673,13 +765,22 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
         else if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, p.d_h, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
         else MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 0, a.s));
     }
+    if (p.fast && a.d_w) {
+        const int rows = n * p.fixes;
+        if (rows <= kHeadScan) {
+            head_fix_kernel<<<dim3(rows, ms_cdiv(d, 512)), 64, 0, a.s>>>(rows, d, p.fix_id, (const bf16_t *)p.fix, (float *)a.d_w);
+            MS_LAUNCH_CHECK();
+        } else {
+            MS_TRY(ms_k_embedding_sorted_backward(dt, rows, d, V, 1.f, p.fix_id, p.fix, (float *)a.d_w, p.fix_scratch, p.fix_scratch_bytes, a.s));
+        }
+    }
     if (!a.d_h) return MS_OK;
     char *out = (char *)a.d_h + (size_t)t0 * d * es;
     const long total = (long)n * d;
     ProfScope ps(11, (4.0 + es) * total, a.s);
     const long part_ld = (long)n * d;
-    if (dt == MS_F32) head_d_h_kernel<float><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, 1, part_ld, p.slot, p.d_h, nullptr, (float *)out);
-    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.parts, part_ld, p.slot, p.d_h, p.fast ? p.ref : nullptr, (bf16_t *)out);
+    if (dt == MS_F32) head_d_h_kernel<float><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, 1, part_ld, p.slot, p.d_h, nullptr, 0, nullptr, nullptr, nullptr, (float *)out);
+    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.parts, part_ld, p.slot, p.d_h, p.fast ? p.ref : nullptr, p.fixes, p.fix_id, p.fix_rest, (const bf16_t *)c->w_dev, (bf16_t *)out);
     MS_LAUNCH_CHECK();
     return MS_OK;
 }
@@ -709,12 +810,7 @@ ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, i
 }
 HeadUse use_of(const void *d_h, const void *d_w) { return d_h || d_w ? HEAD_BACKWARD : HEAD_FORWARD; }
 
-// A block whose tokens' d loss / d logp is in p.grad
-ms_status labels_backward(const HeadCall &a, int t0, int n, const int *labels, const float *logp) {
-    head_label_rows_kernel<<<ms_cdiv(n, 256), 256, 0, a.s>>>(a.p.count, a.p.token, logp, a.p.grad, 1.f / a.c->temperature, a.p.scale, a.p.rho);
-    MS_LAUNCH_CHECK();
-    return rows_backward(a, t0, n, labels);
-}
+LabelRows label_rows(const HeadCall &a) { return LabelRows{a.p.slot, a.p.scale, a.p.rho, -1.f / a.c->temperature}; }
 
 }  // namespace
 
@@ -778,9 +874,9 @@ static ms_status token_logprobs(const char *what, const ms_head_config *c, int n
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
         float *lp = logp ? logp + t0 : p.logp;
         MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp));
-        head_given_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, p.slot, back ? d_logp + t0 : nullptr, lp, back ? p.grad : nullptr);
+        head_given_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, label_rows(a), back ? d_logp + t0 : nullptr, lp);
         MS_LAUNCH_CHECK();
-        if (back) MS_TRY(labels_backward(a, t0, nb, labels + t0, lp));
+        if (back) MS_TRY(rows_backward(a, t0, nb, labels + t0));
     }
     return MS_OK;
 }
@@ -814,9 +910,9 @@ extern "C" ms_status ms_policy_loss_forward_backward(const ms_head_config *c, co
         MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp));
         const PolicyArgs pa = {old_logp + t0, pc->kl_coef > 0.f ? ref_logp + t0 : nullptr, advantages + t0, weights ? weights + t0 : nullptr, pc->clip_low, pc->clip_high, pc->kl_coef,
                                c->loss_scale};
-        head_policy_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, p.slot, pa, lp, p.grad ? p.grad : p.z_sel, terms + t0);
+        head_policy_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, label_rows(a), pa, lp, terms + t0);
         MS_LAUNCH_CHECK();
-        if (d_h || d_w) MS_TRY(labels_backward(a, t0, nb, labels + t0, lp));
+        if (d_h || d_w) MS_TRY(rows_backward(a, t0, nb, labels + t0));
     }
     return total_loss(terms, n, c->loss_scale, loss, a.s);
 }
@@ -847,9 +943,8 @@ extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c
     const HeadPlan &p = a.p;
     float *lp = logp ? logp : p.logp;
     MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp));
-    head_pairs_kernel<<<pairs, 256, 0, a.s>>>(batch->cu_seqlens_dev, p.slot, ref_logp, pc->beta, pc->label_smoothing, c->loss_scale, lp, margin ? margin : p.margin, p.per_token,
-                                              p.grad);
+    head_pairs_kernel<<<pairs, 256, 0, a.s>>>(batch->cu_seqlens_dev, label_rows(a), ref_logp, pc->beta, pc->label_smoothing, c->loss_scale, lp, margin ? margin : p.margin, p.per_token);
     MS_LAUNCH_CHECK();
-    if (d_h || d_w) MS_TRY(labels_backward(a, 0, n, labels, lp));
+    if (d_h || d_w) MS_TRY(rows_backward(a, 0, n, labels));
     return total_loss(p.per_token, pairs, c->loss_scale, loss, a.s);
 }

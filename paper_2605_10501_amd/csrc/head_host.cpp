@@ -60,12 +60,20 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     }
     if (use == HEAD_BACKWARD) {
         p.rho = a.take<float>(r * (k ? k : 1) * 4);
-        p.grad = a.take<float>(r * 4);
         p.scale = a.take<float>(r * 4);
         p.parts = 1;
         if (p.fast) {
             p.choice = head_choose(p.rows, V < p.cols ? V : p.cols, d, true, true);
             p.parts = p.choice.parts;
+            p.fixes = k < 1 ? 1 : k < kHeadFixes ? k : kHeadFixes;
+            const size_t f = r * p.fixes;
+            p.fix_id = a.take<int>(f * 4);
+            p.fix_rest = a.take<float>(f * 4);
+            p.fix = a.take<void>(f * d * 2);
+            if (f > (size_t)kHeadScan) {
+                p.fix_scratch_bytes = ms_k_embedding_sorted_backward_scratch_bytes((int)f, (int)d, (int)V);
+                p.fix_scratch = a.take<void>(p.fix_scratch_bytes);
+            }
         }
         p.d_h = a.take<float>(r * p.parts * d * 4);
         if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(r * p.cols * 2);
