@@ -38,8 +38,8 @@ struct GemmParams {
 };
 
 // EPI_SWIGLU_BWD: the tile holds da = dL/d(silu(gate) * up); sg_gu = the pre-activations [M, sg_ldgu], read; C = [dgate | dup] [M, ldc]
-// EPI_EXP, EPI_LOGITS: the tile holds logits z (head_gemm.hip).  EXP: kd_stats = reference of each row [M]; C (may be null) = 2^(x - reference) with x = z kd_inv_t,
-// bf16, zeros in the columns N .. N + 63 / 64 * 64; LOGITS: C = z, fp32.  kd_part = (offset, sum) of every 64-column strip and row, [strip][kd_ldz].
+// EPI_EXP, EPI_LOGITS: the tile holds logits z (head_gemm.hip).  EXP: kd_stats = (reference, label as an int) of each row [M]; C (may be null) = 2^(x - reference) with
+// x = z kd_inv_t, bf16, zeros in the columns N .. N + 63 / 64 * 64; sg_gu [M] (fp32) = z of a row's label, if that is one of the columns sg_f .. sg_f + N - 1 of the vocabulary; LOGITS: C = z, fp32.  kd_part = (offset, sum) of every 64-column strip and row, [strip][kd_ldz].
 enum { EPI_NONE = 0, EPI_KD_DZ = 1, EPI_KD_STATS = 2, EPI_SWIGLU = 3, EPI_SWIGLU_BWD = 4, EPI_EXP = 5, EPI_LOGITS = 6 };
 
 // Reductions over the four 16-lane groups of a wave, on the vector ALU (no LDS crossbar): lane l gets the result over lanes
@@ -348,7 +348,7 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
         const bool cok = colg < p.N, stored = colg < (p.N + 63) / 64 * 64;
         const float it2 = p.kd_inv_t;
         const unsigned lane_c = (unsigned)((prow * p.ldc + colg) * (EPI == EPI_EXP ? 2 : 4));
-        const __amdgpu_buffer_rsrc_t rl = make_rsrc(EPI == EPI_EXP ? (const void *)p.kd_stats : p.C, EPI == EPI_EXP ? (long)p.M * 4 : 0);
+        const __amdgpu_buffer_rsrc_t rl = make_rsrc(EPI == EPI_EXP ? (const void *)p.kd_stats : p.C, EPI == EPI_EXP ? (long)p.M * 8 : 0);
         const __amdgpu_buffer_rsrc_t rz = make_rsrc(p.C ? p.C : p.kd_part, p.C ? (long)p.M * p.ldc * (EPI == EPI_EXP ? 2 : 4) : 0);
         auto sum = [](float a, float b) { return a + b; };
         auto larger = [](float a, float b) { return fmaxf(a, b); };
@@ -356,9 +356,11 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
         for (int i = 0; i < MI32; ++i) {
             float ref[8], s[8], off[8];
             u32x2 w[8];
+            int label = -1;                                                              // of the row that this lane stores for (idx < 8)
             if constexpr (EPI == EPI_EXP) {
 #pragma unroll
-                for (int ps = 0; ps < 8; ++ps) ref[ps] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rl, prow * 4 + row_bytes(i, ps * 4, 1, 4), 0, 0));
+                for (int ps = 0; ps < 8; ++ps) ref[ps] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rl, prow * 8 + row_bytes(i, ps * 4, 2, 4), 0, 0));
+                label = __builtin_bit_cast(int, __builtin_amdgcn_raw_buffer_load_b32(rl, (idx & 7) * 32 + prow * 8 + 4 + row_bytes(i, 0, 2, 4), 0, 0));
             }
             stage_block(i, [](float a) { return a; });
             auto row_of = [&](int ps, float (&z)[4]) __attribute__((always_inline)) {
@@ -393,6 +395,9 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
                 s[ps] = across_row((e[0] + e[1]) + (e[2] + e[3]), sum);
             }
             if constexpr (EPI == EPI_EXP) {
+                const int row_here = idx * 4 + prow, at = label - p.sg_f - strip;
+                const bool mine = idx < 8 && (unsigned)at < 64 && at < p.N - strip && m0 + row_base(i) + row_here < p.M;
+                if (__any(mine) && mine) ((float *)p.sg_gu)[m0 + row_base(i) + row_here] = stg[row_here * 64 + (at ^ stg_swz(row_here))];
                 bool far = false;
 #pragma unroll
                 for (int ps = 0; ps < 8; ++ps) far |= !(s[ps] < 0x1p64f);

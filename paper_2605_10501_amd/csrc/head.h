@@ -6,7 +6,7 @@
 
 constexpr int kHeadMaxTop = 128;             // entries of a token that the kernels hold
 constexpr int kHeadFixes = 4;                // of a token's entries whose gradients are completed in fp32
-constexpr int kHeadScan = 4096;              // rows of such, up to which each looks for the others of its id by itself
+constexpr int kHeadScan = 8192;              // rows of such, up to which each looks for the others of its id by itself
 constexpr int kStrip = 64;                   // columns that share one partial sum
 
 // Rows of hidden states meet the vocabulary a block of tokens at a time.  What a block keeps of every (row, vocabulary entry) lies in
@@ -16,8 +16,10 @@ struct HeadPlan {
     bool fast;                               // bf16 products whose epilogue meets the logits (head_gemm.hip)
     int *slot, *token, *count;               // [rows] row of a token, [rows] token of a row (-1: none), [1] rows in use
     void *h;                                 // [rows, hidden] hidden states of the rows, later times the row's factor
-    float *ref, *scale;                      // [rows] reference of a row's exponentials in units of log2 e, factor of a row's gradient
+    float2 *ref;                             // [rows] reference of a row's exponentials (in x) and its label as an int (-1: it has entries)
+    float *scale, *factor;                   // [rows] dz = scale q of a row; the factor of what is stored of it
     float2 *stat;                            // [rows] sum of exponentials and its reference
+    float *z_label;                          // [rows] a label's logit as the matrix product has it
     float *z_sel, *rho;                      // [rows, k] logits at the selected ids, and what a row has there in its gradient
     float *log_p, *mass;                     // [rows, k], [rows] of the teacher's entries
     int *ids;                                // [rows, k] the entries that count (-1: ignored)

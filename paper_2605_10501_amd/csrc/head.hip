@@ -11,6 +11,7 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr double kLog2e64 = 1.4426950408889634, kLn264 = 0.6931471805599453;
 
 // Logits [slab][rows][cols] (or what is kept in their place)
 struct Slabs {
@@ -88,16 +89,20 @@ __global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int voc
     }
 }
 
-// Rows of a block: row t for token t, or, with `compact`, the tokens that count (key in [0, limit)) in their order, without gaps.
+// Rows of a block: row t for token t (of whose outputs out0, out1 the left-out ones are 0), or, with `compact`, the tokens that count (key in [0, limit)) in their order, without gaps.
 // One workgroup: a block has at most some 10^5 tokens, of which it reads four bytes.
 __global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__restrict__ key, int limit, int compact, int *__restrict__ slot,
-                                                         int *__restrict__ token, int *__restrict__ count) {
+                                                         int *__restrict__ token, int *__restrict__ count, float *__restrict__ out0, float *__restrict__ out1) {
     __shared__ int sm[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int base = 0;
     for (int t0 = 0; t0 < n; t0 += 1024) {
         const int t = t0 + threadIdx.x;
         const bool in = t < n && key[t] >= 0 && key[t] < limit;
+        if (t < n && !in) {
+            if (out0) out0[t] = 0.f;
+            if (out1) out1[t] = 0.f;
+        }
         if (!compact) {
             if (t < n) {
                 slot[t] = in ? t : -1;
@@ -125,11 +130,11 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__res
 // ------------------------------------------------------------------ rows and their selected logits
 // Copies the hidden states of the rows together, and takes the logits of each row's k selected ids (h rows . w rows, fp32); the reference of the
 // row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.
-// W waves a row: one for a label, four for the teacher's entries, four ids at a time.  Rows that no token has (token -1) are zeros.
+// W waves a row: one for a label, four or eight for the teacher's entries, four ids at a time.  Rows that no token has (token -1) are zeros.
 template <class T, int W>
 __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T *__restrict__ h, const T *__restrict__ w, const int *__restrict__ token,
                                                            const int *__restrict__ count, const int *__restrict__ sel, float it2, T *__restrict__ out,
-                                                           float *__restrict__ z_sel, float *__restrict__ ref) {
+                                                           float *__restrict__ z_sel, float2 *__restrict__ ref) {
     __shared__ float sm[W];
     const int row = blockIdx.x;
     if (row >= *count) return;
@@ -140,11 +145,11 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T
 #pragma unroll
         for (int e = 0; e < N; ++e) zero.v[e] = from_f32<T>(0.f);
         for (int i = threadIdx.x * N; i < d; i += 64 * W * N) stv(out + (long)row * d + i, zero);
-        if (threadIdx.x == 0) ref[row] = 0.f;
         return;
     }
     const T *hr = h + (long)t * d;
     for (int i = threadIdx.x * N; i < d; i += 64 * W * N) stv(out + (long)row * d + i, ldv(hr + i));
+    if (k == 0) return;                                                           // (stored logits have them)
     float best = -INFINITY;
     for (int j0 = wave * 4; j0 < k; j0 += 4 * W) {
         const T *wr[4];
@@ -177,8 +182,16 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < W; ++i) best = fmaxf(best, sm[i]);
-        ref[row] = rintf(best * it2);
+        ref[row] = make_float2(rintf(best * it2), __int_as_float(k == 1 ? sel[t] : -1));
     }
+}
+
+// Stored logits at the selected ids
+__global__ __launch_bounds__(256) void head_gather_kernel(Slabs sl, long total, int k, const int *__restrict__ token, const int *__restrict__ sel, const float *__restrict__ z, float *__restrict__ z_sel) {
+    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int row = (int)(i / k), t = token[row], v = t < 0 ? -1 : sel[(long)t * k + (i - (long)row * k)];
+    if (v >= 0) z_sel[i] = z[sl.at(row, v)];
 }
 
 // ------------------------------------------------------------------ sums over the vocabulary
@@ -196,13 +209,57 @@ __global__ __launch_bounds__(256) void head_strips_kernel(Slabs sl, int rows, in
     }
 }
 
+// ------------------------------------------------------------------ what a token's gradient is
+// Labels: dz = g / T (1_label - q), g = d loss / d logp, so scale = -g / T and rho = q - 1.
+struct LabelRows {
+    const int *slot;
+    float *scale, *rho, minus_inv_t;                                            // scale null: forward only
+    __device__ __forceinline__ void set(int row, float g, float logp) const {
+        if (!scale) return;
+        scale[row] = minus_inv_t * g;
+        rho[row] = expm1f(logp);
+    }
+};
+
+struct PolicyArgs {
+    const float *old_logp, *ref_logp, *adv, *weights;
+    float *loss_tok;
+    float low, high, kl, loss_scale;
+};
+__device__ __forceinline__ float policy_term(const PolicyArgs &a, int t, float l) {                // writes the loss, returns d loss / d logp
+    const float adv = a.adv[t], wt = a.weights ? a.weights[t] : 1.f;
+    const float r = expf(l - a.old_logp[t]);
+    const bool inside = adv > 0.f ? r <= 1.f + a.high : r >= 1.f - a.low;          // (a NaN ratio is not; it is in `gain` all the same)
+    const float gain = adv == 0.f ? 0.f : adv * (inside || !(r == r) ? r : adv > 0.f ? 1.f + a.high : 1.f - a.low);
+    float loss = -gain, g = inside || !(r == r) ? -gain : 0.f;
+    if (a.ref_logp) {
+        const float u = a.ref_logp[t] - l, away = expm1f(u);
+        loss += a.kl * (away - u);
+        g -= a.kl * away;
+    }
+    a.loss_tok[t] = wt * loss;
+    return a.loss_scale * wt * g;
+}
+// What follows for a row with a label once its sum is there
+enum { AFTER_NOTHING = 0, AFTER_LOGP = 1, AFTER_GIVEN = 2, AFTER_POLICY = 3 };
+struct After {
+    int what;
+    double inv_t;
+    const float *z_label;
+    float *logp;                                                                   // by token
+    const float *d_logp;                                                           // given
+    LabelRows rows;
+    PolicyArgs policy;
+};
+
+// ------------------------------------------------------------------ sums over the vocabulary, joined
 // Behind the vocabulary: sum of the strips' sums at a common reference.  part holds (offset, sum) of each strip [strips][ld]: stored logits' offsets are logits
 // (`unit` of x each), those of exponentials (`ref` given) count in x on top of the row's reference.  A row's strips are shared by 64 threads whatever the number
 // of rows, so that a token's sum does not depend on its batch; a workgroup takes `rows_per` rows, up to 16 (128 bytes of neighbouring rows per strip).
-// stat[row] = (sum, offset); logp: by token, lse: by row, where asked for.
-__global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, int rows_per, int strips, const float2 *__restrict__ part, float unit, const float *__restrict__ ref,
+// stat[row] = (sum, offset) and lse, by row, where asked for; then what follows.
+__global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, int rows_per, int strips, const float2 *__restrict__ part, float unit, const float2 *__restrict__ ref,
                                                             const int *__restrict__ token, const int *__restrict__ count, const float *__restrict__ z_sel, float it2,
-                                                            float2 *__restrict__ stat, float *__restrict__ logp, float *__restrict__ lse) {
+                                                            float2 *__restrict__ stat, float *__restrict__ lse, After after) {
     __shared__ float2 sm[1024];
     const int r = threadIdx.x & (rows_per - 1), g = threadIdx.x / rows_per;
     const int row = blockIdx.x * rows_per + r, n = count ? *count : rows;
@@ -233,66 +290,25 @@ __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, in
     }
     if (g != 0 || row >= n) return;
     if (stat) stat[row] = make_float2(s, m);
-    const float base = ref ? ref[row] : 0.f, l2 = __log2f(s);
+    const float l2 = __log2f(s);
     if (lse) lse[row] = kLn2 * (m * unit + l2);
-    if (logp) {
-        const int t = token[row];
-        // (x of the label - reference) first: both are near each other, and the rest is small where the label is likely
-        if (t >= 0) logp[t] = fminf(0.f, kLn2 * ((ref ? __builtin_fmaf(z_sel[row], it2, -base) - m : (z_sel[row] - m) * it2) - l2));
-    }
-}
-
-// ------------------------------------------------------------------ what a token's gradient is
-// Labels: dz = g / T (1_label - q), g = d loss / d logp, so scale = -g / T and rho = q - 1.
-struct LabelRows {
-    const int *slot;
-    float *scale, *rho, minus_inv_t;                                            // scale null: forward only
-    __device__ __forceinline__ void set(int row, float g, float logp) const {
-        if (!scale) return;
-        scale[row] = minus_inv_t * g;
-        rho[row] = expm1f(logp);
-    }
-};
-
-struct PolicyArgs {
-    const float *old_logp, *ref_logp, *adv, *weights;
-    float low, high, kl, loss_scale;
-};
-__global__ __launch_bounds__(256) void head_policy_kernel(int n, LabelRows rows, PolicyArgs a, float *__restrict__ logp, float *__restrict__ loss_tok) {
-    const int t = blockIdx.x * 256 + threadIdx.x;
-    if (t >= n) return;
-    const int row = rows.slot[t];
-    if (row < 0) {
-        logp[t] = loss_tok[t] = 0.f;
-        return;
-    }
-    const float l = logp[t], adv = a.adv[t], wt = a.weights ? a.weights[t] : 1.f;
-    const float r = expf(l - a.old_logp[t]);
-    const bool inside = adv > 0.f ? r <= 1.f + a.high : r >= 1.f - a.low;          // (a NaN ratio is not; it is in `gain` all the same)
-    const float gain = adv == 0.f ? 0.f : adv * (inside || !(r == r) ? r : adv > 0.f ? 1.f + a.high : 1.f - a.low);
-    float loss = -gain, g = inside || !(r == r) ? -gain : 0.f;
-    if (a.ref_logp) {
-        const float u = a.ref_logp[t] - l, away = expm1f(u);
-        loss += a.kl * (away - u);
-        g -= a.kl * away;
-    }
-    loss_tok[t] = wt * loss;
-    rows.set(row, a.loss_scale * wt * g, l);
-}
-
-// logp of the tokens that were left out; the gradient that the caller gives
-__global__ __launch_bounds__(256) void head_given_kernel(int n, LabelRows rows, const float *__restrict__ d_logp, float *__restrict__ logp) {
-    const int t = blockIdx.x * 256 + threadIdx.x;
-    if (t >= n) return;
-    const int row = rows.slot[t];
-    if (row < 0) logp[t] = 0.f;
-    else if (rows.scale) rows.set(row, d_logp[t], logp[t]);
+    if (after.what == AFTER_NOTHING) return;
+    const int t = token[row];
+    if (t < 0) return;
+    // The label's logit is a dot product of its own (64 partial sums), nearer than the matrix product's, whose error would be there in full where the label is unlikely; in the
+    // sum it takes the place of the matrix product's, so that they go together where it is likely.  In 64 bits: logarithms of 15 summed over a sequence, and their differences.
+    const double x = (double)z_sel[row] * after.inv_t * kLog2e64, base = ref ? (double)ref[row].x + m : (double)m * after.inv_t * kLog2e64;
+    const float in_sum = __builtin_amdgcn_exp2f(ref ? __builtin_fmaf(after.z_label[row], it2, -ref[row].x) - m : (after.z_label[row] - m) * it2);
+    const float l = (float)fmin(0.0, kLn264 * (x - base) - log(fmax((double)s - (double)in_sum, 0.0) + exp2(x - base)));
+    after.logp[t] = l;
+    if (after.what == AFTER_POLICY) after.rows.set(row, policy_term(after.policy, t, l), l);
+    else if (after.what == AFTER_GIVEN) after.rows.set(row, after.d_logp[t], l);
 }
 
 // One workgroup per pair: margin, loss, and the gradient of every token of its two sequences.  Sums in 64 bits: differences of
 // some thousand logarithms each.
 __global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__ cu, LabelRows rows, const float *__restrict__ ref_logp, float beta, float smoothing,
-                                                         float loss_scale, float *__restrict__ logp, float *__restrict__ margin, float *__restrict__ loss) {
+                                                         float loss_scale, const float *__restrict__ logp, float *__restrict__ margin, float *__restrict__ loss) {
     __shared__ double sm[4];
     __shared__ int any[4];
     const int pair = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -300,10 +316,7 @@ __global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__
     double sum = 0.0;
     int seen = 0;
     for (int t = a + threadIdx.x; t < c; t += 256) {
-        if (rows.slot[t] < 0) {
-            logp[t] = 0.f;
-            continue;
-        }
+        if (rows.slot[t] < 0) continue;
         const double diff = (double)logp[t] - (ref_logp ? (double)ref_logp[t] : 0.0);
         sum += t < b ? diff : -diff;
         seen = 1;
@@ -338,7 +351,7 @@ __global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__
 
 // Teacher's entries, one wave per row: KL of the token, scale = loss_scale / T sum p, rho = q - p / sum p.
 __global__ __launch_bounds__(256) void head_entry_rows_kernel(int n, int k, const int *__restrict__ slot, const int *__restrict__ ids, const float *__restrict__ log_p,
-                                                              const float *__restrict__ mass, const float *__restrict__ z_sel, const float2 *__restrict__ stat, const float *__restrict__ ref,
+                                                              const float *__restrict__ mass, const float *__restrict__ z_sel, const float2 *__restrict__ stat, const float2 *__restrict__ ref,
                                                               float it2, float coef, float *__restrict__ kl, float *__restrict__ scale, float *__restrict__ rho) {
     const int lane = threadIdx.x & 63;
     const long t = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -349,7 +362,7 @@ __global__ __launch_bounds__(256) void head_entry_rows_kernel(int n, int k, cons
         return;
     }
     const float2 st = stat[row];
-    const float base = ref ? ref[row] : 0.f, l2 = __log2f(st.x), inv_mass = 1.f / mass[t];
+    const float base = ref ? ref[row].x : 0.f, l2 = __log2f(st.x), inv_mass = 1.f / mass[t];
     float sum = 0.f;
     for (int j = lane; j < k; j += 64) {
         if (ids[t * k + j] < 0) continue;
@@ -479,37 +492,122 @@ __global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k,
     }
 }
 
-// d_w[id] += the rows of `fix` with that id, in their order; n <= kHeadScan of them.  A workgroup per row and 512 columns: the first row of an id sums them all.
-__global__ __launch_bounds__(64) void head_fix_kernel(int n, int d, const int *__restrict__ id, const bf16_t *__restrict__ fix, float *__restrict__ d_w) {
-    __shared__ short same[kHeadScan];
-    const int i = blockIdx.x, lane = threadIdx.x, mine = id[i];
-    if (mine < 0) return;
-    for (int j0 = 0; j0 < i; j0 += 64)
-        if (__any(j0 + lane < i && id[j0 + lane] == mine)) return;
-    int rows = 0;
-    for (int j0 = i; j0 < n; j0 += 64) {
-        const bool is = j0 + lane < n && id[j0 + lane] == mine;
-        const unsigned long long mask = __ballot(is);
-        if (is) same[rows + __popcll(mask & ((1ull << lane) - 1))] = (short)(j0 + lane);
-        rows += __popcll(mask);
+// d_w[id] += the rows of `fix` with that id, in their order; n <= kHeadScan of them.  A workgroup takes eight rows and 512 columns: each of its waves looks for the others of one
+// row's id in a copy of the ids in LDS, and the first row of an id sums them all, by itself or, where there are many, with all eight waves (an eighth of the rows each).
+// (A workgroup per row that reads the ids itself: 18 us for 2053 rows of 1024, 41 for 4124; waves by themselves 38 and 26; XX.)
+constexpr int kFixWaves = 8;
+__global__ __launch_bounds__(64 * kFixWaves) void head_fix_kernel(int n, int d, const int *__restrict__ id, const bf16_t *__restrict__ fix, float *__restrict__ d_w) {
+    constexpr int kMany = 8, kList = 256;
+    __shared__ __align__(16) int ids[kHeadScan];
+    __shared__ unsigned short found[kFixWaves][kList];
+    __shared__ float join[(kFixWaves - 1) * 512];
+    __shared__ int many[kFixWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (n + 255) >> 8;
+    for (int j0 = tid; j0 < chunks * 256; j0 += 8 * 64 * kFixWaves) {
+        int q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) q[u] = j0 + u * 64 * kFixWaves < n ? id[j0 + u * 64 * kFixWaves] : -1;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (j0 + u * 64 * kFixWaves < chunks * 256) ids[j0 + u * 64 * kFixWaves] = q[u];
     }
     __syncthreads();
-    const int col = blockIdx.y * 512 + lane * 8;
-    if (col >= d) return;
+    auto wave_sync = []() __attribute__((always_inline)) {                       // the lanes of a wave exchange places through `found`
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    const int i = blockIdx.x * kFixWaves + wave, mine = i < n ? ids[i] : -1, col = blockIdx.y * 512 + lane * 8;
     float acc[8] = {};
-    for (int j = 0; j < rows; j += 4) {
-        Vec16<bf16_t> a[4];
+    auto sum = [&](const unsigned short *list, int from, int to) __attribute__((always_inline)) {
+        if (col < d)
+            for (int j = from; j < to; j += 8) {
+                Vec16<bf16_t> a[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) a[u] = ldv(fix + (long)same[j + u < rows ? j + u : rows - 1] * d + col);
+                for (int u = 0; u < 8; ++u) a[u] = ldv(fix + (long)list[j + u < to ? j + u : to - 1] * d + col);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (j + u < rows)
+                for (int u = 0; u < 8; ++u)
+                    if (j + u < to)
 #pragma unroll
-                for (int x = 0; x < 8; ++x) acc[x] += (float)a[u].v[x];
+                        for (int x = 0; x < 8; ++x) acc[x] += (float)a[u].v[x];
+            }
+    };
+    auto put = [&](int row) __attribute__((always_inline)) {
+        if (col >= d) return;
+        float4 *o = (float4 *)(d_w + (long)row * d + col), x = o[0], y = o[1];
+        o[0] = make_float4(x.x + acc[0], x.y + acc[1], x.z + acc[2], x.w + acc[3]);
+        o[1] = make_float4(y.x + acc[4], y.y + acc[5], y.z + acc[6], y.w + acc[7]);
+    };
+    // the lanes' four ids of a chunk that are this row's
+    auto same = [&](int c) __attribute__((always_inline)) {
+        const int4 q = *(const int4 *)(ids + c * 256 + lane * 4);
+        return (unsigned)(q.x == mine) | (unsigned)(q.y == mine) << 1 | (unsigned)(q.z == mine) << 2 | (unsigned)(q.w == mine) << 3;
+    };
+    bool first = mine >= 0;
+    int total = 0;
+    if (first) {
+        int before = 0;
+        for (int c = 0; c < chunks; ++c) {
+            const unsigned m = same(c);
+            const int j = c * 256 + lane * 4;
+            total += __popc(m);
+            if (j < i) before |= j + 4 <= i ? m : m & ((1u << (i - j)) - 1);
+        }
+        first = !__any(before);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
     }
-    float *o = d_w + (long)mine * d + col;
+    const bool shared = first && total > kMany && total <= kList;
+    if (lane == 0) many[wave] = shared ? total : 0;
+    if (first) {
+        int have = 0;
+        for (int c = i >> 8; c < chunks; ++c) {
+            const unsigned m = same(c);
+            if (!__any(m)) continue;
+            int upto = __popc(m);
 #pragma unroll
-    for (int x = 0; x < 8; ++x) o[x] += acc[x];
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(upto, o, 64);
+                if (lane >= o) upto += v;
+            }
+            int at = have + upto - __popc(m);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (m >> u & 1) found[wave][at++] = (unsigned short)(c * 256 + lane * 4 + u);
+            have += __shfl(upto, 63, 64);
+            if (!shared && have >= kList - 256) {                                // (more than the list holds: it is emptied in between)
+                wave_sync();
+                sum(found[wave], 0, have);
+                wave_sync();
+                have = 0;
+            }
+        }
+        if (!shared) {
+            wave_sync();
+            sum(found[wave], 0, have);
+            put(mine);
+        }
+    }
+    __syncthreads();
+    for (int e = 0; e < kFixWaves; ++e) {
+        const int rows = many[e];
+        if (!rows) continue;                                                     // (the same in all waves)
+        const int per = (rows + kFixWaves - 1) / kFixWaves, from = wave * per, to = from + per < rows ? from + per : rows;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) acc[x] = 0.f;
+        sum(found[e], from, to);
+        if (wave)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) join[(wave - 1) * 512 + x * 64 + lane] = acc[x];
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                for (int w = 0; w < kFixWaves - 1; ++w) acc[x] += join[w * 512 + x * 64 + lane];
+            put(ids[blockIdx.x * kFixWaves + e]);
+        }
+        __syncthreads();
+    }
 }
 
 // d_h of the block's tokens: a row's sums (in `parts` parts) times its factor, and what the selected ids' lack; zeros for tokens that were left out
@@ -548,7 +646,6 @@ __device__ __forceinline__ unsigned ordered(float v) {
     const unsigned u = __float_as_uint(v == v ? v + 0.f : INFINITY);                 // (+ 0: one zero)
     return v == v ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 0xffffffffu;
 }
-__device__ __forceinline__ unsigned long long entry_key(float v, int place) { return (unsigned long long)ordered(v) << 32 | (0xffffffffu - (unsigned)place); }
 __device__ __forceinline__ float entry_value(unsigned long long key) {
     const unsigned u = (unsigned)(key >> 32);
     return u == 0xffffffffu ? NAN : __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
@@ -574,85 +671,148 @@ __device__ __forceinline__ void sort_keys(unsigned long long *key, int n) {
 // The k largest logits of a row, one workgroup each.  They lie in the k strips with the largest maxima (equal ones by their place): an entry of another
 // strip has k maxima before it.  So: those strips, by the bits of the k-th largest maximum (four passes over a histogram of eight bits each); their entries
 // that are not below that maximum, which are few more than k; those sorted.
-constexpr int kTopThreads = 256;
-__global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int strips, int k, const float *__restrict__ z, const float2 *__restrict__ part,
+constexpr int kTopKeys = 2048;                      // candidates that are sorted in LDS
+constexpr int kTopThreads = 512, kTopHeld = 8;      // strips of a thread whose maxima it keeps in registers (V up to 262144); more are read again in each pass
+__global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int rows, int strips, int k, const float *__restrict__ z, const float2 *__restrict__ part,
                                                                float *__restrict__ values, int *__restrict__ ids) {
     __shared__ unsigned hist[256], sh_prefix;
     __shared__ int sh_want, n_strips, n_keys, wsum[kTopThreads / 64];
     __shared__ int list[kHeadMaxTop];
-    __shared__ unsigned long long keys[kHeadMaxTop * kStrip];
-    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int want = k < strips ? k : strips;
-    // the `want`-th largest maximum, eight bits at a time
-    unsigned prefix = 0;
-    int left = want;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kTopThreads) hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < strips; i += kTopThreads) {
-            const unsigned o = ordered(part[(long)i * sl.rows + row].x);
-            if (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(o >> shift) & 255], 1u);
-        }
-        __syncthreads();
-        if (wave == 0) {                                                             // from the top bin down: where the count passes `left`
-            unsigned h[4], mine = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mine += h[e] = hist[255 - (lane * 4 + e)];
-            unsigned upto = mine;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const unsigned v = __shfl_up(upto, o, 64);
-                if (lane >= o) upto += v;
+    __shared__ unsigned long long keys[kTopKeys];
+    // neighbouring rows, whose maxima share cache lines, go to one XCD (workgroups go to the eight in turn)
+    const int each = (rows + 7) >> 3, row = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    if (row >= rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // of n values ordered(value(i)): the `want`-th largest (its bits) and how many of those equal to it belong to the `want` largest
+    auto nth = [&](int n, int want, auto value, unsigned *bits, int *equal) __attribute__((always_inline)) {
+        unsigned prefix = 0;
+        int left = want;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = tid; i < 256; i += kTopThreads) hist[i] = 0;
+            __syncthreads();
+            for (int i = tid; i < n; i += kTopThreads) {
+                const unsigned o = value(i);
+                if (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(o >> shift) & 255], 1u);
             }
-            unsigned before = upto - mine;
+            __syncthreads();
+            if (wave == 0) {                                                         // from the top bin down: where the count passes `left`
+                unsigned h[4], mine = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (before < (unsigned)left && before + h[e] >= (unsigned)left) {
-                    sh_prefix = prefix | (unsigned)(255 - (lane * 4 + e)) << shift;
-                    sh_want = left - (int)before;
+                for (int e = 0; e < 4; ++e) mine += h[e] = hist[255 - (lane * 4 + e)];
+                unsigned upto = mine;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const unsigned v = __shfl_up(upto, o, 64);
+                    if (lane >= o) upto += v;
                 }
-                before += h[e];
+                unsigned before = upto - mine;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (before < (unsigned)left && before + h[e] >= (unsigned)left) {
+                        sh_prefix = prefix | (unsigned)(255 - (lane * 4 + e)) << shift;
+                        sh_want = left - (int)before;
+                    }
+                    before += h[e];
+                }
             }
+            __syncthreads();
+            prefix = sh_prefix;
+            left = sh_want;
         }
+        *bits = prefix;
+        *equal = left;
         __syncthreads();
-        prefix = sh_prefix;
-        left = sh_want;
-        __syncthreads();
-    }
-    // strips above it, and the first `left` of those equal to it
+    };
     if (tid == 0) n_strips = n_keys = 0;
     __syncthreads();
-    int equal = 0;
-    for (int i0 = 0; i0 < strips; i0 += kTopThreads) {
-        const int i = i0 + tid;
-        const unsigned o = i < strips ? ordered(part[(long)i * sl.rows + row].x) : 0;
-        const bool is = i < strips && o == prefix;
-        const unsigned long long mask = __ballot(is);
-        if (lane == 0) wsum[wave] = __popcll(mask);
-        __syncthreads();
-        int place = equal + __popcll(mask & ((1ull << lane) - 1));
-        for (int w = 0; w < kTopThreads / 64; ++w) {
-            if (w < wave) place += wsum[w];
-            equal += wsum[w];
+    unsigned floor_ = 0;
+    const bool all = k >= strips;
+    if (!all) {
+        // strips above the k-th largest maximum, and the first of those equal to it
+        int left;
+        const bool held = strips <= kTopThreads * kTopHeld;
+        unsigned mine[kTopHeld];
+#pragma unroll
+        for (int u = 0; u < kTopHeld; ++u) {
+            const int i = tid + u * kTopThreads;
+            mine[u] = held && i < strips ? ordered(part[(long)i * sl.rows + row].x) : 0;
         }
-        if (i < strips && (o > prefix || (is && place < left))) {
-            const int at = atomicAdd(&n_strips, 1);
-            if (at < kHeadMaxTop) list[at] = i;
+        auto maximum = [&](int i) {
+            if (!held) return ordered(part[(long)i * sl.rows + row].x);
+            const int at = i / kTopThreads;
+            unsigned o = mine[0];
+#pragma unroll
+            for (int u = 1; u < kTopHeld; ++u) o = at == u ? mine[u] : o;
+            return o;
+        };
+        nth(strips, k, maximum, &floor_, &left);
+        int equal = 0;
+        for (int i0 = 0; i0 < strips; i0 += kTopThreads) {
+            const int i = i0 + tid;
+            const unsigned o = i < strips ? maximum(i) : 0;
+            const bool is = i < strips && o == floor_;
+            const unsigned long long mask = __ballot(is);
+            if (lane == 0) wsum[wave] = __popcll(mask);
+            __syncthreads();
+            int place = equal + __popcll(mask & ((1ull << lane) - 1));
+            for (int w = 0; w < kTopThreads / 64; ++w) {
+                if (w < wave) place += wsum[w];
+                equal += wsum[w];
+            }
+            if (i < strips && (o > floor_ || (is && place < left))) {
+                const int at = atomicAdd(&n_strips, 1);
+                if (at < kHeadMaxTop) list[at] = i;
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
     // their entries
-    const int strips_here = n_strips < want ? n_strips : want;
-    const unsigned floor_ = k <= strips ? prefix : 0u;
-    for (int i = wave; i < strips_here; i += kTopThreads / 64) {
-        const int v = list[i] * kStrip + lane;
-        if (v < sl.vocab) {
-            const float a = z[sl.at(row, v)];
-            if (ordered(a) >= floor_) keys[atomicAdd(&n_keys, 1)] = entry_key(a, v);  // (at most 64 of each of k strips)
+    const int strips_here = all ? strips : n_strips < k ? n_strips : k;
+    auto entry = [&](int i, int *v) {                                                // i: place among the strips' columns; 0: outside the vocabulary
+        *v = (all ? i >> 6 : list[i >> 6]) * kStrip + (i & 63);
+        return *v < sl.vocab ? ordered(z[sl.at(row, *v)]) : 0u;
+    };
+    auto collect = [&](auto wanted) __attribute__((always_inline)) {
+        for (int i0 = tid; i0 < strips_here * kStrip; i0 += kTopThreads) {
+            int v;
+            const unsigned o = entry(i0, &v);
+            const bool in = v < sl.vocab && wanted(o, v);
+            const unsigned long long mask = __ballot(in);
+            int base = 0;
+            if (lane == 0 && mask) base = atomicAdd(&n_keys, __popcll(mask));
+            base = __shfl(base, 0, 64) + __popcll(mask & ((1ull << lane) - 1));
+            if (in && base < kTopKeys) keys[base] = (unsigned long long)o << 32 | (0xffffffffu - (unsigned)v);
         }
+        __syncthreads();
+    };
+    collect([&](unsigned o, int) { return o >= floor_; });
+    int have = n_keys;
+    if (have > kTopKeys) {                                                           // equal or nearly equal values: the k-th largest itself, and of those equal to it the first
+        unsigned bits, place;
+        int equal, last;
+        auto value = [&](int i) { int v; return entry(i, &v); };
+        __syncthreads();
+        nth(strips_here * kStrip, k, value, &bits, &equal);
+        nth(strips_here * kStrip, equal, [&](int i) { int v; const unsigned o = entry(i, &v); return o == bits && v < sl.vocab ? 0xffffffffu - (unsigned)v : 0u; }, &place, &last);
+        if (tid == 0) n_keys = 0;
+        __syncthreads();
+        collect([&](unsigned o, int v) { return o > bits || (o == bits && 0xffffffffu - (unsigned)v >= place); });
+        have = n_keys < kTopKeys ? n_keys : kTopKeys;
     }
-    __syncthreads();
-    const int have = n_keys;
+    // many more than k (a small vocabulary): those above the k-th largest value, and those equal to it, to the front
+    if (have > 4 * k && have > 128) {
+        unsigned bits;
+        int equal;
+        nth(have, k, [&](int i) { return (unsigned)(keys[i] >> 32); }, &bits, &equal);
+        if (tid == 0) n_keys = 0;
+        for (int i0 = 0; i0 < have; i0 += kTopThreads) {                             // (what moves goes to a place that has been read)
+            const unsigned long long key = i0 + tid < have ? keys[i0 + tid] : 0;
+            __syncthreads();
+            if (i0 + tid < have && (unsigned)(key >> 32) >= bits) keys[atomicAdd(&n_keys, 1)] = key;
+            __syncthreads();
+        }
+        have = n_keys;
+    }
     int n = 2;
     while (n < have) n <<= 1;
     for (int i = have + tid; i < n; i += kTopThreads) keys[i] = 0;
@@ -677,7 +837,7 @@ ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int ro
         float2 *part = p.part + (size_t)(v0 / kStrip) * p.rows;
         if (!p.fast) MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, w, d, (float *)p.z + slab, p.cols, 1, 0, nullptr, nullptr, 0, 0, 1, s));
         else if (use == HEAD_TOP) MS_TRY(head_gemm_logits(rows, cw, d, h, w, it2, (float *)p.z + slab, p.cols, part, p.rows, s));
-        else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
+        else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, v0, p.z_label, it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
     }
     if (p.fast) return MS_OK;
     ProfScope ps(9, 4.0 * rows * V, s);
@@ -686,11 +846,11 @@ ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int ro
     return MS_OK;
 }
 
-ms_status combine(const HeadPlan &p, int rows, float unit, const float *ref, float it2, float2 *stat, float *logp, float *lse, const int *count, hipStream_t s) {
+ms_status combine(const HeadPlan &p, int rows, float unit, const float2 *ref, float it2, float2 *stat, float *lse, const After &after, const int *count, hipStream_t s) {
     int per = 1;
     while (per < 16 && per < rows) per <<= 1;
     ProfScope ps(9, 8.0 * rows * p.strips, s);
-    head_combine_kernel<<<ms_cdiv(rows, per), per * 64, 0, s>>>(p.rows, rows, per, p.strips, p.part, unit, ref, p.token, count, p.z_sel, it2, stat, logp, lse);
+    head_combine_kernel<<<ms_cdiv(rows, per), per * 64, 0, s>>>(p.rows, rows, per, p.strips, p.part, unit, ref, p.token, count, p.z_sel, it2, stat, lse, after);
     MS_LAUNCH_CHECK();
     return MS_OK;
 }
@@ -706,29 +866,36 @@ struct HeadCall {
     hipStream_t s;
 };
 
-// Rows, their logits, sums over the vocabulary.  key / sel: per token of the block (labels, or the entries' keys and ids).  logp: labels only.
-ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int limit, const int *sel, float *logp) {
+// Rows, their logits, sums over the vocabulary, and what follows.  key / sel: per token of the block (labels, or the entries' keys and ids); out0, out1: zeroed for the
+// tokens that are left out
+ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int limit, const int *sel, float *out0, float *out1, const After &after) {
     const ms_head_config *c = a.c;
     const HeadPlan &p = a.p;
-    const int d = c->hidden;
+    const int d = c->hidden, k = p.fast || after.what ? a.k : 0;
     const float it2 = kLog2e / c->temperature;
     const char *h = (const char *)a.h + (size_t)t0 * d * ms_dtype_size(c->dtype);
     {
         ProfScope ps(11, 0, a.s);
-        head_rows_kernel<<<1, 1024, 0, a.s>>>(n, key, limit, p.fast, p.slot, p.token, p.count);
+        head_rows_kernel<<<1, 1024, 0, a.s>>>(n, key, limit, p.fast, p.slot, p.token, p.count, out0, out1);
     }
     MS_LAUNCH_CHECK();
     {
         ProfScope ps(9, 0, a.s);
-#define GO(T, W) head_pick_kernel<T, W><<<n, 64 * W, 0, a.s>>>(d, a.k, (const T *)h, (const T *)c->w_dev, p.token, p.count, sel, it2, (T *)p.h, p.z_sel, p.ref)
-        if (c->dtype == MS_BF16) { if (a.k > 4) GO(bf16_t, 4); else GO(bf16_t, 1); }
-        else if (a.k > 4) GO(float, 4);
-        else GO(float, 1);
+#define GO(T, W) head_pick_kernel<T, W><<<n, 64 * W, 0, a.s>>>(d, k, (const T *)h, (const T *)c->w_dev, p.token, p.count, sel, it2, (T *)p.h, p.z_sel, p.ref)
+        if (c->dtype == MS_F32) GO(float, 1);
+        else if (k > 16) GO(bf16_t, 8);
+        else if (k > 4) GO(bf16_t, 4);
+        else GO(bf16_t, 1);
 #undef GO
     }
     MS_LAUNCH_CHECK();
     MS_TRY(logits(c, p, a.use, n, p.h, a.s));
-    return combine(p, n, p.fast ? 1.f : it2, p.fast ? p.ref : nullptr, it2, p.stat, logp, nullptr, p.count, a.s);
+    if (!p.fast) {
+        const long total = (long)n * a.k;
+        head_gather_kernel<<<ms_cdiv(total, 256), 256, 0, a.s>>>(Slabs{p.rows, p.cols, c->vocab}, total, a.k, p.token, sel, (const float *)p.z, after.what ? p.z_label : p.z_sel);
+        MS_LAUNCH_CHECK();
+    }
+    return combine(p, n, p.fast ? 1.f : it2, p.fast ? p.ref : nullptr, it2, p.stat, nullptr, after, p.count, a.s);
 }
 
 // scale and rho are there: gradients of the block's hidden states and of the lm_head
@@ -741,7 +908,7 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
     if (p.fast) {
         const Slabs sl = {p.rows, p.cols, V};
         ProfScope ps(10, 4.0 * n * d, a.s);
-        head_apply_kernel<<<n, 256, 0, a.s>>>(sl, d, a.k, p.strips, p.part, p.token, p.count, sel, p.stat, p.scale, p.rho, (bf16_t *)p.z, (bf16_t *)p.h, p.ref, p.fixes, p.fix_id, p.fix_rest,
+        head_apply_kernel<<<n, 256, 0, a.s>>>(sl, d, a.k, p.strips, p.part, p.token, p.count, sel, p.stat, p.scale, p.rho, (bf16_t *)p.z, (bf16_t *)p.h, p.factor, p.fixes, p.fix_id, p.fix_rest,
                                               (bf16_t *)p.fix);
     }
     MS_LAUNCH_CHECK();
@@ -768,7 +935,7 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
     if (p.fast && a.d_w) {
         const int rows = n * p.fixes;
         if (rows <= kHeadScan) {
-            head_fix_kernel<<<dim3(rows, ms_cdiv(d, 512)), 64, 0, a.s>>>(rows, d, p.fix_id, (const bf16_t *)p.fix, (float *)a.d_w);
+            head_fix_kernel<<<dim3(ms_cdiv(rows, kFixWaves), ms_cdiv(d, 512)), 64 * kFixWaves, 0, a.s>>>(rows, d, p.fix_id, (const bf16_t *)p.fix, (float *)a.d_w);
             MS_LAUNCH_CHECK();
         } else {
             MS_TRY(ms_k_embedding_sorted_backward(dt, rows, d, V, 1.f, p.fix_id, p.fix, (float *)a.d_w, p.fix_scratch, p.fix_scratch_bytes, a.s));
@@ -780,7 +947,7 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
     ProfScope ps(11, (4.0 + es) * total, a.s);
     const long part_ld = (long)n * d;
     if (dt == MS_F32) head_d_h_kernel<float><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, 1, part_ld, p.slot, p.d_h, nullptr, 0, nullptr, nullptr, nullptr, (float *)out);
-    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.parts, part_ld, p.slot, p.d_h, p.fast ? p.ref : nullptr, p.fixes, p.fix_id, p.fix_rest, (const bf16_t *)c->w_dev, (bf16_t *)out);
+    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.parts, part_ld, p.slot, p.d_h, p.fast ? p.factor : nullptr, p.fixes, p.fix_id, p.fix_rest, (const bf16_t *)c->w_dev, (bf16_t *)out);
     MS_LAUNCH_CHECK();
     return MS_OK;
 }
@@ -827,8 +994,8 @@ extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const voi
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
         MS_TRY(logits(c, p, HEAD_TOP, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
         const float it2 = kLog2e / c->temperature;
-        MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, nullptr, lse + t0, nullptr, a.s));
-        head_top_kernel<<<nb, kTopThreads, 0, a.s>>>(Slabs{p.rows, p.cols, c->vocab}, p.strips, k, (const float *)p.z, p.part, values + (long)t0 * k, ids + (long)t0 * k);
+        MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, lse + t0, After{}, nullptr, a.s));
+        head_top_kernel<<<ms_cdiv(nb, 8) * 8, kTopThreads, 0, a.s>>>(Slabs{p.rows, p.cols, c->vocab}, nb, p.strips, k, (const float *)p.z, p.part, values + (long)t0 * k, ids + (long)t0 * k);
         MS_LAUNCH_CHECK();
     }
     return MS_OK;
@@ -852,7 +1019,7 @@ extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, i
         head_entries_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, c->vocab, inv_t, top_ids + (long)t0 * k, top_logits + (long)t0 * k, lse_teacher ? lse_teacher + t0 : nullptr,
                                                              p.ids, p.log_p, p.mass, p.key);
         MS_LAUNCH_CHECK();
-        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr));
+        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr, nullptr, After{}));
         head_entry_rows_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, p.slot, p.ids, p.log_p, p.mass, p.z_sel, p.stat, p.fast ? p.ref : nullptr, it2, c->loss_scale * inv_t, kl + t0,
                                                                 back ? p.scale : nullptr, back ? p.rho : nullptr);
         MS_LAUNCH_CHECK();
@@ -873,9 +1040,7 @@ static ms_status token_logprobs(const char *what, const ms_head_config *c, int n
     for (int t0 = 0; t0 < n; t0 += p.rows) {
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
         float *lp = logp ? logp + t0 : p.logp;
-        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp));
-        head_given_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, label_rows(a), back ? d_logp + t0 : nullptr, lp);
-        MS_LAUNCH_CHECK();
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, nullptr, After{back ? AFTER_GIVEN : AFTER_LOGP, 1.0 / c->temperature, p.z_label, lp, back ? d_logp + t0 : nullptr, label_rows(a), {}}));
         if (back) MS_TRY(rows_backward(a, t0, nb, labels + t0));
     }
     return MS_OK;
@@ -907,11 +1072,9 @@ extern "C" ms_status ms_policy_loss_forward_backward(const ms_head_config *c, co
     for (int t0 = 0; t0 < n; t0 += p.rows) {
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
         float *lp = logp ? logp + t0 : p.logp;
-        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp));
-        const PolicyArgs pa = {old_logp + t0, pc->kl_coef > 0.f ? ref_logp + t0 : nullptr, advantages + t0, weights ? weights + t0 : nullptr, pc->clip_low, pc->clip_high, pc->kl_coef,
-                               c->loss_scale};
-        head_policy_kernel<<<ms_cdiv(nb, 256), 256, 0, a.s>>>(nb, label_rows(a), pa, lp, terms + t0);
-        MS_LAUNCH_CHECK();
+        const PolicyArgs pa = {old_logp + t0, pc->kl_coef > 0.f ? ref_logp + t0 : nullptr, advantages + t0, weights ? weights + t0 : nullptr, terms + t0, pc->clip_low, pc->clip_high,
+                               pc->kl_coef, c->loss_scale};
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, terms + t0, After{AFTER_POLICY, 1.0 / c->temperature, p.z_label, lp, nullptr, label_rows(a), pa}));
         if (d_h || d_w) MS_TRY(rows_backward(a, t0, nb, labels + t0));
     }
     return total_loss(terms, n, c->loss_scale, loss, a.s);
@@ -942,7 +1105,7 @@ extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c
     MS_TRY(begin(&a, "preference_loss", c, n, 0, use_of(d_h, d_w), pairs, h, d_h, d_w, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     float *lp = logp ? logp : p.logp;
-    MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp));
+    MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp, nullptr, After{AFTER_LOGP, 1.0 / c->temperature, p.z_label, lp, nullptr, label_rows(a), {}}));
     head_pairs_kernel<<<pairs, 256, 0, a.s>>>(batch->cu_seqlens_dev, label_rows(a), ref_logp, pc->beta, pc->label_smoothing, c->loss_scale, lp, margin ? margin : p.margin, p.per_token);
     MS_LAUNCH_CHECK();
     if (d_h || d_w) MS_TRY(rows_backward(a, 0, n, labels));

@@ -4,9 +4,11 @@
 #include "head_choice.h"
 
 // z = h w^T for `rows` rows (or *count of them, if that is given and less) and cw of the vocabulary's columns, d % 64 == 0; part [strips][ld] as the epilogues
-// EPI_EXP and EPI_LOGITS (gemm_bf16.h) write it.  exp: c = 2^(it2 z - ref), bf16, zeros up to the next multiple of 64 columns (c null: sums only); logits: c = z, fp32.
-ms_status head_gemm_exp(int rows, int cw, int d, const void *h, const void *w, const float *ref, float it2, void *c, long ldc, float2 *part, long ld, const int *count,
-                        hipStream_t s);
+// EPI_EXP and EPI_LOGITS (gemm_bf16.h) write it.  exp: ref = (reference, label) of each row,
+// c = 2^(it2 z - reference), bf16, zeros up to the next multiple of 64 columns (c null: sums only), z_label the rows' logits of their labels (columns from v0 on; null: no row has one);
+// logits: c = z, fp32.
+ms_status head_gemm_exp(int rows, int cw, int d, const void *h, const void *w, const float2 *ref, int v0, float *z_label, float it2, void *c, long ldc, float2 *part, long ld,
+                        const int *count, hipStream_t s);
 ms_status head_gemm_logits(int rows, int cw, int d, const void *h, const void *w, float it2, float *c, long ldc, float2 *part, long ld, hipStream_t s);
 
 // d_h (fp32) = e w and d_w [cw, d] (fp32) += e^T x, e [rows, cw] with rows ld apart and zeros up to the next multiple of 64 columns; either may be null.  d_h comes in

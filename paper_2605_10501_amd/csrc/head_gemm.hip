@@ -60,7 +60,7 @@ GemmParams product(int M, int N, int K, const void *A, long lda, const void *B, 
 }
 
 template <int EPI> ms_status launch_rows(GemmParams &p, double out_bytes, const int *count, hipStream_t s) {
-    const int tile = ms_choose_tile(p.M, p.N, p.k_tiles_per_split, out_bytes, 0, true);
+    const int tile = count ? head_logits_tile(p.M, p.N, p.k_tiles_per_split, out_bytes) : ms_choose_tile(p.M, p.N, p.k_tiles_per_split, out_bytes, 0, true);
     const MsTile &t = kTiles[tile];
     p.tiles_m = ms_cdiv(p.M, t.bm);
     p.tiles_n = ms_cdiv(p.N, t.bn);
@@ -83,10 +83,10 @@ template <int EPI> ms_status launch_rows(GemmParams &p, double out_bytes, const 
 
 }  // namespace
 
-ms_status head_gemm_exp(int rows, int cw, int d, const void *h, const void *w, const float *ref, float it2, void *c, long ldc, float2 *part, long ld, const int *count,
-                        hipStream_t s) {
+ms_status head_gemm_exp(int rows, int cw, int d, const void *h, const void *w, const float2 *ref, int v0, float *z_label, float it2, void *c, long ldc, float2 *part, long ld,
+                        const int *count, hipStream_t s) {
     GemmParams p = product(rows, cw, d, h, d, w, d, c, ldc, 0, 0);
-    p.kd_stats = const_cast<float *>(ref); p.kd_part = (float *)part; p.kd_ldz = ld; p.kd_inv_t = it2;
+    p.kd_stats = (float *)const_cast<float2 *>(ref); p.kd_part = (float *)part; p.kd_ldz = ld; p.kd_inv_t = it2; p.sg_f = v0; p.sg_gu = z_label;
     return launch_rows<EPI_EXP>(p, c ? 4 : 2, count, s);
 }
 

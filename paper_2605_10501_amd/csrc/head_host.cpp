@@ -43,11 +43,12 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     p.token = a.take<int>(r * 4);
     p.count = a.take<int>(4);
     p.h = a.take<void>(r * d * es);
-    p.ref = a.take<float>(r * 4);
+    p.ref = a.take<float2>(r * 8);
     p.stat = a.take<float2>(r * 8);
     p.part = a.take<float2>(r * p.strips * 8);
     if (use != HEAD_TOP) {
         p.z_sel = a.take<float>(r * (k ? k : 1) * 4);
+        p.z_label = a.take<float>(r * 4);
         p.logp = a.take<float>(r * 4);
         if (k) {
             p.log_p = a.take<float>(r * k * 4);
@@ -61,6 +62,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     if (use == HEAD_BACKWARD) {
         p.rho = a.take<float>(r * (k ? k : 1) * 4);
         p.scale = a.take<float>(r * 4);
+        p.factor = a.take<float>(r * 4);
         p.parts = 1;
         if (p.fast) {
             p.choice = head_choose(p.rows, V < p.cols ? V : p.cols, d, true, true);
