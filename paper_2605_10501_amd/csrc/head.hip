@@ -89,10 +89,10 @@ __global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int voc
     }
 }
 
-// Rows of a block: row t for token t (of whose outputs out0, out1 the left-out ones are 0), or, with `compact`, the tokens that count (key in [0, limit)) in their order, without gaps.
-// One workgroup: a block has at most some 10^5 tokens, of which it reads four bytes.
-__global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__restrict__ key, int limit, int compact, int *__restrict__ slot,
-                                                         int *__restrict__ token, int *__restrict__ count, float *__restrict__ out0, float *__restrict__ out1) {
+// Rows of a block: the tokens that count (key in [0, limit)) in their order, without gaps; out0, out1 of the others are 0.  One workgroup: a block has at most
+// some 10^5 tokens, of which it reads four bytes.
+__global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__restrict__ key, int limit, int *__restrict__ slot, int *__restrict__ token, int *__restrict__ count,
+                                                         float *__restrict__ out0, float *__restrict__ out1) {
     __shared__ int sm[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int base = 0;
@@ -102,13 +102,6 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__res
         if (t < n && !in) {
             if (out0) out0[t] = 0.f;
             if (out1) out1[t] = 0.f;
-        }
-        if (!compact) {
-            if (t < n) {
-                slot[t] = in ? t : -1;
-                token[t] = in ? t : -1;
-            }
-            continue;
         }
         const unsigned long long mask = __ballot(in);
         if (lane == 0) sm[wave] = __popcll(mask);
@@ -124,13 +117,48 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__res
         base += all;
         __syncthreads();
     }
-    if (threadIdx.x == 0) *count = compact ? base : n;
+    if (threadIdx.x == 0) *count = base;
+}
+
+// Where logits are stored, row t is token t: hidden states as they are, or zeros for a token that is left out; a label's logit (labels != null) as a dot product of its
+// own.  One wave per row.
+template <class T>
+__global__ __launch_bounds__(256) void head_take_kernel(int n, int d, const int *__restrict__ key, int limit, const int *__restrict__ labels, const T *__restrict__ h, const T *__restrict__ w,
+                                                        int *__restrict__ slot, int *__restrict__ token, float *__restrict__ out0, float *__restrict__ out1, T *__restrict__ out,
+                                                        float *__restrict__ z_sel) {
+    constexpr int N = Vec16<T>::N;
+    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= n) return;
+    const int at = key[row];
+    const bool in = at >= 0 && at < limit;
+    if (lane == 0) {
+        slot[row] = token[row] = in ? row : -1;
+        if (out0 && !in) out0[row] = 0.f;
+        if (out1 && !in) out1[row] = 0.f;
+    }
+    const T *hr = h + (long)row * d, *wr = labels && in ? w + (long)at * d : nullptr;
+    float acc = 0.f;
+    for (int i = lane * N; i < d; i += 64 * N) {
+        Vec16<T> a;
+#pragma unroll
+        for (int e = 0; e < N; ++e) a.v[e] = from_f32<T>(0.f);
+        if (in) a = ldv(hr + i);
+        stv(out + (long)row * d + i, a);
+        if (wr) {
+            const Vec16<T> b = ldv(wr + i);
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc = __builtin_fmaf(to_f32(a.v[e]), to_f32(b.v[e]), acc);
+        }
+    }
+    if (!wr) return;
+    acc = wave_sum(acc);
+    if (lane == 0) z_sel[row] = acc;
 }
 
 // ------------------------------------------------------------------ rows and their selected logits
 // Copies the hidden states of the rows together, and takes the logits of each row's k selected ids (h rows . w rows, fp32); the reference of the
 // row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.
-// W waves a row: one for a label, four or eight for the teacher's entries, four ids at a time.  Rows that no token has (token -1) are zeros.
+// W waves a row: one for a label, four or eight for the teacher's entries, four ids at a time.
 template <class T, int W>
 __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T *__restrict__ h, const T *__restrict__ w, const int *__restrict__ token,
                                                            const int *__restrict__ count, const int *__restrict__ sel, float it2, T *__restrict__ out,
@@ -140,16 +168,8 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T
     if (row >= *count) return;
     const int t = token[row], lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr int N = Vec16<T>::N;
-    if (t < 0) {
-        Vec16<T> zero;
-#pragma unroll
-        for (int e = 0; e < N; ++e) zero.v[e] = from_f32<T>(0.f);
-        for (int i = threadIdx.x * N; i < d; i += 64 * W * N) stv(out + (long)row * d + i, zero);
-        return;
-    }
     const T *hr = h + (long)t * d;
     for (int i = threadIdx.x * N; i < d; i += 64 * W * N) stv(out + (long)row * d + i, ldv(hr + i));
-    if (k == 0) return;                                                           // (stored logits have them)
     float best = -INFINITY;
     for (int j0 = wave * 4; j0 < k; j0 += 4 * W) {
         const T *wr[4];
@@ -184,14 +204,6 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T
         for (int i = 1; i < W; ++i) best = fmaxf(best, sm[i]);
         ref[row] = make_float2(rintf(best * it2), __int_as_float(k == 1 ? sel[t] : -1));
     }
-}
-
-// Stored logits at the selected ids
-__global__ __launch_bounds__(256) void head_gather_kernel(Slabs sl, long total, int k, const int *__restrict__ token, const int *__restrict__ sel, const float *__restrict__ z, float *__restrict__ z_sel) {
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const int row = (int)(i / k), t = token[row], v = t < 0 ? -1 : sel[(long)t * k + (i - (long)row * k)];
-    if (v >= 0) z_sel[i] = z[sl.at(row, v)];
 }
 
 // ------------------------------------------------------------------ sums over the vocabulary
@@ -252,6 +264,18 @@ struct After {
     PolicyArgs policy;
 };
 
+// A row's log-probability and what follows.  x = (x of the label) - (reference of the sum s), in_sum = what the sum has for the label.
+// The label's logit is a dot product of its own (64 partial sums), nearer than the matrix product's, whose error would be there in full where the label is unlikely; in the
+// sum it takes the place of the matrix product's, so that they go together where it is likely.  In 64 bits: logarithms of 15 summed over a sequence, and their differences.
+__device__ __forceinline__ double x_label(const After &a, float z) { return (double)z * a.inv_t * kLog2e64; }
+__device__ __forceinline__ float label_after(const After &a, int t, int row, double x, float s, float in_sum) {
+    const float l = (float)fmin(0.0, kLn264 * x - log(fmax((double)s - (double)in_sum, 0.0) + exp2(x)));
+    a.logp[t] = l;
+    if (a.what == AFTER_POLICY) a.rows.set(row, policy_term(a.policy, t, l), l);
+    else if (a.what == AFTER_GIVEN) a.rows.set(row, a.d_logp[t], l);
+    return l;
+}
+
 // ------------------------------------------------------------------ sums over the vocabulary, joined
 // Behind the vocabulary: sum of the strips' sums at a common reference.  part holds (offset, sum) of each strip [strips][ld]: stored logits' offsets are logits
 // (`unit` of x each), those of exponentials (`ref` given) count in x on top of the row's reference.  A row's strips are shared by 64 threads whatever the number
@@ -293,16 +317,8 @@ __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, in
     const float l2 = __log2f(s);
     if (lse) lse[row] = kLn2 * (m * unit + l2);
     if (after.what == AFTER_NOTHING) return;
-    const int t = token[row];
-    if (t < 0) return;
-    // The label's logit is a dot product of its own (64 partial sums), nearer than the matrix product's, whose error would be there in full where the label is unlikely; in the
-    // sum it takes the place of the matrix product's, so that they go together where it is likely.  In 64 bits: logarithms of 15 summed over a sequence, and their differences.
-    const double x = (double)z_sel[row] * after.inv_t * kLog2e64, base = ref ? (double)ref[row].x + m : (double)m * after.inv_t * kLog2e64;
-    const float in_sum = __builtin_amdgcn_exp2f(ref ? __builtin_fmaf(after.z_label[row], it2, -ref[row].x) - m : (after.z_label[row] - m) * it2);
-    const float l = (float)fmin(0.0, kLn264 * (x - base) - log(fmax((double)s - (double)in_sum, 0.0) + exp2(x - base)));
-    after.logp[t] = l;
-    if (after.what == AFTER_POLICY) after.rows.set(row, policy_term(after.policy, t, l), l);
-    else if (after.what == AFTER_GIVEN) after.rows.set(row, after.d_logp[t], l);
+    label_after(after, token[row], row, x_label(after, z_sel[row]) - (ref ? (double)ref[row].x + m : (double)m * after.inv_t * kLog2e64), s,
+                __builtin_amdgcn_exp2f(ref ? __builtin_fmaf(after.z_label[row], it2, -ref[row].x) - m : (after.z_label[row] - m) * it2));
 }
 
 // One workgroup per pair: margin, loss, and the gradient of every token of its two sequences.  Sums in 64 bits: differences of
@@ -362,12 +378,12 @@ __global__ __launch_bounds__(256) void head_entry_rows_kernel(int n, int k, cons
         return;
     }
     const float2 st = stat[row];
-    const float base = ref ? ref[row].x : 0.f, l2 = __log2f(st.x), inv_mass = 1.f / mass[t];
+    const float base = ref[row].x + st.y, l2 = __log2f(st.x), inv_mass = 1.f / mass[t];
     float sum = 0.f;
     for (int j = lane; j < k; j += 64) {
         if (ids[t * k + j] < 0) continue;
         const float lp = log_p[t * k + j], p = expf(lp);
-        const float zj = z_sel[(long)row * k + j], lq = kLn2 * ((ref ? __builtin_fmaf(zj, it2, -base) - st.y : (zj - st.y) * it2) - l2);
+        const float zj = z_sel[(long)row * k + j], lq = kLn2 * (__builtin_fmaf(zj, it2, -base) - l2);
         if (!(p == 0.f)) sum += p * (lp - lq);
         if (rho) rho[(long)row * k + j] = expf(lq) - p * inv_mass;
     }
@@ -378,13 +394,124 @@ __global__ __launch_bounds__(256) void head_entry_rows_kernel(int n, int k, cons
     }
 }
 
-// one workgroup: the loss from its terms, in an order that only their number fixes
-__global__ __launch_bounds__(1024) void head_loss_kernel(const float *__restrict__ terms, int n, float loss_scale, float *__restrict__ loss) {
-    __shared__ float sm[16];
+// One workgroup of 256: the loss from its terms, in an order that only their number fixes
+struct LossTerms {
+    const float *terms;
+    int n;
+    float scale;
+    float *loss;                                                                   // null: not here
+};
+__device__ __forceinline__ void sum_loss(const LossTerms &a) {
+    __shared__ float sm[4];
     float acc = 0.f;
-    for (int i = threadIdx.x; i < n; i += 1024) acc += terms[i];
+    for (int i = threadIdx.x; i < a.n; i += 256 * 8) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i + u * 256 < a.n ? a.terms[i + u * 256] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) acc += v[u];
+    }
     acc = block_sum(acc, sm);
-    if (threadIdx.x == 0) *loss = loss_scale * acc;
+    if (threadIdx.x == 0) *a.loss = a.scale * acc;
+}
+__global__ __launch_bounds__(256) void head_loss_kernel(LossTerms a) { sum_loss(a); }
+
+// ------------------------------------------------------------------ rows of stored logits
+struct Entries {
+    const float *log_p, *mass;
+    float *kl, coef;                                                               // kl by token; dz = coef (q sum p - p)
+};
+// Everything of a row once its logits are stored: sum of exponentials, log-probabilities of the selected ids, the loss's term, and, with `dz`, the gradient of the logits in their
+// place (fp32).  G threads a row: a wave where a row is a few KB, a workgroup above.
+template <int G>
+__global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, float it2, const int *__restrict__ token, const int *__restrict__ sel, float *z, const float *__restrict__ z_sel, After after,
+                                                       Entries en, float2 *__restrict__ stat, float *__restrict__ scale, float *__restrict__ rho, int dz) {
+    __shared__ float sm[4], sh_scale;
+    const int g = threadIdx.x & (G - 1), row = G == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (row >= n) return;
+    auto join = [&](float v, auto f, auto across) __attribute__((always_inline)) {
+        v = across(v);
+        if constexpr (G > 64) {
+            if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = f(f(sm[0], sm[1]), f(sm[2], sm[3]));
+            __syncthreads();
+        }
+        return v;
+    };
+    auto sum_of = [&](float v) { return join(v, [](float a, float b) { return a + b; }, [](float a) { return wave_sum(a); }); };
+    auto max_of = [&](float v) { return join(v, [](float a, float b) { return fmaxf(a, b); }, [](float a) { return wave_max(a); }); };
+    auto each = [&](auto f) __attribute__((always_inline)) {                        // the row, four columns at a time
+        for (int v0 = 0; v0 < sl.vocab; v0 += sl.cols) {
+            float4 *zr = (float4 *)(z + sl.at(row, v0));
+            const int n4 = (sl.vocab - v0 < sl.cols ? sl.vocab - v0 : sl.cols) >> 2;
+            for (int i = g; i < n4; i += G) f(zr[i]);
+        }
+    };
+    const int t = token[row];
+    if (t < 0) {
+        if (dz) each([](float4 &a) { a = make_float4(0.f, 0.f, 0.f, 0.f); });
+        if (en.kl && g == 0) en.kl[row] = 0.f;
+        return;
+    }
+    float m = -INFINITY, s = 0.f;
+    each([&](float4 &a) { m = fmaxf(fmaxf(m, fmaxf(a.x, a.y)), fmaxf(a.z, a.w)); });
+    m = max_of(m);
+    const float u = m == -INFINITY ? 0.f : m;
+    each([&](float4 &a) {
+        s += __builtin_amdgcn_exp2f((a.x - u) * it2) + __builtin_amdgcn_exp2f((a.y - u) * it2) + __builtin_amdgcn_exp2f((a.z - u) * it2) + __builtin_amdgcn_exp2f((a.w - u) * it2);
+    });
+    s = sum_of(s);
+    if (stat && g == 0) stat[row] = make_float2(s, m);
+    float c = 0.f, r[2] = {0.f, 0.f};                                              // dz = c q, c r[] at the selected ids j = g, g + 64 (k <= 128)
+    int id[2] = {-1, -1};
+    if (after.what != AFTER_NOTHING) {
+        if (g == 0) {
+            id[0] = sel[t];
+            const float l = label_after(after, t, row, x_label(after, z_sel[row]) - (double)m * after.inv_t * kLog2e64, s, __builtin_amdgcn_exp2f((z[sl.at(row, id[0])] - u) * it2));
+            r[0] = expm1f(l);
+            if (dz) c = scale[row];
+        }
+        if (dz) {
+            if constexpr (G == 64) c = __shfl(c, 0, 64);
+            else {
+                if (g == 0) sh_scale = c;
+                __syncthreads();
+                c = sh_scale;
+            }
+        }
+    } else {
+        const float l2 = __log2f(s), mass = en.mass[t], inv_mass = 1.f / mass;
+        c = en.coef * mass;
+        float kl = 0.f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int j = g + 64 * x;
+            if (g >= 64 || j >= k) continue;
+            id[x] = sel[(long)t * k + j];
+            if (id[x] < 0) continue;
+            const float lp = en.log_p[(long)t * k + j], p = expf(lp), lq = kLn2 * ((z[sl.at(row, id[x])] - u) * it2 - l2);
+            if (!(p == 0.f)) kl += p * (lp - lq);
+            r[x] = expf(lq) - p * inv_mass;
+            if (rho) rho[(long)row * k + j] = r[x];
+        }
+        kl = sum_of(kl);
+        if (g == 0) {
+            en.kl[t] = kl;
+            if (scale) scale[row] = c;
+        }
+    }
+    if (!dz) return;
+    const float f = c == 0.f ? 0.f : c / s;
+    if (c == 0.f) each([](float4 &a) { a = make_float4(0.f, 0.f, 0.f, 0.f); });
+    else each([&](float4 &a) {
+        a = make_float4(f * __builtin_amdgcn_exp2f((a.x - u) * it2), f * __builtin_amdgcn_exp2f((a.y - u) * it2), f * __builtin_amdgcn_exp2f((a.z - u) * it2), f * __builtin_amdgcn_exp2f((a.w - u) * it2));
+    });
+    if constexpr (G == 64) __threadfence_block(); else __syncthreads();             // the row's stores come before those at the selected ids
+    if (c == 0.f) return;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (id[x] >= 0) z[sl.at(row, id[x])] = c * r[x];
 }
 
 // ------------------------------------------------------------------ gradients
@@ -494,7 +621,7 @@ __global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k,
 
 // d_w[id] += the rows of `fix` with that id, in their order; n <= kHeadScan of them.  A workgroup takes eight rows and 512 columns: each of its waves looks for the others of one
 // row's id in a copy of the ids in LDS, and the first row of an id sums them all, by itself or, where there are many, with all eight waves (an eighth of the rows each).
-// (A workgroup per row that reads the ids itself: 18 us for 2053 rows of 1024, 41 for 4124; waves by themselves 38 and 26; XX.)
+// (A workgroup per row that reads the ids itself: 18 us for 2053 rows of 1024, 41 for 4124; waves by themselves 38 and 26; now 14 and 22.)
 constexpr int kFixWaves = 8;
 __global__ __launch_bounds__(64 * kFixWaves) void head_fix_kernel(int n, int d, const int *__restrict__ id, const bf16_t *__restrict__ fix, float *__restrict__ d_w) {
     constexpr int kMany = 8, kList = 256;
@@ -613,16 +740,23 @@ __global__ __launch_bounds__(64 * kFixWaves) void head_fix_kernel(int n, int d, 
 // d_h of the block's tokens: a row's sums (in `parts` parts) times its factor, and what the selected ids' lack; zeros for tokens that were left out
 template <class T>
 __global__ __launch_bounds__(256) void head_d_h_kernel(long total, int d, int parts, long part_ld, const int *__restrict__ slot, const float *__restrict__ sums, const float *__restrict__ factor,
-                                                       int fixes, const int *__restrict__ fix_id, const float *__restrict__ fix_rest, const bf16_t *__restrict__ w, T *__restrict__ d_h) {
+                                                       int fixes, const int *__restrict__ fix_id, const float *__restrict__ fix_rest, const bf16_t *__restrict__ w, T *__restrict__ d_h, LossTerms loss) {
+    if (loss.loss && blockIdx.x == gridDim.x - 1) {                                 // (a launch less)
+        sum_loss(loss);
+        return;
+    }
     const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= total) return;
     const int t = (int)(i / d), c = (int)(i - (long)t * d), row = slot[t];
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     const float f = row < 0 ? 0.f : factor ? factor[row] : 1.f;
     if (row >= 0 && f != 0.f) {
-        for (int q = 0; q < parts; ++q) {
-            const float4 a = *(const float4 *)(sums + q * part_ld + (long)row * d + c);
-            v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+        for (int q0 = 0; q0 < parts; q0 += 8) {
+            float4 a[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) a[q] = q0 + q < parts ? *(const float4 *)(sums + (q0 + q) * part_ld + (long)row * d + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) { v.x += a[q].x; v.y += a[q].y; v.z += a[q].z; v.w += a[q].w; }
         }
         v.x *= f; v.y *= f; v.z *= f; v.w *= f;
         for (int q = 0; q < fixes; ++q) {
@@ -673,8 +807,8 @@ __device__ __forceinline__ void sort_keys(unsigned long long *key, int n) {
 // that are not below that maximum, which are few more than k; those sorted.
 constexpr int kTopKeys = 2048;                      // candidates that are sorted in LDS
 constexpr int kTopThreads = 512, kTopHeld = 8;      // strips of a thread whose maxima it keeps in registers (V up to 262144); more are read again in each pass
-__global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int rows, int strips, int k, const float *__restrict__ z, const float2 *__restrict__ part,
-                                                               float *__restrict__ values, int *__restrict__ ids) {
+__global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int rows, int strips, int k, const float *__restrict__ z, const float2 *__restrict__ part, float it2,
+                                                               float *__restrict__ lse, float *__restrict__ values, int *__restrict__ ids) {
     __shared__ unsigned hist[256], sh_prefix;
     __shared__ int sh_want, n_strips, n_keys, wsum[kTopThreads / 64];
     __shared__ int list[kHeadMaxTop];
@@ -726,7 +860,21 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int row
     if (tid == 0) n_strips = n_keys = 0;
     __syncthreads();
     unsigned floor_ = 0;
-    const bool all = k >= strips;
+    const bool all = !part || k >= strips;
+    if (!part) {                                                                    // a small vocabulary: the sum too
+        __shared__ float sm[kTopThreads / 64];
+        float m = -INFINITY, s = 0.f;
+        for (int v = tid; v < sl.vocab; v += kTopThreads) m = fmaxf(m, z[sl.at(row, v)]);
+        m = wave_max(m);
+        if (lane == 0) sm[wave] = m;
+        __syncthreads();
+        for (int w = 0; w < kTopThreads / 64; ++w) m = fmaxf(m, sm[w]);
+        __syncthreads();
+        const float u = m == -INFINITY ? 0.f : m;
+        for (int v = tid; v < sl.vocab; v += kTopThreads) s += __builtin_amdgcn_exp2f((z[sl.at(row, v)] - u) * it2);
+        s = block_sum(s, sm);
+        if (tid == 0) lse[row] = kLn2 * (m * it2 + __log2f(s));
+    }
     if (!all) {
         // strips above the k-th largest maximum, and the first of those equal to it
         int left;
@@ -825,7 +973,7 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int row
 }
 
 // ------------------------------------------------------------------ sequencing
-// Logits of `rows` rows h and the sums of their strips: stored (fp32), or their exponentials at p.ref (fast losses; not stored in a forward pass)
+// Logits of `rows` rows h: stored (fp32), or their exponentials at p.ref (fast losses; not stored in a forward pass); the fast products leave the sums of their strips too
 ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int rows, const void *h, hipStream_t s) {
     const int V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(c->dtype);
@@ -839,10 +987,6 @@ ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int ro
         else if (use == HEAD_TOP) MS_TRY(head_gemm_logits(rows, cw, d, h, w, it2, (float *)p.z + slab, p.cols, part, p.rows, s));
         else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, v0, p.z_label, it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
     }
-    if (p.fast) return MS_OK;
-    ProfScope ps(9, 4.0 * rows * V, s);
-    head_strips_kernel<<<dim3(ms_cdiv(p.strips, 4), rows < 32768 ? rows : 32768), 256, 0, s>>>(Slabs{p.rows, p.cols, V}, rows, p.strips, (const float *)p.z, it2, p.part);
-    MS_LAUNCH_CHECK();
     return MS_OK;
 }
 
@@ -867,39 +1011,63 @@ struct HeadCall {
 };
 
 // Rows, their logits, sums over the vocabulary, and what follows.  key / sel: per token of the block (labels, or the entries' keys and ids); out0, out1: zeroed for the
-// tokens that are left out
-ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int limit, const int *sel, float *out0, float *out1, const After &after) {
+// tokens that are left out.  Labels: after; the teacher's entries: en.  *dz_done: the gradient of stored logits is in their place already.
+ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int limit, const int *sel, float *out0, float *out1, const After &after, const Entries &en, bool dz_here, bool *dz_done) {
     const ms_head_config *c = a.c;
     const HeadPlan &p = a.p;
-    const int d = c->hidden, k = p.fast || after.what ? a.k : 0;
+    const int d = c->hidden, V = c->vocab;
     const float it2 = kLog2e / c->temperature;
     const char *h = (const char *)a.h + (size_t)t0 * d * ms_dtype_size(c->dtype);
+    const bool labels = after.what != AFTER_NOTHING;
+    if (!p.fast) {
+        {
+            ProfScope ps(9, 0, a.s);
+            if (c->dtype == MS_F32) head_take_kernel<float><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, key, limit, labels ? sel : nullptr, (const float *)h, (const float *)c->w_dev, p.slot, p.token, out0, out1, (float *)p.h, p.z_sel);
+            else head_take_kernel<bf16_t><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, key, limit, labels ? sel : nullptr, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.slot, p.token, out0, out1, (bf16_t *)p.h, p.z_sel);
+        }
+        MS_LAUNCH_CHECK();
+        MS_TRY(logits(c, p, a.use, n, p.h, a.s));
+        *dz_done = dz_here && c->dtype == MS_F32 && a.use == HEAD_BACKWARD;
+        const Slabs sl = {p.rows, p.cols, V};
+        float *scale = a.use == HEAD_BACKWARD ? p.scale : nullptr, *rho = a.use == HEAD_BACKWARD ? p.rho : nullptr;
+        ProfScope ps(9, 4.0 * n * V * (*dz_done ? 2 : 1), a.s);
+#define GO(G, rows) head_row_kernel<G><<<rows, 256, 0, a.s>>>(sl, n, a.k, it2, p.token, sel, (float *)p.z, p.z_sel, after, en, p.stat, scale, rho, *dz_done)
+        if (V <= 4096) GO(64, ms_cdiv(n, 4)); else GO(256, n);
+#undef GO
+        MS_LAUNCH_CHECK();
+        return MS_OK;
+    }
     {
         ProfScope ps(11, 0, a.s);
-        head_rows_kernel<<<1, 1024, 0, a.s>>>(n, key, limit, p.fast, p.slot, p.token, p.count, out0, out1);
+        head_rows_kernel<<<1, 1024, 0, a.s>>>(n, key, limit, p.slot, p.token, p.count, out0, out1);
     }
     MS_LAUNCH_CHECK();
     {
         ProfScope ps(9, 0, a.s);
-#define GO(T, W) head_pick_kernel<T, W><<<n, 64 * W, 0, a.s>>>(d, k, (const T *)h, (const T *)c->w_dev, p.token, p.count, sel, it2, (T *)p.h, p.z_sel, p.ref)
-        if (c->dtype == MS_F32) GO(float, 1);
-        else if (k > 16) GO(bf16_t, 8);
-        else if (k > 4) GO(bf16_t, 4);
-        else GO(bf16_t, 1);
+#define GO(W) head_pick_kernel<bf16_t, W><<<n, 64 * W, 0, a.s>>>(d, a.k, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.token, p.count, sel, it2, (bf16_t *)p.h, p.z_sel, p.ref)
+        if (a.k > 16) GO(8);
+        else if (a.k > 4) GO(4);
+        else GO(1);
 #undef GO
     }
     MS_LAUNCH_CHECK();
     MS_TRY(logits(c, p, a.use, n, p.h, a.s));
-    if (!p.fast) {
-        const long total = (long)n * a.k;
-        head_gather_kernel<<<ms_cdiv(total, 256), 256, 0, a.s>>>(Slabs{p.rows, p.cols, c->vocab}, total, a.k, p.token, sel, (const float *)p.z, after.what ? p.z_label : p.z_sel);
-        MS_LAUNCH_CHECK();
-    }
-    return combine(p, n, p.fast ? 1.f : it2, p.fast ? p.ref : nullptr, it2, p.stat, nullptr, after, p.count, a.s);
+    MS_TRY(combine(p, n, 1.f, p.ref, it2, p.stat, nullptr, after, p.count, a.s));
+    if (labels) return MS_OK;
+    const bool back = a.use == HEAD_BACKWARD;
+    head_entry_rows_kernel<<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, a.k, p.slot, p.ids, p.log_p, p.mass, p.z_sel, p.stat, p.ref, it2, en.coef, en.kl, back ? p.scale : nullptr, back ? p.rho : nullptr);
+    MS_LAUNCH_CHECK();
+    return MS_OK;
 }
 
-// scale and rho are there: gradients of the block's hidden states and of the lm_head
-ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
+ms_status total_loss(const LossTerms &a, hipStream_t s) {
+    head_loss_kernel<<<1, 256, 0, s>>>(a);
+    MS_LAUNCH_CHECK();
+    return MS_OK;
+}
+
+// scale and rho are there: gradients of the block's hidden states and of the lm_head; then the loss, if it is asked for here
+ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool dz_done, const LossTerms &loss) {
     const ms_head_config *c = a.c;
     const HeadPlan &p = a.p;
     const int d = c->hidden, V = c->vocab, dt = c->dtype;
@@ -922,14 +1090,16 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
         }
         float *z = (float *)p.z + (size_t)i * p.rows * p.cols, *d_w = a.d_w ? (float *)a.d_w + (size_t)v0 * d : nullptr;
         void *dz = dt == MS_F32 ? (void *)z : p.dz;
-        {
+        if (!dz_done) {
             ProfScope ps(10, (4.0 + es) * n * cw, a.s);
             if (dt == MS_F32) head_dz_kernel<float><<<n, 256, 0, a.s>>>(p.cols, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (float *)dz);
             else head_dz_kernel<bf16_t><<<n, 256, 0, a.s>>>(p.cols, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (bf16_t *)dz);
         }
         MS_LAUNCH_CHECK();
-        if (a.d_h && a.d_w) MS_TRY(ms_k_linear_backward(dt, n, cw, d, dz, p.cols, w, p.h, p.d_h, 1, i > 0, d_w, a.s));
-        else if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, p.d_h, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
+        // (in fp32 the sums are the result: zeros for the tokens that are left out, whose rows of dz are)
+        float *sums = dt == MS_F32 ? (float *)a.d_h + (size_t)t0 * d : p.d_h;
+        if (a.d_h && a.d_w) MS_TRY(ms_k_linear_backward(dt, n, cw, d, dz, p.cols, w, p.h, sums, 1, i > 0, d_w, a.s));
+        else if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, sums, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
         else MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 0, a.s));
     }
     if (p.fast && a.d_w) {
@@ -941,21 +1111,15 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel) {
             MS_TRY(ms_k_embedding_sorted_backward(dt, rows, d, V, 1.f, p.fix_id, p.fix, (float *)a.d_w, p.fix_scratch, p.fix_scratch_bytes, a.s));
         }
     }
-    if (!a.d_h) return MS_OK;
-    char *out = (char *)a.d_h + (size_t)t0 * d * es;
-    const long total = (long)n * d;
-    ProfScope ps(11, (4.0 + es) * total, a.s);
-    const long part_ld = (long)n * d;
-    if (dt == MS_F32) head_d_h_kernel<float><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, 1, part_ld, p.slot, p.d_h, nullptr, 0, nullptr, nullptr, nullptr, (float *)out);
-    else head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024), 256, 0, a.s>>>(total, d, p.parts, part_ld, p.slot, p.d_h, p.fast ? p.factor : nullptr, p.fixes, p.fix_id, p.fix_rest, (const bf16_t *)c->w_dev, (bf16_t *)out);
-    MS_LAUNCH_CHECK();
-    return MS_OK;
-}
-
-ms_status total_loss(const float *terms, int n, float loss_scale, float *loss, hipStream_t s) {
-    head_loss_kernel<<<1, 1024, 0, s>>>(terms, n, loss_scale, loss);
-    MS_LAUNCH_CHECK();
-    return MS_OK;
+    const bool sum_here = a.d_h && dt == MS_BF16 && loss.loss;
+    if (a.d_h && dt == MS_BF16) {
+        const long total = (long)n * d;
+        ProfScope ps(11, (4.0 + es) * total, a.s);
+        head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024) + sum_here, 256, 0, a.s>>>(total, d, p.parts, total, p.slot, p.d_h, p.fast ? p.factor : nullptr, p.fixes, p.fix_id, p.fix_rest, (const bf16_t *)c->w_dev,
+                                                                                  (bf16_t *)a.d_h + (size_t)t0 * d, loss);
+        MS_LAUNCH_CHECK();
+    }
+    return loss.loss && !sum_here ? total_loss(loss, a.s) : MS_OK;
 }
 
 bool aligned(const void *q, int by) { return ((uintptr_t)q & (by - 1)) == 0; }
@@ -978,6 +1142,15 @@ ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, i
 HeadUse use_of(const void *d_h, const void *d_w) { return d_h || d_w ? HEAD_BACKWARD : HEAD_FORWARD; }
 
 LabelRows label_rows(const HeadCall &a) { return LabelRows{a.p.slot, a.p.scale, a.p.rho, -1.f / a.c->temperature}; }
+After after_label(const HeadCall &a, int what, float *logp, const float *d_logp, const PolicyArgs &policy) {
+    return After{what, 1.0 / a.c->temperature, a.p.z_label, logp, d_logp, label_rows(a), policy};
+}
+// Behind rows t0 .. t0 + nb of n: their gradients, and the loss behind the last ones
+ms_status end_of_block(const HeadCall &a, int t0, int nb, int n, const int *sel, bool dz_done, const LossTerms &all) {
+    const LossTerms here = t0 + nb == n ? all : LossTerms{};
+    if (a.d_h || a.d_w) return rows_backward(a, t0, nb, sel, dz_done, here);
+    return here.loss ? total_loss(here, a.s) : MS_OK;
+}
 
 }  // namespace
 
@@ -990,12 +1163,18 @@ extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const voi
     HeadCall a;
     MS_TRY(begin(&a, "top_logits", c, n, k, HEAD_TOP, -1, h, nullptr, nullptr, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
+    const float it2 = kLog2e / c->temperature;
+    const bool whole = !p.fast && c->vocab <= kTopKeys;                            // a row is looked through at once, without sums of strips
     for (int t0 = 0; t0 < n; t0 += p.rows) {
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        const Slabs sl = {p.rows, p.cols, c->vocab};
         MS_TRY(logits(c, p, HEAD_TOP, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
-        const float it2 = kLog2e / c->temperature;
-        MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, lse + t0, After{}, nullptr, a.s));
-        head_top_kernel<<<ms_cdiv(nb, 8) * 8, kTopThreads, 0, a.s>>>(Slabs{p.rows, p.cols, c->vocab}, nb, p.strips, k, (const float *)p.z, p.part, values + (long)t0 * k, ids + (long)t0 * k);
+        if (!p.fast && !whole) {
+            head_strips_kernel<<<dim3(ms_cdiv(p.strips, 4), nb < 32768 ? nb : 32768), 256, 0, a.s>>>(sl, nb, p.strips, (const float *)p.z, it2, p.part);
+            MS_LAUNCH_CHECK();
+        }
+        if (!whole) MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, lse + t0, After{}, nullptr, a.s));
+        head_top_kernel<<<ms_cdiv(nb, 8) * 8, kTopThreads, 0, a.s>>>(sl, nb, p.strips, k, (const float *)p.z, whole ? nullptr : p.part, it2, lse + t0, values + (long)t0 * k, ids + (long)t0 * k);
         MS_LAUNCH_CHECK();
     }
     return MS_OK;
@@ -1011,21 +1190,19 @@ extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, i
     HeadCall a;
     MS_TRY(begin(&a, "topk_kd", c, n, k, use_of(d_h, d_w), -1, h, d_h, d_w, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
-    const bool back = d_h || d_w;
-    const float it2 = kLog2e / c->temperature, inv_t = 1.f / c->temperature;
+    const float inv_t = 1.f / c->temperature;
     float *kl = kl_tok ? kl_tok : p.per_token;
+    const LossTerms all = {kl, n, c->loss_scale, loss};
     for (int t0 = 0; t0 < n; t0 += p.rows) {
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        bool dz_done = false;
         head_entries_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, c->vocab, inv_t, top_ids + (long)t0 * k, top_logits + (long)t0 * k, lse_teacher ? lse_teacher + t0 : nullptr,
                                                              p.ids, p.log_p, p.mass, p.key);
         MS_LAUNCH_CHECK();
-        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr, nullptr, After{}));
-        head_entry_rows_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, p.slot, p.ids, p.log_p, p.mass, p.z_sel, p.stat, p.fast ? p.ref : nullptr, it2, c->loss_scale * inv_t, kl + t0,
-                                                                back ? p.scale : nullptr, back ? p.rho : nullptr);
-        MS_LAUNCH_CHECK();
-        if (back) MS_TRY(rows_backward(a, t0, nb, p.ids));
+        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr, nullptr, After{}, Entries{p.log_p, p.mass, kl + t0, c->loss_scale * inv_t}, true, &dz_done));
+        MS_TRY(end_of_block(a, t0, nb, n, p.ids, dz_done, all));
     }
-    return total_loss(kl, n, c->loss_scale, loss, a.s);
+    return MS_OK;
 }
 
 static ms_status token_logprobs(const char *what, const ms_head_config *c, int n, const void *h, const int32_t *labels, const float *d_logp, float *logp, void *d_h, void *d_w,
@@ -1039,9 +1216,10 @@ static ms_status token_logprobs(const char *what, const ms_head_config *c, int n
     const HeadPlan &p = a.p;
     for (int t0 = 0; t0 < n; t0 += p.rows) {
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        bool dz_done = false;
         float *lp = logp ? logp + t0 : p.logp;
-        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, nullptr, After{back ? AFTER_GIVEN : AFTER_LOGP, 1.0 / c->temperature, p.z_label, lp, back ? d_logp + t0 : nullptr, label_rows(a), {}}));
-        if (back) MS_TRY(rows_backward(a, t0, nb, labels + t0));
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, nullptr, after_label(a, back ? AFTER_GIVEN : AFTER_LOGP, lp, back ? d_logp + t0 : nullptr, {}), Entries{}, true, &dz_done));
+        MS_TRY(end_of_block(a, t0, nb, n, labels + t0, dz_done, LossTerms{}));
     }
     return MS_OK;
 }
@@ -1069,15 +1247,17 @@ extern "C" ms_status ms_policy_loss_forward_backward(const ms_head_config *c, co
     MS_TRY(begin(&a, "policy_loss", c, n, 0, use_of(d_h, d_w), -1, h, d_h, d_w, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     float *terms = loss_tok ? loss_tok : p.per_token;
+    const LossTerms all = {terms, n, c->loss_scale, loss};
     for (int t0 = 0; t0 < n; t0 += p.rows) {
         const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+        bool dz_done = false;
         float *lp = logp ? logp + t0 : p.logp;
         const PolicyArgs pa = {old_logp + t0, pc->kl_coef > 0.f ? ref_logp + t0 : nullptr, advantages + t0, weights ? weights + t0 : nullptr, terms + t0, pc->clip_low, pc->clip_high,
                                pc->kl_coef, c->loss_scale};
-        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, terms + t0, After{AFTER_POLICY, 1.0 / c->temperature, p.z_label, lp, nullptr, label_rows(a), pa}));
-        if (d_h || d_w) MS_TRY(rows_backward(a, t0, nb, labels + t0));
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, terms + t0, after_label(a, AFTER_POLICY, lp, nullptr, pa), Entries{}, true, &dz_done));
+        MS_TRY(end_of_block(a, t0, nb, n, labels + t0, dz_done, all));
     }
-    return total_loss(terms, n, c->loss_scale, loss, a.s);
+    return MS_OK;
 }
 
 extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c, const ms_preference_config *pc, const ms_batch *batch, const void *h, const int32_t *labels,
@@ -1105,9 +1285,9 @@ extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c
     MS_TRY(begin(&a, "preference_loss", c, n, 0, use_of(d_h, d_w), pairs, h, d_h, d_w, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     float *lp = logp ? logp : p.logp;
-    MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp, nullptr, After{AFTER_LOGP, 1.0 / c->temperature, p.z_label, lp, nullptr, label_rows(a), {}}));
+    bool dz_done = false;
+    MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp, nullptr, after_label(a, AFTER_LOGP, lp, nullptr, {}), Entries{}, false, &dz_done));
     head_pairs_kernel<<<pairs, 256, 0, a.s>>>(batch->cu_seqlens_dev, label_rows(a), ref_logp, pc->beta, pc->label_smoothing, c->loss_scale, lp, margin ? margin : p.margin, p.per_token);
     MS_LAUNCH_CHECK();
-    if (d_h || d_w) MS_TRY(rows_backward(a, 0, n, labels));
-    return total_loss(p.per_token, pairs, c->loss_scale, loss, a.s);
+    return end_of_block(a, 0, n, n, labels, dz_done, LossTerms{p.per_token, pairs, c->loss_scale, loss});
 }

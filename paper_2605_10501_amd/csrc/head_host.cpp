@@ -45,7 +45,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     p.h = a.take<void>(r * d * es);
     p.ref = a.take<float2>(r * 8);
     p.stat = a.take<float2>(r * 8);
-    p.part = a.take<float2>(r * p.strips * 8);
+    if (p.fast || use == HEAD_TOP) p.part = a.take<float2>(r * p.strips * 8);
     if (use != HEAD_TOP) {
         p.z_sel = a.take<float>(r * (k ? k : 1) * 4);
         p.z_label = a.take<float>(r * 4);
@@ -77,7 +77,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
                 p.fix_scratch = a.take<void>(p.fix_scratch_bytes);
             }
         }
-        p.d_h = a.take<float>(r * p.parts * d * 4);
+        if (c->dtype == MS_BF16) p.d_h = a.take<float>(r * p.parts * d * 4);
         if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(r * p.cols * 2);
     }
     if (keeps) p.z = a.take<void>((size_t)p.slabs * r * p.cols * ez);
