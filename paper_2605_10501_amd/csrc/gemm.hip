@@ -545,6 +545,8 @@ int set_splits(Bf16Gemm &g, int splits) {
 
 }  // namespace
 
+int gemm_forced_tile() { return forced_tile(); }
+
 extern "C" ms_status ms_k_gemm_config(int32_t tile, int32_t mfma16) {
     bool known = tile == -1 || tile == 0 || tile == kPingPong;
     for (const MsTile &t : kTiles) known = known || tile == t.code;

@@ -345,7 +345,7 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
         static_assert(!TA && !TB && M16, "head epilogues are built for K-contiguous operands and 16-row fragments");
         const int prow = lane >> 4, pcol = (lane & 15) * 4, idx = lane & 15;
         const int colg = n0 + col_base(pcol >> 5) + (pcol & 31), strip = n0 + col_base(0);
-        const bool cok = colg < p.N, stored = colg < (p.N + 63) / 64 * 64;
+        const bool cok = colg < p.N, stored = colg < (p.N + 63) / 64 * 64, full = strip + 64 <= p.N;     // (full: wave-uniform)
         const float it2 = p.kd_inv_t;
         const unsigned lane_c = (unsigned)((prow * p.ldc + colg) * (EPI == EPI_EXP ? 2 : 4));
         const __amdgpu_buffer_rsrc_t rl = make_rsrc(EPI == EPI_EXP ? (const void *)p.kd_stats : p.C, EPI == EPI_EXP ? (long)p.M * 8 : 0);
@@ -374,9 +374,10 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
                 row_of(ps, z);
                 if constexpr (EPI == EPI_EXP) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[k], it2, -ref[ps]));
-                        if (!cok) e[k] = 0.f;
+                    for (int k = 0; k < 4; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[k], it2, -ref[ps]));
+                    if (!full) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) e[k] = cok ? e[k] : 0.f;
                     }
                     w[ps] = pack4(e);
                     off[ps] = 0.f;

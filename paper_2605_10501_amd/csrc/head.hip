@@ -441,11 +441,12 @@ __global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, f
     };
     auto sum_of = [&](float v) { return join(v, [](float a, float b) { return a + b; }, [](float a) { return wave_sum(a); }); };
     auto max_of = [&](float v) { return join(v, [](float a, float b) { return fmaxf(a, b); }, [](float a) { return wave_max(a); }); };
-    auto each = [&](auto f) __attribute__((always_inline)) {                        // the row, four columns at a time
-        for (int v0 = 0; v0 < sl.vocab; v0 += sl.cols) {
-            float4 *zr = (float4 *)(z + sl.at(row, v0));
-            const int n4 = (sl.vocab - v0 < sl.cols ? sl.vocab - v0 : sl.cols) >> 2;
-            for (int i = g; i < n4; i += G) f(zr[i]);
+    auto each = [&](auto f) __attribute__((always_inline)) {                        // the row, four columns at a time, the same ones whatever the slabs
+        if (sl.cols >= sl.vocab) {
+            float4 *zr = (float4 *)(z + (long)row * sl.cols);
+            for (int i = g; i < sl.vocab >> 2; i += G) f(zr[i]);
+        } else {
+            for (int i = g; i < sl.vocab >> 2; i += G) f(*(float4 *)(z + sl.at(row, i * 4)));
         }
     };
     const int t = token[row];
@@ -809,7 +810,7 @@ constexpr int kTopKeys = 2048;                      // candidates that are sorte
 constexpr int kTopThreads = 512, kTopHeld = 8;      // strips of a thread whose maxima it keeps in registers (V up to 262144); more are read again in each pass
 __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int rows, int strips, int k, const float *__restrict__ z, const float2 *__restrict__ part, float it2,
                                                                float *__restrict__ lse, float *__restrict__ values, int *__restrict__ ids) {
-    __shared__ unsigned hist[256], sh_prefix;
+    __shared__ unsigned hist[kTopThreads / 64][256], sh_prefix;                     // one for each wave: maxima share their leading bits
     __shared__ int sh_want, n_strips, n_keys, wsum[kTopThreads / 64];
     __shared__ int list[kHeadMaxTop];
     __shared__ unsigned long long keys[kTopKeys];
@@ -822,17 +823,21 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int row
         unsigned prefix = 0;
         int left = want;
         for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kTopThreads) hist[i] = 0;
+            for (int i = tid; i < (kTopThreads / 64) * 256; i += kTopThreads) (&hist[0][0])[i] = 0;
             __syncthreads();
             for (int i = tid; i < n; i += kTopThreads) {
                 const unsigned o = value(i);
-                if (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(o >> shift) & 255], 1u);
+                if (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[wave][(o >> shift) & 255], 1u);
             }
             __syncthreads();
             if (wave == 0) {                                                         // from the top bin down: where the count passes `left`
                 unsigned h[4], mine = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) mine += h[e] = hist[255 - (lane * 4 + e)];
+                for (int e = 0; e < 4; ++e) {
+                    h[e] = 0;
+                    for (int w = 0; w < kTopThreads / 64; ++w) h[e] += hist[w][255 - (lane * 4 + e)];
+                    mine += h[e];
+                }
                 unsigned upto = mine;
 #pragma unroll
                 for (int o = 1; o < 64; o <<= 1) {
@@ -921,15 +926,24 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int row
         return *v < sl.vocab ? ordered(z[sl.at(row, *v)]) : 0u;
     };
     auto collect = [&](auto wanted) __attribute__((always_inline)) {
-        for (int i0 = tid; i0 < strips_here * kStrip; i0 += kTopThreads) {
-            int v;
-            const unsigned o = entry(i0, &v);
-            const bool in = v < sl.vocab && wanted(o, v);
-            const unsigned long long mask = __ballot(in);
-            int base = 0;
-            if (lane == 0 && mask) base = atomicAdd(&n_keys, __popcll(mask));
-            base = __shfl(base, 0, 64) + __popcll(mask & ((1ull << lane) - 1));
-            if (in && base < kTopKeys) keys[base] = (unsigned long long)o << 32 | (0xffffffffu - (unsigned)v);
+        for (int i0 = tid; i0 < strips_here * kStrip; i0 += 8 * kTopThreads) {
+            unsigned o[8];
+            int v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                v[u] = sl.vocab;
+                o[u] = i0 + u * kTopThreads < strips_here * kStrip ? entry(i0 + u * kTopThreads, &v[u]) : 0u;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const bool in = v[u] < sl.vocab && wanted(o[u], v[u]);
+                const unsigned long long mask = __ballot(in);
+                if (!mask) continue;
+                int base = 0;
+                if (lane == 0) base = atomicAdd(&n_keys, __popcll(mask));
+                base = __shfl(base, 0, 64) + __popcll(mask & ((1ull << lane) - 1));
+                if (in && base < kTopKeys) keys[base] = (unsigned long long)o[u] << 32 | (0xffffffffu - (unsigned)v[u]);
+            }
         }
         __syncthreads();
     };
@@ -961,14 +975,28 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int row
         }
         have = n_keys;
     }
-    int n = 2;
-    while (n < have) n <<= 1;
-    for (int i = have + tid; i < n; i += kTopThreads) keys[i] = 0;
-    sort_keys(keys, n);
-    for (int i = tid; i < k; i += kTopThreads) {
-        const bool in = i < have;
-        values[(long)row * k + i] = in ? entry_value(keys[i]) : -INFINITY;
-        ids[(long)row * k + i] = in ? (int)(0xffffffffu - (unsigned)keys[i]) : -1;
+    __syncthreads();
+    auto put = [&](int i, unsigned long long key) {
+        values[(long)row * k + i] = entry_value(key);
+        ids[(long)row * k + i] = (int)(0xffffffffu - (unsigned)key);
+    };
+    if (have <= kTopThreads) {                                                       // each key to its rank (they all differ): no barriers (sorted step by step, 128 keys: 7 us more)
+        if (tid < have) {
+            const unsigned long long key = keys[tid];
+            int rank = 0;
+            for (int i = 0; i < have; ++i) rank += keys[i] > key;
+            if (rank < k) put(rank, key);
+        }
+    } else {
+        int n = 2;
+        while (n < have) n <<= 1;
+        for (int i = have + tid; i < n; i += kTopThreads) keys[i] = 0;
+        sort_keys(keys, n);
+        for (int i = tid; i < k; i += kTopThreads) put(i, keys[i]);                   // (have > k)
+    }
+    for (int i = have + tid; i < k; i += kTopThreads) {
+        values[(long)row * k + i] = -INFINITY;
+        ids[(long)row * k + i] = -1;
     }
 }
 
@@ -1130,6 +1158,10 @@ ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, i
     if (n && (!h || !ws)) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer", what);
     if (!aligned(h, 16) || !aligned(c->w_dev, 16) || !aligned(d_h, 16) || !aligned(d_w, 16) || !aligned(ws, 16))
         return ms_fail(MS_ERR_UNSUPPORTED, "%s: hidden states, lm_head, their gradients and the workspace must be 16-byte aligned", what);
+    const size_t hb = (size_t)n * c->hidden * ms_dtype_size(c->dtype), wb = (size_t)c->vocab * c->hidden * ms_dtype_size(c->dtype), db = (size_t)c->vocab * c->hidden * 4;
+    auto apart = [](const void *x, size_t xb, const void *y, size_t yb) { return !x || !y || (const char *)x + xb <= (const char *)y || (const char *)y + yb <= (const char *)x; };
+    if ((d_h != h && !apart(d_h, hb, h, hb)) || !apart(d_h, hb, c->w_dev, wb) || !apart(d_h, hb, d_w, db) || !apart(d_w, db, h, hb) || !apart(d_w, db, c->w_dev, wb))
+        return ms_fail(MS_ERR_INVALID_ARG, "%s: d_h may be h, else the gradients must not overlap the hidden states, the lm_head or each other", what);
     a->c = c;
     a->use = use;
     a->k = k ? k : 1;

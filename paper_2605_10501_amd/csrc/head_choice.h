@@ -7,35 +7,38 @@
 // least time by the estimate of ms_choose_pair, plus what the parts cost to write and read (4.5 TB/s).  How many of the rows count is known on the device only, so it is the
 // sum of the times for all of them and for half (chosen for all 8192 tokens of pairs half of which was scored, V = 151936: d_h in one part, 3.85 ms; now in two, 3.2).
 struct HeadChoice { int tile, parts, wgrad_first; double us; };
-inline double head_backward_us(int tile, long rows, long cw, long d, bool d_h, bool d_w, int parts, bool *wgrad_first) {
+inline double head_backward_us(int tile, long rows, long cw, long d, int parts, bool *wgrad_first) {
     const MsTile &t = kTiles[tile];
     const MsPairTimes &c = kPairTimes[tile];
     const int ktd = (int)((cw + 63) / 64), ktw = (int)((rows + 63) / 64);
-    const long nd = d_h ? ms_tiles(t, rows, d) * parts : 0, nw = d_w ? ms_tiles(t, cw, d) : 0, slots = 256L * t.per_cu;
+    const long nd = ms_tiles(t, rows, d) * parts, nw = ms_tiles(t, cw, d), slots = 256L * t.per_cu;
     const double dd = (ktd + parts - 1) / parts * ms_ktile_us(c.d, t.per_cu, nd + nw) + c.us_round + c.us_out * 4 * t.bm * t.bn / 65536.0;
     const double dw = ktw * ms_ktile_us(c.w, t.per_cu, nd + nw) + c.us_round_w;
     *wgrad_first = dw > dd;
-    return c.us_call + (dw > dd ? ms_two_kinds(slots, nw, dw, nd, dd) : ms_two_kinds(slots, nd, dd, nw, dw)) + (d_w ? c.us_c * 1e-6 * cw * d : 0.0) +
-           (d_h ? 8.0 * parts * rows * d / 4.5e6 : 0.0);
+    return c.us_call + (dw > dd ? ms_two_kinds(slots, nw, dw, nd, dd) : ms_two_kinds(slots, nd, dd, nw, dw)) + c.us_c * 1e-6 * cw * d +
+           8.0 * parts * rows * d / 4.5e6;
 }
-inline HeadChoice head_choose(long rows, long cw, long d, bool d_h, bool d_w) {
+inline HeadChoice head_choose(long rows, long cw, long d, int forced) {
     const int ktd = (int)((cw + 63) / 64);
     HeadChoice best = {T128, 1, 0, 1e30};
-    for (int i = 0; i < kNumTiles; ++i)
-        for (int parts = 1; parts <= 64 && (parts == 1 || (d_h && ktd / parts >= 8)); parts *= 2) {
+    for (int i = 0; i < kNumTiles; ++i) {
+        if (!ms_tile_allowed(i, forced, true)) continue;
+        for (int parts = 1; parts <= 64 && (parts == 1 || ktd / parts >= 8); parts *= 2) {
             bool first = false, half_first = false;
-            const double us = head_backward_us(i, (rows + 1) / 2, cw, d, d_h, d_w, parts, &half_first) + head_backward_us(i, rows, cw, d, d_h, d_w, parts, &first);
+            const double us = head_backward_us(i, (rows + 1) / 2, cw, d, parts, &half_first) + head_backward_us(i, rows, cw, d, parts, &first);
             const int per = (ktd + parts - 1) / parts;
             if (us < best.us) best = {i, (ktd + per - 1) / per, first, us};
         }
+    }
     return best;
 }
 
 // The tile of the logits' product, by the same two numbers of rows
-inline int head_logits_tile(long rows, long cw, int kt, double out_bytes) {
+inline int head_logits_tile(long rows, long cw, int kt, double out_bytes, int forced) {
     int best = T256;
     double best_us = 1e30;
     for (int i = 0; i < kNumTiles; ++i) {
+        if (!ms_tile_allowed(i, forced, true)) continue;
         double us = 0;
         for (int half = 0; half < 2; ++half) us += ms_tile_time(kTiles[i], kTiles[i].lin, ms_tiles(kTiles[i], half ? (rows + 1) / 2 : rows, cw), kt, out_bytes);
         if (i == T256) us *= 0.9;                         // (the estimate is of the two-stage kernel; these products run the ping-pong one)

@@ -60,7 +60,7 @@ GemmParams product(int M, int N, int K, const void *A, long lda, const void *B, 
 }
 
 template <int EPI> ms_status launch_rows(GemmParams &p, double out_bytes, const int *count, hipStream_t s) {
-    const int tile = count ? head_logits_tile(p.M, p.N, p.k_tiles_per_split, out_bytes) : ms_choose_tile(p.M, p.N, p.k_tiles_per_split, out_bytes, 0, true);
+    const int tile = count ? head_logits_tile(p.M, p.N, p.k_tiles_per_split, out_bytes, gemm_forced_tile()) : ms_choose_tile(p.M, p.N, p.k_tiles_per_split, out_bytes, gemm_forced_tile(), true);
     const MsTile &t = kTiles[tile];
     p.tiles_m = ms_cdiv(p.M, t.bm);
     p.tiles_n = ms_cdiv(p.N, t.bn);

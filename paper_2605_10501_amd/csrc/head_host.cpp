@@ -1,5 +1,6 @@
 // Host-side plan and validation of the losses at the end of a section (see head.h); kernels and their sequencing are in head.hip.
 #include "head.h"
+#include "launch.h"
 #include <math.h>
 
 namespace {
@@ -18,7 +19,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     const bool whole = pairs >= 0;
     const long V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(c->dtype);
-    p.fast = c->dtype == MS_BF16 && d % 64 == 0;
+    p.fast = c->dtype == MS_BF16 && d % 64 == 0 && gemm_forced_tile() >= 0;
     const bool keeps = use != HEAD_FORWARD || !p.fast;                       // something of every (row, vocabulary entry)
     const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
     // tokens of a block: the caller's choice, or what the memory above holds, in blocks of about equal size
@@ -65,7 +66,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
         p.factor = a.take<float>(r * 4);
         p.parts = 1;
         if (p.fast) {
-            p.choice = head_choose(p.rows, V < p.cols ? V : p.cols, d, true, true);
+            p.choice = head_choose(p.rows, V < p.cols ? V : p.cols, d, gemm_forced_tile());
             p.parts = p.choice.parts;
             p.fixes = k < 1 ? 1 : k < kHeadFixes ? k : kHeadFixes;
             const size_t f = r * p.fixes;

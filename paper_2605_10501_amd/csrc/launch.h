@@ -6,6 +6,9 @@ ms_status launch_fill_f32(float *p, long n, float v, hipStream_t s);
 ms_status launch_convert_from_f32(int dtype, const float *src, void *dst, long n, hipStream_t s);
 ms_status launch_convert_bf16_to_f32(const void *src, float *dst, long n, hipStream_t s);
 
+// The tile that ms_k_gemm_config (or the environment) asks of the bf16 products: 0 none, -1 only the generic kernels
+int gemm_forced_tile();
+
 // Student-logits GEMM whose epilogue consumes the logits instead of storing them (gemm.hip); mode 1: dz, mode 2:
 // per-strip partial statistics [M][nparts][8] = (m_t, s_t, m_s, s_s, A, -, -, -) over 64-column strips.
 bool gemm_kd_epilogue_supported(int M, int N, int K, const void *A, long lda, const void *B, long ldb, const float *zt,

@@ -156,8 +156,7 @@ def test_preference_loss(dtype, n, d, vocab, eps, with_ref):
 @pytest.mark.parametrize("whole", [False, True])
 @pytest.mark.parametrize("dtype,n,d,vocab", SHAPES)
 def test_entries(dtype, n, d, vocab, whole, k):
-    if k > vocab:
-        pytest.skip("more entries than the vocabulary has")
+    k = min(k, vocab)
     c = Case(dtype, n, d, vocab, t=1.5, left_out=False)
     ids = torch.stack([torch.randperm(vocab, generator=c.g)[:k] for _ in range(n)]).to(torch.int32)
     top = c.normal((n, k), 3.0)
@@ -188,8 +187,7 @@ def _grid(c):
 @pytest.mark.parametrize("k", [1, 7, 64, 128])
 @pytest.mark.parametrize("dtype,n,d,vocab", SHAPES + [("bf16", 3, 64, 20000), ("fp32", 3, 8, 20000)])
 def test_top_logits(dtype, n, d, vocab, k):
-    if k > vocab:
-        pytest.skip("more entries than the vocabulary has")
+    k = min(k, vocab)
     c = Case(dtype, n, d, vocab, t=0.8, left_out=False)
     _grid(c)
     values, ids, lse = oracle.top_logits(f64(c.h), f64(c.w), k, 0.8)
@@ -369,3 +367,29 @@ def test_sections_learn_through_them():
     a = B.policy_loss_forward_backward(h_s, head_s, labels, old, adv, ref_logp=old, kl_coef=0.1, loss_scale=1.0)
     b = B.token_logprobs_backward(h_s, head_s, labels, -adv)
     assert torch.allclose(a["d_h"], b["d_h"], rtol=1e-5, atol=1e-6) and a["loss"].item() == pytest.approx(-adv.sum().item(), rel=1e-4, abs=1e-4)
+
+
+# every tile of the products, ragged rows, columns and rows that do not count; the generic kernels on the same sizes; -1: logits stored in fp32
+@pytest.mark.parametrize("tile", [256, 128, 128128, 128256, 64128, 64064, -1])
+@pytest.mark.parametrize("n,d,vocab", [(300, 192, 1000), (45, 64, 4104), (700, 320, 2568)])
+def test_every_tile(tile, n, d, vocab):
+    c = Case("bf16", n, d, vocab)
+    g = c.normal((n,))
+    ref = oracle.token_logprobs(f64(c.h), f64(c.w), f64(c.labels), 1.0, f64(g))
+    h, w, labels, g = c.dev(c.h, True), c.dev(c.w), c.dev(c.labels), c.dev(g, True)
+    free = B.token_logprobs(h, w, labels)
+    t = Case("bf16", n, d, vocab, left_out=False)
+    _grid(t)
+    values, ids, lse = oracle.top_logits(f64(t.h), f64(t.w), 20, 1.0)
+    try:
+        B.k_gemm_config(tile)
+        d_w = torch.zeros(vocab, d, device="cuda")
+        out = B.token_logprobs_backward(h, w, labels, g, d_w=d_w)
+        only = B.token_logprobs(h, w, labels)
+        top = B.top_logits(t.h.cuda(), t.w.cuda(), 20)
+    finally:
+        B.k_gemm_config(0)
+    assert np.all(np.abs(f64(out["logp"]) - ref["logp"]) <= c.delta()) and torch.equal(only, out["logp"])
+    assert tile < 0 or torch.equal(free, only)                                           # all tiles add up in one order
+    c.check_gradients(ref, out["d_h"], d_w)
+    assert np.array_equal(f64(top[0]), values) and np.array_equal(f64(top[1]), ids) and np.all(np.abs(f64(top[2]) - lse) <= t.delta())
