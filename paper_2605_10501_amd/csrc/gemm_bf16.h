@@ -39,7 +39,9 @@ struct GemmParams {
 
 // EPI_SWIGLU_BWD: the tile holds da = dL/d(silu(gate) * up); sg_gu = the pre-activations [M, sg_ldgu], read; C = [dgate | dup] [M, ldc]
 // EPI_EXP, EPI_LOGITS: the tile holds logits z (head_gemm.hip).  EXP: kd_stats = (reference, label as an int) of each row [M]; C (may be null) = 2^(x - reference) with
-// x = z kd_inv_t, bf16, zeros in the columns N .. N + 63 / 64 * 64; sg_gu [M] (fp32) = z of a row's label, if that is one of the columns sg_f .. sg_f + N - 1 of the vocabulary; LOGITS: C = z, fp32.  kd_part = (offset, sum) of every 64-column strip and row, [strip][kd_ldz].
+// x = z kd_inv_t, bf16, zeros in the columns N .. N + 63 / 64 * 64; sg_gu (fp32) = z of a row's label [M], if that is one of the columns sg_f .. sg_f + N - 1 of the vocabulary,
+// or, with marks, of a row's selected ids [M][ldr]: residual = which columns of a strip those are (a 64-bit word for each strip and row, [strip][kd_ldz]), bias = the place of the
+// first (a byte each); LOGITS: C = z, fp32.  kd_part = (offset, sum) of every 64-column strip and row, [strip][kd_ldz].
 enum { EPI_NONE = 0, EPI_KD_DZ = 1, EPI_KD_STATS = 2, EPI_SWIGLU = 3, EPI_SWIGLU_BWD = 4, EPI_EXP = 5, EPI_LOGITS = 6 };
 
 // Reductions over the four 16-lane groups of a wave, on the vector ALU (no LDS crossbar): lane l gets the result over lanes
@@ -52,6 +54,39 @@ template <class F> __device__ __forceinline__ float across_groups(float v, F f) 
     const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
     return f(__builtin_bit_cast(float, (unsigned)h[0]), __builtin_bit_cast(float, (unsigned)h[1]));
 }
+// What EPI_EXP reads of a tile's rows, (reference, label) and the marks of their strips, comes to LDS by direct loads that a workgroup issues before all others: read in the
+// epilogue, each of its 32-row blocks waited for memory (marks, 32768 x 50688 x 1536: 4.22 ms without any, 4.41 read there, 4.37 so).  At least 128 rows, the 1 KB of a wave's load.
+struct HeadRowsLds {
+    float2 *rows;                            // [128 or 256]
+    unsigned long long *marks;               // [tile's strips][128 or 256]
+    unsigned char *first;                    // the same
+};
+#define MS_HEAD_LDS(BM, BN)                                                                                            \
+    constexpr int kHeadRows = BM > 128 ? BM : 128;                                                                     \
+    __shared__ __align__(16) float2 head_rows[kHeadRows];                                                              \
+    __shared__ __align__(16) unsigned long long head_marks[BN / 64 * kHeadRows];                                       \
+    __shared__ __align__(16) unsigned char head_first[BN / 64 * kHeadRows]
+template <int BM, int BN, int WAVES>
+__device__ __forceinline__ void head_rows_fetch(const GemmParams &p, const HeadRowsLds &lds, int m0, int n0, int wave, int lane) {
+    constexpr int kRows = BM > 128 ? BM : 128, kPieces = kRows / 128;
+    const __amdgpu_buffer_rsrc_t rr = make_rsrc(p.kd_stats, (long)((p.M + 1) / 2) * 16);
+#pragma unroll
+    for (int i = wave; i < kPieces; i += WAVES)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rr, (lds_void *)(lds.rows + i * 128), 16, (unsigned)(m0 + i * 128) * 8 + lane * 16, 0, 0, 0);
+    if (!p.residual) return;
+    // (rows past the last one read the next strip's words, which nobody looks at; the last strip's end is the descriptor's)
+    const int strips = (p.N + 63) >> 6, first = n0 >> 6;
+#pragma unroll
+    for (int i = wave; i < BN / 64 * kPieces; i += WAVES) {
+        const int strip = i / kPieces, piece = i % kPieces;
+        const long at = (long)(first + strip) * p.kd_ldz + m0 + piece * 128, left = (long)strips * p.kd_ldz - at;
+        const __amdgpu_buffer_rsrc_t rm = make_rsrc((const unsigned long long *)p.residual + (left > 0 ? at : 0), left > 0 ? (left < 128 ? left : 128) * 8 : 0);      // (kd_ldz is a multiple of 16)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rm, (lds_void *)(lds.marks + i * 128), 16, lane * 16, 0, 0, 0);
+        const __amdgpu_buffer_rsrc_t rf = make_rsrc((const unsigned char *)p.bias + (left > 0 ? at : 0), left > 0 ? (left < 128 ? left : 128) : 0);
+        if (lane < 8) __builtin_amdgcn_raw_ptr_buffer_load_lds(rf, (lds_void *)(lds.first + i * 128), 16, lane * 16, 0, 0, 0);
+    }
+}
+
 // Reductions over each 16 lanes that hold a row's 64 columns four by four; every lane gets the result
 template <class F> __device__ __forceinline__ float across_row(float v, F f) {
     auto turned = [](float a, auto by) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a), 0x120 + decltype(by)::value, 0xf, 0xf, true)); };
@@ -243,7 +278,7 @@ struct KFragAddr16 {
 // col_base(j); stg: 8 KB of LDS that belong to the wave (the operand buffers are idle by now).
 template <int EPI, bool M16, bool TA, bool TB, int MI, int NI, class ACC, class RB, class CB>
 __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI][NI], float *stg, int m0, int n0, int wn, int lane,
-                                              RB row_base, CB col_base) {
+                                              RB row_base, CB col_base, const HeadRowsLds &head, int head_ld) {
     constexpr int FR = M16 ? 16 : 32, ACC_N = M16 ? 4 : 16, MI32 = MI * FR / 32, WTN = 64;
     static_assert(NI * FR == WTN, "staging assumes 64-column wave tiles");
     const int frow = lane & (FR - 1), fhalf = lane / FR;
@@ -348,7 +383,6 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
         const bool cok = colg < p.N, stored = colg < (p.N + 63) / 64 * 64, full = strip + 64 <= p.N;     // (full: wave-uniform)
         const float it2 = p.kd_inv_t;
         const unsigned lane_c = (unsigned)((prow * p.ldc + colg) * (EPI == EPI_EXP ? 2 : 4));
-        const __amdgpu_buffer_rsrc_t rl = make_rsrc(EPI == EPI_EXP ? (const void *)p.kd_stats : p.C, EPI == EPI_EXP ? (long)p.M * 8 : 0);
         const __amdgpu_buffer_rsrc_t rz = make_rsrc(p.C ? p.C : p.kd_part, p.C ? (long)p.M * p.ldc * (EPI == EPI_EXP ? 2 : 4) : 0);
         auto sum = [](float a, float b) { return a + b; };
         auto larger = [](float a, float b) { return fmaxf(a, b); };
@@ -359,8 +393,8 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
             int label = -1;                                                              // of the row that this lane stores for (idx < 8)
             if constexpr (EPI == EPI_EXP) {
 #pragma unroll
-                for (int ps = 0; ps < 8; ++ps) ref[ps] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rl, prow * 8 + row_bytes(i, ps * 4, 2, 4), 0, 0));
-                label = __builtin_bit_cast(int, __builtin_amdgcn_raw_buffer_load_b32(rl, (idx & 7) * 32 + prow * 8 + 4 + row_bytes(i, 0, 2, 4), 0, 0));
+                for (int ps = 0; ps < 8; ++ps) ref[ps] = head.rows[row_base(i) + ps * 4 + prow].x;
+                label = __float_as_int(head.rows[row_base(i) + (idx & 7) * 4 + prow].y);
             }
             stage_block(i, [](float a) { return a; });
             auto row_of = [&](int ps, float (&z)[4]) __attribute__((always_inline)) {
@@ -399,6 +433,14 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
                 const int row_here = idx * 4 + prow, at = label - p.sg_f - strip;
                 const bool mine = idx < 8 && (unsigned)at < 64 && at < p.N - strip && m0 + row_base(i) + row_here < p.M;
                 if (__any(mine) && mine) ((float *)p.sg_gu)[m0 + row_base(i) + row_here] = stg[row_here * 64 + (at ^ stg_swz(row_here))];
+                if (p.residual) {
+                    unsigned long long marks = idx < 8 && strip < p.N && m0 + row_base(i) + row_here < p.M ? head.marks[((strip - n0) >> 6) * head_ld + row_base(i) + row_here] : 0;
+                    if (__any(marks != 0)) {
+                        float *o = (float *)p.sg_gu + (m0 + row_base(i) + row_here) * p.ldr;
+                        if (marks) o += head.first[((strip - n0) >> 6) * head_ld + row_base(i) + row_here];
+                        for (; marks; marks &= marks - 1) *o++ = stg[row_here * 64 + ((__ffsll((long long)marks) - 1) ^ stg_swz(row_here))];
+                    }
+                }
                 bool far = false;
 #pragma unroll
                 for (int ps = 0; ps < 8; ++ps) far |= !(s[ps] < 0x1p64f);
@@ -697,6 +739,7 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
 constexpr int fast_waves_per_simd(int bm, int waves, int epi, int nst) { return waves == 8 || (bm == 128 && nst == 2 && epi == EPI_KD_DZ) ? 2 : 1; }
 template <int BM, int BN, int NST> struct FastLds {
     bf16_t *a[4], *b[4];
+    HeadRowsLds head;
 };
 // The kernel's LDS: separate objects (not one carved array), because the compiler orders LDS reads against in-flight
 // direct-to-LDS loads by alias analysis, and can only tell the buffer being filled from the buffer being read when
@@ -742,6 +785,7 @@ __device__ __forceinline__ void gemm_fast_body(const GemmParams &p, const FastLd
     const int nk = kt_end - kt_begin;
     if (nk <= 0) return;
 
+    if constexpr (EPI == EPI_EXP) head_rows_fetch<BM, BN, WM * WN>(p, lds.head, m0, n0, wave, lane);
     const bf16_t *A = (const bf16_t *)p.A, *B = (const bf16_t *)p.B;
     std::conditional_t<TA, RowTileStager<BM, WM * WN>, DmaStager<BM, WM * WN>> da;
     std::conditional_t<EPI == EPI_SWIGLU, GateUpStager<BN, WM * WN>,
@@ -902,7 +946,7 @@ __device__ __forceinline__ void gemm_fast_body(const GemmParams &p, const FastLd
     constexpr int WPA = BM / 64;
     const int sq = wave / WPA;
     float *stg = (float *)(sq == 0 ? As0 : sq == 1 ? As1 : sq == 2 ? Bs0 : Bs1) + (wave % WPA) * 2048;
-    gemm_epilogue<EPI, M16, TA, TB>(p, acc, stg, m0, n0, wn, lane, row_base, col_base);
+    gemm_epilogue<EPI, M16, TA, TB>(p, acc, stg, m0, n0, wn, lane, row_base, col_base, lds.head, BM > 128 ? BM : 128);
 }
 
 // The 256 x 256 tile with two wave groups that take turns on the matrix cores; K-contiguous operands only.
@@ -944,6 +988,7 @@ struct HalfStager {
 };
 struct PpLds {
     bf16_t *a[2][2], *b[2][2];                          // [stage][half]
+    HeadRowsLds head;
 };
 #define MS_PP_LDS                                                                                                     \
     constexpr int HS = 128 * BK; /* elements of a half tile */                                                        \
@@ -1074,6 +1119,7 @@ __device__ __forceinline__ void gemm_pp_body(const GemmParams &p, const PpLds &l
         fetch_a(kt + 2, 1, a1);
         turn(I1{}, FH{});
     };
+    if constexpr (EPI == EPI_EXP) head_rows_fetch<256, 256, 8>(p, lds.head, m0, n0, wave, lane);
     // in the order in which the loop would have requested them
     fetch_b(0, 0, B00); fetch_a(0, 0, A00); fetch_b(0, 1, B01); fetch_a(0, 1, A01);
     fetch_b(1, 1, B11); fetch_a(1, 0, A10); fetch_b(1, 0, B10); fetch_a(1, 1, A11);
@@ -1094,7 +1140,7 @@ __device__ __forceinline__ void gemm_pp_body(const GemmParams &p, const PpLds &l
     auto col_base = [&](int j) { return wn * 64 + j * 32; };
     const int sq = wave >> 1;
     float *stg = (float *)(sq == 0 ? A00 : sq == 1 ? A01 : sq == 2 ? A10 : A11) + (wave & 1) * 2048;
-    gemm_epilogue<EPI, true, false, false>(p, acc, stg, m0, n0, wn, lane, row_base, col_base);
+    gemm_epilogue<EPI, true, false, false>(p, acc, stg, m0, n0, wn, lane, row_base, col_base, lds.head, 256);
 }
 
 }  // namespace

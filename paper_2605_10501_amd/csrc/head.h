@@ -12,7 +12,7 @@ constexpr int kStrip = 64;                   // columns that share one partial s
 // Rows of hidden states meet the vocabulary a block of tokens at a time.  What a block keeps of every (row, vocabulary entry) lies in
 // slabs of `cols` columns, [slab][rows][cols], because a matrix product's operand has to be within reach of 32-bit offsets.
 struct HeadPlan {
-    int rows, cols, slabs, strips;           // of a block; strips over all slabs, cols / kStrip in each but the last
+    int block, rows, cols, slabs, strips;    // tokens of a block, rows that there is room for; strips over all slabs, cols / kStrip in each but the last
     bool fast;                               // bf16 products whose epilogue meets the logits (head_gemm.hip)
     int *slot, *token, *count;               // [rows] row of a token, [rows] token of a row (-1: none), [1] rows in use
     void *h;                                 // [rows, hidden] hidden states of the rows, later times the row's factor
@@ -23,6 +23,9 @@ struct HeadPlan {
     float *z_sel, *rho;                      // [rows, k] logits at the selected ids, and what a row has there in its gradient
     float *log_p, *mass;                     // [rows, k], [rows] of the teacher's entries
     int *ids;                                // [rows, k] the entries that count (-1: ignored)
+    int *best;                               // [rows] the entry that the teacher thinks most of
+    unsigned long long *marks;               // [strips, rows] which columns of a strip are among a row's entries, and how many entries are before them; null: the entries'
+    unsigned char *marks_first;              // logits are dot products of their own
     int *key;                                // [rows] < 0: the token is left out
     float *logp;                             // [rows] by token of the block
     float2 *part;                            // [strips, rows]
@@ -41,6 +44,11 @@ struct HeadPlan {
 };
 
 enum HeadUse { HEAD_TOP = 0, HEAD_FORWARD = 1, HEAD_BACKWARD = 2 };
+
+// Whether the logits of a row's k entries come out of the matrix product by marks, or are dot products of their own.  A dot product of d numbers takes 0.26 d ps (its row of w comes from
+// behind the L2s); marks take 8 ps for every strip and row, to clear, set and look at (32768 tokens, V = 151936, d = 1536, 64 entries: 0.85 and 0.7 ms; 32000 tokens, V = 32000,
+// d = 1024, 100 entries: 0.95 and 0.25).
+constexpr bool head_use_marks(long k, long d, long strips) { return k > 1 && k * d > 31 * strips; }
 
 // pairs >= 0: a preference loss of that many pairs, all n tokens in one block
 HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws);

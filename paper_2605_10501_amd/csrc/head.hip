@@ -38,30 +38,37 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 }
 
 // ------------------------------------------------------------------ which tokens count
-// The teacher's entries of a token, one wave each: the ids that count, ln p of each and the sum of p.
+// The teacher's entries of a token, one wave each: those that count, in the order of their ids (-1 behind them), ln p of each, the sum of p, and the id of the largest.
 __global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int vocab, float inv_t, const int *__restrict__ top_ids,
                                                            const float *__restrict__ top, const float *__restrict__ lse_teacher,
-                                                           int *__restrict__ ids, float *__restrict__ log_p, float *__restrict__ mass, int *__restrict__ key) {
+                                                           int *__restrict__ ids, float *__restrict__ log_p, float *__restrict__ mass, int *__restrict__ best, int *__restrict__ key) {
     __shared__ int seen[4][kHeadMaxTop];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long t = (long)blockIdx.x * 4 + wave;
     if (t < n)
         for (int j = lane; j < k; j += 64) seen[wave][j] = top_ids[t * k + j];
     __syncthreads();
-    if (t >= n) return;
-    float y[2], m = -INFINITY;
-    int id[2];
+    float y[2] = {-INFINITY, -INFINITY}, m = -INFINITY;
+    int id[2] = {-1, -1};
+    if (t < n) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int j = lane + 64 * e;
-        id[e] = j < k ? seen[wave][j] : -1;
-        if (id[e] >= vocab) id[e] = -1;
-        if (id[e] >= 0)
-            for (int i = 0; i < j; ++i)
-                if (seen[wave][i] == id[e]) id[e] = -1;
-        y[e] = id[e] >= 0 ? top[t * k + j] * inv_t : -INFINITY;
-        m = fmaxf(m, y[e]);                                                     // (passes over NaN, which the sum has)
+        for (int e = 0; e < 2; ++e) {
+            const int j = lane + 64 * e;
+            id[e] = j < k ? seen[wave][j] : -1;
+            if (id[e] >= vocab) id[e] = -1;
+            if (id[e] >= 0)
+                for (int i = 0; i < j; ++i)
+                    if (seen[wave][i] == id[e]) id[e] = -1;
+            y[e] = id[e] >= 0 ? top[t * k + j] * inv_t : -INFINITY;
+            m = fmaxf(m, y[e]);                                                     // (passes over NaN, which the sum has)
+        }
     }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (lane + 64 * e < k) seen[wave][lane + 64 * e] = id[e];
+    __syncthreads();
+    if (t >= n) return;
     m = wave_max(m);
     float s = 0.f;
 #pragma unroll
@@ -71,21 +78,27 @@ __global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int voc
     const bool some = !(s == 0.f);                                              // an entry above -inf, or a NaN
     const float L = lse_teacher ? (some ? lse_teacher[t] : 0.f) : m + logf(s);
     float total = 0.f;
+    int valid = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int j = lane + 64 * e;
-        if (j >= k) continue;
         const bool in = some && id[e] >= 0;
-        const float lp = in ? y[e] - L : -INFINITY;
-        ids[t * k + j] = in ? id[e] : -1;
-        log_p[t * k + j] = lp;
-        if (in) total += expf(lp);
+        valid += __popcll(__ballot(in));
+        if (!in) continue;
+        const float lp = y[e] - L;
+        int at = 0;
+        for (int i = 0; i < k; ++i) at += seen[wave][i] >= 0 && seen[wave][i] < id[e];
+        ids[t * k + at] = id[e];
+        log_p[t * k + at] = lp;
+        total += expf(lp);
+        if (y[e] == m) best[t] = id[e];                                         // (any of equal ones)
     }
+    for (int j = valid + lane; j < k; j += 64) ids[t * k + j] = -1;
     total = wave_sum(total);
     if (lane == 0) {
         const bool counts = some && !(total == 0.f);
         mass[t] = counts ? total : 0.f;
         key[t] = counts ? 0 : -1;
+        if (m == -INFINITY) best[t] = valid ? 0 : -1;                           // (only NaN among them)
     }
 }
 
@@ -157,7 +170,8 @@ __global__ __launch_bounds__(256) void head_take_kernel(int n, int d, const int 
 
 // ------------------------------------------------------------------ rows and their selected logits
 // Copies the hidden states of the rows together, and takes the logits of each row's k selected ids (h rows . w rows, fp32); the reference of the
-// row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.
+// row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.  Of many entries only the teacher's
+// best is taken here (sel its id, k = 1, z_sel null): their logits come out of the matrix product, see head_marks_kernel.
 // W waves a row: one for a label, four or eight for the teacher's entries, four ids at a time.
 template <class T, int W>
 __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T *__restrict__ h, const T *__restrict__ w, const int *__restrict__ token,
@@ -195,14 +209,30 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T
             acc[j] = wave_sum(acc[j]);
             if (id[j] < 0) continue;
             best = fmaxf(best, acc[j]);
-            if (lane == 0) z_sel[(long)row * k + j0 + j] = acc[j];
+            if (lane == 0 && z_sel) z_sel[(long)row * k + j0 + j] = acc[j];
         }
     }
     if (lane == 0) sm[wave] = best;
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < W; ++i) best = fmaxf(best, sm[i]);
-        ref[row] = make_float2(rintf(best * it2), __int_as_float(k == 1 ? sel[t] : -1));
+        ref[row] = make_float2(rintf(best * it2), __int_as_float(k == 1 && z_sel ? sel[t] : -1));
+    }
+}
+
+// Marks of the entries of every row, whose logits the matrix product then leaves in z_sel; one wave per row, the words are zero before.
+__global__ __launch_bounds__(256) void head_marks_kernel(int ld, int k, const int *__restrict__ token, const int *__restrict__ count, const int *__restrict__ ids,
+                                                         unsigned long long *__restrict__ marks, unsigned char *__restrict__ first) {
+    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= *count) return;
+    const int *r = ids + (long)token[row] * k;
+    for (int j = lane; j < k; j += 64) {
+        const int id = r[j], strip = id >> 6;
+        if (id < 0 || (j > 0 && r[j - 1] >> 6 == strip)) continue;              // the first of its strip writes the word
+        unsigned long long word = 0;
+        for (int i = j; i < k && r[i] >= 0 && r[i] >> 6 == strip; ++i) word |= 1ull << (r[i] & 63);
+        marks[(long)strip * ld + row] = word;
+        first[(long)strip * ld + row] = (unsigned char)j;
     }
 }
 
@@ -1002,7 +1032,12 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int row
 
 // ------------------------------------------------------------------ sequencing
 // Logits of `rows` rows h: stored (fp32), or their exponentials at p.ref (fast losses; not stored in a forward pass); the fast products leave the sums of their strips too
-ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int rows, const void *h, hipStream_t s) {
+HeadMarks marks_of(const HeadPlan &p, int v0, int k) {
+    if (!p.marks) return {};
+    const size_t at = (size_t)(v0 / kStrip) * p.rows;
+    return {p.marks + at, p.marks_first + at, p.z_sel, k};
+}
+ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int k, int rows, const void *h, hipStream_t s) {
     const int V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(c->dtype);
     const float it2 = kLog2e / c->temperature;
@@ -1013,7 +1048,7 @@ ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int ro
         float2 *part = p.part + (size_t)(v0 / kStrip) * p.rows;
         if (!p.fast) MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, w, d, (float *)p.z + slab, p.cols, 1, 0, nullptr, nullptr, 0, 0, 1, s));
         else if (use == HEAD_TOP) MS_TRY(head_gemm_logits(rows, cw, d, h, w, it2, (float *)p.z + slab, p.cols, part, p.rows, s));
-        else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, v0, p.z_label, it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
+        else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, v0, p.z_label, marks_of(p, v0, k), it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
     }
     return MS_OK;
 }
@@ -1054,7 +1089,7 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
             else head_take_kernel<bf16_t><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, key, limit, labels ? sel : nullptr, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.slot, p.token, out0, out1, (bf16_t *)p.h, p.z_sel);
         }
         MS_LAUNCH_CHECK();
-        MS_TRY(logits(c, p, a.use, n, p.h, a.s));
+        MS_TRY(logits(c, p, a.use, a.k, n, p.h, a.s));
         *dz_done = dz_here && c->dtype == MS_F32 && a.use == HEAD_BACKWARD;
         const Slabs sl = {p.rows, p.cols, V};
         float *scale = a.use == HEAD_BACKWARD ? p.scale : nullptr, *rho = a.use == HEAD_BACKWARD ? p.rho : nullptr;
@@ -1072,14 +1107,19 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
     MS_LAUNCH_CHECK();
     {
         ProfScope ps(9, 0, a.s);
-#define GO(W) head_pick_kernel<bf16_t, W><<<n, 64 * W, 0, a.s>>>(d, a.k, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.token, p.count, sel, it2, (bf16_t *)p.h, p.z_sel, p.ref)
-        if (a.k > 16) GO(8);
-        else if (a.k > 4) GO(4);
-        else GO(1);
+#define GO(W, k, sel, z_sel) head_pick_kernel<bf16_t, W><<<n, 64 * W, 0, a.s>>>(d, k, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.token, p.count, sel, it2, (bf16_t *)p.h, z_sel, p.ref)
+        if (p.marks) GO(1, 1, p.best, nullptr);
+        else if (a.k > 4) GO(4, a.k, sel, p.z_sel);
+        else GO(1, a.k, sel, p.z_sel);
 #undef GO
     }
     MS_LAUNCH_CHECK();
-    MS_TRY(logits(c, p, a.use, n, p.h, a.s));
+    if (p.marks) {
+        MS_TRY(launch_fill_f32((float *)p.marks, 2L * p.rows * p.strips, 0.f, a.s));
+        head_marks_kernel<<<ms_cdiv(n, 4), 256, 0, a.s>>>(p.rows, a.k, p.token, p.count, sel, p.marks, p.marks_first);
+        MS_LAUNCH_CHECK();
+    }
+    MS_TRY(logits(c, p, a.use, a.k, n, p.h, a.s));
     MS_TRY(combine(p, n, 1.f, p.ref, it2, p.stat, nullptr, after, p.count, a.s));
     if (labels) return MS_OK;
     const bool back = a.use == HEAD_BACKWARD;
@@ -1197,10 +1237,10 @@ extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const voi
     const HeadPlan &p = a.p;
     const float it2 = kLog2e / c->temperature;
     const bool whole = !p.fast && c->vocab <= kTopKeys;                            // a row is looked through at once, without sums of strips
-    for (int t0 = 0; t0 < n; t0 += p.rows) {
-        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+    for (int t0 = 0; t0 < n; t0 += p.block) {
+        const int nb = n - t0 < p.block ? n - t0 : p.block;
         const Slabs sl = {p.rows, p.cols, c->vocab};
-        MS_TRY(logits(c, p, HEAD_TOP, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
+        MS_TRY(logits(c, p, HEAD_TOP, k, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
         if (!p.fast && !whole) {
             head_strips_kernel<<<dim3(ms_cdiv(p.strips, 4), nb < 32768 ? nb : 32768), 256, 0, a.s>>>(sl, nb, p.strips, (const float *)p.z, it2, p.part);
             MS_LAUNCH_CHECK();
@@ -1225,11 +1265,11 @@ extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, i
     const float inv_t = 1.f / c->temperature;
     float *kl = kl_tok ? kl_tok : p.per_token;
     const LossTerms all = {kl, n, c->loss_scale, loss};
-    for (int t0 = 0; t0 < n; t0 += p.rows) {
-        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+    for (int t0 = 0; t0 < n; t0 += p.block) {
+        const int nb = n - t0 < p.block ? n - t0 : p.block;
         bool dz_done = false;
         head_entries_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, c->vocab, inv_t, top_ids + (long)t0 * k, top_logits + (long)t0 * k, lse_teacher ? lse_teacher + t0 : nullptr,
-                                                             p.ids, p.log_p, p.mass, p.key);
+                                                             p.ids, p.log_p, p.mass, p.best, p.key);
         MS_LAUNCH_CHECK();
         MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr, nullptr, After{}, Entries{p.log_p, p.mass, kl + t0, c->loss_scale * inv_t}, true, &dz_done));
         MS_TRY(end_of_block(a, t0, nb, n, p.ids, dz_done, all));
@@ -1246,8 +1286,8 @@ static ms_status token_logprobs(const char *what, const ms_head_config *c, int n
     HeadCall a;
     MS_TRY(begin(&a, what, c, n, 0, back ? HEAD_BACKWARD : HEAD_FORWARD, -1, h, d_h, d_w, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
-    for (int t0 = 0; t0 < n; t0 += p.rows) {
-        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+    for (int t0 = 0; t0 < n; t0 += p.block) {
+        const int nb = n - t0 < p.block ? n - t0 : p.block;
         bool dz_done = false;
         float *lp = logp ? logp + t0 : p.logp;
         MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, nullptr, after_label(a, back ? AFTER_GIVEN : AFTER_LOGP, lp, back ? d_logp + t0 : nullptr, {}), Entries{}, true, &dz_done));
@@ -1280,8 +1320,8 @@ extern "C" ms_status ms_policy_loss_forward_backward(const ms_head_config *c, co
     const HeadPlan &p = a.p;
     float *terms = loss_tok ? loss_tok : p.per_token;
     const LossTerms all = {terms, n, c->loss_scale, loss};
-    for (int t0 = 0; t0 < n; t0 += p.rows) {
-        const int nb = n - t0 < p.rows ? n - t0 : p.rows;
+    for (int t0 = 0; t0 < n; t0 += p.block) {
+        const int nb = n - t0 < p.block ? n - t0 : p.block;
         bool dz_done = false;
         float *lp = logp ? logp + t0 : p.logp;
         const PolicyArgs pa = {old_logp + t0, pc->kl_coef > 0.f ? ref_logp + t0 : nullptr, advantages + t0, weights ? weights + t0 : nullptr, terms + t0, pc->clip_low, pc->clip_high,

@@ -14,20 +14,30 @@ __device__ __forceinline__ int rows_in_use(int rows, const int *count) { return 
 template <int EPI>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void head_pp_kernel(GemmParams p, const int *count) {
     MS_PP_LDS;
+    PpLds all = lds;
+    if constexpr (EPI == EPI_EXP) {
+        MS_HEAD_LDS(256, 256);
+        all.head = {head_rows, head_marks, head_first};
+    }
     p.M = rows_in_use(p.M, count);
     p.tiles_m = (p.M + 255) / 256;
     const int nb = p.tiles_m * p.tiles_n;
     if ((int)blockIdx.x >= nb) return;
-    gemm_pp_body<EPI>(p, lds, blockIdx.x, nb, 0);
+    gemm_pp_body<EPI>(p, all, blockIdx.x, nb, 0);
 }
 template <int BM, int BN, int WM, int WN, int NST, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(fast_waves_per_simd(BM, WM * WN, EPI, NST)))) void head_tile_kernel(GemmParams p, const int *count) {
     MS_FAST_LDS(BM, BN, NST);
+    FastLds<BM, BN, NST> all = lds;
+    if constexpr (EPI == EPI_EXP) {
+        MS_HEAD_LDS(BM, BN);
+        all.head = {head_rows, head_marks, head_first};
+    }
     p.M = rows_in_use(p.M, count);
     p.tiles_m = (p.M + BM - 1) / BM;
     const int nb = p.tiles_m * p.tiles_n;
     if ((int)blockIdx.x >= nb) return;
-    gemm_fast_body<BM, BN, WM, WN, false, false, EPI, true, NST>(p, lds, blockIdx.x, nb, 0);
+    gemm_fast_body<BM, BN, WM, WN, false, false, EPI, true, NST>(p, all, blockIdx.x, nb, 0);
 }
 
 // Input gradient (pd: rows = M, in `parts` parts of K, each with a result of its own, part_ld elements apart) and weight gradient (pw: rows = K) in one grid, as
@@ -83,10 +93,11 @@ template <int EPI> ms_status launch_rows(GemmParams &p, double out_bytes, const 
 
 }  // namespace
 
-ms_status head_gemm_exp(int rows, int cw, int d, const void *h, const void *w, const float2 *ref, int v0, float *z_label, float it2, void *c, long ldc, float2 *part, long ld,
+ms_status head_gemm_exp(int rows, int cw, int d, const void *h, const void *w, const float2 *ref, int v0, float *z_label, const HeadMarks &marks, float it2, void *c, long ldc, float2 *part, long ld,
                         const int *count, hipStream_t s) {
     GemmParams p = product(rows, cw, d, h, d, w, d, c, ldc, 0, 0);
     p.kd_stats = (float *)const_cast<float2 *>(ref); p.kd_part = (float *)part; p.kd_ldz = ld; p.kd_inv_t = it2; p.sg_f = v0; p.sg_gu = z_label;
+    if (marks.word) p.residual = marks.word, p.bias = marks.first, p.sg_gu = marks.z, p.ldr = marks.k;
     return launch_rows<EPI_EXP>(p, c ? 4 : 2, count, s);
 }
 

@@ -30,7 +30,8 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
         else most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
     }
     const long blocks = whole || n <= most ? 1 : (n + most - 1) / most;
-    p.rows = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
+    p.block = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
+    p.rows = (int)round_up(p.block, 16);                                       // (a strip's words and bytes start at 16 bytes)
     long widest = kReach / (2 * d) - 512;
     if (keeps) widest = least(widest, kReach / (long)(ez * (p.rows + 256L)));
     p.slabs = (int)((V + widest - 1) / widest);
@@ -56,6 +57,11 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
             p.mass = a.take<float>(r * 4);
             p.ids = a.take<int>(r * k * 4);
             p.key = a.take<int>(r * 4);
+            p.best = a.take<int>(r * 4);
+            if (p.fast && head_use_marks(k, d, p.strips)) {
+                p.marks = a.take<unsigned long long>(r * p.strips * 8);
+                p.marks_first = a.take<unsigned char>(r * p.strips);
+            }
         }
         p.per_token = a.take<float>((size_t)(whole ? pairs : n) * 4);
         if (whole) p.margin = a.take<float>((size_t)pairs * 4);
@@ -66,7 +72,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
         p.factor = a.take<float>(r * 4);
         p.parts = 1;
         if (p.fast) {
-            p.choice = head_choose(p.rows, V < p.cols ? V : p.cols, d, gemm_forced_tile());
+            p.choice = head_choose(p.block, V < p.cols ? V : p.cols, d, gemm_forced_tile());
             p.parts = p.choice.parts;
             p.fixes = k < 1 ? 1 : k < kHeadFixes ? k : kHeadFixes;
             const size_t f = r * p.fixes;

@@ -22,8 +22,8 @@ static void check(const ms_head_config &c, int n, int k, HeadUse use, int pairs)
     CHECK(size.bytes == p.bytes && size.rows == p.rows && size.cols == p.cols && size.parts == p.parts);
     const long V = c.vocab, d = c.hidden, r = p.rows, es = c.dtype == MS_BF16 ? 2 : 4, kk = k ? k : 1, reach = (1L << 32) - (1L << 20);
     if (n == 0) return;
-    CHECK(r >= 1 && r <= n && (pairs < 0 || r == n));
-    CHECK(c.token_block == 0 || pairs >= 0 || r <= c.token_block);
+    CHECK(r % 16 == 0 && r >= p.block && r < p.block + 16 && p.block >= 1 && p.block <= n && (pairs < 0 || p.block == n));
+    CHECK(c.token_block == 0 || pairs >= 0 || p.block <= c.token_block);
     CHECK((long)p.slabs * p.cols >= V && (long)(p.slabs - 1) * p.cols < V && (long)p.strips * 64 >= V && (long)(p.strips - 1) * 64 < V);
     CHECK(p.slabs == 1 || p.cols % 256 == 0);
     CHECK(p.fast == (c.dtype == MS_BF16 && d % 64 == 0 && forced >= 0));
@@ -44,6 +44,12 @@ static void check(const ms_head_config &c, int n, int k, HeadUse use, int pairs)
             all.push_back({p.mass, (size_t)r * 4});
             all.push_back({p.ids, (size_t)(r * k * 4)});
             all.push_back({p.key, (size_t)r * 4});
+            all.push_back({p.best, (size_t)r * 4});
+            CHECK((p.marks != nullptr) == (p.fast && head_use_marks(k, d, p.strips)));
+            if (p.marks) {
+                all.push_back({p.marks, (size_t)r * p.strips * 8});
+                all.push_back({p.marks_first, (size_t)r * p.strips});
+            }
         }
         all.push_back({p.per_token, (size_t)(pairs >= 0 ? pairs : n) * 4});
         if (pairs >= 0) all.push_back({p.margin, (size_t)pairs * 4});
