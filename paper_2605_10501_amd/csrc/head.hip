@@ -172,21 +172,20 @@ __global__ __launch_bounds__(256) void head_take_kernel(int n, int d, const int 
 // Copies the hidden states of the rows together, and takes the logits of each row's k selected ids (h rows . w rows, fp32); the reference of the
 // row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.  Of many entries only the teacher's
 // best is taken here (sel its id, k = 1, z_sel null): their logits come out of the matrix product, see head_marks_kernel.
-// W waves a row: one for a label, four or eight for the teacher's entries, four ids at a time.
-template <class T, int W>
-__global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T *__restrict__ h, const T *__restrict__ w, const int *__restrict__ token,
-                                                           const int *__restrict__ count, const int *__restrict__ sel, float it2, T *__restrict__ out,
+// W waves a row, four ids at a time.
+template <int W>
+__global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const bf16_t *__restrict__ h, const bf16_t *__restrict__ w, const int *__restrict__ token,
+                                                           const int *__restrict__ count, const int *__restrict__ sel, float it2, bf16_t *__restrict__ out,
                                                            float *__restrict__ z_sel, float2 *__restrict__ ref) {
     __shared__ float sm[W];
     const int row = blockIdx.x;
     if (row >= *count) return;
     const int t = token[row], lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr int N = Vec16<T>::N;
-    const T *hr = h + (long)t * d;
-    for (int i = threadIdx.x * N; i < d; i += 64 * W * N) stv(out + (long)row * d + i, ldv(hr + i));
+    const bf16_t *hr = h + (long)t * d;
+    for (int i = threadIdx.x * 8; i < d; i += 64 * W * 8) stv(out + (long)row * d + i, ldv(hr + i));
     float best = -INFINITY;
     for (int j0 = wave * 4; j0 < k; j0 += 4 * W) {
-        const T *wr[4];
+        const bf16_t *wr[4];
         int id[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -194,14 +193,14 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T
             wr[j] = w + (long)(id[j] < 0 ? 0 : id[j]) * d;
         }
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int i = lane * N; i < d; i += 64 * N) {
-            const Vec16<T> a = ldv(hr + i);
+        for (int i = lane * 8; i < d; i += 64 * 8) {
+            const Vec16<bf16_t> a = ldv(hr + i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (id[j] < 0) continue;
-                const Vec16<T> b = ldv(wr[j] + i);
+                const Vec16<bf16_t> b = ldv(wr[j] + i);
 #pragma unroll
-                for (int e = 0; e < N; ++e) acc[j] = __builtin_fmaf(to_f32(a.v[e]), to_f32(b.v[e]), acc[j]);
+                for (int e = 0; e < 8; ++e) acc[j] = __builtin_fmaf((float)a.v[e], (float)b.v[e], acc[j]);
             }
         }
 #pragma unroll
@@ -209,15 +208,70 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const T
             acc[j] = wave_sum(acc[j]);
             if (id[j] < 0) continue;
             best = fmaxf(best, acc[j]);
-            if (lane == 0 && z_sel) z_sel[(long)row * k + j0 + j] = acc[j];
+            if (lane == 0) z_sel[(long)row * k + j0 + j] = acc[j];
         }
     }
     if (lane == 0) sm[wave] = best;
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < W; ++i) best = fmaxf(best, sm[i]);
-        ref[row] = make_float2(rintf(best * it2), __int_as_float(k == 1 && z_sel ? sel[t] : -1));
+        ref[row] = make_float2(rintf(best * it2), __int_as_float(-1));
     }
+}
+
+// The same with one id a row, a label's (z_sel given) or the teacher's best, one wave per row.  FIND: the rows are found here too, instead of by head_rows_kernel (a launch
+// less): wave j is token j, and its workgroup counts the tokens before it that have rows.  For n <= kHeadFind, which is then a load of 16 keys by every thread.
+constexpr int kHeadFind = 4096;
+template <bool FIND>
+__global__ __launch_bounds__(256) void head_pick_one_kernel(int n, int d, const bf16_t *__restrict__ h, const bf16_t *__restrict__ w, const int *__restrict__ key, int limit, int *slot, int *token,
+                                                            int *count, float *__restrict__ out0, float *__restrict__ out1, const int *__restrict__ sel, float it2, bf16_t *__restrict__ out,
+                                                            float *__restrict__ z_sel, float2 *__restrict__ ref) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int row = blockIdx.x * 4 + wave, t;
+    if constexpr (FIND) {
+        __shared__ int sm[4];
+        const int first = blockIdx.x * 4;
+        auto counts = [&](int j) { return key[j] >= 0 && key[j] < limit; };
+        int before = 0;
+#pragma unroll
+        for (int u = 0; u < kHeadFind / 256; ++u) {
+            const int j = u * 256 + threadIdx.x;
+            before += __popcll(__ballot(j < first && counts(j)));
+        }
+        if (lane == 0) sm[wave] = before;
+        __syncthreads();
+        t = row;
+        row = sm[0] + sm[1] + sm[2] + sm[3];
+        if (t >= n) return;
+        for (int j = first; j < t; ++j) row += counts(j);
+        const bool in = counts(t);
+        if (lane == 0) {
+            slot[t] = in ? row : -1;
+            if (in) token[row] = t;
+            else {
+                if (out0) out0[t] = 0.f;
+                if (out1) out1[t] = 0.f;
+            }
+            if (t == n - 1) *count = row + in;
+        }
+        if (!in) return;
+    } else {
+        if (row >= *count) return;
+        t = token[row];
+    }
+    const int id = sel[t];
+    const bf16_t *hr = h + (long)t * d, *wr = w + (long)(id < 0 ? 0 : id) * d;
+    float acc = 0.f;
+    for (int i = lane * 8; i < d; i += 64 * 8) {
+        const Vec16<bf16_t> a = ldv(hr + i), b = ldv(wr + i);
+        stv(out + (long)row * d + i, a);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc = __builtin_fmaf((float)a.v[e], (float)b.v[e], acc);
+    }
+    acc = wave_sum(acc);
+    if (lane != 0) return;
+    if (z_sel) z_sel[row] = acc;
+    ref[row] = make_float2(rintf(acc * it2), __int_as_float(z_sel ? id : -1));
 }
 
 // Marks of the entries of every row, whose logits the matrix product then leaves in z_sel; one wave per row, the words are zero before.
@@ -1100,18 +1154,21 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
         MS_LAUNCH_CHECK();
         return MS_OK;
     }
-    {
+    const bool one = p.marks || a.k == 1, find = one && n <= kHeadFind;
+    if (!find) {
         ProfScope ps(11, 0, a.s);
         head_rows_kernel<<<1, 1024, 0, a.s>>>(n, key, limit, p.slot, p.token, p.count, out0, out1);
+        MS_LAUNCH_CHECK();
     }
-    MS_LAUNCH_CHECK();
     {
         ProfScope ps(9, 0, a.s);
-#define GO(W, k, sel, z_sel) head_pick_kernel<bf16_t, W><<<n, 64 * W, 0, a.s>>>(d, k, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.token, p.count, sel, it2, (bf16_t *)p.h, z_sel, p.ref)
-        if (p.marks) GO(1, 1, p.best, nullptr);
-        else if (a.k > 4) GO(4, a.k, sel, p.z_sel);
-        else GO(1, a.k, sel, p.z_sel);
-#undef GO
+        const bf16_t *hb = (const bf16_t *)h, *wb = (const bf16_t *)c->w_dev;
+        const int *id = p.marks ? p.best : sel;
+        float *z = p.marks ? nullptr : p.z_sel;
+        if (find) head_pick_one_kernel<true><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, hb, wb, key, limit, p.slot, p.token, p.count, out0, out1, id, it2, (bf16_t *)p.h, z, p.ref);
+        else if (one) head_pick_one_kernel<false><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, hb, wb, key, limit, p.slot, p.token, p.count, out0, out1, id, it2, (bf16_t *)p.h, z, p.ref);
+        else if (a.k > 4) head_pick_kernel<4><<<n, 256, 0, a.s>>>(d, a.k, hb, wb, p.token, p.count, sel, it2, (bf16_t *)p.h, p.z_sel, p.ref);
+        else head_pick_kernel<1><<<n, 64, 0, a.s>>>(d, a.k, hb, wb, p.token, p.count, sel, it2, (bf16_t *)p.h, p.z_sel, p.ref);
     }
     MS_LAUNCH_CHECK();
     if (p.marks) {
