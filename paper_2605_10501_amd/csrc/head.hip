@@ -22,15 +22,6 @@ struct Slabs {
     }
 };
 
-__device__ __forceinline__ float block_sum(float v, float *sm) {
-    v = wave_sum(v);
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float r = 0.f;
-    for (int i = 0; i < (int)(blockDim.x >> 6); ++i) r += sm[i];
-    __syncthreads();
-    return r;
-}
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -39,14 +30,19 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 
 // ------------------------------------------------------------------ which tokens count
 // The teacher's entries of a token, one wave each: those that count, in the order of their ids (-1 behind them), ln p of each, the sum of p, and the id of the largest.
-__global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int vocab, float inv_t, const int *__restrict__ top_ids,
-                                                           const float *__restrict__ top, const float *__restrict__ lse_teacher,
-                                                           int *__restrict__ ids, float *__restrict__ log_p, float *__restrict__ mass, int *__restrict__ best, int *__restrict__ key) {
-    __shared__ int seen[4][kHeadMaxTop];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long t = (long)blockIdx.x * 4 + wave;
+struct Teacher {
+    int k, vocab;
+    float inv_t;
+    const int *top_ids;                                                            // [n][k]; null: no entries
+    const float *top, *lse;
+    int *ids, *best, *key;
+    float *log_p, *mass;
+};
+// Token t for this wave (not below n: none), of four in the workgroup, all of which come here; returns whether the token counts
+__device__ __forceinline__ bool teacher_entries(const Teacher &a, int n, long t, int (&seen)[kHeadMaxTop]) {
+    const int lane = threadIdx.x & 63, k = a.k;
     if (t < n)
-        for (int j = lane; j < k; j += 64) seen[wave][j] = top_ids[t * k + j];
+        for (int j = lane; j < k; j += 64) seen[j] = a.top_ids[t * k + j];
     __syncthreads();
     float y[2] = {-INFINITY, -INFINITY}, m = -INFINITY;
     int id[2] = {-1, -1};
@@ -54,21 +50,21 @@ __global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int voc
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int j = lane + 64 * e;
-            id[e] = j < k ? seen[wave][j] : -1;
-            if (id[e] >= vocab) id[e] = -1;
+            id[e] = j < k ? seen[j] : -1;
+            if (id[e] >= a.vocab) id[e] = -1;
             if (id[e] >= 0)
                 for (int i = 0; i < j; ++i)
-                    if (seen[wave][i] == id[e]) id[e] = -1;
-            y[e] = id[e] >= 0 ? top[t * k + j] * inv_t : -INFINITY;
+                    if (seen[i] == id[e]) id[e] = -1;
+            y[e] = id[e] >= 0 ? a.top[t * k + j] * a.inv_t : -INFINITY;
             m = fmaxf(m, y[e]);                                                     // (passes over NaN, which the sum has)
         }
     }
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-        if (lane + 64 * e < k) seen[wave][lane + 64 * e] = id[e];
+        if (lane + 64 * e < k) seen[lane + 64 * e] = id[e];
     __syncthreads();
-    if (t >= n) return;
+    if (t >= n) return false;
     m = wave_max(m);
     float s = 0.f;
 #pragma unroll
@@ -76,7 +72,7 @@ __global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int voc
         if (id[e] >= 0 && !(y[e] == -INFINITY)) s += expf(y[e] - (m == -INFINITY ? 0.f : m));
     s = wave_sum(s);
     const bool some = !(s == 0.f);                                              // an entry above -inf, or a NaN
-    const float L = lse_teacher ? (some ? lse_teacher[t] : 0.f) : m + logf(s);
+    const float L = a.lse ? (some ? a.lse[t] : 0.f) : m + logf(s);
     float total = 0.f;
     int valid = 0;
 #pragma unroll
@@ -86,20 +82,25 @@ __global__ __launch_bounds__(256) void head_entries_kernel(int n, int k, int voc
         if (!in) continue;
         const float lp = y[e] - L;
         int at = 0;
-        for (int i = 0; i < k; ++i) at += seen[wave][i] >= 0 && seen[wave][i] < id[e];
-        ids[t * k + at] = id[e];
-        log_p[t * k + at] = lp;
+        for (int i = 0; i < k; ++i) at += seen[i] >= 0 && seen[i] < id[e];
+        a.ids[t * k + at] = id[e];
+        a.log_p[t * k + at] = lp;
         total += expf(lp);
-        if (y[e] == m) best[t] = id[e];                                         // (any of equal ones)
+        if (y[e] == m) a.best[t] = id[e];                                       // (any of equal ones)
     }
-    for (int j = valid + lane; j < k; j += 64) ids[t * k + j] = -1;
+    for (int j = valid + lane; j < k; j += 64) a.ids[t * k + j] = -1;
     total = wave_sum(total);
+    const bool counts = some && !(total == 0.f);
     if (lane == 0) {
-        const bool counts = some && !(total == 0.f);
-        mass[t] = counts ? total : 0.f;
-        key[t] = counts ? 0 : -1;
-        if (m == -INFINITY) best[t] = valid ? 0 : -1;                           // (only NaN among them)
+        a.mass[t] = counts ? total : 0.f;
+        a.key[t] = counts ? 0 : -1;
+        if (m == -INFINITY) a.best[t] = valid ? 0 : -1;                         // (only NaN among them)
     }
+    return counts;
+}
+__global__ __launch_bounds__(256) void head_entries_kernel(int n, Teacher a) {
+    __shared__ int seen[4][kHeadMaxTop];
+    teacher_entries(a, n, (long)blockIdx.x * 4 + (threadIdx.x >> 6), seen[threadIdx.x >> 6]);
 }
 
 // Rows of a block: the tokens that count (key in [0, limit)) in their order, without gaps; out0, out1 of the others are 0.  One workgroup: a block has at most
@@ -134,16 +135,21 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__res
 }
 
 // Where logits are stored, row t is token t: hidden states as they are, or zeros for a token that is left out; a label's logit (labels != null) as a dot product of its
-// own.  One wave per row.
+// own.  One wave per row, which sorts out the teacher's entries as well.
 template <class T>
-__global__ __launch_bounds__(256) void head_take_kernel(int n, int d, const int *__restrict__ key, int limit, const int *__restrict__ labels, const T *__restrict__ h, const T *__restrict__ w,
+__global__ __launch_bounds__(256) void head_take_kernel(int n, int d, Teacher teacher, int limit, const int *__restrict__ labels, const T *__restrict__ h, const T *__restrict__ w,
                                                         int *__restrict__ slot, int *__restrict__ token, float *__restrict__ out0, float *__restrict__ out1, T *__restrict__ out,
                                                         float *__restrict__ z_sel) {
     constexpr int N = Vec16<T>::N;
     const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    bool in;
+    if (teacher.top_ids) {
+        __shared__ int seen[4][kHeadMaxTop];
+        in = teacher_entries(teacher, n, row, seen[threadIdx.x >> 6]);
+    }
     if (row >= n) return;
-    const int at = key[row];
-    const bool in = at >= 0 && at < limit;
+    const int at = labels ? labels[row] : -1;
+    if (!teacher.top_ids) in = at >= 0 && at < limit;
     if (lane == 0) {
         slot[row] = token[row] = in ? row : -1;
         if (out0 && !in) out0[row] = 0.f;
@@ -485,18 +491,21 @@ struct LossTerms {
     float scale;
     float *loss;                                                                   // null: not here
 };
-__device__ __forceinline__ void sum_loss(const LossTerms &a) {
+__device__ __forceinline__ void sum_loss(const LossTerms &a) {                      // by the first 256 threads; all of the workgroup come here
     __shared__ float sm[4];
     float acc = 0.f;
-    for (int i = threadIdx.x; i < a.n; i += 256 * 8) {
-        float v[8];
+    if (threadIdx.x < 256)
+        for (int i = threadIdx.x; i < a.n; i += 256 * 8) {
+            float v[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = i + u * 256 < a.n ? a.terms[i + u * 256] : 0.f;
+            for (int u = 0; u < 8; ++u) v[u] = i + u * 256 < a.n ? a.terms[i + u * 256] : 0.f;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) acc += v[u];
-    }
-    acc = block_sum(acc, sm);
-    if (threadIdx.x == 0) *a.loss = a.scale * acc;
+            for (int u = 0; u < 8; ++u) acc += v[u];
+        }
+    acc = wave_sum(acc);
+    if (threadIdx.x < 256 && (threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = acc;
+    __syncthreads();
+    if (threadIdx.x == 0) *a.loss = a.scale * (sm[0] + sm[1] + sm[2] + sm[3]);
 }
 __global__ __launch_bounds__(256) void head_loss_kernel(LossTerms a) { sum_loss(a); }
 
@@ -707,13 +716,19 @@ __global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k,
 // d_w[id] += the rows of `fix` with that id, in their order; n <= kHeadScan of them.  A workgroup takes eight rows and 512 columns: each of its waves looks for the others of one
 // row's id in a copy of the ids in LDS, and the first row of an id sums them all, by itself or, where there are many, with all eight waves (an eighth of the rows each).
 // (A workgroup per row that reads the ids itself: 18 us for 2053 rows of 1024, 41 for 4124; waves by themselves 38 and 26; now 14 and 22.)
-constexpr int kFixWaves = 8;
-__global__ __launch_bounds__(64 * kFixWaves) void head_fix_kernel(int n, int d, const int *__restrict__ id, const bf16_t *__restrict__ fix, float *__restrict__ d_w) {
-    constexpr int kMany = 8, kList = 256;
-    __shared__ __align__(16) int ids[kHeadScan];
-    __shared__ unsigned short found[kFixWaves][kList];
-    __shared__ float join[(kFixWaves - 1) * 512];
-    __shared__ int many[kFixWaves];
+constexpr int kFixWaves = 8, kFixMany = 8, kFixList = 256;
+struct FixLds {
+    __align__(16) int ids[kHeadScan];
+    unsigned short found[kFixWaves][kFixList];
+    float join[(kFixWaves - 1) * 512];
+    int many[kFixWaves];
+};
+__device__ __forceinline__ void fix_rows(FixLds &lds, int block, int block_col, int n, int d, const int *__restrict__ id, const bf16_t *__restrict__ fix, float *__restrict__ d_w) {
+    constexpr int kMany = kFixMany, kList = kFixList;
+    auto &ids = lds.ids;
+    auto &found = lds.found;
+    auto &join = lds.join;
+    auto &many = lds.many;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (n + 255) >> 8;
     for (int j0 = tid; j0 < chunks * 256; j0 += 8 * 64 * kFixWaves) {
         int q[8];
@@ -729,7 +744,7 @@ __global__ __launch_bounds__(64 * kFixWaves) void head_fix_kernel(int n, int d, 
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
-    const int i = blockIdx.x * kFixWaves + wave, mine = i < n ? ids[i] : -1, col = blockIdx.y * 512 + lane * 8;
+    const int i = block * kFixWaves + wave, mine = i < n ? ids[i] : -1, col = block_col * 512 + lane * 8;
     float acc[8] = {};
     auto sum = [&](const unsigned short *list, int from, int to) __attribute__((always_inline)) {
         if (col < d)
@@ -816,47 +831,71 @@ __global__ __launch_bounds__(64 * kFixWaves) void head_fix_kernel(int n, int d, 
 #pragma unroll
             for (int x = 0; x < 8; ++x)
                 for (int w = 0; w < kFixWaves - 1; ++w) acc[x] += join[w * 512 + x * 64 + lane];
-            put(ids[blockIdx.x * kFixWaves + e]);
+            put(ids[block * kFixWaves + e]);
         }
         __syncthreads();
     }
 }
 
 // d_h of the block's tokens: a row's sums (in `parts` parts) times its factor, and what the selected ids' lack; zeros for tokens that were left out
-template <class T>
-__global__ __launch_bounds__(256) void head_d_h_kernel(long total, int d, int parts, long part_ld, const int *__restrict__ slot, const float *__restrict__ sums, const float *__restrict__ factor,
-                                                       int fixes, const int *__restrict__ fix_id, const float *__restrict__ fix_rest, const bf16_t *__restrict__ w, T *__restrict__ d_h, LossTerms loss) {
-    if (loss.loss && blockIdx.x == gridDim.x - 1) {                                 // (a launch less)
+struct RowSums {
+    const float *sums, *factor;                                                    // [parts][part_ld], [rows] (null: 1)
+    int parts;
+    long part_ld;
+    int fixes;
+    const int *fix_id;
+    const float *fix_rest;
+    const bf16_t *w;
+    const int *slot;
+};
+__device__ __forceinline__ void row_gradient(const RowSums &a, long i, int d, bf16_t *d_h) {       // four columns from i on
+    const int t = (int)(i / d), c = (int)(i - (long)t * d), row = a.slot[t];
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float f = row < 0 ? 0.f : a.factor ? a.factor[row] : 1.f;
+    if (row >= 0 && f != 0.f) {
+        for (int q0 = 0; q0 < a.parts; q0 += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = q0 + q < a.parts ? *(const float4 *)(a.sums + (q0 + q) * a.part_ld + (long)row * d + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) { v.x += x[q].x; v.y += x[q].y; v.z += x[q].z; v.w += x[q].w; }
+        }
+        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+        for (int q = 0; q < a.fixes; ++q) {
+            const int id = a.fix_id[(long)row * a.fixes + q];
+            if (id < 0) continue;
+            const float rest = a.fix_rest[(long)row * a.fixes + q];
+            const bf16_t *x = a.w + (long)id * d + c;
+            v.x = __builtin_fmaf(rest, (float)x[0], v.x);
+            v.y = __builtin_fmaf(rest, (float)x[1], v.y);
+            v.z = __builtin_fmaf(rest, (float)x[2], v.z);
+            v.w = __builtin_fmaf(rest, (float)x[3], v.w);
+        }
+    }
+    bf16_t *o = d_h + i;
+    o[0] = (bf16_t)v.x; o[1] = (bf16_t)v.y; o[2] = (bf16_t)v.z; o[3] = (bf16_t)v.w;
+}
+
+// What is left behind the gradients' products, in one launch: rows of d_w to complete (fix_blocks workgroups, fix_cols of them for each eight rows; FIX: there are some), d_h, and the
+// loss (the last workgroup).  Apart they took 15, 12 and 5 us at 2053 tokens of 1024, each of them latency.
+template <bool FIX>
+__global__ __launch_bounds__(64 * kFixWaves) void head_end_kernel(int fix_blocks, int fix_cols, int n_fix, const int *__restrict__ fix_id, const bf16_t *__restrict__ fix, float *__restrict__ d_w, RowSums rows,
+                                                                  long total, int d, bf16_t *d_h, LossTerms loss) {
+    int b = blockIdx.x;
+    if constexpr (FIX) {
+        __shared__ FixLds lds;
+        if (b < fix_blocks) {
+            fix_rows(lds, b / fix_cols, b % fix_cols, n_fix, d, fix_id, fix, d_w);
+            return;
+        }
+        b -= fix_blocks;
+    }
+    if (loss.loss && blockIdx.x == gridDim.x - 1) {
         sum_loss(loss);
         return;
     }
-    const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= total) return;
-    const int t = (int)(i / d), c = (int)(i - (long)t * d), row = slot[t];
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float f = row < 0 ? 0.f : factor ? factor[row] : 1.f;
-    if (row >= 0 && f != 0.f) {
-        for (int q0 = 0; q0 < parts; q0 += 8) {
-            float4 a[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) a[q] = q0 + q < parts ? *(const float4 *)(sums + (q0 + q) * part_ld + (long)row * d + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) { v.x += a[q].x; v.y += a[q].y; v.z += a[q].z; v.w += a[q].w; }
-        }
-        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-        for (int q = 0; q < fixes; ++q) {
-            const int id = fix_id[(long)row * fixes + q];
-            if (id < 0) continue;
-            const float rest = fix_rest[(long)row * fixes + q];
-            const bf16_t *a = w + (long)id * d + c;
-            v.x = __builtin_fmaf(rest, (float)a[0], v.x);
-            v.y = __builtin_fmaf(rest, (float)a[1], v.y);
-            v.z = __builtin_fmaf(rest, (float)a[2], v.z);
-            v.w = __builtin_fmaf(rest, (float)a[3], v.w);
-        }
-    }
-    T *o = d_h + i;
-    o[0] = from_f32<T>(v.x); o[1] = from_f32<T>(v.y); o[2] = from_f32<T>(v.z); o[3] = from_f32<T>(v.w);
+    const long i = ((long)b * 64 * kFixWaves + threadIdx.x) * 4;
+    if (i < total) row_gradient(rows, i, d, d_h);
 }
 
 // ------------------------------------------------------------------ top logits
@@ -961,7 +1000,11 @@ __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int row
         __syncthreads();
         const float u = m == -INFINITY ? 0.f : m;
         for (int v = tid; v < sl.vocab; v += kTopThreads) s += __builtin_amdgcn_exp2f((z[sl.at(row, v)] - u) * it2);
-        s = block_sum(s, sm);
+        s = wave_sum(s);
+        if (lane == 0) sm[wave] = s;
+        __syncthreads();
+        s = 0.f;
+        for (int w = 0; w < kTopThreads / 64; ++w) s += sm[w];
         if (tid == 0) lse[row] = kLn2 * (m * it2 + __log2f(s));
     }
     if (!all) {
@@ -1128,8 +1171,9 @@ struct HeadCall {
 };
 
 // Rows, their logits, sums over the vocabulary, and what follows.  key / sel: per token of the block (labels, or the entries' keys and ids); out0, out1: zeroed for the
-// tokens that are left out.  Labels: after; the teacher's entries: en.  *dz_done: the gradient of stored logits is in their place already.
-ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int limit, const int *sel, float *out0, float *out1, const After &after, const Entries &en, bool dz_here, bool *dz_done) {
+// tokens that are left out.  Labels: after; the teacher's entries: teacher, en.  *dz_done: the gradient of stored logits is in their place already.
+ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int limit, const int *sel, float *out0, float *out1, const After &after, const Teacher &teacher, const Entries &en, bool dz_here,
+                       bool *dz_done) {
     const ms_head_config *c = a.c;
     const HeadPlan &p = a.p;
     const int d = c->hidden, V = c->vocab;
@@ -1139,8 +1183,8 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
     if (!p.fast) {
         {
             ProfScope ps(9, 0, a.s);
-            if (c->dtype == MS_F32) head_take_kernel<float><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, key, limit, labels ? sel : nullptr, (const float *)h, (const float *)c->w_dev, p.slot, p.token, out0, out1, (float *)p.h, p.z_sel);
-            else head_take_kernel<bf16_t><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, key, limit, labels ? sel : nullptr, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.slot, p.token, out0, out1, (bf16_t *)p.h, p.z_sel);
+            if (c->dtype == MS_F32) head_take_kernel<float><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, teacher, limit, labels ? sel : nullptr, (const float *)h, (const float *)c->w_dev, p.slot, p.token, out0, out1, (float *)p.h, p.z_sel);
+            else head_take_kernel<bf16_t><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, teacher, limit, labels ? sel : nullptr, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.slot, p.token, out0, out1, (bf16_t *)p.h, p.z_sel);
         }
         MS_LAUNCH_CHECK();
         MS_TRY(logits(c, p, a.use, a.k, n, p.h, a.s));
@@ -1153,6 +1197,10 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
 #undef GO
         MS_LAUNCH_CHECK();
         return MS_OK;
+    }
+    if (teacher.top_ids) {
+        head_entries_kernel<<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, teacher);
+        MS_LAUNCH_CHECK();
     }
     const bool one = p.marks || a.k == 1, find = one && n <= kHeadFind;
     if (!find) {
@@ -1227,24 +1275,21 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool d
         else if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, sums, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
         else MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 0, a.s));
     }
-    if (p.fast && a.d_w) {
-        const int rows = n * p.fixes;
-        if (rows <= kHeadScan) {
-            head_fix_kernel<<<dim3(ms_cdiv(rows, kFixWaves), ms_cdiv(d, 512)), 64 * kFixWaves, 0, a.s>>>(rows, d, p.fix_id, (const bf16_t *)p.fix, (float *)a.d_w);
-            MS_LAUNCH_CHECK();
-        } else {
-            MS_TRY(ms_k_embedding_sorted_backward(dt, rows, d, V, 1.f, p.fix_id, p.fix, (float *)a.d_w, p.fix_scratch, p.fix_scratch_bytes, a.s));
-        }
-    }
-    const bool sum_here = a.d_h && dt == MS_BF16 && loss.loss;
-    if (a.d_h && dt == MS_BF16) {
-        const long total = (long)n * d;
-        ProfScope ps(11, (4.0 + es) * total, a.s);
-        head_d_h_kernel<bf16_t><<<ms_cdiv(total, 1024) + sum_here, 256, 0, a.s>>>(total, d, p.parts, total, p.slot, p.d_h, p.fast ? p.factor : nullptr, p.fixes, p.fix_id, p.fix_rest, (const bf16_t *)c->w_dev,
-                                                                                  (bf16_t *)a.d_h + (size_t)t0 * d, loss);
-        MS_LAUNCH_CHECK();
-    }
-    return loss.loss && !sum_here ? total_loss(loss, a.s) : MS_OK;
+    if (dt == MS_F32) return loss.loss ? total_loss(loss, a.s) : MS_OK;
+    const int n_fix = p.fast && a.d_w ? n * p.fixes : 0;
+    if (n_fix > kHeadScan) MS_TRY(ms_k_embedding_sorted_backward(dt, n_fix, d, V, 1.f, p.fix_id, p.fix, (float *)a.d_w, p.fix_scratch, p.fix_scratch_bytes, a.s));
+    const bool fix_here = n_fix > 0 && n_fix <= kHeadScan;
+    const int fix_cols = ms_cdiv(d, 512), fix_blocks = fix_here ? ms_cdiv(n_fix, kFixWaves) * fix_cols : 0;
+    const long total = a.d_h ? (long)n * d : 0, blocks = fix_blocks + ms_cdiv(total, 256 * kFixWaves) + (loss.loss != nullptr);
+    if (blocks == 0) return MS_OK;
+    const RowSums rows = {p.d_h, p.fast ? p.factor : nullptr, p.parts, (long)n * d, p.fast ? p.fixes : 0, p.fix_id, p.fix_rest, (const bf16_t *)c->w_dev, p.slot};
+    bf16_t *out = a.d_h ? (bf16_t *)a.d_h + (size_t)t0 * d : nullptr;
+    ProfScope ps(11, (4.0 + es) * total, a.s);
+#define GO(FIX) head_end_kernel<FIX><<<(unsigned)blocks, 64 * kFixWaves, 0, a.s>>>(fix_blocks, fix_cols, n_fix, p.fix_id, (const bf16_t *)p.fix, (float *)a.d_w, rows, total, d, out, loss)
+    if (fix_here) GO(true); else GO(false);
+#undef GO
+    MS_LAUNCH_CHECK();
+    return MS_OK;
 }
 
 bool aligned(const void *q, int by) { return ((uintptr_t)q & (by - 1)) == 0; }
@@ -1325,10 +1370,8 @@ extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, i
     for (int t0 = 0; t0 < n; t0 += p.block) {
         const int nb = n - t0 < p.block ? n - t0 : p.block;
         bool dz_done = false;
-        head_entries_kernel<<<ms_cdiv(nb, 4), 256, 0, a.s>>>(nb, k, c->vocab, inv_t, top_ids + (long)t0 * k, top_logits + (long)t0 * k, lse_teacher ? lse_teacher + t0 : nullptr,
-                                                             p.ids, p.log_p, p.mass, p.best, p.key);
-        MS_LAUNCH_CHECK();
-        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr, nullptr, After{}, Entries{p.log_p, p.mass, kl + t0, c->loss_scale * inv_t}, true, &dz_done));
+        const Teacher teacher = {k, c->vocab, inv_t, top_ids + (long)t0 * k, top_logits + (long)t0 * k, lse_teacher ? lse_teacher + t0 : nullptr, p.ids, p.best, p.key, p.log_p, p.mass};
+        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr, nullptr, After{}, teacher, Entries{p.log_p, p.mass, kl + t0, c->loss_scale * inv_t}, true, &dz_done));
         MS_TRY(end_of_block(a, t0, nb, n, p.ids, dz_done, all));
     }
     return MS_OK;
@@ -1347,7 +1390,7 @@ static ms_status token_logprobs(const char *what, const ms_head_config *c, int n
         const int nb = n - t0 < p.block ? n - t0 : p.block;
         bool dz_done = false;
         float *lp = logp ? logp + t0 : p.logp;
-        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, nullptr, after_label(a, back ? AFTER_GIVEN : AFTER_LOGP, lp, back ? d_logp + t0 : nullptr, {}), Entries{}, true, &dz_done));
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, nullptr, after_label(a, back ? AFTER_GIVEN : AFTER_LOGP, lp, back ? d_logp + t0 : nullptr, {}), {}, {}, true, &dz_done));
         MS_TRY(end_of_block(a, t0, nb, n, labels + t0, dz_done, LossTerms{}));
     }
     return MS_OK;
@@ -1383,7 +1426,7 @@ extern "C" ms_status ms_policy_loss_forward_backward(const ms_head_config *c, co
         float *lp = logp ? logp + t0 : p.logp;
         const PolicyArgs pa = {old_logp + t0, pc->kl_coef > 0.f ? ref_logp + t0 : nullptr, advantages + t0, weights ? weights + t0 : nullptr, terms + t0, pc->clip_low, pc->clip_high,
                                pc->kl_coef, c->loss_scale};
-        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, terms + t0, after_label(a, AFTER_POLICY, lp, nullptr, pa), Entries{}, true, &dz_done));
+        MS_TRY(rows_forward(a, t0, nb, labels + t0, c->vocab, labels + t0, lp, terms + t0, after_label(a, AFTER_POLICY, lp, nullptr, pa), {}, {}, true, &dz_done));
         MS_TRY(end_of_block(a, t0, nb, n, labels + t0, dz_done, all));
     }
     return MS_OK;
@@ -1415,7 +1458,7 @@ extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c
     const HeadPlan &p = a.p;
     float *lp = logp ? logp : p.logp;
     bool dz_done = false;
-    MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp, nullptr, after_label(a, AFTER_LOGP, lp, nullptr, {}), Entries{}, false, &dz_done));
+    MS_TRY(rows_forward(a, 0, n, labels, c->vocab, labels, lp, nullptr, after_label(a, AFTER_LOGP, lp, nullptr, {}), {}, {}, false, &dz_done));
     head_pairs_kernel<<<pairs, 256, 0, a.s>>>(batch->cu_seqlens_dev, label_rows(a), ref_logp, pc->beta, pc->label_smoothing, c->loss_scale, lp, margin ? margin : p.margin, p.per_token);
     MS_LAUNCH_CHECK();
     return end_of_block(a, 0, n, n, labels, dz_done, LossTerms{p.per_token, pairs, c->loss_scale, loss});
