@@ -564,7 +564,7 @@ __global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, f
             id[0] = sel[t];
             const float l = label_after(after, t, row, x_label(after, z_sel[row]) - (double)m * after.inv_t * kLog2e64, s, __builtin_amdgcn_exp2f((z[sl.at(row, id[0])] - u) * it2));
             r[0] = expm1f(l);
-            if (dz) c = scale[row];
+            if (dz) c = after.rows.scale[row];
         }
         if (dz) {
             if constexpr (G == 64) c = __shfl(c, 0, 64);

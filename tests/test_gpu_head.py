@@ -393,3 +393,34 @@ def test_every_tile(tile, n, d, vocab):
     assert tile < 0 or torch.equal(free, only)                                           # all tiles add up in one order
     c.check_gradients(ref, out["d_h"], d_w)
     assert np.array_equal(f64(top[0]), values) and np.array_equal(f64(top[1]), ids) and np.all(np.abs(f64(top[2]) - lse) <= t.delta())
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 72), ("fp32", 72)])
+@pytest.mark.parametrize("n,vocab,k", [(137, 2056, 3), (90, 4104, 100), (1, 264, 9)])
+def test_a_workspace_holds_whatever_it_held(monkeypatch, dtype, d, n, vocab, k):
+    """The same bits with a workspace of zeros, of NaN, of large numbers and of what another call left behind."""
+    c = Case(dtype, n, d, vocab)
+    old, adv = (c.normal((n,)) - 7).cuda(), c.normal((n,)).cuda()
+    h, w, labels = c.dev(c.h), c.w.cuda(), c.labels.cuda()
+    ids, top = torch.randint(-1, vocab, (n, k), generator=c.g, dtype=torch.int32).cuda(), c.normal((n, k)).cuda()
+    cu = B.Batch([0, n // 3, n])
+    one = torch.zeros(1 << 26, dtype=torch.uint8, device="cuda")
+
+    def calls(fill):
+        def workspace(nbytes, device="cuda", tag=None):
+            assert nbytes <= one.numel()
+            if fill is not None:
+                one.fill_(fill)
+            return one[:max(int(nbytes), 256)]
+        monkeypatch.setattr(B, "workspace", workspace)
+        d_w = [torch.zeros(vocab, d, device="cuda") for _ in range(4)]
+        out = [B.policy_loss_forward_backward(h, w, labels, old, adv, ref_logp=old, kl_coef=0.1, d_w=d_w[0]), B.topk_kd_loss_forward_backward(h, w, ids, top, d_w=d_w[1]),
+               B.preference_loss_forward_backward(h, w, labels, cu, 0.1, d_w=d_w[2]), B.token_logprobs_backward(h, w, labels, adv, d_w=d_w[3]), dict(enumerate(B.top_logits(h, w, k))),
+               dict(a=B.token_logprobs(h, w, labels))]
+        return out, d_w
+    ref = calls(0)
+    for fill in (0xff, 0x7f, None):
+        got = calls(fill)
+        for a, b in zip(ref[0], got[0]):
+            assert all(torch.equal(a[x], b[x]) for x in a)
+        assert all(torch.equal(a, b) for a, b in zip(ref[1], got[1]))
