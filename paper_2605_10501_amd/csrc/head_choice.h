@@ -6,6 +6,8 @@
 // K tiles each, beside the 3564 short workgroups of d_w.  So the vocabulary is cut into parts, whose sums are added when d_h is rounded: as many as give the
 // least time by the estimate of ms_choose_pair, plus what the parts cost to write and read (4.5 TB/s).  How many of the rows count is known on the device only, so it is the
 // sum of the times for all of them and for half (chosen for all 8192 tokens of pairs half of which was scored, V = 151936: d_h in one part, 3.85 ms; now in two, 3.2).
+// The parts' sums take 2^25 numbers at most (128 MB), so that the workspace grows with the rows.
+constexpr long kHeadMostParts = 64, kHeadPartsRoom = 1L << 25;
 struct HeadChoice { int tile, parts, wgrad_first; double us; };
 inline double head_backward_us(int tile, long rows, long cw, long d, int parts, bool *wgrad_first) {
     const MsTile &t = kTiles[tile];
@@ -23,7 +25,7 @@ inline HeadChoice head_choose(long rows, long cw, long d, int forced) {
     HeadChoice best = {T128, 1, 0, 1e30};
     for (int i = 0; i < kNumTiles; ++i) {
         if (!ms_tile_allowed(i, forced, true)) continue;
-        for (int parts = 1; parts <= 64 && (parts == 1 || ktd / parts >= 8); parts *= 2) {
+        for (int parts = 1; parts <= kHeadMostParts && (parts == 1 || (ktd / parts >= 8 && parts * rows * d <= kHeadPartsRoom)); parts *= 2) {
             bool first = false, half_first = false;
             const double us = head_backward_us(i, (rows + 1) / 2, cw, d, parts, &half_first) + head_backward_us(i, rows, cw, d, parts, &first);
             const int per = (ktd + parts - 1) / parts;

@@ -32,14 +32,18 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     const long blocks = whole || n <= most ? 1 : (n + most - 1) / most;
     p.block = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
     p.rows = (int)round_up(p.block, 16);                                       // (a strip's words and bytes start at 16 bytes)
-    long widest = kReach / (2 * d) - 512;
-    if (keeps) widest = least(widest, kReach / (long)(ez * (p.rows + 256L)));
-    p.slabs = (int)((V + widest - 1) / widest);
+    auto slabs_of = [&](long rows) {
+        long widest = kReach / (2 * d) - 512;
+        if (keeps) widest = least(widest, kReach / (long)(ez * (rows + 256L)));
+        widest = widest / 256 * 256;
+        return (V + widest - 1) / widest;
+    };
+    p.slabs = (int)slabs_of(p.rows);
     p.cols = p.slabs == 1 ? (int)V : (int)round_up((V + p.slabs - 1) / p.slabs, 256);
-    if (p.slabs > 1 && p.cols > widest) p.cols -= 256, p.slabs = (int)((V + p.cols - 1) / p.cols);
     if (p.fast) p.cols = (int)round_up(p.cols, 64);                          // (d_h's product reads whole K tiles)
     p.strips = (int)((V + kStrip - 1) / kStrip);
-    const size_t r = (size_t)p.rows;
+    // What is taken is for the largest block of calls up to this one, so that memory for n tokens serves fewer (97 tokens in blocks of at most 80 are two of 56)
+    const size_t r = (size_t)round_up(least(n, most), 16);
     Arena a(ws);
     p.slot = a.take<int>(r * 4);
     p.token = a.take<int>(r * 4);
@@ -84,10 +88,11 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
                 p.fix_scratch = a.take<void>(p.fix_scratch_bytes);
             }
         }
-        if (c->dtype == MS_BF16) p.d_h = a.take<float>(r * p.parts * d * 4);
-        if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(r * p.cols * 2);
+        const long sums = (long)r * d, in_parts = least(kHeadMostParts * sums, kHeadPartsRoom);
+        if (c->dtype == MS_BF16) p.d_h = a.take<float>((p.fast && in_parts > sums ? in_parts : sums) * 4);
+        if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(least((long)r * (V + 256), kReach / 4) * 2);
     }
-    if (keeps) p.z = a.take<void>((size_t)p.slabs * r * p.cols * ez);
+    if (keeps) p.z = a.take<void>(r * (V + 257 * slabs_of((long)r)) * ez);
     p.bytes = a.off;
     return p;
 }

@@ -101,3 +101,17 @@ def test_workspace_grows_with_the_call():
             need = B._fn("ms_head_workspace_bytes")(C.byref(c), n, 64, 1)
             assert 0 < need < 40 << 30
             assert 0 < B._fn("ms_top_logits_workspace_bytes")(C.byref(c), n, 64) < 16 << 30
+
+
+@pytest.mark.parametrize("vocab,hidden,dtype", [(151936, 1536, "bf16"), (32000, 1024, "bf16"), (32000, 64, "bf16"), (32000, 72, "bf16"), (1024, 128, "fp32"), (151936, 512, "fp32")])
+@pytest.mark.parametrize("k", [0, 64])
+@pytest.mark.parametrize("block", [0, 40, 4096])
+def test_memory_for_many_tokens_serves_fewer(vocab, hidden, dtype, k, block):
+    c = C.byref(cfg(vocab=vocab, hidden=hidden, dtype=B.MS_F32 if dtype == "fp32" else B.MS_BF16, token_block=block))
+    ns = [*range(0, 700), *range(700, 9000, 13), *range(9000, 140000, 397)]
+    queries = [lambda n, b=b: B._fn("ms_head_workspace_bytes")(c, n, k, b) for b in (0, 1)]
+    queries.append(lambda n: B._fn("ms_preference_workspace_bytes")(c, n, n // 2, 1) if k == 0 and n < 100000 else 0)
+    queries.append(lambda n: B._fn("ms_top_logits_workspace_bytes")(c, n, k) if k else 0)
+    for q in queries:
+        need = [q(n) for n in ns]
+        assert all(a <= b or b == 0 for a, b in zip(need, need[1:]))
