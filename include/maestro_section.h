@@ -211,7 +211,8 @@ ms_status ms_kd_loss_forward_backward_static(const ms_kd_config *kd, int32_t n_t
  *     inputs may hold anything there, NaN included.
  *   - d_h (storage type, [n_tokens, hidden]) is overwritten, and may be h itself; d_w (fp32, [vocab, hidden]) is accumulated.  Otherwise they must not overlap
  *     what is read, or each other.  Either may be NULL; both NULL: forward only.  loss_dev: device float.
- *   - Sums run in an order that the sizes alone fix: the same call gives the same bits.  A token's loss and log-probability do not depend on what it is packed with.
+ *   - Sums run in an order that the sizes alone fix: the same call gives the same bits.  A token's loss and log-probability do not depend on what it is packed with
+ *     (fp32: apart from which of two products a call takes, by its tokens x vocab: up to about a million, and above).
  *   - A bf16 head keeps e^(z - reference) of a block's tokens (bf16, [tokens, vocab]) between the two halves of the pass instead of computing the logits
  *     twice; that is where the gradient of the logits is rounded to the storage type.  token_block: the tokens of a block (a multiple of 8;
  *     0: as many as 16 GB hold).  A preference loss has all its tokens in one block.

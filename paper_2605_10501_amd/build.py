@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmaestro_section.so")
 BUILD = os.path.join(ROOT, "_build")
-SOURCES = ["api.cpp", "profile.cpp", "scheduler.cpp", "kd_host.cpp", "head_host.cpp", "column_work.cpp", "elementwise.hip", "qk_norm.hip", "embedding_sorted.hip", "gemm.hip", "fp8_quantize.hip", "gemm_fp8.hip", "linear_f32.hip", "attention.hip", "attention_mfma.hip", "kd.hip", "head.hip", "head_gemm.hip",
+SOURCES = ["api.cpp", "profile.cpp", "scheduler.cpp", "kd_host.cpp", "head_host.cpp", "column_work.cpp", "elementwise.hip", "qk_norm.hip", "embedding_sorted.hip", "gemm.hip", "fp8_quantize.hip", "gemm_fp8.hip", "linear_f32.hip", "attention.hip", "attention_mfma.hip", "kd.hip", "head.hip", "head_gemm.hip", "head_f32.hip",
            "section.hip", "section_options.hip", "merger.hip", "probes.hip"]
 INLINE_PRODUCTS = {"gemm_fp8.hip": "gemm_fp8_big_kernel"}      # kernels with matrix products as inline assembly
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-x", "hip",

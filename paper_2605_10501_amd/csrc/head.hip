@@ -5,6 +5,7 @@
 // (its label, or the teacher's entries), where rho = dz / scale_row is q - 1 or q - p / sum p.  The logits there are dot products of their own.
 #include "common.h"
 #include "head.h"
+#include "head_f32.h"
 #include "head_gemm.h"
 #include "launch.h"
 
@@ -1143,7 +1144,8 @@ ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int k,
         const char *w = (const char *)c->w_dev + (size_t)v0 * d * es;
         const size_t slab = (size_t)i * p.rows * p.cols;
         float2 *part = p.part + (size_t)(v0 / kStrip) * p.rows;
-        if (!p.fast) MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, w, d, (float *)p.z + slab, p.cols, 1, 0, nullptr, nullptr, 0, 0, 1, s));
+        if (c->dtype == MS_F32 && head_f32_logits_tiled(rows, V)) MS_TRY(head_f32_logits(rows, cw, d, (const float *)h, (const float *)w, (float *)p.z + slab, p.cols, s));
+        else if (!p.fast) MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, w, d, (float *)p.z + slab, p.cols, 1, 0, nullptr, nullptr, 0, 0, 1, s));
         else if (use == HEAD_TOP) MS_TRY(head_gemm_logits(rows, cw, d, h, w, it2, (float *)p.z + slab, p.cols, part, p.rows, s));
         else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, v0, p.z_label, marks_of(p, v0, k), it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
     }

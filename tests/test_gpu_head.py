@@ -424,3 +424,13 @@ def test_a_workspace_holds_whatever_it_held(monkeypatch, dtype, d, n, vocab, k):
         for a, b in zip(ref[0], got[0]):
             assert all(torch.equal(a[x], b[x]) for x in a)
         assert all(torch.equal(a, b) for a, b in zip(ref[1], got[1]))
+
+
+# logits in tiles of 64 and of 128, ragged in every direction, and of more hidden numbers than one accumulator takes
+@pytest.mark.parametrize("n,d,vocab", [(700, 72, 1992), (1300, 136, 1032), (4100, 40, 2056), (530, 8, 2560), (290, 1032, 4104)])
+def test_many_rows_in_fp32(n, d, vocab):
+    test_log_probabilities("fp32", n, d, vocab, 0.6)
+    c = Case("fp32", n, d, vocab)
+    h, w, labels = c.dev(c.h, True), c.dev(c.w), c.dev(c.labels)
+    a, b = B.token_logprobs(h, w, labels), B.token_logprobs(h, w, labels, token_block=520)
+    assert np.all(np.abs(f64(a) - f64(b)) <= 2 * c.delta())                              # (fewer rows than a few hundred have products of another order)
