@@ -99,8 +99,10 @@ __device__ __forceinline__ bool teacher_entries(const Teacher &a, int n, long t,
     }
     return counts;
 }
-__global__ __launch_bounds__(256) void head_entries_kernel(int n, Teacher a) {
+// clear: n_clear 16-byte words (the marks, see MarkWords) that are zero afterwards
+__global__ __launch_bounds__(256) void head_entries_kernel(int n, Teacher a, float4 *__restrict__ clear, long n_clear) {
     __shared__ int seen[4][kHeadMaxTop];
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n_clear; i += 256L * gridDim.x) clear[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     teacher_entries(a, n, (long)blockIdx.x * 4 + (threadIdx.x >> 6), seen[threadIdx.x >> 6]);
 }
 
@@ -178,7 +180,7 @@ __global__ __launch_bounds__(256) void head_take_kernel(int n, int d, Teacher te
 // ------------------------------------------------------------------ rows and their selected logits
 // Copies the hidden states of the rows together, and takes the logits of each row's k selected ids (h rows . w rows, fp32); the reference of the
 // row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.  Of many entries only the teacher's
-// best is taken here (sel its id, k = 1, z_sel null): their logits come out of the matrix product, see head_marks_kernel.
+// best is taken here (sel its id, k = 1, z_sel null): their logits come out of the matrix product, see mark_entries.
 // W waves a row, four ids at a time.
 template <int W>
 __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const bf16_t *__restrict__ h, const bf16_t *__restrict__ w, const int *__restrict__ token,
@@ -226,13 +228,32 @@ __global__ __launch_bounds__(64 * W) void head_pick_kernel(int d, int k, const b
     }
 }
 
-// The same with one id a row, a label's (z_sel given) or the teacher's best, one wave per row.  FIND: the rows are found here too, instead of by head_rows_kernel (a launch
+// Marks of a row's entries (ids of its token in their order), whose logits the matrix product then leaves in z_sel; the words are zero before
+struct MarkWords {
+    int k, ld;
+    const int *ids;
+    unsigned long long *word;                                                      // [strips][ld]; null: no marks
+    unsigned char *first;
+};
+__device__ __forceinline__ void mark_entries(const MarkWords &a, int t, int row) {  // by a wave
+    const int *r = a.ids + (long)t * a.k;
+    for (int j = threadIdx.x & 63; j < a.k; j += 64) {
+        const int id = r[j], strip = id >> 6;
+        if (id < 0 || (j > 0 && r[j - 1] >> 6 == strip)) continue;              // the first of its strip writes the word
+        unsigned long long word = 0;
+        for (int i = j; i < a.k && r[i] >= 0 && r[i] >> 6 == strip; ++i) word |= 1ull << (r[i] & 63);
+        a.word[(long)strip * a.ld + row] = word;
+        a.first[(long)strip * a.ld + row] = (unsigned char)j;
+    }
+}
+
+// The same with one id a row, a label's (z_sel given) or the teacher's best, one wave per row, which marks its entries too.  FIND: the rows are found here too, instead of by head_rows_kernel (a launch
 // less): wave j is token j, and its workgroup counts the tokens before it that have rows.  For n <= kHeadFind, which is then a load of 16 keys by every thread.
 constexpr int kHeadFind = 4096;
 template <bool FIND>
 __global__ __launch_bounds__(256) void head_pick_one_kernel(int n, int d, const bf16_t *__restrict__ h, const bf16_t *__restrict__ w, const int *__restrict__ key, int limit, int *slot, int *token,
                                                             int *count, float *__restrict__ out0, float *__restrict__ out1, const int *__restrict__ sel, float it2, bf16_t *__restrict__ out,
-                                                            float *__restrict__ z_sel, float2 *__restrict__ ref) {
+                                                            float *__restrict__ z_sel, float2 *__restrict__ ref, MarkWords marks) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int row = blockIdx.x * 4 + wave, t;
     if constexpr (FIND) {
@@ -276,25 +297,10 @@ __global__ __launch_bounds__(256) void head_pick_one_kernel(int n, int d, const 
         for (int e = 0; e < 8; ++e) acc = __builtin_fmaf((float)a.v[e], (float)b.v[e], acc);
     }
     acc = wave_sum(acc);
+    if (marks.word) mark_entries(marks, t, row);
     if (lane != 0) return;
     if (z_sel) z_sel[row] = acc;
     ref[row] = make_float2(rintf(acc * it2), __int_as_float(z_sel ? id : -1));
-}
-
-// Marks of the entries of every row, whose logits the matrix product then leaves in z_sel; one wave per row, the words are zero before.
-__global__ __launch_bounds__(256) void head_marks_kernel(int ld, int k, const int *__restrict__ token, const int *__restrict__ count, const int *__restrict__ ids,
-                                                         unsigned long long *__restrict__ marks, unsigned char *__restrict__ first) {
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= *count) return;
-    const int *r = ids + (long)token[row] * k;
-    for (int j = lane; j < k; j += 64) {
-        const int id = r[j], strip = id >> 6;
-        if (id < 0 || (j > 0 && r[j - 1] >> 6 == strip)) continue;              // the first of its strip writes the word
-        unsigned long long word = 0;
-        for (int i = j; i < k && r[i] >= 0 && r[i] >> 6 == strip; ++i) word |= 1ull << (r[i] & 63);
-        marks[(long)strip * ld + row] = word;
-        first[(long)strip * ld + row] = (unsigned char)j;
-    }
 }
 
 // ------------------------------------------------------------------ sums over the vocabulary
@@ -367,6 +373,32 @@ __device__ __forceinline__ float label_after(const After &a, int t, int row, dou
     return l;
 }
 
+// What follows for a row with the teacher's entries (one wave): KL of the token, scale = loss_scale / T sum p, rho = q - p / sum p
+struct EntryRows {
+    int k;
+    const int *ids;                                                                // by token, as log_p, mass and kl
+    const float *log_p, *mass, *z_sel;
+    float it2, coef;
+    float *kl, *scale, *rho;                                                       // kl null: no entries; scale, rho null: forward only
+};
+__device__ __forceinline__ void entries_after(const EntryRows &a, int t, int row, float base, float sum) {       // sum of 2^(x - base)
+    const int lane = threadIdx.x & 63;
+    const float l2 = __log2f(sum), mass = a.mass[t], inv_mass = 1.f / mass;
+    float kl = 0.f;
+    for (int j = lane; j < a.k; j += 64) {
+        if (a.ids[(long)t * a.k + j] < 0) continue;
+        const float lp = a.log_p[(long)t * a.k + j], p = expf(lp);
+        const float zj = a.z_sel[(long)row * a.k + j], lq = kLn2 * (__builtin_fmaf(zj, a.it2, -base) - l2);
+        if (!(p == 0.f)) kl += p * (lp - lq);
+        if (a.rho) a.rho[(long)row * a.k + j] = expf(lq) - p * inv_mass;
+    }
+    kl = wave_sum(kl);
+    if (lane == 0) {
+        a.kl[t] = kl;
+        if (a.scale) a.scale[row] = a.coef * mass;
+    }
+}
+
 // ------------------------------------------------------------------ sums over the vocabulary, joined
 // Behind the vocabulary: sum of the strips' sums at a common reference.  part holds (offset, sum) of each strip [strips][ld]: stored logits' offsets are logits
 // (`unit` of x each), those of exponentials (`ref` given) count in x on top of the row's reference.  A row's strips are shared by 64 threads whatever the number
@@ -374,7 +406,7 @@ __device__ __forceinline__ float label_after(const After &a, int t, int row, dou
 // stat[row] = (sum, offset) and lse, by row, where asked for; then what follows.
 __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, int rows_per, int strips, const float2 *__restrict__ part, float unit, const float2 *__restrict__ ref,
                                                             const int *__restrict__ token, const int *__restrict__ count, const float *__restrict__ z_sel, float it2,
-                                                            float2 *__restrict__ stat, float *__restrict__ lse, After after) {
+                                                            float2 *__restrict__ stat, float *__restrict__ lse, After after, EntryRows en) {
     __shared__ float2 sm[1024];
     const int r = threadIdx.x & (rows_per - 1), g = threadIdx.x / rows_per;
     const int row = blockIdx.x * rows_per + r, n = count ? *count : rows;
@@ -403,13 +435,17 @@ __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, in
             sm[threadIdx.x] = make_float2(m, s);
         }
     }
-    if (g != 0 || row >= n) return;
-    if (stat) stat[row] = make_float2(s, m);
-    const float l2 = __log2f(s);
-    if (lse) lse[row] = kLn2 * (m * unit + l2);
-    if (after.what == AFTER_NOTHING) return;
-    label_after(after, token[row], row, x_label(after, z_sel[row]) - (ref ? (double)ref[row].x + m : (double)m * after.inv_t * kLog2e64), s,
-                __builtin_amdgcn_exp2f(ref ? __builtin_fmaf(after.z_label[row], it2, -ref[row].x) - m : (after.z_label[row] - m) * it2));
+    if (g == 0 && row < n) {
+        if (stat) stat[row] = make_float2(s, m);
+        if (lse) lse[row] = kLn2 * (m * unit + __log2f(s));
+        if (after.what != AFTER_NOTHING)
+            label_after(after, token[row], row, x_label(after, z_sel[row]) - (ref ? (double)ref[row].x + m : (double)m * after.inv_t * kLog2e64), s,
+                        __builtin_amdgcn_exp2f(ref ? __builtin_fmaf(after.z_label[row], it2, -ref[row].x) - m : (after.z_label[row] - m) * it2));
+    }
+    if (!en.kl) return;
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, mine = blockIdx.x * rows_per + wave;          // as many waves as rows
+    if (mine < n) entries_after(en, token[mine], mine, ref[mine].x + sm[wave].x, sm[wave].y);
 }
 
 // One workgroup per pair: margin, loss, and the gradient of every token of its two sequences.  Sums in 64 bits: differences of
@@ -454,35 +490,6 @@ __global__ __launch_bounds__(256) void head_pairs_kernel(const int *__restrict__
             const int row = rows.slot[t];
             if (row >= 0) rows.set(row, t < b ? g : -g, logp[t]);
         }
-}
-
-// Teacher's entries, one wave per row: KL of the token, scale = loss_scale / T sum p, rho = q - p / sum p.
-__global__ __launch_bounds__(256) void head_entry_rows_kernel(int n, int k, const int *__restrict__ slot, const int *__restrict__ ids, const float *__restrict__ log_p,
-                                                              const float *__restrict__ mass, const float *__restrict__ z_sel, const float2 *__restrict__ stat, const float2 *__restrict__ ref,
-                                                              float it2, float coef, float *__restrict__ kl, float *__restrict__ scale, float *__restrict__ rho) {
-    const int lane = threadIdx.x & 63;
-    const long t = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= n) return;
-    const int row = slot[t];
-    if (row < 0) {
-        if (lane == 0) kl[t] = 0.f;
-        return;
-    }
-    const float2 st = stat[row];
-    const float base = ref[row].x + st.y, l2 = __log2f(st.x), inv_mass = 1.f / mass[t];
-    float sum = 0.f;
-    for (int j = lane; j < k; j += 64) {
-        if (ids[t * k + j] < 0) continue;
-        const float lp = log_p[t * k + j], p = expf(lp);
-        const float zj = z_sel[(long)row * k + j], lq = kLn2 * (__builtin_fmaf(zj, it2, -base) - l2);
-        if (!(p == 0.f)) sum += p * (lp - lq);
-        if (rho) rho[(long)row * k + j] = expf(lq) - p * inv_mass;
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) {
-        kl[t] = sum;
-        if (scale) scale[row] = coef * mass[t];
-    }
 }
 
 // One workgroup of 256: the loss from its terms, in an order that only their number fixes
@@ -1152,11 +1159,11 @@ ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int k,
     return MS_OK;
 }
 
-ms_status combine(const HeadPlan &p, int rows, float unit, const float2 *ref, float it2, float2 *stat, float *lse, const After &after, const int *count, hipStream_t s) {
+ms_status combine(const HeadPlan &p, int rows, float unit, const float2 *ref, float it2, float2 *stat, float *lse, const After &after, const EntryRows &en, const int *count, hipStream_t s) {
     int per = 1;
     while (per < 16 && per < rows) per <<= 1;
     ProfScope ps(9, 8.0 * rows * p.strips, s);
-    head_combine_kernel<<<ms_cdiv(rows, per), per * 64, 0, s>>>(p.rows, rows, per, p.strips, p.part, unit, ref, p.token, count, p.z_sel, it2, stat, lse, after);
+    head_combine_kernel<<<ms_cdiv(rows, per), per * 64, 0, s>>>(p.rows, rows, per, p.strips, p.part, unit, ref, p.token, count, p.z_sel, it2, stat, lse, after, en);
     MS_LAUNCH_CHECK();
     return MS_OK;
 }
@@ -1201,7 +1208,8 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
         return MS_OK;
     }
     if (teacher.top_ids) {
-        head_entries_kernel<<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, teacher);
+        const long clear = p.marks ? (long)p.rows * p.strips / 2 : 0, most = clear / 1024 < 2048 ? clear / 1024 : 2048;      // (rows are a multiple of 16)
+        head_entries_kernel<<<(unsigned)(most > ms_cdiv(n, 4) ? most : ms_cdiv(n, 4)), 256, 0, a.s>>>(n, teacher, (float4 *)p.marks, clear);
         MS_LAUNCH_CHECK();
     }
     const bool one = p.marks || a.k == 1, find = one && n <= kHeadFind;
@@ -1215,24 +1223,17 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
         const bf16_t *hb = (const bf16_t *)h, *wb = (const bf16_t *)c->w_dev;
         const int *id = p.marks ? p.best : sel;
         float *z = p.marks ? nullptr : p.z_sel;
-        if (find) head_pick_one_kernel<true><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, hb, wb, key, limit, p.slot, p.token, p.count, out0, out1, id, it2, (bf16_t *)p.h, z, p.ref);
-        else if (one) head_pick_one_kernel<false><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, hb, wb, key, limit, p.slot, p.token, p.count, out0, out1, id, it2, (bf16_t *)p.h, z, p.ref);
+        const MarkWords marks = {a.k, p.rows, p.ids, p.marks, p.marks_first};
+        if (find) head_pick_one_kernel<true><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, hb, wb, key, limit, p.slot, p.token, p.count, out0, out1, id, it2, (bf16_t *)p.h, z, p.ref, marks);
+        else if (one) head_pick_one_kernel<false><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, hb, wb, key, limit, p.slot, p.token, p.count, out0, out1, id, it2, (bf16_t *)p.h, z, p.ref, marks);
         else if (a.k > 4) head_pick_kernel<4><<<n, 256, 0, a.s>>>(d, a.k, hb, wb, p.token, p.count, sel, it2, (bf16_t *)p.h, p.z_sel, p.ref);
         else head_pick_kernel<1><<<n, 64, 0, a.s>>>(d, a.k, hb, wb, p.token, p.count, sel, it2, (bf16_t *)p.h, p.z_sel, p.ref);
     }
     MS_LAUNCH_CHECK();
-    if (p.marks) {
-        MS_TRY(launch_fill_f32((float *)p.marks, 2L * p.rows * p.strips, 0.f, a.s));
-        head_marks_kernel<<<ms_cdiv(n, 4), 256, 0, a.s>>>(p.rows, a.k, p.token, p.count, sel, p.marks, p.marks_first);
-        MS_LAUNCH_CHECK();
-    }
     MS_TRY(logits(c, p, a.use, a.k, n, p.h, a.s));
-    MS_TRY(combine(p, n, 1.f, p.ref, it2, p.stat, nullptr, after, p.count, a.s));
-    if (labels) return MS_OK;
     const bool back = a.use == HEAD_BACKWARD;
-    head_entry_rows_kernel<<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, a.k, p.slot, p.ids, p.log_p, p.mass, p.z_sel, p.stat, p.ref, it2, en.coef, en.kl, back ? p.scale : nullptr, back ? p.rho : nullptr);
-    MS_LAUNCH_CHECK();
-    return MS_OK;
+    const EntryRows entries = {a.k, p.ids, p.log_p, p.mass, p.z_sel, it2, en.coef, en.kl, back ? p.scale : nullptr, back ? p.rho : nullptr};
+    return combine(p, n, 1.f, p.ref, it2, p.stat, nullptr, after, labels ? EntryRows{} : entries, p.count, a.s);
 }
 
 ms_status total_loss(const LossTerms &a, hipStream_t s) {
@@ -1349,7 +1350,7 @@ extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const voi
             head_strips_kernel<<<dim3(ms_cdiv(p.strips, 4), nb < 32768 ? nb : 32768), 256, 0, a.s>>>(sl, nb, p.strips, (const float *)p.z, it2, p.part);
             MS_LAUNCH_CHECK();
         }
-        if (!whole) MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, lse + t0, After{}, nullptr, a.s));
+        if (!whole) MS_TRY(combine(p, nb, it2, nullptr, it2, nullptr, lse + t0, After{}, EntryRows{}, nullptr, a.s));
         head_top_kernel<<<ms_cdiv(nb, 8) * 8, kTopThreads, 0, a.s>>>(sl, nb, p.strips, k, (const float *)p.z, whole ? nullptr : p.part, it2, lse + t0, values + (long)t0 * k, ids + (long)t0 * k);
         MS_LAUNCH_CHECK();
     }
@@ -1373,7 +1374,7 @@ extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, i
         const int nb = n - t0 < p.block ? n - t0 : p.block;
         bool dz_done = false;
         const Teacher teacher = {k, c->vocab, inv_t, top_ids + (long)t0 * k, top_logits + (long)t0 * k, lse_teacher ? lse_teacher + t0 : nullptr, p.ids, p.best, p.key, p.log_p, p.mass};
-        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, nullptr, nullptr, After{}, teacher, Entries{p.log_p, p.mass, kl + t0, c->loss_scale * inv_t}, true, &dz_done));
+        MS_TRY(rows_forward(a, t0, nb, p.key, 1, p.ids, kl + t0, nullptr, After{}, teacher, Entries{p.log_p, p.mass, kl + t0, c->loss_scale * inv_t}, true, &dz_done));
         MS_TRY(end_of_block(a, t0, nb, n, p.ids, dz_done, all));
     }
     return MS_OK;
