@@ -99,7 +99,7 @@ __device__ __forceinline__ bool teacher_entries(const Teacher &a, int n, long t,
     }
     return counts;
 }
-// clear: n_clear 16-byte words (the marks, see MarkWords) that are zero afterwards
+// 32768 tokens of 64 entries: 30 us, and the marks' 622 MB cleared beside them 115 (HBM).  clear: n_clear 16-byte words (the marks, see MarkWords) that are zero afterwards
 __global__ __launch_bounds__(256) void head_entries_kernel(int n, Teacher a, float4 *__restrict__ clear, long n_clear) {
     __shared__ int seen[4][kHeadMaxTop];
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n_clear; i += 256L * gridDim.x) clear[i] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -249,6 +249,7 @@ __device__ __forceinline__ void mark_entries(const MarkWords &a, int t, int row)
 
 // The same with one id a row, a label's (z_sel given) or the teacher's best, one wave per row, which marks its entries too.  FIND: the rows are found here too, instead of by head_rows_kernel (a launch
 // less): wave j is token j, and its workgroup counts the tokens before it that have rows.  For n <= kHeadFind, which is then a load of 16 keys by every thread.
+// HBM: 32768 rows of 1536, 302 MB, 59 us; with 64 entries to mark, whose words lie in as many cache lines, 169.
 constexpr int kHeadFind = 4096;
 template <bool FIND>
 __global__ __launch_bounds__(256) void head_pick_one_kernel(int n, int d, const bf16_t *__restrict__ h, const bf16_t *__restrict__ w, const int *__restrict__ key, int limit, int *slot, int *token,
@@ -403,7 +404,7 @@ __device__ __forceinline__ void entries_after(const EntryRows &a, int t, int row
 // Behind the vocabulary: sum of the strips' sums at a common reference.  part holds (offset, sum) of each strip [strips][ld]: stored logits' offsets are logits
 // (`unit` of x each), those of exponentials (`ref` given) count in x on top of the row's reference.  A row's strips are shared by 64 threads whatever the number
 // of rows, so that a token's sum does not depend on its batch; a workgroup takes `rows_per` rows, up to 16 (128 bytes of neighbouring rows per strip).
-// stat[row] = (sum, offset) and lse, by row, where asked for; then what follows.
+// stat[row] = (sum, offset) and lse, by row, where asked for; then what follows.  HBM: 32768 rows x 2374 strips, 622 MB, 127 us (4.9 TB/s); 1000 rows x 500 5, of latency.
 __global__ __launch_bounds__(1024) void head_combine_kernel(int ld, int rows, int rows_per, int strips, const float2 *__restrict__ part, float unit, const float2 *__restrict__ ref,
                                                             const int *__restrict__ token, const int *__restrict__ count, const float *__restrict__ z_sel, float it2,
                                                             float2 *__restrict__ stat, float *__restrict__ lse, After after, EntryRows en) {
@@ -523,7 +524,8 @@ struct Entries {
     float *kl, coef;                                                               // kl by token; dz = coef (q sum p - p)
 };
 // Everything of a row once its logits are stored: sum of exponentials, log-probabilities of the selected ids, the loss's term, and, with `dz`, the gradient of the logits in their
-// place (fp32).  G threads a row: a wave where a row is a few KB, a workgroup above.
+// place (fp32).  G threads a row: a wave where a row is a few KB, a workgroup above.  Two or three passes over a row that the caches hold: 30000 rows of 1024 26 us (sums only, 4.7 TB/s),
+// 20000 rows with their gradient 39 (4.2 TB/s read and written).
 template <int G>
 __global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, float it2, const int *__restrict__ token, const int *__restrict__ sel, float *z, const float *__restrict__ z_sel, After after,
                                                        Entries en, float2 *__restrict__ stat, float *__restrict__ scale, float *__restrict__ rho, int dz) {
@@ -645,7 +647,7 @@ __global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int v0
 // The exponentials are rounded to the storage type where they are stored, and c h here.  The selected ids with the largest gradients are most of the gradient's norm (a label's is the sum
 // of all others'), so what those two roundings take from them is put back: rest = dz - c (stored e), which d_h adds times its row of w, and dz h - (stored e) (stored c h),
 // a row that head_fix_kernel or the sorted sums of embedding_sorted.hip add to the id's row of d_w.  Error of d_w, rounded to bf16 by itself, against 64 bits: 2.9e-3 without, with
-// 1.8e-3; the rounding alone is 1.7e-3.
+// 1.8e-3; the rounding alone is 1.7e-3.  HBM: 32768 rows of 1536 with four rows to complete each, 0.6 GB, 140 us.
 __global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k, int strips, const float2 *__restrict__ part, const int *__restrict__ token, const int *__restrict__ count,
                                                          const int *__restrict__ sel, const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho,
                                                          bf16_t *__restrict__ e, bf16_t *__restrict__ h, float *__restrict__ factor, int fixes, int *__restrict__ fix_id,
@@ -885,7 +887,7 @@ __device__ __forceinline__ void row_gradient(const RowSums &a, long i, int d, bf
 }
 
 // What is left behind the gradients' products, in one launch: rows of d_w to complete (fix_blocks workgroups, fix_cols of them for each eight rows; FIX: there are some), d_h, and the
-// loss (the last workgroup).  Apart they took 15, 12 and 5 us at 2053 tokens of 1024, each of them latency.
+// loss (the last workgroup).  Apart they took 15, 12 and 5 us at 2053 tokens of 1024, each of them latency; now 17.  d_h of 32768 tokens of 1536 with four rows of w for each: 0.7 GB, 215 us.
 template <bool FIX>
 __global__ __launch_bounds__(64 * kFixWaves) void head_end_kernel(int fix_blocks, int fix_cols, int n_fix, const int *__restrict__ fix_id, const bf16_t *__restrict__ fix, float *__restrict__ d_w, RowSums rows,
                                                                   long total, int d, bf16_t *d_h, LossTerms loss) {
@@ -936,7 +938,8 @@ __device__ __forceinline__ void sort_keys(unsigned long long *key, int n) {
 
 // The k largest logits of a row, one workgroup each.  They lie in the k strips with the largest maxima (equal ones by their place): an entry of another
 // strip has k maxima before it.  So: those strips, by the bits of the k-th largest maximum (four passes over a histogram of eight bits each); their entries
-// that are not below that maximum, which are few more than k; those sorted.
+// that are not below that maximum, which are few more than k; those sorted.  One row of 151936, 64 entries: 21 us, a chain of some 30 barriers; 4096 rows 164, the same chain with four rows
+// a CU (78 MB of maxima and 70 MB of strips are read).
 constexpr int kTopKeys = 2048;                      // candidates that are sorted in LDS
 constexpr int kTopThreads = 512, kTopHeld = 8;      // strips of a thread whose maxima it keeps in registers (V up to 262144); more are read again in each pass
 __global__ __launch_bounds__(kTopThreads) void head_top_kernel(Slabs sl, int rows, int strips, int k, const float *__restrict__ z, const float2 *__restrict__ part, float it2,
