@@ -137,46 +137,6 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__res
     if (threadIdx.x == 0) *count = base;
 }
 
-// Where logits are stored, row t is token t: hidden states as they are, or zeros for a token that is left out; a label's logit (labels != null) as a dot product of its
-// own.  One wave per row, which sorts out the teacher's entries as well.
-template <class T>
-__global__ __launch_bounds__(256) void head_take_kernel(int n, int d, Teacher teacher, int limit, const int *__restrict__ labels, const T *__restrict__ h, const T *__restrict__ w,
-                                                        int *__restrict__ slot, int *__restrict__ token, float *__restrict__ out0, float *__restrict__ out1, T *__restrict__ out,
-                                                        float *__restrict__ z_sel) {
-    constexpr int N = Vec16<T>::N;
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
-    bool in;
-    if (teacher.top_ids) {
-        __shared__ int seen[4][kHeadMaxTop];
-        in = teacher_entries(teacher, n, row, seen[threadIdx.x >> 6]);
-    }
-    if (row >= n) return;
-    const int at = labels ? labels[row] : -1;
-    if (!teacher.top_ids) in = at >= 0 && at < limit;
-    if (lane == 0) {
-        slot[row] = token[row] = in ? row : -1;
-        if (out0 && !in) out0[row] = 0.f;
-        if (out1 && !in) out1[row] = 0.f;
-    }
-    const T *hr = h + (long)row * d, *wr = labels && in ? w + (long)at * d : nullptr;
-    float acc = 0.f;
-    for (int i = lane * N; i < d; i += 64 * N) {
-        Vec16<T> a;
-#pragma unroll
-        for (int e = 0; e < N; ++e) a.v[e] = from_f32<T>(0.f);
-        if (in) a = ldv(hr + i);
-        stv(out + (long)row * d + i, a);
-        if (wr) {
-            const Vec16<T> b = ldv(wr + i);
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc = __builtin_fmaf(to_f32(a.v[e]), to_f32(b.v[e]), acc);
-        }
-    }
-    if (!wr) return;
-    acc = wave_sum(acc);
-    if (lane == 0) z_sel[row] = acc;
-}
-
 // ------------------------------------------------------------------ rows and their selected logits
 // Copies the hidden states of the rows together, and takes the logits of each row's k selected ids (h rows . w rows, fp32); the reference of the
 // row's exponentials is the largest of them, as a whole power of two, so that 2^(x - reference) of a row sum to one or more.  Of many entries only the teacher's
@@ -523,15 +483,46 @@ struct Entries {
     const float *log_p, *mass;
     float *kl, coef;                                                               // kl by token; dz = coef (q sum p - p)
 };
-// Everything of a row once its logits are stored: sum of exponentials, log-probabilities of the selected ids, the loss's term, and, with `dz`, the gradient of the logits in their
-// place (fp32).  G threads a row: a wave where a row is a few KB, a workgroup above.  Two or three passes over a row that the caches hold: 30000 rows of 1024 26 us (sums only, 4.7 TB/s),
-// 20000 rows with their gradient 39 (4.2 TB/s read and written).
-template <int G>
-__global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, float it2, const int *__restrict__ token, const int *__restrict__ sel, float *z, const float *__restrict__ z_sel, After after,
-                                                       Entries en, float2 *__restrict__ stat, float *__restrict__ scale, float *__restrict__ rho, int dz) {
+// Where logits are stored, row t is token t, and a token that is left out has a row too: its hidden states may hold anything, and its logits are not looked at.
+struct RowInputs {
+    int d, limit;
+    const int *labels;                                                             // null: the teacher's entries
+    const void *h, *w;
+    void *h_out;                                                                   // hidden states for d_w, zeros for a token that is left out; null: forward only
+    int *slot, *token;
+    float *out0, *out1;                                                            // zeroed for a token that is left out
+};
+// Everything of a row once its logits are stored: its teacher's entries in their order, a label's logit as a dot product of its own, the hidden states for d_w, the sum of exponentials, the
+// log-probabilities of the selected ids, the loss's term, and, with `dz`, the gradient of the logits in their place (fp32).  G threads a row: a wave where a row is a few KB, a workgroup
+// above.  Two or three passes over logits that the caches hold: 30000 rows of 1024 33 us (sums only, 123 MB), 20000 rows with entries and gradient 48 (164 MB read and written).  Hidden states and
+// entries in a launch of their own before the product took 5.8 us of 293 tokens' 31 and 18 of 20000's 285; here they add 3 and 9.
+template <int G, class T>
+__global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, float it2, RowInputs in, Teacher teacher, const int *sel, float *z, After after, Entries en, float2 *stat, float *scale,
+                                                       float *rho, int dz) {
     __shared__ float sm[4], sh_scale;
     const int g = threadIdx.x & (G - 1), row = G == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    bool counts;
+    if (teacher.top_ids) {                                                          // (the first wave's work where a workgroup has one row)
+        __shared__ int seen[4][kHeadMaxTop], sh_counts;
+        const int wave = threadIdx.x >> 6;
+        counts = teacher_entries(teacher, n, G == 64 || wave == 0 ? row : n, seen[wave]);
+        if constexpr (G > 64) {
+            if (threadIdx.x == 0) sh_counts = counts;
+            __syncthreads();
+            counts = sh_counts;
+        } else {
+            __threadfence_block();                                                  // entries go from lane to lane through memory
+        }
+    } else {
+        const int at = row < n ? in.labels[row] : -1;
+        counts = at >= 0 && at < in.limit;
+    }
     if (row >= n) return;
+    if (g == 0) {
+        in.slot[row] = in.token[row] = counts ? row : -1;
+        if (in.out0 && !counts) in.out0[row] = 0.f;
+        if (in.out1 && !counts) in.out1[row] = 0.f;
+    }
     auto join = [&](float v, auto f, auto across) __attribute__((always_inline)) {
         v = across(v);
         if constexpr (G > 64) {
@@ -552,8 +543,27 @@ __global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, f
             for (int i = g; i < sl.vocab >> 2; i += G) f(*(float4 *)(z + sl.at(row, i * 4)));
         }
     };
-    const int t = token[row];
-    if (t < 0) {
+    constexpr int N = Vec16<T>::N;
+    const T *hr = (const T *)in.h + (long)row * in.d;
+    float z_label = 0.f;
+    if (in.h_out || (in.labels && counts)) {
+        const T *wr = in.labels && counts ? (const T *)in.w + (long)in.labels[row] * in.d : nullptr;
+        for (int i = g * N; i < in.d; i += G * N) {
+            Vec16<T> a;
+#pragma unroll
+            for (int e = 0; e < N; ++e) a.v[e] = from_f32<T>(0.f);
+            if (counts) a = ldv(hr + i);
+            if (in.h_out) stv((T *)in.h_out + (long)row * in.d + i, a);
+            if (wr) {
+                const Vec16<T> b = ldv(wr + i);
+#pragma unroll
+                for (int e = 0; e < N; ++e) z_label = __builtin_fmaf(to_f32(a.v[e]), to_f32(b.v[e]), z_label);
+            }
+        }
+        if (wr) z_label = sum_of(z_label);
+    }
+    const int t = row;
+    if (!counts) {
         if (dz) each([](float4 &a) { a = make_float4(0.f, 0.f, 0.f, 0.f); });
         if (en.kl && g == 0) en.kl[row] = 0.f;
         return;
@@ -572,7 +582,7 @@ __global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, f
     if (after.what != AFTER_NOTHING) {
         if (g == 0) {
             id[0] = sel[t];
-            const float l = label_after(after, t, row, x_label(after, z_sel[row]) - (double)m * after.inv_t * kLog2e64, s, __builtin_amdgcn_exp2f((z[sl.at(row, id[0])] - u) * it2));
+            const float l = label_after(after, t, row, x_label(after, z_label) - (double)m * after.inv_t * kLog2e64, s, __builtin_amdgcn_exp2f((z[sl.at(row, id[0])] - u) * it2));
             r[0] = expm1f(l);
             if (dz) c = after.rows.scale[row];
         }
@@ -1193,19 +1203,18 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
     const char *h = (const char *)a.h + (size_t)t0 * d * ms_dtype_size(c->dtype);
     const bool labels = after.what != AFTER_NOTHING;
     if (!p.fast) {
-        {
-            ProfScope ps(9, 0, a.s);
-            if (c->dtype == MS_F32) head_take_kernel<float><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, teacher, limit, labels ? sel : nullptr, (const float *)h, (const float *)c->w_dev, p.slot, p.token, out0, out1, (float *)p.h, p.z_sel);
-            else head_take_kernel<bf16_t><<<ms_cdiv(n, 4), 256, 0, a.s>>>(n, d, teacher, limit, labels ? sel : nullptr, (const bf16_t *)h, (const bf16_t *)c->w_dev, p.slot, p.token, out0, out1, (bf16_t *)p.h, p.z_sel);
-        }
-        MS_LAUNCH_CHECK();
-        MS_TRY(logits(c, p, a.use, a.k, n, p.h, a.s));
+        MS_TRY(logits(c, p, a.use, a.k, n, h, a.s));
         *dz_done = dz_here && c->dtype == MS_F32 && a.use == HEAD_BACKWARD;
         const Slabs sl = {p.rows, p.cols, V};
         float *scale = a.use == HEAD_BACKWARD ? p.scale : nullptr, *rho = a.use == HEAD_BACKWARD ? p.rho : nullptr;
         ProfScope ps(9, 4.0 * n * V * (*dz_done ? 2 : 1), a.s);
-#define GO(G, rows) head_row_kernel<G><<<rows, 256, 0, a.s>>>(sl, n, a.k, it2, p.token, sel, (float *)p.z, p.z_sel, after, en, p.stat, scale, rho, *dz_done)
-        if (V <= 4096) GO(64, ms_cdiv(n, 4)); else GO(256, n);
+        const RowInputs in = {d, limit, labels ? sel : nullptr, h, c->w_dev, a.use == HEAD_BACKWARD ? p.h : nullptr, p.slot, p.token, out0, out1};
+#define GO(G, T, rows) head_row_kernel<G, T><<<rows, 256, 0, a.s>>>(sl, n, a.k, it2, in, teacher, sel, (float *)p.z, after, en, p.stat, scale, rho, *dz_done)
+        if (c->dtype == MS_F32) {
+            if (V <= 4096) GO(64, float, ms_cdiv(n, 4)); else GO(256, float, n);
+        } else {
+            if (V <= 4096) GO(64, bf16_t, ms_cdiv(n, 4)); else GO(256, bf16_t, n);
+        }
 #undef GO
         MS_LAUNCH_CHECK();
         return MS_OK;
