@@ -52,5 +52,5 @@ constexpr bool head_use_marks(long k, long d, long strips) { return k > 1 && k *
 
 // pairs >= 0: a preference loss of that many pairs, all n tokens in one block
 HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws);
-long head_most_rows(const ms_head_config *c);                              // of a block
+long head_most_rows(const ms_head_config *c, HeadUse use = HEAD_BACKWARD);   // of a block
 ms_status validate_head(const ms_head_config *c, int n, int k, const char *what);

@@ -1468,8 +1468,9 @@ extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c
     }
     if (!labels) return ms_fail(MS_ERR_INVALID_ARG, "preference_loss: null pointer");
     HeadCall a;
-    if (n > head_most_rows(c)) return ms_fail(MS_ERR_UNSUPPORTED, "preference_loss: %d tokens in one block, at most %ld", n, head_most_rows(c));
-    MS_TRY(begin(&a, "preference_loss", c, n, 0, use_of(d_h, d_w), pairs, h, d_h, d_w, ws, ws_bytes, stream));
+    const HeadUse use = use_of(d_h, d_w);
+    if (n > head_most_rows(c, use)) return ms_fail(MS_ERR_UNSUPPORTED, "preference_loss: %d tokens in one block, at most %ld", n, head_most_rows(c, use));
+    MS_TRY(begin(&a, "preference_loss", c, n, 0, use, pairs, h, d_h, d_w, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     float *lp = logp ? logp : p.logp;
     bool dz_done = false;

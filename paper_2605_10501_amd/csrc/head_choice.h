@@ -2,6 +2,9 @@
 #pragma once
 #include "launch_plan.h"
 
+// Bytes of a matrix, with 256 rows more than it has, that the bf16 products reach by 32-bit offsets: what they read and what they write, which for gradients are fp32 numbers
+constexpr long kHeadReach = (1L << 32) - (1L << 20);
+
 // d_h [rows, d] = e w sums over the vocabulary, which is long, in few workgroups if there are few rows: 512 rows at d = 1536 are 12 tiles of 256 x 256 with 2374
 // K tiles each, beside the 3564 short workgroups of d_w.  So the vocabulary is cut into parts, whose sums are added when d_h is rounded: as many as give the
 // least time by the estimate of ms_choose_pair, plus what the parts cost to write and read (4.5 TB/s).  How many of the rows count is known on the device only, so it is the

@@ -69,7 +69,12 @@ GemmParams product(int M, int N, int K, const void *A, long lda, const void *B, 
     return p;
 }
 
+// Whether `rows` rows of ld numbers lie within reach of 32-bit offsets, as the plan sees to (head_plan)
+bool in_reach(long rows, long ld, int bytes) { return (rows + 256) * ld * bytes <= kHeadReach; }
+
 template <int EPI> ms_status launch_rows(GemmParams &p, double out_bytes, const int *count, hipStream_t s) {
+    if (!in_reach(p.M, p.lda, 2) || !in_reach(p.N, p.ldb, 2) || (p.C && !in_reach(p.M, p.ldc, p.c_fp32 ? 4 : 2)))
+        return ms_fail(MS_ERR_UNSUPPORTED, "head: operands or logits of %d x %d x %d beyond 4 GB", p.M, p.N, p.K);
     const int tile = count ? head_logits_tile(p.M, p.N, p.k_tiles_per_split, out_bytes, gemm_forced_tile()) : ms_choose_tile(p.M, p.N, p.k_tiles_per_split, out_bytes, gemm_forced_tile(), true);
     const MsTile &t = kTiles[tile];
     p.tiles_m = ms_cdiv(p.M, t.bm);
@@ -111,6 +116,7 @@ ms_status head_gemm_backward(const HeadChoice &c, int rows, int cw, int d, const
                              const int *count, hipStream_t s) {
     GemmParams pd = product(d_h ? rows : 0, d, cw, e, ld, w, d, d_h, d, 1, add), pw = product(cw, d, rows, e, ld, x, d, d_w, d, 1, 1);
     const MsTile &t = kTiles[c.tile];
+    if (!in_reach(rows, ld, 2) || !in_reach(cw, d, d_w ? 4 : 2) || !in_reach(rows, d, d_h ? 4 : 2)) return ms_fail(MS_ERR_UNSUPPORTED, "head: gradients of %d x %d x %d beyond 4 GB", rows, cw, d);
     pd.k_tiles_per_split = ms_cdiv(pd.k_tiles_per_split, c.parts);
     const int parts = ms_cdiv(ms_cdiv(cw, BK), pd.k_tiles_per_split);
     if (d_h && !add && parts != c.parts) return ms_fail(MS_ERR_INVALID_ARG, "head: %d parts of %d columns", c.parts, cw);   // (later slabs may add to fewer)

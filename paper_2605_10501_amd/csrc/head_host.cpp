@@ -4,7 +4,7 @@
 #include <math.h>
 
 namespace {
-constexpr long kReach = (1L << 32) - (1L << 20);        // bytes that a buffer descriptor reaches, with room for a tile past the end
+constexpr long kReach = kHeadReach;
 constexpr long kBlockBytes = 16L << 30;                 // a block's exponentials or logits, if the caller does not say (288 GB per GPU)
 constexpr long kTopBlockBytes = 4L << 30;               // the same for logits that are only looked through
 constexpr long kForwardRows = 65536;                    // tokens of a block that keeps only its strips' sums
@@ -12,18 +12,22 @@ long least(long a, long b) { return a < b ? a : b; }
 long round_up(long x, long a) { return (x + a - 1) / a * a; }
 }  // namespace
 
-long head_most_rows(const ms_head_config *c) { return least(kReach / (2L * c->hidden) - 512, kReach / (4 * 256) - 512); }
+static bool fast_products(const ms_head_config *c) { return c->dtype == MS_BF16 && c->hidden % 64 == 0 && gemm_forced_tile() >= 0; }
+// Bytes of a number of the widest matrix with rows of the hidden size that a product addresses by 32-bit offsets: gradients come out in fp32.  (The products of the other path look at their
+// operands themselves and take 64-bit ones where they have to.)
+static long widest_number(const ms_head_config *c, HeadUse use) { return use == HEAD_BACKWARD && fast_products(c) ? 4 : 2; }
+long head_most_rows(const ms_head_config *c, HeadUse use) { return least(kReach / (widest_number(c, use) * c->hidden) - 512, kReach / (4 * 256) - 512); }
 
 HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws) {
     HeadPlan p = {};
     const bool whole = pairs >= 0;
     const long V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(c->dtype);
-    p.fast = c->dtype == MS_BF16 && d % 64 == 0 && gemm_forced_tile() >= 0;
+    p.fast = fast_products(c);
     const bool keeps = use != HEAD_FORWARD || !p.fast;                       // something of every (row, vocabulary entry)
     const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
     // tokens of a block: the caller's choice, or what the memory above holds, in blocks of about equal size
-    long most = head_most_rows(c);
+    long most = head_most_rows(c, use);
     if (!whole) {
         if (c->token_block > 0) most = least(most, c->token_block);
         else if (!keeps) most = least(most, kForwardRows);
@@ -33,7 +37,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     p.block = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
     p.rows = (int)round_up(p.block, 16);                                       // (a strip's words and bytes start at 16 bytes)
     auto slabs_of = [&](long rows) {
-        long widest = kReach / (2 * d) - 512;
+        long widest = kReach / (widest_number(c, use) * d) - 512;
         if (keeps) widest = least(widest, kReach / (long)(ez * (rows + 256L)));
         widest = widest / 256 * 256;
         return (V + widest - 1) / widest;
@@ -115,7 +119,7 @@ ms_status validate_head(const ms_head_config *c, int n, int k, const char *what)
 
 static size_t bytes_of(const ms_head_config *c, int n, int k, HeadUse use, int pairs) {
     if (!c || n < 0 || c->vocab <= 0 || c->hidden <= 0 || c->hidden > 65536 || c->vocab > (1 << 24) || c->token_block < 0 || k < 0 || k > kHeadMaxTop) return 0;
-    if (pairs >= 0 && n > head_most_rows(c)) return 0;
+    if (pairs >= 0 && n > head_most_rows(c, use)) return 0;
     return head_plan(c, n, k, use, pairs, nullptr).bytes;
 }
 extern "C" size_t ms_top_logits_workspace_bytes(const ms_head_config *c, int32_t max_tokens, int32_t k) { return k < 1 ? 0 : bytes_of(c, max_tokens, k, HEAD_TOP, -1); }

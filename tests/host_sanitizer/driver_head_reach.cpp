@@ -1,0 +1,46 @@
+// Plans of the losses at the end of a section (csrc/head_host.cpp) whose gradients are 32-bit numbers: the bf16 products reach what they read and what they write by 32-bit byte offsets, up to 256
+// rows past the last one, so every slab of the lm_head and its fp32 gradient, every block of hidden states and its fp32 gradient, and every slab of what is kept between the halves of a pass
+// have to lie below 4 GB, at sizes on both sides of it; and memory for more tokens serves fewer there too.
+#include <stdio.h>
+
+#include "head.h"
+
+static int failures;
+#define CHECK(x) do { if (!(x) && ++failures < 20) printf("line %d: %s (vocab %d hidden %d block %d n %d use %d pairs %d: slabs %d cols %d rows %d)\n", __LINE__, #x, c.vocab, c.hidden, c.token_block, n, use, pairs, p.slabs, p.cols, p.rows); } while (0)
+
+int gemm_forced_tile() { return 0; }
+extern "C" size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_t d, int32_t vocab) { return n > 0 && d > 0 && vocab > 0 ? (size_t)n * 24 : 0; }
+
+int main() {
+    const struct { int vocab, hidden; } heads[] = {{152064, 8192}, {151936, 7040}, {151936, 7104}, {262144, 5376}, {262208, 5376}, {262144, 4096}, {262136, 4096}, {128256, 16384}, {256000, 12288},
+                                                   {1 << 24, 64}, {1 << 24, 65536}, {32768, 32768}, {16384, 65536}, {1024, 4096}, {32000, 4096}, {8, 65536}, {151936, 1536}};
+    const int tokens[] = {1, 64, 100, 4096, 15000, 33000, 65536, 131072, 262144, 265000, 300000, 530000, 3000000};
+    const long reach = 1L << 32;
+    long plans = 0;
+    for (auto [v, d] : heads)
+        for (int b : {0, 4096, 300000, 1 << 24})
+            for (HeadUse use : {HEAD_TOP, HEAD_FORWARD, HEAD_BACKWARD})
+                for (int whole = 0; whole < 2; ++whole) {
+                    ms_head_config c = {};
+                    c.vocab = v; c.hidden = d; c.dtype = MS_BF16; c.token_block = b; c.temperature = 1.f; c.loss_scale = 1.f; c.w_dev = (const void *)4096;
+                    size_t before = 0;
+                    for (int n : tokens) {
+                        const int k = use == HEAD_TOP ? 8 : 0, pairs = whole ? n / 2 : -1;
+                        if (whole && use == HEAD_TOP) continue;
+                        const size_t bytes = use == HEAD_TOP ? ms_top_logits_workspace_bytes(&c, n, k) : whole ? ms_preference_workspace_bytes(&c, n, pairs, use == HEAD_BACKWARD)
+                                                                                                               : ms_head_workspace_bytes(&c, n, k, use == HEAD_BACKWARD);
+                        if (whole && bytes == 0) continue;                     // (more tokens than one block takes: refused)
+                        const HeadPlan p = head_plan(&c, n, k, use, pairs, nullptr);
+                        const long r = p.rows + 256L, w = p.cols + 256L;
+                        CHECK(validate_head(&c, n, k, "plan") == MS_OK && p.fast && p.bytes == bytes && bytes >= before);
+                        before = bytes;
+                        CHECK(r * d * 2 < reach && w * d * 2 < reach);
+                        if (use == HEAD_BACKWARD) CHECK(r * d * 4 < reach && w * d * 4 < reach);
+                        if (use != HEAD_FORWARD) CHECK(r * p.cols * (use == HEAD_TOP ? 4 : 2) < reach);
+                        ++plans;
+                    }
+                }
+    if (failures) { printf("%d failures\n", failures); return 1; }
+    printf("head reach: OK (%ld)\n", plans);
+    return 0;
+}
