@@ -327,7 +327,8 @@ struct After {
 // sum it takes the place of the matrix product's, so that they go together where it is likely.  In 64 bits: logarithms of 15 summed over a sequence, and their differences.
 __device__ __forceinline__ double x_label(const After &a, float z) { return (double)z * a.inv_t * kLog2e64; }
 __device__ __forceinline__ float label_after(const After &a, int t, int row, double x, float s, float in_sum) {
-    const float l = (float)fmin(0.0, kLn264 * x - log(fmax((double)s - (double)in_sum, 0.0) + exp2(x)));
+    const double others = (double)s - (double)in_sum, v = kLn264 * x - log((others < 0.0 ? 0.0 : others) + exp2(x));       // (comparisons that a NaN passes, as fmax and fmin do not let it)
+    const float l = (float)(v > 0.0 ? 0.0 : v);
     a.logp[t] = l;
     if (a.what == AFTER_POLICY) a.rows.set(row, policy_term(a.policy, t, l), l);
     else if (a.what == AFTER_GIVEN) a.rows.set(row, a.d_logp[t], l);

@@ -1,0 +1,67 @@
+"""Ends of sections where values are not as usual: NaN among the logits of a token that counts."""
+import pytest
+import torch
+
+from paper_2605_10501_amd import binding as B
+from test_gpu_head import Case
+
+pytestmark = pytest.mark.gpu
+KINDS = [("bf16", 64), ("bf16", 40), ("fp32", 40)]
+
+
+def _calls(c, h, w, d_w=None):
+    """All losses of the case's labels, and log-probabilities, forward and backward: dicts.  Three pairs of sequences."""
+    n = c.n
+    labels, x = c.labels.cuda(), torch.full((n,), -5.0, device="cuda")
+    cu = B.Batch([0, n // 6, n // 3, n // 2, 2 * n // 3, 5 * n // 6, n])
+    ones = torch.ones(n, device="cuda")
+    return (dict(logp=B.token_logprobs(h, w, labels)), B.token_logprobs_backward(h, w, labels, ones, d_w=d_w), B.policy_loss_forward_backward(h, w, labels, x, ones, ref_logp=x, kl_coef=0.1),
+            B.preference_loss_forward_backward(h, w, labels, cu, 0.1, ref_logp=x), B.policy_loss_forward_backward(h, w, labels, x, -ones, need_d_h=False))
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("vocab", [328, 4360])
+def test_nan_in_hidden_states_of_a_token_that_counts(dtype, d, vocab):
+    c = Case(dtype, 60, d, vocab)
+    at = int(torch.nonzero(c.ok)[5])
+    pair = at // 20
+    bad = c.h.clone()
+    bad[at, d // 2] = float("nan")
+    others = torch.ones(60, dtype=torch.bool, device="cuda")
+    others[at] = False
+    fine, got = _calls(c, c.h.cuda(), c.w.cuda()), _calls(c, bad.cuda(), c.w.cuda())
+    for a, b in zip(fine, got):
+        for k in a:
+            if k == "d_h" and a[k] is not None:
+                assert torch.isnan(b[k][at]).all()
+            elif k in ("logp", "loss_tok"):
+                assert torch.isnan(b[k][at]) and torch.equal(a[k][others], b[k][others])
+            elif k == "margin":
+                assert torch.isnan(b[k][pair]) and all(torch.equal(a[k][i], b[k][i]) for i in range(3) if i != pair)
+            elif k == "loss":
+                assert torch.isnan(b[k]) and torch.isfinite(a[k])
+        if "margin" not in a and a.get("d_h") is not None:                              # (a pair's gradients all go by its margin)
+            assert torch.equal(a["d_h"][others], b["d_h"][others])
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("vocab", [328, 4360])
+@pytest.mark.parametrize("which", ["a label's", "another"])
+def test_nan_in_a_row_of_the_lm_head(dtype, d, vocab, which):
+    c = Case(dtype, 60, d, vocab)
+    ok = c.ok.cuda()
+    used = set(c.labels.tolist())
+    row = int(c.labels[c.ok][3]) if which == "a label's" else next(v for v in range(vocab // 2, vocab) if v not in used)
+    c.w[row, 0] = float("nan")
+    for out in _calls(c, c.dev(c.h, True), c.w.cuda()):
+        assert torch.isnan(out["logp"][ok]).all() and torch.all(out["logp"][~ok] == 0)
+        if "loss" in out:
+            assert torch.isnan(out["loss"])
+        if "loss_tok" in out:
+            assert torch.isnan(out["loss_tok"][ok]).all() and torch.all(out["loss_tok"][~ok] == 0)
+        if out.get("d_h") is not None:
+            assert torch.isnan(out["d_h"][ok]).all()
+    ids, top = c.labels.cuda()[:, None].contiguous(), torch.zeros(60, 1, device="cuda")
+    kd = B.topk_kd_loss_forward_backward(c.dev(c.h, True), c.w.cuda(), ids, top)
+    assert torch.isnan(kd["kl_tok"][ok]).all() and torch.all(kd["kl_tok"][~ok] == 0) and torch.isnan(kd["loss"])
+
