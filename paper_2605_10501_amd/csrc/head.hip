@@ -478,6 +478,17 @@ __device__ __forceinline__ void sum_loss(const LossTerms &a) {                  
     if (threadIdx.x == 0) *a.loss = a.scale * (sm[0] + sm[1] + sm[2] + sm[3]);
 }
 __global__ __launch_bounds__(256) void head_loss_kernel(LossTerms a) { sum_loss(a); }
+// fp32, whose d_h the product has written, zeros of dz times the lm_head for a token that is left out: NaN where the lm_head has NaN or an infinity, so those rows are set here, 16 to a workgroup.  Then the loss,
+// if it is asked for (the last workgroup).
+__global__ __launch_bounds__(256) void head_end_f32_kernel(const int *__restrict__ slot, int n, int d, float *__restrict__ d_h, LossTerms loss) {
+    if (loss.loss && blockIdx.x == gridDim.x - 1) {
+        sum_loss(loss);
+        return;
+    }
+    const int row = blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (row >= n || slot[row] >= 0) return;
+    for (int i = (threadIdx.x & 15) * 4; i < d; i += 64) *(float4 *)(d_h + (long)row * d + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+}
 
 // ------------------------------------------------------------------ rows of stored logits
 struct Entries {
@@ -1291,7 +1302,12 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool d
         else if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, sums, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
         else MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 0, a.s));
     }
-    if (dt == MS_F32) return loss.loss ? total_loss(loss, a.s) : MS_OK;
+    if (dt == MS_F32) {
+        if (!a.d_h) return loss.loss ? total_loss(loss, a.s) : MS_OK;
+        head_end_f32_kernel<<<ms_cdiv(n, 16) + (loss.loss != nullptr), 256, 0, a.s>>>(p.slot, n, d, (float *)a.d_h + (size_t)t0 * d, loss);
+        MS_LAUNCH_CHECK();
+        return MS_OK;
+    }
     const int n_fix = p.fast && a.d_w ? n * p.fixes : 0;
     if (n_fix > kHeadScan) MS_TRY(ms_k_embedding_sorted_backward(dt, n_fix, d, V, 1.f, p.fix_id, p.fix, (float *)a.d_w, p.fix_scratch, p.fix_scratch_bytes, a.s));
     const bool fix_here = n_fix > 0 && n_fix <= kHeadScan;
