@@ -30,7 +30,8 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 }
 
 // ------------------------------------------------------------------ which tokens count
-// The teacher's entries of a token, one wave each: those that count, in the order of their ids (-1 behind them), ln p of each, the sum of p, and the id of the largest.
+// The teacher's entries of a token, one wave each: those that count, in the order of their ids (-1 behind them), ln p of each, the sum of p, and the id of the largest (the lowest of equal ones:
+// it is the reference of the row's exponentials, whose roundings go by it).
 struct Teacher {
     int k, vocab;
     float inv_t;
@@ -75,7 +76,7 @@ __device__ __forceinline__ bool teacher_entries(const Teacher &a, int n, long t,
     const bool some = !(s == 0.f);                                              // an entry above -inf, or a NaN
     const float L = a.lse ? (some ? a.lse[t] : 0.f) : m + logf(s);
     float total = 0.f;
-    int valid = 0;
+    int valid = 0, best = 0x7fffffff;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const bool in = some && id[e] >= 0;
@@ -87,15 +88,20 @@ __device__ __forceinline__ bool teacher_entries(const Teacher &a, int n, long t,
         a.ids[t * k + at] = id[e];
         a.log_p[t * k + at] = lp;
         total += expf(lp);
-        if (y[e] == m) a.best[t] = id[e];                                       // (any of equal ones)
+        if (y[e] == m) best = id[e] < best ? id[e] : best;
     }
     for (int j = valid + lane; j < k; j += 64) a.ids[t * k + j] = -1;
     total = wave_sum(total);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const int other = __shfl_xor(best, o, 64);
+        best = other < best ? other : best;
+    }
     const bool counts = some && !(total == 0.f);
     if (lane == 0) {
         a.mass[t] = counts ? total : 0.f;
         a.key[t] = counts ? 0 : -1;
-        if (m == -INFINITY) a.best[t] = valid ? 0 : -1;                         // (only NaN among them)
+        a.best[t] = m == -INFINITY ? (valid ? 0 : -1) : some ? best : -1;       // (-infinity: only NaN among them)
     }
     return counts;
 }

@@ -1,4 +1,4 @@
-"""Ends of sections where values are not as usual: NaN among the logits of a token that counts."""
+"""Ends of sections where values are not as usual: NaN among the logits of a token that counts, entries of equal value."""
 import pytest
 import torch
 
@@ -65,3 +65,20 @@ def test_nan_in_a_row_of_the_lm_head(dtype, d, vocab, which):
     kd = B.topk_kd_loss_forward_backward(c.dev(c.h, True), c.w.cuda(), ids, top)
     assert torch.isnan(kd["kl_tok"][ok]).all() and torch.all(kd["kl_tok"][~ok] == 0) and torch.isnan(kd["loss"])
 
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 72), ("fp32", 72)])
+def test_order_of_equal_entries(dtype, d):
+    """A teacher's logits that are equal (they were stored in few bits): what is computed does not depend on the places they stand in.  (Sums of equal numbers are the same in any order.)"""
+    n, vocab, k = 50, 4104, 100
+    c = Case(dtype, n, d, vocab, left_out=False)
+    h, w = c.h.cuda(), c.w.cuda()
+    ids = torch.stack([torch.randperm(vocab, generator=c.g)[:k] for _ in range(n)]).to(torch.int32)
+    top = torch.full((n, k), 3.0).cuda()
+    first = None
+    for i in range(4):
+        order = torch.randperm(k, generator=c.g) if i else torch.arange(k)
+        d_w = torch.zeros(vocab, d, device="cuda")
+        out = B.topk_kd_loss_forward_backward(h, w, ids[:, order].contiguous().cuda(), top, d_w=d_w)
+        out["d_w"] = d_w
+        first = first or out
+        assert all(torch.equal(out[x], first[x]) for x in out)
