@@ -239,7 +239,7 @@ ms_status ms_top_logits(const ms_head_config *cfg, int32_t n_tokens, const void 
  *   p = e^(t / T - L),  L = lse_teacher[token] (at the same T), or, if that is NULL, ln of the sum of the token's e^(t / T) (then sum p = 1)
  *   kl_per_token = sum over the entries of p (ln p - ln q),   dz = (loss_scale / T) (q sum p - p)
  * An entry whose id is outside [0, vocab), or stands in the token's list before it, is ignored; a token without an entry (or with none
- * above -inf) is left out as above. */
+ * above -inf, or whose p sum to less than 2^-100) is left out as above. */
 ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *cfg, int32_t n_tokens, const void *h, int32_t k,
                                            const int32_t *top_ids, const float *top_logits, const float *lse_teacher,
                                            float *loss_dev, float *kl_per_token_dev, void *d_h, void *d_w,

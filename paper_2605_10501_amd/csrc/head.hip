@@ -40,6 +40,8 @@ struct Teacher {
     int *ids, *best, *key;
     float *log_p, *mass;
 };
+// Sum of p below which a token is left out: its terms are as small, and the entries' shares p / sum p, by which the gradient goes, would need 1 / sum p beyond fp32
+constexpr float kLeastMass = 0x1p-100f;
 // Token t for this wave (not below n: none), of four in the workgroup, all of which come here; returns whether the token counts
 __device__ __forceinline__ bool teacher_entries(const Teacher &a, int n, long t, int (&seen)[kHeadMaxTop]) {
     const int lane = threadIdx.x & 63, k = a.k;
@@ -97,7 +99,7 @@ __device__ __forceinline__ bool teacher_entries(const Teacher &a, int n, long t,
         const int other = __shfl_xor(best, o, 64);
         best = other < best ? other : best;
     }
-    const bool counts = some && !(total == 0.f);
+    const bool counts = some && !(total < kLeastMass);
     if (lane == 0) {
         a.mass[t] = counts ? total : 0.f;
         a.key[t] = counts ? 0 : -1;

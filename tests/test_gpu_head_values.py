@@ -1,9 +1,12 @@
-"""Ends of sections where values are not as usual: NaN among the logits of a token that counts, entries of equal value."""
+"""Ends of sections where values are not as usual: NaN among the logits of a token that counts, entries of equal value, entries that are next to nothing beside the teacher's whole
+vocabulary."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import head as oracle
 from paper_2605_10501_amd import binding as B
-from test_gpu_head import Case
+from test_gpu_head import U, Case, f64
 
 pytestmark = pytest.mark.gpu
 KINDS = [("bf16", 64), ("bf16", 40), ("fp32", 40)]
@@ -82,3 +85,30 @@ def test_order_of_equal_entries(dtype, d):
         out["d_w"] = d_w
         first = first or out
         assert all(torch.equal(out[x], first[x]) for x in out)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 72), ("fp32", 72)])
+@pytest.mark.parametrize("k", [2, 40])
+def test_entries_that_are_next_to_nothing(dtype, d, k):
+    """lse_teacher far above the entries: a token's probabilities sum to e^-away.  Its KL and its gradient go to zero with them."""
+    away = torch.tensor([0.5, 10.0, 30.0, 60.0, 69.0, 70.0, 80.0, 87.0, 88.5, 95.0, 103.0, 150.0, 1e4, 0.0])
+    n, vocab = len(away), 4104
+    c = Case(dtype, n, d, vocab, left_out=False)
+    ids = torch.stack([torch.randperm(vocab, generator=c.g)[:k] for _ in range(n)]).to(torch.int32)
+    top = c.normal((n, k), 2.0)
+    lse = torch.logsumexp(top, 1) + away
+    ref = oracle.topk_kd(f64(c.h), f64(c.w), f64(ids), f64(top), 1.0, 1.0, f64(lse))
+    h, w = c.h.cuda(), c.w.cuda()
+    d_w = torch.zeros(vocab, d, device="cuda")
+    out = B.topk_kd_loss_forward_backward(h, w, ids.cuda(), top.cuda(), lse.cuda(), loss_scale=1.0, d_w=d_w)
+    # a token's terms, each off by the logarithms' errors (of p: those of numbers as large as lse, too), of its mass; what fp32 does not hold is left out: 2^-100 of a token
+    mass, big = np.exp(-f64(away)), np.abs(f64(lse)) + 20
+    tol = mass * (c.delta() + U * (64 + 8 * big) * (1 + np.abs(f64(away)) + 20)) + 2.0 ** -100 * (big + 100)
+    assert np.all(np.abs(f64(out["kl_tok"]) - ref["kl_tok"]) <= tol)
+    got, size = f64(out["d_h"]), np.linalg.norm(f64(c.w), axis=1).max()
+    # by norm: dz of a token is off by U (64 + 8 big) of itself beside what the other tests allow, and |dz| <= 2 mass
+    for t in range(n):
+        allowed = (2.0 ** -7 if dtype == "bf16" else 40 * c.delta()) * np.linalg.norm(ref["d_h"][t]) + 2 * mass[t] * U * (64 + 8 * big[t]) * size + 2.0 ** -99 * size
+        assert np.isfinite(got[t]).all() and np.linalg.norm(got[t] - ref["d_h"][t]) <= allowed
+    got = f64(d_w)
+    assert np.isfinite(got).all() and np.linalg.norm(got - ref["d_w"]) <= (2.0 ** -7 if dtype == "bf16" else 40 * c.delta()) * np.linalg.norm(ref["d_w"])
