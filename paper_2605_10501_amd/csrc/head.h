@@ -14,6 +14,7 @@ constexpr int kStrip = 64;                   // columns that share one partial s
 struct HeadPlan {
     int block, rows, cols, slabs, strips;    // tokens of a block, rows that there is room for; strips over all slabs, cols / kStrip in each but the last
     bool fast;                               // bf16 products whose epilogue meets the logits (head_gemm.hip)
+    bool tiles;                              // the gradients are products of head_gemm.hip too (bf16)
     int *slot, *token, *count;               // [rows] row of a token, [rows] token of a row (-1: none), [1] rows in use
     void *h;                                 // [rows, hidden] hidden states of the rows, later times the row's factor
     float2 *ref;                             // [rows] reference of a row's exponentials (in x) and its label as an int (-1: it has entries)
@@ -34,7 +35,7 @@ struct HeadPlan {
     float *fix_rest;                         // [rows, fixes] what the stored gradient of the logit lacks
     void *fix, *fix_scratch;                 // [rows fixes, hidden] what d_w's row lacks; for the sum over the rows of an id
     size_t fix_scratch_bytes;
-    HeadChoice choice;                       // of the gradients' products (fast)
+    HeadChoice choice;                       // of the gradients' products (tiles)
     int parts;                               // of d_h
     float *d_h;                              // [parts, rows, hidden]
     void *z;                                 // slabs: logits (fp32), or their exponentials (bf16)

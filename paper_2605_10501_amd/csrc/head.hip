@@ -649,18 +649,16 @@ __global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, f
 }
 
 // ------------------------------------------------------------------ gradients
-// Stored fp32 logits of a slab -> their gradient (in place for fp32).  One workgroup per row.  A row without a token, or with scale 0, is zeros.
+// Stored fp32 logits of a slab -> their gradient (in place for fp32), zeros in the columns cw .. cw_zero.  One workgroup per row.  A row without a token, or with scale 0, is zeros.
 template <class T>
-__global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int v0, int k, const int *__restrict__ token, const int *__restrict__ sel, const float *z, float it2,
+__global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int cw_zero, int v0, int k, const int *__restrict__ token, const int *__restrict__ sel, const float *z, float it2,
                                                       const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho, T *dz) {
     const int row = blockIdx.x, t = token[row];
     const float *zr = z + (long)row * d_cols;
     T *o = dz + (long)row * d_cols;
     const float c = t < 0 ? 0.f : scale[row];                                   // (a row without a token has none)
-    if (c == 0.f) {
-        for (int i = threadIdx.x; i < cw; i += 256) o[i] = from_f32<T>(0.f);
-        return;
-    }
+    for (int i = (c == 0.f ? 0 : cw) + threadIdx.x; i < cw_zero; i += 256) o[i] = from_f32<T>(0.f);
+    if (c == 0.f) return;
     const float2 st = stat[row];
     const float f = c / st.x;
     for (int i = threadIdx.x; i < cw; i += 256) o[i] = from_f32<T>(f * __builtin_amdgcn_exp2f((zr[i] - st.y) * it2));
@@ -1300,15 +1298,23 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool d
         void *dz = dt == MS_F32 ? (void *)z : p.dz;
         if (!dz_done) {
             ProfScope ps(10, (4.0 + es) * n * cw, a.s);
-            if (dt == MS_F32) head_dz_kernel<float><<<n, 256, 0, a.s>>>(p.cols, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (float *)dz);
-            else head_dz_kernel<bf16_t><<<n, 256, 0, a.s>>>(p.cols, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (bf16_t *)dz);
+            if (dt == MS_F32) head_dz_kernel<float><<<n, 256, 0, a.s>>>(p.cols, cw, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (float *)dz);
+            else head_dz_kernel<bf16_t><<<n, 256, 0, a.s>>>(p.cols, cw, p.tiles ? (cw + 63) / 64 * 64 : cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (bf16_t *)dz);
         }
         MS_LAUNCH_CHECK();
         // (in fp32 the sums are the result: zeros for the tokens that are left out, whose rows of dz are)
         float *sums = dt == MS_F32 ? (float *)a.d_h + (size_t)t0 * d : p.d_h;
-        if (a.d_h && a.d_w) MS_TRY(ms_k_linear_backward(dt, n, cw, d, dz, p.cols, w, p.h, sums, 1, i > 0, d_w, a.s));
-        else if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, sums, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
-        else MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 0, a.s));
+        if (p.tiles) {
+            MS_TRY(head_gemm_backward(p.choice, n, cw, d, dz, p.cols, w, p.h, a.d_h ? p.d_h : nullptr, i > 0, d_w, nullptr, a.s));
+            continue;
+        }
+        if (dt == MS_F32 && a.d_h && a.d_w) {
+            MS_TRY(ms_k_linear_backward(dt, n, cw, d, dz, p.cols, w, p.h, sums, 1, i > 0, d_w, a.s));
+            continue;
+        }
+        // (K in one piece: bf16 pieces would be added up by atomics, in any order)
+        if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, sums, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
+        if (a.d_w) MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 1, a.s));
     }
     if (dt == MS_F32) {
         if (!a.d_h) return loss.loss ? total_loss(loss, a.s) : MS_OK;

@@ -12,10 +12,9 @@ long least(long a, long b) { return a < b ? a : b; }
 long round_up(long x, long a) { return (x + a - 1) / a * a; }
 }  // namespace
 
-static bool fast_products(const ms_head_config *c) { return c->dtype == MS_BF16 && c->hidden % 64 == 0 && gemm_forced_tile() >= 0; }
-// Bytes of a number of the widest matrix with rows of the hidden size that a product addresses by 32-bit offsets: gradients come out in fp32.  (The products of the other path look at their
+// Bytes of a number of the widest matrix with rows of the hidden size that a product addresses by 32-bit offsets: gradients come out in fp32.  (fp32 products look at their
 // operands themselves and take 64-bit ones where they have to.)
-static long widest_number(const ms_head_config *c, HeadUse use) { return use == HEAD_BACKWARD && fast_products(c) ? 4 : 2; }
+static long widest_number(const ms_head_config *c, HeadUse use) { return use == HEAD_BACKWARD && c->dtype == MS_BF16 ? 4 : 2; }
 long head_most_rows(const ms_head_config *c, HeadUse use) { return least(kReach / (widest_number(c, use) * c->hidden) - 512, kReach / (4 * 256) - 512); }
 
 HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws) {
@@ -23,7 +22,9 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     const bool whole = pairs >= 0;
     const long V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(c->dtype);
-    p.fast = fast_products(c);
+    const bool bf16_tiles = c->dtype == MS_BF16 && gemm_forced_tile() >= 0;
+    p.fast = bf16_tiles && d % 64 == 0;
+    p.tiles = bf16_tiles && use == HEAD_BACKWARD;
     const bool keeps = use != HEAD_FORWARD || !p.fast;                       // something of every (row, vocabulary entry)
     const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
     // tokens of a block: the caller's choice, or what the memory above holds, in blocks of about equal size
@@ -44,7 +45,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     };
     p.slabs = (int)slabs_of(p.rows);
     p.cols = p.slabs == 1 ? (int)V : (int)round_up((V + p.slabs - 1) / p.slabs, 256);
-    if (p.fast) p.cols = (int)round_up(p.cols, 64);                          // (d_h's product reads whole K tiles)
+    if (p.fast || p.tiles) p.cols = (int)round_up(p.cols, 64);               // (d_h's product reads whole K tiles)
     p.strips = (int)((V + kStrip - 1) / kStrip);
     // What is taken is for the largest block of calls up to this one, so that memory for n tokens serves fewer (97 tokens in blocks of at most 80 are two of 56)
     const size_t r = (size_t)round_up(least(n, most), 16);
@@ -79,9 +80,11 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
         p.scale = a.take<float>(r * 4);
         p.factor = a.take<float>(r * 4);
         p.parts = 1;
-        if (p.fast) {
+        if (p.tiles) {
             p.choice = head_choose(p.block, V < p.cols ? V : p.cols, d, gemm_forced_tile());
             p.parts = p.choice.parts;
+        }
+        if (p.fast) {
             p.fixes = k < 1 ? 1 : k < kHeadFixes ? k : kHeadFixes;
             const size_t f = r * p.fixes;
             p.fix_id = a.take<int>(f * 4);
@@ -93,7 +96,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
             }
         }
         const long sums = (long)r * d, in_parts = least(kHeadMostParts * sums, kHeadPartsRoom);
-        if (c->dtype == MS_BF16) p.d_h = a.take<float>((p.fast && in_parts > sums ? in_parts : sums) * 4);
+        if (c->dtype == MS_BF16) p.d_h = a.take<float>((p.tiles && in_parts > sums ? in_parts : sums) * 4);
         if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(least((long)r * (V + 256), kReach / 4) * 2);
     }
     if (keeps) p.z = a.take<void>(r * (V + 257 * slabs_of((long)r)) * ez);

@@ -13,7 +13,7 @@ extern "C" size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_
 
 int main() {
     const struct { int vocab, hidden; } heads[] = {{152064, 8192}, {151936, 7040}, {151936, 7104}, {262144, 5376}, {262208, 5376}, {262144, 4096}, {262136, 4096}, {128256, 16384}, {256000, 12288},
-                                                   {1 << 24, 64}, {1 << 24, 65536}, {32768, 32768}, {16384, 65536}, {1024, 4096}, {32000, 4096}, {8, 65536}, {151936, 1536}};
+                                                   {1 << 24, 64}, {1 << 24, 65536}, {32768, 32768}, {16384, 65536}, {1024, 4096}, {32000, 4096}, {8, 65536}, {151936, 1536}, {151936, 7112}, {1024, 4104}};
     const int tokens[] = {1, 64, 100, 4096, 15000, 33000, 65536, 131072, 262144, 265000, 300000, 530000, 3000000};
     const long reach = 1L << 32;
     long plans = 0;
@@ -32,11 +32,11 @@ int main() {
                         if (whole && bytes == 0) continue;                     // (more tokens than one block takes: refused)
                         const HeadPlan p = head_plan(&c, n, k, use, pairs, nullptr);
                         const long r = p.rows + 256L, w = p.cols + 256L;
-                        CHECK(validate_head(&c, n, k, "plan") == MS_OK && p.fast && p.bytes == bytes && bytes >= before);
+                        CHECK(validate_head(&c, n, k, "plan") == MS_OK && p.fast == (d % 64 == 0) && p.bytes == bytes && bytes >= before);
                         before = bytes;
                         CHECK(r * d * 2 < reach && w * d * 2 < reach);
                         if (use == HEAD_BACKWARD) CHECK(r * d * 4 < reach && w * d * 4 < reach);
-                        if (use != HEAD_FORWARD) CHECK(r * p.cols * (use == HEAD_TOP ? 4 : 2) < reach);
+                        if (use != HEAD_FORWARD || !p.fast) CHECK(r * p.cols * (use == HEAD_TOP || !p.fast ? 4 : 2) < reach);
                         ++plans;
                     }
                 }

@@ -1,5 +1,5 @@
 """Ends of sections where values are not as usual: NaN among the logits of a token that counts, entries of equal value, entries that are next to nothing beside the teacher's whole
-vocabulary."""
+vocabulary; and the same bits from the same call where many tokens meet a small lm_head."""
 import numpy as np
 import pytest
 import torch
@@ -112,3 +112,16 @@ def test_entries_that_are_next_to_nothing(dtype, d, k):
         assert np.isfinite(got[t]).all() and np.linalg.norm(got[t] - ref["d_h"][t]) <= allowed
     got = f64(d_w)
     assert np.isfinite(got).all() and np.linalg.norm(got - ref["d_w"]) <= (2.0 ** -7 if dtype == "bf16" else 40 * c.delta()) * np.linalg.norm(ref["d_w"])
+
+
+@pytest.mark.parametrize("n,d,vocab", [(20000, 72, 1032), (20000, 72, 1024), (9000, 40, 4104), (20000, 128, 1032)])
+def test_many_tokens_of_a_small_lm_head_have_the_same_bits(n, d, vocab):
+    c = Case("bf16", n, d, vocab)
+    g = c.normal((n,)).cuda()
+    h, w, labels = c.dev(c.h, True), c.w.cuda(), c.labels.cuda()
+    first = None
+    for need in (True, True, True, False, False):
+        d_w = torch.zeros(vocab, d, device="cuda")
+        out = B.token_logprobs_backward(h, w, labels, g, d_w=d_w, need_d_h=need)
+        first = first or (out, d_w)
+        assert torch.equal(d_w, first[1]) and torch.equal(out["logp"], first[0]["logp"]) and (not need or torch.equal(out["d_h"], first[0]["d_h"]))
