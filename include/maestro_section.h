@@ -211,6 +211,7 @@ ms_status ms_kd_loss_forward_backward_static(const ms_kd_config *kd, int32_t n_t
  *     inputs may hold anything there, NaN included.
  *   - d_h (storage type, [n_tokens, hidden]) is overwritten, and may be h itself; d_w (fp32, [vocab, hidden]) is accumulated.  Otherwise they must not overlap
  *     what is read, or each other.  Either may be NULL; both NULL: forward only.  loss_dev: device float.
+ *   - The other outputs and the workspace must not overlap anything that the call reads or writes (MS_ERR_INVALID_ARG).
  *   - Sums run in an order that the sizes alone fix: the same call gives the same bits.  A token's loss and log-probability do not depend on what it is packed with
  *     (fp32: apart from which of two products a call takes, by its tokens x vocab: up to about a million, and above).
  *   - A bf16 head keeps e^(z - reference) of a block's tokens (bf16, [tokens, vocab]) between the two halves of the pass instead of computing the logits

@@ -3,6 +3,8 @@
 // With x = z log2(e), z = h w^T / T the logits of a row (a token that counts), everything goes by sums of 2^(x - reference) over strips of 64 columns:
 //   lse = ln 2 (reference + log2 sum),   q_v = 2^(x_v - reference) / sum,   dz_v = scale_row q_v but at the few selected ids of the row
 // (its label, or the teacher's entries), where rho = dz / scale_row is q - 1 or q - p / sum p.  The logits there are dot products of their own.
+#include <initializer_list>
+
 #include "common.h"
 #include "head.h"
 #include "head_f32.h"
@@ -1340,15 +1342,23 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool d
 
 bool aligned(const void *q, int by) { return ((uintptr_t)q & (by - 1)) == 0; }
 
+// What a call reads and writes beside the hidden states, the lm_head, their gradients and the workspace
+struct Span {
+    const void *at;                                                                // null: not given
+    size_t bytes;
+};
+Span span(const void *at, long numbers) { return {at, (size_t)numbers * 4}; }
+bool apart(const Span &x, const Span &y) { return !x.at || !y.at || (const char *)x.at + x.bytes <= (const char *)y.at || (const char *)y.at + y.bytes <= (const char *)x.at; }
+
 // Arguments that all calls have
-ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, int k, HeadUse use, int pairs, const void *h, void *d_h, void *d_w,
-                void *ws, size_t ws_bytes, void *stream) {
+ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, int k, HeadUse use, int pairs, const void *h, void *d_h, void *d_w, std::initializer_list<Span> reads,
+                std::initializer_list<Span> writes, void *ws, size_t ws_bytes, void *stream) {
     if (n && (!h || !ws)) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer", what);
     if (!aligned(h, 16) || !aligned(c->w_dev, 16) || !aligned(d_h, 16) || !aligned(d_w, 16) || !aligned(ws, 16))
         return ms_fail(MS_ERR_UNSUPPORTED, "%s: hidden states, lm_head, their gradients and the workspace must be 16-byte aligned", what);
-    const size_t hb = (size_t)n * c->hidden * ms_dtype_size(c->dtype), wb = (size_t)c->vocab * c->hidden * ms_dtype_size(c->dtype), db = (size_t)c->vocab * c->hidden * 4;
-    auto apart = [](const void *x, size_t xb, const void *y, size_t yb) { return !x || !y || (const char *)x + xb <= (const char *)y || (const char *)y + yb <= (const char *)x; };
-    if ((d_h != h && !apart(d_h, hb, h, hb)) || !apart(d_h, hb, c->w_dev, wb) || !apart(d_h, hb, d_w, db) || !apart(d_w, db, h, hb) || !apart(d_w, db, c->w_dev, wb))
+    const size_t hb = (size_t)n * c->hidden * ms_dtype_size(c->dtype), wb = (size_t)c->vocab * c->hidden * ms_dtype_size(c->dtype);
+    const Span states = {h, hb}, lm_head = {c->w_dev, wb}, d_states = {d_h, hb}, d_lm_head = span(d_w, (long)c->vocab * c->hidden);
+    if ((d_h != h && !apart(d_states, states)) || !apart(d_states, lm_head) || !apart(d_states, d_lm_head) || !apart(d_lm_head, states) || !apart(d_lm_head, lm_head))
         return ms_fail(MS_ERR_INVALID_ARG, "%s: d_h may be h, else the gradients must not overlap the hidden states, the lm_head or each other", what);
     a->c = c;
     a->use = use;
@@ -1357,7 +1367,18 @@ ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, i
     a->s = (hipStream_t)stream;
     a->p = head_plan(c, n, k, use, pairs, ws);
     if (n && ws_bytes < a->p.bytes) return ms_fail(MS_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", what, ws_bytes, a->p.bytes);
-    return MS_OK;
+    // the workspace and the other outputs: apart from everything else
+    const Span space = {ws, a->p.bytes}, large[] = {states, lm_head, d_states, d_lm_head};
+    bool clear = true;
+    for (const Span &x : large) clear = clear && apart(space, x);
+    for (const Span &x : reads) clear = clear && apart(space, x) && apart(d_states, x) && apart(d_lm_head, x);
+    for (const Span *x = writes.begin(); x != writes.end(); ++x) {
+        clear = clear && apart(*x, space);
+        for (const Span &y : large) clear = clear && apart(*x, y);
+        for (const Span &y : reads) clear = clear && apart(*x, y);
+        for (const Span *y = writes.begin(); y != x; ++y) clear = clear && apart(*x, *y);
+    }
+    return clear ? MS_OK : ms_fail(MS_ERR_INVALID_ARG, "%s: outputs and workspace must not overlap each other or what the call reads", what);
 }
 HeadUse use_of(const void *d_h, const void *d_w) { return d_h || d_w ? HEAD_BACKWARD : HEAD_FORWARD; }
 
@@ -1381,7 +1402,7 @@ extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const voi
     if (n == 0) return MS_OK;
     if (!values || !ids || !lse) return ms_fail(MS_ERR_INVALID_ARG, "top_logits: null pointer");
     HeadCall a;
-    MS_TRY(begin(&a, "top_logits", c, n, k, HEAD_TOP, -1, h, nullptr, nullptr, ws, ws_bytes, stream));
+    MS_TRY(begin(&a, "top_logits", c, n, k, HEAD_TOP, -1, h, nullptr, nullptr, {}, {span(values, (long)n * k), span(ids, (long)n * k), span(lse, n)}, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     const float it2 = kLog2e / c->temperature;
     const bool whole = !p.fast && c->vocab <= kTopKeys;                            // a row is looked through at once, without sums of strips
@@ -1408,7 +1429,8 @@ extern "C" ms_status ms_topk_kd_loss_forward_backward(const ms_head_config *c, i
     if (n == 0) return launch_fill_f32(loss, 1, 0.f, (hipStream_t)stream);
     if (!top_ids || !top_logits) return ms_fail(MS_ERR_INVALID_ARG, "topk_kd: null pointer");
     HeadCall a;
-    MS_TRY(begin(&a, "topk_kd", c, n, k, use_of(d_h, d_w), -1, h, d_h, d_w, ws, ws_bytes, stream));
+    MS_TRY(begin(&a, "topk_kd", c, n, k, use_of(d_h, d_w), -1, h, d_h, d_w, {span(top_ids, (long)n * k), span(top_logits, (long)n * k), span(lse_teacher, n)}, {span(loss, 1), span(kl_tok, n)},
+                 ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     const float inv_t = 1.f / c->temperature;
     float *kl = kl_tok ? kl_tok : p.per_token;
@@ -1430,7 +1452,7 @@ static ms_status token_logprobs(const char *what, const ms_head_config *c, int n
     const bool back = d_logp != nullptr;
     if (!labels) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer", what);
     HeadCall a;
-    MS_TRY(begin(&a, what, c, n, 0, back ? HEAD_BACKWARD : HEAD_FORWARD, -1, h, d_h, d_w, ws, ws_bytes, stream));
+    MS_TRY(begin(&a, what, c, n, 0, back ? HEAD_BACKWARD : HEAD_FORWARD, -1, h, d_h, d_w, {span(labels, n), span(d_logp, n)}, {span(logp, n)}, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     for (int t0 = 0; t0 < n; t0 += p.block) {
         const int nb = n - t0 < p.block ? n - t0 : p.block;
@@ -1462,7 +1484,8 @@ extern "C" ms_status ms_policy_loss_forward_backward(const ms_head_config *c, co
     if (n == 0) return launch_fill_f32(loss, 1, 0.f, (hipStream_t)stream);
     if (!labels || !old_logp || !advantages) return ms_fail(MS_ERR_INVALID_ARG, "policy_loss: null pointer");
     HeadCall a;
-    MS_TRY(begin(&a, "policy_loss", c, n, 0, use_of(d_h, d_w), -1, h, d_h, d_w, ws, ws_bytes, stream));
+    MS_TRY(begin(&a, "policy_loss", c, n, 0, use_of(d_h, d_w), -1, h, d_h, d_w, {span(labels, n), span(old_logp, n), span(ref_logp, n), span(advantages, n), span(weights, n)},
+                 {span(loss, 1), span(loss_tok, n), span(logp, n)}, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     float *terms = loss_tok ? loss_tok : p.per_token;
     const LossTerms all = {terms, n, c->loss_scale, loss};
@@ -1501,7 +1524,8 @@ extern "C" ms_status ms_preference_loss_forward_backward(const ms_head_config *c
     HeadCall a;
     const HeadUse use = use_of(d_h, d_w);
     if (n > head_most_rows(c, use)) return ms_fail(MS_ERR_UNSUPPORTED, "preference_loss: %d tokens in one block, at most %ld", n, head_most_rows(c, use));
-    MS_TRY(begin(&a, "preference_loss", c, n, 0, use, pairs, h, d_h, d_w, ws, ws_bytes, stream));
+    MS_TRY(begin(&a, "preference_loss", c, n, 0, use, pairs, h, d_h, d_w, {span(labels, n), span(ref_logp, n), span(batch->cu_seqlens_dev, batch->n_seqs + 1L)},
+                 {span(loss, 1), span(margin, pairs), span(logp, n)}, ws, ws_bytes, stream));
     const HeadPlan &p = a.p;
     float *lp = logp ? logp : p.logp;
     bool dz_done = false;
