@@ -216,7 +216,7 @@ ms_status ms_kd_loss_forward_backward_static(const ms_kd_config *kd, int32_t n_t
  *     (fp32: apart from which of two products a call takes, by its tokens x vocab: up to about a million, and above).
  *   - A bf16 head keeps e^(z - reference) of a block's tokens (bf16, [tokens, vocab]) between the two halves of the pass instead of computing the logits
  *     twice; that is where the gradient of the logits is rounded to the storage type.  token_block: the tokens of a block (a multiple of 8;
- *     0: as many as 16 GB hold).  A preference loss has all its tokens in one block.
+ *     0: as many as 16 GB hold, at most 65536 where the hidden size is a multiple of 64).  A preference loss has all its tokens in one block.
  *   - vocab and hidden: multiples of 8.  Alignment: 16 bytes for h, w, d_h and d_w, else 4.  Refused (MS_ERR_UNSUPPORTED) otherwise.
  * n_tokens == 0: a loss of 0. */
 typedef struct {

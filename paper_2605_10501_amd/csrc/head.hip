@@ -117,7 +117,7 @@ __global__ __launch_bounds__(256) void head_entries_kernel(int n, Teacher a, flo
 }
 
 // Rows of a block: the tokens that count (key in [0, limit)) in their order, without gaps; out0, out1 of the others are 0.  One workgroup: a block has at most
-// some 10^5 tokens, of which it reads four bytes.
+// 65536 tokens, of which it reads four bytes (if the caller does not ask for longer ones; a preference loss, whose tokens are one block, up to some million, 1024 at a time).
 __global__ __launch_bounds__(1024) void head_rows_kernel(int n, const int *__restrict__ key, int limit, int *__restrict__ slot, int *__restrict__ token, int *__restrict__ count,
                                                          float *__restrict__ out0, float *__restrict__ out1) {
     __shared__ int sm[16];

@@ -7,7 +7,9 @@ namespace {
 constexpr long kReach = kHeadReach;
 constexpr long kBlockBytes = 16L << 30;                 // a block's exponentials or logits, if the caller does not say (288 GB per GPU)
 constexpr long kTopBlockBytes = 4L << 30;               // the same for logits that are only looked through
-constexpr long kForwardRows = 65536;                    // tokens of a block that keeps only its strips' sums
+// Tokens of a block of the fast products, whose rows one workgroup finds (head_rows_kernel): 300000 tokens of V = 8192, d = 256 forward and backward in one block 10.36 ms, so 6.97; 2 million of V = 1024, d = 128
+// 20.3 and 17.8; 131072 of V = 32000, d = 1024 21.4 with both, in blocks of 32768 21.7
+constexpr long kBlockRows = 65536;
 long least(long a, long b) { return a < b ? a : b; }
 long round_up(long x, long a) { return (x + a - 1) / a * a; }
 }  // namespace
@@ -29,10 +31,10 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
     // tokens of a block: the caller's choice, or what the memory above holds, in blocks of about equal size
     long most = head_most_rows(c, use);
-    if (!whole) {
-        if (c->token_block > 0) most = least(most, c->token_block);
-        else if (!keeps) most = least(most, kForwardRows);
-        else most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
+    if (!whole && c->token_block > 0) most = least(most, c->token_block);
+    else if (!whole) {
+        if (p.fast && use != HEAD_TOP) most = least(most, kBlockRows);
+        if (keeps) most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
     }
     const long blocks = whole || n <= most ? 1 : (n + most - 1) / most;
     p.block = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));

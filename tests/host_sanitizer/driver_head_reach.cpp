@@ -37,6 +37,7 @@ int main() {
                         CHECK(r * d * 2 < reach && w * d * 2 < reach);
                         if (use == HEAD_BACKWARD) CHECK(r * d * 4 < reach && w * d * 4 < reach);
                         if (use != HEAD_FORWARD || !p.fast) CHECK(r * p.cols * (use == HEAD_TOP || !p.fast ? 4 : 2) < reach);
+                        if (p.fast && use != HEAD_TOP && b == 0 && !whole) CHECK(p.block <= 65536);       // (one workgroup finds its rows)
                         ++plans;
                     }
                 }
