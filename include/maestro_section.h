@@ -215,10 +215,14 @@ ms_status ms_kd_loss_forward_backward_static(const ms_kd_config *kd, int32_t n_t
  *   - Sums run in an order that the sizes alone fix: the same call gives the same bits.  A token's loss and log-probability do not depend on what it is packed with
  *     (fp32: apart from which of two products a call takes, by its tokens x vocab: up to about a million, and above).
  *   - A bf16 head keeps e^(z - reference) of a block's tokens (bf16, [tokens, vocab]) between the two halves of the pass instead of computing the logits
- *     twice; that is where the gradient of the logits is rounded to the storage type.  token_block: the tokens of a block (a multiple of 8;
+ *     twice.  So the gradient of the logits is rounded to the storage type: where the exponentials are stored, and, for d_w, once more with the hidden states of the token that the
+ *     token's factor is put on (but for the four selected ids of a token with the largest gradients, which are completed in fp32; d_w against 64 bits: 1e-5 of it from labels, up to 1.3e-3
+ *     from many entries of a token).  With MS_HEAD_FP32_DZ added to dtype MS_BF16 the gradient of the logits is kept in fp32's place as two bf16 numbers, rounded to 2^-16 of itself, at about twice the time (logits
+ *     stored in fp32, two pairs of products).  A hidden size that is no multiple of 64 rounds it once without that.  token_block: the tokens of a block (a multiple of 8;
  *     0: as many as 16 GB hold, at most 65536 where the hidden size is a multiple of 64).  A preference loss has all its tokens in one block.
  *   - vocab and hidden: multiples of 8.  Alignment: 16 bytes for h, w, d_h and d_w, else 4.  Refused (MS_ERR_UNSUPPORTED) otherwise.
  * n_tokens == 0: a loss of 0. */
+#define MS_HEAD_FP32_DZ 256
 typedef struct {
     int32_t vocab, hidden, dtype, token_block;
     float temperature;             /* T                                                */

@@ -755,6 +755,10 @@ def k_gemm_fp8_swiglu(a, sa, w, sw, fp32_sums=False):
 
 
 # ------------------------------------------------------------------ losses and log-probabilities at the end of a section
+# fp32_dz of the calls with gradients: a bf16 head keeps the gradient of its logits as two bf16 numbers instead of one (rounded to 2^-16 of itself), at about twice the time
+_FP32_DZ = 256
+
+
 class _HeadCfg(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("vocab", "hidden", "dtype", "token_block")] + [("temperature", C.c_float), ("loss_scale", C.c_float), ("w_dev", C.c_void_p)]
 
@@ -767,14 +771,19 @@ class _PreferenceCfg(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("beta", "label_smoothing")]
 
 
-def _head(h, w, temperature, loss_scale, token_block, need_d_h=False, d_w=None):
+def _head(h, w, temperature, loss_scale, token_block, need_d_h=False, d_w=None, fp32_dz=False):
     """(config, tokens, d_h or None), arguments checked."""
     _need("h", h, _STORE, (None, None), None)
     _need("w", w, (h.dtype,), (None, h.shape[1]), h.device)
     if d_w is not None:
         _need("d_w", d_w, _F32, w.shape, h.device)
-    c = _HeadCfg(w.shape[0], w.shape[1], _dt(h.dtype), int(token_block), float(temperature), float(loss_scale), w.data_ptr())
+    c = _HeadCfg(w.shape[0], w.shape[1], _head_dt(h.dtype, fp32_dz), int(token_block), float(temperature), float(loss_scale), w.data_ptr())
     return c, h.shape[0], torch.empty_like(h) if need_d_h else None
+
+
+def _head_dt(dtype, fp32_dz):
+    """With fp32_dz for a bf16 head (fp32 heads keep the gradient of their logits in fp32 anyway)."""
+    return _dt(dtype) | (_FP32_DZ if fp32_dz and dtype == torch.bfloat16 else 0)
 
 
 def _per_token(dev, n, **named):
@@ -794,9 +803,9 @@ def _head_ws(ws, query, c, *args, device):
     return ws
 
 
-def head_workspace_bytes(w, max_tokens, k=0, need_backward=True, token_block=0):
+def head_workspace_bytes(w, max_tokens, k=0, need_backward=True, token_block=0, fp32_dz=False):
     """Workspace of the calls with labels (k = 0) or with k entries per token."""
-    c = _HeadCfg(w.shape[0], w.shape[1], _dt(w.dtype), int(token_block), 1.0, 1.0, w.data_ptr())
+    c = _HeadCfg(w.shape[0], w.shape[1], _head_dt(w.dtype, fp32_dz), int(token_block), 1.0, 1.0, w.data_ptr())
     return _fn("ms_head_workspace_bytes")(C.byref(c), max_tokens, k, int(need_backward))
 
 
@@ -811,12 +820,12 @@ def top_logits(h, w, k, temperature=1.0, token_block=0, ws=None):
     return values, ids, lse
 
 
-def topk_kd_loss_forward_backward(h, w, top_ids, top_logits, lse_teacher=None, temperature=1.0, loss_scale=None, need_d_h=True, d_w=None, token_block=0, ws=None):
+def topk_kd_loss_forward_backward(h, w, top_ids, top_logits, lse_teacher=None, temperature=1.0, loss_scale=None, need_d_h=True, d_w=None, token_block=0, ws=None, fp32_dz=False):
     """Distillation from a teacher's stored logits (top_ids int32, top_logits fp32, [n, k]; ids outside the vocabulary or repeated are ignored).
     lse_teacher: log-sum-exp of the teacher's whole vocabulary at T; without it the entries' probabilities sum to 1.  Returns dict(loss, kl_tok, d_h);
     d_w (fp32, as w) is accumulated in place.  loss_scale: 1 / n by default."""
     n = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
-    c, n, d_h = _head(h, w, temperature, 1.0 / max(n, 1) if loss_scale is None else loss_scale, token_block, need_d_h, d_w)
+    c, n, d_h = _head(h, w, temperature, 1.0 / max(n, 1) if loss_scale is None else loss_scale, token_block, need_d_h, d_w, fp32_dz)
     dev = h.device
     _need("top_ids", top_ids, _I32, (n, None), dev)
     k = top_ids.shape[1]
@@ -840,9 +849,9 @@ def token_logprobs(h, w, labels, temperature=1.0, token_block=0, ws=None):
     return logp
 
 
-def token_logprobs_backward(h, w, labels, d_logp, temperature=1.0, need_d_h=True, d_w=None, token_block=0, ws=None):
+def token_logprobs_backward(h, w, labels, d_logp, temperature=1.0, need_d_h=True, d_w=None, token_block=0, ws=None, fp32_dz=False):
     """Gradients of sum(d_logp * token_logprobs(h, w, labels)): dict(logp, d_h); d_w (fp32, as w) is accumulated in place."""
-    c, n, d_h = _head(h, w, temperature, 1.0, token_block, need_d_h, d_w)
+    c, n, d_h = _head(h, w, temperature, 1.0, token_block, need_d_h, d_w, fp32_dz)
     dev = h.device
     _need("labels", labels, _I32, (n,), dev)
     _need("d_logp", d_logp, _F32, (n,), dev)
@@ -853,11 +862,11 @@ def token_logprobs_backward(h, w, labels, d_logp, temperature=1.0, need_d_h=True
 
 
 def policy_loss_forward_backward(h, w, labels, old_logp, advantages, clip_low=0.2, clip_high=0.2, ref_logp=None, kl_coef=0.0, weights=None, temperature=1.0,
-                                 loss_scale=None, need_d_h=True, d_w=None, token_block=0, ws=None):
+                                 loss_scale=None, need_d_h=True, d_w=None, token_block=0, ws=None, fp32_dz=False):
     """Clipped policy loss over the tokens with a label inside the vocabulary, with a KL term towards ref_logp if kl_coef > 0; all per-token inputs fp32.
     Returns dict(loss, loss_tok, logp, d_h); d_w (fp32, as w) is accumulated in place.  loss_scale: 1 / n by default."""
     n = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
-    c, n, d_h = _head(h, w, temperature, 1.0 / max(n, 1) if loss_scale is None else loss_scale, token_block, need_d_h, d_w)
+    c, n, d_h = _head(h, w, temperature, 1.0 / max(n, 1) if loss_scale is None else loss_scale, token_block, need_d_h, d_w, fp32_dz)
     dev = h.device
     _need("labels", labels, _I32, (n,), dev)
     _need("old_logp", old_logp, _F32, (n,), dev)
@@ -872,11 +881,11 @@ def policy_loss_forward_backward(h, w, labels, old_logp, advantages, clip_low=0.
     return dict(loss=loss, loss_tok=loss_tok, logp=logp, d_h=d_h)
 
 
-def preference_loss_forward_backward(h, w, labels, batch, beta, ref_logp=None, label_smoothing=0.0, temperature=1.0, loss_scale=None, need_d_h=True, d_w=None, ws=None):
+def preference_loss_forward_backward(h, w, labels, batch, beta, ref_logp=None, label_smoothing=0.0, temperature=1.0, loss_scale=None, need_d_h=True, d_w=None, ws=None, fp32_dz=False):
     """Preference loss; sequences 2 i and 2 i + 1 of `batch` (Batch) are the chosen and the rejected answer of pair i.  Returns dict(loss, margin [pairs],
     logp, d_h); d_w (fp32, as w) is accumulated in place.  loss_scale: 1 / pairs by default."""
     pairs = batch.n_seqs // 2
-    c, n, d_h = _head(h, w, temperature, 1.0 / max(pairs, 1) if loss_scale is None else loss_scale, 0, need_d_h, d_w)
+    c, n, d_h = _head(h, w, temperature, 1.0 / max(pairs, 1) if loss_scale is None else loss_scale, 0, need_d_h, d_w, fp32_dz)
     dev = h.device
     if batch.n_tokens != n:
         raise ValueError(f"batch: expected sequences of {n} tokens, got {batch.n_tokens}")

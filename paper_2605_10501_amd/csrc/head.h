@@ -39,7 +39,7 @@ struct HeadPlan {
     int parts;                               // of d_h
     float *d_h;                              // [parts, rows, hidden]
     void *z;                                 // slabs: logits (fp32), or their exponentials (bf16)
-    void *dz;                                // [rows, cols] gradient of a slab's logits where it does not take the logits' place
+    void *dz, *dz_rest;                      // [rows, cols] gradient of a slab's logits where it does not take the logits' place, and what it lacks of fp32 (null: not taken along)
     float *per_token, *margin;               // [n] terms of the loss, or [pairs] both
     size_t bytes;
 };
@@ -50,6 +50,10 @@ enum HeadUse { HEAD_TOP = 0, HEAD_FORWARD = 1, HEAD_BACKWARD = 2 };
 // behind the L2s); marks take 8 ps for every strip and row, to clear, set and look at (32768 tokens, V = 151936, d = 1536, 64 entries: 0.85 and 0.7 ms; 32000 tokens, V = 32000,
 // d = 1024, 100 entries: 0.95 and 0.25).
 constexpr bool head_use_marks(long k, long d, long strips) { return k > 1 && k * d > 31 * strips; }
+
+// The storage type, and whether a bf16 head keeps the gradient of its logits in two bf16 numbers
+inline int head_dtype(const ms_head_config *c) { return c->dtype & ~MS_HEAD_FP32_DZ; }
+inline bool head_fp32_dz(const ms_head_config *c) { return (c->dtype & MS_HEAD_FP32_DZ) != 0; }
 
 // pairs >= 0: a preference loss of that many pairs, all n tokens in one block
 HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws);

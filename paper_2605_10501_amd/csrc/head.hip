@@ -652,22 +652,28 @@ __global__ __launch_bounds__(256) void head_row_kernel(Slabs sl, int n, int k, f
 
 // ------------------------------------------------------------------ gradients
 // Stored fp32 logits of a slab -> their gradient (in place for fp32), zeros in the columns cw .. cw_zero.  One workgroup per row.  A row without a token, or with scale 0, is zeros.
+// bf16: the gradient rounded once, or, with `rest`, as the sum of two bf16 numbers (2^-16 of it is lost), each with a pair of products of its own.  1031 tokens of 33 entries, V = 32000, d = 1024: error of
+// d_w 1.3e-3 from stored exponentials, 2.5e-6 so, 291 -> 589 us; 32768 tokens of 64 entries, V = 151936, d = 1536 37.8 -> 79.6 ms.
 template <class T>
 __global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int cw_zero, int v0, int k, const int *__restrict__ token, const int *__restrict__ sel, const float *z, float it2,
-                                                      const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho, T *dz) {
+                                                      const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho, T *dz, T *rest) {
     const int row = blockIdx.x, t = token[row];
     const float *zr = z + (long)row * d_cols;
-    T *o = dz + (long)row * d_cols;
+    T *o = dz + (long)row * d_cols, *more = rest ? rest + (long)row * d_cols : nullptr;
+    auto put = [&](int i, float v) __attribute__((always_inline)) {
+        o[i] = from_f32<T>(v);
+        if (more) more[i] = from_f32<T>(v - to_f32(from_f32<T>(v)));
+    };
     const float c = t < 0 ? 0.f : scale[row];                                   // (a row without a token has none)
-    for (int i = (c == 0.f ? 0 : cw) + threadIdx.x; i < cw_zero; i += 256) o[i] = from_f32<T>(0.f);
+    for (int i = (c == 0.f ? 0 : cw) + threadIdx.x; i < cw_zero; i += 256) put(i, 0.f);
     if (c == 0.f) return;
     const float2 st = stat[row];
     const float f = c / st.x;
-    for (int i = threadIdx.x; i < cw; i += 256) o[i] = from_f32<T>(f * __builtin_amdgcn_exp2f((zr[i] - st.y) * it2));
+    for (int i = threadIdx.x; i < cw; i += 256) put(i, f * __builtin_amdgcn_exp2f((zr[i] - st.y) * it2));
     __syncthreads();
     for (int j = threadIdx.x; j < k; j += 256) {
         const int v = sel[(long)t * k + j] - v0;
-        if (v >= 0 && v < cw) o[v] = from_f32<T>(c * rho[(long)row * k + j]);
+        if (v >= 0 && v < cw) put(v, c * rho[(long)row * k + j]);
     }
 }
 
@@ -677,7 +683,7 @@ __global__ __launch_bounds__(256) void head_dz_kernel(int d_cols, int cw, int cw
 // The exponentials are rounded to the storage type where they are stored, and c h here.  The selected ids with the largest gradients are most of the gradient's norm (a label's is the sum
 // of all others'), so what those two roundings take from them is put back: rest = dz - c (stored e), which d_h adds times its row of w, and dz h - (stored e) (stored c h),
 // a row that head_fix_kernel or the sorted sums of embedding_sorted.hip add to the id's row of d_w.  Error of d_w, rounded to bf16 by itself, against 64 bits: 2.9e-3 without, with
-// 1.8e-3; the rounding alone is 1.7e-3.  HBM: 32768 rows of 1536 with four rows to complete each, 0.6 GB, 140 us.
+// 1.8e-3; the rounding alone is 1.7e-3.  (A caller who wants less of it asks for fp32's precision instead: MS_HEAD_FP32_DZ, head_dz_kernel.)  HBM: 32768 rows of 1536 with four rows to complete each, 0.6 GB, 140 us.
 __global__ __launch_bounds__(256) void head_apply_kernel(Slabs sl, int d, int k, int strips, const float2 *__restrict__ part, const int *__restrict__ token, const int *__restrict__ count,
                                                          const int *__restrict__ sel, const float2 *__restrict__ stat, const float *__restrict__ scale, const float *__restrict__ rho,
                                                          bf16_t *__restrict__ e, bf16_t *__restrict__ h, float *__restrict__ factor, int fixes, int *__restrict__ fix_id,
@@ -1177,15 +1183,15 @@ HeadMarks marks_of(const HeadPlan &p, int v0, int k) {
 }
 ms_status logits(const ms_head_config *c, const HeadPlan &p, HeadUse use, int k, int rows, const void *h, hipStream_t s) {
     const int V = c->vocab, d = c->hidden;
-    const size_t es = ms_dtype_size(c->dtype);
+    const size_t es = ms_dtype_size(head_dtype(c));
     const float it2 = kLog2e / c->temperature;
     for (int i = 0; i < p.slabs; ++i) {
         const int v0 = i * p.cols, cw = V - v0 < p.cols ? V - v0 : p.cols;
         const char *w = (const char *)c->w_dev + (size_t)v0 * d * es;
         const size_t slab = (size_t)i * p.rows * p.cols;
         float2 *part = p.part + (size_t)(v0 / kStrip) * p.rows;
-        if (c->dtype == MS_F32 && head_f32_logits_tiled(rows, V)) MS_TRY(head_f32_logits(rows, cw, d, (const float *)h, (const float *)w, (float *)p.z + slab, p.cols, s));
-        else if (!p.fast) MS_TRY(ms_k_gemm(c->dtype, 0, 0, rows, cw, d, 1.f, h, d, w, d, (float *)p.z + slab, p.cols, 1, 0, nullptr, nullptr, 0, 0, 1, s));
+        if (head_dtype(c) == MS_F32 && head_f32_logits_tiled(rows, V)) MS_TRY(head_f32_logits(rows, cw, d, (const float *)h, (const float *)w, (float *)p.z + slab, p.cols, s));
+        else if (!p.fast) MS_TRY(ms_k_gemm(head_dtype(c), 0, 0, rows, cw, d, 1.f, h, d, w, d, (float *)p.z + slab, p.cols, 1, 0, nullptr, nullptr, 0, 0, 1, s));
         else if (use == HEAD_TOP) MS_TRY(head_gemm_logits(rows, cw, d, h, w, it2, (float *)p.z + slab, p.cols, part, p.rows, s));
         else MS_TRY(head_gemm_exp(rows, cw, d, h, w, p.ref, v0, p.z_label, marks_of(p, v0, k), it2, use == HEAD_BACKWARD ? (bf16_t *)p.z + slab : nullptr, p.cols, part, p.rows, p.count, s));
     }
@@ -1220,17 +1226,17 @@ ms_status rows_forward(const HeadCall &a, int t0, int n, const int *key, int lim
     const HeadPlan &p = a.p;
     const int d = c->hidden, V = c->vocab;
     const float it2 = kLog2e / c->temperature;
-    const char *h = (const char *)a.h + (size_t)t0 * d * ms_dtype_size(c->dtype);
+    const char *h = (const char *)a.h + (size_t)t0 * d * ms_dtype_size(head_dtype(c));
     const bool labels = after.what != AFTER_NOTHING;
     if (!p.fast) {
         MS_TRY(logits(c, p, a.use, a.k, n, h, a.s));
-        *dz_done = dz_here && c->dtype == MS_F32 && a.use == HEAD_BACKWARD;
+        *dz_done = dz_here && head_dtype(c) == MS_F32 && a.use == HEAD_BACKWARD;
         const Slabs sl = {p.rows, p.cols, V};
         float *scale = a.use == HEAD_BACKWARD ? p.scale : nullptr, *rho = a.use == HEAD_BACKWARD ? p.rho : nullptr;
         ProfScope ps(9, 4.0 * n * V * (*dz_done ? 2 : 1), a.s);
         const RowInputs in = {d, limit, labels ? sel : nullptr, h, c->w_dev, a.use == HEAD_BACKWARD ? p.h : nullptr, p.slot, p.token, out0, out1};
 #define GO(G, T, rows) head_row_kernel<G, T><<<rows, 256, 0, a.s>>>(sl, n, a.k, it2, in, teacher, sel, (float *)p.z, after, en, p.stat, scale, rho, *dz_done)
-        if (c->dtype == MS_F32) {
+        if (head_dtype(c) == MS_F32) {
             if (V <= 4096) GO(64, float, ms_cdiv(n, 4)); else GO(256, float, n);
         } else {
             if (V <= 4096) GO(64, bf16_t, ms_cdiv(n, 4)); else GO(256, bf16_t, n);
@@ -1278,7 +1284,7 @@ ms_status total_loss(const LossTerms &a, hipStream_t s) {
 ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool dz_done, const LossTerms &loss) {
     const ms_head_config *c = a.c;
     const HeadPlan &p = a.p;
-    const int d = c->hidden, V = c->vocab, dt = c->dtype;
+    const int d = c->hidden, V = c->vocab, dt = head_dtype(c);
     const size_t es = ms_dtype_size(dt);
     const float it2 = kLog2e / c->temperature;
     if (p.fast) {
@@ -1300,14 +1306,15 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool d
         void *dz = dt == MS_F32 ? (void *)z : p.dz;
         if (!dz_done) {
             ProfScope ps(10, (4.0 + es) * n * cw, a.s);
-            if (dt == MS_F32) head_dz_kernel<float><<<n, 256, 0, a.s>>>(p.cols, cw, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (float *)dz);
-            else head_dz_kernel<bf16_t><<<n, 256, 0, a.s>>>(p.cols, cw, p.tiles ? (cw + 63) / 64 * 64 : cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (bf16_t *)dz);
+            if (dt == MS_F32) head_dz_kernel<float><<<n, 256, 0, a.s>>>(p.cols, cw, cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (float *)dz, (float *)nullptr);
+            else head_dz_kernel<bf16_t><<<n, 256, 0, a.s>>>(p.cols, cw, p.tiles ? (cw + 63) / 64 * 64 : cw, v0, a.k, p.token, sel, z, it2, p.stat, p.scale, p.rho, (bf16_t *)dz, (bf16_t *)p.dz_rest);
         }
         MS_LAUNCH_CHECK();
         // (in fp32 the sums are the result: zeros for the tokens that are left out, whose rows of dz are)
         float *sums = dt == MS_F32 ? (float *)a.d_h + (size_t)t0 * d : p.d_h;
         if (p.tiles) {
             MS_TRY(head_gemm_backward(p.choice, n, cw, d, dz, p.cols, w, p.h, a.d_h ? p.d_h : nullptr, i > 0, d_w, nullptr, a.s));
+            if (p.dz_rest) MS_TRY(head_gemm_backward(p.choice, n, cw, d, p.dz_rest, p.cols, w, p.h, a.d_h ? p.d_h : nullptr, 1, d_w, nullptr, a.s));
             continue;
         }
         if (dt == MS_F32 && a.d_h && a.d_w) {
@@ -1315,8 +1322,11 @@ ms_status rows_backward(const HeadCall &a, int t0, int n, const int *sel, bool d
             continue;
         }
         // (K in one piece: bf16 pieces would be added up by atomics, in any order)
-        if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, dz, p.cols, w, d, sums, d, 1, i > 0, nullptr, nullptr, 0, 0, 1, a.s));
-        if (a.d_w) MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, dz, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 1, a.s));
+        for (const void *e : {(const void *)dz, (const void *)p.dz_rest}) {
+            if (!e) continue;
+            if (a.d_h) MS_TRY(ms_k_gemm(dt, 0, 1, n, d, cw, 1.f, e, p.cols, w, d, sums, d, 1, i > 0 || e != dz, nullptr, nullptr, 0, 0, 1, a.s));
+            if (a.d_w) MS_TRY(ms_k_gemm(dt, 1, 1, cw, d, n, 1.f, e, p.cols, p.h, d, d_w, d, 1, 1, nullptr, nullptr, 0, 0, 1, a.s));
+        }
     }
     if (dt == MS_F32) {
         if (!a.d_h) return loss.loss ? total_loss(loss, a.s) : MS_OK;
@@ -1356,7 +1366,7 @@ ms_status begin(HeadCall *a, const char *what, const ms_head_config *c, int n, i
     if (n && (!h || !ws)) return ms_fail(MS_ERR_INVALID_ARG, "%s: null pointer", what);
     if (!aligned(h, 16) || !aligned(c->w_dev, 16) || !aligned(d_h, 16) || !aligned(d_w, 16) || !aligned(ws, 16))
         return ms_fail(MS_ERR_UNSUPPORTED, "%s: hidden states, lm_head, their gradients and the workspace must be 16-byte aligned", what);
-    const size_t hb = (size_t)n * c->hidden * ms_dtype_size(c->dtype), wb = (size_t)c->vocab * c->hidden * ms_dtype_size(c->dtype);
+    const size_t hb = (size_t)n * c->hidden * ms_dtype_size(head_dtype(c)), wb = (size_t)c->vocab * c->hidden * ms_dtype_size(head_dtype(c));
     const Span states = {h, hb}, lm_head = {c->w_dev, wb}, d_states = {d_h, hb}, d_lm_head = span(d_w, (long)c->vocab * c->hidden);
     if ((d_h != h && !apart(d_states, states)) || !apart(d_states, lm_head) || !apart(d_states, d_lm_head) || !apart(d_lm_head, states) || !apart(d_lm_head, lm_head))
         return ms_fail(MS_ERR_INVALID_ARG, "%s: d_h may be h, else the gradients must not overlap the hidden states, the lm_head or each other", what);
@@ -1409,7 +1419,7 @@ extern "C" ms_status ms_top_logits(const ms_head_config *c, int32_t n, const voi
     for (int t0 = 0; t0 < n; t0 += p.block) {
         const int nb = n - t0 < p.block ? n - t0 : p.block;
         const Slabs sl = {p.rows, p.cols, c->vocab};
-        MS_TRY(logits(c, p, HEAD_TOP, k, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(c->dtype), a.s));
+        MS_TRY(logits(c, p, HEAD_TOP, k, nb, (const char *)h + (size_t)t0 * c->hidden * ms_dtype_size(head_dtype(c)), a.s));
         if (!p.fast && !whole) {
             head_strips_kernel<<<dim3(ms_cdiv(p.strips, 4), nb < 32768 ? nb : 32768), 256, 0, a.s>>>(sl, nb, p.strips, (const float *)p.z, it2, p.part);
             MS_LAUNCH_CHECK();

@@ -16,16 +16,16 @@ long round_up(long x, long a) { return (x + a - 1) / a * a; }
 
 // Bytes of a number of the widest matrix with rows of the hidden size that a product addresses by 32-bit offsets: gradients come out in fp32.  (fp32 products look at their
 // operands themselves and take 64-bit ones where they have to.)
-static long widest_number(const ms_head_config *c, HeadUse use) { return use == HEAD_BACKWARD && c->dtype == MS_BF16 ? 4 : 2; }
+static long widest_number(const ms_head_config *c, HeadUse use) { return use == HEAD_BACKWARD && head_dtype(c) == MS_BF16 ? 4 : 2; }
 long head_most_rows(const ms_head_config *c, HeadUse use) { return least(kReach / (widest_number(c, use) * c->hidden) - 512, kReach / (4 * 256) - 512); }
 
 HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws) {
     HeadPlan p = {};
     const bool whole = pairs >= 0;
     const long V = c->vocab, d = c->hidden;
-    const size_t es = ms_dtype_size(c->dtype);
-    const bool bf16_tiles = c->dtype == MS_BF16 && gemm_forced_tile() >= 0;
-    p.fast = bf16_tiles && d % 64 == 0;
+    const size_t es = ms_dtype_size(head_dtype(c));
+    const bool bf16_tiles = head_dtype(c) == MS_BF16 && gemm_forced_tile() >= 0;
+    p.fast = bf16_tiles && d % 64 == 0 && (use == HEAD_TOP || !head_fp32_dz(c));
     p.tiles = bf16_tiles && use == HEAD_BACKWARD;
     const bool keeps = use != HEAD_FORWARD || !p.fast;                       // something of every (row, vocabulary entry)
     const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
@@ -98,8 +98,12 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
             }
         }
         const long sums = (long)r * d, in_parts = least(kHeadMostParts * sums, kHeadPartsRoom);
-        if (c->dtype == MS_BF16) p.d_h = a.take<float>((p.tiles && in_parts > sums ? in_parts : sums) * 4);
-        if (!p.fast && c->dtype == MS_BF16) p.dz = a.take<void>(least((long)r * (V + 256), kReach / 4) * 2);
+        if (head_dtype(c) == MS_BF16) p.d_h = a.take<float>((p.tiles && in_parts > sums ? in_parts : sums) * 4);
+        if (!p.fast && head_dtype(c) == MS_BF16) {
+            const size_t most_dz = least((long)r * (V + 256), kReach / 4) * 2;
+            p.dz = a.take<void>(most_dz);
+            if (head_fp32_dz(c)) p.dz_rest = a.take<void>(most_dz);
+        }
     }
     if (keeps) p.z = a.take<void>(r * (V + 257 * slabs_of((long)r)) * ez);
     p.bytes = a.off;
@@ -109,7 +113,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
 ms_status validate_head(const ms_head_config *c, int n, int k, const char *what) {
     if (!c) return ms_fail(MS_ERR_INVALID_ARG, "%s: null config", what);
     if (n < 0) return ms_fail(MS_ERR_INVALID_ARG, "%s: negative token count", what);
-    if (c->dtype != MS_BF16 && c->dtype != MS_F32) return ms_fail(MS_ERR_INVALID_ARG, "%s: bad dtype", what);
+    if (head_dtype(c) != MS_BF16 && c->dtype != MS_F32) return ms_fail(MS_ERR_INVALID_ARG, "%s: bad dtype", what);
     if (c->vocab <= 0 || c->hidden <= 0) return ms_fail(MS_ERR_SHAPE, "%s: vocab and hidden size must be positive", what);
     if (c->vocab % 8 || c->hidden % 8) return ms_fail(MS_ERR_UNSUPPORTED, "%s: vocab and hidden size must be multiples of 8", what);
     if ((long)c->hidden > 65536 || c->vocab > (1 << 24)) return ms_fail(MS_ERR_UNSUPPORTED, "%s: hidden size over 65536 or vocab over 2^24", what);

@@ -17,12 +17,13 @@ int main() {
     const int tokens[] = {1, 64, 100, 4096, 15000, 33000, 65536, 131072, 262144, 265000, 300000, 530000, 3000000};
     const long reach = 1L << 32;
     long plans = 0;
+    for (int dtype : {(int)MS_BF16, MS_BF16 | MS_HEAD_FP32_DZ})
     for (auto [v, d] : heads)
         for (int b : {0, 4096, 300000, 1 << 24})
             for (HeadUse use : {HEAD_TOP, HEAD_FORWARD, HEAD_BACKWARD})
                 for (int whole = 0; whole < 2; ++whole) {
                     ms_head_config c = {};
-                    c.vocab = v; c.hidden = d; c.dtype = MS_BF16; c.token_block = b; c.temperature = 1.f; c.loss_scale = 1.f; c.w_dev = (const void *)4096;
+                    c.vocab = v; c.hidden = d; c.dtype = dtype; c.token_block = b; c.temperature = 1.f; c.loss_scale = 1.f; c.w_dev = (const void *)4096;
                     size_t before = 0;
                     for (int n : tokens) {
                         const int k = use == HEAD_TOP ? 8 : 0, pairs = whole ? n / 2 : -1;
@@ -32,12 +33,18 @@ int main() {
                         if (whole && bytes == 0) continue;                     // (more tokens than one block takes: refused)
                         const HeadPlan p = head_plan(&c, n, k, use, pairs, nullptr);
                         const long r = p.rows + 256L, w = p.cols + 256L;
-                        CHECK(validate_head(&c, n, k, "plan") == MS_OK && p.fast == (d % 64 == 0) && p.bytes == bytes && bytes >= before);
+                        CHECK(validate_head(&c, n, k, "plan") == MS_OK && p.fast == (d % 64 == 0 && (use == HEAD_TOP || dtype == MS_BF16)) && p.bytes == bytes && bytes >= before);
                         before = bytes;
                         CHECK(r * d * 2 < reach && w * d * 2 < reach);
                         if (use == HEAD_BACKWARD) CHECK(r * d * 4 < reach && w * d * 4 < reach);
                         if (use != HEAD_FORWARD || !p.fast) CHECK(r * p.cols * (use == HEAD_TOP || !p.fast ? 4 : 2) < reach);
                         if (p.fast && use != HEAD_TOP && b == 0 && !whole) CHECK(p.block <= 65536);       // (one workgroup finds its rows)
+                        if (p.dz_rest || (use == HEAD_BACKWARD && dtype != MS_BF16)) {
+                            char *const base = (char *)(1ul << 45);            // (never followed)
+                            const HeadPlan q = head_plan(&c, n, k, use, pairs, base);
+                            const long slab = (long)p.rows * p.cols;
+                            CHECK(q.dz && (char *)q.dz + slab * 2 <= (char *)q.dz_rest && (char *)q.dz_rest + slab * 2 <= (char *)q.z && (char *)q.z + slab * 4 * p.slabs <= base + bytes);
+                        }
                         ++plans;
                     }
                 }
