@@ -6,6 +6,7 @@
 namespace {
 constexpr long kReach = kHeadReach;
 constexpr long kBlockBytes = 16L << 30;                 // a block's exponentials or logits, if the caller does not say (288 GB per GPU)
+constexpr long kLaunchLogits = 1L << 34;                // logits of one launch: 2^22 of the smallest tiles, of the 2^23 workgroups of 512 threads that fit one
 constexpr long kTopBlockBytes = 4L << 30;               // the same for logits that are only looked through
 // Tokens of a block of the fast products, whose rows one workgroup finds (head_rows_kernel): 300000 tokens of V = 8192, d = 256 forward and backward in one block 10.36 ms, so 6.97; 2 million of V = 1024, d = 128
 // 20.3 and 17.8; 131072 of V = 32000, d = 1024 21.4 with both, in blocks of 32768 21.7
@@ -34,7 +35,8 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     if (!whole && c->token_block > 0) most = least(most, c->token_block);
     else if (!whole) {
         if (p.fast && use != HEAD_TOP) most = least(most, kBlockRows);
-        if (keeps) most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
+        if (!keeps) most = least(most, round_up(kBlockBytes / (8 * ((V + kStrip - 1) / kStrip)) + 1, 256));
+        else most = least(most, round_up((use == HEAD_TOP ? kTopBlockBytes : kBlockBytes) / (long)(ez * V) + 1, 256));
     }
     const long blocks = whole || n <= most ? 1 : (n + most - 1) / most;
     p.block = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
@@ -42,6 +44,7 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     auto slabs_of = [&](long rows) {
         long widest = kReach / (widest_number(c, use) * d) - 512;
         if (keeps) widest = least(widest, kReach / (long)(ez * (rows + 256L)));
+        else widest = least(widest, kLaunchLogits / (rows + 256L));
         widest = widest / 256 * 256;
         return (V + widest - 1) / widest;
     };

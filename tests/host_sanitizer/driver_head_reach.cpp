@@ -13,7 +13,7 @@ extern "C" size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_
 
 int main() {
     const struct { int vocab, hidden; } heads[] = {{152064, 8192}, {151936, 7040}, {151936, 7104}, {262144, 5376}, {262208, 5376}, {262144, 4096}, {262136, 4096}, {128256, 16384}, {256000, 12288},
-                                                   {1 << 24, 64}, {1 << 24, 65536}, {32768, 32768}, {16384, 65536}, {1024, 4096}, {32000, 4096}, {8, 65536}, {151936, 1536}, {151936, 7112}, {1024, 4104}};
+                                                   {1 << 24, 64}, {1 << 21, 128}, {1 << 24, 65536}, {32768, 32768}, {16384, 65536}, {1024, 4096}, {32000, 4096}, {8, 65536}, {151936, 1536}, {151936, 7112}, {1024, 4104}};
     const int tokens[] = {1, 64, 100, 4096, 15000, 33000, 65536, 131072, 262144, 265000, 300000, 530000, 3000000};
     const long reach = 1L << 32;
     long plans = 0;
@@ -38,6 +38,9 @@ int main() {
                         CHECK(r * d * 2 < reach && w * d * 2 < reach);
                         if (use == HEAD_BACKWARD) CHECK(r * d * 4 < reach && w * d * 4 < reach);
                         if (use != HEAD_FORWARD || !p.fast) CHECK(r * p.cols * (use == HEAD_TOP || !p.fast ? 4 : 2) < reach);
+                        // a forward pass keeps nothing of the logits: what bounds it is the largest launch, and its strips' sums
+                        if (p.fast && use == HEAD_FORWARD) CHECK(ms_launch_fits((long)ms_cdiv(p.rows, 64) * ms_cdiv(v < p.cols ? v : p.cols, 64), 512));
+                        if (p.fast && use == HEAD_FORWARD && b == 0 && !whole) CHECK(p.bytes < 40ul << 30);
                         if (p.fast && use != HEAD_TOP && b == 0 && !whole) CHECK(p.block <= 65536);       // (one workgroup finds its rows)
                         if (p.dz_rest || (use == HEAD_BACKWARD && dtype != MS_BF16)) {
                             char *const base = (char *)(1ul << 45);            // (never followed)
