@@ -319,7 +319,7 @@ __device__ __forceinline__ void gemm_epilogue(const GemmParams &p, ACC (&acc)[MI
         }
         wave_sync();     // every lane's values are in LDS before any lane reads
     };
-    // ---- epilogue.  C and the residual are addressed through buffer descriptors: rows past M are
+    // ---- epilogue (EPI_EXP, which has other things in p.residual, p.bias and p.ldr, comes back before anything of rr is read).  C and the residual are addressed through buffer descriptors: rows past M are
     // dropped (stores) or read as zero by the range check, columns past N by one select.
     // Byte offset of row r of the wave's block i: the lane's part (its row within the pass and its column) once, the rest, which is
     // the same in all lanes, on the scalar unit.  A product per row and lane on the vector ALU is a quarter-rate instruction; with the
