@@ -15,23 +15,25 @@ long least(long a, long b) { return a < b ? a : b; }
 long round_up(long x, long a) { return (x + a - 1) / a * a; }
 }  // namespace
 
-// Bytes of a number of the widest matrix with rows of the hidden size that a product addresses by 32-bit offsets: gradients come out in fp32.  (fp32 products look at their
-// operands themselves and take 64-bit ones where they have to.)
-static long widest_number(const ms_head_config *c, HeadUse use) { return use == HEAD_BACKWARD && head_dtype(c) == MS_BF16 ? 4 : 2; }
-long head_most_rows(const ms_head_config *c, HeadUse use) { return least(kReach / (widest_number(c, use) * c->hidden) - 512, kReach / (4 * 256) - 512); }
+static bool bf16_tiles(const ms_head_config *c) { return head_dtype(c) == MS_BF16 && gemm_forced_tile() >= 0; }
+static bool fast_products(const ms_head_config *c, HeadUse use) { return bf16_tiles(c) && c->hidden % 64 == 0 && (use == HEAD_TOP || !head_fp32_dz(c)); }
+// Rows of the hidden size, of numbers of so many bytes, that the products of head_gemm.hip reach; their gradients come out in fp32.  (The products of the other path look at their operands themselves
+// and take 64-bit offsets where they have to.)
+static long reached_rows(const ms_head_config *c, int bytes) { return kReach / (bytes * (long)c->hidden) - 512; }
+long head_most_rows(const ms_head_config *c, HeadUse use) { return least(reached_rows(c, use == HEAD_BACKWARD && fast_products(c, use) ? 4 : 2), kReach / (4 * 256) - 512); }
 
 HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs, void *ws) {
     HeadPlan p = {};
     const bool whole = pairs >= 0;
     const long V = c->vocab, d = c->hidden;
     const size_t es = ms_dtype_size(head_dtype(c));
-    const bool bf16_tiles = head_dtype(c) == MS_BF16 && gemm_forced_tile() >= 0;
-    p.fast = bf16_tiles && d % 64 == 0 && (use == HEAD_TOP || !head_fp32_dz(c));
-    p.tiles = bf16_tiles && use == HEAD_BACKWARD;
+    const bool gradients = use == HEAD_BACKWARD && head_dtype(c) == MS_BF16;
+    p.fast = fast_products(c, use);
     const bool keeps = use != HEAD_FORWARD || !p.fast;                       // something of every (row, vocabulary entry)
     const size_t ez = p.fast && use != HEAD_TOP ? 2 : 4;
     // tokens of a block: the caller's choice, or what the memory above holds, in blocks of about equal size
     long most = head_most_rows(c, use);
+    if (gradients && !whole) most = least(most, reached_rows(c, 4));
     if (!whole && c->token_block > 0) most = least(most, c->token_block);
     else if (!whole) {
         if (p.fast && use != HEAD_TOP) most = least(most, kBlockRows);
@@ -41,8 +43,9 @@ HeadPlan head_plan(const ms_head_config *c, int n, int k, HeadUse use, int pairs
     const long blocks = whole || n <= most ? 1 : (n + most - 1) / most;
     p.block = (int)(blocks == 1 ? n : least(most, round_up((n + blocks - 1) / blocks, 8)));
     p.rows = (int)round_up(p.block, 16);                                       // (a strip's words and bytes start at 16 bytes)
+    p.tiles = gradients && bf16_tiles(c) && p.block <= reached_rows(c, 4);
     auto slabs_of = [&](long rows) {
-        long widest = kReach / (widest_number(c, use) * d) - 512;
+        long widest = reached_rows(c, gradients ? 4 : 2);
         if (keeps) widest = least(widest, kReach / (long)(ez * (rows + 256L)));
         else widest = least(widest, kLaunchLogits / (rows + 256L));
         widest = widest / 256 * 256;

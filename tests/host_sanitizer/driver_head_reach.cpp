@@ -3,6 +3,9 @@
 // have to lie below 4 GB, at sizes on both sides of it; and memory for more tokens serves fewer there too.
 #include <stdio.h>
 
+#include <algorithm>
+#include <vector>
+
 #include "head.h"
 
 static int failures;
@@ -13,7 +16,7 @@ extern "C" size_t ms_k_embedding_sorted_backward_scratch_bytes(int32_t n, int32_
 
 int main() {
     const struct { int vocab, hidden; } heads[] = {{152064, 8192}, {151936, 7040}, {151936, 7104}, {262144, 5376}, {262208, 5376}, {262144, 4096}, {262136, 4096}, {128256, 16384}, {256000, 12288},
-                                                   {1 << 24, 64}, {1 << 21, 128}, {1 << 24, 65536}, {32768, 32768}, {16384, 65536}, {1024, 4096}, {32000, 4096}, {8, 65536}, {151936, 1536}, {151936, 7112}, {1024, 4104}};
+                                                   {1 << 24, 64}, {1 << 21, 128}, {1 << 24, 65536}, {32768, 32768}, {16384, 65536}, {1024, 4096}, {32000, 4096}, {8, 65536}, {151936, 1536}, {151936, 7112}, {1024, 4104}, {1024, 65528}};
     const int tokens[] = {1, 64, 100, 4096, 15000, 33000, 65536, 131072, 262144, 265000, 300000, 530000, 3000000};
     const long reach = 1L << 32;
     long plans = 0;
@@ -25,7 +28,12 @@ int main() {
                     ms_head_config c = {};
                     c.vocab = v; c.hidden = d; c.dtype = dtype; c.token_block = b; c.temperature = 1.f; c.loss_scale = 1.f; c.w_dev = (const void *)4096;
                     size_t before = 0;
-                    for (int n : tokens) {
+                    std::vector<long> counts(std::begin(tokens), std::end(tokens));
+                    for (long bytes : {2, 4})                                   // the longest blocks there are, and a token more and less
+                        for (long more : {-1, 0, 1}) counts.push_back(std::min(((1L << 32) - (1L << 20)) / (bytes * d) - 512 + more, 1L << 24));
+                    std::sort(counts.begin(), counts.end());
+                    for (long count : counts) {
+                        const int n = (int)count;
                         const int k = use == HEAD_TOP ? 8 : 0, pairs = whole ? n / 2 : -1;
                         if (whole && use == HEAD_TOP) continue;
                         const size_t bytes = use == HEAD_TOP ? ms_top_logits_workspace_bytes(&c, n, k) : whole ? ms_preference_workspace_bytes(&c, n, pairs, use == HEAD_BACKWARD)
@@ -36,7 +44,8 @@ int main() {
                         CHECK(validate_head(&c, n, k, "plan") == MS_OK && p.fast == (d % 64 == 0 && (use == HEAD_TOP || dtype == MS_BF16)) && p.bytes == bytes && bytes >= before);
                         before = bytes;
                         CHECK(r * d * 2 < reach && w * d * 2 < reach);
-                        if (use == HEAD_BACKWARD) CHECK(r * d * 4 < reach && w * d * 4 < reach);
+                        if (use == HEAD_BACKWARD && p.tiles) CHECK(r * d * 4 < reach && w * d * 4 < reach);
+                        if (use == HEAD_BACKWARD) CHECK(p.tiles || (whole && !p.fast));       // (one block that is too long for them has products that take 64-bit offsets)
                         if (use != HEAD_FORWARD || !p.fast) CHECK(r * p.cols * (use == HEAD_TOP || !p.fast ? 4 : 2) < reach);
                         // a forward pass keeps nothing of the logits: what bounds it is the largest launch, and its strips' sums
                         if (p.fast && use == HEAD_FORWARD) CHECK(ms_launch_fits((long)ms_cdiv(p.rows, 64) * ms_cdiv(v < p.cols ? v : p.cols, 64), 512));
