@@ -105,3 +105,28 @@ def test_preference_loss_over_several_slabs(dtype, n, d, vocab):
     _near(out["d_h"], d_h, _tol(dtype) + beta * n * delta)
     _near(got_w, d_w, _tol(dtype) + beta * n * delta)
     assert torch.all(out["d_h"][~ok] == 0)
+
+
+def test_forward_passes_over_several_slabs():
+    """More logits than one launch takes (2^34): a token's numbers are those of blocks with one slab, logits of entries by marks among them."""
+    n, d, vocab, k = 65536, 1024, 262144 + 8, 128
+    h, w, labels, _ = _scaled(torch.bfloat16, n, d, vocab)
+    cut = (-(-vocab // 2) + 255) // 256 * 256                                             # two slabs
+    labels[5:9] = torch.tensor([cut - 1, cut, cut + 1, vocab - 1], dtype=torch.int32, device="cuda")
+    logp = B.token_logprobs(h, w, labels)
+    assert torch.equal(logp, B.token_logprobs(h, w, labels, token_block=4096))
+    a = torch.arange(1024, device="cuda")
+    lq = torch.log_softmax(h[a].double() @ w.double().T, 1)
+    ref = torch.where(labels[a] >= 0, lq.gather(1, labels[a].long().clamp(min=0)[:, None])[:, 0], 0.0)
+    delta = 2.0 ** -24 * (2 * d * 20 + 4 * 20 + 256)
+    assert ((logp[a].double() - ref).abs() <= delta).all()
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    step = vocab // k
+    ids = (torch.arange(k, device="cuda") * step + torch.randint(0, step, (n, k), generator=gen, device="cuda")).int()
+    ids[0::3, min(cut // step, k - 1)], ids[1::3, (cut - 1) // step], ids[2::3, k - 1] = cut, cut - 1, vocab - 1
+    top = torch.empty(n, k, device="cuda").normal_(0, 2, generator=gen)
+    one, many = (B.topk_kd_loss_forward_backward(h, w, ids, top, need_d_h=False, token_block=b) for b in (0, 4096))
+    assert torch.equal(one["kl_tok"], many["kl_tok"])
+    lp = torch.log_softmax(top[a].double(), 1)
+    kl = (lp.exp() * (lp - lq.gather(1, ids[a].long()))).sum(1)
+    assert ((one["kl_tok"][a].double() - kl).abs() <= delta + 2.0 ** -24 * (64 + 8 * kl.abs())).all()
